@@ -294,6 +294,81 @@ int rsvd_stage_lift(rsvd_ctx *ctx, void *stream, rsvd_dtype dtype,
                     void *U, int64_t ldu, int transpose_out,
                     void *workspace, size_t workspace_bytes);
 
+/* ---- a linear layer out of a decomposition, held in 8 bits ----
+ *
+ * A weight W (m x n, W = U Vt + rest) is held as its low-rank factors in bf16
+ * and the rest as 8-bit codes with one scale for each row:
+ *     W_ij  ~  scale_i codes_ij + sum_p U_ip Vt_pj .
+ * Tokens are the rows of X (tokens x n), in bf16, fp16 or fp32 (rsvd_xtype);
+ * results have the type of the tokens.  Sums are held in 32 bits.
+ *   - tokens, n, m are at least 1 (tokens may be 0: nothing is launched, apart
+ *     from the zeros of rsvd_keep8_grad); r may be 0, the factors then NULL.
+ *     r at most 1024; n and m at most RSVD_Q8_MAX_FEATURES, beyond which sums of
+ *     8-bit products leave 32 bits (RSVD_ERR_UNSUPPORTED).
+ *   - X, Y, dX, dY, the factors and the bias may have any leading dimension and
+ *     the alignment of their elements; 16-byte aligned rows are faster.
+ *   - 8-bit codes have rows of ldq bytes, ldq a multiple of 16 and at least n,
+ *     from a 16-byte aligned address; every row has all of its ldq bytes (those
+ *     beyond n may be read, what they hold does not matter).
+ *   - Infinities and NaN: a row (of X, or of a weight) that holds one has
+ *     the scale NaN and codes 0, and makes its row (column) of Y NaN.  No
+ *     other row is touched.
+ */
+typedef enum { RSVD_X_BF16 = 0, RSVD_X_F16 = 1, RSVD_X_F32 = 2 } rsvd_xtype;
+#define RSVD_Q8_MAX_FEATURES 131072
+
+/* Rows to 8 bits with a scale each: a = max_j |x_j|; scale = a / 127 and
+ * codes_j = x_j (127 / a) rounded to the nearest integer, ties to even, where
+ * the two quotients and the product are single fp32 operations.  a < 2^-116:
+ * scale 0 and codes 0.  The bytes of a row from n to the next multiple of 16
+ * are set to 0.  (Lays out the weight; rsvd_q8_product does the same to X.) */
+int rsvd_q8_rows(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t rows, int64_t n,
+                 const void *X, int64_t ldx, int8_t *codes, int64_t ldq, float *scale);
+
+/* Bytes of device workspace for rsvd_q8_product, rsvd_q8_product_grad and
+ * rsvd_keep8_grad with these sizes (r = 0 for the last). */
+int rsvd_q8_product_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int64_t r, size_t *bytes);
+int rsvd_q8_product_grad_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int64_t r, size_t *bytes);
+int rsvd_keep8_grad_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, size_t *bytes);
+
+/* Y (tokens x m) = X W^T + bias: the rows of X go to 8 bits (rsvd_q8_rows),
+ * the 8-bit products are summed as integers; the low-rank term takes X itself.
+ *   U m x r (ldu >= r), Vt r x n (ldvt >= n), bf16; bias m fp32 values or NULL */
+int rsvd_q8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int64_t r,
+                    const void *X, int64_t ldx, const int8_t *codes, int64_t ldq, const float *scale,
+                    const void *U, int64_t ldu, const void *Vt, int64_t ldvt, const float *bias,
+                    void *Y, int64_t ldy, void *workspace, size_t workspace_bytes);
+
+/* dX (tokens x n) = dY W, the gradient of rsvd_q8_product with respect to X
+ * (the rounding of X to its codes is passed straight through).  The factors
+ * are given by rows of the other index: Ut r x m (ldut >= m), V n x r (ldv >= r).
+ * For bf16 tokens scale_i codes_ij is rounded to bf16 once; for fp16 and
+ * fp32 dY_ti scale_i is split into two and three bf16 numbers. */
+int rsvd_q8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int64_t r,
+                         const void *dY, int64_t lddy, const int8_t *codes, int64_t ldq, const float *scale,
+                         const void *Ut, int64_t ldut, const void *V, int64_t ldv,
+                         void *dX, int64_t lddx, void *workspace, size_t workspace_bytes);
+
+/* Activations kept in 8 bits for the backward pass.  The 32 features from 32 b
+ * on of a token share a power of two: with a = max |x| = f 2^E, 1/2 <= f < 1,
+ * it is 2^e, e = max(E - 7, -126); codes are x 2^-e rounded to the nearest
+ * integer, ties to even, cut at +-127; powers[b] = e + 127.  A block that
+ * holds an infinity or NaN has powers[b] = 255 and codes 0 and reads back as
+ * NaN.  codes: tokens x n, rows of ldc bytes as above; powers: tokens x
+ * ceil(n / 32) bytes, rows of ldp bytes, any alignment. */
+int rsvd_keep8_save(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n,
+                    const void *X, int64_t ldx, int8_t *codes, int64_t ldc, uint8_t *powers, int64_t ldp);
+int rsvd_keep8_load(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n,
+                    const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp, void *X, int64_t ldx);
+
+/* dW (m x n, fp32) = dY^T X^ and db (m, fp32, may be NULL) = column sums of dY,
+ * X^ the kept activations; accumulate != 0 adds to dW and db instead.  `type`
+ * is that of dY (tokens x m).  X^ is a bf16 number and dY a sum of one
+ * (bf16), two (fp16) or three (fp32) of them, so every product is exact. */
+int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m,
+                    const void *dY, int64_t lddy, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp,
+                    float *dW, int64_t lddw, float *db, int accumulate, void *workspace, size_t workspace_bytes);
+
 #ifdef __cplusplus
 }
 #endif

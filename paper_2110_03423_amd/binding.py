@@ -58,7 +58,19 @@ PROTOTYPES = {
                              C.POINTER(_Info)],
     "rsvd_stage_jacobi": [_VP, _VP, _INT, _I64, _VP, _VP, _VP, _VP, _VP, _SZ, C.POINTER(_Info)],
     "rsvd_stage_lift": [_VP, _VP, _INT, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _INT, _VP, _SZ],
+    "rsvd_q8_rows": [_VP, _VP, _INT, _I64, _I64, _VP, _I64, _VP, _I64, _VP],
+    "rsvd_q8_product_bytes": [_VP, _INT, _I64, _I64, _I64, _I64, C.POINTER(_SZ)],
+    "rsvd_q8_product_grad_bytes": [_VP, _INT, _I64, _I64, _I64, _I64, C.POINTER(_SZ)],
+    "rsvd_keep8_grad_bytes": [_VP, _INT, _I64, _I64, _I64, C.POINTER(_SZ)],
+    "rsvd_q8_product": [_VP, _VP, _INT, _I64, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I64, _VP, _I64, _VP, _VP,
+                        _I64, _VP, _SZ],
+    "rsvd_q8_product_grad": [_VP, _VP, _INT, _I64, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _VP, _I64, _VP, _I64, _VP,
+                             _I64, _VP, _SZ],
+    "rsvd_keep8_save": [_VP, _VP, _INT, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64],
+    "rsvd_keep8_load": [_VP, _VP, _INT, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64],
+    "rsvd_keep8_grad": [_VP, _VP, _INT, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _INT, _VP, _SZ],
 }
+X_BF16, X_F16, X_F32 = 0, 1, 2
 
 
 def load_library():
@@ -92,6 +104,88 @@ def _dtype_code(t):
     if t.dtype == torch.float64:
         return F64
     raise TypeError("fp32 or fp64 tensors only")
+
+
+def _xtype_code(dtype):
+    import torch
+    codes = {torch.bfloat16: X_BF16, torch.float16: X_F16, torch.float32: X_F32}
+    if dtype not in codes:
+        raise TypeError("bf16, fp16 or fp32 tokens only")
+    return codes[dtype]
+
+
+def _empty_codes(rows, n, device):
+    """Room for `rows` rows of 8-bit codes, each a multiple of 128 bytes long; the view has n columns."""
+    import torch
+    return torch.empty((rows, -(-n // 128) * 128), dtype=torch.int8, device=device)[:, :n]
+
+
+def _laid_out(codes):
+    """The codes in rows as the C entry points want them (a copy unless they are already)."""
+    if codes.dim() == 2 and codes.stride(1) == 1 and codes.stride(0) % 128 == 0 and codes.data_ptr() % 16 == 0:
+        return codes
+    out = _empty_codes(codes.shape[0], codes.shape[1], codes.device)
+    out.copy_(codes)
+    return out
+
+
+def _rows(t, cols, what, rows=None, dtype=None):
+    """A matrix with `cols` columns (and `rows` rows of `dtype`) whose rows are contiguous, on the GPU."""
+    if not t.is_cuda or t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1) or t.stride(0) < 0:
+        raise ValueError(f"{what}: a row-major GPU matrix with {cols} columns is needed")
+    if (rows is not None and t.shape[0] != rows) or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{what}: {rows} rows of {dtype} are needed")
+    return t
+
+
+def _ld(t):
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+
+
+class Weight8:
+    """A linear layer's weight (m x n) as rsvd_q8_product takes it: 8-bit codes with a scale for each row, and beside them
+    bf16 factors U (m x r), Vt (r x n) or None; bias: m values or None.  The codes are laid out, and the factors
+    transposed for the backward pass, once, here."""
+
+    def __init__(self, codes, scale, U=None, Vt=None, bias=None):
+        import torch
+        if codes.dtype != torch.int8 or codes.dim() != 2:
+            raise TypeError("codes: an int8 matrix")
+        m, n = codes.shape
+        if scale.dtype != torch.float32 or scale.shape != (m,):
+            raise ValueError("scale: one fp32 value for each row of codes")
+        if (U is None) != (Vt is None):
+            raise ValueError("U and Vt come together")
+        self.codes, self.scale = _laid_out(codes), scale.contiguous()
+        self.m, self.n, self.r = m, n, 0
+        self.U = self.Vt = self.Ut = self.V = None
+        if U is not None and U.shape[1] > 0:
+            if U.dtype != torch.bfloat16 or Vt.dtype != torch.bfloat16:
+                raise TypeError("U, Vt: bf16 factors")
+            if U.shape[0] != m or Vt.shape != (U.shape[1], n):
+                raise ValueError("U, Vt: m x r and r x n")
+            self.r = U.shape[1]
+            self.U, self.Vt = U.contiguous(), Vt.contiguous()
+            self.Ut, self.V = U.t().contiguous(), Vt.t().contiguous()
+        if bias is not None and bias.shape != (m,):
+            raise ValueError("bias: m values")
+        self.bias = None if bias is None else bias.float().contiguous()
+
+
+class Kept8:
+    """Activations (tokens x n) kept in 8 bits: codes, and a byte of power for each 32 of them (rsvd_keep8_save).  `dtype` is
+    the type of the activations."""
+
+    def __init__(self, codes, powers, dtype):
+        import torch
+        if codes.dtype != torch.int8 or codes.dim() != 2 or powers.dtype != torch.uint8:
+            raise TypeError("codes: an int8 matrix; powers: uint8")
+        if powers.shape != (codes.shape[0], -(-codes.shape[1] // 32)):
+            raise ValueError("powers: one byte for each 32 columns of codes")
+        _xtype_code(dtype)
+        self.codes, self.dtype = _laid_out(codes), dtype
+        self.powers = powers if powers.stride(1) == 1 or powers.shape[1] == 1 else powers.contiguous()
+        self.tokens, self.n = codes.shape
 
 
 def _ptr(t):
@@ -334,3 +428,85 @@ class Rsvd:
                                              _ptr(W), W.stride(0), _ptr(U), U.stride(0), int(transpose_out),
                                              None, 0))
         return U
+
+    # ---- a linear layer held in 8 bits
+    def rsvd_q8_rows(self, X):
+        """Rows of X (bf16, fp16, fp32) to 8 bits.  Returns (codes int8, scale fp32), the codes laid out for Weight8."""
+        _rows(X, X.shape[1], "X")
+        rows, n = X.shape
+        codes = _empty_codes(rows, n, X.device)
+        scale = self.torch.empty(rows, dtype=self.torch.float32, device=X.device)
+        self._check(self.lib.rsvd_q8_rows(self.h, self._stream(), _xtype_code(X.dtype), rows, n, _ptr(X), _ld(X), _ptr(codes),
+                                          _ld(codes), _ptr(scale)))
+        return codes, scale
+
+    def _layer_ws(self, fn, *sizes):
+        need = C.c_size_t()
+        self._check(fn(self.h, *sizes, C.byref(need)))
+        return self._grow(need.value)
+
+    def rsvd_q8_product(self, X, weight, workspace=None, out=None):
+        """X (tokens x n) through the layer `weight` (Weight8): tokens x m, in the type of X."""
+        w = weight
+        _rows(X, w.n, "X")
+        xt, tokens = _xtype_code(X.dtype), X.shape[0]
+        ws = workspace if workspace is not None else self._layer_ws(self.lib.rsvd_q8_product_bytes, xt, tokens, w.n, w.m, w.r)
+        Y = _rows(out, w.m, "out", tokens, X.dtype) if out is not None else self._empty((tokens, w.m), X)
+        self._check(self.lib.rsvd_q8_product(
+            self.h, self._stream(), xt, tokens, w.n, w.m, w.r, _ptr(X), _ld(X), _ptr(w.codes), _ld(w.codes), _ptr(w.scale),
+            _ptr(w.U), w.r, _ptr(w.Vt), w.n, _ptr(w.bias), _ptr(Y), _ld(Y), _ptr(ws), ws.numel()))
+        return Y
+
+    def rsvd_q8_product_grad(self, dY, weight, workspace=None, out=None):
+        """Gradient of rsvd_q8_product with respect to X: dY (tokens x m) to tokens x n, in the type of dY."""
+        w = weight
+        _rows(dY, w.m, "dY")
+        xt, tokens = _xtype_code(dY.dtype), dY.shape[0]
+        ws = workspace if workspace is not None else self._layer_ws(self.lib.rsvd_q8_product_grad_bytes, xt, tokens, w.n, w.m, w.r)
+        dX = _rows(out, w.n, "out", tokens, dY.dtype) if out is not None else self._empty((tokens, w.n), dY)
+        self._check(self.lib.rsvd_q8_product_grad(
+            self.h, self._stream(), xt, tokens, w.n, w.m, w.r, _ptr(dY), _ld(dY), _ptr(w.codes), _ld(w.codes), _ptr(w.scale),
+            _ptr(w.Ut), w.m, _ptr(w.V), w.r, _ptr(dX), _ld(dX), _ptr(ws), ws.numel()))
+        return dX
+
+    def rsvd_keep8_save(self, X):
+        """X (tokens x n) kept in 8 bits for the backward pass (Kept8)."""
+        _rows(X, X.shape[1], "X")
+        tokens, n = X.shape
+        codes = _empty_codes(tokens, n, X.device)
+        powers = self.torch.empty((tokens, -(-n // 32)), dtype=self.torch.uint8, device=X.device)
+        self._check(self.lib.rsvd_keep8_save(self.h, self._stream(), _xtype_code(X.dtype), tokens, n, _ptr(X), _ld(X),
+                                             _ptr(codes), _ld(codes), _ptr(powers), _ld(powers)))
+        return Kept8(codes, powers, X.dtype)
+
+    def rsvd_keep8_load(self, kept, out=None):
+        """The kept activations, in their type."""
+        X = out if out is not None else self.torch.empty((kept.tokens, kept.n), dtype=kept.dtype, device=kept.codes.device)
+        _rows(X, kept.n, "out", kept.tokens, kept.dtype)
+        self._check(self.lib.rsvd_keep8_load(self.h, self._stream(), _xtype_code(X.dtype), kept.tokens, kept.n,
+                                             _ptr(kept.codes), _ld(kept.codes), _ptr(kept.powers), _ld(kept.powers), _ptr(X), _ld(X)))
+        return X
+
+    def rsvd_keep8_grad(self, dY, kept, out=None, accumulate=False, workspace=None):
+        """Gradients of a weight and a bias from dY (tokens x m) and the kept activations: (dW (m x n), db (m)), fp32.
+        `out` = (dW, db) of the caller, db may be None; accumulate: they are added to."""
+        if dY.shape[0] != kept.tokens:
+            raise ValueError("dY: one row for each kept token")
+        _rows(dY, dY.shape[1], "dY")
+        if accumulate and out is None:
+            raise ValueError("accumulate: into which gradients?")
+        xt, m = _xtype_code(dY.dtype), dY.shape[1]
+        t = self.torch
+        if out is None:
+            dW = t.empty((m, kept.n), dtype=t.float32, device=dY.device)
+            db = t.empty(m, dtype=t.float32, device=dY.device)
+        else:
+            dW, db = out
+            _rows(dW, kept.n, "dW")
+            if dW.dtype != t.float32 or dW.shape[0] != m or (db is not None and (db.dtype != t.float32 or db.shape != (m,) or not db.is_contiguous())):
+                raise ValueError("out: fp32 gradients, m x n and m")
+        ws = workspace if workspace is not None else self._layer_ws(self.lib.rsvd_keep8_grad_bytes, xt, kept.tokens, kept.n, m)
+        self._check(self.lib.rsvd_keep8_grad(
+            self.h, self._stream(), xt, kept.tokens, kept.n, m, _ptr(dY), _ld(dY), _ptr(kept.codes), _ld(kept.codes),
+            _ptr(kept.powers), _ld(kept.powers), _ptr(dW), _ld(dW), _ptr(db), int(accumulate), _ptr(ws), ws.numel()))
+        return dW, db

@@ -129,6 +129,7 @@ hipError_t gemm_launch(rsvd_ctx *ctx, hipStream_t s, GemmKind kind, const GemmDe
 // Without them the product gives the same result, bit for bit, in more time.
 size_t gemm_packed_bytes(int64_t M, int64_t N, int64_t K);
 hipError_t gemm_split_init_device(rsvd_ctx *ctx);
+hipError_t layer8_init_device(rsvd_ctx *ctx);
 
 // ---------------------------------------------------------------- sketch
 // batch > 1: problem b (blockIdx.y) writes to out + b * stride_out bytes with seed + b.  zero: n_zero ints are cleared on the way.

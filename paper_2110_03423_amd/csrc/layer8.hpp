@@ -1,0 +1,170 @@
+// Shared declarations of the layer operators: products with 8-bit weights and low-rank factors, activations kept in 8 bits.
+#pragma once
+
+#include "common.hpp"
+
+namespace rsvd {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+#define RSVD_INLINE __attribute__((always_inline))
+
+inline int64_t xtype_size(rsvd_xtype t) { return t == RSVD_X_F32 ? 4 : 2; }
+// bf16 numbers whose sum is exactly a number of the type.
+inline int xtype_parts(rsvd_xtype t) { return t == RSVD_X_BF16 ? 1 : t == RSVD_X_F16 ? 2 : 3; }
+// Rows that may be read and written in 16-byte pieces.
+inline bool rows_aligned(const void *p, int64_t ld, int64_t size) { return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0; }
+
+#ifdef __HIPCC__
+template <int XT> struct XTraits;
+template <> struct XTraits<RSVD_X_BF16> { static constexpr int SIZE = 2, PARTS = 1; };
+template <> struct XTraits<RSVD_X_F16> { static constexpr int SIZE = 2, PARTS = 2; };
+template <> struct XTraits<RSVD_X_F32> { static constexpr int SIZE = 4, PARTS = 3; };
+
+// Element i behind p, as fp32.
+template <int XT> __device__ __forceinline__ float x_value(const char *p, int64_t i) {
+  if constexpr (XT == RSVD_X_F32) return reinterpret_cast<const float *>(p)[i];
+  else if constexpr (XT == RSVD_X_F16) return (float)reinterpret_cast<const _Float16 *>(p)[i];
+  else return __uint_as_float((unsigned)reinterpret_cast<const uint16_t *>(p)[i] << 16);
+}
+
+// Eight consecutive elements from p on, `left` of which exist (the others are zero).  vec: p is a 16-byte address.
+template <int XT> __device__ __forceinline__ void x_load8(const char *p, int64_t left, bool vec, float (&v)[8]) {
+  if (vec && left >= 8) {
+    if constexpr (XT == RSVD_X_F32) {
+      const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+    } else {
+      const u32x4 a = *reinterpret_cast<const u32x4 *>(p);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (XT == RSVD_X_BF16) {
+          v[2 * e] = __uint_as_float(a[e] << 16);
+          v[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u);
+        } else {
+          const unsigned pair = a[e];      // (a copy: the cast of a vector's element takes its first one)
+          const f16x2 h = __builtin_bit_cast(f16x2, pair);
+          v[2 * e] = (float)h[0];
+          v[2 * e + 1] = (float)h[1];
+        }
+      }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = e < left ? x_value<XT>(p, e) : 0.f;
+  }
+}
+
+__device__ __forceinline__ unsigned bf16_pair(float a, float b) {      // rounded to nearest even
+  return __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{a, b}, bf16x2));
+}
+__device__ __forceinline__ float bf16_low(unsigned pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float bf16_high(unsigned pair) { return __uint_as_float(pair & 0xffff0000u); }
+
+// The parts of two numbers as bf16 numbers, the largest first, each the rounded rest of the ones before: three hold every fp32
+// number, two every fp16 number and any other to 2^-17 of itself.  Numbers that round to infinity are cut off instead; an infinity
+// or NaN has zeros behind its first part.
+template <int PARTS> __device__ __forceinline__ void bf16_parts2(float a, float b, unsigned (&p)[PARTS]) {
+#pragma unroll
+  for (int s = 0; s < PARTS; ++s) {
+    p[s] = bf16_pair(a, b);
+    if (s + 1 < PARTS) {
+      float ra = a - bf16_low(p[s]), rb = b - bf16_high(p[s]);
+      if (s == 0 && ((p[0] & 0x7f80u) == 0x7f80u || (p[0] & 0x7f800000u) == 0x7f800000u)) {
+        const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
+        if ((p[0] & 0x7f80u) == 0x7f80u) {
+          const bool finite = (ua & 0x7f800000u) != 0x7f800000u;
+          if (finite) p[0] = (p[0] & 0xffff0000u) | (ua >> 16);
+          ra = finite ? a - __uint_as_float(ua & 0xffff0000u) : 0.f;
+        }
+        if ((p[0] & 0x7f800000u) == 0x7f800000u) {
+          const bool finite = (ub & 0x7f800000u) != 0x7f800000u;
+          if (finite) p[0] = (p[0] & 0x0000ffffu) | (ub & 0xffff0000u);
+          rb = finite ? b - __uint_as_float(ub & 0xffff0000u) : 0.f;
+        }
+      }
+      a = ra;
+      b = rb;
+    }
+  }
+}
+#endif
+
+// ---------------------------------------------------------------- layer8_rows.hip
+// Rows of X (rows x n) to codes with a scale each; a row of codes is written up to `width` (>= n, a multiple of 8) with zeros behind n.
+hipError_t rows8_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, int8_t *codes,
+                        int64_t ldq, int64_t width, float *scale);
+hipError_t keep8_save_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, const void *X, int64_t ldx, int8_t *codes,
+                             int64_t ldc, uint8_t *powers, int64_t ldp);
+hipError_t keep8_load_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, const int8_t *codes, int64_t ldc,
+                             const uint8_t *powers, int64_t ldp, void *X, int64_t ldx);
+// planes[p][row][0 .. width): the bf16 parts of X_rj factor_j (factor NULL: of X_rj), zeros from n on.
+hipError_t split_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, const float *factor,
+                             uint16_t *planes, int64_t width);
+// planes[p][j][0 .. width): the bf16 parts of X_rj at place r, zeros from `rows` on.  sums != NULL: sums[b][j] is the sum of column j over
+// the 64 rows from 64 b on.
+hipError_t transpose_split_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint16_t *planes,
+                                  int64_t width, float *sums);
+// plane[j][0 .. width): codes_rj factor_r (factor NULL: codes_rj) as bf16 at place r, zeros from `rows` on.
+hipError_t transpose_codes_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldq, const float *factor,
+                                  uint16_t *plane, int64_t width);
+hipError_t transpose_kept_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers,
+                                 int64_t ldp, uint16_t *plane, int64_t width);
+// out[j] (+)= sum over b of sums[b][j]
+hipError_t add_sums_launch(hipStream_t s, int64_t blocks, int64_t n, const float *sums, float *out, int accumulate);
+hipError_t fill_zero_launch(hipStream_t s, int64_t rows, int64_t cols, float *out, int64_t ld);
+
+// ---------------------------------------------------------------- the low-rank term
+// t (tokens x 2 rp bf16): the sums of X (tokens x n) with the rows of F (r x n, bf16) as two bf16 numbers each, the rounded sum in the first
+// rp places and the rounded rest of it in the others; zeros from r on.
+constexpr int64_t kMaxRank = 1024;
+inline int64_t rank_places(int64_t r) { return align_up((size_t)r, 32); }
+hipError_t lowrank_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, int64_t r, const void *X, int64_t ldx,
+                          const void *F, int64_t ldf, uint16_t *t);
+
+// What becomes of a sum over k: value_ti = rs_t cs_i sum + sum_p t_tp G_ip + bias_i
+struct Layer8Out {
+  const float *rs = nullptr, *cs = nullptr, *bias = nullptr;      // NULL: ones, ones, zeros
+  const uint16_t *t = nullptr;                                    // as lowrank_launch leaves it
+  const uint16_t *G = nullptr; int64_t ldg = 0; int r = 0;        // bf16, N x r
+  void *C = nullptr; int64_t ldc = 0; int type = RSVD_X_F32;      // M x N
+  int accumulate = 0;                                             // (fp32)
+};
+
+// ---------------------------------------------------------------- layer8_gemm.hip
+// C (M x N) out of sums over k of A (M rows) and B (N rows), both with consecutive k, in k-tiles of 128 bytes: 128 8-bit codes or 64 bf16
+// numbers.  Both start at 16-byte addresses and have row lengths of a multiple of 16 bytes.
+struct NtDesc {
+  bool codes = false;                    // 8-bit codes, summed as integers; else bf16
+  int64_t M = 0, N = 0;
+  int64_t ktiles = 0;                    // every row of A has that many whole k-tiles, zeros behind the last k
+  const void *A = nullptr; int64_t lda = 0;      // bytes
+  int planes = 1; int64_t plane = 0;     // A is a sum of `planes` matrices, `plane` bytes apart (the largest first)
+  const void *B = nullptr; int64_t ldb = 0;      // bytes
+  int64_t b_bytes = 0;                   // bytes of a row of B that may be read (a multiple of 16); finite
+  Layer8Out out;
+  float *partial = nullptr; size_t partial_bytes = 0;      // for sums over k in several parts
+};
+size_t nt_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t ktiles, bool lowrank);      // ktiles of all planes
+hipError_t nt_launch(rsvd_ctx *ctx, hipStream_t s, const NtDesc &d);
+
+// ---------------------------------------------------------------- layer8_few.hip
+// The product of codes for a few tokens.
+constexpr int64_t kFewTokens = 64;
+struct FewDesc {
+  int64_t M = 0, N = 0, k = 0;           // k: a multiple of 64, zeros in A behind the last
+  const int8_t *A = nullptr; int64_t lda = 0;
+  const int8_t *B = nullptr; int64_t ldb = 0;
+  Layer8Out out;
+};
+hipError_t few_launch(rsvd_ctx *ctx, hipStream_t s, const FewDesc &d);
+
+}  // namespace rsvd

@@ -1,0 +1,394 @@
+// Numbers to 8 bits and back, and the operand planes of the bf16 products of the layer operators.
+#include "layer8.hpp"
+
+namespace rsvd {
+
+__device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+
+// Eight integers in [-127, 127], given as floats, as bytes.
+__device__ __forceinline__ u32x2 pack8(const float (&q)[8]) {
+  u32x2 w;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+    w[h] = ((unsigned)(int)q[4 * h] & 255u) | (((unsigned)(int)q[4 * h + 1] & 255u) << 8) | (((unsigned)(int)q[4 * h + 2] & 255u) << 16) |
+           ((unsigned)(int)q[4 * h + 3] << 24);
+  return w;
+}
+
+// ---------------------------------------------------------------- rows with a scale each
+// One workgroup per row.  The largest magnitude is found among the bit patterns (as integers they are ordered like the
+// magnitudes, infinity and NaN on top).  CH chunks of 8 elements stay in a thread's registers between the maximum and
+// the codes; CH = 0: longer rows are read twice.
+template <int XT, int CH>
+__global__ __launch_bounds__(256) void rows8_kernel(const char *__restrict__ X, int64_t ldx, int n, int8_t *__restrict__ codes,
+                                                    int64_t ldq, int width, float *__restrict__ scale, int vec) {
+  __shared__ unsigned part[4];
+  const int tid = threadIdx.x;
+  const int64_t row = blockIdx.x;
+  const char *x = X + row * ldx * XTraits<XT>::SIZE;
+  const int chunks = (width + 7) / 8;
+  float v[CH > 0 ? CH : 1][8];
+  unsigned top = 0u;
+  if constexpr (CH > 0) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int j = 8 * (tid + 256 * c);
+      x_load8<XT>(x + (int64_t)j * XTraits<XT>::SIZE, n - j, vec != 0, v[c]);
+    }
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[c][e]));
+  } else {
+    for (int c = tid; c < chunks; c += 256) {
+      x_load8<XT>(x + (int64_t)8 * c * XTraits<XT>::SIZE, n - 8 * c, vec != 0, v[0]);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[0][e]));
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, d));
+  if ((tid & 63) == 0) part[tid >> 6] = top;
+  __syncthreads();
+  top = max(max(part[0], part[1]), max(part[2], part[3]));
+  const float a = __uint_as_float(top);
+  const bool bad = top >= 0x7f800000u, none = bad || a < 0x1p-116f;
+  const float per = none ? 0.f : 127.f / a;
+  if (tid == 0) scale[row] = bad ? __uint_as_float(0x7fc00000u) : none ? 0.f : a / 127.f;
+  auto store = [&](int c, const float (&w)[8]) RSVD_INLINE {
+    float q[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) q[e] = none ? 0.f : __builtin_rintf(w[e] * per);
+    *reinterpret_cast<u32x2 *>(codes + row * ldq + 8 * c) = pack8(q);
+  };
+  if constexpr (CH > 0) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (tid + 256 * c < chunks) store(tid + 256 * c, v[c]);
+  } else {
+    for (int c = tid; c < chunks; c += 256) {
+      x_load8<XT>(x + (int64_t)8 * c * XTraits<XT>::SIZE, n - 8 * c, vec != 0, v[0]);
+      store(c, v[0]);
+    }
+  }
+}
+
+template <int XT>
+static void rows8_typed(hipStream_t s, int64_t rows, int64_t n, const void *X, int64_t ldx, int8_t *codes, int64_t ldq, int64_t width,
+                        float *scale) {
+  const int vec = rows_aligned(X, ldx, XTraits<XT>::SIZE) ? 1 : 0;
+  const int64_t chunks = ceil_div(width, 8);
+#define ROWS8(CH)                                                                                                                     \
+  hipLaunchKernelGGL((rows8_kernel<XT, CH>), dim3((unsigned)rows), dim3(256), 0, s, (const char *)X, ldx, (int)n, codes, ldq, (int)width, \
+                     scale, vec)
+  if (chunks <= 256) ROWS8(1);
+  else if (chunks <= 512) ROWS8(2);
+  else if (chunks <= 1024) ROWS8(4);
+  else if (chunks <= 2048) ROWS8(8);
+  else ROWS8(0);
+#undef ROWS8
+}
+
+hipError_t rows8_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, int8_t *codes, int64_t ldq,
+                        int64_t width, float *scale) {
+  if (type == RSVD_X_BF16) rows8_typed<RSVD_X_BF16>(s, rows, n, X, ldx, codes, ldq, width, scale);
+  else if (type == RSVD_X_F16) rows8_typed<RSVD_X_F16>(s, rows, n, X, ldx, codes, ldq, width, scale);
+  else rows8_typed<RSVD_X_F32>(s, rows, n, X, ldx, codes, ldq, width, scale);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- blocks of 32 with a power of two
+// Eight features a thread, so four lanes share a block.  A workgroup covers `lanes` chunks (a power of two, at least 4) of 256 / lanes rows.
+__device__ __forceinline__ unsigned quad_max(unsigned x) {
+  x = max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0xb1, 0xf, 0xf, true));      // lanes 1 0 3 2
+  return max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0x4e, 0xf, 0xf, true));   // lanes 2 3 0 1
+}
+
+template <int XT>
+__global__ __launch_bounds__(256) void keep8_save_kernel(const char *__restrict__ X, int64_t ldx, int64_t tokens, int n,
+                                                         int8_t *__restrict__ codes, int64_t ldc, uint8_t *__restrict__ powers, int64_t ldp,
+                                                         int shift, int vec) {
+  const int c = (int)(blockIdx.x << shift) + (int)(threadIdx.x & ((1u << shift) - 1u));
+  const int rows = 256 >> shift;
+  if ((c >> 2) * 32 >= n) return;                       // (whole blocks only: the quads stay together)
+  for (int64_t t = (int64_t)blockIdx.y * rows + (threadIdx.x >> shift); t < tokens; t += (int64_t)gridDim.y * rows) {
+    float v[8], q[8];
+    x_load8<XT>(X + (t * ldx + 8 * c) * XTraits<XT>::SIZE, n - 8 * c, vec != 0, v);
+    unsigned top = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[e]));
+    top = quad_max(top);
+    const bool bad = top >= 0x7f800000u;
+    // a = f 2^E in [2^(E-1), 2^E): its biased exponent is E + 126 (0 below 2^-126), and e + 127 = E + 120
+    int byte = (int)(top >> 23) - 6;
+    byte = byte < 1 ? 1 : byte;
+    const float per = __uint_as_float((unsigned)(254 - byte) << 23);      // 2^-e: 2^126 at the most, 2^-121 at the least
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float y = __builtin_rintf(v[e] * per);
+      q[e] = bad ? 0.f : y > 127.f ? 127.f : y < -127.f ? -127.f : y;
+    }
+    if (8 * c < (n + 15) / 16 * 16) *reinterpret_cast<u32x2 *>(codes + t * ldc + 8 * c) = pack8(q);
+    if ((c & 3) == 0) powers[t * ldp + (c >> 2)] = (uint8_t)(bad ? 255 : byte);
+  }
+}
+
+// The value of code q of a block with power byte b: exact in bf16.
+__device__ __forceinline__ float kept_unit(unsigned b) { return b == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(b << 23); }
+
+template <int XT>
+__global__ __launch_bounds__(256) void keep8_load_kernel(const int8_t *__restrict__ codes, int64_t ldc, const uint8_t *__restrict__ powers,
+                                                         int64_t ldp, int64_t tokens, int n, char *__restrict__ X, int64_t ldx, int shift,
+                                                         int vec) {
+  const int c = (int)(blockIdx.x << shift) + (int)(threadIdx.x & ((1u << shift) - 1u));
+  const int rows = 256 >> shift;
+  if (8 * c >= n) return;
+  for (int64_t t = (int64_t)blockIdx.y * rows + (threadIdx.x >> shift); t < tokens; t += (int64_t)gridDim.y * rows) {
+    const u32x2 w = *reinterpret_cast<const u32x2 *>(codes + t * ldc + 8 * c);
+    const float unit = kept_unit(powers[t * ldp + (c >> 2)]);
+    float v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = (float)((int)(w[e >> 2] << (24 - 8 * (e & 3))) >> 24) * unit;
+    char *x = X + (t * ldx + 8 * c) * XTraits<XT>::SIZE;
+    if constexpr (XT == RSVD_X_F32) {
+      if (vec && n - 8 * c >= 8) {
+        reinterpret_cast<f32x4 *>(x)[0] = f32x4{v[0], v[1], v[2], v[3]};
+        reinterpret_cast<f32x4 *>(x)[1] = f32x4{v[4], v[5], v[6], v[7]};
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (8 * c + e < n) reinterpret_cast<float *>(x)[e] = v[e];
+      }
+    } else {
+      u32x4 p;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (XT == RSVD_X_BF16) p[e] = bf16_pair(v[2 * e], v[2 * e + 1]);
+        else p[e] = __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{v[2 * e], v[2 * e + 1]}, f16x2));
+      }
+      if (vec && n - 8 * c >= 8) {
+        *reinterpret_cast<u32x4 *>(x) = p;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (8 * c + e < n) reinterpret_cast<uint16_t *>(x)[e] = (uint16_t)(p[e >> 1] >> (16 * (e & 1)));
+      }
+    }
+  }
+}
+
+// Lanes along a row (log2) and grid of the two kernels above.
+static dim3 keep8_grid(int64_t tokens, int64_t n, int &shift) {
+  const int64_t chunks = ceil_div(n, 32) * 4;
+  shift = 2;
+  while (shift < 8 && (1 << shift) < chunks) ++shift;
+  int64_t groups = ceil_div(tokens, 256 >> shift);
+  if (groups > 65535) groups = 65535;
+  return dim3((unsigned)ceil_div(chunks, 1 << shift), (unsigned)groups);
+}
+
+hipError_t keep8_save_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, const void *X, int64_t ldx, int8_t *codes,
+                             int64_t ldc, uint8_t *powers, int64_t ldp) {
+  int shift;
+  const dim3 grid = keep8_grid(tokens, n, shift);
+  const int vec = rows_aligned(X, ldx, xtype_size(type)) ? 1 : 0;
+#define SAVE(XT)                                                                                                                        \
+  hipLaunchKernelGGL(keep8_save_kernel<XT>, grid, dim3(256), 0, s, (const char *)X, ldx, tokens, (int)n, codes, ldc, powers, ldp, shift, vec)
+  if (type == RSVD_X_BF16) SAVE(RSVD_X_BF16);
+  else if (type == RSVD_X_F16) SAVE(RSVD_X_F16);
+  else SAVE(RSVD_X_F32);
+#undef SAVE
+  return hipGetLastError();
+}
+
+hipError_t keep8_load_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, const int8_t *codes, int64_t ldc,
+                             const uint8_t *powers, int64_t ldp, void *X, int64_t ldx) {
+  int shift;
+  const dim3 grid = keep8_grid(tokens, n, shift);
+  const int vec = rows_aligned(X, ldx, xtype_size(type)) ? 1 : 0;
+#define LOAD(XT)                                                                                                                    \
+  hipLaunchKernelGGL(keep8_load_kernel<XT>, grid, dim3(256), 0, s, codes, ldc, powers, ldp, tokens, (int)n, (char *)X, ldx, shift, vec)
+  if (type == RSVD_X_BF16) LOAD(RSVD_X_BF16);
+  else if (type == RSVD_X_F16) LOAD(RSVD_X_F16);
+  else LOAD(RSVD_X_F32);
+#undef LOAD
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- operand planes
+template <int XT>
+__global__ __launch_bounds__(256) void split_rows_kernel(const char *__restrict__ X, int64_t ldx, int64_t n, const float *__restrict__ factor,
+                                                         uint16_t *__restrict__ planes, int64_t width, int64_t plane, int vec) {
+  constexpr int P = XTraits<XT>::PARTS;
+  const int64_t j = 8 * ((int64_t)blockIdx.x * 256 + threadIdx.x), row = blockIdx.y + (int64_t)blockIdx.z * 65535;
+  if (j >= width || row * width >= plane) return;
+  float v[8];
+  x_load8<XT>(X + (row * ldx + j) * XTraits<XT>::SIZE, n - j, vec != 0, v);
+  if (factor != nullptr) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (j + e < n) v[e] *= factor[j + e];
+  }
+  u32x4 out[P];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    unsigned p[P];
+    bf16_parts2<P>(v[2 * e], v[2 * e + 1], p);
+#pragma unroll
+    for (int q = 0; q < P; ++q) out[q][e] = p[q];
+  }
+#pragma unroll
+  for (int q = 0; q < P; ++q) *reinterpret_cast<u32x4 *>(planes + q * plane + row * width + j) = out[q];
+}
+
+hipError_t split_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, const float *factor,
+                             uint16_t *planes, int64_t width) {
+  const int vec = rows_aligned(X, ldx, xtype_size(type)) ? 1 : 0;
+  const dim3 grid((unsigned)ceil_div(width, 2048), (unsigned)(rows < 65535 ? rows : 65535), (unsigned)ceil_div(rows, 65535));
+#define SPLIT(XT) \
+  hipLaunchKernelGGL(split_rows_kernel<XT>, grid, dim3(256), 0, s, (const char *)X, ldx, n, factor, planes, width, rows * width, vec)
+  if (type == RSVD_X_BF16) SPLIT(RSVD_X_BF16);
+  else if (type == RSVD_X_F16) SPLIT(RSVD_X_F16);
+  else SPLIT(RSVD_X_F32);
+#undef SPLIT
+  return hipGetLastError();
+}
+
+// Transposes through LDS, 64 rows x 64 columns a workgroup.  SRC: 0 ... 2 numbers of an rsvd_xtype, 3 codes with a factor for each row,
+// 4 kept codes.
+constexpr int kFromCodes = 3, kFromKept = 4;
+template <int SRC> struct SrcTraits { static constexpr int PARTS = 1; };
+template <> struct SrcTraits<RSVD_X_F16> { static constexpr int PARTS = 2; };
+template <> struct SrcTraits<RSVD_X_F32> { static constexpr int PARTS = 3; };
+
+struct TransposeParams {
+  const char *X; int64_t ldx, rows, n;
+  const float *factor;
+  const uint8_t *powers; int64_t ldp;
+  uint16_t *planes; int64_t width, plane;
+  float *sums;
+  int vec;
+};
+
+template <int SRC> __global__ __launch_bounds__(256) void transpose_kernel(const TransposeParams P) {
+  constexpr int PARTS = SrcTraits<SRC>::PARTS, PITCH = 66;      // 33 dwords: rows start at different banks
+  __shared__ uint16_t tile[PARTS][64 * PITCH];
+  const int tid = threadIdx.x;
+  const int64_t r0 = (int64_t)blockIdx.x * 64, j0 = (int64_t)blockIdx.y * 64;
+  {
+    const int r = tid >> 2, j = (tid & 3) * 16;
+    const int64_t row = r0 + r;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t col = j0 + j + 8 * h;
+      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (row < P.rows && col < P.n) {
+        if constexpr (SRC < kFromCodes) {
+          x_load8<SRC>(P.X + (row * P.ldx + col) * XTraits<SRC>::SIZE, P.n - col, P.vec != 0, v);
+        } else {
+          const u32x2 w = *reinterpret_cast<const u32x2 *>(P.X + row * P.ldx + col);
+          const float unit = SRC == kFromKept ? kept_unit(P.powers[row * P.ldp + (col >> 5)]) : P.factor != nullptr ? P.factor[row] : 1.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = (float)((int)(w[e >> 2] << (24 - 8 * (e & 3))) >> 24) * unit;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        unsigned p[PARTS];
+        bf16_parts2<PARTS>(v[2 * e], v[2 * e + 1], p);
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q) {
+          tile[q][(j + 8 * h + 2 * e) * PITCH + r] = (uint16_t)p[q];
+          tile[q][(j + 8 * h + 2 * e + 1) * PITCH + r] = (uint16_t)(p[q] >> 16);
+        }
+      }
+    }
+  }
+  __syncthreads();
+  const int j = tid >> 2, r = (tid & 3) * 16;
+  const int64_t col = j0 + j;
+  if (SRC < kFromCodes && P.sums != nullptr) {
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      float x = 0.f;
+#pragma unroll
+      for (int q = PARTS - 1; q >= 0; --q) x += __uint_as_float((unsigned)tile[q][j * PITCH + r + e] << 16);
+      sum += x;
+    }
+    sum += __shfl_xor(sum, 1);
+    sum += __shfl_xor(sum, 2);
+    if ((tid & 3) == 0 && col < P.n) P.sums[(int64_t)blockIdx.x * P.n + col] = sum;
+  }
+  if (col >= P.n) return;
+#pragma unroll
+  for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t place = r0 + r + 8 * h;
+      if (place >= P.width) continue;
+      u32x4 out;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[e] = *reinterpret_cast<const unsigned *>(&tile[q][j * PITCH + r + 8 * h + 2 * e]);
+      *reinterpret_cast<u32x4 *>(P.planes + q * P.plane + col * P.width + place) = out;
+    }
+}
+
+static dim3 transpose_grid(int64_t rows, int64_t n) { return dim3((unsigned)ceil_div(rows, 64), (unsigned)ceil_div(n, 64)); }
+
+hipError_t transpose_split_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint16_t *planes,
+                                  int64_t width, float *sums) {
+  const TransposeParams P = {(const char *)X, ldx, rows, n, nullptr, nullptr, 0, planes, width, n * width, sums,
+                             rows_aligned(X, ldx, xtype_size(type)) ? 1 : 0};
+  const dim3 grid = transpose_grid(rows, n);
+  if (type == RSVD_X_BF16) hipLaunchKernelGGL(transpose_kernel<RSVD_X_BF16>, grid, dim3(256), 0, s, P);
+  else if (type == RSVD_X_F16) hipLaunchKernelGGL(transpose_kernel<RSVD_X_F16>, grid, dim3(256), 0, s, P);
+  else hipLaunchKernelGGL(transpose_kernel<RSVD_X_F32>, grid, dim3(256), 0, s, P);
+  return hipGetLastError();
+}
+
+hipError_t transpose_codes_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldq, const float *factor,
+                                  uint16_t *plane, int64_t width) {
+  const TransposeParams P = {(const char *)codes, ldq, rows, n, factor, nullptr, 0, plane, width, n * width, nullptr, 1};
+  hipLaunchKernelGGL(transpose_kernel<kFromCodes>, transpose_grid(rows, n), dim3(256), 0, s, P);
+  return hipGetLastError();
+}
+
+hipError_t transpose_kept_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp,
+                                 uint16_t *plane, int64_t width) {
+  const TransposeParams P = {(const char *)codes, ldc, rows, n, nullptr, powers, ldp, plane, width, n * width, nullptr, 1};
+  hipLaunchKernelGGL(transpose_kernel<kFromKept>, transpose_grid(rows, n), dim3(256), 0, s, P);
+  return hipGetLastError();
+}
+
+__global__ __launch_bounds__(256) void add_sums_kernel(const float *__restrict__ sums, int64_t blocks, int64_t n, float *__restrict__ out,
+                                                       int accumulate) {
+  const int64_t j = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
+  __shared__ float part[4][64];
+  float sum = 0.f;
+  if (j < n)
+    for (int64_t b = threadIdx.x >> 6; b < blocks; b += 4) sum += sums[b * n + j];
+  part[threadIdx.x >> 6][threadIdx.x & 63] = sum;
+  __syncthreads();
+  if (threadIdx.x >= 64 || j >= n) return;
+  sum = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+  out[j] = accumulate ? out[j] + sum : sum;
+}
+
+hipError_t add_sums_launch(hipStream_t s, int64_t blocks, int64_t n, const float *sums, float *out, int accumulate) {
+  hipLaunchKernelGGL(add_sums_kernel, dim3((unsigned)ceil_div(n, 64)), dim3(256), 0, s, sums, blocks, n, out, accumulate);
+  return hipGetLastError();
+}
+
+__global__ __launch_bounds__(256) void fill_zero_kernel(float *__restrict__ out, int64_t rows, int64_t cols, int64_t ld) {
+  for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
+    for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < cols; c += (int64_t)gridDim.x * 256) out[r * ld + c] = 0.f;
+}
+
+hipError_t fill_zero_launch(hipStream_t s, int64_t rows, int64_t cols, float *out, int64_t ld) {
+  const int64_t gx = ceil_div(cols, 256), gy = rows < 4096 ? rows : 4096;
+  hipLaunchKernelGGL(fill_zero_kernel, dim3((unsigned)(gx < 64 ? gx : 64), (unsigned)gy), dim3(256), 0, s, out, rows, cols, ld);
+  return hipGetLastError();
+}
+
+}  // namespace rsvd

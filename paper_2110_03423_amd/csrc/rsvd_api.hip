@@ -524,6 +524,7 @@ int rsvd_create(rsvd_ctx **out, int device) {
       if (e2 == hipSuccess) e2 = apply_init_device(c);
       if (e2 == hipSuccess) e2 = gram_init_device(c);
       if (e2 == hipSuccess) e2 = gemm_split_init_device(c);
+      if (e2 == hipSuccess) e2 = layer8_init_device(c);
       if (cur >= 0 && cur != device) (void)hipSetDevice(cur);
       if (e2 != hipSuccess) {
         (void)hipGetLastError();

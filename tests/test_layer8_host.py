@@ -1,0 +1,149 @@
+"""Argument checks and workspace sizes of the layer operators on a planning context: no GPU.  The fake device pointers are
+never dereferenced."""
+import ctypes as C
+
+import pytest
+
+from paper_2110_03423_amd import binding
+from paper_2110_03423_amd.binding import ERR_NO_DEVICE, X_BF16, X_F16, X_F32
+
+UNSUPPORTED = 4
+PTR = C.c_void_p(1 << 20)
+ODD = C.c_void_p((1 << 20) + 1)
+HALF = C.c_void_p((1 << 20) + 2)
+NULL = C.c_void_p(0)
+
+
+@pytest.fixture(scope="module")
+def plan():
+    import os
+    if not os.path.exists(binding.library_path()):
+        from paper_2110_03423_amd import build
+        build.build_library()
+    return binding.Rsvd(device=None)
+
+
+def _call(plan, name, order, base, **kw):
+    a = dict(base, **kw)
+    return getattr(plan.lib, name)(*[a[k] for k in order])
+
+
+PRODUCT = "ctx stream type tokens n m r X ldx codes ldq scale U ldu Vt ldvt bias Y ldy ws bytes".split()
+GRAD = "ctx stream type tokens n m r dY lddy codes ldq scale Ut ldut V ldv dX lddx ws bytes".split()
+ROWS = "ctx stream type rows n X ldx codes ldq scale".split()
+SAVE = "ctx stream type tokens n X ldx codes ldc powers ldp".split()
+LOAD = "ctx stream type tokens n codes ldc powers ldp X ldx".split()
+WGRAD = "ctx stream type tokens n m dY lddy codes ldc powers ldp dW lddw db accumulate ws bytes".split()
+
+
+def test_product_checks_every_argument(plan):
+    base = dict(ctx=plan.h, stream=NULL, type=X_BF16, tokens=100, n=70, m=50, r=9, X=PTR, ldx=70, codes=PTR, ldq=80, scale=PTR, U=PTR, ldu=9,
+                Vt=PTR, ldvt=70, bias=PTR, Y=PTR, ldy=50, ws=PTR, bytes=1 << 40)
+    call = lambda **kw: _call(plan, "rsvd_q8_product", PRODUCT, base, **kw)
+    assert call() == ERR_NO_DEVICE
+    assert call(ctx=None) == -1 and call(type=3) == -3 and call(type=-1) == -3
+    assert call(tokens=-1) == -4 and call(n=0) == -5 and call(m=0) == -6 and call(r=-1) == -7
+    assert call(tokens=0, X=NULL, Y=NULL, ws=NULL) == 0
+    assert call(X=NULL) == -8 and call(X=ODD) == -8 and call(X=HALF) == ERR_NO_DEVICE and call(type=X_F32, X=HALF) == -8
+    assert call(ldx=69) == -9 and call(codes=NULL) == -10 and call(codes=HALF) == -10
+    assert call(ldq=64) == -11 and call(ldq=72) == -11 and call(scale=NULL) == -12 and call(scale=HALF) == -12
+    assert call(U=NULL) == -13 and call(U=ODD) == -13 and call(ldu=8) == -14 and call(Vt=NULL) == -15 and call(ldvt=69) == -16
+    assert call(r=0, U=NULL, Vt=NULL, ldu=0, ldvt=0) == ERR_NO_DEVICE
+    assert call(bias=HALF) == -17 and call(bias=NULL) == ERR_NO_DEVICE
+    assert call(Y=NULL) == -18 and call(Y=ODD) == -18 and call(ldy=49) == -19
+    assert call(ws=NULL) == -20 and call(ws=C.c_void_p((1 << 20) + 128)) == -20
+    need = C.c_size_t()
+    assert plan.lib.rsvd_q8_product_bytes(plan.h, X_BF16, 100, 70, 50, 9, C.byref(need)) == 0
+    assert call(bytes=need.value - 1) == -21 and call(bytes=need.value) == ERR_NO_DEVICE
+    wide = binding_limit()
+    assert call(n=wide, ldx=wide, ldq=wide, ldvt=wide) == ERR_NO_DEVICE
+    assert call(n=wide + 1, ldx=wide + 1, ldq=wide + 16, ldvt=wide + 1) == UNSUPPORTED
+    assert call(r=1025, ldu=1025) == UNSUPPORTED
+
+
+def binding_limit():
+    return 131072
+
+
+def test_product_gradient_checks_every_argument(plan):
+    base = dict(ctx=plan.h, stream=NULL, type=X_F16, tokens=100, n=70, m=50, r=9, dY=PTR, lddy=50, codes=PTR, ldq=80, scale=PTR, Ut=PTR,
+                ldut=50, V=PTR, ldv=9, dX=PTR, lddx=70, ws=PTR, bytes=1 << 40)
+    call = lambda **kw: _call(plan, "rsvd_q8_product_grad", GRAD, base, **kw)
+    assert call() == ERR_NO_DEVICE
+    assert call(ctx=None) == -1 and call(type=9) == -3 and call(tokens=-5) == -4 and call(n=0) == -5 and call(m=0) == -6 and call(r=-1) == -7
+    assert call(tokens=0) == 0
+    assert call(dY=NULL) == -8 and call(lddy=49) == -9 and call(codes=NULL) == -10 and call(ldq=79) == -11 and call(scale=NULL) == -12
+    assert call(Ut=NULL) == -13 and call(ldut=49) == -14 and call(V=NULL) == -15 and call(ldv=8) == -16
+    assert call(dX=NULL) == -17 and call(lddx=69) == -18 and call(ws=NULL) == -19
+    need = C.c_size_t()
+    assert plan.lib.rsvd_q8_product_grad_bytes(plan.h, X_F16, 100, 70, 50, 9, C.byref(need)) == 0
+    assert call(bytes=need.value - 1) == -20 and call(bytes=need.value) == ERR_NO_DEVICE
+    assert call(tokens=(1 << 22) + 1) == UNSUPPORTED
+
+
+def test_rows_and_kept_activations_check_every_argument(plan):
+    base = dict(ctx=plan.h, stream=NULL, type=X_F32, rows=10, n=33, X=PTR, ldx=33, codes=PTR, ldq=48, scale=PTR)
+    call = lambda **kw: _call(plan, "rsvd_q8_rows", ROWS, base, **kw)
+    assert call() == ERR_NO_DEVICE and call(rows=0) == 0
+    assert call(ctx=None) == -1 and call(type=3) == -3 and call(rows=-1) == -4 and call(n=0) == -5 and call(X=HALF) == -6
+    assert call(ldx=32) == -7 and call(codes=HALF) == -8 and call(ldq=32) == -9 and call(scale=NULL) == -10
+    base = dict(ctx=plan.h, stream=NULL, type=X_F32, tokens=10, n=33, X=PTR, ldx=33, codes=PTR, ldc=48, powers=ODD, ldp=2)
+    call = lambda **kw: _call(plan, "rsvd_keep8_save", SAVE, base, **kw)
+    assert call() == ERR_NO_DEVICE and call(tokens=0) == 0
+    assert call(type=3) == -3 and call(tokens=-1) == -4 and call(n=0) == -5 and call(X=NULL) == -6 and call(ldx=32) == -7
+    assert call(codes=NULL) == -8 and call(ldc=40) == -9 and call(powers=NULL) == -10 and call(ldp=1) == -11
+    call = lambda **kw: _call(plan, "rsvd_keep8_load", LOAD, base, **kw)
+    assert call() == ERR_NO_DEVICE and call(tokens=0) == 0
+    assert call(codes=HALF) == -6 and call(ldc=32) == -7 and call(powers=NULL) == -8 and call(ldp=1) == -9
+    assert call(X=NULL) == -10 and call(ldx=32) == -11
+
+
+def test_weight_gradient_checks_every_argument(plan):
+    base = dict(ctx=plan.h, stream=NULL, type=X_BF16, tokens=100, n=70, m=50, dY=PTR, lddy=50, codes=PTR, ldc=80, powers=ODD, ldp=3, dW=PTR,
+                lddw=70, db=PTR, accumulate=0, ws=PTR, bytes=1 << 40)
+    call = lambda **kw: _call(plan, "rsvd_keep8_grad", WGRAD, base, **kw)
+    assert call() == ERR_NO_DEVICE and call(db=NULL) == ERR_NO_DEVICE and call(accumulate=1) == ERR_NO_DEVICE
+    assert call(ctx=None) == -1 and call(type=3) == -3 and call(tokens=-1) == -4 and call(n=0) == -5 and call(m=0) == -6
+    assert call(dY=NULL) == -7 and call(lddy=49) == -8 and call(codes=NULL) == -9 and call(ldc=79) == -10 and call(powers=NULL) == -11
+    assert call(ldp=2) == -12 and call(dW=NULL) == -13 and call(lddw=69) == -14 and call(db=HALF) == -15
+    assert call(ws=NULL) == -17 and call(bytes=0) == -18
+    assert call(tokens=0, dY=NULL, codes=NULL, ws=NULL) == ERR_NO_DEVICE          # (zeros are written)
+    assert call(tokens=0, dW=NULL) == -13
+
+
+def test_workspace_queries(plan):
+    lib, h, out = plan.lib, plan.h, C.c_size_t()
+    for fn, extra in ((lib.rsvd_q8_product_bytes, (9,)), (lib.rsvd_q8_product_grad_bytes, (9,)), (lib.rsvd_keep8_grad_bytes, ())):
+        sizes = []
+        for tokens in (0, 1, 64, 65, 1000, 20000):
+            assert fn(h, X_F32, tokens, 512, 384, *extra, C.byref(out)) == 0
+            assert out.value % 256 == 0
+            sizes.append(out.value)
+        assert sizes[0] == 0 and sizes[1] > 0 and sizes[-1] > sizes[1]
+        assert fn(None, X_F32, 1, 1, 1, *extra, C.byref(out)) == -1
+        assert fn(h, 5, 1, 1, 1, *extra, C.byref(out)) == -2
+        assert fn(h, X_F32, -1, 1, 1, *extra, C.byref(out)) == -3
+        assert fn(h, X_F32, 1, 0, 1, *extra, C.byref(out)) == -4
+        assert fn(h, X_F32, 1, 1, 0, *extra, C.byref(out)) == -5
+        assert fn(h, X_F32, 1, 1 << 20, 1, *extra, C.byref(out)) == UNSUPPORTED
+        assert fn(h, X_F32, 1, 1, 1, *extra, None) == -6 - len(extra)
+    assert lib.rsvd_q8_product_bytes(h, X_F32, 1, 1, 1, -1, C.byref(out)) == -6
+
+
+def test_binding_refuses_what_does_not_fit_together():
+    torch = pytest.importorskip("torch")
+    codes, scale = torch.zeros(6, 5, dtype=torch.int8), torch.zeros(6)
+    U, Vt = torch.zeros(6, 2, dtype=torch.bfloat16), torch.zeros(2, 5, dtype=torch.bfloat16)
+    w = binding.Weight8(codes, scale, U, Vt, torch.zeros(6))
+    assert (w.m, w.n, w.r) == (6, 5, 2) and w.codes.stride(0) % 128 == 0 and w.Ut.shape == (2, 6) and w.V.shape == (5, 2)
+    assert binding.Weight8(codes, scale).r == 0 and binding.Weight8(codes, scale, U[:, :0], Vt[:0]).U is None
+    for bad in ((codes.float(), scale), (codes, scale[:5]), (codes, scale.double()), (codes, scale, U), (codes, scale, U.float(), Vt),
+                (codes, scale, U, Vt[:1]), (codes, scale, U[:5], Vt), (codes, scale, None, None, torch.zeros(5))):
+        with pytest.raises((TypeError, ValueError)):
+            binding.Weight8(*bad)
+    powers = torch.zeros(6, 1, dtype=torch.uint8)
+    assert binding.Kept8(codes, powers, torch.float16).n == 5
+    for bad in ((codes.short(), powers, torch.float32), (codes, powers.int(), torch.float32), (codes, powers[:5], torch.float32),
+                (codes, powers, torch.float64)):
+        with pytest.raises((TypeError, ValueError)):
+            binding.Kept8(*bad)

@@ -13,6 +13,10 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+// (memory takes any alignment of the elements; one instruction all the same)
+typedef unsigned u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
+typedef unsigned u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 
 #define RSVD_INLINE __attribute__((always_inline))
 
@@ -35,15 +39,15 @@ template <int XT> __device__ __forceinline__ float x_value(const char *p, int64_
   else return __uint_as_float((unsigned)reinterpret_cast<const uint16_t *>(p)[i] << 16);
 }
 
-// Eight consecutive elements from p on, `left` of which exist (the others are zero).  vec: p is a 16-byte address.
-template <int XT> __device__ __forceinline__ void x_load8(const char *p, int64_t left, bool vec, float (&v)[8]) {
-  if (vec && left >= 8) {
+// Eight consecutive elements from p on, `left` of which exist (the others are zero).
+template <int XT> __device__ __forceinline__ void x_load8(const char *p, int64_t left, float (&v)[8]) {
+  if (left >= 8) {
     if constexpr (XT == RSVD_X_F32) {
-      const f32x4 a = reinterpret_cast<const f32x4 *>(p)[0], b = reinterpret_cast<const f32x4 *>(p)[1];
+      const f32x4 a = reinterpret_cast<const f32x4_any *>(p)[0], b = reinterpret_cast<const f32x4_any *>(p)[1];
 #pragma unroll
       for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
     } else {
-      const u32x4 a = *reinterpret_cast<const u32x4 *>(p);
+      const u32x4 a = *reinterpret_cast<const u32x4_any *>(p);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         if constexpr (XT == RSVD_X_BF16) {
@@ -61,6 +65,37 @@ template <int XT> __device__ __forceinline__ void x_load8(const char *p, int64_t
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = e < left ? x_value<XT>(p, e) : 0.f;
   }
+}
+
+// Eight consecutive bf16 numbers from p on, as they are.
+__device__ __forceinline__ u32x4 halves8(const uint16_t *p, int64_t left) {
+  u32x4 v = {0u, 0u, 0u, 0u};
+  if (left >= 8) {
+    v = *reinterpret_cast<const u32x4_any *>(p);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) v[e >> 1] |= (unsigned)p[e] << (16 * (e & 1));
+  }
+  return v;
+}
+
+// The same of any type.
+template <int XT> struct Raw8 { u32x4 w[XTraits<XT>::SIZE / 2]; };
+template <int XT> __device__ __forceinline__ Raw8<XT> raw_load8(const char *p, int64_t left) {
+  Raw8<XT> v;
+  if constexpr (XT == RSVD_X_F32) {
+    if (left >= 8) {
+      v.w[0] = reinterpret_cast<const u32x4_any *>(p)[0];
+      v.w[1] = reinterpret_cast<const u32x4_any *>(p)[1];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v.w[e >> 2][e & 3] = e < left ? reinterpret_cast<const unsigned *>(p)[e] : 0u;
+    }
+  } else {
+    v.w[0] = halves8(reinterpret_cast<const uint16_t *>(p), left);
+  }
+  return v;
 }
 
 __device__ __forceinline__ unsigned bf16_pair(float a, float b) {      // rounded to nearest even
@@ -96,12 +131,36 @@ template <int PARTS> __device__ __forceinline__ void bf16_parts2(float a, float 
     }
   }
 }
+
+// Operands of the bf16 matrix instruction out of eight numbers, the largest part first.
+template <int XT> __device__ __forceinline__ void split_operand(const Raw8<XT> &v, u32x4 (&x)[XTraits<XT>::PARTS]) {
+  constexpr int PARTS = XTraits<XT>::PARTS;
+  if constexpr (XT == RSVD_X_BF16) {
+    x[0] = v.w[0];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      unsigned p[PARTS];
+      if constexpr (XT == RSVD_X_F32) {
+        bf16_parts2<PARTS>(__uint_as_float(v.w[e >> 1][2 * (e & 1)]), __uint_as_float(v.w[e >> 1][2 * (e & 1) + 1]), p);
+      } else {
+        const unsigned pair = v.w[0][e];
+        const f16x2 h = __builtin_bit_cast(f16x2, pair);
+        bf16_parts2<PARTS>((float)h[0], (float)h[1], p);
+      }
+#pragma unroll
+      for (int q = 0; q < PARTS; ++q) x[q][e] = p[q];
+    }
+  }
+}
 #endif
 
 // ---------------------------------------------------------------- layer8_rows.hip
 // Rows of X (rows x n) to codes with a scale each; a row of codes is written up to `width` (>= n, a multiple of 8) with zeros behind n.
+// sums != NULL: t is joined on the way (lowrank_join_launch).
 hipError_t rows8_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, int8_t *codes,
-                        int64_t ldq, int64_t width, float *scale);
+                        int64_t ldq, int64_t width, float *scale, const float *sums = nullptr, int splits = 0, int64_t r = 0, int parts = 0,
+                        uint16_t *t = nullptr);
 hipError_t keep8_save_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, const void *X, int64_t ldx, int8_t *codes,
                              int64_t ldc, uint8_t *powers, int64_t ldp);
 hipError_t keep8_load_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, const int8_t *codes, int64_t ldc,
@@ -122,18 +181,25 @@ hipError_t transpose_kept_launch(hipStream_t s, int64_t rows, int64_t n, const i
 hipError_t add_sums_launch(hipStream_t s, int64_t blocks, int64_t n, const float *sums, float *out, int accumulate);
 hipError_t fill_zero_launch(hipStream_t s, int64_t rows, int64_t cols, float *out, int64_t ld);
 
-// ---------------------------------------------------------------- the low-rank term
-// t (tokens x 2 rp bf16): the sums of X (tokens x n) with the rows of F (r x n, bf16) as two bf16 numbers each, the rounded sum in the first
-// rp places and the rounded rest of it in the others; zeros from r on.
-constexpr int64_t kMaxRank = 1024;
+// ---------------------------------------------------------------- layer8_lowrank.hip
+constexpr int64_t kMaxRank = 1024, kFewTokens = 64;
 inline int64_t rank_places(int64_t r) { return align_up((size_t)r, 32); }
-hipError_t lowrank_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, int64_t r, const void *X, int64_t ldx,
-                          const void *F, int64_t ldf, uint16_t *t);
+// bf16 numbers that hold a number of t between the two products: 2^-17 of it is left out with two, nothing with three.
+inline int lowrank_parts(rsvd_xtype type) { return type == RSVD_X_F32 ? 3 : 2; }
+// sums [splits][tokens][rank_places(r)]: the products of X (tokens x n) with the rows of F (r x n, bf16) over ranges of k; zeros from r on.
+int lowrank_splits(const rsvd_ctx *ctx, int64_t tokens, int64_t n, int64_t r);
+hipError_t lowrank_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, int64_t r, const void *X, int64_t ldx,
+                          const void *F, int64_t ldf, float *sums);
+// The same for up to kFewTokens tokens, together with rows8_launch.
+hipError_t front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, int64_t r, const void *X, int64_t ldx,
+                        const void *F, int64_t ldf, float *sums, int8_t *codes, int64_t ldq, int64_t width, float *scale);
+// t [tokens][parts][rank_places(r)]: the sums added up, as bf16 numbers, the largest first.
+hipError_t lowrank_join_launch(hipStream_t s, const float *sums, int splits, int64_t tokens, int64_t r, int parts, uint16_t *t);
 
 // What becomes of a sum over k: value_ti = rs_t cs_i sum + sum_p t_tp G_ip + bias_i
 struct Layer8Out {
   const float *rs = nullptr, *cs = nullptr, *bias = nullptr;      // NULL: ones, ones, zeros
-  const uint16_t *t = nullptr;                                    // as lowrank_launch leaves it
+  const uint16_t *t = nullptr; int parts = 2;                     // as lowrank_join_launch leaves it
   const uint16_t *G = nullptr; int64_t ldg = 0; int r = 0;        // bf16, N x r
   void *C = nullptr; int64_t ldc = 0; int type = RSVD_X_F32;      // M x N
   int accumulate = 0;                                             // (fp32)
@@ -157,12 +223,12 @@ size_t nt_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t ktile
 hipError_t nt_launch(rsvd_ctx *ctx, hipStream_t s, const NtDesc &d);
 
 // ---------------------------------------------------------------- layer8_few.hip
-// The product of codes for a few tokens.
-constexpr int64_t kFewTokens = 64;
+// The product of codes for up to kFewTokens tokens.
 struct FewDesc {
   int64_t M = 0, N = 0, k = 0;           // k: a multiple of 64, zeros in A behind the last
   const int8_t *A = nullptr; int64_t lda = 0;
   const int8_t *B = nullptr; int64_t ldb = 0;
+  const float *sums = nullptr; int splits = 0;      // the low-rank sums as they are, in the place of out.t (NULL: out.t)
   Layer8Out out;
 };
 hipError_t few_launch(rsvd_ctx *ctx, hipStream_t s, const FewDesc &d);

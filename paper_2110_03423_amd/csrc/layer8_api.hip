@@ -25,21 +25,27 @@ bool element_aligned(const void *p, int64_t size) { return ((uintptr_t)p & (uint
 // Sizes that the kernels index: rows of up to 2^23 elements (32-bit offsets inside a tile of rows), 2^31 rows.
 constexpr int64_t kMaxLd = (int64_t)1 << 23, kMaxTokens = (int64_t)1 << 22;
 
+// Sums over ranges of k times ranks up to which the product of a few tokens takes them as they are (eight pieces of 32 for each of its
+// wavefronts); beyond, a launch that joins them first is less.
+constexpr int64_t kFewUnjoined = 2048;
+
 struct Take {
   size_t off = 0;
   size_t operator()(size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; }
 };
 
-// codes of X, their scales, the sums with Vt, parts of sums
-struct ProductLayout { size_t codes, scale, t, partial, partial_bytes, total; int64_t width; };
+// codes of X, their scales, the sums with Vt before and after they are joined, parts of sums
+struct ProductLayout { size_t codes, scale, sums, t, partial, partial_bytes, total; int64_t width; int splits; };
 
-ProductLayout product_layout(const rsvd_ctx *ctx, int64_t tokens, int64_t n, int64_t m, int64_t r) {
+ProductLayout product_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int64_t r) {
   ProductLayout L;
   Take take;
   L.width = (int64_t)align_up((size_t)n, 128);
   L.codes = take((size_t)tokens * L.width);
   L.scale = take((size_t)tokens * 4);
-  L.t = take(r > 0 ? (size_t)tokens * rank_places(r) * 4 : 0);
+  L.splits = r > 0 ? lowrank_splits(ctx, tokens, n, r) : 0;
+  L.sums = take((size_t)L.splits * tokens * rank_places(r) * 4);
+  L.t = take((size_t)tokens * rank_places(r) * 2 * lowrank_parts(type));
   L.partial_bytes = tokens > kFewTokens ? nt_partial_bytes(ctx, tokens, m, L.width / 128, r > 0) : 0;
   L.partial = take(L.partial_bytes);
   L.total = take.off;
@@ -47,7 +53,7 @@ ProductLayout product_layout(const rsvd_ctx *ctx, int64_t tokens, int64_t n, int
 }
 
 // planes of dY, the codes transposed, the sums with Ut, parts of sums
-struct GradLayout { size_t a, b, t, partial, partial_bytes, total; int64_t width; int planes; };
+struct GradLayout { size_t a, b, sums, t, partial, partial_bytes, total; int64_t width; int planes, splits; };
 
 GradLayout product_grad_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int64_t r) {
   GradLayout L;
@@ -56,7 +62,9 @@ GradLayout product_grad_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t tok
   L.width = (int64_t)align_up((size_t)m, 64);
   L.a = take((size_t)L.planes * tokens * L.width * 2);
   L.b = take((size_t)n * L.width * 2);
-  L.t = take(r > 0 ? (size_t)tokens * rank_places(r) * 4 : 0);
+  L.splits = r > 0 ? lowrank_splits(ctx, tokens, m, r) : 0;
+  L.sums = take((size_t)L.splits * tokens * rank_places(r) * 4);
+  L.t = take((size_t)tokens * rank_places(r) * 2 * lowrank_parts(type));
   L.partial_bytes = nt_partial_bytes(ctx, tokens, n, L.width / 64 * L.planes, r > 0);
   L.partial = take(L.partial_bytes);
   L.total = take.off;
@@ -71,7 +79,9 @@ GradLayout keep8_grad_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t token
   L.width = (int64_t)align_up((size_t)tokens, 64);
   L.a = take((size_t)L.planes * m * L.width * 2);
   L.b = take((size_t)n * L.width * 2);
-  L.t = take((size_t)(L.width / 64) * m * 4);
+  L.sums = take((size_t)(L.width / 64) * m * 4);
+  L.t = L.sums;
+  L.splits = 0;
   L.partial_bytes = tokens > 0 ? nt_partial_bytes(ctx, m, n, L.width / 64 * L.planes, false) : 0;
   L.partial = take(L.partial_bytes);
   L.total = take.off;
@@ -119,7 +129,7 @@ int rsvd_q8_product_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_
   if (const int rc = check_sizes(type, tokens, n, m, r, 2)) return rc;
   if (bytes == nullptr) return -7;
   if (!sizes_supported(tokens, n, m, r)) return RSVD_ERR_UNSUPPORTED;
-  *bytes = tokens > 0 ? product_layout(ctx, tokens, n, m, r).total : 0;
+  *bytes = tokens > 0 ? product_layout(ctx, type, tokens, n, m, r).total : 0;
   return RSVD_OK;
 }
 
@@ -161,7 +171,7 @@ int rsvd_q8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
   if (Y == nullptr || !element_aligned(Y, es)) return -18;
   if (ldy < m) return -19;
   if (!sizes_supported(tokens, n, m, r) || ldq > kMaxLd) return RSVD_ERR_UNSUPPORTED;
-  const ProductLayout L = product_layout(ctx, tokens, n, m, r);
+  const ProductLayout L = product_layout(ctx, type, tokens, n, m, r);
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0) return -20;
   if (workspace_bytes < L.total) return -21;
   if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
@@ -170,18 +180,27 @@ int rsvd_q8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
   int8_t *q = (int8_t *)(ws + L.codes);
   float *rs = (float *)(ws + L.scale);
   uint16_t *t = (uint16_t *)(ws + L.t);
+  float *sums = r > 0 ? (float *)(ws + L.sums) : nullptr;
+  const int parts = lowrank_parts(type);
+  const bool few = tokens <= kFewTokens, unjoined = few && L.splits * rank_places(r) <= kFewUnjoined;
   {
     ProfScope ps(ctx, s, PK_SMALL);
-    RSVD_TRY(rows8_launch(s, type, tokens, n, X, ldx, q, L.width, L.width, rs), "rows to 8 bits");
-    if (r > 0) RSVD_TRY(lowrank_launch(s, type, tokens, n, r, X, ldx, Vt, ldvt, t), "low-rank term");
+    if (few) {
+      RSVD_TRY(front_launch(ctx, s, type, tokens, n, r, X, ldx, Vt, ldvt, sums, q, L.width, L.width, rs), "rows to 8 bits, low-rank term");
+      if (r > 0 && !unjoined) RSVD_TRY(lowrank_join_launch(s, sums, L.splits, tokens, r, parts, t), "low-rank term");
+    } else {
+      if (r > 0) RSVD_TRY(lowrank_launch(ctx, s, type, tokens, n, r, X, ldx, Vt, ldvt, sums), "low-rank term");
+      RSVD_TRY(rows8_launch(s, type, tokens, n, X, ldx, q, L.width, L.width, rs, sums, L.splits, r, parts, t), "rows to 8 bits");
+    }
   }
   Layer8Out o;
   o.rs = rs; o.cs = scale; o.bias = bias;
-  o.t = t; o.G = (const uint16_t *)U; o.ldg = ldu; o.r = (int)r;
+  o.t = t; o.parts = parts; o.G = (const uint16_t *)U; o.ldg = ldu; o.r = (int)r;
   o.C = Y; o.ldc = ldy; o.type = type;
   ProfScope ps(ctx, s, PK_GEMM_AX);
-  if (tokens <= kFewTokens) {
+  if (few) {
     FewDesc d;
+    d.sums = unjoined ? sums : nullptr; d.splits = L.splits;
     d.M = tokens; d.N = m; d.k = L.width;
     d.A = q; d.lda = L.width; d.B = codes; d.ldb = ldq;
     d.out = o;
@@ -230,13 +249,17 @@ int rsvd_q8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t t
     ProfScope ps(ctx, s, PK_SMALL);
     RSVD_TRY(split_rows_launch(s, type, tokens, m, dY, lddy, single ? nullptr : scale, a, L.width), "parts of the gradient");
     RSVD_TRY(transpose_codes_launch(s, m, n, codes, ldq, single ? scale : nullptr, b, L.width), "codes by columns");
-    if (r > 0) RSVD_TRY(lowrank_launch(s, type, tokens, m, r, dY, lddy, Ut, ldut, t), "low-rank term");
+    if (r > 0) {
+      float *sums = (float *)(ws + L.sums);
+      RSVD_TRY(lowrank_launch(ctx, s, type, tokens, m, r, dY, lddy, Ut, ldut, sums), "low-rank term");
+      RSVD_TRY(lowrank_join_launch(s, sums, L.splits, tokens, r, lowrank_parts(type), t), "low-rank term");
+    }
   }
   NtDesc d;
   d.M = tokens; d.N = n; d.ktiles = L.width / 64;
   d.A = a; d.lda = L.width * 2; d.planes = L.planes; d.plane = tokens * L.width * 2;
   d.B = b; d.ldb = L.width * 2; d.b_bytes = L.width * 2;
-  d.out.t = t; d.out.G = (const uint16_t *)V; d.out.ldg = ldv; d.out.r = (int)r;
+  d.out.t = t; d.out.parts = lowrank_parts(type); d.out.G = (const uint16_t *)V; d.out.ldg = ldv; d.out.r = (int)r;
   d.out.C = dX; d.out.ldc = lddx; d.out.type = type;
   d.partial = (float *)(ws + L.partial); d.partial_bytes = L.partial_bytes;
   ProfScope ps(ctx, s, PK_GEMM_ATX);
@@ -316,7 +339,7 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
   if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
   char *ws = (char *)workspace;
   uint16_t *a = (uint16_t *)(ws + L.a), *b = (uint16_t *)(ws + L.b);
-  float *sums = (float *)(ws + L.t);
+  float *sums = (float *)(ws + L.sums);
   {
     ProfScope ps(ctx, s, PK_SMALL);
     RSVD_TRY(transpose_split_launch(s, type, tokens, m, dY, lddy, a, L.width, db != nullptr ? sums : nullptr), "parts of the gradient");

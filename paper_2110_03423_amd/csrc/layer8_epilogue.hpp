@@ -19,10 +19,10 @@ struct Layer8Epilogue {
   const float *rs, *cs, *bias;
   const uint16_t *t, *G;
   int64_t ldg;
-  int r, rp, g_vec;
+  int r, rp, parts;
   void *C;
   int64_t ldc;
-  int type, c_vec, accumulate;
+  int type, accumulate;
 };
 
 inline Layer8Epilogue layer8_epilogue(const Layer8Out &o) {
@@ -30,26 +30,13 @@ inline Layer8Epilogue layer8_epilogue(const Layer8Out &o) {
   e.rs = o.rs; e.cs = o.cs; e.bias = o.bias;
   e.t = o.t; e.G = o.G; e.ldg = o.ldg;
   e.r = o.r; e.rp = (int)rank_places(o.r);
-  e.g_vec = rows_aligned(o.G, o.ldg, 2) && o.r % 8 == 0 ? 1 : 0;
+  e.parts = o.parts;
   e.C = o.C; e.ldc = o.ldc; e.type = o.type; e.accumulate = o.accumulate;
-  const int64_t size = o.type == RSVD_X_F32 ? 4 : 2;
-  e.c_vec = (uintptr_t)o.C % (4 * size) == 0 && o.ldc % 4 == 0 ? 1 : 0;
   return e;
 }
 
 // Eight bf16 numbers of row i of G from p on, zeros from r on.
-__device__ __forceinline__ u32x4 factor8(const Layer8Epilogue &E, int64_t i, int p) {
-  const uint16_t *g = E.G + i * E.ldg + p;
-  u32x4 out = {0u, 0u, 0u, 0u};
-  if (E.g_vec && p < E.r) {
-    out = *reinterpret_cast<const u32x4 *>(g);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (p + e < E.r) out[e >> 1] |= (unsigned)g[e] << (16 * (e & 1));
-  }
-  return out;
-}
+__device__ __forceinline__ u32x4 factor8(const Layer8Epilogue &E, int64_t i, int p) { return halves8(E.G + i * E.ldg + p, E.r - p); }
 
 // Four values for the columns from n on; `other` where there are none.
 __device__ __forceinline__ f32x4 column4(const float *p, int64_t n, int64_t N, float other) {
@@ -65,12 +52,12 @@ __device__ __forceinline__ f32x4 column4(const float *p, int64_t n, int64_t N, f
 // Four consecutive results of row m from column n on, of which those before column N exist.
 __device__ __forceinline__ void store4(const Layer8Epilogue &E, int64_t m, int64_t n, int64_t N, f32x4 v) {
   const int64_t at = m * E.ldc + n;
-  const bool whole = E.c_vec && n + 4 <= N;
+  const bool whole = n + 4 <= N;
   if (E.type == RSVD_X_F32) {
     float *c = reinterpret_cast<float *>(E.C) + at;
     if (whole) {
-      if (E.accumulate) v += *reinterpret_cast<const f32x4 *>(c);
-      *reinterpret_cast<f32x4 *>(c) = v;
+      if (E.accumulate) v += *reinterpret_cast<const f32x4_any *>(c);
+      *reinterpret_cast<f32x4_any *>(c) = v;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)
@@ -87,7 +74,7 @@ __device__ __forceinline__ void store4(const Layer8Epilogue &E, int64_t m, int64
     }
     uint16_t *c = reinterpret_cast<uint16_t *>(E.C) + at;
     if (whole) {
-      *reinterpret_cast<u32x2 *>(c) = p;
+      *reinterpret_cast<u32x2_any *>(c) = p;
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e)

@@ -151,7 +151,6 @@ __global__ __launch_bounds__(64 * WGM * WGN, PERSIMD) void nt_kernel(const NtPar
     W.C = P.partial + (int64_t)plane * P.M * P.N;
     W.ldc = P.N;
     W.type = RSVD_X_F32;
-    W.c_vec = P.N % 4 == 0;
     W.accumulate = 0;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -186,8 +185,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, PERSIMD) void nt_kernel(const NtPar
         for (int v = 0; v < 4; ++v) val[i][j][v] = (float)acc[i][j][v] * rs[i] * cs[v];
     }
   }
-  for (int p = 0; p < 2 * E.rp; p += 32) {
-    const int pr = (p < E.rp ? p : p - E.rp) + 8 * kq;
+  for (int p = 0, pr = 8 * kq; p < E.parts * E.rp; p += 32, pr = pr + 32 < E.rp ? pr + 32 : 8 * kq) {
     u32x4 a[TM], b[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
@@ -197,7 +195,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, PERSIMD) void nt_kernel(const NtPar
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int64_t m = m0 + wm0 + i * 16 + r16;
-      a[i] = *reinterpret_cast<const u32x4 *>(E.t + (m < P.M ? m : P.M - 1) * 2 * E.rp + p + 8 * kq);
+      a[i] = *reinterpret_cast<const u32x4 *>(E.t + (m < P.M ? m : P.M - 1) * E.parts * E.rp + p + 8 * kq);
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -232,8 +230,8 @@ __global__ __launch_bounds__(256) void nt_reduce_kernel(const float *__restrict_
       typedef decltype(zero) vec;
       vec v = zero;
       const float *p = partial + ((int64_t)s * M + m) * N + n;
-      if (N % 4 == 0) {
-        v = *reinterpret_cast<const vec *>(p);
+      if (n + 4 <= N) {
+        v = __builtin_bit_cast(vec, *reinterpret_cast<const f32x4_any *>(p));
       } else {
 #pragma unroll
         for (int u = 0; u < 4; ++u)

@@ -1,99 +1,26 @@
 // Numbers to 8 bits and back, and the operand planes of the bf16 products of the layer operators.
-#include "layer8.hpp"
+#include "layer8_rows.hpp"
 
 namespace rsvd {
 
-__device__ __forceinline__ unsigned magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
-
-// Eight integers in [-127, 127], given as floats, as bytes.
-__device__ __forceinline__ u32x2 pack8(const float (&q)[8]) {
-  u32x2 w;
-#pragma unroll
-  for (int h = 0; h < 2; ++h)
-    w[h] = ((unsigned)(int)q[4 * h] & 255u) | (((unsigned)(int)q[4 * h + 1] & 255u) << 8) | (((unsigned)(int)q[4 * h + 2] & 255u) << 16) |
-           ((unsigned)(int)q[4 * h + 3] << 24);
-  return w;
-}
-
 // ---------------------------------------------------------------- rows with a scale each
-// One workgroup per row.  The largest magnitude is found among the bit patterns (as integers they are ordered like the
-// magnitudes, infinity and NaN on top).  CH chunks of 8 elements stay in a thread's registers between the maximum and
-// the codes; CH = 0: longer rows are read twice.
-template <int XT, int CH>
-__global__ __launch_bounds__(256) void rows8_kernel(const char *__restrict__ X, int64_t ldx, int n, int8_t *__restrict__ codes,
-                                                    int64_t ldq, int width, float *__restrict__ scale, int vec) {
-  __shared__ unsigned part[4];
-  const int tid = threadIdx.x;
-  const int64_t row = blockIdx.x;
-  const char *x = X + row * ldx * XTraits<XT>::SIZE;
-  const int chunks = (width + 7) / 8;
-  float v[CH > 0 ? CH : 1][8];
-  unsigned top = 0u;
-  if constexpr (CH > 0) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int j = 8 * (tid + 256 * c);
-      x_load8<XT>(x + (int64_t)j * XTraits<XT>::SIZE, n - j, vec != 0, v[c]);
-    }
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[c][e]));
-  } else {
-    for (int c = tid; c < chunks; c += 256) {
-      x_load8<XT>(x + (int64_t)8 * c * XTraits<XT>::SIZE, n - 8 * c, vec != 0, v[0]);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[0][e]));
-    }
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) top = max(top, (unsigned)__shfl_xor((int)top, d));
-  if ((tid & 63) == 0) part[tid >> 6] = top;
-  __syncthreads();
-  top = max(max(part[0], part[1]), max(part[2], part[3]));
-  const float a = __uint_as_float(top);
-  const bool bad = top >= 0x7f800000u, none = bad || a < 0x1p-116f;
-  const float per = none ? 0.f : 127.f / a;
-  if (tid == 0) scale[row] = bad ? __uint_as_float(0x7fc00000u) : none ? 0.f : a / 127.f;
-  auto store = [&](int c, const float (&w)[8]) RSVD_INLINE {
-    float q[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) q[e] = none ? 0.f : __builtin_rintf(w[e] * per);
-    *reinterpret_cast<u32x2 *>(codes + row * ldq + 8 * c) = pack8(q);
-  };
-  if constexpr (CH > 0) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-      if (tid + 256 * c < chunks) store(tid + 256 * c, v[c]);
-  } else {
-    for (int c = tid; c < chunks; c += 256) {
-      x_load8<XT>(x + (int64_t)8 * c * XTraits<XT>::SIZE, n - 8 * c, vec != 0, v[0]);
-      store(c, v[0]);
-    }
-  }
-}
+template <int XT, int CH> __global__ __launch_bounds__(256) void rows8_kernel(const Rows8Params P) { rows8_row<XT, CH>(P, blockIdx.x); }
 
-template <int XT>
-static void rows8_typed(hipStream_t s, int64_t rows, int64_t n, const void *X, int64_t ldx, int8_t *codes, int64_t ldq, int64_t width,
-                        float *scale) {
-  const int vec = rows_aligned(X, ldx, XTraits<XT>::SIZE) ? 1 : 0;
-  const int64_t chunks = ceil_div(width, 8);
-#define ROWS8(CH)                                                                                                                     \
-  hipLaunchKernelGGL((rows8_kernel<XT, CH>), dim3((unsigned)rows), dim3(256), 0, s, (const char *)X, ldx, (int)n, codes, ldq, (int)width, \
-                     scale, vec)
-  if (chunks <= 256) ROWS8(1);
-  else if (chunks <= 512) ROWS8(2);
-  else if (chunks <= 1024) ROWS8(4);
-  else if (chunks <= 2048) ROWS8(8);
-  else ROWS8(0);
-#undef ROWS8
+template <int XT> static void rows8_typed(hipStream_t s, const Rows8Params &P) {
+  const int64_t chunks = ceil_div(P.width, 8);
+  const dim3 grid((unsigned)P.rows);
+  if (chunks <= 256) hipLaunchKernelGGL((rows8_kernel<XT, 1>), grid, dim3(256), 0, s, P);
+  else if (chunks <= 512) hipLaunchKernelGGL((rows8_kernel<XT, 2>), grid, dim3(256), 0, s, P);
+  else if (chunks <= 1024) hipLaunchKernelGGL((rows8_kernel<XT, 4>), grid, dim3(256), 0, s, P);
+  else hipLaunchKernelGGL((rows8_kernel<XT, 8>), grid, dim3(256), 0, s, P);
 }
 
 hipError_t rows8_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, int8_t *codes, int64_t ldq,
-                        int64_t width, float *scale) {
-  if (type == RSVD_X_BF16) rows8_typed<RSVD_X_BF16>(s, rows, n, X, ldx, codes, ldq, width, scale);
-  else if (type == RSVD_X_F16) rows8_typed<RSVD_X_F16>(s, rows, n, X, ldx, codes, ldq, width, scale);
-  else rows8_typed<RSVD_X_F32>(s, rows, n, X, ldx, codes, ldq, width, scale);
+                        int64_t width, float *scale, const float *sums, int splits, int64_t r, int parts, uint16_t *t) {
+  const Rows8Params P = {(const char *)X, ldx, rows, (int)n, codes, ldq, (int)width, scale, sums, splits, (int)rank_places(r), parts, t};
+  if (type == RSVD_X_BF16) rows8_typed<RSVD_X_BF16>(s, P);
+  else if (type == RSVD_X_F16) rows8_typed<RSVD_X_F16>(s, P);
+  else rows8_typed<RSVD_X_F32>(s, P);
   return hipGetLastError();
 }
 
@@ -107,13 +34,13 @@ __device__ __forceinline__ unsigned quad_max(unsigned x) {
 template <int XT>
 __global__ __launch_bounds__(256) void keep8_save_kernel(const char *__restrict__ X, int64_t ldx, int64_t tokens, int n,
                                                          int8_t *__restrict__ codes, int64_t ldc, uint8_t *__restrict__ powers, int64_t ldp,
-                                                         int shift, int vec) {
+                                                         int shift) {
   const int c = (int)(blockIdx.x << shift) + (int)(threadIdx.x & ((1u << shift) - 1u));
   const int rows = 256 >> shift;
   if ((c >> 2) * 32 >= n) return;                       // (whole blocks only: the quads stay together)
   for (int64_t t = (int64_t)blockIdx.y * rows + (threadIdx.x >> shift); t < tokens; t += (int64_t)gridDim.y * rows) {
     float v[8], q[8];
-    x_load8<XT>(X + (t * ldx + 8 * c) * XTraits<XT>::SIZE, n - 8 * c, vec != 0, v);
+    x_load8<XT>(X + (t * ldx + 8 * c) * XTraits<XT>::SIZE, n - 8 * c, v);
     unsigned top = 0u;
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = max(top, magnitude(v[e]));
@@ -138,8 +65,7 @@ __device__ __forceinline__ float kept_unit(unsigned b) { return b == 255u ? __ui
 
 template <int XT>
 __global__ __launch_bounds__(256) void keep8_load_kernel(const int8_t *__restrict__ codes, int64_t ldc, const uint8_t *__restrict__ powers,
-                                                         int64_t ldp, int64_t tokens, int n, char *__restrict__ X, int64_t ldx, int shift,
-                                                         int vec) {
+                                                         int64_t ldp, int64_t tokens, int n, char *__restrict__ X, int64_t ldx, int shift) {
   const int c = (int)(blockIdx.x << shift) + (int)(threadIdx.x & ((1u << shift) - 1u));
   const int rows = 256 >> shift;
   if (8 * c >= n) return;
@@ -151,9 +77,9 @@ __global__ __launch_bounds__(256) void keep8_load_kernel(const int8_t *__restric
     for (int e = 0; e < 8; ++e) v[e] = (float)((int)(w[e >> 2] << (24 - 8 * (e & 3))) >> 24) * unit;
     char *x = X + (t * ldx + 8 * c) * XTraits<XT>::SIZE;
     if constexpr (XT == RSVD_X_F32) {
-      if (vec && n - 8 * c >= 8) {
-        reinterpret_cast<f32x4 *>(x)[0] = f32x4{v[0], v[1], v[2], v[3]};
-        reinterpret_cast<f32x4 *>(x)[1] = f32x4{v[4], v[5], v[6], v[7]};
+      if (n - 8 * c >= 8) {
+        reinterpret_cast<f32x4_any *>(x)[0] = f32x4{v[0], v[1], v[2], v[3]};
+        reinterpret_cast<f32x4_any *>(x)[1] = f32x4{v[4], v[5], v[6], v[7]};
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -166,8 +92,8 @@ __global__ __launch_bounds__(256) void keep8_load_kernel(const int8_t *__restric
         if constexpr (XT == RSVD_X_BF16) p[e] = bf16_pair(v[2 * e], v[2 * e + 1]);
         else p[e] = __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{v[2 * e], v[2 * e + 1]}, f16x2));
       }
-      if (vec && n - 8 * c >= 8) {
-        *reinterpret_cast<u32x4 *>(x) = p;
+      if (n - 8 * c >= 8) {
+        *reinterpret_cast<u32x4_any *>(x) = p;
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -191,9 +117,8 @@ hipError_t keep8_save_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int
                              int64_t ldc, uint8_t *powers, int64_t ldp) {
   int shift;
   const dim3 grid = keep8_grid(tokens, n, shift);
-  const int vec = rows_aligned(X, ldx, xtype_size(type)) ? 1 : 0;
 #define SAVE(XT)                                                                                                                        \
-  hipLaunchKernelGGL(keep8_save_kernel<XT>, grid, dim3(256), 0, s, (const char *)X, ldx, tokens, (int)n, codes, ldc, powers, ldp, shift, vec)
+  hipLaunchKernelGGL(keep8_save_kernel<XT>, grid, dim3(256), 0, s, (const char *)X, ldx, tokens, (int)n, codes, ldc, powers, ldp, shift)
   if (type == RSVD_X_BF16) SAVE(RSVD_X_BF16);
   else if (type == RSVD_X_F16) SAVE(RSVD_X_F16);
   else SAVE(RSVD_X_F32);
@@ -205,9 +130,8 @@ hipError_t keep8_load_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int
                              const uint8_t *powers, int64_t ldp, void *X, int64_t ldx) {
   int shift;
   const dim3 grid = keep8_grid(tokens, n, shift);
-  const int vec = rows_aligned(X, ldx, xtype_size(type)) ? 1 : 0;
 #define LOAD(XT)                                                                                                                    \
-  hipLaunchKernelGGL(keep8_load_kernel<XT>, grid, dim3(256), 0, s, codes, ldc, powers, ldp, tokens, (int)n, (char *)X, ldx, shift, vec)
+  hipLaunchKernelGGL(keep8_load_kernel<XT>, grid, dim3(256), 0, s, codes, ldc, powers, ldp, tokens, (int)n, (char *)X, ldx, shift)
   if (type == RSVD_X_BF16) LOAD(RSVD_X_BF16);
   else if (type == RSVD_X_F16) LOAD(RSVD_X_F16);
   else LOAD(RSVD_X_F32);
@@ -218,12 +142,12 @@ hipError_t keep8_load_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int
 // ---------------------------------------------------------------- operand planes
 template <int XT>
 __global__ __launch_bounds__(256) void split_rows_kernel(const char *__restrict__ X, int64_t ldx, int64_t n, const float *__restrict__ factor,
-                                                         uint16_t *__restrict__ planes, int64_t width, int64_t plane, int vec) {
+                                                         uint16_t *__restrict__ planes, int64_t width, int64_t plane) {
   constexpr int P = XTraits<XT>::PARTS;
   const int64_t j = 8 * ((int64_t)blockIdx.x * 256 + threadIdx.x), row = blockIdx.y + (int64_t)blockIdx.z * 65535;
   if (j >= width || row * width >= plane) return;
   float v[8];
-  x_load8<XT>(X + (row * ldx + j) * XTraits<XT>::SIZE, n - j, vec != 0, v);
+  x_load8<XT>(X + (row * ldx + j) * XTraits<XT>::SIZE, n - j, v);
   if (factor != nullptr) {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -243,10 +167,9 @@ __global__ __launch_bounds__(256) void split_rows_kernel(const char *__restrict_
 
 hipError_t split_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, const float *factor,
                              uint16_t *planes, int64_t width) {
-  const int vec = rows_aligned(X, ldx, xtype_size(type)) ? 1 : 0;
   const dim3 grid((unsigned)ceil_div(width, 2048), (unsigned)(rows < 65535 ? rows : 65535), (unsigned)ceil_div(rows, 65535));
 #define SPLIT(XT) \
-  hipLaunchKernelGGL(split_rows_kernel<XT>, grid, dim3(256), 0, s, (const char *)X, ldx, n, factor, planes, width, rows * width, vec)
+  hipLaunchKernelGGL(split_rows_kernel<XT>, grid, dim3(256), 0, s, (const char *)X, ldx, n, factor, planes, width, rows * width)
   if (type == RSVD_X_BF16) SPLIT(RSVD_X_BF16);
   else if (type == RSVD_X_F16) SPLIT(RSVD_X_F16);
   else SPLIT(RSVD_X_F32);
@@ -267,7 +190,6 @@ struct TransposeParams {
   const uint8_t *powers; int64_t ldp;
   uint16_t *planes; int64_t width, plane;
   float *sums;
-  int vec;
 };
 
 template <int SRC> __global__ __launch_bounds__(256) void transpose_kernel(const TransposeParams P) {
@@ -284,7 +206,7 @@ template <int SRC> __global__ __launch_bounds__(256) void transpose_kernel(const
       float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (row < P.rows && col < P.n) {
         if constexpr (SRC < kFromCodes) {
-          x_load8<SRC>(P.X + (row * P.ldx + col) * XTraits<SRC>::SIZE, P.n - col, P.vec != 0, v);
+          x_load8<SRC>(P.X + (row * P.ldx + col) * XTraits<SRC>::SIZE, P.n - col, v);
         } else {
           const u32x2 w = *reinterpret_cast<const u32x2 *>(P.X + row * P.ldx + col);
           const float unit = SRC == kFromKept ? kept_unit(P.powers[row * P.ldp + (col >> 5)]) : P.factor != nullptr ? P.factor[row] : 1.f;
@@ -338,8 +260,7 @@ static dim3 transpose_grid(int64_t rows, int64_t n) { return dim3((unsigned)ceil
 
 hipError_t transpose_split_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint16_t *planes,
                                   int64_t width, float *sums) {
-  const TransposeParams P = {(const char *)X, ldx, rows, n, nullptr, nullptr, 0, planes, width, n * width, sums,
-                             rows_aligned(X, ldx, xtype_size(type)) ? 1 : 0};
+  const TransposeParams P = {(const char *)X, ldx, rows, n, nullptr, nullptr, 0, planes, width, n * width, sums};
   const dim3 grid = transpose_grid(rows, n);
   if (type == RSVD_X_BF16) hipLaunchKernelGGL(transpose_kernel<RSVD_X_BF16>, grid, dim3(256), 0, s, P);
   else if (type == RSVD_X_F16) hipLaunchKernelGGL(transpose_kernel<RSVD_X_F16>, grid, dim3(256), 0, s, P);
@@ -349,14 +270,14 @@ hipError_t transpose_split_launch(hipStream_t s, rsvd_xtype type, int64_t rows, 
 
 hipError_t transpose_codes_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldq, const float *factor,
                                   uint16_t *plane, int64_t width) {
-  const TransposeParams P = {(const char *)codes, ldq, rows, n, factor, nullptr, 0, plane, width, n * width, nullptr, 1};
+  const TransposeParams P = {(const char *)codes, ldq, rows, n, factor, nullptr, 0, plane, width, n * width, nullptr};
   hipLaunchKernelGGL(transpose_kernel<kFromCodes>, transpose_grid(rows, n), dim3(256), 0, s, P);
   return hipGetLastError();
 }
 
 hipError_t transpose_kept_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp,
                                  uint16_t *plane, int64_t width) {
-  const TransposeParams P = {(const char *)codes, ldc, rows, n, nullptr, powers, ldp, plane, width, n * width, nullptr, 1};
+  const TransposeParams P = {(const char *)codes, ldc, rows, n, nullptr, powers, ldp, plane, width, n * width, nullptr};
   hipLaunchKernelGGL(transpose_kernel<kFromKept>, transpose_grid(rows, n), dim3(256), 0, s, P);
   return hipGetLastError();
 }

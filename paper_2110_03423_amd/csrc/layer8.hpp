@@ -168,15 +168,12 @@ hipError_t keep8_load_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int
 // planes[p][row][0 .. width): the bf16 parts of X_rj factor_j (factor NULL: of X_rj), zeros from n on.
 hipError_t split_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, const float *factor,
                              uint16_t *planes, int64_t width);
-// planes[p][j][0 .. width): the bf16 parts of X_rj at place r, zeros from `rows` on.  sums != NULL: sums[b][j] is the sum of column j over
-// the 64 rows from 64 b on.
-hipError_t transpose_split_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint16_t *planes,
-                                  int64_t width, float *sums);
-// plane[j][0 .. width): codes_rj factor_r (factor NULL: codes_rj) as bf16 at place r, zeros from `rows` on.
-hipError_t transpose_codes_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldq, const float *factor,
-                                  uint16_t *plane, int64_t width);
-hipError_t transpose_kept_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers,
-                                 int64_t ldp, uint16_t *plane, int64_t width);
+// plane[row][0 .. width): the codes of a row as bf16 numbers, multiplied by factor_row (NULL: as they are), or by the powers of two of kept
+// activations; width >= n, a multiple of 8.
+hipError_t widen_codes_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldq, const float *factor, uint16_t *plane,
+                              int64_t width);
+hipError_t widen_kept_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp,
+                             uint16_t *plane, int64_t width);
 // out[j] (+)= sum over b of sums[b][j]
 hipError_t add_sums_launch(hipStream_t s, int64_t blocks, int64_t n, const float *sums, float *out, int accumulate);
 hipError_t fill_zero_launch(hipStream_t s, int64_t rows, int64_t cols, float *out, int64_t ld);
@@ -206,21 +203,36 @@ struct Layer8Out {
 };
 
 // ---------------------------------------------------------------- layer8_gemm.hip
-// C (M x N) out of sums over k of A (M rows) and B (N rows), both with consecutive k, in k-tiles of 128 bytes: 128 8-bit codes or 64 bf16
-// numbers.  Both start at 16-byte addresses and have row lengths of a multiple of 16 bytes.
+// C (M x N) out of the integer sums over k of codes A (M rows) and B (N rows), both with consecutive k, in k-tiles of 128.  Both start at 16-byte
+// addresses and have row lengths of a multiple of 16 bytes.
 struct NtDesc {
-  bool codes = false;                    // 8-bit codes, summed as integers; else bf16
   int64_t M = 0, N = 0;
   int64_t ktiles = 0;                    // every row of A has that many whole k-tiles, zeros behind the last k
-  const void *A = nullptr; int64_t lda = 0;      // bytes
-  int planes = 1; int64_t plane = 0;     // A is a sum of `planes` matrices, `plane` bytes apart (the largest first)
-  const void *B = nullptr; int64_t ldb = 0;      // bytes
-  int64_t b_bytes = 0;                   // bytes of a row of B that may be read (a multiple of 16); finite
+  const int8_t *A = nullptr; int64_t lda = 0;
+  const int8_t *B = nullptr; int64_t ldb = 0;
+  int64_t b_bytes = 0;                   // bytes of a row of B that may be read (a multiple of 16)
   Layer8Out out;
-  float *partial = nullptr; size_t partial_bytes = 0;      // for sums over k in several parts
+  float *partial = nullptr; size_t partial_bytes = 0;      // for sums over k in several ranges
 };
-size_t nt_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t ktiles, bool lowrank);      // ktiles of all planes
+size_t nt_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t ktiles, bool lowrank);
 hipError_t nt_launch(rsvd_ctx *ctx, hipStream_t s, const NtDesc &d);
+
+// ---------------------------------------------------------------- layer8_grad.hip
+// C (M x N) = sum over k < K of A_mk B_kn of bf16 numbers, A a sum of `planes` matrices (`plane` bytes apart, the largest first), B with rows of n.
+// a_krows: A is stored K x M, else M x K.  Rows of both may be read in 16-byte pieces as far as these hold an element.
+struct KnDesc {
+  int64_t M = 0, N = 0, K = 0;
+  bool a_krows = false;
+  const uint16_t *A = nullptr; int64_t lda = 0;            // bytes
+  int planes = 1; int64_t plane = 0;
+  const uint16_t *B = nullptr; int64_t ldb = 0;            // bytes
+  float *sums = nullptr;                                   // a_krows: receives kn_sum_rows() partial sums of A over k, M each; or NULL
+  Layer8Out out;
+  float *partial = nullptr; size_t partial_bytes = 0;
+};
+size_t kn_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, bool lowrank);
+int64_t kn_sum_rows(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes);
+hipError_t kn_launch(rsvd_ctx *ctx, hipStream_t s, const KnDesc &d);
 
 // ---------------------------------------------------------------- layer8_few.hip
 // The product of codes for up to kFewTokens tokens.

@@ -52,37 +52,43 @@ ProductLayout product_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t token
   return L;
 }
 
-// planes of dY, the codes transposed, the sums with Ut, parts of sums
-struct GradLayout { size_t a, b, sums, t, partial, partial_bytes, total; int64_t width; int planes, splits; };
+// Whether rows of bf16 numbers can be taken as they are by kn_launch (as a matrix M x K, or K x M): no byte is read that is not theirs.
+bool takes_rows(rsvd_xtype type, const void *p, int64_t cols, int64_t ld) {
+  return type == RSVD_X_BF16 && cols % 8 == 0 && rows_aligned(p, ld, 2) && ld <= kMaxLd / 4;
+}
+
+// planes of dY where it cannot be taken as it is, codes as bf16 numbers, low-rank sums before and after they are joined, or column sums of dY, parts of sums
+struct GradLayout { size_t a, b, sums, t, partial, partial_bytes, total; int64_t width, b_width; int planes, splits; };
 
 GradLayout product_grad_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int64_t r) {
   GradLayout L;
   Take take;
   L.planes = xtype_parts(type);
-  L.width = (int64_t)align_up((size_t)m, 64);
+  L.width = (int64_t)align_up((size_t)m, 8);
+  L.b_width = (int64_t)align_up((size_t)n, 8);
   L.a = take((size_t)L.planes * tokens * L.width * 2);
-  L.b = take((size_t)n * L.width * 2);
+  L.b = take((size_t)m * L.b_width * 2);
   L.splits = r > 0 ? lowrank_splits(ctx, tokens, m, r) : 0;
   L.sums = take((size_t)L.splits * tokens * rank_places(r) * 4);
   L.t = take((size_t)tokens * rank_places(r) * 2 * lowrank_parts(type));
-  L.partial_bytes = nt_partial_bytes(ctx, tokens, n, L.width / 64 * L.planes, r > 0);
+  L.partial_bytes = kn_partial_bytes(ctx, tokens, n, m, L.planes, r > 0);
   L.partial = take(L.partial_bytes);
   L.total = take.off;
   return L;
 }
 
-// planes of dY transposed, the kept activations transposed, column sums of dY, parts of sums
 GradLayout keep8_grad_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m) {
   GradLayout L;
   Take take;
   L.planes = xtype_parts(type);
-  L.width = (int64_t)align_up((size_t)tokens, 64);
-  L.a = take((size_t)L.planes * m * L.width * 2);
-  L.b = take((size_t)n * L.width * 2);
-  L.sums = take((size_t)(L.width / 64) * m * 4);
+  L.width = (int64_t)align_up((size_t)m, 8);
+  L.b_width = (int64_t)align_up((size_t)n, 8);
+  L.a = take((size_t)L.planes * tokens * L.width * 2);
+  L.b = take((size_t)tokens * L.b_width * 2);
+  L.sums = take((size_t)kn_sum_rows(ctx, m, n, tokens, L.planes) * m * 4);
   L.t = L.sums;
   L.splits = 0;
-  L.partial_bytes = tokens > 0 ? nt_partial_bytes(ctx, m, n, L.width / 64 * L.planes, false) : 0;
+  L.partial_bytes = kn_partial_bytes(ctx, m, n, tokens, L.planes, false);
   L.partial = take(L.partial_bytes);
   L.total = take.off;
   return L;
@@ -208,7 +214,6 @@ int rsvd_q8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
     return RSVD_OK;
   }
   NtDesc d;
-  d.codes = true;
   d.M = tokens; d.N = m; d.ktiles = L.width / 128;
   d.A = q; d.lda = L.width; d.B = codes; d.ldb = ldq; d.b_bytes = (int64_t)align_up((size_t)n, 16);
   d.out = o;
@@ -244,26 +249,26 @@ int rsvd_q8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t t
   char *ws = (char *)workspace;
   uint16_t *a = (uint16_t *)(ws + L.a), *b = (uint16_t *)(ws + L.b), *t = (uint16_t *)(ws + L.t);
   // one part: the scale goes to the codes; several: to dY before it is split, and the codes stay exact
-  const bool single = L.planes == 1;
+  const bool single = L.planes == 1, direct = takes_rows(type, dY, m, lddy);
   {
     ProfScope ps(ctx, s, PK_SMALL);
-    RSVD_TRY(split_rows_launch(s, type, tokens, m, dY, lddy, single ? nullptr : scale, a, L.width), "parts of the gradient");
-    RSVD_TRY(transpose_codes_launch(s, m, n, codes, ldq, single ? scale : nullptr, b, L.width), "codes by columns");
+    if (!direct) RSVD_TRY(split_rows_launch(s, type, tokens, m, dY, lddy, single ? nullptr : scale, a, L.width), "parts of the gradient");
+    RSVD_TRY(widen_codes_launch(s, m, n, codes, ldq, single ? scale : nullptr, b, L.b_width), "codes as bf16 numbers");
     if (r > 0) {
       float *sums = (float *)(ws + L.sums);
       RSVD_TRY(lowrank_launch(ctx, s, type, tokens, m, r, dY, lddy, Ut, ldut, sums), "low-rank term");
       RSVD_TRY(lowrank_join_launch(s, sums, L.splits, tokens, r, lowrank_parts(type), t), "low-rank term");
     }
   }
-  NtDesc d;
-  d.M = tokens; d.N = n; d.ktiles = L.width / 64;
-  d.A = a; d.lda = L.width * 2; d.planes = L.planes; d.plane = tokens * L.width * 2;
-  d.B = b; d.ldb = L.width * 2; d.b_bytes = L.width * 2;
+  KnDesc d;
+  d.M = tokens; d.N = n; d.K = m;
+  d.A = direct ? (const uint16_t *)dY : a; d.lda = (direct ? lddy : L.width) * 2; d.planes = L.planes; d.plane = tokens * L.width * 2;
+  d.B = b; d.ldb = L.b_width * 2;
   d.out.t = t; d.out.parts = lowrank_parts(type); d.out.G = (const uint16_t *)V; d.out.ldg = ldv; d.out.r = (int)r;
   d.out.C = dX; d.out.ldc = lddx; d.out.type = type;
   d.partial = (float *)(ws + L.partial); d.partial_bytes = L.partial_bytes;
   ProfScope ps(ctx, s, PK_GEMM_ATX);
-  RSVD_TRY(nt_launch(ctx, s, d), "gradient of a product of codes");
+  RSVD_TRY(kn_launch(ctx, s, d), "gradient of a product of codes");
   return RSVD_OK;
 }
 
@@ -339,21 +344,29 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
   if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
   char *ws = (char *)workspace;
   uint16_t *a = (uint16_t *)(ws + L.a), *b = (uint16_t *)(ws + L.b);
-  float *sums = (float *)(ws + L.sums);
+  float *sums = db != nullptr ? (float *)(ws + L.sums) : nullptr;
+  const bool direct = takes_rows(type, dY, m, lddy);
   {
     ProfScope ps(ctx, s, PK_SMALL);
-    RSVD_TRY(transpose_split_launch(s, type, tokens, m, dY, lddy, a, L.width, db != nullptr ? sums : nullptr), "parts of the gradient");
-    RSVD_TRY(transpose_kept_launch(s, tokens, n, codes, ldc, powers, ldp, b, L.width), "kept numbers by columns");
-    if (db != nullptr) RSVD_TRY(add_sums_launch(s, L.width / 64, m, sums, db, accumulate), "column sums");
+    if (!direct) RSVD_TRY(split_rows_launch(s, type, tokens, m, dY, lddy, nullptr, a, L.width), "parts of the gradient");
+    RSVD_TRY(widen_kept_launch(s, tokens, n, codes, ldc, powers, ldp, b, L.b_width), "kept numbers");
   }
-  NtDesc d;
-  d.M = m; d.N = n; d.ktiles = L.width / 64;
-  d.A = a; d.lda = L.width * 2; d.planes = L.planes; d.plane = m * L.width * 2;
-  d.B = b; d.ldb = L.width * 2; d.b_bytes = L.width * 2;
+  KnDesc d;
+  d.M = m; d.N = n; d.K = tokens;
+  d.a_krows = true;
+  d.A = direct ? (const uint16_t *)dY : a; d.lda = (direct ? lddy : L.width) * 2; d.planes = L.planes; d.plane = tokens * L.width * 2;
+  d.B = b; d.ldb = L.b_width * 2;
+  d.sums = sums;
   d.out.C = dW; d.out.ldc = lddw; d.out.type = RSVD_X_F32; d.out.accumulate = accumulate;
   d.partial = (float *)(ws + L.partial); d.partial_bytes = L.partial_bytes;
-  ProfScope ps(ctx, s, PK_GEMM_ATX);
-  RSVD_TRY(nt_launch(ctx, s, d), "gradient of a weight");
+  {
+    ProfScope ps(ctx, s, PK_GEMM_ATX);
+    RSVD_TRY(kn_launch(ctx, s, d), "gradient of a weight");
+  }
+  if (db != nullptr) {
+    ProfScope ps(ctx, s, PK_SMALL);
+    RSVD_TRY(add_sums_launch(s, kn_sum_rows(ctx, m, n, tokens, L.planes), m, sums, db, accumulate), "column sums");
+  }
   return RSVD_OK;
 }
 

@@ -38,13 +38,12 @@ inline Layer8Epilogue layer8_epilogue(const Layer8Out &o) {
 // Eight bf16 numbers of row i of G from p on, zeros from r on.
 __device__ __forceinline__ u32x4 factor8(const Layer8Epilogue &E, int64_t i, int p) { return halves8(E.G + i * E.ldg + p, E.r - p); }
 
-// Four values for the columns from n on; `other` where there are none.
-__device__ __forceinline__ f32x4 column4(const float *p, int64_t n, int64_t N, float other) {
-  f32x4 v = {other, other, other, other};
+// Four values for the columns from n on, for columns that do not exist those of the last one; `all` for p = NULL.
+__device__ __forceinline__ f32x4 column4(const float *p, int64_t n, int64_t N, float all) {
+  f32x4 v = {all, all, all, all};
   if (p != nullptr) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (n + e < N) v[e] = p[n + e];
+    for (int e = 0; e < 4; ++e) v[e] = p[n + e < N ? n + e : N - 1];
   }
   return v;
 }

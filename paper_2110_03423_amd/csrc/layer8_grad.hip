@@ -1,0 +1,274 @@
+// Products of bf16 numbers for gradients, C = sum over k of A_p[m][k] B[k][n], in the orders that the operands lie in memory.
+//
+// B runs along n from k to k, and so does A in the gradient of a weight, where k counts tokens.  Neither is transposed in memory:
+// tiles [k][x] of bf16 numbers in LDS are read with the transposing LDS load (sixteen lanes read four k of sixteen columns and get one column of
+// four k each).  LDS rows of such a tile have their 32-byte pieces exchanged by the low bits of k, so that the eight rows that half a wavefront
+// reads start at different banks; rows of consecutive k have their 16-byte pieces exchanged by the row.
+// Both operands go from memory to registers and from there to LDS, among the matrix instructions of the tile before, and a register is loaded for
+// the tile after next as soon as it has been written.  (Loads straight to LDS: the compiler lets the transposing loads wait for all of them,
+// wherever they go.)
+// Several planes of A are taken as further k, the smallest first.
+#include "layer8_tile.hpp"
+
+namespace rsvd {
+
+constexpr int kKnK = 64;                   // k of a k-tile
+
+struct KnParams {
+  const char *A; int64_t lda, plane;       // bytes
+  int planes, ktiles;                      // k-tiles of a plane
+  int64_t K;
+  const char *B; int64_t ldb;              // bytes
+  float *sums;                             // A_KROWS: sums of A over k by ranges, [split][tile_n][M], or NULL
+  TileParams T;
+};
+
+// Place of 32-byte piece c of row k of a [k][X] tile.
+template <int X> __device__ __forceinline__ int krow_piece(int c, int k) {
+  if (X >= 128) return c ^ ((k & 3) | ((k >> 1) & 4));
+  return c ^ (((k >> 1) & 1) | ((k >> 2) & 2));            // (two rows of 64 columns share 256 bytes)
+}
+
+// What one of NT threads stages of a k-tile of X rows (consecutive k) or columns (KROWS): N pieces of 16 bytes.
+template <int NT, int X, bool KROWS> struct Staged {
+  static constexpr int ROW = KROWS ? X * 2 : 128, PER = ROW / 16, STEP = NT / PER, N = X * 128 / 16 / NT;      // bytes of a row; pieces; rows between a thread's
+  static_assert(X * 128 % (16 * NT) == 0 && STEP % 8 == 0, "whole rounds; a thread's rows have their pieces exchanged alike, but for bit 3 of k");
+  u32x4 reg[N];
+  uint32_t off[N];
+  int pos, place;
+  // left: rows (columns) of the tile that exist; others are read as one that does, and not stored
+  __device__ __forceinline__ void init(int64_t ld, int64_t left, int tid) {
+    const int row = tid / PER, last = (int)(left < X ? left : X) - 1;
+    pos = tid % PER;
+    place = row * ROW + (KROWS ? (krow_piece<X>(pos >> 1, row) << 5) + ((pos & 1) << 4) : (pos ^ (row & 7)) << 4);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int r = row + STEP * i;
+      off[i] = KROWS ? (uint32_t)r * (uint32_t)ld + (8 * pos > last ? 0u : 16u * pos)
+                     : (uint32_t)(r < last ? r : last) * (uint32_t)ld + 16u * pos;
+      asm volatile("" : "+v"(off[i]));                   // (one register, not the pair that the product came in)
+    }
+  }
+  // base: the tile in memory; k_left: k of it that exist.  Those that do not are read beyond the end of the buffer, which gives zeros: behind the
+  // last row of a [k][x] tile, and a long way off where k is consecutive.
+  __device__ __forceinline__ void load(int i, const char *base, int64_t ld, int k_left) {
+    const int bytes = KROWS ? (int)(k_left * (uint32_t)ld) : 0x7fffffff;
+    const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, bytes, 0x00027000);
+    const uint32_t o = KROWS || 8 * pos < k_left ? off[i] : 0x80000000u;
+    reg[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(all, o, 0, 0));
+  }
+  __device__ __forceinline__ void write(int i, char *lds) const {
+    *reinterpret_cast<u32x4 *>(lds + (place ^ (KROWS && STEP % 16 == 8 ? (i & 1) << 7 : 0)) + i * STEP * ROW) = reg[i];
+  }
+};
+
+template <int BM, int BN> struct KnCfg {
+  static constexpr int A = BM * 128, B = BN * 128, STAGE = A + B;
+  static constexpr size_t lds = 2 * (size_t)STAGE;      // (more than the wavefronts need in the end)
+};
+
+template <bool A_KROWS, int BM, int BN, int WGM, int WGN>
+__global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P) {
+  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = KnCfg<BM, BN>::STAGE, A_BYTES = KnCfg<BM, BN>::A;
+  extern __shared__ __attribute__((aligned(16))) char kn_lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, kq = lane >> 4;
+  const int wave_m = wave / WGN, wave_n = wave % WGN, wm0 = wave_m * WM, wn0 = wave_n * WN;
+  int tile_m, tile_n, split;
+  tile_of(P.T, tile_m, tile_n, split);
+  const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
+  const int kt_begin = split * P.T.kt_per_split;
+  const int nkt = split == P.T.splits ? 0 : P.T.kt_all - kt_begin < P.T.kt_per_split ? P.T.kt_all - kt_begin : P.T.kt_per_split;
+
+  f32x4 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      acc[i][j] = (f32x4)0.f;
+      pin<BM == 256>(acc[i][j]);
+    }
+
+  // k-tiles of the planes one after the other, the smallest plane first; next: the one that is loaded next
+  int next_kt = __builtin_amdgcn_readfirstlane(kt_begin % P.ktiles), next_plane = __builtin_amdgcn_readfirstlane(kt_begin / P.ktiles);
+  int64_t next_k = (int64_t)next_kt * kKnK;
+  int next_left = (int)(P.K - next_k < kKnK ? P.K - next_k : kKnK);      // k of it that exist
+  const char *const a_first = P.A + (A_KROWS ? m0 * 2 : m0 * P.lda), *const b_first = P.B + n0 * 2;
+  Staged<NT, BM, A_KROWS> sa;
+  Staged<NT, BN, true> sb;
+  sa.init(P.lda, P.T.M - m0, tid);
+  sb.init(P.ldb, P.T.N - n0, tid);
+  constexpr int NA = decltype(sa)::N, PIECES = NA + decltype(sb)::N;
+  auto load = [&](int p) RSVD_INLINE {
+    if (p < NA) sa.load(p, a_first + (P.planes - 1 - next_plane) * P.plane + (A_KROWS ? next_k * P.lda : next_k * 2), P.lda, next_left);
+    else sb.load(p - NA, b_first + next_k * P.ldb, P.ldb, next_left);
+  };
+  auto write = [&](int p, int buf) RSVD_INLINE {
+    if (p < NA) sa.write(p, kn_lds + buf * STAGE);
+    else sb.write(p - NA, kn_lds + buf * STAGE + A_BYTES);
+  };
+  auto advance = [&]() RSVD_INLINE {                    // (behind the last tile of this workgroup's range: loads stay inside the operands)
+    next_k += kKnK;
+    if (++next_kt == P.ktiles) {
+      next_kt = 0;
+      next_k = 0;
+      if (next_plane + 1 < P.planes) ++next_plane;
+    }
+    next_left = (int)(P.K - next_k < kKnK ? P.K - next_k : kKnK);
+  };
+
+  // ---- operands of this lane
+  constexpr int A_ROW = decltype(sa)::ROW;
+  const int key_row = 8 * kq + (r16 >> 2), part = (r16 & 3) * 8;
+  // (blocks of 16 columns differ from the first one of the wavefront in the bits that are exchanged)
+  static_assert((TM == 8 || TM == 4 || TM == 2) && (TN == 8 || TN == 4 || TN == 2), "blocks of a power of two");
+  const int a_at = A_KROWS ? key_row * A_ROW + (krow_piece<BM>(wm0 / 16, key_row) << 5) + part : (wm0 + r16) * 128;
+  const int b_at = A_BYTES + key_row * (BN * 2) + (krow_piece<BN>(wn0 / 16, key_row) << 5) + part;
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  auto transposed = [&](const char *p, int row_bytes) RSVD_INLINE {
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p)));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p + 4 * row_bytes)));
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+  };
+  // A barrier that waits for what was written to LDS but not for loads.
+  auto meet = [&]() RSVD_INLINE {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(tile_wait(63));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // ---- sums of A over k: k-tile kt is summed by the tiles of column kt mod tiles_n, each wavefront its share of the rows
+  constexpr int SHARE = A_KROWS ? (TM + WGN - 1) / WGN : 1;
+  float asum[SHARE];
+#pragma unroll
+  for (int i = 0; i < SHARE; ++i) asum[i] = 0.f;
+  int now_column = __builtin_amdgcn_readfirstlane(kt_begin % P.T.tiles_n);      // of the tile that is multiplied
+  auto sum_a = [&](int buf) RSVD_INLINE {
+    const int at = a_at + buf * STAGE, first = wave_n * SHARE;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < SHARE; ++i)
+        if (first + i < TM) {
+          const u32x4 v = transposed(kn_lds + (at ^ ((first + i) << 5)) + h * 32 * A_ROW, A_ROW);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) asum[i] += bf16_low(v[e]) + bf16_high(v[e]);
+        }
+  };
+
+  // The matrix instructions of a tile, with the next one going to LDS in step.  (Behind the last tile that is one that nobody reads: no
+  // branches.)
+  auto body = [&](int buf) RSVD_INLINE {
+    const int a_now = a_at + buf * STAGE, b_now = b_at + buf * STAGE;
+    auto read_a = [&](int step) RSVD_INLINE {
+      const int h = step / TM, i = step % TM;
+      if (A_KROWS) return transposed(kn_lds + (a_now ^ (i << 5)) + h * 32 * A_ROW, A_ROW);
+      return *reinterpret_cast<const u32x4 *>(kn_lds + a_now + i * 2048 + (((4 * h + kq) ^ (r16 & 7)) << 4));
+    };
+    auto read_b = [&](int h, int j) RSVD_INLINE { return transposed(kn_lds + (b_now ^ (j << 5)) + h * 32 * BN * 2, BN * 2); };
+    constexpr int AHEAD = TM >= 4 ? 3 : 1;             // rows of blocks read ahead, not all of them: registers
+    u32x4 a[AHEAD + 1], b[2][TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) b[0][j] = read_b(0, j);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) a[i] = read_a(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int step = 0; step < 2 * TM; ++step) {
+      const int h = step / TM, i = step % TM;
+      if (step + AHEAD < 2 * TM) a[(step + AHEAD) % (AHEAD + 1)] = read_a(step + AHEAD);
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        if (h == 0 && i == j * TM / TN) b[1][j] = read_b(1, j);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(b[h][j], a[step % (AHEAD + 1)], acc[i][j]);
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p)
+        if (p * (2 * TM) / PIECES == step) {
+          write(p, buf ^ 1);
+          load(p);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  if (nkt > 0) {
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) load(p);
+    advance();
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      write(p, 0);
+      load(p);
+    }
+    advance();
+    meet();
+  }
+  for (int kt = 0; kt < nkt; ++kt) {
+    if (A_KROWS && P.sums != nullptr && now_column == tile_n) sum_a(kt & 1);
+    body(kt & 1);
+    advance();
+    if (++now_column == P.T.tiles_n) now_column = 0;
+    meet();
+  }
+  if (A_KROWS && P.sums != nullptr) {      // (no low-rank term there: split is a range of k)
+#pragma unroll
+    for (int i = 0; i < SHARE; ++i) {
+      float sum = asum[i];
+      sum += __shfl_xor(sum, 16);
+      sum += __shfl_xor(sum, 32);
+      const int64_t m = m0 + wm0 + (wave_n * SHARE + i) * 16 + r16;
+      if (lane < 16 && wave_n * SHARE + i < TM && m < P.T.M) P.sums[((int64_t)split * P.T.tiles_n + tile_n) * P.T.M + m] = sum;
+    }
+  }
+  int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
+  asm volatile("" : "+v"(last_lane));
+  // (behind the last meeting nobody reads the tiles)
+  finish_tile<TM, TN, BM == 256>(P.T, acc, split, m0 + wm0, n0 + wn0, last_lane, reinterpret_cast<float *>(kn_lds + wave * finish_lds<TN>()));
+}
+
+size_t kn_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, bool lowrank) {
+  return tile_partial_bytes(ctx, M, N, ceil_div(K, kKnK) * planes, lowrank);
+}
+int64_t kn_sum_rows(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes) {
+  const TileChoice c = tile_choose(ctx, M, N, ceil_div(K, kKnK) * planes);
+  return c.splits * ceil_div(N, c.bn);
+}
+
+template <bool A_KROWS, int BM, int BN, int WGM, int WGN> static hipError_t kn_run(hipStream_t s, const KnParams &P) {
+  hipLaunchKernelGGL((kn_kernel<A_KROWS, BM, BN, WGM, WGN>), dim3(tile_groups(P.T)), dim3(64 * WGM * WGN), (KnCfg<BM, BN>::lds), s, P);
+  return hipGetLastError();
+}
+
+template <bool A_KROWS> static hipError_t kn_run_tile(hipStream_t s, const KnParams &P, int bm) {
+  if (bm == 256) return kn_run<A_KROWS, 256, 256, 2, 4>(s, P);
+  if (bm == 128) return kn_run<A_KROWS, 128, 128, 2, 2>(s, P);
+  return kn_run<A_KROWS, 64, 64, 2, 2>(s, P);
+}
+
+hipError_t nt_init_device();
+hipError_t layer8_init_device(rsvd_ctx *) {
+  hipError_t e = nt_init_device();
+  const void *wide[2] = {reinterpret_cast<const void *>(&kn_kernel<true, 256, 256, 2, 4>),
+                         reinterpret_cast<const void *>(&kn_kernel<false, 256, 256, 2, 4>)};
+  for (const void *k : wide)
+    if (e == hipSuccess) e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)KnCfg<256, 256>::lds);
+  return e;
+}
+
+hipError_t kn_launch(rsvd_ctx *ctx, hipStream_t s, const KnDesc &d) {
+  const int64_t ktiles = ceil_div(d.K, kKnK), kt = ktiles * d.planes;
+  const TileChoice c = tile_choose(ctx, d.M, d.N, kt);
+  if (c.splits > 1 && (d.partial == nullptr || d.partial_bytes < tile_partial_bytes(ctx, d.M, d.N, kt, d.out.r > 0))) return hipErrorInvalidValue;
+  KnParams P;
+  P.A = (const char *)d.A; P.lda = d.lda; P.plane = d.plane; P.planes = d.planes;
+  P.ktiles = (int)ktiles; P.K = d.K;
+  P.B = (const char *)d.B; P.ldb = d.ldb;
+  P.sums = d.a_krows ? d.sums : nullptr;
+  P.T = tile_params(c, d.M, d.N, kt, d.partial, d.out);
+  const hipError_t e = d.a_krows ? kn_run_tile<true>(s, P, c.bm) : kn_run_tile<false>(s, P, c.bm);
+  return e == hipSuccess ? tile_reduce<false>(s, P.T) : e;
+}
+
+}  // namespace rsvd

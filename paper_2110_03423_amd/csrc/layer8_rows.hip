@@ -177,108 +177,39 @@ hipError_t split_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64
   return hipGetLastError();
 }
 
-// Transposes through LDS, 64 rows x 64 columns a workgroup.  SRC: 0 ... 2 numbers of an rsvd_xtype, 3 codes with a factor for each row,
-// 4 kept codes.
-constexpr int kFromCodes = 3, kFromKept = 4;
-template <int SRC> struct SrcTraits { static constexpr int PARTS = 1; };
-template <> struct SrcTraits<RSVD_X_F16> { static constexpr int PARTS = 2; };
-template <> struct SrcTraits<RSVD_X_F32> { static constexpr int PARTS = 3; };
-
-struct TransposeParams {
-  const char *X; int64_t ldx, rows, n;
-  const float *factor;
-  const uint8_t *powers; int64_t ldp;
-  uint16_t *planes; int64_t width, plane;
-  float *sums;
-};
-
-template <int SRC> __global__ __launch_bounds__(256) void transpose_kernel(const TransposeParams P) {
-  constexpr int PARTS = SrcTraits<SRC>::PARTS, PITCH = 66;      // 33 dwords: rows start at different banks
-  __shared__ uint16_t tile[PARTS][64 * PITCH];
-  const int tid = threadIdx.x;
-  const int64_t r0 = (int64_t)blockIdx.x * 64, j0 = (int64_t)blockIdx.y * 64;
-  {
-    const int r = tid >> 2, j = (tid & 3) * 16;
-    const int64_t row = r0 + r;
+template <bool KEPT>
+__global__ __launch_bounds__(256) void widen_kernel8(const int8_t *__restrict__ codes, int64_t ldc, const float *__restrict__ factor,
+                                                     const uint8_t *__restrict__ powers, int64_t ldp, int64_t rows, int n,
+                                                     uint16_t *__restrict__ plane, int64_t width, int shift) {
+  const int c = (int)(blockIdx.x << shift) + (int)(threadIdx.x & ((1u << shift) - 1u));
+  const int per = 256 >> shift;
+  if (8 * c >= n) return;
+  for (int64_t r = (int64_t)blockIdx.y * per + (threadIdx.x >> shift); r < rows; r += (int64_t)gridDim.y * per) {
+    const u32x2 w = *reinterpret_cast<const u32x2 *>(codes + r * ldc + 8 * c);
+    const float unit = KEPT ? kept_unit(powers[r * ldp + (c >> 2)]) : factor != nullptr ? factor[r] : 1.f;
+    float v[8];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t col = j0 + j + 8 * h;
-      float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (row < P.rows && col < P.n) {
-        if constexpr (SRC < kFromCodes) {
-          x_load8<SRC>(P.X + (row * P.ldx + col) * XTraits<SRC>::SIZE, P.n - col, v);
-        } else {
-          const u32x2 w = *reinterpret_cast<const u32x2 *>(P.X + row * P.ldx + col);
-          const float unit = SRC == kFromKept ? kept_unit(P.powers[row * P.ldp + (col >> 5)]) : P.factor != nullptr ? P.factor[row] : 1.f;
+    for (int e = 0; e < 8; ++e) v[e] = (float)((int)(w[e >> 2] << (24 - 8 * (e & 3))) >> 24) * unit;
+    u32x4 p;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = (float)((int)(w[e >> 2] << (24 - 8 * (e & 3))) >> 24) * unit;
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        unsigned p[PARTS];
-        bf16_parts2<PARTS>(v[2 * e], v[2 * e + 1], p);
-#pragma unroll
-        for (int q = 0; q < PARTS; ++q) {
-          tile[q][(j + 8 * h + 2 * e) * PITCH + r] = (uint16_t)p[q];
-          tile[q][(j + 8 * h + 2 * e + 1) * PITCH + r] = (uint16_t)(p[q] >> 16);
-        }
-      }
-    }
+    for (int e = 0; e < 4; ++e) p[e] = bf16_pair(v[2 * e], v[2 * e + 1]);
+    *reinterpret_cast<u32x4 *>(plane + r * width + 8 * c) = p;
   }
-  __syncthreads();
-  const int j = tid >> 2, r = (tid & 3) * 16;
-  const int64_t col = j0 + j;
-  if (SRC < kFromCodes && P.sums != nullptr) {
-    float sum = 0.f;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float x = 0.f;
-#pragma unroll
-      for (int q = PARTS - 1; q >= 0; --q) x += __uint_as_float((unsigned)tile[q][j * PITCH + r + e] << 16);
-      sum += x;
-    }
-    sum += __shfl_xor(sum, 1);
-    sum += __shfl_xor(sum, 2);
-    if ((tid & 3) == 0 && col < P.n) P.sums[(int64_t)blockIdx.x * P.n + col] = sum;
-  }
-  if (col >= P.n) return;
-#pragma unroll
-  for (int q = 0; q < PARTS; ++q)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t place = r0 + r + 8 * h;
-      if (place >= P.width) continue;
-      u32x4 out;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) out[e] = *reinterpret_cast<const unsigned *>(&tile[q][j * PITCH + r + 8 * h + 2 * e]);
-      *reinterpret_cast<u32x4 *>(P.planes + q * P.plane + col * P.width + place) = out;
-    }
 }
 
-static dim3 transpose_grid(int64_t rows, int64_t n) { return dim3((unsigned)ceil_div(rows, 64), (unsigned)ceil_div(n, 64)); }
-
-hipError_t transpose_split_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint16_t *planes,
-                                  int64_t width, float *sums) {
-  const TransposeParams P = {(const char *)X, ldx, rows, n, nullptr, nullptr, 0, planes, width, n * width, sums};
-  const dim3 grid = transpose_grid(rows, n);
-  if (type == RSVD_X_BF16) hipLaunchKernelGGL(transpose_kernel<RSVD_X_BF16>, grid, dim3(256), 0, s, P);
-  else if (type == RSVD_X_F16) hipLaunchKernelGGL(transpose_kernel<RSVD_X_F16>, grid, dim3(256), 0, s, P);
-  else hipLaunchKernelGGL(transpose_kernel<RSVD_X_F32>, grid, dim3(256), 0, s, P);
+hipError_t widen_codes_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldq, const float *factor, uint16_t *plane,
+                              int64_t width) {
+  int shift;
+  const dim3 grid = keep8_grid(rows, n, shift);
+  hipLaunchKernelGGL(widen_kernel8<false>, grid, dim3(256), 0, s, codes, ldq, factor, nullptr, 0, rows, (int)n, plane, width, shift);
   return hipGetLastError();
 }
 
-hipError_t transpose_codes_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldq, const float *factor,
-                                  uint16_t *plane, int64_t width) {
-  const TransposeParams P = {(const char *)codes, ldq, rows, n, factor, nullptr, 0, plane, width, n * width, nullptr};
-  hipLaunchKernelGGL(transpose_kernel<kFromCodes>, transpose_grid(rows, n), dim3(256), 0, s, P);
-  return hipGetLastError();
-}
-
-hipError_t transpose_kept_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp,
-                                 uint16_t *plane, int64_t width) {
-  const TransposeParams P = {(const char *)codes, ldc, rows, n, nullptr, powers, ldp, plane, width, n * width, nullptr};
-  hipLaunchKernelGGL(transpose_kernel<kFromKept>, transpose_grid(rows, n), dim3(256), 0, s, P);
+hipError_t widen_kept_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp,
+                             uint16_t *plane, int64_t width) {
+  int shift;
+  const dim3 grid = keep8_grid(rows, n, shift);
+  hipLaunchKernelGGL(widen_kernel8<true>, grid, dim3(256), 0, s, codes, ldc, nullptr, powers, ldp, rows, (int)n, plane, width, shift);
   return hipGetLastError();
 }
 

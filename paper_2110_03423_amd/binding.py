@@ -106,12 +106,17 @@ def _dtype_code(t):
     raise TypeError("fp32 or fp64 tensors only")
 
 
+_XTYPES = {}
+
+
 def _xtype_code(dtype):
-    import torch
-    codes = {torch.bfloat16: X_BF16, torch.float16: X_F16, torch.float32: X_F32}
-    if dtype not in codes:
-        raise TypeError("bf16, fp16 or fp32 tokens only")
-    return codes[dtype]
+    if not _XTYPES:
+        import torch
+        _XTYPES.update({torch.bfloat16: X_BF16, torch.float16: X_F16, torch.float32: X_F32})
+    try:
+        return _XTYPES[dtype]
+    except KeyError:
+        raise TypeError("bf16, fp16 or fp32 tokens only") from None
 
 
 def _empty_codes(rows, n, device):
@@ -183,9 +188,16 @@ class Kept8:
         if powers.shape != (codes.shape[0], -(-codes.shape[1] // 32)):
             raise ValueError("powers: one byte for each 32 columns of codes")
         _xtype_code(dtype)
-        self.codes, self.dtype = _laid_out(codes), dtype
-        self.powers = powers if powers.stride(1) == 1 or powers.shape[1] == 1 else powers.contiguous()
+        self._set(_laid_out(codes), powers if powers.stride(1) == 1 or powers.shape[1] == 1 else powers.contiguous(), dtype)
+
+    def _set(self, codes, powers, dtype):
+        self.codes, self.powers, self.dtype = codes, powers, dtype
         self.tokens, self.n = codes.shape
+        return self
+
+
+def _at(t):
+    return t.data_ptr() if t is not None else None
 
 
 def _ptr(t):
@@ -200,6 +212,7 @@ class Rsvd:
         no GPU and no torch needed."""
         self.lib = load_library()
         self._ws = None
+        self._needs = {}        # workspace of the layer calls, by their sizes
         h = C.c_void_p()
         if device is None:
             self.torch = None
@@ -235,6 +248,11 @@ class Rsvd:
 
     def _stream(self):
         return C.c_void_p(self.torch.cuda.current_stream(self.device).cuda_stream)
+
+    def _raw_stream(self):
+        """The current stream's handle, by the short way where torch has it (a tenth of the time, which small layer calls notice)."""
+        get = getattr(self.torch._C, "_cuda_getCurrentRawStream", None)
+        return get(self.device.index) if get is not None else self.torch.cuda.current_stream(self.device).cuda_stream
 
     def rsvd_profile_enable(self, on):
         self._check(self.lib.rsvd_profile_enable(self.h, int(on)))
@@ -436,25 +454,31 @@ class Rsvd:
         rows, n = X.shape
         codes = _empty_codes(rows, n, X.device)
         scale = self.torch.empty(rows, dtype=self.torch.float32, device=X.device)
-        self._check(self.lib.rsvd_q8_rows(self.h, self._stream(), _xtype_code(X.dtype), rows, n, _ptr(X), _ld(X), _ptr(codes),
-                                          _ld(codes), _ptr(scale)))
+        self._check(self.lib.rsvd_q8_rows(self.h, self._raw_stream(), _xtype_code(X.dtype), rows, n, _at(X), _ld(X), _at(codes),
+                                          _ld(codes), _at(scale)))
         return codes, scale
 
-    def _layer_ws(self, fn, *sizes):
-        need = C.c_size_t()
-        self._check(fn(self.h, *sizes, C.byref(need)))
-        return self._grow(need.value)
+    def _layer_ws(self, name, *sizes):
+        """The cached workspace; what a call of these sizes needs is asked for once."""
+        need = self._needs.get((name, sizes))
+        if need is None:
+            out = C.c_size_t()
+            self._check(getattr(self.lib, name)(self.h, *sizes, C.byref(out)))
+            if len(self._needs) >= 1024:
+                self._needs.clear()
+            need = self._needs[(name, sizes)] = out.value
+        return self._grow(need)
 
     def rsvd_q8_product(self, X, weight, workspace=None, out=None):
         """X (tokens x n) through the layer `weight` (Weight8): tokens x m, in the type of X."""
         w = weight
         _rows(X, w.n, "X")
         xt, tokens = _xtype_code(X.dtype), X.shape[0]
-        ws = workspace if workspace is not None else self._layer_ws(self.lib.rsvd_q8_product_bytes, xt, tokens, w.n, w.m, w.r)
+        ws = workspace if workspace is not None else self._layer_ws("rsvd_q8_product_bytes", xt, tokens, w.n, w.m, w.r)
         Y = _rows(out, w.m, "out", tokens, X.dtype) if out is not None else self._empty((tokens, w.m), X)
         self._check(self.lib.rsvd_q8_product(
-            self.h, self._stream(), xt, tokens, w.n, w.m, w.r, _ptr(X), _ld(X), _ptr(w.codes), _ld(w.codes), _ptr(w.scale),
-            _ptr(w.U), w.r, _ptr(w.Vt), w.n, _ptr(w.bias), _ptr(Y), _ld(Y), _ptr(ws), ws.numel()))
+            self.h, self._raw_stream(), xt, tokens, w.n, w.m, w.r, _at(X), _ld(X), _at(w.codes), _ld(w.codes), _at(w.scale),
+            _at(w.U), w.r, _at(w.Vt), w.n, _at(w.bias), _at(Y), _ld(Y), _at(ws), ws.numel()))
         return Y
 
     def rsvd_q8_product_grad(self, dY, weight, workspace=None, out=None):
@@ -462,11 +486,11 @@ class Rsvd:
         w = weight
         _rows(dY, w.m, "dY")
         xt, tokens = _xtype_code(dY.dtype), dY.shape[0]
-        ws = workspace if workspace is not None else self._layer_ws(self.lib.rsvd_q8_product_grad_bytes, xt, tokens, w.n, w.m, w.r)
+        ws = workspace if workspace is not None else self._layer_ws("rsvd_q8_product_grad_bytes", xt, tokens, w.n, w.m, w.r)
         dX = _rows(out, w.n, "out", tokens, dY.dtype) if out is not None else self._empty((tokens, w.n), dY)
         self._check(self.lib.rsvd_q8_product_grad(
-            self.h, self._stream(), xt, tokens, w.n, w.m, w.r, _ptr(dY), _ld(dY), _ptr(w.codes), _ld(w.codes), _ptr(w.scale),
-            _ptr(w.Ut), w.m, _ptr(w.V), w.r, _ptr(dX), _ld(dX), _ptr(ws), ws.numel()))
+            self.h, self._raw_stream(), xt, tokens, w.n, w.m, w.r, _at(dY), _ld(dY), _at(w.codes), _ld(w.codes), _at(w.scale),
+            _at(w.Ut), w.m, _at(w.V), w.r, _at(dX), _ld(dX), _at(ws), ws.numel()))
         return dX
 
     def rsvd_keep8_save(self, X):
@@ -475,16 +499,16 @@ class Rsvd:
         tokens, n = X.shape
         codes = _empty_codes(tokens, n, X.device)
         powers = self.torch.empty((tokens, -(-n // 32)), dtype=self.torch.uint8, device=X.device)
-        self._check(self.lib.rsvd_keep8_save(self.h, self._stream(), _xtype_code(X.dtype), tokens, n, _ptr(X), _ld(X),
-                                             _ptr(codes), _ld(codes), _ptr(powers), _ld(powers)))
-        return Kept8(codes, powers, X.dtype)
+        self._check(self.lib.rsvd_keep8_save(self.h, self._raw_stream(), _xtype_code(X.dtype), tokens, n, _at(X), _ld(X),
+                                             _at(codes), _ld(codes), _at(powers), _ld(powers)))
+        return Kept8.__new__(Kept8)._set(codes, powers, X.dtype)
 
     def rsvd_keep8_load(self, kept, out=None):
         """The kept activations, in their type."""
         X = out if out is not None else self.torch.empty((kept.tokens, kept.n), dtype=kept.dtype, device=kept.codes.device)
         _rows(X, kept.n, "out", kept.tokens, kept.dtype)
-        self._check(self.lib.rsvd_keep8_load(self.h, self._stream(), _xtype_code(X.dtype), kept.tokens, kept.n,
-                                             _ptr(kept.codes), _ld(kept.codes), _ptr(kept.powers), _ld(kept.powers), _ptr(X), _ld(X)))
+        self._check(self.lib.rsvd_keep8_load(self.h, self._raw_stream(), _xtype_code(X.dtype), kept.tokens, kept.n,
+                                             _at(kept.codes), _ld(kept.codes), _at(kept.powers), _ld(kept.powers), _at(X), _ld(X)))
         return X
 
     def rsvd_keep8_grad(self, dY, kept, out=None, accumulate=False, workspace=None):
@@ -505,8 +529,8 @@ class Rsvd:
             _rows(dW, kept.n, "dW")
             if dW.dtype != t.float32 or dW.shape[0] != m or (db is not None and (db.dtype != t.float32 or db.shape != (m,) or not db.is_contiguous())):
                 raise ValueError("out: fp32 gradients, m x n and m")
-        ws = workspace if workspace is not None else self._layer_ws(self.lib.rsvd_keep8_grad_bytes, xt, kept.tokens, kept.n, m)
+        ws = workspace if workspace is not None else self._layer_ws("rsvd_keep8_grad_bytes", xt, kept.tokens, kept.n, m)
         self._check(self.lib.rsvd_keep8_grad(
-            self.h, self._stream(), xt, kept.tokens, kept.n, m, _ptr(dY), _ld(dY), _ptr(kept.codes), _ld(kept.codes),
-            _ptr(kept.powers), _ld(kept.powers), _ptr(dW), _ld(dW), _ptr(db), int(accumulate), _ptr(ws), ws.numel()))
+            self.h, self._raw_stream(), xt, kept.tokens, kept.n, m, _at(dY), _ld(dY), _at(kept.codes), _ld(kept.codes),
+            _at(kept.powers), _ld(kept.powers), _at(dW), _ld(dW), _at(db), int(accumulate), _at(ws), ws.numel()))
         return dW, db

@@ -165,15 +165,6 @@ hipError_t keep8_save_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int
                              int64_t ldc, uint8_t *powers, int64_t ldp);
 hipError_t keep8_load_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, const int8_t *codes, int64_t ldc,
                              const uint8_t *powers, int64_t ldp, void *X, int64_t ldx);
-// planes[p][row][0 .. width): the bf16 parts of X_rj factor_j (factor NULL: of X_rj), zeros from n on.
-hipError_t split_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, const float *factor,
-                             uint16_t *planes, int64_t width);
-// plane[row][0 .. width): the codes of a row as bf16 numbers, multiplied by factor_row (NULL: as they are), or by the powers of two of kept
-// activations; width >= n, a multiple of 8.
-hipError_t widen_codes_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldq, const float *factor, uint16_t *plane,
-                              int64_t width);
-hipError_t widen_kept_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp,
-                             uint16_t *plane, int64_t width);
 // out[j] (+)= sum over b of sums[b][j]
 hipError_t add_sums_launch(hipStream_t s, int64_t blocks, int64_t n, const float *sums, float *out, int accumulate);
 hipError_t fill_zero_launch(hipStream_t s, int64_t rows, int64_t cols, float *out, int64_t ld);
@@ -190,6 +181,13 @@ hipError_t lowrank_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t
 // The same for up to kFewTokens tokens, together with rows8_launch.
 hipError_t front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, int64_t r, const void *X, int64_t ldx,
                         const void *F, int64_t ldf, float *sums, int8_t *codes, int64_t ldq, int64_t width, float *scale);
+// The operands of kn_launch for a gradient, and lowrank_launch for dY (r = 0: without): planes[q][token][0 .. planes_width) the bf16 parts of dY
+// (tokens x m, times dy_factor_j or NULL), zeros from m on (planes NULL: not wanted); plane[row][0 .. width) the codes (rows x n) as bf16 numbers, multiplied by
+// factor_row (NULL: as they are) or by the powers of two of kept activations.  Widths are m and n up to a multiple of 8.
+hipError_t grad_front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t m, int64_t r, const void *dY, int64_t lddy,
+                             const void *F, int64_t ldf, float *sums, const float *dy_factor, uint16_t *planes, int64_t planes_width,
+                             int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const float *factor, const uint8_t *powers, int64_t ldp,
+                             uint16_t *plane, int64_t width);
 // t [tokens][parts][rank_places(r)]: the sums added up, as bf16 numbers, the largest first.
 hipError_t lowrank_join_launch(hipStream_t s, const float *sums, int splits, int64_t tokens, int64_t r, int parts, uint16_t *t);
 

@@ -252,13 +252,11 @@ int rsvd_q8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t t
   const bool single = L.planes == 1, direct = takes_rows(type, dY, m, lddy);
   {
     ProfScope ps(ctx, s, PK_SMALL);
-    if (!direct) RSVD_TRY(split_rows_launch(s, type, tokens, m, dY, lddy, single ? nullptr : scale, a, L.width), "parts of the gradient");
-    RSVD_TRY(widen_codes_launch(s, m, n, codes, ldq, single ? scale : nullptr, b, L.b_width), "codes as bf16 numbers");
-    if (r > 0) {
-      float *sums = (float *)(ws + L.sums);
-      RSVD_TRY(lowrank_launch(ctx, s, type, tokens, m, r, dY, lddy, Ut, ldut, sums), "low-rank term");
-      RSVD_TRY(lowrank_join_launch(s, sums, L.splits, tokens, r, lowrank_parts(type), t), "low-rank term");
-    }
+    float *sums = (float *)(ws + L.sums);
+    RSVD_TRY(grad_front_launch(ctx, s, type, tokens, m, r, dY, lddy, Ut, ldut, sums, single ? nullptr : scale, direct ? nullptr : a, L.width,
+                               m, n, codes, ldq, single ? scale : nullptr, nullptr, 0, b, L.b_width),
+             "operands of the gradient");
+    if (r > 0) RSVD_TRY(lowrank_join_launch(s, sums, L.splits, tokens, r, lowrank_parts(type), t), "low-rank term");
   }
   KnDesc d;
   d.M = tokens; d.N = n; d.K = m;
@@ -348,8 +346,9 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
   const bool direct = takes_rows(type, dY, m, lddy);
   {
     ProfScope ps(ctx, s, PK_SMALL);
-    if (!direct) RSVD_TRY(split_rows_launch(s, type, tokens, m, dY, lddy, nullptr, a, L.width), "parts of the gradient");
-    RSVD_TRY(widen_kept_launch(s, tokens, n, codes, ldc, powers, ldp, b, L.b_width), "kept numbers");
+    RSVD_TRY(grad_front_launch(ctx, s, type, tokens, m, 0, dY, lddy, nullptr, 0, nullptr, nullptr, direct ? nullptr : a, L.width, tokens, n, codes,
+                               ldc, nullptr, powers, ldp, b, L.b_width),
+             "operands of the gradient");
   }
   KnDesc d;
   d.M = m; d.N = n; d.K = tokens;

@@ -132,21 +132,30 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void nt_kernel(c
 }
 
 // ---------------------------------------------------------------- choice of tile and of the ranges of k
+// The time of each tile and number of ranges is estimated, and the least taken.  Measured with both product kernels (4096 to 8192 k, one to four
+// workgroups on a CU): a k-tile takes a CU 0.22, 0.55 and 2.05 us for each workgroup of 64, 128 and 256 rows and columns, but no less than 0.33,
+// 0.78 and 1.8 us; a launch 5 us beside that; ranges of k a second launch and their sums written and read (5 bytes / ps).  What that decides:
+// 2048 x 2048, 64 k-tiles: 128 in 55 us, 256 and four ranges in 64, 64 in 65; 2048 x 1024: 128 and four ranges in 36, one in 46, 64 in 38;
+// 512 x 2048: 128 and four ranges in 24, 64 in 25; 4096 x 64, 128 k-tiles: 64 and four ranges in 19, sixteen in 23.
 TileChoice tile_choose(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt) {
-  TileChoice c = {64, 64, 1, kt};
-  const int64_t cus = ctx->cu_count;
-  if (ceil_div(M, 256) * ceil_div(N, 256) >= cus / 2) c.bm = c.bn = 256;
-  else if (ceil_div(M, 128) * ceil_div(N, 128) >= cus / 2) c.bm = c.bn = 128;
-  const int64_t tiles = ceil_div(M, c.bm) * ceil_div(N, c.bn);
-  const int64_t want = c.bm == 64 ? 2 * cus : cus;
-  int64_t splits = want / tiles;
-  if (splits > kt / 8) splits = kt / 8;
-  if (splits > 16) splits = 16;
-  if (splits > 1 && c.bm < 256) {
-    c.kt_per_split = ceil_div(kt, splits);
-    c.splits = (int)ceil_div(kt, c.kt_per_split);
-  }
-  return c;
+  static const struct { int b; double step, least; } tile[3] = {{64, 0.22, 0.33}, {128, 0.55, 0.78}, {256, 2.05, 1.8}};
+  static const int ranges[8] = {1, 2, 3, 4, 6, 8, 12, 16};
+  TileChoice best = {64, 64, 1, kt};
+  double least = 1e300;
+  for (const auto &t : tile)
+    for (const int r : ranges) {
+      if (r > 1 && kt < 4 * r) break;
+      const int64_t per = ceil_div(kt, r), used = ceil_div(kt, per);
+      const int64_t groups = ceil_div(ceil_div(M, t.b) * ceil_div(N, t.b) * used, ctx->cu_count);
+      const double step = (double)groups * t.step;
+      double us = (double)per * (step > t.least ? step : t.least);
+      if (used > 1) us += 3.0 + (double)used * (double)M * (double)N * 8.0 / 5e6;
+      if (us < least) {
+        least = us;
+        best = TileChoice{t.b, t.b, (int)used, per};
+      }
+    }
+  return best;
 }
 
 size_t nt_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt, bool lowrank) { return tile_partial_bytes(ctx, M, N, kt, lowrank); }

@@ -19,7 +19,7 @@ struct KnParams {
   int planes, ktiles;                      // k-tiles of a plane
   int64_t K;
   const char *B; int64_t ldb;              // bytes
-  float *sums;                             // A_KROWS: sums of A over k by ranges, [split][tile_n][M], or NULL
+  float *sums; int sum_columns;            // A_KROWS: sums of A over k by ranges, [split][sum_columns][M], or NULL
   TileParams T;
 };
 
@@ -139,12 +139,12 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  // ---- sums of A over k: k-tile kt is summed by the tiles of column kt mod tiles_n, each wavefront its share of the rows
+  // ---- sums of A over k: k-tile kt is summed by the tiles of column kt mod sum_columns, each wavefront its share of the rows
   constexpr int SHARE = A_KROWS ? (TM + WGN - 1) / WGN : 1;
   float asum[SHARE];
 #pragma unroll
   for (int i = 0; i < SHARE; ++i) asum[i] = 0.f;
-  int now_column = __builtin_amdgcn_readfirstlane(kt_begin % P.T.tiles_n);      // of the tile that is multiplied
+  int now_column = __builtin_amdgcn_readfirstlane(kt_begin % P.sum_columns);      // of the tile that is multiplied
   auto sum_a = [&](int buf) RSVD_INLINE {
     const int at = a_at + buf * STAGE, first = wave_n * SHARE;
 #pragma unroll
@@ -209,17 +209,17 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
     if (A_KROWS && P.sums != nullptr && now_column == tile_n) sum_a(kt & 1);
     body(kt & 1);
     advance();
-    if (++now_column == P.T.tiles_n) now_column = 0;
+    if (++now_column == P.sum_columns) now_column = 0;
     meet();
   }
-  if (A_KROWS && P.sums != nullptr) {      // (no low-rank term there: split is a range of k)
+  if (A_KROWS && P.sums != nullptr && tile_n < P.sum_columns) {      // (no low-rank term there: split is a range of k)
 #pragma unroll
     for (int i = 0; i < SHARE; ++i) {
       float sum = asum[i];
       sum += __shfl_xor(sum, 16);
       sum += __shfl_xor(sum, 32);
       const int64_t m = m0 + wm0 + (wave_n * SHARE + i) * 16 + r16;
-      if (lane < 16 && wave_n * SHARE + i < TM && m < P.T.M) P.sums[((int64_t)split * P.T.tiles_n + tile_n) * P.T.M + m] = sum;
+      if (lane < 16 && wave_n * SHARE + i < TM && m < P.T.M) P.sums[((int64_t)split * P.sum_columns + tile_n) * P.T.M + m] = sum;
     }
   }
   int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
@@ -231,9 +231,11 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
 size_t kn_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, bool lowrank) {
   return tile_partial_bytes(ctx, M, N, ceil_div(K, kKnK) * planes, lowrank);
 }
+// Columns of tiles that share the sums of A.
+static int64_t kn_sum_columns(int64_t N, int bn) { return ceil_div(N, bn) < 8 ? ceil_div(N, bn) : 8; }
 int64_t kn_sum_rows(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes) {
   const TileChoice c = tile_choose(ctx, M, N, ceil_div(K, kKnK) * planes);
-  return c.splits * ceil_div(N, c.bn);
+  return c.splits * kn_sum_columns(N, c.bn);
 }
 
 template <bool A_KROWS, int BM, int BN, int WGM, int WGN> static hipError_t kn_run(hipStream_t s, const KnParams &P) {
@@ -266,6 +268,7 @@ hipError_t kn_launch(rsvd_ctx *ctx, hipStream_t s, const KnDesc &d) {
   P.ktiles = (int)ktiles; P.K = d.K;
   P.B = (const char *)d.B; P.ldb = d.ldb;
   P.sums = d.a_krows ? d.sums : nullptr;
+  P.sum_columns = (int)kn_sum_columns(d.N, c.bn);
   P.T = tile_params(c, d.M, d.N, kt, d.partial, d.out);
   const hipError_t e = d.a_krows ? kn_run_tile<true>(s, P, c.bm) : kn_run_tile<false>(s, P, c.bm);
   return e == hipSuccess ? tile_reduce<false>(s, P.T) : e;

@@ -13,19 +13,20 @@ struct LowrankParams {
   const uint16_t *F; int64_t ldf; int r, rp;
   float *sums;                     // [split][token][rp]
   int splits; int64_t k_per_split; // a multiple of 64
+  int rank_tiles;                  // of 128 ranks
 };
 
 // ---------------------------------------------------------------- many tokens
 // 64 tokens a workgroup, sixteen a wavefront, 16 RB ranks; k-steps of 64; those of F are loaded one ahead, those of X, which come
 // from further away, two.
-template <int XT, int RB> __global__ __launch_bounds__(256, 2) void lowrank_kernel(const LowrankParams P) {
+template <int XT, int RB> __device__ __forceinline__ void lowrank_group(const LowrankParams &P, int group, char (*tile)[16 * RB * 128]) {
   constexpr int PARTS = XTraits<XT>::PARTS, ROWS = 16 * RB, NF = (ROWS * 8 + 255) / 256;      // 16-byte pieces of a k-step of F per thread
-  __shared__ __attribute__((aligned(16))) char tile[2][ROWS * 128];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
-  const int split = (int)blockIdx.x % P.splits;      // (workgroups of an XCD share a range of F where there are eight)
-  const int64_t t0 = (int64_t)(blockIdx.x / P.splits) * 64 + 16 * wave;
-  const int p0 = (int)blockIdx.y * 128;
+  const int p0 = group % P.rank_tiles * 128;
+  group /= P.rank_tiles;
+  const int split = group % P.splits;      // (workgroups of an XCD share a range of F where there are eight)
+  const int64_t t0 = (int64_t)(group / P.splits) * 64 + 16 * wave;
   const int64_t k0 = split * P.k_per_split, k1 = k0 + P.k_per_split < P.n ? k0 + P.k_per_split : P.n;
   const int64_t token = t0 + r16 < P.tokens ? t0 + r16 : P.tokens - 1;
   const char *x = P.X + token * P.ldx * XTraits<XT>::SIZE;
@@ -90,6 +91,32 @@ template <int XT, int RB> __global__ __launch_bounds__(256, 2) void lowrank_kern
     for (int v = 0; v < 4; ++v) acc[j][v] = p0 + p + v < P.r ? acc[j][v] : 0.f;
     *reinterpret_cast<f32x4 *>(out + p) = acc[j];
   }
+}
+
+template <int XT, int RB> __global__ __launch_bounds__(256, 2) void lowrank_kernel(const LowrankParams P) {
+  __shared__ __attribute__((aligned(16))) char tile[2][16 * RB * 128];
+  lowrank_group<XT, RB>(P, (int)blockIdx.x, tile);
+}
+
+// The same, and behind it the operands of the gradients: three things that have nothing to do with each other, in one launch.
+struct GradFrontParams {
+  LowrankParams L; int64_t lowrank_groups;
+  SplitParams S;
+  WidenParams W;
+};
+template <int XT, int RB> __global__ __launch_bounds__(256, 2) void grad_front_kernel(const GradFrontParams P) {
+  __shared__ __attribute__((aligned(16))) char tile[2][16 * RB * 128];
+  int64_t group = blockIdx.x;
+  if (group < P.lowrank_groups) {
+    lowrank_group<XT, RB>(P.L, (int)group, tile);
+    return;
+  }
+  group -= P.lowrank_groups;
+  if (group < P.W.groups) {
+    widen_group(P.W, group);
+    return;
+  }
+  split_rows_group<XT>(P.S, group - P.W.groups);
 }
 
 // ---------------------------------------------------------------- a few tokens
@@ -168,11 +195,14 @@ static LowrankParams lowrank_params(const rsvd_ctx *ctx, int64_t tokens, int64_t
   P.sums = sums;
   P.splits = lowrank_splits(ctx, tokens, n, r);
   P.k_per_split = (int64_t)align_up((size_t)ceil_div(n, P.splits), 64);
+  P.rank_tiles = (int)ceil_div(r, 128);
   return P;
 }
 
+static int64_t lowrank_groups(const LowrankParams &P) { return ceil_div(P.tokens, 64) * P.splits * P.rank_tiles; }
+
 template <int XT> static void lowrank_typed(hipStream_t s, const LowrankParams &P) {
-  const dim3 grid((unsigned)(ceil_div(P.tokens, 64) * P.splits), (unsigned)ceil_div(P.r, 128));
+  const dim3 grid((unsigned)lowrank_groups(P));
   if (P.r <= 32) hipLaunchKernelGGL((lowrank_kernel<XT, 2>), grid, dim3(256), 0, s, P);
   else if (P.r <= 64) hipLaunchKernelGGL((lowrank_kernel<XT, 4>), grid, dim3(256), 0, s, P);
   else hipLaunchKernelGGL((lowrank_kernel<XT, 8>), grid, dim3(256), 0, s, P);
@@ -184,6 +214,29 @@ hipError_t lowrank_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t
   if (type == RSVD_X_BF16) lowrank_typed<RSVD_X_BF16>(s, P);
   else if (type == RSVD_X_F16) lowrank_typed<RSVD_X_F16>(s, P);
   else lowrank_typed<RSVD_X_F32>(s, P);
+  return hipGetLastError();
+}
+
+template <int XT> static void grad_front_typed(hipStream_t s, const GradFrontParams &P) {
+  const dim3 grid((unsigned)(P.lowrank_groups + P.W.groups + P.S.groups));
+  if (P.L.r <= 32) hipLaunchKernelGGL((grad_front_kernel<XT, 2>), grid, dim3(256), 0, s, P);
+  else if (P.L.r <= 64) hipLaunchKernelGGL((grad_front_kernel<XT, 4>), grid, dim3(256), 0, s, P);
+  else hipLaunchKernelGGL((grad_front_kernel<XT, 8>), grid, dim3(256), 0, s, P);
+}
+
+hipError_t grad_front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t m, int64_t r, const void *dY, int64_t lddy,
+                             const void *F, int64_t ldf, float *sums, const float *dy_factor, uint16_t *planes, int64_t planes_width,
+                             int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const float *factor, const uint8_t *powers, int64_t ldp,
+                             uint16_t *plane, int64_t width) {
+  GradFrontParams P;
+  P.L = lowrank_params(ctx, tokens, m, r < 1 ? 1 : r, dY, lddy, F, ldf, sums);
+  P.lowrank_groups = r > 0 ? lowrank_groups(P.L) : 0;
+  P.S = SplitParams{(const char *)dY, lddy, tokens, m, dy_factor, planes, planes_width, 0};
+  if (planes != nullptr) P.S.groups = ceil_div(tokens * (planes_width / 8), 256);
+  P.W = WidenParams{codes, ldc, factor, powers, ldp, rows, n, plane, width, ceil_div(rows * ceil_div(n, 16), 256)};
+  if (type == RSVD_X_BF16) grad_front_typed<RSVD_X_BF16>(s, P);
+  else if (type == RSVD_X_F16) grad_front_typed<RSVD_X_F16>(s, P);
+  else grad_front_typed<RSVD_X_F32>(s, P);
   return hipGetLastError();
 }
 

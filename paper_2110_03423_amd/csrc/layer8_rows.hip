@@ -60,9 +60,6 @@ __global__ __launch_bounds__(256) void keep8_save_kernel(const char *__restrict_
   }
 }
 
-// The value of code q of a block with power byte b: exact in bf16.
-__device__ __forceinline__ float kept_unit(unsigned b) { return b == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(b << 23); }
-
 template <int XT>
 __global__ __launch_bounds__(256) void keep8_load_kernel(const int8_t *__restrict__ codes, int64_t ldc, const uint8_t *__restrict__ powers,
                                                          int64_t ldp, int64_t tokens, int n, char *__restrict__ X, int64_t ldx, int shift) {
@@ -139,96 +136,33 @@ hipError_t keep8_load_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int
   return hipGetLastError();
 }
 
-// ---------------------------------------------------------------- operand planes
-template <int XT>
-__global__ __launch_bounds__(256) void split_rows_kernel(const char *__restrict__ X, int64_t ldx, int64_t n, const float *__restrict__ factor,
-                                                         uint16_t *__restrict__ planes, int64_t width, int64_t plane) {
-  constexpr int P = XTraits<XT>::PARTS;
-  const int64_t j = 8 * ((int64_t)blockIdx.x * 256 + threadIdx.x), row = blockIdx.y + (int64_t)blockIdx.z * 65535;
-  if (j >= width || row * width >= plane) return;
-  float v[8];
-  x_load8<XT>(X + (row * ldx + j) * XTraits<XT>::SIZE, n - j, v);
-  if (factor != nullptr) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (j + e < n) v[e] *= factor[j + e];
-  }
-  u32x4 out[P];
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    unsigned p[P];
-    bf16_parts2<P>(v[2 * e], v[2 * e + 1], p);
-#pragma unroll
-    for (int q = 0; q < P; ++q) out[q][e] = p[q];
-  }
-#pragma unroll
-  for (int q = 0; q < P; ++q) *reinterpret_cast<u32x4 *>(planes + q * plane + row * width + j) = out[q];
-}
-
-hipError_t split_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, const float *factor,
-                             uint16_t *planes, int64_t width) {
-  const dim3 grid((unsigned)ceil_div(width, 2048), (unsigned)(rows < 65535 ? rows : 65535), (unsigned)ceil_div(rows, 65535));
-#define SPLIT(XT) \
-  hipLaunchKernelGGL(split_rows_kernel<XT>, grid, dim3(256), 0, s, (const char *)X, ldx, n, factor, planes, width, rows * width)
-  if (type == RSVD_X_BF16) SPLIT(RSVD_X_BF16);
-  else if (type == RSVD_X_F16) SPLIT(RSVD_X_F16);
-  else SPLIT(RSVD_X_F32);
-#undef SPLIT
-  return hipGetLastError();
-}
-
-template <bool KEPT>
-__global__ __launch_bounds__(256) void widen_kernel8(const int8_t *__restrict__ codes, int64_t ldc, const float *__restrict__ factor,
-                                                     const uint8_t *__restrict__ powers, int64_t ldp, int64_t rows, int n,
-                                                     uint16_t *__restrict__ plane, int64_t width, int shift) {
-  const int c = (int)(blockIdx.x << shift) + (int)(threadIdx.x & ((1u << shift) - 1u));
-  const int per = 256 >> shift;
-  if (8 * c >= n) return;
-  for (int64_t r = (int64_t)blockIdx.y * per + (threadIdx.x >> shift); r < rows; r += (int64_t)gridDim.y * per) {
-    const u32x2 w = *reinterpret_cast<const u32x2 *>(codes + r * ldc + 8 * c);
-    const float unit = KEPT ? kept_unit(powers[r * ldp + (c >> 2)]) : factor != nullptr ? factor[r] : 1.f;
-    float v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = (float)((int)(w[e >> 2] << (24 - 8 * (e & 3))) >> 24) * unit;
-    u32x4 p;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) p[e] = bf16_pair(v[2 * e], v[2 * e + 1]);
-    *reinterpret_cast<u32x4 *>(plane + r * width + 8 * c) = p;
-  }
-}
-
-hipError_t widen_codes_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldq, const float *factor, uint16_t *plane,
-                              int64_t width) {
-  int shift;
-  const dim3 grid = keep8_grid(rows, n, shift);
-  hipLaunchKernelGGL(widen_kernel8<false>, grid, dim3(256), 0, s, codes, ldq, factor, nullptr, 0, rows, (int)n, plane, width, shift);
-  return hipGetLastError();
-}
-
-hipError_t widen_kept_launch(hipStream_t s, int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp,
-                             uint16_t *plane, int64_t width) {
-  int shift;
-  const dim3 grid = keep8_grid(rows, n, shift);
-  hipLaunchKernelGGL(widen_kernel8<true>, grid, dim3(256), 0, s, codes, ldc, nullptr, powers, ldp, rows, (int)n, plane, width, shift);
-  return hipGetLastError();
-}
-
+// ---------------------------------------------------------------- sums
+// Sixteen columns a workgroup, sixteen threads for the rows of each.
 __global__ __launch_bounds__(256) void add_sums_kernel(const float *__restrict__ sums, int64_t blocks, int64_t n, float *__restrict__ out,
                                                        int accumulate) {
-  const int64_t j = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-  __shared__ float part[4][64];
+  const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
+  const int64_t j = (int64_t)blockIdx.x * 16 + col;
+  __shared__ float parts[16][17];
   float sum = 0.f;
-  if (j < n)
-    for (int64_t b = threadIdx.x >> 6; b < blocks; b += 4) sum += sums[b * n + j];
-  part[threadIdx.x >> 6][threadIdx.x & 63] = sum;
+  if (j < n) {
+    for (int64_t b = part; b < blocks; b += 64) {
+      float v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = b + 16 * u < blocks ? sums[(b + 16 * u) * n + j] : 0.f;
+      sum += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+  }
+  parts[part][col] = sum;
   __syncthreads();
-  if (threadIdx.x >= 64 || j >= n) return;
-  sum = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+  if (threadIdx.x >= 16 || j >= n) return;
+  sum = 0.f;
+#pragma unroll
+  for (int p = 0; p < 16; ++p) sum += parts[p][col];
   out[j] = accumulate ? out[j] + sum : sum;
 }
 
 hipError_t add_sums_launch(hipStream_t s, int64_t blocks, int64_t n, const float *sums, float *out, int accumulate) {
-  hipLaunchKernelGGL(add_sums_kernel, dim3((unsigned)ceil_div(n, 64)), dim3(256), 0, s, sums, blocks, n, out, accumulate);
+  hipLaunchKernelGGL(add_sums_kernel, dim3((unsigned)ceil_div(n, 16)), dim3(256), 0, s, sums, blocks, n, out, accumulate);
   return hipGetLastError();
 }
 

@@ -107,4 +107,85 @@ template <int XT, int CH> __device__ __forceinline__ void rows8_row(const Rows8P
   }
 }
 
+// The value of code q of a block with power byte b: exact in bf16.
+__device__ __forceinline__ float kept_unit(unsigned b) { return b == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float(b << 23); }
+
+// ---------------------------------------------------------------- operands of the gradients
+// Row and place in it of piece group * 256 + thread, per_row pieces a row.  (One long division for the workgroup, a short one for the thread.)
+__device__ __forceinline__ void piece_of(int64_t group, int per_row, int64_t &row, int &place) {
+  const int64_t first = group * 256, row0 = first / per_row;
+  const unsigned at = (unsigned)(first - row0 * per_row) + threadIdx.x, more = at / (unsigned)per_row;
+  row = row0 + more;
+  place = (int)(at - more * (unsigned)per_row);
+}
+
+// planes[q][row][0 .. width): the bf16 parts of X_rj factor_j (factor NULL: of X_rj), zeros from n on; width: a multiple of 8.
+struct SplitParams {
+  const char *X; int64_t ldx, rows, n;
+  const float *factor;
+  uint16_t *planes; int64_t width;
+  int64_t groups;                  // workgroups: 256 pieces of eight each
+};
+template <int XT> __device__ __forceinline__ void split_rows_group(const SplitParams &P, int64_t group) {
+  constexpr int PARTS = XTraits<XT>::PARTS;
+  int64_t row;
+  int place;
+  piece_of(group, (int)(P.width / 8), row, place);
+  const int64_t j = 8 * (int64_t)place;
+  if (row >= P.rows) return;
+  const int64_t left = P.n - j;
+  const char *x = P.X + (row * P.ldx + j) * XTraits<XT>::SIZE;
+  u32x4 out[PARTS];
+  if (P.factor != nullptr) {
+    float v[8];
+    x_load8<XT>(x, left, v);
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (u < left) v[u] *= P.factor[j + u];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      unsigned p[PARTS];
+      bf16_parts2<PARTS>(v[2 * u], v[2 * u + 1], p);
+#pragma unroll
+      for (int q = 0; q < PARTS; ++q) out[q][u] = p[q];
+    }
+  } else {
+    split_operand<XT>(raw_load8<XT>(x, left), out);
+  }
+#pragma unroll
+  for (int q = 0; q < PARTS; ++q) *reinterpret_cast<u32x4 *>(P.planes + q * P.rows * P.width + row * P.width + j) = out[q];
+}
+
+// plane[row][0 .. width): the codes of a row as bf16 numbers, multiplied by factor_row (NULL: as they are), or by the powers of two of kept
+// activations (powers != NULL); width: n up to a multiple of 8.
+struct WidenParams {
+  const int8_t *codes; int64_t ldc;
+  const float *factor;
+  const uint8_t *powers; int64_t ldp;
+  int64_t rows, n;
+  uint16_t *plane; int64_t width;
+  int64_t groups;                  // workgroups: 256 pieces of sixteen each
+};
+__device__ __forceinline__ void widen_group(const WidenParams &P, int64_t group) {
+  int64_t row;
+  int place;
+  piece_of(group, (int)((P.n + 15) / 16), row, place);
+  const int64_t j = 16 * (int64_t)place;
+  if (row >= P.rows) return;
+  const u32x4 w = *reinterpret_cast<const u32x4 *>(P.codes + row * P.ldc + j);
+  const float unit = P.powers != nullptr ? kept_unit(P.powers[row * P.ldp + (j >> 5)]) : P.factor != nullptr ? P.factor[row] : 1.f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (j + 8 * h >= P.width) break;
+    u32x4 p;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const unsigned d = w[2 * h + (u >> 1)];
+      const float a = (float)((int)(d << (24 - 16 * (u & 1))) >> 24) * unit, b = (float)((int)(d << (16 - 16 * (u & 1))) >> 24) * unit;
+      p[u] = bf16_pair(a, b);
+    }
+    *reinterpret_cast<u32x4 *>(P.plane + row * P.width + j + 8 * h) = p;
+  }
+}
+
 }  // namespace rsvd

@@ -48,11 +48,18 @@ __device__ __forceinline__ f32x4 column4(const float *p, int64_t n, int64_t N, f
   return v;
 }
 
+// Four numbers rounded to a 16-bit type.
+template <int TYPE> __device__ __forceinline__ u32x2 halves4(f32x4 v) {
+  if constexpr (TYPE == RSVD_X_BF16) return u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+  else return u32x2{__builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{v[0], v[1]}, f16x2)),
+                    __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{v[2], v[3]}, f16x2))};
+}
+
 // Four consecutive results of row m from column n on, of which those before column N exist.
-__device__ __forceinline__ void store4(const Layer8Epilogue &E, int64_t m, int64_t n, int64_t N, f32x4 v) {
+template <int TYPE> __device__ __forceinline__ void store4(const Layer8Epilogue &E, int64_t m, int64_t n, int64_t N, f32x4 v) {
   const int64_t at = m * E.ldc + n;
   const bool whole = n + 4 <= N;
-  if (E.type == RSVD_X_F32) {
+  if constexpr (TYPE == RSVD_X_F32) {
     float *c = reinterpret_cast<float *>(E.C) + at;
     if (whole) {
       if (E.accumulate) v += *reinterpret_cast<const f32x4_any *>(c);
@@ -63,14 +70,7 @@ __device__ __forceinline__ void store4(const Layer8Epilogue &E, int64_t m, int64
         if (n + e < N) c[e] = E.accumulate ? c[e] + v[e] : v[e];
     }
   } else {
-    u32x2 p;
-    if (E.type == RSVD_X_BF16) {
-      p[0] = bf16_pair(v[0], v[1]);
-      p[1] = bf16_pair(v[2], v[3]);
-    } else {
-      p[0] = __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{v[0], v[1]}, f16x2));
-      p[1] = __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{v[2], v[3]}, f16x2));
-    }
+    const u32x2 p = halves4<TYPE>(v);
     uint16_t *c = reinterpret_cast<uint16_t *>(E.C) + at;
     if (whole) {
       *reinterpret_cast<u32x2_any *>(c) = p;
@@ -80,6 +80,11 @@ __device__ __forceinline__ void store4(const Layer8Epilogue &E, int64_t m, int64
         if (n + e < N) c[e] = (uint16_t)(p[e >> 1] >> (16 * (e & 1)));
     }
   }
+}
+__device__ __forceinline__ void store4(const Layer8Epilogue &E, int64_t m, int64_t n, int64_t N, f32x4 v) {
+  if (E.type == RSVD_X_F32) store4<RSVD_X_F32>(E, m, n, N, v);
+  else if (E.type == RSVD_X_BF16) store4<RSVD_X_BF16>(E, m, n, N, v);
+  else store4<RSVD_X_F16>(E, m, n, N, v);
 }
 
 }  // namespace rsvd

@@ -37,24 +37,39 @@ __device__ __forceinline__ void tile_of(const TileParams &P, int &tile_m, int &t
 template <int TN> constexpr int finish_lds() { return 16 * (16 * TN + 4) * 4; }
 
 // Stores a wavefront's blocks through LDS, sixteen rows at a time, so that lanes next to each other write what is next to each other.  The
-// value of block (i, j) that lane L has are row 16 i + L % 16 and four columns from 16 j + 4 (L / 16) on.
-template <int TM, int TN, typename vec_t>
+// value of block (i, j) that lane L has are row 16 i + L % 16 and four columns from 16 j + 4 (L / 16) on.  Where all rows and columns exist, what
+// sixteen rows hold is read at once and stored without a look at each.
+template <int TYPE, int TM, int TN, typename vec_t>
 __device__ __forceinline__ void store_blocks(const Layer8Epilogue &E, int64_t M, int64_t N, const vec_t (&val)[TM][TN], int64_t m1, int64_t n1,
                                              int lane, float *lds) {
-  constexpr int PITCH = 16 * TN + 4, PER_ROW = 4 * TN, ROWS = 64 / PER_ROW;
+  constexpr int PITCH = 16 * TN + 4, PER_ROW = 4 * TN, ROWS = 64 / PER_ROW, PASSES = 16 / ROWS, SIZE = TYPE == RSVD_X_F32 ? 4 : 2;
   const int r16 = lane & 15, kq = lane >> 4, row = lane / PER_ROW, col = 4 * (lane % PER_ROW);
   const int64_t n = n1 + col;
+  const bool whole = m1 + 16 * TM <= M && n1 + 16 * TN <= N && E.accumulate == 0;
+  char *const c = reinterpret_cast<char *>(E.C) + ((m1 + row) * E.ldc + n) * SIZE;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
 #pragma unroll
     for (int j = 0; j < TN; ++j) *reinterpret_cast<vec_t *>(lds + r16 * PITCH + 16 * j + 4 * kq) = val[i][j];
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
+    if (whole) {
+      f32x4 v[PASSES];
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) v[p] = *reinterpret_cast<const f32x4 *>(lds + (p * ROWS + row) * PITCH + col);
+#pragma unroll
+      for (int p = 0; p < PASSES; ++p) {
+        char *at = c + (int64_t)(16 * i + p * ROWS) * E.ldc * SIZE;
+        if constexpr (TYPE == RSVD_X_F32) *reinterpret_cast<f32x4_any *>(at) = v[p];
+        else *reinterpret_cast<u32x2_any *>(at) = halves4<TYPE>(v[p]);
+      }
+    } else {
 #pragma unroll 1
-    for (int p = 0; p < 16 / ROWS; ++p) {
-      const int64_t m = m1 + 16 * i + p * ROWS + row;
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(lds + (p * ROWS + row) * PITCH + col);
-      if (m < M && n < N) store4(E, m, n, N, v);
+      for (int p = 0; p < PASSES; ++p) {
+        const int64_t m = m1 + 16 * i + p * ROWS + row;
+        const f32x4 v = *reinterpret_cast<const f32x4 *>(lds + (p * ROWS + row) * PITCH + col);
+        if (m < M && n < N) store4<TYPE>(E, m, n, N, v);
+      }
     }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
@@ -112,21 +127,43 @@ __device__ __forceinline__ void finish_tile(const TileParams &P, acc_t (&acc)[TM
       }
     }
   }
-  // the low-rank term
+  // the low-rank term; the operands of a step are loaded during the one before
+  const int steps = W.parts * W.rp / 32;
+  if (steps > 0) {
+    u32x4 a[2][TM], b[2][TN];
+    auto fetch = [&](auto set, int step) RSVD_INLINE {
+      constexpr int S = decltype(set)::value;
+      const int p = 32 * step, pr = p % W.rp + 8 * kq;
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const int64_t n = n1 + j * 16 + r16;
+        b[S][j] = factor8(E, n < P.N ? n : P.N - 1, pr);
+      }
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const int64_t m = m1 + i * 16 + r16;
+        a[S][i] = *reinterpret_cast<const u32x4 *>(E.t + (m < P.M ? m : P.M - 1) * E.parts * E.rp + p + 8 * kq);
+      }
+    };
+    auto multiply = [&](auto set) RSVD_INLINE {
+      constexpr int S = decltype(set)::value;
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) val[i][j] = mfma_bf16(b[S][j], a[S][i], val[i][j]);
+    };
+    fetch(std::integral_constant<int, 0>(), 0);
 #pragma unroll 1
-  for (int p = 0, pr = 8 * kq; p < W.parts * W.rp; p += 32, pr = pr + 32 < E.rp ? pr + 32 : 8 * kq) {
-    u32x4 b[TN];
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int64_t n = n1 + j * 16 + r16;
-      b[j] = factor8(E, n < P.N ? n : P.N - 1, pr);
-    }
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int64_t m = m1 + i * 16 + r16;
-      const u32x4 a = *reinterpret_cast<const u32x4 *>(E.t + (m < P.M ? m : P.M - 1) * E.parts * E.rp + p + 8 * kq);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) val[i][j] = mfma_bf16(b[j], a, val[i][j]);
+    for (int step = 0; step < steps; step += 2) {
+      if (step + 1 < steps) fetch(std::integral_constant<int, 1>(), step + 1);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(std::integral_constant<int, 0>());
+      __builtin_amdgcn_sched_barrier(0);
+      if (step + 1 >= steps) break;
+      if (step + 2 < steps) fetch(std::integral_constant<int, 0>(), step + 2);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(std::integral_constant<int, 1>());
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
   if (W.bias != nullptr) {
@@ -140,7 +177,9 @@ __device__ __forceinline__ void finish_tile(const TileParams &P, acc_t (&acc)[TM
       }
     }
   }
-  store_blocks(W, P.M, P.N, val, m1, n1, lane, lds);
+  if (W.type == RSVD_X_F32) store_blocks<RSVD_X_F32>(W, P.M, P.N, val, m1, n1, lane, lds);
+  else if (W.type == RSVD_X_BF16) store_blocks<RSVD_X_BF16>(W, P.M, P.N, val, m1, n1, lane, lds);
+  else store_blocks<RSVD_X_F16>(W, P.M, P.N, val, m1, n1, lane, lds);
 }
 
 // The parts of sums over k, added in their order, and the rest of the epilogue.

@@ -107,13 +107,14 @@ __device__ __forceinline__ float bf16_high(unsigned pair) { return __uint_as_flo
 // The parts of two numbers as bf16 numbers, the largest first, each the rounded rest of the ones before: three hold every fp32
 // number, two every fp16 number and any other to 2^-17 of itself.  Numbers that round to infinity are cut off instead; an infinity
 // or NaN has zeros behind its first part.
-template <int PARTS> __device__ __forceinline__ void bf16_parts2(float a, float b, unsigned (&p)[PARTS]) {
+// CHECK = false: an infinity has NaN behind its first part, and no finite number may round to one.
+template <int PARTS, bool CHECK = true> __device__ __forceinline__ void bf16_parts2(float a, float b, unsigned (&p)[PARTS]) {
 #pragma unroll
   for (int s = 0; s < PARTS; ++s) {
     p[s] = bf16_pair(a, b);
     if (s + 1 < PARTS) {
       float ra = a - bf16_low(p[s]), rb = b - bf16_high(p[s]);
-      if (s == 0 && ((p[0] & 0x7f80u) == 0x7f80u || (p[0] & 0x7f800000u) == 0x7f800000u)) {
+      if (CHECK && s == 0 && ((p[0] & 0x7f80u) == 0x7f80u || (p[0] & 0x7f800000u) == 0x7f800000u)) {
         const unsigned ua = __float_as_uint(a), ub = __float_as_uint(b);
         if ((p[0] & 0x7f80u) == 0x7f80u) {
           const bool finite = (ua & 0x7f800000u) != 0x7f800000u;
@@ -133,7 +134,7 @@ template <int PARTS> __device__ __forceinline__ void bf16_parts2(float a, float 
 }
 
 // Operands of the bf16 matrix instruction out of eight numbers, the largest part first.
-template <int XT> __device__ __forceinline__ void split_operand(const Raw8<XT> &v, u32x4 (&x)[XTraits<XT>::PARTS]) {
+template <int XT, bool CHECK = true> __device__ __forceinline__ void split_operand(const Raw8<XT> &v, u32x4 (&x)[XTraits<XT>::PARTS]) {
   constexpr int PARTS = XTraits<XT>::PARTS;
   if constexpr (XT == RSVD_X_BF16) {
     x[0] = v.w[0];
@@ -146,7 +147,7 @@ template <int XT> __device__ __forceinline__ void split_operand(const Raw8<XT> &
       } else {
         const unsigned pair = v.w[0][e];
         const f16x2 h = __builtin_bit_cast(f16x2, pair);
-        bf16_parts2<PARTS>((float)h[0], (float)h[1], p);
+        bf16_parts2<PARTS, CHECK>((float)h[0], (float)h[1], p);
       }
 #pragma unroll
       for (int q = 0; q < PARTS; ++q) x[q][e] = p[q];

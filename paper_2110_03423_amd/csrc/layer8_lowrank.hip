@@ -3,6 +3,8 @@
 // X is read once and is most of what there is to read, so a workgroup takes all ranks (up to 128 at a time) of its tokens.  X goes straight
 // from memory into the matrix instructions, split into bf16 numbers on the way (one for bf16, two for fp16, three for fp32: exact); F goes
 // through LDS, once for the four wavefronts.  Sums over ranges of k are left in fp32 for whoever needs t next to add up.
+#include <type_traits>
+
 #include "layer8_epilogue.hpp"
 #include "layer8_rows.hpp"
 
@@ -17,35 +19,56 @@ struct LowrankParams {
 };
 
 // ---------------------------------------------------------------- many tokens
-// 64 tokens a workgroup, sixteen a wavefront, 16 RB ranks; k-steps of 64; those of F are loaded one ahead, those of X, which come
-// from further away, two.
-template <int XT, int RB> __device__ __forceinline__ void lowrank_group(const LowrankParams &P, int group, char (*tile)[16 * RB * 128]) {
+// 64 TB tokens a workgroup, sixteen TB a wavefront, 16 RB ranks; k-steps of 64; those of F are loaded one ahead, those of X, which come
+// from further away, two.  CHECK: whether infinities are looked for, which a product of rows that are NaN with one need not.
+template <int XT, int RB, int TB, bool CHECK> __device__ __forceinline__ void lowrank_group(const LowrankParams &P, int group, char (*tile)[16 * RB * 128]) {
   constexpr int PARTS = XTraits<XT>::PARTS, ROWS = 16 * RB, NF = (ROWS * 8 + 255) / 256;      // 16-byte pieces of a k-step of F per thread
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
   const int p0 = group % P.rank_tiles * 128;
   group /= P.rank_tiles;
   const int split = group % P.splits;      // (workgroups of an XCD share a range of F where there are eight)
-  const int64_t t0 = (int64_t)(group / P.splits) * 64 + 16 * wave;
+  const int64_t t0 = (int64_t)(group / P.splits) * (64 * TB) + 16 * TB * wave;
   const int64_t k0 = split * P.k_per_split, k1 = k0 + P.k_per_split < P.n ? k0 + P.k_per_split : P.n;
-  const int64_t token = t0 + r16 < P.tokens ? t0 + r16 : P.tokens - 1;
-  const char *x = P.X + token * P.ldx * XTraits<XT>::SIZE;
-  f32x4 acc[RB];
+  const char *x[TB];
 #pragma unroll
-  for (int j = 0; j < RB; ++j) acc[j] = (f32x4)0.f;
+  for (int i = 0; i < TB; ++i) {
+    const int64_t token = t0 + 16 * i + r16;
+    x[i] = P.X + (token < P.tokens ? token : P.tokens - 1) * P.ldx * XTraits<XT>::SIZE;
+  }
+  f32x4 acc[TB][RB];
+#pragma unroll
+  for (int i = 0; i < TB; ++i)
+#pragma unroll
+    for (int j = 0; j < RB; ++j) acc[i][j] = (f32x4)0.f;
 
-  Raw8<XT> xa[2], xb[2];
+  Raw8<XT> xa[TB][2], xb[TB][2];
   u32x4 fv[NF];
-  auto load_x = [&](int64_t k, Raw8<XT> (&v)[2]) RSVD_INLINE {
+  // (whole k-steps without a look at each lane's end: a branch for every load would keep them from being under way together)
+  auto load_x = [&](int64_t k, Raw8<XT> (&v)[TB][2]) RSVD_INLINE {
+    auto all = [&](auto whole) RSVD_INLINE {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) v[h] = raw_load8<XT>(x + (k + 32 * h + 8 * kq) * XTraits<XT>::SIZE, k1 - (k + 32 * h + 8 * kq));
+      for (int i = 0; i < TB; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int64_t at = k + 16 * kq + 8 * h;
+          v[i][h] = raw_load8<XT>(x[i] + at * XTraits<XT>::SIZE, decltype(whole)::value ? 8 : k1 - at);
+        }
+    };
+    if (k + 64 <= k1) all(std::true_type());
+    else all(std::false_type());
   };
   auto load_f = [&](int64_t k) RSVD_INLINE {
+    auto all = [&](auto whole) RSVD_INLINE {
 #pragma unroll
-    for (int i = 0; i < NF; ++i) {
-      const int q = tid + 256 * i, row = p0 + (q >> 3);
-      if (ROWS * 8 % 256 == 0 || q < ROWS * 8) fv[i] = halves8(P.F + (int64_t)(row < P.r ? row : P.r - 1) * P.ldf + k + 8 * (q & 7), k1 - k - 8 * (q & 7));
-    }
+      for (int i = 0; i < NF; ++i) {
+        const int q = tid + 256 * i, row = p0 + (q >> 3);
+        if (ROWS * 8 % 256 == 0 || q < ROWS * 8)
+          fv[i] = halves8(P.F + (int64_t)(row < P.r ? row : P.r - 1) * P.ldf + k + 8 * (q & 7), decltype(whole)::value ? 8 : k1 - k - 8 * (q & 7));
+      }
+    };
+    if (k + 64 <= k1) all(std::true_type());
+    else all(std::false_type());
   };
   auto place = [&](int buf) RSVD_INLINE {
 #pragma unroll
@@ -54,20 +77,28 @@ template <int XT, int RB> __device__ __forceinline__ void lowrank_group(const Lo
       if (ROWS * 8 % 256 == 0 || q < ROWS * 8) *reinterpret_cast<u32x4 *>(&tile[buf][row * 128 + (((q & 7) ^ (row & 7)) << 4)]) = fv[i];
     }
   };
-  auto step = [&](int64_t k, int buf, Raw8<XT> (&v)[2]) RSVD_INLINE {
-    u32x4 a[2][PARTS];
+  auto step = [&](int64_t k, int buf, Raw8<XT> (&v)[TB][2]) RSVD_INLINE {
+    u32x4 a[TB][2][PARTS];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) split_operand<XT>(v[h], a[h]);
-    __syncthreads();
+    for (int i = 0; i < TB; ++i)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) split_operand<XT, CHECK>(v[i][h], a[i][h]);
+    // (a barrier that leaves the loads in flight, which __syncthreads() would not)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xc07f);                  // LDS
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     if (k + 64 < k1) load_f(k + 64);
     if (k + 128 < k1) load_x(k + 128, v);
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int j = 0; j < RB; ++j) {
-        const u32x4 f = *reinterpret_cast<const u32x4 *>(&tile[buf][(16 * j + r16) * 128 + (((4 * h + kq) ^ (r16 & 7)) << 4)]);
+        const u32x4 f = *reinterpret_cast<const u32x4 *>(&tile[buf][(16 * j + r16) * 128 + (((2 * kq + h) ^ (r16 & 7)) << 4)]);
 #pragma unroll
-        for (int q = PARTS - 1; q >= 0; --q) acc[j] = mfma_bf16(f, a[h][q], acc[j]);
+        for (int q = PARTS - 1; q >= 0; --q)
+#pragma unroll
+          for (int i = 0; i < TB; ++i) acc[i][j] = mfma_bf16(f, a[i][h][q], acc[i][j]);
       }
     if (k + 64 < k1) place(buf ^ 1);
   };
@@ -81,21 +112,26 @@ template <int XT, int RB> __device__ __forceinline__ void lowrank_group(const Lo
     step(k, 0, xa);
     if (k + 64 < k1) step(k + 64, 1, xb);
   }
-  if (t0 + r16 >= P.tokens) return;
-  float *out = P.sums + ((int64_t)split * P.tokens + t0 + r16) * P.rp + p0;
 #pragma unroll
-  for (int j = 0; j < RB; ++j) {
-    const int p = 16 * j + 4 * kq;
-    if (p0 + p >= P.rp) continue;
+  for (int i = 0; i < TB; ++i) {
+    const int64_t token = t0 + 16 * i + r16;
+    if (token >= P.tokens) continue;
+    float *out = P.sums + ((int64_t)split * P.tokens + token) * P.rp + p0;
 #pragma unroll
-    for (int v = 0; v < 4; ++v) acc[j][v] = p0 + p + v < P.r ? acc[j][v] : 0.f;
-    *reinterpret_cast<f32x4 *>(out + p) = acc[j];
+    for (int j = 0; j < RB; ++j) {
+      const int p = 16 * j + 4 * kq;
+      if (p0 + p >= P.rp) continue;
+      f32x4 v = acc[i][j];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = p0 + p + e < P.r ? v[e] : 0.f;
+      *reinterpret_cast<f32x4 *>(out + p) = v;
+    }
   }
 }
 
-template <int XT, int RB> __global__ __launch_bounds__(256, 2) void lowrank_kernel(const LowrankParams P) {
+template <int XT, int RB, int TB> __global__ __launch_bounds__(256, 2) void lowrank_kernel(const LowrankParams P) {
   __shared__ __attribute__((aligned(16))) char tile[2][16 * RB * 128];
-  lowrank_group<XT, RB>(P, (int)blockIdx.x, tile);
+  lowrank_group<XT, RB, TB, XT == RSVD_X_F32>(P, (int)blockIdx.x, tile);
 }
 
 // The same, and behind it the operands of the gradients: three things that have nothing to do with each other, in one launch.
@@ -108,7 +144,7 @@ template <int XT, int RB> __global__ __launch_bounds__(256, 2) void grad_front_k
   __shared__ __attribute__((aligned(16))) char tile[2][16 * RB * 128];
   int64_t group = blockIdx.x;
   if (group < P.lowrank_groups) {
-    lowrank_group<XT, RB>(P.L, (int)group, tile);
+    lowrank_group<XT, RB, 1, true>(P.L, (int)group, tile);
     return;
   }
   group -= P.lowrank_groups;
@@ -199,21 +235,27 @@ static LowrankParams lowrank_params(const rsvd_ctx *ctx, int64_t tokens, int64_t
   return P;
 }
 
-static int64_t lowrank_groups(const LowrankParams &P) { return ceil_div(P.tokens, 64) * P.splits * P.rank_tiles; }
+static int64_t lowrank_groups(const LowrankParams &P, int tb) { return ceil_div(P.tokens, 64 * tb) * P.splits * P.rank_tiles; }
 
-template <int XT> static void lowrank_typed(hipStream_t s, const LowrankParams &P) {
-  const dim3 grid((unsigned)lowrank_groups(P));
-  if (P.r <= 32) hipLaunchKernelGGL((lowrank_kernel<XT, 2>), grid, dim3(256), 0, s, P);
-  else if (P.r <= 64) hipLaunchKernelGGL((lowrank_kernel<XT, 4>), grid, dim3(256), 0, s, P);
-  else hipLaunchKernelGGL((lowrank_kernel<XT, 8>), grid, dim3(256), 0, s, P);
+// Two blocks of tokens a wavefront read F half as often, where that leaves every CU two workgroups: 16384 x 16384 fp16, 128 ranks, takes 165 us
+// with two and 179 with one.
+template <int XT, int TB> static void lowrank_typed(hipStream_t s, const LowrankParams &P) {
+  const dim3 grid((unsigned)lowrank_groups(P, TB));
+  if (P.r <= 32) hipLaunchKernelGGL((lowrank_kernel<XT, 2, TB>), grid, dim3(256), 0, s, P);
+  else if (P.r <= 64) hipLaunchKernelGGL((lowrank_kernel<XT, 4, TB>), grid, dim3(256), 0, s, P);
+  else hipLaunchKernelGGL((lowrank_kernel<XT, 8, TB>), grid, dim3(256), 0, s, P);
+}
+template <int XT> static void lowrank_blocks(rsvd_ctx *ctx, hipStream_t s, const LowrankParams &P) {
+  if (lowrank_groups(P, 2) >= 2 * ctx->cu_count) lowrank_typed<XT, 2>(s, P);
+  else lowrank_typed<XT, 1>(s, P);
 }
 
 hipError_t lowrank_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, int64_t r, const void *X, int64_t ldx,
                           const void *F, int64_t ldf, float *sums) {
   const LowrankParams P = lowrank_params(ctx, tokens, n, r, X, ldx, F, ldf, sums);
-  if (type == RSVD_X_BF16) lowrank_typed<RSVD_X_BF16>(s, P);
-  else if (type == RSVD_X_F16) lowrank_typed<RSVD_X_F16>(s, P);
-  else lowrank_typed<RSVD_X_F32>(s, P);
+  if (type == RSVD_X_BF16) lowrank_blocks<RSVD_X_BF16>(ctx, s, P);
+  else if (type == RSVD_X_F16) lowrank_blocks<RSVD_X_F16>(ctx, s, P);
+  else lowrank_blocks<RSVD_X_F32>(ctx, s, P);
   return hipGetLastError();
 }
 
@@ -230,7 +272,7 @@ hipError_t grad_front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int6
                              uint16_t *plane, int64_t width) {
   GradFrontParams P;
   P.L = lowrank_params(ctx, tokens, m, r < 1 ? 1 : r, dY, lddy, F, ldf, sums);
-  P.lowrank_groups = r > 0 ? lowrank_groups(P.L) : 0;
+  P.lowrank_groups = r > 0 ? lowrank_groups(P.L, 1) : 0;
   P.S = SplitParams{(const char *)dY, lddy, tokens, m, dy_factor, planes, planes_width, 0};
   if (planes != nullptr) P.S.groups = ceil_div(tokens * (planes_width / 8), 256);
   P.W = WidenParams{codes, ldc, factor, powers, ldp, rows, n, plane, width, ceil_div(rows * ceil_div(n, 16), 256)};

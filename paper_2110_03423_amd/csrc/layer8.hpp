@@ -156,6 +156,9 @@ template <int XT, bool CHECK = true> __device__ __forceinline__ void split_opera
 }
 #endif
 
+// Leading dimensions that rows in tiles may have: 32-bit offsets inside a tile.
+constexpr int64_t kMaxLd = (int64_t)1 << 23;
+
 // ---------------------------------------------------------------- layer8_rows.hip
 // Rows of X (rows x n) to codes with a scale each; a row of codes is written up to `width` (>= n, a multiple of 8) with zeros behind n.
 // sums != NULL: t is joined on the way (lowrank_join_launch).
@@ -166,8 +169,6 @@ hipError_t keep8_save_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int
                              int64_t ldc, uint8_t *powers, int64_t ldp);
 hipError_t keep8_load_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, const int8_t *codes, int64_t ldc,
                              const uint8_t *powers, int64_t ldp, void *X, int64_t ldx);
-// out[j] (+)= sum over b of sums[b][j]
-hipError_t add_sums_launch(hipStream_t s, int64_t blocks, int64_t n, const float *sums, float *out, int accumulate);
 hipError_t fill_zero_launch(hipStream_t s, int64_t rows, int64_t cols, float *out, int64_t ld);
 
 // ---------------------------------------------------------------- layer8_lowrank.hip
@@ -184,7 +185,7 @@ hipError_t front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t t
                         const void *F, int64_t ldf, float *sums, int8_t *codes, int64_t ldq, int64_t width, float *scale);
 // The operands of kn_launch for a gradient, and lowrank_launch for dY (r = 0: without): planes[q][token][0 .. planes_width) the bf16 parts of dY
 // (tokens x m, times dy_factor_j or NULL), zeros from m on (planes NULL: not wanted); plane[row][0 .. width) the codes (rows x n) as bf16 numbers, multiplied by
-// factor_row (NULL: as they are) or by the powers of two of kept activations.  Widths are m and n up to a multiple of 8.
+// factor_row (NULL: as they are) or by the powers of two of kept activations (plane NULL: not wanted).  Widths are m and n up to a multiple of 8.
 hipError_t grad_front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t m, int64_t r, const void *dY, int64_t lddy,
                              const void *F, int64_t ldf, float *sums, const float *dy_factor, uint16_t *planes, int64_t planes_width,
                              int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const float *factor, const uint8_t *powers, int64_t ldp,
@@ -219,18 +220,26 @@ hipError_t nt_launch(rsvd_ctx *ctx, hipStream_t s, const NtDesc &d);
 // ---------------------------------------------------------------- layer8_grad.hip
 // C (M x N) = sum over k < K of A_mk B_kn of bf16 numbers, A a sum of `planes` matrices (`plane` bytes apart, the largest first), B with rows of n.
 // a_krows: A is stored K x M, else M x K.  Rows of both may be read in 16-byte pieces as far as these hold an element.
+// What codes are multiplied by: powers of two of kept activations (row k, blocks of 32 columns), or a factor for each row, or nothing.
+struct CodeUnits {
+  const float *factor = nullptr;
+  const uint8_t *powers = nullptr; int64_t ldp = 0;
+};
 struct KnDesc {
   int64_t M = 0, N = 0, K = 0;
   bool a_krows = false;
   const uint16_t *A = nullptr; int64_t lda = 0;            // bytes
   int planes = 1; int64_t plane = 0;
   const uint16_t *B = nullptr; int64_t ldb = 0;            // bytes
-  float *sums = nullptr;                                   // a_krows: receives kn_sum_rows() partial sums of A over k, M each; or NULL
+  const int8_t *codes = nullptr; int64_t ldc = 0;          // in the place of B, where kn_takes_codes(): codes (K x N)
+  CodeUnits units;
+  float *sums = nullptr, *sums_out = nullptr;              // a_krows: place for kn_sum_rows() parts of the sums of A over k, M each, and for the sums; or NULL
   Layer8Out out;
   float *partial = nullptr; size_t partial_bytes = 0;
 };
 size_t kn_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, bool lowrank);
 int64_t kn_sum_rows(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes);
+bool kn_takes_codes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, int64_t ldc, int64_t ldp);
 hipError_t kn_launch(rsvd_ctx *ctx, hipStream_t s, const KnDesc &d);
 
 // ---------------------------------------------------------------- layer8_few.hip

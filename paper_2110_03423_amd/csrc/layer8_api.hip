@@ -22,8 +22,8 @@ bool valid_xtype(rsvd_xtype t) { return t == RSVD_X_BF16 || t == RSVD_X_F16 || t
 bool valid_codes(const void *p) { return p != nullptr && ((uintptr_t)p & 15) == 0; }
 bool element_aligned(const void *p, int64_t size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) == 0; }
 
-// Sizes that the kernels index: rows of up to 2^23 elements (32-bit offsets inside a tile of rows), 2^31 rows.
-constexpr int64_t kMaxLd = (int64_t)1 << 23, kMaxTokens = (int64_t)1 << 22;
+// (sums over tokens and indexes of workgroups)
+constexpr int64_t kMaxTokens = (int64_t)1 << 22;
 
 // Sums over ranges of k times ranks up to which the product of a few tokens takes them as they are (eight pieces of 32 for each of its
 // wavefronts); beyond, a launch that joins them first is less.
@@ -249,12 +249,12 @@ int rsvd_q8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t t
   char *ws = (char *)workspace;
   uint16_t *a = (uint16_t *)(ws + L.a), *b = (uint16_t *)(ws + L.b), *t = (uint16_t *)(ws + L.t);
   // one part: the scale goes to the codes; several: to dY before it is split, and the codes stay exact
-  const bool single = L.planes == 1, direct = takes_rows(type, dY, m, lddy);
+  const bool single = L.planes == 1, direct = takes_rows(type, dY, m, lddy), as_codes = kn_takes_codes(ctx, tokens, n, m, L.planes, ldq, 0);
   {
     ProfScope ps(ctx, s, PK_SMALL);
     float *sums = (float *)(ws + L.sums);
     RSVD_TRY(grad_front_launch(ctx, s, type, tokens, m, r, dY, lddy, Ut, ldut, sums, single ? nullptr : scale, direct ? nullptr : a, L.width,
-                               m, n, codes, ldq, single ? scale : nullptr, nullptr, 0, b, L.b_width),
+                               m, n, codes, ldq, single ? scale : nullptr, nullptr, 0, as_codes ? nullptr : b, L.b_width),
              "operands of the gradient");
     if (r > 0) RSVD_TRY(lowrank_join_launch(s, sums, L.splits, tokens, r, lowrank_parts(type), t), "low-rank term");
   }
@@ -262,6 +262,8 @@ int rsvd_q8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t t
   d.M = tokens; d.N = n; d.K = m;
   d.A = direct ? (const uint16_t *)dY : a; d.lda = (direct ? lddy : L.width) * 2; d.planes = L.planes; d.plane = tokens * L.width * 2;
   d.B = b; d.ldb = L.b_width * 2;
+  if (as_codes) d.codes = codes;
+  d.ldc = ldq; d.units.factor = single ? scale : nullptr;
   d.out.t = t; d.out.parts = lowrank_parts(type); d.out.G = (const uint16_t *)V; d.out.ldg = ldv; d.out.r = (int)r;
   d.out.C = dX; d.out.ldc = lddx; d.out.type = type;
   d.partial = (float *)(ws + L.partial); d.partial_bytes = L.partial_bytes;
@@ -343,11 +345,11 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
   char *ws = (char *)workspace;
   uint16_t *a = (uint16_t *)(ws + L.a), *b = (uint16_t *)(ws + L.b);
   float *sums = db != nullptr ? (float *)(ws + L.sums) : nullptr;
-  const bool direct = takes_rows(type, dY, m, lddy);
+  const bool direct = takes_rows(type, dY, m, lddy), as_codes = kn_takes_codes(ctx, m, n, tokens, L.planes, ldc, ldp);
   {
     ProfScope ps(ctx, s, PK_SMALL);
     RSVD_TRY(grad_front_launch(ctx, s, type, tokens, m, 0, dY, lddy, nullptr, 0, nullptr, nullptr, direct ? nullptr : a, L.width, tokens, n, codes,
-                               ldc, nullptr, powers, ldp, b, L.b_width),
+                               ldc, nullptr, powers, ldp, as_codes ? nullptr : b, L.b_width),
              "operands of the gradient");
   }
   KnDesc d;
@@ -355,17 +357,13 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
   d.a_krows = true;
   d.A = direct ? (const uint16_t *)dY : a; d.lda = (direct ? lddy : L.width) * 2; d.planes = L.planes; d.plane = tokens * L.width * 2;
   d.B = b; d.ldb = L.b_width * 2;
-  d.sums = sums;
+  if (as_codes) d.codes = codes;
+  d.ldc = ldc; d.units.powers = powers; d.units.ldp = ldp;
+  d.sums = sums; d.sums_out = db;
   d.out.C = dW; d.out.ldc = lddw; d.out.type = RSVD_X_F32; d.out.accumulate = accumulate;
   d.partial = (float *)(ws + L.partial); d.partial_bytes = L.partial_bytes;
-  {
-    ProfScope ps(ctx, s, PK_GEMM_ATX);
-    RSVD_TRY(kn_launch(ctx, s, d), "gradient of a weight");
-  }
-  if (db != nullptr) {
-    ProfScope ps(ctx, s, PK_SMALL);
-    RSVD_TRY(add_sums_launch(s, kn_sum_rows(ctx, m, n, tokens, L.planes), m, sums, db, accumulate), "column sums");
-  }
+  ProfScope ps(ctx, s, PK_GEMM_ATX);
+  RSVD_TRY(kn_launch(ctx, s, d), "gradient of a weight");
   return RSVD_OK;
 }
 

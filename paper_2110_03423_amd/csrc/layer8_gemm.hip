@@ -131,6 +131,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void nt_kernel(c
   finish_tile<TM, TN, BM == 256>(P.T, acc, split, m0 + wm0, n0 + wn0, last_lane, reinterpret_cast<float *>(nt_lds + wave * finish_lds<TN>()));
 }
 
+__global__ __launch_bounds__(256) void nt_reduce_kernel(const ReduceParams P) { reduce_group<true>(P, blockIdx.x); }
+
 // ---------------------------------------------------------------- choice of tile and of the ranges of k
 // The time of each tile and number of ranges is estimated, and the least taken.  Measured with both product kernels (4096 to 8192 k, one to four
 // workgroups on a CU): a k-tile takes a CU 0.22, 0.55 and 2.05 us for each workgroup of 64, 128 and 256 rows and columns, but no less than 0.33,
@@ -179,7 +181,10 @@ hipError_t nt_launch(rsvd_ctx *ctx, hipStream_t s, const NtDesc &d) {
   if (c.bm == 256) e = nt_run<256, 256, 2, 2>(s, P);
   else if (c.bm == 128) e = nt_run<128, 128, 2, 2>(s, P);
   else e = nt_run<64, 64, 2, 2>(s, P);
-  return e == hipSuccess ? tile_reduce<true>(s, P.T) : e;
+  const ReduceParams R = reduce_params(P.T);
+  if (e != hipSuccess || R.groups == 0) return e;
+  hipLaunchKernelGGL(nt_reduce_kernel, dim3((unsigned)R.groups), dim3(256), 0, s, R);
+  return hipGetLastError();
 }
 
 }  // namespace rsvd

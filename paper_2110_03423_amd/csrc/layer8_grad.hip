@@ -8,6 +8,10 @@
 // the tile after next as soon as it has been written.  (Loads straight to LDS: the compiler lets the transposing loads wait for all of them,
 // wherever they go.)
 // Several planes of A are taken as further k, the smallest first.
+// Where few rows of tiles need it, B is taken as the 8-bit codes that it comes from and made bf16 numbers on the way to LDS.
+#include <type_traits>
+
+#include "layer8_rows.hpp"
 #include "layer8_tile.hpp"
 
 namespace rsvd {
@@ -19,6 +23,7 @@ struct KnParams {
   int planes, ktiles;                      // k-tiles of a plane
   int64_t K;
   const char *B; int64_t ldb;              // bytes
+  CodeUnits units;                         // B holds codes
   float *sums; int sum_columns;            // A_KROWS: sums of A over k by ranges, [split][sum_columns][M], or NULL
   TileParams T;
 };
@@ -62,12 +67,55 @@ template <int NT, int X, bool KROWS> struct Staged {
   }
 };
 
+// The same for codes: N pieces of sixteen codes of a row, as bf16 numbers in LDS.
+template <int NT, int X> struct StagedCodes {
+  static constexpr int ROW = X * 2, PER = X / 16, STEP = NT / PER, N = X * kKnK / 16 / NT;
+  static_assert(X * kKnK % (16 * NT) == 0 && STEP % 16 == 0, "whole rounds; a thread's rows have their pieces exchanged alike");
+  u32x4 reg[N];
+  unsigned unit[N];
+  uint32_t off[N], unit_off[N];
+  int place, half;
+  __device__ __forceinline__ void init(int64_t ld, int64_t left, int tid, const CodeUnits &units) {
+    const int row = tid / PER, pos = tid % PER, col = 16 * pos < left ? 16 * pos : 0;
+    half = (pos & 1) << 4;                               // (neighbours start with different halves of their pieces: other banks)
+    place = row * ROW + (krow_piece<X>(pos, row) << 5);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint32_t r = row + STEP * i;
+      off[i] = r * (uint32_t)ld + (uint32_t)col;
+      unit_off[i] = units.powers != nullptr ? r * (uint32_t)units.ldp + (uint32_t)(col >> 5) : 4 * r;
+      asm volatile("" : "+v"(off[i]), "+v"(unit_off[i]));
+    }
+  }
+  // k: the first of the tile; base: its codes; what is behind the last row is read as zeros, codes and units
+  __device__ __forceinline__ void load(int i, const char *base, int64_t ld, int k_left, const CodeUnits &units, int64_t k, int64_t n0) {
+    const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)(k_left * (uint32_t)ld), 0x00027000);
+    reg[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(all, off[i], 0, 0));
+    if (units.powers != nullptr) {
+      const __amdgpu_buffer_rsrc_t u =
+          __builtin_amdgcn_make_buffer_rsrc((void *)(units.powers + k * units.ldp + n0 / 32), 0, (int)(k_left * (uint32_t)units.ldp), 0x00027000);
+      unit[i] = __builtin_amdgcn_raw_buffer_load_b8(u, unit_off[i], 0, 0);
+    } else if (units.factor != nullptr) {
+      const __amdgpu_buffer_rsrc_t u = __builtin_amdgcn_make_buffer_rsrc((void *)(units.factor + k), 0, k_left * 4, 0x00027000);
+      unit[i] = __builtin_amdgcn_raw_buffer_load_b32(u, unit_off[i], 0, 0);
+    }
+  }
+  __device__ __forceinline__ void write(int i, char *lds, const CodeUnits &units) const {
+    const float by = units.powers != nullptr ? kept_unit(unit[i]) : units.factor != nullptr ? __uint_as_float(unit[i]) : 1.f;
+    u32x4 p[2];
+    widen16(reg[i], by, p);
+    char *at = lds + place + i * STEP * ROW;
+    *reinterpret_cast<u32x4 *>(at + half) = half ? p[1] : p[0];
+    *reinterpret_cast<u32x4 *>(at + (half ^ 16)) = half ? p[0] : p[1];
+  }
+};
+
 template <int BM, int BN> struct KnCfg {
   static constexpr int A = BM * 128, B = BN * 128, STAGE = A + B;
   static constexpr size_t lds = 2 * (size_t)STAGE;      // (more than the wavefronts need in the end)
 };
 
-template <bool A_KROWS, int BM, int BN, int WGM, int WGN>
+template <bool A_KROWS, bool CODES, int BM, int BN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P) {
   constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = KnCfg<BM, BN>::STAGE, A_BYTES = KnCfg<BM, BN>::A;
   extern __shared__ __attribute__((aligned(16))) char kn_lds[];
@@ -93,18 +141,21 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
   int next_kt = __builtin_amdgcn_readfirstlane(kt_begin % P.ktiles), next_plane = __builtin_amdgcn_readfirstlane(kt_begin / P.ktiles);
   int64_t next_k = (int64_t)next_kt * kKnK;
   int next_left = (int)(P.K - next_k < kKnK ? P.K - next_k : kKnK);      // k of it that exist
-  const char *const a_first = P.A + (A_KROWS ? m0 * 2 : m0 * P.lda), *const b_first = P.B + n0 * 2;
+  const char *const a_first = P.A + (A_KROWS ? m0 * 2 : m0 * P.lda), *const b_first = P.B + n0 * (CODES ? 1 : 2);
   Staged<NT, BM, A_KROWS> sa;
-  Staged<NT, BN, true> sb;
+  std::conditional_t<CODES, StagedCodes<NT, BN>, Staged<NT, BN, true>> sb;
   sa.init(P.lda, P.T.M - m0, tid);
-  sb.init(P.ldb, P.T.N - n0, tid);
+  if constexpr (CODES) sb.init(P.ldb, P.T.N - n0, tid, P.units);
+  else sb.init(P.ldb, P.T.N - n0, tid);
   constexpr int NA = decltype(sa)::N, PIECES = NA + decltype(sb)::N;
   auto load = [&](int p) RSVD_INLINE {
     if (p < NA) sa.load(p, a_first + (P.planes - 1 - next_plane) * P.plane + (A_KROWS ? next_k * P.lda : next_k * 2), P.lda, next_left);
+    else if constexpr (CODES) sb.load(p - NA, b_first + next_k * P.ldb, P.ldb, next_left, P.units, next_k, n0);
     else sb.load(p - NA, b_first + next_k * P.ldb, P.ldb, next_left);
   };
   auto write = [&](int p, int buf) RSVD_INLINE {
     if (p < NA) sa.write(p, kn_lds + buf * STAGE);
+    else if constexpr (CODES) sb.write(p - NA, kn_lds + buf * STAGE + A_BYTES, P.units);
     else sb.write(p - NA, kn_lds + buf * STAGE + A_BYTES);
   };
   auto advance = [&]() RSVD_INLINE {                    // (behind the last tile of this workgroup's range: loads stay inside the operands)
@@ -228,6 +279,34 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
   finish_tile<TM, TN, BM == 256>(P.T, acc, split, m0 + wm0, n0 + wn0, last_lane, reinterpret_cast<float *>(kn_lds + wave * finish_lds<TN>()));
 }
 
+// What is left to add up: ranges of k, and behind them sums of A, sixteen columns a workgroup with sixteen threads for the rows of each.
+struct SumsParams { const float *sums; int64_t blocks, n; float *out; int accumulate; };
+__global__ __launch_bounds__(256) void kn_end_kernel(const ReduceParams R, const SumsParams P) {
+  if ((int64_t)blockIdx.x < R.groups) {
+    reduce_group<false>(R, blockIdx.x);
+    return;
+  }
+  const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
+  const int64_t j = ((int64_t)blockIdx.x - R.groups) * 16 + col;
+  __shared__ float parts[16][17];
+  float sum = 0.f;
+  if (j < P.n) {
+    for (int64_t b = part; b < P.blocks; b += 64) {
+      float v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) v[u] = b + 16 * u < P.blocks ? P.sums[(b + 16 * u) * P.n + j] : 0.f;
+      sum += (v[0] + v[1]) + (v[2] + v[3]);
+    }
+  }
+  parts[part][col] = sum;
+  __syncthreads();
+  if (threadIdx.x >= 16 || j >= P.n) return;
+  sum = 0.f;
+#pragma unroll
+  for (int p = 0; p < 16; ++p) sum += parts[p][col];
+  P.out[j] = P.accumulate ? P.out[j] + sum : sum;
+}
+
 size_t kn_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, bool lowrank) {
   return tile_partial_bytes(ctx, M, N, ceil_div(K, kKnK) * planes, lowrank);
 }
@@ -238,22 +317,31 @@ int64_t kn_sum_rows(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int pl
   return c.splits * kn_sum_columns(N, c.bn);
 }
 
-template <bool A_KROWS, int BM, int BN, int WGM, int WGN> static hipError_t kn_run(hipStream_t s, const KnParams &P) {
-  hipLaunchKernelGGL((kn_kernel<A_KROWS, BM, BN, WGM, WGN>), dim3(tile_groups(P.T)), dim3(64 * WGM * WGN), (KnCfg<BM, BN>::lds), s, P);
+template <bool A_KROWS, bool CODES, int BM, int BN, int WGM, int WGN> static hipError_t kn_run(hipStream_t s, const KnParams &P) {
+  hipLaunchKernelGGL((kn_kernel<A_KROWS, CODES, BM, BN, WGM, WGN>), dim3(tile_groups(P.T)), dim3(64 * WGM * WGN), (KnCfg<BM, BN>::lds), s, P);
   return hipGetLastError();
 }
 
-template <bool A_KROWS> static hipError_t kn_run_tile(hipStream_t s, const KnParams &P, int bm) {
-  if (bm == 256) return kn_run<A_KROWS, 256, 256, 2, 4>(s, P);
-  if (bm == 128) return kn_run<A_KROWS, 128, 128, 2, 2>(s, P);
-  return kn_run<A_KROWS, 64, 64, 2, 2>(s, P);
+template <bool A_KROWS> static hipError_t kn_run_tile(hipStream_t s, const KnParams &P, int bm, bool codes) {
+  if (bm == 256) return kn_run<A_KROWS, false, 256, 256, 2, 4>(s, P);
+  if (codes) return bm == 128 ? kn_run<A_KROWS, true, 128, 128, 2, 2>(s, P) : kn_run<A_KROWS, true, 64, 64, 2, 2>(s, P);
+  return bm == 128 ? kn_run<A_KROWS, false, 128, 128, 2, 2>(s, P) : kn_run<A_KROWS, false, 64, 64, 2, 2>(s, P);
+}
+
+// Every row of tiles makes bf16 numbers of all the codes again, and every plane; a matrix of them is made once and read twice as long.  Rows of tiles
+// times planes up to which the codes are taken as they are, measured as codes / matrix: 4096 x 4096 codes with 64 columns of dY, bf16 (1) 21 / 34 us,
+// 128 (2) 26 / 35, 256 (4) 37 / 42, 512 (8) 57 / 52; 64 of fp32 (3) 33 / 41, 128 (6) 50 / 49; 1000 x 1000 with 1000 of fp32 (48) 39 / 31.
+constexpr int64_t kCodeRows = 4;
+bool kn_takes_codes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, int64_t ldc, int64_t ldp) {
+  const TileChoice c = tile_choose(ctx, M, N, ceil_div(K, kKnK) * planes);
+  return c.bm < 256 && ceil_div(M, c.bm) * planes <= kCodeRows && ldc <= kMaxLd && ldp <= kMaxLd;
 }
 
 hipError_t nt_init_device();
 hipError_t layer8_init_device(rsvd_ctx *) {
   hipError_t e = nt_init_device();
-  const void *wide[2] = {reinterpret_cast<const void *>(&kn_kernel<true, 256, 256, 2, 4>),
-                         reinterpret_cast<const void *>(&kn_kernel<false, 256, 256, 2, 4>)};
+  const void *wide[2] = {reinterpret_cast<const void *>(&kn_kernel<true, false, 256, 256, 2, 4>),
+                         reinterpret_cast<const void *>(&kn_kernel<false, false, 256, 256, 2, 4>)};
   for (const void *k : wide)
     if (e == hipSuccess) e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)KnCfg<256, 256>::lds);
   return e;
@@ -267,11 +355,22 @@ hipError_t kn_launch(rsvd_ctx *ctx, hipStream_t s, const KnDesc &d) {
   P.A = (const char *)d.A; P.lda = d.lda; P.plane = d.plane; P.planes = d.planes;
   P.ktiles = (int)ktiles; P.K = d.K;
   P.B = (const char *)d.B; P.ldb = d.ldb;
+  const bool codes = d.codes != nullptr;
+  if (codes) {
+    if (!kn_takes_codes(ctx, d.M, d.N, d.K, d.planes, d.ldc, d.units.ldp)) return hipErrorInvalidValue;
+    P.B = (const char *)d.codes; P.ldb = d.ldc;
+  }
+  P.units = d.units;
   P.sums = d.a_krows ? d.sums : nullptr;
   P.sum_columns = (int)kn_sum_columns(d.N, c.bn);
   P.T = tile_params(c, d.M, d.N, kt, d.partial, d.out);
-  const hipError_t e = d.a_krows ? kn_run_tile<true>(s, P, c.bm) : kn_run_tile<false>(s, P, c.bm);
-  return e == hipSuccess ? tile_reduce<false>(s, P.T) : e;
+  const hipError_t e = d.a_krows ? kn_run_tile<true>(s, P, c.bm, codes) : kn_run_tile<false>(s, P, c.bm, codes);
+  const ReduceParams R = reduce_params(P.T);
+  const SumsParams S = {P.sums, (int64_t)c.splits * P.sum_columns, d.M, d.sums_out, d.out.accumulate};
+  const int64_t groups = R.groups + (P.sums != nullptr ? ceil_div(d.M, 16) : 0);
+  if (e != hipSuccess || groups == 0) return e;
+  hipLaunchKernelGGL(kn_end_kernel, dim3((unsigned)groups), dim3(256), 0, s, R, S);
+  return hipGetLastError();
 }
 
 }  // namespace rsvd

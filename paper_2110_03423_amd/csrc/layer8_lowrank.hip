@@ -275,7 +275,8 @@ hipError_t grad_front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int6
   P.lowrank_groups = r > 0 ? lowrank_groups(P.L, 1) : 0;
   P.S = SplitParams{(const char *)dY, lddy, tokens, m, dy_factor, planes, planes_width, 0};
   if (planes != nullptr) P.S.groups = ceil_div(tokens * (planes_width / 8), 256);
-  P.W = WidenParams{codes, ldc, factor, powers, ldp, rows, n, plane, width, ceil_div(rows * ceil_div(n, 16), 256)};
+  P.W = WidenParams{codes, ldc, factor, powers, ldp, rows, n, plane, width, plane != nullptr ? ceil_div(rows * ceil_div(n, 16), 256) : 0};
+  if (P.lowrank_groups + P.S.groups + P.W.groups == 0) return hipSuccess;
   if (type == RSVD_X_BF16) grad_front_typed<RSVD_X_BF16>(s, P);
   else if (type == RSVD_X_F16) grad_front_typed<RSVD_X_F16>(s, P);
   else grad_front_typed<RSVD_X_F32>(s, P);

@@ -136,36 +136,7 @@ hipError_t keep8_load_launch(hipStream_t s, rsvd_xtype type, int64_t tokens, int
   return hipGetLastError();
 }
 
-// ---------------------------------------------------------------- sums
-// Sixteen columns a workgroup, sixteen threads for the rows of each.
-__global__ __launch_bounds__(256) void add_sums_kernel(const float *__restrict__ sums, int64_t blocks, int64_t n, float *__restrict__ out,
-                                                       int accumulate) {
-  const int col = threadIdx.x & 15, part = threadIdx.x >> 4;
-  const int64_t j = (int64_t)blockIdx.x * 16 + col;
-  __shared__ float parts[16][17];
-  float sum = 0.f;
-  if (j < n) {
-    for (int64_t b = part; b < blocks; b += 64) {
-      float v[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) v[u] = b + 16 * u < blocks ? sums[(b + 16 * u) * n + j] : 0.f;
-      sum += (v[0] + v[1]) + (v[2] + v[3]);
-    }
-  }
-  parts[part][col] = sum;
-  __syncthreads();
-  if (threadIdx.x >= 16 || j >= n) return;
-  sum = 0.f;
-#pragma unroll
-  for (int p = 0; p < 16; ++p) sum += parts[p][col];
-  out[j] = accumulate ? out[j] + sum : sum;
-}
-
-hipError_t add_sums_launch(hipStream_t s, int64_t blocks, int64_t n, const float *sums, float *out, int accumulate) {
-  hipLaunchKernelGGL(add_sums_kernel, dim3((unsigned)ceil_div(n, 16)), dim3(256), 0, s, sums, blocks, n, out, accumulate);
-  return hipGetLastError();
-}
-
+// ---------------------------------------------------------------- zeros
 __global__ __launch_bounds__(256) void fill_zero_kernel(float *__restrict__ out, int64_t rows, int64_t cols, int64_t ld) {
   for (int64_t r = blockIdx.y; r < rows; r += gridDim.y)
     for (int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x; c < cols; c += (int64_t)gridDim.x * 256) out[r * ld + c] = 0.f;

@@ -156,6 +156,18 @@ template <int XT> __device__ __forceinline__ void split_rows_group(const SplitPa
   for (int q = 0; q < PARTS; ++q) *reinterpret_cast<u32x4 *>(P.planes + q * P.rows * P.width + row * P.width + j) = out[q];
 }
 
+// Sixteen codes times `unit` as bf16 numbers.
+__device__ __forceinline__ void widen16(const u32x4 &w, float unit, u32x4 (&p)[2]) {
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const unsigned d = w[2 * h + (u >> 1)];
+      const float a = (float)((int)(d << (24 - 16 * (u & 1))) >> 24) * unit, b = (float)((int)(d << (16 - 16 * (u & 1))) >> 24) * unit;
+      p[h][u] = bf16_pair(a, b);
+    }
+}
+
 // plane[row][0 .. width): the codes of a row as bf16 numbers, multiplied by factor_row (NULL: as they are), or by the powers of two of kept
 // activations (powers != NULL); width: n up to a multiple of 8.
 struct WidenParams {
@@ -174,18 +186,11 @@ __device__ __forceinline__ void widen_group(const WidenParams &P, int64_t group)
   if (row >= P.rows) return;
   const u32x4 w = *reinterpret_cast<const u32x4 *>(P.codes + row * P.ldc + j);
   const float unit = P.powers != nullptr ? kept_unit(P.powers[row * P.ldp + (j >> 5)]) : P.factor != nullptr ? P.factor[row] : 1.f;
+  u32x4 p[2];
+  widen16(w, unit, p);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (j + 8 * h >= P.width) break;
-    u32x4 p;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const unsigned d = w[2 * h + (u >> 1)];
-      const float a = (float)((int)(d << (24 - 16 * (u & 1))) >> 24) * unit, b = (float)((int)(d << (16 - 16 * (u & 1))) >> 24) * unit;
-      p[u] = bf16_pair(a, b);
-    }
-    *reinterpret_cast<u32x4 *>(P.plane + row * P.width + j + 8 * h) = p;
-  }
+  for (int h = 0; h < 2; ++h)
+    if (j + 8 * h < P.width) *reinterpret_cast<u32x4 *>(P.plane + row * P.width + j + 8 * h) = p[h];
 }
 
 }  // namespace rsvd

@@ -183,12 +183,19 @@ __device__ __forceinline__ void finish_tile(const TileParams &P, acc_t (&acc)[TM
 }
 
 // The parts of sums over k, added in their order, and the rest of the epilogue.
-template <bool CODES>
-__global__ __launch_bounds__(256) void tile_reduce_kernel(const float *__restrict__ partial, int splits, int64_t M, int64_t N, Layer8Epilogue E) {
+struct ReduceParams {
+  const float *partial; int splits;
+  int64_t M, N, groups;            // groups: workgroups that share the work
+  Layer8Epilogue E;
+};
+template <bool CODES> __device__ __forceinline__ void reduce_group(const ReduceParams &P, int64_t group) {
+  const float *__restrict__ partial = P.partial;
+  const Layer8Epilogue &E = P.E;
+  const int64_t M = P.M, N = P.N;
   typedef typename std::conditional<CODES, i32x4, f32x4>::type acc_t;
   typedef typename std::conditional<CODES, int, float>::type one_t;
   const int64_t per_row = (N + 3) / 4, total = M * per_row;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
+  for (int64_t e = group * 256 + threadIdx.x; e < total; e += P.groups * 256) {
     const int64_t m = e / per_row, n = (e - m * per_row) * 4;
     auto part = [&](int s, auto zero) RSVD_INLINE {
       typedef decltype(zero) vec;
@@ -207,13 +214,14 @@ __global__ __launch_bounds__(256) void tile_reduce_kernel(const float *__restric
       return v;
     };
     acc_t sum = (acc_t)(one_t)0;
-    for (int s = 0; s < splits; ++s) sum += part(s, (acc_t)(one_t)0);
+#pragma unroll 4
+    for (int s = 0; s < P.splits; ++s) sum += part(s, (acc_t)(one_t)0);
     const float rs = E.rs != nullptr ? E.rs[m] : 1.f;
     const f32x4 cs = column4(E.cs, n, N, 1.f);
     f32x4 val;
 #pragma unroll
     for (int v = 0; v < 4; ++v) val[v] = (float)sum[v] * rs * cs[v];
-    if (E.r > 0) val += part(splits, (f32x4)0.f);
+    if (E.r > 0) val += part(P.splits, (f32x4)0.f);
     if (E.bias != nullptr) val += column4(E.bias, n, N, 0.f);
     store4(E, m, n, N, val);
   }
@@ -240,12 +248,11 @@ inline TileParams tile_params(const TileChoice &c, int64_t M, int64_t N, int64_t
 inline unsigned tile_groups(const TileParams &P) {
   return (unsigned)((int64_t)P.tiles_m * P.tiles_n * (P.splits > 1 && P.E.r > 0 ? P.splits + 1 : P.splits));
 }
-template <bool CODES> inline hipError_t tile_reduce(hipStream_t s, const TileParams &P) {
-  if (P.splits <= 1) return hipSuccess;
-  int64_t blocks = ceil_div(P.M * ceil_div(P.N, 4), 256);
-  if (blocks > 4096) blocks = 4096;
-  hipLaunchKernelGGL(tile_reduce_kernel<CODES>, dim3((unsigned)blocks), dim3(256), 0, s, P.partial, P.splits, P.M, P.N, P.E);
-  return hipGetLastError();
+// groups: 0 where there is one range of k, and nothing to add
+inline ReduceParams reduce_params(const TileParams &P) {
+  int64_t groups = P.splits <= 1 ? 0 : ceil_div(P.M * ceil_div(P.N, 4), 256);
+  if (groups > 4096) groups = 4096;
+  return ReduceParams{P.partial, P.splits, P.M, P.N, groups, P.E};
 }
 
 }  // namespace rsvd

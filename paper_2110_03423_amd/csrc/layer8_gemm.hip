@@ -17,8 +17,8 @@ struct NtParams {
 };
 
 template <int BM, int BN> struct NtCfg {
-  static constexpr int STAGE = (BM + BN) * 128;
-  static constexpr size_t lds = 2 * (size_t)STAGE;      // (more than the wavefronts need in the end)
+  static constexpr int STAGE = (BM + BN) * 128, RING = BM == 64 ? 3 : 2;
+  static constexpr size_t lds = RING * (size_t)STAGE;      // (more than the wavefronts need in the end)
 };
 
 // The loads of ROWS rows of a k-tile by NT threads.
@@ -50,7 +50,7 @@ template <int NT, int ROWS> struct NtLoad {
 
 template <int BM, int BN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void nt_kernel(const NtParams P) {
-  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = NtCfg<BM, BN>::STAGE;
+  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = NtCfg<BM, BN>::STAGE, RING = NtCfg<BM, BN>::RING;
   extern __shared__ __attribute__((aligned(16))) char nt_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
@@ -81,22 +81,24 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void nt_kernel(c
   const __amdgpu_buffer_rsrc_t b_all = __builtin_amdgcn_make_buffer_rsrc((void *)b_row, 0, 0x7fffffff, 0x00027000);
   auto issue = [&](int kt, int l) RSVD_INLINE {
     const int k = kt < nkt ? kt : nkt - 1;              // (behind the last tile that one again, where nobody reads it: no branches)
-    char *st = nt_lds + (kt & 1) * STAGE;
+    char *st = nt_lds + (kt % RING) * STAGE;
     if (l < decltype(la)::N) la.issue(l, a_all, k * 128, st, 8, wave, tid);
     else lb.issue(l - decltype(la)::N, b_all, k * 128, st + BM * 128, P.b_pieces - (kt_begin + k) * 8, wave, tid);
   };
   if (nkt > 0) {
 #pragma unroll
-    for (int l = 0; l < LOADS; ++l) issue(0, l);
+    for (int t = 0; t < RING - 1; ++t)
+#pragma unroll
+      for (int l = 0; l < LOADS; ++l) issue(t, l);
   }
   const int swz = r16 & 7;                       // (rows of a wavefront's blocks start at multiples of 16)
   const char *const a_lds = nt_lds + (wm0 + r16) * 128, *const b_lds = nt_lds + BM * 128 + (wn0 + r16) * 128;
   for (int kt = 0; kt < nkt; ++kt) {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(tile_wait(0));
+    __builtin_amdgcn_s_waitcnt(tile_wait((RING - 2) * LOADS));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    const int at = (kt & 1) * STAGE;
+    const int at = (kt % RING) * STAGE;
     auto read_a = [&](int step) RSVD_INLINE {
       return *reinterpret_cast<const u32x4 *>(a_lds + at + step % TM * 2048 + (((4 * (step / TM) + kq) ^ swz) << 4));
     };
@@ -119,7 +121,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void nt_kernel(c
       for (int j = 0; j < TN; ++j) acc[i][j] = mfma_codes(b[h][j], a[step % (AHEAD + 1)], acc[i][j]);
 #pragma unroll
       for (int l = 0; l < LOADS; ++l)
-        if (l * TM / LOADS == step) issue(kt + 1, l);
+        if (l * TM / LOADS == step) issue(kt + RING - 1, l);
       __builtin_amdgcn_sched_barrier(0);
     }
   }

@@ -5,7 +5,7 @@
 // four k each).  LDS rows of such a tile have their 32-byte pieces exchanged by the low bits of k, so that the eight rows that half a wavefront
 // reads start at different banks; rows of consecutive k have their 16-byte pieces exchanged by the row.
 // Both operands go from memory to registers and from there to LDS, among the matrix instructions of the tile before, and a register is loaded for
-// the tile after next as soon as it has been written.  (Loads straight to LDS: the compiler lets the transposing loads wait for all of them,
+// the tile after next (or, of small tiles, which are done before a load arrives, the one behind) as soon as it has been written.  (Loads straight to LDS: the compiler lets the transposing loads wait for all of them,
 // wherever they go.)
 // Several planes of A are taken as further k, the smallest first.
 // Where few rows of tiles need it, B is taken as the 8-bit codes that it comes from and made bf16 numbers on the way to LDS.
@@ -35,10 +35,10 @@ template <int X> __device__ __forceinline__ int krow_piece(int c, int k) {
 }
 
 // What one of NT threads stages of a k-tile of X rows (consecutive k) or columns (KROWS): N pieces of 16 bytes.
-template <int NT, int X, bool KROWS> struct Staged {
+template <int NT, int X, bool KROWS, int DEPTH> struct Staged {
   static constexpr int ROW = KROWS ? X * 2 : 128, PER = ROW / 16, STEP = NT / PER, N = X * 128 / 16 / NT;      // bytes of a row; pieces; rows between a thread's
   static_assert(X * 128 % (16 * NT) == 0 && STEP % 8 == 0, "whole rounds; a thread's rows have their pieces exchanged alike, but for bit 3 of k");
-  u32x4 reg[N];
+  u32x4 reg[DEPTH][N];
   uint32_t off[N];
   int pos, place;
   // left: rows (columns) of the tile that exist; others are read as one that does, and not stored
@@ -56,23 +56,23 @@ template <int NT, int X, bool KROWS> struct Staged {
   }
   // base: the tile in memory; k_left: k of it that exist.  Those that do not are read beyond the end of the buffer, which gives zeros: behind the
   // last row of a [k][x] tile, and a long way off where k is consecutive.
-  __device__ __forceinline__ void load(int i, const char *base, int64_t ld, int k_left) {
+  __device__ __forceinline__ void load(int set, int i, const char *base, int64_t ld, int k_left) {
     const int bytes = KROWS ? (int)(k_left * (uint32_t)ld) : 0x7fffffff;
     const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, bytes, 0x00027000);
     const uint32_t o = KROWS || 8 * pos < k_left ? off[i] : 0x80000000u;
-    reg[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(all, o, 0, 0));
+    reg[set][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(all, o, 0, 0));
   }
-  __device__ __forceinline__ void write(int i, char *lds) const {
-    *reinterpret_cast<u32x4 *>(lds + (place ^ (KROWS && STEP % 16 == 8 ? (i & 1) << 7 : 0)) + i * STEP * ROW) = reg[i];
+  __device__ __forceinline__ void write(int set, int i, char *lds) const {
+    *reinterpret_cast<u32x4 *>(lds + (place ^ (KROWS && STEP % 16 == 8 ? (i & 1) << 7 : 0)) + i * STEP * ROW) = reg[set][i];
   }
 };
 
 // The same for codes: N pieces of sixteen codes of a row, as bf16 numbers in LDS.
-template <int NT, int X> struct StagedCodes {
+template <int NT, int X, int DEPTH> struct StagedCodes {
   static constexpr int ROW = X * 2, PER = X / 16, STEP = NT / PER, N = X * kKnK / 16 / NT;
   static_assert(X * kKnK % (16 * NT) == 0 && STEP % 16 == 0, "whole rounds; a thread's rows have their pieces exchanged alike");
-  u32x4 reg[N];
-  unsigned unit[N];
+  u32x4 reg[DEPTH][N];
+  unsigned unit[DEPTH][N];
   uint32_t off[N], unit_off[N];
   int place, half;
   __device__ __forceinline__ void init(int64_t ld, int64_t left, int tid, const CodeUnits &units) {
@@ -88,22 +88,22 @@ template <int NT, int X> struct StagedCodes {
     }
   }
   // k: the first of the tile; base: its codes; what is behind the last row is read as zeros, codes and units
-  __device__ __forceinline__ void load(int i, const char *base, int64_t ld, int k_left, const CodeUnits &units, int64_t k, int64_t n0) {
+  __device__ __forceinline__ void load(int set, int i, const char *base, int64_t ld, int k_left, const CodeUnits &units, int64_t k, int64_t n0) {
     const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)(k_left * (uint32_t)ld), 0x00027000);
-    reg[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(all, off[i], 0, 0));
+    reg[set][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(all, off[i], 0, 0));
     if (units.powers != nullptr) {
       const __amdgpu_buffer_rsrc_t u =
           __builtin_amdgcn_make_buffer_rsrc((void *)(units.powers + k * units.ldp + n0 / 32), 0, (int)(k_left * (uint32_t)units.ldp), 0x00027000);
-      unit[i] = __builtin_amdgcn_raw_buffer_load_b8(u, unit_off[i], 0, 0);
+      unit[set][i] = __builtin_amdgcn_raw_buffer_load_b8(u, unit_off[i], 0, 0);
     } else if (units.factor != nullptr) {
       const __amdgpu_buffer_rsrc_t u = __builtin_amdgcn_make_buffer_rsrc((void *)(units.factor + k), 0, k_left * 4, 0x00027000);
-      unit[i] = __builtin_amdgcn_raw_buffer_load_b32(u, unit_off[i], 0, 0);
+      unit[set][i] = __builtin_amdgcn_raw_buffer_load_b32(u, unit_off[i], 0, 0);
     }
   }
-  __device__ __forceinline__ void write(int i, char *lds, const CodeUnits &units) const {
-    const float by = units.powers != nullptr ? kept_unit(unit[i]) : units.factor != nullptr ? __uint_as_float(unit[i]) : 1.f;
+  __device__ __forceinline__ void write(int set, int i, char *lds, const CodeUnits &units) const {
+    const float by = units.powers != nullptr ? kept_unit(unit[set][i]) : units.factor != nullptr ? __uint_as_float(unit[set][i]) : 1.f;
     u32x4 p[2];
-    widen16(reg[i], by, p);
+    widen16(reg[set][i], by, p);
     char *at = lds + place + i * STEP * ROW;
     *reinterpret_cast<u32x4 *>(at + half) = half ? p[1] : p[0];
     *reinterpret_cast<u32x4 *>(at + (half ^ 16)) = half ? p[0] : p[1];
@@ -111,13 +111,14 @@ template <int NT, int X> struct StagedCodes {
 };
 
 template <int BM, int BN> struct KnCfg {
-  static constexpr int A = BM * 128, B = BN * 128, STAGE = A + B;
+  static constexpr int A = BM * 128, B = BN * 128, STAGE = A + B, DEPTH = BM == 256 ? 1 : 2;
   static constexpr size_t lds = 2 * (size_t)STAGE;      // (more than the wavefronts need in the end)
 };
 
 template <bool A_KROWS, bool CODES, int BM, int BN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P) {
-  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = KnCfg<BM, BN>::STAGE, A_BYTES = KnCfg<BM, BN>::A;
+  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, DEPTH = KnCfg<BM, BN>::DEPTH;
+  constexpr int STAGE = KnCfg<BM, BN>::STAGE, A_BYTES = KnCfg<BM, BN>::A;
   extern __shared__ __attribute__((aligned(16))) char kn_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
@@ -142,21 +143,21 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
   int64_t next_k = (int64_t)next_kt * kKnK;
   int next_left = (int)(P.K - next_k < kKnK ? P.K - next_k : kKnK);      // k of it that exist
   const char *const a_first = P.A + (A_KROWS ? m0 * 2 : m0 * P.lda), *const b_first = P.B + n0 * (CODES ? 1 : 2);
-  Staged<NT, BM, A_KROWS> sa;
-  std::conditional_t<CODES, StagedCodes<NT, BN>, Staged<NT, BN, true>> sb;
+  Staged<NT, BM, A_KROWS, DEPTH> sa;
+  std::conditional_t<CODES, StagedCodes<NT, BN, DEPTH>, Staged<NT, BN, true, DEPTH>> sb;
   sa.init(P.lda, P.T.M - m0, tid);
   if constexpr (CODES) sb.init(P.ldb, P.T.N - n0, tid, P.units);
   else sb.init(P.ldb, P.T.N - n0, tid);
   constexpr int NA = decltype(sa)::N, PIECES = NA + decltype(sb)::N;
-  auto load = [&](int p) RSVD_INLINE {
-    if (p < NA) sa.load(p, a_first + (P.planes - 1 - next_plane) * P.plane + (A_KROWS ? next_k * P.lda : next_k * 2), P.lda, next_left);
-    else if constexpr (CODES) sb.load(p - NA, b_first + next_k * P.ldb, P.ldb, next_left, P.units, next_k, n0);
-    else sb.load(p - NA, b_first + next_k * P.ldb, P.ldb, next_left);
+  auto load = [&](int set, int p) RSVD_INLINE {
+    if (p < NA) sa.load(set, p, a_first + (P.planes - 1 - next_plane) * P.plane + (A_KROWS ? next_k * P.lda : next_k * 2), P.lda, next_left);
+    else if constexpr (CODES) sb.load(set, p - NA, b_first + next_k * P.ldb, P.ldb, next_left, P.units, next_k, n0);
+    else sb.load(set, p - NA, b_first + next_k * P.ldb, P.ldb, next_left);
   };
-  auto write = [&](int p, int buf) RSVD_INLINE {
-    if (p < NA) sa.write(p, kn_lds + buf * STAGE);
-    else if constexpr (CODES) sb.write(p - NA, kn_lds + buf * STAGE + A_BYTES, P.units);
-    else sb.write(p - NA, kn_lds + buf * STAGE + A_BYTES);
+  auto write = [&](int set, int p, int buf) RSVD_INLINE {
+    if (p < NA) sa.write(set, p, kn_lds + buf * STAGE);
+    else if constexpr (CODES) sb.write(set, p - NA, kn_lds + buf * STAGE + A_BYTES, P.units);
+    else sb.write(set, p - NA, kn_lds + buf * STAGE + A_BYTES);
   };
   auto advance = [&]() RSVD_INLINE {                    // (behind the last tile of this workgroup's range: loads stay inside the operands)
     next_k += kKnK;
@@ -211,7 +212,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
 
   // The matrix instructions of a tile, with the next one going to LDS in step.  (Behind the last tile that is one that nobody reads: no
   // branches.)
-  auto body = [&](int buf) RSVD_INLINE {
+  auto body = [&](int buf, auto from) RSVD_INLINE {
+    constexpr int SET = decltype(from)::value;
     const int a_now = a_at + buf * STAGE, b_now = b_at + buf * STAGE;
     auto read_a = [&](int step) RSVD_INLINE {
       const int h = step / TM, i = step % TM;
@@ -238,30 +240,42 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
 #pragma unroll
       for (int p = 0; p < PIECES; ++p)
         if (p * (2 * TM) / PIECES == step) {
-          write(p, buf ^ 1);
-          load(p);
+          write(SET, p, buf ^ 1);
+          load(SET, p);
         }
       __builtin_amdgcn_sched_barrier(0);
     }
   };
+  // Tile kt goes through register set kt mod DEPTH.
   if (nkt > 0) {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) load(p);
-    advance();
+    for (int set = 0; set < DEPTH; ++set) {
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) load(set, p);
+      advance();
+    }
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      write(p, 0);
-      load(p);
+      write(0, p, 0);
+      load(0, p);
     }
     advance();
     meet();
   }
-  for (int kt = 0; kt < nkt; ++kt) {
-    if (A_KROWS && P.sums != nullptr && now_column == tile_n) sum_a(kt & 1);
-    body(kt & 1);
+  auto tile = [&](int buf, auto from) RSVD_INLINE {
+    if (A_KROWS && P.sums != nullptr && now_column == tile_n) sum_a(buf);
+    body(buf, from);
     advance();
     if (++now_column == P.sum_columns) now_column = 0;
     meet();
+  };
+  if constexpr (DEPTH == 1) {
+    for (int kt = 0; kt < nkt; ++kt) tile(kt & 1, std::integral_constant<int, 0>());
+  } else {
+    for (int kt = 0; kt < nkt; kt += 2) {
+      tile(0, std::integral_constant<int, 1>());
+      if (kt + 1 < nkt) tile(1, std::integral_constant<int, 0>());
+    }
   }
   if (A_KROWS && P.sums != nullptr && tile_n < P.sum_columns) {      // (no low-rank term there: split is a range of k)
 #pragma unroll

@@ -67,8 +67,9 @@ template <int NT, int X, bool KROWS, int DEPTH> struct Staged {
   }
 };
 
-// The same for codes: N pieces of sixteen codes of a row, as bf16 numbers in LDS.
-template <int NT, int X, int DEPTH> struct StagedCodes {
+// The same for codes: N pieces of sixteen codes of a row, as bf16 numbers in LDS.  POWERS: their units are powers of two, otherwise factors or ones.
+// (No branch between the loads: where it ends the compiler would wait for all of them.)
+template <int NT, int X, bool POWERS, int DEPTH> struct StagedCodes {
   static constexpr int ROW = X * 2, PER = X / 16, STEP = NT / PER, N = X * kKnK / 16 / NT;
   static_assert(X * kKnK % (16 * NT) == 0 && STEP % 16 == 0, "whole rounds; a thread's rows have their pieces exchanged alike");
   u32x4 reg[DEPTH][N];
@@ -83,7 +84,7 @@ template <int NT, int X, int DEPTH> struct StagedCodes {
     for (int i = 0; i < N; ++i) {
       const uint32_t r = row + STEP * i;
       off[i] = r * (uint32_t)ld + (uint32_t)col;
-      unit_off[i] = units.powers != nullptr ? r * (uint32_t)units.ldp + (uint32_t)(col >> 5) : 4 * r;
+      unit_off[i] = POWERS ? r * (uint32_t)units.ldp + (uint32_t)(col >> 5) : 4 * r;
       asm volatile("" : "+v"(off[i]), "+v"(unit_off[i]));
     }
   }
@@ -91,17 +92,13 @@ template <int NT, int X, int DEPTH> struct StagedCodes {
   __device__ __forceinline__ void load(int set, int i, const char *base, int64_t ld, int k_left, const CodeUnits &units, int64_t k, int64_t n0) {
     const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)(k_left * (uint32_t)ld), 0x00027000);
     reg[set][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(all, off[i], 0, 0));
-    if (units.powers != nullptr) {
-      const __amdgpu_buffer_rsrc_t u =
-          __builtin_amdgcn_make_buffer_rsrc((void *)(units.powers + k * units.ldp + n0 / 32), 0, (int)(k_left * (uint32_t)units.ldp), 0x00027000);
-      unit[set][i] = __builtin_amdgcn_raw_buffer_load_b8(u, unit_off[i], 0, 0);
-    } else if (units.factor != nullptr) {
-      const __amdgpu_buffer_rsrc_t u = __builtin_amdgcn_make_buffer_rsrc((void *)(units.factor + k), 0, k_left * 4, 0x00027000);
-      unit[set][i] = __builtin_amdgcn_raw_buffer_load_b32(u, unit_off[i], 0, 0);
-    }
+    const char *first = POWERS ? (const char *)(units.powers + k * units.ldp + n0 / 32) : (const char *)(units.factor + (units.factor != nullptr ? k : 0));
+    const int bytes = POWERS ? (int)(k_left * (uint32_t)units.ldp) : units.factor != nullptr ? 4 * k_left : 0;      // (none: nothing is read)
+    const __amdgpu_buffer_rsrc_t u = __builtin_amdgcn_make_buffer_rsrc((void *)first, 0, bytes, 0x00027000);
+    unit[set][i] = POWERS ? __builtin_amdgcn_raw_buffer_load_b8(u, unit_off[i], 0, 0) : __builtin_amdgcn_raw_buffer_load_b32(u, unit_off[i], 0, 0);
   }
   __device__ __forceinline__ void write(int set, int i, char *lds, const CodeUnits &units) const {
-    const float by = units.powers != nullptr ? kept_unit(unit[set][i]) : units.factor != nullptr ? __uint_as_float(unit[set][i]) : 1.f;
+    const float by = POWERS ? kept_unit(unit[set][i]) : units.factor != nullptr ? __uint_as_float(unit[set][i]) : 1.f;
     u32x4 p[2];
     widen16(reg[set][i], by, p);
     char *at = lds + place + i * STEP * ROW;
@@ -144,7 +141,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
   int next_left = (int)(P.K - next_k < kKnK ? P.K - next_k : kKnK);      // k of it that exist
   const char *const a_first = P.A + (A_KROWS ? m0 * 2 : m0 * P.lda), *const b_first = P.B + n0 * (CODES ? 1 : 2);
   Staged<NT, BM, A_KROWS, DEPTH> sa;
-  std::conditional_t<CODES, StagedCodes<NT, BN, DEPTH>, Staged<NT, BN, true, DEPTH>> sb;
+  std::conditional_t<CODES, StagedCodes<NT, BN, A_KROWS, DEPTH>, Staged<NT, BN, true, DEPTH>> sb;
   sa.init(P.lda, P.T.M - m0, tid);
   if constexpr (CODES) sb.init(P.ldb, P.T.N - n0, tid, P.units);
   else sb.init(P.ldb, P.T.N - n0, tid);

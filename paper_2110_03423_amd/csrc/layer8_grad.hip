@@ -340,12 +340,13 @@ template <bool A_KROWS> static hipError_t kn_run_tile(hipStream_t s, const KnPar
 }
 
 // Every row of tiles makes bf16 numbers of all the codes again, and every plane; a matrix of them is made once and read twice as long.  Rows of tiles
-// times planes up to which the codes are taken as they are, measured as codes / matrix: 4096 x 4096 codes with 64 columns of dY, bf16 (1) 21 / 34 us,
-// 128 (2) 26 / 35, 256 (4) 37 / 42, 512 (8) 57 / 52; 64 of fp32 (3) 33 / 41, 128 (6) 50 / 49; 1000 x 1000 with 1000 of fp32 (48) 39 / 31.
-constexpr int64_t kCodeRows = 4;
-bool kn_takes_codes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, int64_t ldc, int64_t ldp) {
+// times planes up to which the codes are taken as they are, measured as codes / matrix.  Weight, 4096 x 4096 codes with 64 columns of dY in
+// bf16 (1) 18 / 34 us, 256 (4) 31 / 42, 512 (8) 49 / 51; 2048 x 2048 with 1024 (16) 28 / 33; 4096 x 4096 with 256 of fp32 (12) 49 / 53, 512 (24)
+// 78 / 75.  X, where a launch before the product is needed anyway: 128 tokens with 16384 x 4096 codes, bf16 (1) 62 / 81 us, fp32 (3) 126 / 145;
+// 256 with 4096 x 4096 (4) 43 / 46, 512 (8) 52 / 48, 256 of fp32 (12) 70 / 68.
+bool kn_takes_codes(const rsvd_ctx *ctx, bool a_krows, int64_t M, int64_t N, int64_t K, int planes, int64_t ldc, int64_t ldp) {
   const TileChoice c = tile_choose(ctx, M, N, ceil_div(K, kKnK) * planes);
-  return c.bm < 256 && ceil_div(M, c.bm) * planes <= kCodeRows && ldc <= kMaxLd && ldp <= kMaxLd;
+  return c.bm < 256 && ceil_div(M, c.bm) * planes <= (a_krows ? 16 : 4) && ldc <= kMaxLd && ldp <= kMaxLd;
 }
 
 hipError_t nt_init_device();
@@ -368,7 +369,7 @@ hipError_t kn_launch(rsvd_ctx *ctx, hipStream_t s, const KnDesc &d) {
   P.B = (const char *)d.B; P.ldb = d.ldb;
   const bool codes = d.codes != nullptr;
   if (codes) {
-    if (!kn_takes_codes(ctx, d.M, d.N, d.K, d.planes, d.ldc, d.units.ldp)) return hipErrorInvalidValue;
+    if (!kn_takes_codes(ctx, d.a_krows, d.M, d.N, d.K, d.planes, d.ldc, d.units.ldp)) return hipErrorInvalidValue;
     P.B = (const char *)d.codes; P.ldb = d.ldc;
   }
   P.units = d.units;

@@ -318,8 +318,9 @@ typedef enum { RSVD_X_BF16 = 0, RSVD_X_F16 = 1, RSVD_X_F32 = 2 } rsvd_xtype;
 #define RSVD_Q8_MAX_FEATURES 131072
 
 /* Rows to 8 bits with a scale each: a = max_j |x_j|; scale = a / 127 and
- * codes_j = x_j (127 / a) rounded to the nearest integer, ties to even, where
- * the two quotients and the product are single fp32 operations.  a < 2^-116:
+ * codes_j = x_j (127 (1 / a)) rounded to the nearest integer, ties to even, where
+ * the quotients and products are single fp32 operations (127 / a the way torch
+ * computes it, so that its codes and these are the same).  a < 2^-116:
  * scale 0 and codes 0.  The bytes of a row from n to the next multiple of 16
  * are set to 0.  (Lays out the weight; rsvd_q8_product does the same to X.) */
 int rsvd_q8_rows(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t rows, int64_t n,

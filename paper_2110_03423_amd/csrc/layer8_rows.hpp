@@ -89,7 +89,7 @@ template <int XT, int CH> __device__ __forceinline__ void rows8_row(const Rows8P
   top = max(max(part[0], part[1]), max(part[2], part[3]));
   const float a = __uint_as_float(top);
   const bool bad = top >= 0x7f800000u, none = bad || a < 0x1p-116f;
-  const float per = none ? 0.f : 127.f / a;
+  const float per = none ? 0.f : 127.f * (1.f / a);
   if (tid == 0) P.scale[row] = bad ? __uint_as_float(0x7fc00000u) : none ? 0.f : a / 127.f;
   auto store = [&](int c, const float (&w)[8]) RSVD_INLINE {
     float q[8];

@@ -37,7 +37,7 @@ def rows8(x):
     none = bad | (a < np.float32(2.0 ** -116))
     safe = np.where(none, np.float32(1), a).astype(np.float32)
     with np.errstate(all="ignore"):
-        q = np.rint(x * (np.float32(127) / safe)[:, None])
+        q = np.rint(x * (np.float32(127) * (np.float32(1) / safe))[:, None])
     q[none] = 0
     s = np.where(none, np.float32(0), a / np.float32(127)).astype(np.float32)
     s[bad] = np.nan

@@ -122,7 +122,8 @@ def _xtype_code(dtype):
 def _empty_codes(rows, n, device):
     """Room for `rows` rows of 8-bit codes, each a multiple of 128 bytes long; the view has n columns."""
     import torch
-    return torch.empty((rows, -(-n // 128) * 128), dtype=torch.int8, device=device)[:, :n]
+    codes = torch.empty((rows, -(-n // 128) * 128), dtype=torch.int8, device=device)
+    return codes if n % 128 == 0 else codes[:, :n]
 
 
 def _laid_out(codes):
@@ -140,7 +141,7 @@ def _rows(t, cols, what, rows=None, dtype=None):
         raise ValueError(f"{what}: a row-major GPU matrix with {cols} columns is needed")
     if (rows is not None and t.shape[0] != rows) or (dtype is not None and t.dtype != dtype):
         raise ValueError(f"{what}: {rows} rows of {dtype} are needed")
-    return t
+    return t.shape[0]
 
 
 def _ld(t):
@@ -175,6 +176,16 @@ class Weight8:
         if bias is not None and bias.shape != (m,):
             raise ValueError("bias: m values")
         self.bias = None if bias is None else bias.float().contiguous()
+        # what the C entry points are told of it, put together once: a call of a single token is short
+        at = (_at(self.codes), _ld(self.codes), _at(self.scale))
+        self._sizes = (n, m, self.r)
+        self._product = (*at, _at(self.U), self.r, _at(self.Vt), n, _at(self.bias))
+        self._grad = (*at, _at(self.Ut), m, _at(self.V), self.r)
+
+    def __setattr__(self, name, value):
+        if "_grad" in self.__dict__:
+            raise AttributeError("a Weight8 keeps its tensors (their values may change): make another one")
+        object.__setattr__(self, name, value)
 
 
 class Kept8:
@@ -200,6 +211,10 @@ def _at(t):
     return t.data_ptr() if t is not None else None
 
 
+def _given(workspace):
+    return workspace.data_ptr(), workspace.numel()
+
+
 def _ptr(t):
     return C.c_void_p(t.data_ptr()) if t is not None else C.c_void_p(0)
 
@@ -213,6 +228,7 @@ class Rsvd:
         self.lib = load_library()
         self._ws = None
         self._needs = {}        # workspace of the layer calls, by their sizes
+        self._layer = {}        # and the workspaces themselves, one for each stream
         h = C.c_void_p()
         if device is None:
             self.torch = None
@@ -458,8 +474,8 @@ class Rsvd:
                                           _ld(codes), _at(scale)))
         return codes, scale
 
-    def _layer_ws(self, name, *sizes):
-        """The cached workspace; what a call of these sizes needs is asked for once."""
+    def _layer_ws(self, stream, name, sizes):
+        """Address and bytes of the workspace that is kept for calls on `stream`; what a call of these sizes needs is asked for once."""
         need = self._needs.get((name, sizes))
         if need is None:
             out = C.c_size_t()
@@ -467,30 +483,39 @@ class Rsvd:
             if len(self._needs) >= 1024:
                 self._needs.clear()
             need = self._needs[(name, sizes)] = out.value
-        return self._grow(need)
+        kept = self._layer.get(stream)
+        if kept is None or kept[1] < need:
+            self._layer.pop(stream, None)
+            ws = self.torch.empty(need, dtype=self.torch.uint8, device=self.device)
+            kept = (ws.data_ptr(), need, ws)
+            if not self.torch.cuda.is_current_stream_capturing():      # (what is allocated for a graph belongs to that graph)
+                self._layer[stream] = kept
+        return kept
 
     def rsvd_q8_product(self, X, weight, workspace=None, out=None):
         """X (tokens x n) through the layer `weight` (Weight8): tokens x m, in the type of X."""
-        w = weight
-        _rows(X, w.n, "X")
-        xt, tokens = _xtype_code(X.dtype), X.shape[0]
-        ws = workspace if workspace is not None else self._layer_ws("rsvd_q8_product_bytes", xt, tokens, w.n, w.m, w.r)
-        Y = _rows(out, w.m, "out", tokens, X.dtype) if out is not None else self._empty((tokens, w.m), X)
-        self._check(self.lib.rsvd_q8_product(
-            self.h, self._raw_stream(), xt, tokens, w.n, w.m, w.r, _at(X), _ld(X), _at(w.codes), _ld(w.codes), _at(w.scale),
-            _at(w.U), w.r, _at(w.Vt), w.n, _at(w.bias), _at(Y), _ld(Y), _at(ws), ws.numel()))
+        n, m, r = sizes = weight._sizes
+        tokens, xt = _rows(X, n, "X"), _xtype_code(X.dtype)
+        stream = self._raw_stream()
+        ws = _given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_q8_product_bytes", (xt, tokens, *sizes))
+        Y = X.new_empty((tokens, m)) if out is None else out
+        if out is not None:
+            _rows(out, m, "out", tokens, X.dtype)
+        self._check(self.lib.rsvd_q8_product(self.h, stream, xt, tokens, n, m, r, X.data_ptr(), _ld(X), *weight._product,
+                                             Y.data_ptr(), _ld(Y), ws[0], ws[1]))
         return Y
 
     def rsvd_q8_product_grad(self, dY, weight, workspace=None, out=None):
         """Gradient of rsvd_q8_product with respect to X: dY (tokens x m) to tokens x n, in the type of dY."""
-        w = weight
-        _rows(dY, w.m, "dY")
-        xt, tokens = _xtype_code(dY.dtype), dY.shape[0]
-        ws = workspace if workspace is not None else self._layer_ws("rsvd_q8_product_grad_bytes", xt, tokens, w.n, w.m, w.r)
-        dX = _rows(out, w.n, "out", tokens, dY.dtype) if out is not None else self._empty((tokens, w.n), dY)
-        self._check(self.lib.rsvd_q8_product_grad(
-            self.h, self._raw_stream(), xt, tokens, w.n, w.m, w.r, _at(dY), _ld(dY), _at(w.codes), _ld(w.codes), _at(w.scale),
-            _at(w.Ut), w.m, _at(w.V), w.r, _at(dX), _ld(dX), _at(ws), ws.numel()))
+        n, m, r = sizes = weight._sizes
+        tokens, xt = _rows(dY, m, "dY"), _xtype_code(dY.dtype)
+        stream = self._raw_stream()
+        ws = _given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_q8_product_grad_bytes", (xt, tokens, *sizes))
+        dX = dY.new_empty((tokens, n)) if out is None else out
+        if out is not None:
+            _rows(out, n, "out", tokens, dY.dtype)
+        self._check(self.lib.rsvd_q8_product_grad(self.h, stream, xt, tokens, n, m, r, dY.data_ptr(), _ld(dY), *weight._grad,
+                                                  dX.data_ptr(), _ld(dX), ws[0], ws[1]))
         return dX
 
     def rsvd_keep8_save(self, X):
@@ -529,8 +554,9 @@ class Rsvd:
             _rows(dW, kept.n, "dW")
             if dW.dtype != t.float32 or dW.shape[0] != m or (db is not None and (db.dtype != t.float32 or db.shape != (m,) or not db.is_contiguous())):
                 raise ValueError("out: fp32 gradients, m x n and m")
-        ws = workspace if workspace is not None else self._layer_ws("rsvd_keep8_grad_bytes", xt, kept.tokens, kept.n, m)
+        stream = self._raw_stream()
+        ws = _given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_keep8_grad_bytes", (xt, kept.tokens, kept.n, m))
         self._check(self.lib.rsvd_keep8_grad(
-            self.h, self._raw_stream(), xt, kept.tokens, kept.n, m, _at(dY), _ld(dY), _at(kept.codes), _ld(kept.codes),
-            _at(kept.powers), _ld(kept.powers), _at(dW), _ld(dW), _at(db), int(accumulate), _at(ws), ws.numel()))
+            self.h, stream, xt, kept.tokens, kept.n, m, _at(dY), _ld(dY), _at(kept.codes), _ld(kept.codes),
+            _at(kept.powers), _ld(kept.powers), _at(dW), _ld(dW), _at(db), int(accumulate), ws[0], ws[1]))
         return dW, db

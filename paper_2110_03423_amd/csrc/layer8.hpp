@@ -239,7 +239,7 @@ struct KnDesc {
 };
 size_t kn_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, bool lowrank);
 int64_t kn_sum_rows(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes);
-bool kn_takes_codes(const rsvd_ctx *ctx, bool a_krows, int64_t M, int64_t N, int64_t K, int planes, int64_t ldc, int64_t ldp);
+bool kn_takes_codes(const rsvd_ctx *ctx, bool a_krows, int64_t M, int64_t N, int64_t K, int planes, bool lowrank, int64_t ldc, int64_t ldp);
 hipError_t kn_launch(rsvd_ctx *ctx, hipStream_t s, const KnDesc &d);
 
 // ---------------------------------------------------------------- layer8_few.hip

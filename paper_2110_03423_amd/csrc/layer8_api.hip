@@ -249,7 +249,7 @@ int rsvd_q8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t t
   char *ws = (char *)workspace;
   uint16_t *a = (uint16_t *)(ws + L.a), *b = (uint16_t *)(ws + L.b), *t = (uint16_t *)(ws + L.t);
   // one part: the scale goes to the codes; several: to dY before it is split, and the codes stay exact
-  const bool single = L.planes == 1, direct = takes_rows(type, dY, m, lddy), as_codes = kn_takes_codes(ctx, false, tokens, n, m, L.planes, ldq, 0);
+  const bool single = L.planes == 1, direct = takes_rows(type, dY, m, lddy), as_codes = kn_takes_codes(ctx, false, tokens, n, m, L.planes, r > 0, ldq, 0);
   {
     ProfScope ps(ctx, s, PK_SMALL);
     float *sums = (float *)(ws + L.sums);
@@ -345,7 +345,7 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
   char *ws = (char *)workspace;
   uint16_t *a = (uint16_t *)(ws + L.a), *b = (uint16_t *)(ws + L.b);
   float *sums = db != nullptr ? (float *)(ws + L.sums) : nullptr;
-  const bool direct = takes_rows(type, dY, m, lddy), as_codes = kn_takes_codes(ctx, true, m, n, tokens, L.planes, ldc, ldp);
+  const bool direct = takes_rows(type, dY, m, lddy), as_codes = kn_takes_codes(ctx, true, m, n, tokens, L.planes, false, ldc, ldp);
   {
     ProfScope ps(ctx, s, PK_SMALL);
     RSVD_TRY(grad_front_launch(ctx, s, type, tokens, m, 0, dY, lddy, nullptr, 0, nullptr, nullptr, direct ? nullptr : a, L.width, tokens, n, codes,

@@ -138,31 +138,35 @@ __global__ __launch_bounds__(256) void nt_reduce_kernel(const ReduceParams P) { 
 // ---------------------------------------------------------------- choice of tile and of the ranges of k
 // The time of each tile and number of ranges is estimated, and the least taken.  Measured with both product kernels (4096 to 8192 k, one to four
 // workgroups on a CU): a k-tile takes a CU 0.22, 0.55 and 2.05 us for each workgroup of 64, 128 and 256 rows and columns, but no less than 0.33,
-// 0.78 and 1.8 us; a launch 5 us beside that; ranges of k a second launch and their sums written and read (5 bytes / ps).  What that decides:
+// 0.78 and 1.8 us, and small tiles 0.15 us more for each further plane of A; a launch 5 us beside that; ranges of k a second launch, and their sums
+// and those of a low-rank term are written and read (5 bytes / ps).  What that decides:
 // 2048 x 2048, 64 k-tiles: 128 in 55 us, 256 and four ranges in 64, 64 in 65; 2048 x 1024: 128 and four ranges in 36, one in 46, 64 in 38;
-// 512 x 2048: 128 and four ranges in 24, 64 in 25; 4096 x 64, 128 k-tiles: 64 and four ranges in 19, sixteen in 23.
-TileChoice tile_choose(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt) {
-  static const struct { int b; double step, least; } tile[3] = {{64, 0.22, 0.33}, {128, 0.55, 0.78}, {256, 2.05, 1.8}};
+// 512 x 2048: 128 and four ranges in 24, 64 in 25; 4096 x 64, 128 k-tiles: 64 and four ranges in 19, sixteen in 23.  Three planes (gradients of
+// fp32), 64 k-tiles each: 256 x 4096 with a low-rank term 64 and one range in 55, two ranges in 69; 512 x 4096: 64 in 81, 128 and four in 103.
+TileChoice tile_choose(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt, int planes, bool lowrank) {
+  const struct { int b; double step, least; } tile[3] = {{64, 0.07 + 0.15 * planes, 0.18 + 0.15 * planes}, {128, 0.55, 0.78}, {256, 2.05, 1.8}};
   static const int ranges[8] = {1, 2, 3, 4, 6, 8, 12, 16};
-  TileChoice best = {64, 64, 1, kt};
+  TileChoice best = {64, 64, 1, kt, kt};
   double least = 1e300;
-  for (const auto &t : tile)
+  for (const auto &t : tile) {
+    const int64_t all = t.b == 64 ? kt : kt * planes;
     for (const int r : ranges) {
-      if (r > 1 && kt < 4 * r) break;
-      const int64_t per = ceil_div(kt, r), used = ceil_div(kt, per);
+      if (r > 1 && all < 4 * r) break;
+      const int64_t per = ceil_div(all, r), used = ceil_div(all, per);
       const int64_t groups = ceil_div(ceil_div(M, t.b) * ceil_div(N, t.b) * used, ctx->cu_count);
       const double step = (double)groups * t.step;
       double us = (double)per * (step > t.least ? step : t.least);
-      if (used > 1) us += 3.0 + (double)used * (double)M * (double)N * 8.0 / 5e6;
+      if (used > 1) us += 3.0 + (double)(used + (lowrank ? 1 : 0)) * (double)M * (double)N * 8.0 / 5e6;
       if (us < least) {
         least = us;
-        best = TileChoice{t.b, t.b, (int)used, per};
+        best = TileChoice{t.b, t.b, (int)used, per, all};
       }
     }
+  }
   return best;
 }
 
-size_t nt_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt, bool lowrank) { return tile_partial_bytes(ctx, M, N, kt, lowrank); }
+size_t nt_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt, bool lowrank) { return tile_partial_bytes(tile_choose(ctx, M, N, kt, 1, lowrank), M, N, lowrank); }
 
 template <int BM, int BN, int WGM, int WGN> static hipError_t nt_run(hipStream_t s, const NtParams &P) {
   hipLaunchKernelGGL((nt_kernel<BM, BN, WGM, WGN>), dim3(tile_groups(P.T)), dim3(64 * WGM * WGN), (NtCfg<BM, BN>::lds), s, P);
@@ -175,8 +179,8 @@ hipError_t nt_init_device() {
 }
 
 hipError_t nt_launch(rsvd_ctx *ctx, hipStream_t s, const NtDesc &d) {
-  const TileChoice c = tile_choose(ctx, d.M, d.N, d.ktiles);
-  if (c.splits > 1 && (d.partial == nullptr || d.partial_bytes < nt_partial_bytes(ctx, d.M, d.N, d.ktiles, d.out.r > 0))) return hipErrorInvalidValue;
+  const TileChoice c = tile_choose(ctx, d.M, d.N, d.ktiles, 1, d.out.r > 0);
+  if (c.splits > 1 && (d.partial == nullptr || d.partial_bytes < tile_partial_bytes(c, d.M, d.N, d.out.r > 0))) return hipErrorInvalidValue;
   const NtParams P = {(const char *)d.A, (const char *)d.B, d.lda, d.ldb, (int)(d.b_bytes / 16),
                       tile_params(c, d.M, d.N, d.ktiles, d.partial, d.out)};
   hipError_t e;

@@ -7,7 +7,8 @@
 // Both operands go from memory to registers and from there to LDS, among the matrix instructions of the tile before, and a register is loaded for
 // the tile after next (or, of small tiles, which are done before a load arrives, the one behind) as soon as it has been written.  (Loads straight to LDS: the compiler lets the transposing loads wait for all of them,
 // wherever they go.)
-// Several planes of A are taken as further k, the smallest first.
+// Several planes of A are taken as further k, the smallest first; by small tiles together with each k-tile of B, which is then staged and read once
+// for all of them (2048 x 2048 x 1024 tokens, three planes: 60 -> 47 us; larger tiles would have no room for two workgroups on a CU).
 // Where few rows of tiles need it, B is taken as the 8-bit codes that it comes from and made bf16 numbers on the way to LDS.
 #include <type_traits>
 
@@ -107,15 +108,16 @@ template <int NT, int X, bool POWERS, int DEPTH> struct StagedCodes {
   }
 };
 
-template <int BM, int BN> struct KnCfg {
-  static constexpr int A = BM * 128, B = BN * 128, STAGE = A + B, DEPTH = BM == 256 ? 1 : 2;
+template <int BM, int BN, int PL> struct KnCfg {
+  static constexpr int A = BM * 128, B = BN * 128, STAGE = PL * A + B, DEPTH = BM == 256 ? 1 : 2;
   static constexpr size_t lds = 2 * (size_t)STAGE;      // (more than the wavefronts need in the end)
 };
 
-template <bool A_KROWS, bool CODES, int BM, int BN, int WGM, int WGN>
+// PL planes of A are multiplied by a k-tile of B while it is in LDS; 1: the planes are further k.
+template <bool A_KROWS, bool CODES, int PL, int BM, int BN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P) {
-  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, DEPTH = KnCfg<BM, BN>::DEPTH;
-  constexpr int STAGE = KnCfg<BM, BN>::STAGE, A_BYTES = KnCfg<BM, BN>::A;
+  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, DEPTH = KnCfg<BM, BN, PL>::DEPTH;
+  constexpr int STAGE = KnCfg<BM, BN, PL>::STAGE, A_BYTES = KnCfg<BM, BN, PL>::A, B_LDS = PL * A_BYTES;
   extern __shared__ __attribute__((aligned(16))) char kn_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
@@ -140,28 +142,30 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
   int64_t next_k = (int64_t)next_kt * kKnK;
   int next_left = (int)(P.K - next_k < kKnK ? P.K - next_k : kKnK);      // k of it that exist
   const char *const a_first = P.A + (A_KROWS ? m0 * 2 : m0 * P.lda), *const b_first = P.B + n0 * (CODES ? 1 : 2);
-  Staged<NT, BM, A_KROWS, DEPTH> sa;
+  Staged<NT, BM, A_KROWS, DEPTH * PL> sa;
   std::conditional_t<CODES, StagedCodes<NT, BN, A_KROWS, DEPTH>, Staged<NT, BN, true, DEPTH>> sb;
   sa.init(P.lda, P.T.M - m0, tid);
   if constexpr (CODES) sb.init(P.ldb, P.T.N - n0, tid, P.units);
   else sb.init(P.ldb, P.T.N - n0, tid);
-  constexpr int NA = decltype(sa)::N, PIECES = NA + decltype(sb)::N;
+  constexpr int NA = decltype(sa)::N, PIECES = PL * NA + decltype(sb)::N;
   auto load = [&](int set, int p) RSVD_INLINE {
-    if (p < NA) sa.load(set, p, a_first + (P.planes - 1 - next_plane) * P.plane + (A_KROWS ? next_k * P.lda : next_k * 2), P.lda, next_left);
-    else if constexpr (CODES) sb.load(set, p - NA, b_first + next_k * P.ldb, P.ldb, next_left, P.units, next_k, n0);
-    else sb.load(set, p - NA, b_first + next_k * P.ldb, P.ldb, next_left);
+    if (p < PL * NA) {
+      const int plane = PL > 1 ? p / NA : P.planes - 1 - next_plane;
+      sa.load(PL * set + p / NA, p % NA, a_first + plane * P.plane + (A_KROWS ? next_k * P.lda : next_k * 2), P.lda, next_left);
+    } else if constexpr (CODES) sb.load(set, p - PL * NA, b_first + next_k * P.ldb, P.ldb, next_left, P.units, next_k, n0);
+    else sb.load(set, p - PL * NA, b_first + next_k * P.ldb, P.ldb, next_left);
   };
   auto write = [&](int set, int p, int buf) RSVD_INLINE {
-    if (p < NA) sa.write(set, p, kn_lds + buf * STAGE);
-    else if constexpr (CODES) sb.write(set, p - NA, kn_lds + buf * STAGE + A_BYTES, P.units);
-    else sb.write(set, p - NA, kn_lds + buf * STAGE + A_BYTES);
+    if (p < PL * NA) sa.write(PL * set + p / NA, p % NA, kn_lds + buf * STAGE + p / NA * A_BYTES);
+    else if constexpr (CODES) sb.write(set, p - PL * NA, kn_lds + buf * STAGE + B_LDS, P.units);
+    else sb.write(set, p - PL * NA, kn_lds + buf * STAGE + B_LDS);
   };
   auto advance = [&]() RSVD_INLINE {                    // (behind the last tile of this workgroup's range: loads stay inside the operands)
     next_k += kKnK;
     if (++next_kt == P.ktiles) {
       next_kt = 0;
       next_k = 0;
-      if (next_plane + 1 < P.planes) ++next_plane;
+      if (PL == 1 && next_plane + 1 < P.planes) ++next_plane;
     }
     next_left = (int)(P.K - next_k < kKnK ? P.K - next_k : kKnK);
   };
@@ -172,7 +176,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
   // (blocks of 16 columns differ from the first one of the wavefront in the bits that are exchanged)
   static_assert((TM == 8 || TM == 4 || TM == 2) && (TN == 8 || TN == 4 || TN == 2), "blocks of a power of two");
   const int a_at = A_KROWS ? key_row * A_ROW + (krow_piece<BM>(wm0 / 16, key_row) << 5) + part : (wm0 + r16) * 128;
-  const int b_at = A_BYTES + key_row * (BN * 2) + (krow_piece<BN>(wn0 / 16, key_row) << 5) + part;
+  const int b_at = B_LDS + key_row * (BN * 2) + (krow_piece<BN>(wn0 / 16, key_row) << 5) + part;
   typedef short s16x4 __attribute__((ext_vector_type(4)));
   auto transposed = [&](const char *p, int row_bytes) RSVD_INLINE {
     const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p)));
@@ -197,11 +201,13 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
   auto sum_a = [&](int buf) RSVD_INLINE {
     const int at = a_at + buf * STAGE, first = wave_n * SHARE;
 #pragma unroll
+    for (int q = PL - 1; q >= 0; --q)
+#pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < SHARE; ++i)
         if (first + i < TM) {
-          const u32x4 v = transposed(kn_lds + (at ^ ((first + i) << 5)) + h * 32 * A_ROW, A_ROW);
+          const u32x4 v = transposed(kn_lds + q * A_BYTES + (at ^ ((first + i) << 5)) + h * 32 * A_ROW, A_ROW);
 #pragma unroll
           for (int e = 0; e < 4; ++e) asum[i] += bf16_low(v[e]) + bf16_high(v[e]);
         }
@@ -212,28 +218,32 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
   auto body = [&](int buf, auto from) RSVD_INLINE {
     constexpr int SET = decltype(from)::value;
     const int a_now = a_at + buf * STAGE, b_now = b_at + buf * STAGE;
-    auto read_a = [&](int step) RSVD_INLINE {
+    auto read_a = [&](int step, u32x4 (&to)[PL]) RSVD_INLINE {
       const int h = step / TM, i = step % TM;
-      if (A_KROWS) return transposed(kn_lds + (a_now ^ (i << 5)) + h * 32 * A_ROW, A_ROW);
-      return *reinterpret_cast<const u32x4 *>(kn_lds + a_now + i * 2048 + (((4 * h + kq) ^ (r16 & 7)) << 4));
+#pragma unroll
+      for (int q = 0; q < PL; ++q)
+        to[q] = A_KROWS ? transposed(kn_lds + q * A_BYTES + (a_now ^ (i << 5)) + h * 32 * A_ROW, A_ROW)
+                        : *reinterpret_cast<const u32x4 *>(kn_lds + q * A_BYTES + a_now + i * 2048 + (((4 * h + kq) ^ (r16 & 7)) << 4));
     };
     auto read_b = [&](int h, int j) RSVD_INLINE { return transposed(kn_lds + (b_now ^ (j << 5)) + h * 32 * BN * 2, BN * 2); };
     constexpr int AHEAD = TM >= 4 ? 3 : 1;             // rows of blocks read ahead, not all of them: registers
-    u32x4 a[AHEAD + 1], b[2][TN];
+    u32x4 a[AHEAD + 1][PL], b[2][TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) b[0][j] = read_b(0, j);
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) a[i] = read_a(i);
+    for (int i = 0; i < AHEAD; ++i) read_a(i, a[i]);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int step = 0; step < 2 * TM; ++step) {
       const int h = step / TM, i = step % TM;
-      if (step + AHEAD < 2 * TM) a[(step + AHEAD) % (AHEAD + 1)] = read_a(step + AHEAD);
+      if (step + AHEAD < 2 * TM) read_a(step + AHEAD, a[(step + AHEAD) % (AHEAD + 1)]);
 #pragma unroll
       for (int j = 0; j < TN; ++j)
         if (h == 0 && i == j * TM / TN) b[1][j] = read_b(1, j);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(b[h][j], a[step % (AHEAD + 1)], acc[i][j]);
+      for (int q = PL - 1; q >= 0; --q)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(b[h][j], a[step % (AHEAD + 1)][q], acc[i][j]);
 #pragma unroll
       for (int p = 0; p < PIECES; ++p)
         if (p * (2 * TM) / PIECES == step) {
@@ -318,58 +328,66 @@ __global__ __launch_bounds__(256) void kn_end_kernel(const ReduceParams R, const
   P.out[j] = P.accumulate ? P.out[j] + sum : sum;
 }
 
+static TileChoice kn_choose(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, bool lowrank) {
+  return tile_choose(ctx, M, N, ceil_div(K, kKnK), planes, lowrank);
+}
 size_t kn_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, bool lowrank) {
-  return tile_partial_bytes(ctx, M, N, ceil_div(K, kKnK) * planes, lowrank);
+  return tile_partial_bytes(kn_choose(ctx, M, N, K, planes, lowrank), M, N, lowrank);
 }
 // Columns of tiles that share the sums of A.
 static int64_t kn_sum_columns(int64_t N, int bn) { return ceil_div(N, bn) < 8 ? ceil_div(N, bn) : 8; }
 int64_t kn_sum_rows(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes) {
-  const TileChoice c = tile_choose(ctx, M, N, ceil_div(K, kKnK) * planes);
+  const TileChoice c = kn_choose(ctx, M, N, K, planes, false);
   return c.splits * kn_sum_columns(N, c.bn);
 }
 
-template <bool A_KROWS, bool CODES, int BM, int BN, int WGM, int WGN> static hipError_t kn_run(hipStream_t s, const KnParams &P) {
-  hipLaunchKernelGGL((kn_kernel<A_KROWS, CODES, BM, BN, WGM, WGN>), dim3(tile_groups(P.T)), dim3(64 * WGM * WGN), (KnCfg<BM, BN>::lds), s, P);
+template <bool A_KROWS, bool CODES, int PL, int BM, int BN, int WGM, int WGN> static hipError_t kn_run(hipStream_t s, const KnParams &P) {
+  hipLaunchKernelGGL((kn_kernel<A_KROWS, CODES, PL, BM, BN, WGM, WGN>), dim3(tile_groups(P.T)), dim3(64 * WGM * WGN), (KnCfg<BM, BN, PL>::lds), s, P);
   return hipGetLastError();
 }
 
+template <bool A_KROWS, bool CODES> static hipError_t kn_run_small(hipStream_t s, const KnParams &P, int bm) {
+  if (bm == 128) return kn_run<A_KROWS, CODES, 1, 128, 128, 2, 2>(s, P);
+  if (P.planes == 1) return kn_run<A_KROWS, CODES, 1, 64, 64, 2, 2>(s, P);
+  return P.planes == 2 ? kn_run<A_KROWS, CODES, 2, 64, 64, 2, 2>(s, P) : kn_run<A_KROWS, CODES, 3, 64, 64, 2, 2>(s, P);
+}
 template <bool A_KROWS> static hipError_t kn_run_tile(hipStream_t s, const KnParams &P, int bm, bool codes) {
-  if (bm == 256) return kn_run<A_KROWS, false, 256, 256, 2, 4>(s, P);
-  if (codes) return bm == 128 ? kn_run<A_KROWS, true, 128, 128, 2, 2>(s, P) : kn_run<A_KROWS, true, 64, 64, 2, 2>(s, P);
-  return bm == 128 ? kn_run<A_KROWS, false, 128, 128, 2, 2>(s, P) : kn_run<A_KROWS, false, 64, 64, 2, 2>(s, P);
+  if (bm == 256) return kn_run<A_KROWS, false, 1, 256, 256, 2, 4>(s, P);
+  return codes ? kn_run_small<A_KROWS, true>(s, P, bm) : kn_run_small<A_KROWS, false>(s, P, bm);
 }
 
-// Every row of tiles makes bf16 numbers of all the codes again, and every plane; a matrix of them is made once and read twice as long.  Rows of tiles
-// times planes up to which the codes are taken as they are, measured as codes / matrix.  Weight, 4096 x 4096 codes with 64 columns of dY in
-// bf16 (1) 18 / 34 us, 256 (4) 31 / 42, 512 (8) 49 / 51; 2048 x 2048 with 1024 (16) 28 / 33; 4096 x 4096 with 256 of fp32 (12) 49 / 53, 512 (24)
-// 78 / 75.  X, where a launch before the product is needed anyway: 128 tokens with 16384 x 4096 codes, bf16 (1) 62 / 81 us, fp32 (3) 126 / 145;
-// 256 with 4096 x 4096 (4) 43 / 46, 512 (8) 52 / 48, 256 of fp32 (12) 70 / 68.
-bool kn_takes_codes(const rsvd_ctx *ctx, bool a_krows, int64_t M, int64_t N, int64_t K, int planes, int64_t ldc, int64_t ldp) {
-  const TileChoice c = tile_choose(ctx, M, N, ceil_div(K, kKnK) * planes);
-  return c.bm < 256 && ceil_div(M, c.bm) * planes <= (a_krows ? 16 : 4) && ldc <= kMaxLd && ldp <= kMaxLd;
+// Every row of tiles makes bf16 numbers of all the codes again, and so does every plane that is further k; a matrix of them is made once and read twice as
+// long.  Rows of tiles (times such planes) up to which the codes are taken as they are, measured as codes / matrix.  Weight: 4096 x 4096 codes with
+// 64 columns of dY in bf16 (1) 18 / 34 us, fp32 (1) 23 / 33, 256 of bf16 (4) 31 / 42, 512 (8) 49 / 51, 512 of fp16 (8) 68 / 66; 2048 x 2048 with 1024 of
+// bf16 (16) 28 / 33.  X, where a launch before the product is needed anyway: 128 tokens with 16384 x 4096 codes, bf16 (1) 62 / 81 us, fp32 (3)
+// 126 / 145; 256 with 4096 x 4096 (4) 43 / 46, 512 (8) 52 / 48; fp16 54 / 57 and 67 / 66.
+bool kn_takes_codes(const rsvd_ctx *ctx, bool a_krows, int64_t M, int64_t N, int64_t K, int planes, bool lowrank, int64_t ldc,
+                    int64_t ldp) {
+  const TileChoice c = kn_choose(ctx, M, N, K, planes, lowrank);
+  return c.bm < 256 && ceil_div(M, c.bm) * (c.bm == 64 ? 1 : planes) <= (a_krows ? 16 : 4) && ldc <= kMaxLd && ldp <= kMaxLd;
 }
 
 hipError_t nt_init_device();
 hipError_t layer8_init_device(rsvd_ctx *) {
   hipError_t e = nt_init_device();
-  const void *wide[2] = {reinterpret_cast<const void *>(&kn_kernel<true, false, 256, 256, 2, 4>),
-                         reinterpret_cast<const void *>(&kn_kernel<false, false, 256, 256, 2, 4>)};
+  const void *wide[2] = {reinterpret_cast<const void *>(&kn_kernel<true, false, 1, 256, 256, 2, 4>),
+                         reinterpret_cast<const void *>(&kn_kernel<false, false, 1, 256, 256, 2, 4>)};
   for (const void *k : wide)
-    if (e == hipSuccess) e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)KnCfg<256, 256>::lds);
+    if (e == hipSuccess) e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)KnCfg<256, 256, 1>::lds);
   return e;
 }
 
 hipError_t kn_launch(rsvd_ctx *ctx, hipStream_t s, const KnDesc &d) {
-  const int64_t ktiles = ceil_div(d.K, kKnK), kt = ktiles * d.planes;
-  const TileChoice c = tile_choose(ctx, d.M, d.N, kt);
-  if (c.splits > 1 && (d.partial == nullptr || d.partial_bytes < tile_partial_bytes(ctx, d.M, d.N, kt, d.out.r > 0))) return hipErrorInvalidValue;
+  const TileChoice c = kn_choose(ctx, d.M, d.N, d.K, d.planes, d.out.r > 0);
+  const int64_t ktiles = ceil_div(d.K, kKnK), kt = c.kt;
+  if (c.splits > 1 && (d.partial == nullptr || d.partial_bytes < tile_partial_bytes(c, d.M, d.N, d.out.r > 0))) return hipErrorInvalidValue;
   KnParams P;
   P.A = (const char *)d.A; P.lda = d.lda; P.plane = d.plane; P.planes = d.planes;
   P.ktiles = (int)ktiles; P.K = d.K;
   P.B = (const char *)d.B; P.ldb = d.ldb;
   const bool codes = d.codes != nullptr;
   if (codes) {
-    if (!kn_takes_codes(ctx, d.a_krows, d.M, d.N, d.K, d.planes, d.ldc, d.units.ldp)) return hipErrorInvalidValue;
+    if (!kn_takes_codes(ctx, d.a_krows, d.M, d.N, d.K, d.planes, d.out.r > 0, d.ldc, d.units.ldp)) return hipErrorInvalidValue;
     P.B = (const char *)d.codes; P.ldb = d.ldc;
   }
   P.units = d.units;

@@ -228,11 +228,11 @@ template <bool CODES> __device__ __forceinline__ void reduce_group(const ReduceP
 }
 
 
-// Tile and ranges of k for kt k-tiles.
-struct TileChoice { int bm, bn, splits; int64_t kt_per_split; };
-TileChoice tile_choose(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt);
-inline size_t tile_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt, bool lowrank) {
-  const TileChoice c = tile_choose(ctx, M, N, kt);
+// Tile and ranges of k for kt k-tiles of each of `planes` matrices A.  Small tiles take a k-tile of all planes at once, others one after
+// the other (TileChoice::kt in all).  lowrank: a low-rank term is added.
+struct TileChoice { int bm, bn, splits; int64_t kt_per_split, kt; };
+TileChoice tile_choose(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt, int planes, bool lowrank);
+inline size_t tile_partial_bytes(const TileChoice &c, int64_t M, int64_t N, bool lowrank) {
   return c.splits > 1 ? (size_t)(c.splits + (lowrank ? 1 : 0)) * M * N * 4 : 0;
 }
 inline TileParams tile_params(const TileChoice &c, int64_t M, int64_t N, int64_t kt, float *partial, const Layer8Out &out) {

@@ -25,6 +25,7 @@ hipError_t rows8_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n,
 }
 
 // ---------------------------------------------------------------- blocks of 32 with a power of two
+// Memory is the bound.  16384 x 4096 bf16: 42 us to save (203 MB, 4.8 TB/s), 31 us to load; 1001 x 2999 fp32 4.4 and 6.4 us.
 // Eight features a thread, so four lanes share a block.  A workgroup covers `lanes` chunks (a power of two, at least 4) of 256 / lanes rows.
 __device__ __forceinline__ unsigned quad_max(unsigned x) {
   x = max(x, (unsigned)__builtin_amdgcn_mov_dpp((int)x, 0xb1, 0xf, 0xf, true));      // lanes 1 0 3 2

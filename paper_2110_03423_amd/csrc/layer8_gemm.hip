@@ -1,13 +1,14 @@
 // Products of two matrices of 8-bit codes with consecutive k, for many tokens.
 //
-// Tiles of BM x BN outputs by WGM x WGN wavefronts.  A k-tile is 128 codes of every row of both operands; two of them have room in LDS, which is
+// Tiles of BM x BN outputs by WGM x WGN wavefronts.  A k-tile is 128 codes of every row of both operands; two of them (three of small tiles, which
+// are done before a load arrives: 333 x 2999 x 1410 26 -> 21 us) have room in LDS, which is
 // filled by loads that write there themselves, issued over the first half of the matrix instructions of the tile before.  LDS is written in the
 // order of the lanes, 16 bytes each, so a lane fetches the piece that belongs to its place: piece ch of row r lies in place ch ^ (r mod 8), which
 // lets the eight rows that are read together start at different banks.
-// Large products are bound by the power that the card may take (59 % of the matrix pipe's cycles at 1.9 GHz): 16384 x 4096 x 16384 948 us (2.32 POP/s, a large product of
-// the library 2.06), 2048 x 16384 x 4096 141 us (1.96, two tiles a CU and the stores of both).  256 rows and columns by four wavefronts of 128 x 128 read LDS
-// least (14 % busy) and have the room for it in the accumulation registers.
-// The first operand of the instruction is B, so that a lane ends with four consecutive columns of C in its registers.
+// Large products are bound by the power that the card may take (59 % of the matrix pipe's cycles at 1.9 GHz): 16384 x 4096 x 16384 939 to 986
+// us (2.23 to 2.34 POP/s, a large product of the library 2.06), 2048 x 16384 x 4096 141 us (1.96, two tiles a CU and the stores of both).  256
+// rows and columns by four wavefronts of 128 x 128 read LDS least (14 % busy) and have the room for it in the accumulation registers. The
+// first operand of the instruction is B, so that a lane ends with four consecutive columns of C in its registers.
 #include "layer8_tile.hpp"
 
 namespace rsvd {
@@ -169,7 +170,9 @@ TileChoice tile_choose(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt, in
   return best;
 }
 
-size_t nt_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt, bool lowrank) { return tile_partial_bytes(tile_choose(ctx, M, N, kt, 1, lowrank), M, N, lowrank); }
+size_t nt_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t kt, bool lowrank) {
+  return tile_partial_bytes(tile_choose(ctx, M, N, kt, 1, lowrank), M, N, lowrank);
+}
 
 template <int BM, int BN, int WGM, int WGN> static hipError_t nt_run(hipStream_t s, const NtParams &P) {
   hipLaunchKernelGGL((nt_kernel<BM, BN, WGM, WGN>), dim3(tile_groups(P.T)), dim3(64 * WGM * WGN), (NtCfg<BM, BN>::lds), s, P);

@@ -4,15 +4,15 @@
 // tiles [k][x] of bf16 numbers in LDS are read with the transposing LDS load (sixteen lanes read four k of sixteen columns and get one column of
 // four k each).  LDS rows of such a tile have their 32-byte pieces exchanged by the low bits of k, so that the eight rows that half a wavefront
 // reads start at different banks; rows of consecutive k have their 16-byte pieces exchanged by the row.
-// Both operands go from memory to registers and from there to LDS, among the matrix instructions of the tile before, and a register is loaded for
-// the tile after next (or, of small tiles, which are done before a load arrives, the one behind) as soon as it has been written.  (Loads straight to LDS: the compiler lets the transposing loads wait for all of them,
-// wherever they go.)
-// Large products are bound by power like those of codes (60 % of the matrix pipe's cycles at 1.8 GHz): gradient of a weight 16384 x 4096 over 16384 tokens 1823 to
-// 1929 us (1.14 to 1.2 PFLOP/s; the library takes 1932 for operands in these orders), 4096 tokens of 16384 to 4096 445 to 479 us (1.15 to 1.24).  Eight
-// wavefronts of 128 x 64: four of 128 x 128 would have no registers left for what they stage.
-// Several planes of A are taken as further k, the smallest first; by small tiles together with each k-tile of B, which is then staged and read once
-// for all of them (2048 x 2048 x 1024 tokens, three planes: 60 -> 47 us; larger tiles would have no room for two workgroups on a CU).
-// Where few rows of tiles need it, B is taken as the 8-bit codes that it comes from and made bf16 numbers on the way to LDS.
+// Both operands go from memory to registers and from there to LDS, among the matrix instructions of the tile before, and a register is loaded
+// for the tile after next (or, of small tiles, which are done before a load arrives, the one behind) as soon as it has been written.  (Loads
+// straight to LDS: the compiler lets the transposing loads wait for all of them, wherever they go.) Large products are bound by power like
+// those of codes (60 % of the matrix pipe's cycles at 1.8 GHz): gradient of a weight 16384 x 4096 over 16384 tokens 1823 to 1929 us (1.14 to
+// 1.2 PFLOP/s; the library takes 1932 for operands in these orders), 4096 tokens of 16384 to 4096 445 to 479 us (1.15 to 1.24).  Eight
+// wavefronts of 128 x 64: four of 128 x 128 would have no registers left for what they stage. Several planes of A are taken as further k, the
+// smallest first; by small tiles together with each k-tile of B, which is then staged and read once for all of them (2048 x 2048 x 1024
+// tokens, three planes: 60 -> 47 us; larger tiles would have no room for two workgroups on a CU). Where few rows of tiles need it, B is taken
+// as the 8-bit codes that it comes from and made bf16 numbers on the way to LDS.
 #include <type_traits>
 
 #include "layer8_rows.hpp"

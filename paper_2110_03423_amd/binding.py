@@ -520,20 +520,21 @@ class Rsvd:
 
     def rsvd_keep8_save(self, X):
         """X (tokens x n) kept in 8 bits for the backward pass (Kept8)."""
-        _rows(X, X.shape[1], "X")
-        tokens, n = X.shape
+        tokens, n = _rows(X, X.shape[-1], "X"), X.shape[1]
         codes = _empty_codes(tokens, n, X.device)
-        powers = self.torch.empty((tokens, -(-n // 32)), dtype=self.torch.uint8, device=X.device)
-        self._check(self.lib.rsvd_keep8_save(self.h, self._raw_stream(), _xtype_code(X.dtype), tokens, n, _at(X), _ld(X),
-                                             _at(codes), _ld(codes), _at(powers), _ld(powers)))
+        powers = X.new_empty((tokens, -(-n // 32)), dtype=self.torch.uint8)
+        self._check(self.lib.rsvd_keep8_save(self.h, self._raw_stream(), _xtype_code(X.dtype), tokens, n, X.data_ptr(), _ld(X),
+                                             codes.data_ptr(), codes.stride(0), powers.data_ptr(), -(-n // 32)))
         return Kept8.__new__(Kept8)._set(codes, powers, X.dtype)
 
     def rsvd_keep8_load(self, kept, out=None):
         """The kept activations, in their type."""
-        X = out if out is not None else self.torch.empty((kept.tokens, kept.n), dtype=kept.dtype, device=kept.codes.device)
-        _rows(X, kept.n, "out", kept.tokens, kept.dtype)
-        self._check(self.lib.rsvd_keep8_load(self.h, self._raw_stream(), _xtype_code(X.dtype), kept.tokens, kept.n,
-                                             _at(kept.codes), _ld(kept.codes), _at(kept.powers), _ld(kept.powers), _at(X), _ld(X)))
+        tokens, n, codes, powers = kept.tokens, kept.n, kept.codes, kept.powers
+        X = codes.new_empty((tokens, n), dtype=kept.dtype) if out is None else out
+        if out is not None:
+            _rows(out, n, "out", tokens, kept.dtype)
+        self._check(self.lib.rsvd_keep8_load(self.h, self._raw_stream(), _xtype_code(kept.dtype), tokens, n,
+                                             codes.data_ptr(), _ld(codes), powers.data_ptr(), _ld(powers), X.data_ptr(), _ld(X)))
         return X
 
     def rsvd_keep8_grad(self, dY, kept, out=None, accumulate=False, workspace=None):

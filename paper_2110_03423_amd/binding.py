@@ -176,14 +176,10 @@ class Weight8:
         if bias is not None and bias.shape != (m,):
             raise ValueError("bias: m values")
         self.bias = None if bias is None else bias.float().contiguous()
-        # what the C entry points are told of it, put together once: a call of a single token is short
-        at = (_at(self.codes), _ld(self.codes), _at(self.scale))
         self._sizes = (n, m, self.r)
-        self._product = (*at, _at(self.U), self.r, _at(self.Vt), n, _at(self.bias))
-        self._grad = (*at, _at(self.Ut), m, _at(self.V), self.r)
 
     def __setattr__(self, name, value):
-        if "_grad" in self.__dict__:
+        if "_sizes" in self.__dict__:
             raise AttributeError("a Weight8 keeps its tensors (their values may change): make another one")
         object.__setattr__(self, name, value)
 
@@ -494,28 +490,32 @@ class Rsvd:
 
     def rsvd_q8_product(self, X, weight, workspace=None, out=None):
         """X (tokens x n) through the layer `weight` (Weight8): tokens x m, in the type of X."""
-        n, m, r = sizes = weight._sizes
+        w = weight
+        n, m, r = sizes = w._sizes
         tokens, xt = _rows(X, n, "X"), _xtype_code(X.dtype)
         stream = self._raw_stream()
         ws = _given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_q8_product_bytes", (xt, tokens, *sizes))
         Y = X.new_empty((tokens, m)) if out is None else out
         if out is not None:
             _rows(out, m, "out", tokens, X.dtype)
-        self._check(self.lib.rsvd_q8_product(self.h, stream, xt, tokens, n, m, r, X.data_ptr(), _ld(X), *weight._product,
-                                             Y.data_ptr(), _ld(Y), ws[0], ws[1]))
+        self._check(self.lib.rsvd_q8_product(self.h, stream, xt, tokens, n, m, r, X.data_ptr(), _ld(X),
+                                             w.codes.data_ptr(), _ld(w.codes), w.scale.data_ptr(),
+                                             _at(w.U), r, _at(w.Vt), n, _at(w.bias), Y.data_ptr(), _ld(Y), ws[0], ws[1]))
         return Y
 
     def rsvd_q8_product_grad(self, dY, weight, workspace=None, out=None):
         """Gradient of rsvd_q8_product with respect to X: dY (tokens x m) to tokens x n, in the type of dY."""
-        n, m, r = sizes = weight._sizes
+        w = weight
+        n, m, r = sizes = w._sizes
         tokens, xt = _rows(dY, m, "dY"), _xtype_code(dY.dtype)
         stream = self._raw_stream()
         ws = _given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_q8_product_grad_bytes", (xt, tokens, *sizes))
         dX = dY.new_empty((tokens, n)) if out is None else out
         if out is not None:
             _rows(out, n, "out", tokens, dY.dtype)
-        self._check(self.lib.rsvd_q8_product_grad(self.h, stream, xt, tokens, n, m, r, dY.data_ptr(), _ld(dY), *weight._grad,
-                                                  dX.data_ptr(), _ld(dX), ws[0], ws[1]))
+        self._check(self.lib.rsvd_q8_product_grad(self.h, stream, xt, tokens, n, m, r, dY.data_ptr(), _ld(dY),
+                                                  w.codes.data_ptr(), _ld(w.codes), w.scale.data_ptr(),
+                                                  _at(w.Ut), m, _at(w.V), r, dX.data_ptr(), _ld(dX), ws[0], ws[1]))
         return dX
 
     def rsvd_keep8_save(self, X):

@@ -29,6 +29,7 @@ struct KnParams {
   const char *B; int64_t ldb;              // bytes
   CodeUnits units;                         // B holds codes
   float *sums; int sum_columns;            // A_KROWS: sums of A over k by ranges, [split][sum_columns][M], or NULL
+  int sums_whole, sums_accumulate;         // they are one row, and what is wanted (added to it)
   TileParams T;
 };
 
@@ -195,31 +196,35 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
     __builtin_amdgcn_sched_barrier(0);
   };
 
-  // ---- sums of A over k: k-tile kt is summed by the tiles of column kt mod sum_columns, each wavefront its share of the rows
+  // ---- sums of A over k
+  // Large tiles: k-tile kt is summed by the tiles of column kt mod sum_columns, each wavefront its share of the rows.  Small ones: by the tiles of the first
+  // column (sum_columns is 1), as products with ones of what is in registers anyway.
   constexpr int SHARE = A_KROWS ? (TM + WGN - 1) / WGN : 1;
-  float asum[SHARE];
+  const bool sums_here = A_KROWS && P.sums != nullptr && tile_n < P.sum_columns;
+  f32x4 asum[SHARE][PL];                               // (of each plane: no chain of instructions that wait for each other)
 #pragma unroll
-  for (int i = 0; i < SHARE; ++i) asum[i] = 0.f;
+  for (int i = 0; i < SHARE; ++i)
+#pragma unroll
+    for (int q = 0; q < PL; ++q) asum[i][q] = (f32x4)0.f;
   int now_column = __builtin_amdgcn_readfirstlane(kt_begin % P.sum_columns);      // of the tile that is multiplied
   auto sum_a = [&](int buf) RSVD_INLINE {
     const int at = a_at + buf * STAGE, first = wave_n * SHARE;
-#pragma unroll
-    for (int q = PL - 1; q >= 0; --q)
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int i = 0; i < SHARE; ++i)
         if (first + i < TM) {
-          const u32x4 v = transposed(kn_lds + q * A_BYTES + (at ^ ((first + i) << 5)) + h * 32 * A_ROW, A_ROW);
+          const u32x4 v = transposed(kn_lds + (at ^ ((first + i) << 5)) + h * 32 * A_ROW, A_ROW);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) asum[i] += bf16_low(v[e]) + bf16_high(v[e]);
+          for (int e = 0; e < 4; ++e) asum[i][0][0] += bf16_low(v[e]) + bf16_high(v[e]);
         }
   };
 
   // The matrix instructions of a tile, with the next one going to LDS in step.  (Behind the last tile that is one that nobody reads: no
   // branches.)
-  auto body = [&](int buf, auto from) RSVD_INLINE {
+  auto body = [&](int buf, auto from, auto sums) RSVD_INLINE {
     constexpr int SET = decltype(from)::value;
+    constexpr bool SUMS = decltype(sums)::value;
     const int a_now = a_at + buf * STAGE, b_now = b_at + buf * STAGE;
     auto read_a = [&](int step, u32x4 (&to)[PL]) RSVD_INLINE {
       const int h = step / TM, i = step % TM;
@@ -247,6 +252,11 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
       for (int q = PL - 1; q >= 0; --q)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(b[h][j], a[step % (AHEAD + 1)][q], acc[i][j]);
+      if (SUMS && i / SHARE == wave_n) {
+        const u32x4 ones = {0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u};
+#pragma unroll
+        for (int q = PL - 1; q >= 0; --q) asum[i % SHARE][q] = mfma_bf16(ones, a[step % (AHEAD + 1)][q], asum[i % SHARE][q]);
+      }
 #pragma unroll
       for (int p = 0; p < PIECES; ++p)
         if (p * (2 * TM) / PIECES == step) {
@@ -272,29 +282,44 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
     advance();
     meet();
   }
-  auto tile = [&](int buf, auto from) RSVD_INLINE {
-    if (A_KROWS && P.sums != nullptr && now_column == tile_n) sum_a(buf);
-    body(buf, from);
+  auto tile = [&](int buf, auto from, auto sums) RSVD_INLINE {
+    if (BM > 64 && sums_here && now_column == tile_n) sum_a(buf);
+    body(buf, from, sums);
     advance();
     if (++now_column == P.sum_columns) now_column = 0;
     meet();
   };
-  if constexpr (DEPTH == 1) {
-    for (int kt = 0; kt < nkt; ++kt) tile(kt & 1, std::integral_constant<int, 0>());
-  } else {
-    for (int kt = 0; kt < nkt; kt += 2) {
-      tile(0, std::integral_constant<int, 1>());
-      if (kt + 1 < nkt) tile(1, std::integral_constant<int, 0>());
+  auto all = [&](auto sums) RSVD_INLINE {
+    if constexpr (DEPTH == 1) {
+      for (int kt = 0; kt < nkt; ++kt) tile(kt & 1, std::integral_constant<int, 0>(), sums);
+    } else {
+      for (int kt = 0; kt < nkt; kt += 2) {
+        tile(0, std::integral_constant<int, 1>(), sums);
+        if (kt + 1 < nkt) tile(1, std::integral_constant<int, 0>(), sums);
+      }
     }
+  };
+  if constexpr (A_KROWS && BM == 64) {
+    if (sums_here) all(std::true_type());
+    else all(std::false_type());
+  } else {
+    all(std::false_type());
   }
-  if (A_KROWS && P.sums != nullptr && tile_n < P.sum_columns) {      // (no low-rank term there: split is a range of k)
+  if (sums_here) {      // (no low-rank term there: split is a range of k)
 #pragma unroll
     for (int i = 0; i < SHARE; ++i) {
-      float sum = asum[i];
-      sum += __shfl_xor(sum, 16);
-      sum += __shfl_xor(sum, 32);
+      float sum = asum[i][PL - 1][0];
+#pragma unroll
+      for (int q = PL - 2; q >= 0; --q) sum += asum[i][q][0];
+      if (BM > 64) {
+        sum += __shfl_xor(sum, 16);
+        sum += __shfl_xor(sum, 32);
+      }
       const int64_t m = m0 + wm0 + (wave_n * SHARE + i) * 16 + r16;
-      if (lane < 16 && wave_n * SHARE + i < TM && m < P.T.M) P.sums[((int64_t)split * P.sum_columns + tile_n) * P.T.M + m] = sum;
+      if (lane < 16 && wave_n * SHARE + i < TM && m < P.T.M) {
+        float *to = P.sums + ((int64_t)split * P.sum_columns + tile_n) * P.T.M + m;
+        *to = P.sums_whole && P.sums_accumulate ? *to + sum : sum;
+      }
     }
   }
   int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
@@ -337,11 +362,15 @@ static TileChoice kn_choose(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K
 size_t kn_partial_bytes(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes, bool lowrank) {
   return tile_partial_bytes(kn_choose(ctx, M, N, K, planes, lowrank), M, N, lowrank);
 }
-// Columns of tiles that share the sums of A.
-static int64_t kn_sum_columns(int64_t N, int bn) { return ceil_div(N, bn) < 8 ? ceil_div(N, bn) : 8; }
+// Columns of tiles that share the sums of A.  (Small tiles with one range of k need no launch to add them up: 1000 x 1000 x 1000 bf16 15.2 -> 13.5 us.  128
+// rows and columns have no registers for it.)
+static int64_t kn_sum_columns(const TileChoice &c, int64_t N) {
+  const int64_t most = c.bm == 64 ? 1 : 8;
+  return ceil_div(N, c.bn) < most ? ceil_div(N, c.bn) : most;
+}
 int64_t kn_sum_rows(const rsvd_ctx *ctx, int64_t M, int64_t N, int64_t K, int planes) {
   const TileChoice c = kn_choose(ctx, M, N, K, planes, false);
-  return c.splits * kn_sum_columns(N, c.bn);
+  return c.splits * kn_sum_columns(c, N);
 }
 
 template <bool A_KROWS, bool CODES, int PL, int BM, int BN, int WGM, int WGN> static hipError_t kn_run(hipStream_t s, const KnParams &P) {
@@ -395,12 +424,15 @@ hipError_t kn_launch(rsvd_ctx *ctx, hipStream_t s, const KnDesc &d) {
   }
   P.units = d.units;
   P.sums = d.a_krows ? d.sums : nullptr;
-  P.sum_columns = (int)kn_sum_columns(d.N, c.bn);
+  P.sum_columns = (int)kn_sum_columns(c, d.N);
+  P.sums_whole = c.splits * P.sum_columns == 1;
+  P.sums_accumulate = d.out.accumulate;
+  if (P.sums != nullptr && P.sums_whole) P.sums = d.sums_out;
   P.T = tile_params(c, d.M, d.N, kt, d.partial, d.out);
   const hipError_t e = d.a_krows ? kn_run_tile<true>(s, P, c.bm, codes) : kn_run_tile<false>(s, P, c.bm, codes);
   const ReduceParams R = reduce_params(P.T);
   const SumsParams S = {P.sums, (int64_t)c.splits * P.sum_columns, d.M, d.sums_out, d.out.accumulate};
-  const int64_t groups = R.groups + (P.sums != nullptr ? ceil_div(d.M, 16) : 0);
+  const int64_t groups = R.groups + (P.sums != nullptr && !P.sums_whole ? ceil_div(d.M, 16) : 0);
   if (e != hipSuccess || groups == 0) return e;
   hipLaunchKernelGGL(kn_end_kernel, dim3((unsigned)groups), dim3(256), 0, s, R, S);
   return hipGetLastError();

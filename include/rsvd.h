@@ -343,8 +343,9 @@ int rsvd_q8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
 /* dX (tokens x n) = dY W, the gradient of rsvd_q8_product with respect to X
  * (the rounding of X to its codes is passed straight through).  The factors
  * are given by rows of the other index: Ut r x m (ldut >= m), V n x r (ldv >= r).
- * For bf16 tokens scale_i codes_ij is rounded to bf16 once; for fp16 and
- * fp32 dY_ti scale_i is split into two and three bf16 numbers. */
+ * dY_ti scale_i is rounded to fp32 and taken as two bf16 numbers (bf16 and
+ * fp16 tokens; 2^-17 of it is left out) or three (fp32; nothing is); the codes
+ * are exact. */
 int rsvd_q8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int64_t r,
                          const void *dY, int64_t lddy, const int8_t *codes, int64_t ldq, const float *scale,
                          const void *Ut, int64_t ldut, const void *V, int64_t ldv,

@@ -23,6 +23,9 @@ typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
 inline int64_t xtype_size(rsvd_xtype t) { return t == RSVD_X_F32 ? 4 : 2; }
 // bf16 numbers whose sum is exactly a number of the type.
 inline int xtype_parts(rsvd_xtype t) { return t == RSVD_X_BF16 ? 1 : t == RSVD_X_F16 ? 2 : 3; }
+// bf16 numbers that hold such a number times an fp32 scale: to 2^-17 of it (two; results of 16 bits), or as fp32 has it (three).  One, with the scale
+// rounded into the weight, would be half the product, and was not kept: an error of 1.24 times the rounding of a bf16 result.
+inline int scaled_parts(rsvd_xtype t) { return t == RSVD_X_F32 ? 3 : 2; }
 // Rows that may be read and written in 16-byte pieces.
 inline bool rows_aligned(const void *p, int64_t ld, int64_t size) { return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0; }
 
@@ -184,12 +187,12 @@ hipError_t lowrank_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t
 hipError_t front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t n, int64_t r, const void *X, int64_t ldx,
                         const void *F, int64_t ldf, float *sums, int8_t *codes, int64_t ldq, int64_t width, float *scale);
 // The operands of kn_launch for a gradient, and lowrank_launch for dY (r = 0: without): planes[q][token][0 .. planes_width) the bf16 parts of dY
-// (tokens x m, times dy_factor_j or NULL), zeros from m on (planes NULL: not wanted); plane[row][0 .. width) the codes (rows x n) as bf16 numbers, multiplied by
-// factor_row (NULL: as they are) or by the powers of two of kept activations (plane NULL: not wanted).  Widths are m and n up to a multiple of 8.
+// (tokens x m), or of dY_tj dy_factor_j (scaled_parts() of them), zeros from m on (planes NULL: not wanted); plane[row][0 .. width) the codes (rows x n) as
+// bf16 numbers, multiplied by the powers of two of kept activations (NULL: as they are; plane NULL: not wanted).  Widths are m and n up to a multiple of 8.
 hipError_t grad_front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t m, int64_t r, const void *dY, int64_t lddy,
                              const void *F, int64_t ldf, float *sums, const float *dy_factor, uint16_t *planes, int64_t planes_width,
-                             int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const float *factor, const uint8_t *powers, int64_t ldp,
-                             uint16_t *plane, int64_t width);
+                             int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp, uint16_t *plane,
+                             int64_t width);
 // t [tokens][parts][rank_places(r)]: the sums added up, as bf16 numbers, the largest first.
 hipError_t lowrank_join_launch(hipStream_t s, const float *sums, int splits, int64_t tokens, int64_t r, int parts, uint16_t *t);
 
@@ -220,11 +223,6 @@ hipError_t nt_launch(rsvd_ctx *ctx, hipStream_t s, const NtDesc &d);
 // ---------------------------------------------------------------- layer8_grad.hip
 // C (M x N) = sum over k < K of A_mk B_kn of bf16 numbers, A a sum of `planes` matrices (`plane` bytes apart, the largest first), B with rows of n.
 // a_krows: A is stored K x M, else M x K.  Rows of both may be read in 16-byte pieces as far as these hold an element.
-// What codes are multiplied by: powers of two of kept activations (row k, blocks of 32 columns), or a factor for each row, or nothing.
-struct CodeUnits {
-  const float *factor = nullptr;
-  const uint8_t *powers = nullptr; int64_t ldp = 0;
-};
 struct KnDesc {
   int64_t M = 0, N = 0, K = 0;
   bool a_krows = false;
@@ -232,7 +230,7 @@ struct KnDesc {
   int planes = 1; int64_t plane = 0;
   const uint16_t *B = nullptr; int64_t ldb = 0;            // bytes
   const int8_t *codes = nullptr; int64_t ldc = 0;          // in the place of B, where kn_takes_codes(): codes (K x N)
-  CodeUnits units;
+  const uint8_t *powers = nullptr; int64_t ldp = 0;        // a_krows: their powers of two (row k, blocks of 32 columns)
   float *sums = nullptr, *sums_out = nullptr;              // a_krows: place for kn_sum_rows() parts of the sums of A over k, M each, and for the sums; or NULL
   Layer8Out out;
   float *partial = nullptr; size_t partial_bytes = 0;

@@ -57,13 +57,13 @@ bool takes_rows(rsvd_xtype type, const void *p, int64_t cols, int64_t ld) {
   return type == RSVD_X_BF16 && cols % 8 == 0 && rows_aligned(p, ld, 2) && ld <= kMaxLd / 4;
 }
 
-// planes of dY where it cannot be taken as it is, codes as bf16 numbers, low-rank sums before and after they are joined, or column sums of dY, parts of sums
+// planes of dY (of a weight gradient: where it cannot be taken as it is), codes as bf16 numbers, low-rank sums before and after they are joined, or column sums of dY, parts of sums
 struct GradLayout { size_t a, b, sums, t, partial, partial_bytes, total; int64_t width, b_width; int planes, splits; };
 
 GradLayout product_grad_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int64_t r) {
   GradLayout L;
   Take take;
-  L.planes = xtype_parts(type);
+  L.planes = scaled_parts(type);
   L.width = (int64_t)align_up((size_t)m, 8);
   L.b_width = (int64_t)align_up((size_t)n, 8);
   L.a = take((size_t)L.planes * tokens * L.width * 2);
@@ -248,22 +248,22 @@ int rsvd_q8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t t
   hipStream_t s = (hipStream_t)stream;
   char *ws = (char *)workspace;
   uint16_t *a = (uint16_t *)(ws + L.a), *b = (uint16_t *)(ws + L.b), *t = (uint16_t *)(ws + L.t);
-  // one part: the scale goes to the codes; several: to dY before it is split, and the codes stay exact
-  const bool single = L.planes == 1, direct = takes_rows(type, dY, m, lddy), as_codes = kn_takes_codes(ctx, false, tokens, n, m, L.planes, r > 0, ldq, 0);
+  // (the scale goes to dY before that is split, and the codes stay exact)
+  const bool as_codes = kn_takes_codes(ctx, false, tokens, n, m, L.planes, r > 0, ldq, 0);
   {
     ProfScope ps(ctx, s, PK_SMALL);
     float *sums = (float *)(ws + L.sums);
-    RSVD_TRY(grad_front_launch(ctx, s, type, tokens, m, r, dY, lddy, Ut, ldut, sums, single ? nullptr : scale, direct ? nullptr : a, L.width,
-                               m, n, codes, ldq, single ? scale : nullptr, nullptr, 0, as_codes ? nullptr : b, L.b_width),
+    RSVD_TRY(grad_front_launch(ctx, s, type, tokens, m, r, dY, lddy, Ut, ldut, sums, scale, a, L.width, m, n, codes, ldq, nullptr, 0,
+                               as_codes ? nullptr : b, L.b_width),
              "operands of the gradient");
     if (r > 0) RSVD_TRY(lowrank_join_launch(s, sums, L.splits, tokens, r, lowrank_parts(type), t), "low-rank term");
   }
   KnDesc d;
   d.M = tokens; d.N = n; d.K = m;
-  d.A = direct ? (const uint16_t *)dY : a; d.lda = (direct ? lddy : L.width) * 2; d.planes = L.planes; d.plane = tokens * L.width * 2;
+  d.A = a; d.lda = L.width * 2; d.planes = L.planes; d.plane = tokens * L.width * 2;
   d.B = b; d.ldb = L.b_width * 2;
   if (as_codes) d.codes = codes;
-  d.ldc = ldq; d.units.factor = single ? scale : nullptr;
+  d.ldc = ldq;
   d.out.t = t; d.out.parts = lowrank_parts(type); d.out.G = (const uint16_t *)V; d.out.ldg = ldv; d.out.r = (int)r;
   d.out.C = dX; d.out.ldc = lddx; d.out.type = type;
   d.partial = (float *)(ws + L.partial); d.partial_bytes = L.partial_bytes;
@@ -349,7 +349,7 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
   {
     ProfScope ps(ctx, s, PK_SMALL);
     RSVD_TRY(grad_front_launch(ctx, s, type, tokens, m, 0, dY, lddy, nullptr, 0, nullptr, nullptr, direct ? nullptr : a, L.width, tokens, n, codes,
-                               ldc, nullptr, powers, ldp, as_codes ? nullptr : b, L.b_width),
+                               ldc, powers, ldp, as_codes ? nullptr : b, L.b_width),
              "operands of the gradient");
   }
   KnDesc d;
@@ -358,7 +358,7 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
   d.A = direct ? (const uint16_t *)dY : a; d.lda = (direct ? lddy : L.width) * 2; d.planes = L.planes; d.plane = tokens * L.width * 2;
   d.B = b; d.ldb = L.b_width * 2;
   if (as_codes) d.codes = codes;
-  d.ldc = ldc; d.units.powers = powers; d.units.ldp = ldp;
+  d.ldc = ldc; d.powers = powers; d.ldp = ldp;
   d.sums = sums; d.sums_out = db;
   d.out.C = dW; d.out.ldc = lddw; d.out.type = RSVD_X_F32; d.out.accumulate = accumulate;
   d.partial = (float *)(ws + L.partial); d.partial_bytes = L.partial_bytes;

@@ -27,7 +27,7 @@ struct KnParams {
   int planes, ktiles;                      // k-tiles of a plane
   int64_t K;
   const char *B; int64_t ldb;              // bytes
-  CodeUnits units;                         // B holds codes
+  const uint8_t *powers; int64_t ldp;      // of codes in the place of B: their powers of two, or NULL
   float *sums; int sum_columns;            // A_KROWS: sums of A over k by ranges, [split][sum_columns][M], or NULL
   int sums_whole, sums_accumulate;         // they are one row, and what is wanted (added to it)
   TileParams T;
@@ -72,16 +72,16 @@ template <int NT, int X, bool KROWS, int DEPTH> struct Staged {
   }
 };
 
-// The same for codes: N pieces of sixteen codes of a row, as bf16 numbers in LDS.  POWERS: their units are powers of two, otherwise factors or ones.
+// The same for codes: N pieces of sixteen codes of a row, as bf16 numbers in LDS.  POWERS: multiplied by their powers of two.
 // (No branch between the loads: where it ends the compiler would wait for all of them.)
 template <int NT, int X, bool POWERS, int DEPTH> struct StagedCodes {
   static constexpr int ROW = X * 2, PER = X / 16, STEP = NT / PER, N = X * kKnK / 16 / NT;
   static_assert(X * kKnK % (16 * NT) == 0 && STEP % 16 == 0, "whole rounds; a thread's rows have their pieces exchanged alike");
   u32x4 reg[DEPTH][N];
-  unsigned unit[DEPTH][N];
-  uint32_t off[N], unit_off[N];
+  unsigned unit[DEPTH][POWERS ? N : 1];
+  uint32_t off[N], unit_off[POWERS ? N : 1];
   int place, half;
-  __device__ __forceinline__ void init(int64_t ld, int64_t left, int tid, const CodeUnits &units) {
+  __device__ __forceinline__ void init(int64_t ld, int64_t left, int tid, int64_t ldp) {
     const int row = tid / PER, pos = tid % PER, col = 16 * pos < left ? 16 * pos : 0;
     half = (pos & 1) << 4;                               // (neighbours start with different halves of their pieces: other banks)
     place = row * ROW + (krow_piece<X>(pos, row) << 5);
@@ -89,21 +89,25 @@ template <int NT, int X, bool POWERS, int DEPTH> struct StagedCodes {
     for (int i = 0; i < N; ++i) {
       const uint32_t r = row + STEP * i;
       off[i] = r * (uint32_t)ld + (uint32_t)col;
-      unit_off[i] = POWERS ? r * (uint32_t)units.ldp + (uint32_t)(col >> 5) : 4 * r;
-      asm volatile("" : "+v"(off[i]), "+v"(unit_off[i]));
+      asm volatile("" : "+v"(off[i]));
+      if constexpr (POWERS) {
+        unit_off[i] = r * (uint32_t)ldp + (uint32_t)(col >> 5);
+        asm volatile("" : "+v"(unit_off[i]));
+      }
     }
   }
-  // k: the first of the tile; base: its codes; what is behind the last row is read as zeros, codes and units
-  __device__ __forceinline__ void load(int set, int i, const char *base, int64_t ld, int k_left, const CodeUnits &units, int64_t k, int64_t n0) {
+  // base, powers: of the tile's first k and column; what is behind the last row is read as zeros, codes and units
+  __device__ __forceinline__ void load(int set, int i, const char *base, int64_t ld, int k_left, const uint8_t *powers, int64_t ldp) {
     const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)(k_left * (uint32_t)ld), 0x00027000);
     reg[set][i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(all, off[i], 0, 0));
-    const char *first = POWERS ? (const char *)(units.powers + k * units.ldp + n0 / 32) : (const char *)(units.factor + (units.factor != nullptr ? k : 0));
-    const int bytes = POWERS ? (int)(k_left * (uint32_t)units.ldp) : units.factor != nullptr ? 4 * k_left : 0;      // (none: nothing is read)
-    const __amdgpu_buffer_rsrc_t u = __builtin_amdgcn_make_buffer_rsrc((void *)first, 0, bytes, 0x00027000);
-    unit[set][i] = POWERS ? __builtin_amdgcn_raw_buffer_load_b8(u, unit_off[i], 0, 0) : __builtin_amdgcn_raw_buffer_load_b32(u, unit_off[i], 0, 0);
+    if constexpr (POWERS) {
+      const __amdgpu_buffer_rsrc_t u = __builtin_amdgcn_make_buffer_rsrc((void *)powers, 0, (int)(k_left * (uint32_t)ldp), 0x00027000);
+      unit[set][i] = __builtin_amdgcn_raw_buffer_load_b8(u, unit_off[i], 0, 0);
+    }
   }
-  __device__ __forceinline__ void write(int set, int i, char *lds, const CodeUnits &units) const {
-    const float by = POWERS ? kept_unit(unit[set][i]) : units.factor != nullptr ? __uint_as_float(unit[set][i]) : 1.f;
+  __device__ __forceinline__ void write(int set, int i, char *lds) const {
+    float by = 1.f;
+    if constexpr (POWERS) by = kept_unit(unit[set][i]);
     u32x4 p[2];
     widen16(reg[set][i], by, p);
     char *at = lds + place + i * STEP * ROW;
@@ -149,19 +153,18 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void kn_kernel(const KnParams P)
   Staged<NT, BM, A_KROWS, DEPTH * PL> sa;
   std::conditional_t<CODES, StagedCodes<NT, BN, A_KROWS, DEPTH>, Staged<NT, BN, true, DEPTH>> sb;
   sa.init(P.lda, P.T.M - m0, tid);
-  if constexpr (CODES) sb.init(P.ldb, P.T.N - n0, tid, P.units);
+  if constexpr (CODES) sb.init(P.ldb, P.T.N - n0, tid, P.ldp);
   else sb.init(P.ldb, P.T.N - n0, tid);
   constexpr int NA = decltype(sa)::N, PIECES = PL * NA + decltype(sb)::N;
   auto load = [&](int set, int p) RSVD_INLINE {
     if (p < PL * NA) {
       const int plane = PL > 1 ? p / NA : P.planes - 1 - next_plane;
       sa.load(PL * set + p / NA, p % NA, a_first + plane * P.plane + (A_KROWS ? next_k * P.lda : next_k * 2), P.lda, next_left);
-    } else if constexpr (CODES) sb.load(set, p - PL * NA, b_first + next_k * P.ldb, P.ldb, next_left, P.units, next_k, n0);
+    } else if constexpr (CODES) sb.load(set, p - PL * NA, b_first + next_k * P.ldb, P.ldb, next_left, P.powers + next_k * P.ldp + n0 / 32, P.ldp);
     else sb.load(set, p - PL * NA, b_first + next_k * P.ldb, P.ldb, next_left);
   };
   auto write = [&](int set, int p, int buf) RSVD_INLINE {
     if (p < PL * NA) sa.write(PL * set + p / NA, p % NA, kn_lds + buf * STAGE + p / NA * A_BYTES);
-    else if constexpr (CODES) sb.write(set, p - PL * NA, kn_lds + buf * STAGE + B_LDS, P.units);
     else sb.write(set, p - PL * NA, kn_lds + buf * STAGE + B_LDS);
   };
   auto advance = [&]() RSVD_INLINE {                    // (behind the last tile of this workgroup's range: loads stay inside the operands)
@@ -380,7 +383,8 @@ template <bool A_KROWS, bool CODES, int PL, int BM, int BN, int WGM, int WGN> st
 
 template <bool A_KROWS, bool CODES> static hipError_t kn_run_small(hipStream_t s, const KnParams &P, int bm) {
   if (bm == 128) return kn_run<A_KROWS, CODES, 1, 128, 128, 2, 2>(s, P);
-  if (P.planes == 1) return kn_run<A_KROWS, CODES, 1, 64, 64, 2, 2>(s, P);
+  if constexpr (A_KROWS)                                  // (the other's are two or three)
+    if (P.planes == 1) return kn_run<A_KROWS, CODES, 1, 64, 64, 2, 2>(s, P);
   return P.planes == 2 ? kn_run<A_KROWS, CODES, 2, 64, 64, 2, 2>(s, P) : kn_run<A_KROWS, CODES, 3, 64, 64, 2, 2>(s, P);
 }
 template <bool A_KROWS> static hipError_t kn_run_tile(hipStream_t s, const KnParams &P, int bm, bool codes) {
@@ -419,10 +423,10 @@ hipError_t kn_launch(rsvd_ctx *ctx, hipStream_t s, const KnDesc &d) {
   P.B = (const char *)d.B; P.ldb = d.ldb;
   const bool codes = d.codes != nullptr;
   if (codes) {
-    if (!kn_takes_codes(ctx, d.a_krows, d.M, d.N, d.K, d.planes, d.out.r > 0, d.ldc, d.units.ldp)) return hipErrorInvalidValue;
+    if (!kn_takes_codes(ctx, d.a_krows, d.M, d.N, d.K, d.planes, d.out.r > 0, d.ldc, d.ldp)) return hipErrorInvalidValue;
     P.B = (const char *)d.codes; P.ldb = d.ldc;
   }
-  P.units = d.units;
+  P.powers = d.powers; P.ldp = d.ldp;
   P.sums = d.a_krows ? d.sums : nullptr;
   P.sum_columns = (int)kn_sum_columns(c, d.N);
   P.sums_whole = c.splits * P.sum_columns == 1;

@@ -155,7 +155,9 @@ template <int XT, int RB> __global__ __launch_bounds__(256, 2) void grad_front_k
     widen_group(P.W, group);
     return;
   }
-  split_rows_group<XT>(P.S, group - P.W.groups);
+  group -= P.W.groups;
+  if (P.S.factor != nullptr) split_rows_group<XT, true>(P.S, group);
+  else split_rows_group<XT, false>(P.S, group);
 }
 
 // ---------------------------------------------------------------- a few tokens
@@ -271,14 +273,14 @@ template <int XT> static void grad_front_typed(hipStream_t s, const GradFrontPar
 
 hipError_t grad_front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int64_t tokens, int64_t m, int64_t r, const void *dY, int64_t lddy,
                              const void *F, int64_t ldf, float *sums, const float *dy_factor, uint16_t *planes, int64_t planes_width,
-                             int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const float *factor, const uint8_t *powers, int64_t ldp,
-                             uint16_t *plane, int64_t width) {
+                             int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp, uint16_t *plane,
+                             int64_t width) {
   GradFrontParams P;
   P.L = lowrank_params(ctx, tokens, m, r < 1 ? 1 : r, dY, lddy, F, ldf, sums);
   P.lowrank_groups = r > 0 ? lowrank_groups(P.L, 1) : 0;
   P.S = SplitParams{(const char *)dY, lddy, tokens, m, dy_factor, planes, planes_width, 0};
   if (planes != nullptr) P.S.groups = ceil_div(tokens * (planes_width / 8), 256);
-  P.W = WidenParams{codes, ldc, factor, powers, ldp, rows, n, plane, width, plane != nullptr ? ceil_div(rows * ceil_div(n, 16), 256) : 0};
+  P.W = WidenParams{codes, ldc, powers, ldp, rows, n, plane, width, plane != nullptr ? ceil_div(rows * ceil_div(n, 16), 256) : 0};
   if (P.lowrank_groups + P.S.groups + P.W.groups == 0) return hipSuccess;
   if (type == RSVD_X_BF16) grad_front_typed<RSVD_X_BF16>(s, P);
   else if (type == RSVD_X_F16) grad_front_typed<RSVD_X_F16>(s, P);

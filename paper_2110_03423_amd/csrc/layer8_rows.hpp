@@ -120,15 +120,15 @@ __device__ __forceinline__ void piece_of(int64_t group, int per_row, int64_t &ro
   place = (int)(at - more * (unsigned)per_row);
 }
 
-// planes[q][row][0 .. width): the bf16 parts of X_rj factor_j (factor NULL: of X_rj), zeros from n on; width: a multiple of 8.
+// planes[q][row][0 .. width): the bf16 parts of X_rj, or with SCALED of X_rj factor_j, zeros from n on; width: a multiple of 8.
 struct SplitParams {
   const char *X; int64_t ldx, rows, n;
   const float *factor;
   uint16_t *planes; int64_t width;
   int64_t groups;                  // workgroups: 256 pieces of eight each
 };
-template <int XT> __device__ __forceinline__ void split_rows_group(const SplitParams &P, int64_t group) {
-  constexpr int PARTS = XTraits<XT>::PARTS;
+template <int XT, bool SCALED> __device__ __forceinline__ void split_rows_group(const SplitParams &P, int64_t group) {
+  constexpr int PARTS = SCALED && XT == RSVD_X_BF16 ? 2 : XTraits<XT>::PARTS;
   int64_t row;
   int place;
   piece_of(group, (int)(P.width / 8), row, place);
@@ -137,7 +137,7 @@ template <int XT> __device__ __forceinline__ void split_rows_group(const SplitPa
   const int64_t left = P.n - j;
   const char *x = P.X + (row * P.ldx + j) * XTraits<XT>::SIZE;
   u32x4 out[PARTS];
-  if (P.factor != nullptr) {
+  if constexpr (SCALED) {
     float v[8];
     x_load8<XT>(x, left, v);
 #pragma unroll
@@ -169,11 +169,10 @@ __device__ __forceinline__ void widen16(const u32x4 &w, float unit, u32x4 (&p)[2
     }
 }
 
-// plane[row][0 .. width): the codes of a row as bf16 numbers, multiplied by factor_row (NULL: as they are), or by the powers of two of kept
-// activations (powers != NULL); width: n up to a multiple of 8.
+// plane[row][0 .. width): the codes of a row as bf16 numbers, multiplied by the powers of two of kept activations (NULL: as they are); width: n up to
+// a multiple of 8.
 struct WidenParams {
   const int8_t *codes; int64_t ldc;
-  const float *factor;
   const uint8_t *powers; int64_t ldp;
   int64_t rows, n;
   uint16_t *plane; int64_t width;
@@ -186,7 +185,7 @@ __device__ __forceinline__ void widen_group(const WidenParams &P, int64_t group)
   const int64_t j = 16 * (int64_t)place;
   if (row >= P.rows) return;
   const u32x4 w = *reinterpret_cast<const u32x4 *>(P.codes + row * P.ldc + j);
-  const float unit = P.powers != nullptr ? kept_unit(P.powers[row * P.ldp + (j >> 5)]) : P.factor != nullptr ? P.factor[row] : 1.f;
+  const float unit = P.powers != nullptr ? kept_unit(P.powers[row * P.ldp + (j >> 5)]) : 1.f;
   u32x4 p[2];
   widen16(w, unit, p);
 #pragma unroll

@@ -150,8 +150,11 @@ def _ld(t):
 
 class Weight8:
     """A linear layer's weight (m x n) as rsvd_q8_product takes it: 8-bit codes with a scale for each row, and beside them
-    bf16 factors U (m x r), Vt (r x n) or None; bias: m values or None.  The codes are laid out, and the factors
-    transposed for the backward pass, once, here."""
+    bf16 factors U (m x r), Vt (r x n) or None; bias: m values or None.
+
+    The layer's tensors are `codes`, `scale`, `U`, `Vt` and `bias`: those that were given where they lie as the kernels want
+    them (contiguous; codes in rows of a multiple of 128 bytes; an fp32 bias), copies where they do not.  Their values may change in
+    place, and every call takes what they hold then."""
 
     def __init__(self, codes, scale, U=None, Vt=None, bias=None):
         import torch
@@ -164,7 +167,7 @@ class Weight8:
             raise ValueError("U and Vt come together")
         self.codes, self.scale = _laid_out(codes), scale.contiguous()
         self.m, self.n, self.r = m, n, 0
-        self.U = self.Vt = self.Ut = self.V = None
+        self.U = self.Vt = None
         if U is not None and U.shape[1] > 0:
             if U.dtype != torch.bfloat16 or Vt.dtype != torch.bfloat16:
                 raise TypeError("U, Vt: bf16 factors")
@@ -172,11 +175,20 @@ class Weight8:
                 raise ValueError("U, Vt: m x r and r x n")
             self.r = U.shape[1]
             self.U, self.Vt = U.contiguous(), Vt.contiguous()
-            self.Ut, self.V = U.t().contiguous(), Vt.t().contiguous()
         if bias is not None and bias.shape != (m,):
             raise ValueError("bias: m values")
         self.bias = None if bias is None else bias.float().contiguous()
         self._sizes = (n, m, self.r)
+
+    # The factors by rows of the other index, for the backward pass.  Made anew each time: nothing tells reliably whether U and Vt
+    # have changed since (an optimizer that writes through `.data` leaves no trace), or on which stream.
+    @property
+    def Ut(self):
+        return None if self.U is None else self.U.t().contiguous()
+
+    @property
+    def V(self):
+        return None if self.Vt is None else self.Vt.t().contiguous()
 
     def __setattr__(self, name, value):
         if "_sizes" in self.__dict__:
@@ -510,12 +522,13 @@ class Rsvd:
         tokens, xt = _rows(dY, m, "dY"), _xtype_code(dY.dtype)
         stream = self._raw_stream()
         ws = _given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_q8_product_grad_bytes", (xt, tokens, *sizes))
+        Ut, V = w.Ut, w.V
         dX = dY.new_empty((tokens, n)) if out is None else out
         if out is not None:
             _rows(out, n, "out", tokens, dY.dtype)
         self._check(self.lib.rsvd_q8_product_grad(self.h, stream, xt, tokens, n, m, r, dY.data_ptr(), _ld(dY),
                                                   w.codes.data_ptr(), _ld(w.codes), w.scale.data_ptr(),
-                                                  _at(w.Ut), m, _at(w.V), r, dX.data_ptr(), _ld(dX), ws[0], ws[1]))
+                                                  _at(Ut), m, _at(V), r, dX.data_ptr(), _ld(dX), ws[0], ws[1]))
         return dX
 
     def rsvd_keep8_save(self, X):

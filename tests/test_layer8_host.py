@@ -147,3 +147,14 @@ def test_binding_refuses_what_does_not_fit_together():
                 (codes, powers, torch.float64)):
         with pytest.raises((TypeError, ValueError)):
             binding.Kept8(*bad)
+
+
+def test_transposed_factors_follow_the_factors():
+    torch = pytest.importorskip("torch")
+    for U, Vt in ((torch.zeros(6, 2, dtype=torch.bfloat16), torch.zeros(2, 5, dtype=torch.bfloat16)),
+                  (torch.zeros(2, 6, dtype=torch.bfloat16).t(), torch.zeros(5, 2, dtype=torch.bfloat16).t())):
+        w = binding.Weight8(torch.zeros(6, 5, dtype=torch.int8), torch.zeros(6), U, Vt)
+        for value in (1.0, 2.0):
+            w.U.data.fill_(value)
+            w.Vt[1] = value
+            assert torch.equal(w.Ut, w.U.t()) and torch.equal(w.V, w.Vt.t()) and w.Ut.is_contiguous() and w.V.is_contiguous()

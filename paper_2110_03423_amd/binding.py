@@ -483,7 +483,8 @@ class Rsvd:
         return codes, scale
 
     def _layer_ws(self, stream, name, sizes):
-        """Address and bytes of the workspace that is kept for calls on `stream`; what a call of these sizes needs is asked for once."""
+        """Address and bytes of the workspace that is kept for calls on `stream`; what a call of these sizes needs is asked for once.
+        A call that is captured has a workspace of its graph's own: the kept one may be replaced, and used, while the graph lives."""
         need = self._needs.get((name, sizes))
         if need is None:
             out = C.c_size_t()
@@ -491,14 +492,17 @@ class Rsvd:
             if len(self._needs) >= 1024:
                 self._needs.clear()
             need = self._needs[(name, sizes)] = out.value
+        if self.torch.cuda.is_current_stream_capturing():
+            return self._room(need)
         kept = self._layer.get(stream)
         if kept is None or kept[1] < need:
             self._layer.pop(stream, None)
-            ws = self.torch.empty(need, dtype=self.torch.uint8, device=self.device)
-            kept = (ws.data_ptr(), need, ws)
-            if not self.torch.cuda.is_current_stream_capturing():      # (what is allocated for a graph belongs to that graph)
-                self._layer[stream] = kept
+            kept = self._layer[stream] = self._room(need)
         return kept
+
+    def _room(self, need):
+        ws = self.torch.empty(need, dtype=self.torch.uint8, device=self.device)
+        return ws.data_ptr(), need, ws
 
     def rsvd_q8_product(self, X, weight, workspace=None, out=None):
         """X (tokens x n) through the layer `weight` (Weight8): tokens x m, in the type of X."""

@@ -3,7 +3,7 @@ import pytest
 import torch
 
 from gpu_util import ctx
-from test_gpu_layer8 import BF16, TYPES, activations, check, gen, grad_reference, product_reference, weight
+from test_gpu_layer8 import BF16, F32, TYPES, activations, check, gen, grad_reference, product_reference, weight
 
 pytestmark = pytest.mark.gpu
 
@@ -45,3 +45,48 @@ def test_a_captured_gradient_takes_the_factors_of_the_replay():
         torch.cuda.synchronize()
         assert torch.equal(dx, ctx().rsvd_q8_product_grad(dy, w))
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("tokens", [1, 200])
+def test_a_graph_captured_on_the_stream_of_ordinary_calls_keeps_its_workspace(tokens):
+    """Ordinary calls, the capture and a larger call on one stream, and the memory that the larger call gave up filled by others."""
+    from paper_2110_03423_amd import Rsvd
+    g = gen(4)
+    c, stream = Rsvd(0), torch.cuda.Stream()
+    w, large = weight(g, 260, 2100, 40), weight(g, 1000, 2100, 64)
+    x, dy = activations(g, tokens, 2100, BF16), activations(g, tokens, 260, BF16)
+    more, dmore = activations(g, 3000, 2100, F32), activations(g, 3000, 1000, F32)
+
+    def step(c, x, dy, w):
+        return [c.rsvd_q8_product(x, w), c.rsvd_q8_product_grad(dy, w), *c.rsvd_keep8_grad(dy, c.rsvd_keep8_save(x))]
+
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        step(c, x, dy, w)
+        stream.synchronize()
+        before = dict(c._layer)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            out = step(c, x, dy, w)
+        assert dict(c._layer) == before
+        stream.synchronize()
+        kept = c._layer[stream.cuda_stream][0]
+        step(c, more, dmore, large)
+        assert c._layer[stream.cuda_stream][0] != kept
+        filled = [torch.full((1 << 20,), 7, dtype=torch.uint8, device="cuda") for _ in range(64)]
+    torch.cuda.synchronize()
+    for trial in range(4):
+        x.copy_(activations(g, tokens, 2100, BF16))
+        dy.copy_(activations(g, tokens, 260, BF16))
+        torch.cuda.synchronize()
+        graph.replay()
+        # ordinary calls of the same context on the stream of the capture, while the graph runs on this one
+        with torch.cuda.stream(stream):
+            beside = step(c, more, dmore, large)
+        torch.cuda.synchronize()
+        got = [t.clone() for t in out]
+        for a, b in zip(got, step(Rsvd(0), x, dy, w)):
+            assert torch.equal(a, b)
+        for a, b in zip(beside, step(Rsvd(0), more, dmore, large)):
+            assert torch.equal(a, b)
+        assert all(bool((t == 7).all()) for t in filled)

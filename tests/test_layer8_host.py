@@ -158,3 +158,24 @@ def test_transposed_factors_follow_the_factors():
             w.U.data.fill_(value)
             w.Vt[1] = value
             assert torch.equal(w.Ut, w.U.t()) and torch.equal(w.V, w.Vt.t()) and w.Ut.is_contiguous() and w.V.is_contiguous()
+
+
+def test_a_captured_call_leaves_the_kept_workspace_alone(plan):
+    """A graph outlives the call that recorded it: a kept workspace is neither recorded nor exchanged while a stream is captured.  (The context has the
+    parts of torch that it asks for from the CPU.)"""
+    torch = pytest.importorskip("torch")
+    from types import SimpleNamespace
+    capturing = [False]
+    ctx = binding.Rsvd(device=None)
+    ctx.device = torch.device("cpu")
+    ctx.torch = SimpleNamespace(empty=torch.empty, uint8=torch.uint8, cuda=SimpleNamespace(is_current_stream_capturing=lambda: capturing[0]))
+    room = lambda tokens: ctx._layer_ws(7, "rsvd_keep8_grad_bytes", (X_BF16, tokens, 512, 384))
+    small = room(100)
+    assert room(100) is small and room(50) is small
+    capturing[0] = True
+    recorded, larger = room(100), room(1000)
+    assert recorded[0] != small[0] and larger[0] != small[0] and larger[1] > small[1]
+    capturing[0] = False
+    assert room(100) is small
+    grown = room(1000)
+    assert grown[0] not in (recorded[0], larger[0]) and room(100) is grown

@@ -308,8 +308,9 @@ int rsvd_stage_lift(rsvd_ctx *ctx, void *stream, rsvd_dtype dtype,
  *   - X, Y, dX, dY, the factors and the bias may have any leading dimension and
  *     the alignment of their elements; 16-byte aligned rows are faster.
  *   - 8-bit codes have rows of ldq bytes, ldq a multiple of 16 and at least n,
- *     from a 16-byte aligned address; every row has all of its ldq bytes (those
- *     beyond n may be read, what they hold does not matter).
+ *     from a 16-byte aligned address.  Of a row, the bytes from n to the next
+ *     multiple of 16 may be read, too (what they hold does not matter); nothing
+ *     behind those is.
  *   - Infinities and NaN: a row (of X, or of a weight) that holds one has
  *     the scale NaN and codes 0, and makes its row (column) of Y NaN.  No
  *     other row is touched.

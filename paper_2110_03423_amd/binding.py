@@ -129,7 +129,10 @@ def _empty_codes(rows, n, device):
 def _laid_out(codes):
     """The codes in rows as the C entry points want them (a copy unless they are already)."""
     if codes.dim() == 2 and codes.stride(1) == 1 and codes.stride(0) % 128 == 0 and codes.data_ptr() % 16 == 0:
-        return codes
+        # (rows are read in 16-byte pieces; the last one's may reach behind what the tensor was cut out of)
+        end = codes.storage_offset() + (codes.shape[0] - 1) * codes.stride(0) + -(-codes.shape[1] // 16) * 16
+        if end <= codes.untyped_storage().nbytes():
+            return codes
     out = _empty_codes(codes.shape[0], codes.shape[1], codes.device)
     out.copy_(codes)
     return out

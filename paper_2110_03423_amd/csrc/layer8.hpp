@@ -246,6 +246,7 @@ struct FewDesc {
   int64_t M = 0, N = 0, k = 0;           // k: a multiple of 64, zeros in A behind the last
   const int8_t *A = nullptr; int64_t lda = 0;
   const int8_t *B = nullptr; int64_t ldb = 0;
+  int64_t b_bytes = 0;                   // bytes of a row of B that may be read (a multiple of 16)
   const float *sums = nullptr; int splits = 0;      // the low-rank sums as they are, in the place of out.t (NULL: out.t)
   Layer8Out out;
 };

@@ -208,7 +208,7 @@ int rsvd_q8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
     FewDesc d;
     d.sums = unjoined ? sums : nullptr; d.splits = L.splits;
     d.M = tokens; d.N = m; d.k = L.width;
-    d.A = q; d.lda = L.width; d.B = codes; d.ldb = ldq;
+    d.A = q; d.lda = L.width; d.B = codes; d.ldb = ldq; d.b_bytes = (int64_t)align_up((size_t)n, 16);
     d.out = o;
     RSVD_TRY(few_launch(ctx, s, d), "product of a few tokens");
     return RSVD_OK;

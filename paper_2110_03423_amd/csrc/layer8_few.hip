@@ -10,6 +10,7 @@ struct FewParams {
   const char *A, *B;
   int64_t lda, ldb, M, N;
   int steps;                       // of 64 k
+  int b_pieces;                    // 16-byte pieces of a row of B that may be read
   const float *sums; int splits;             // the low-rank sums over ranges of k, or NULL: E.t
   Layer8Epilogue E;
 };
@@ -28,8 +29,6 @@ template <int TB, int WAVES> __global__ __launch_bounds__(64 * WAVES) void few_k
     const int64_t m = 16 * i + r16;
     a[i] = P.A + (m < P.M ? m : P.M - 1) * P.lda + 16 * kq;
   }
-  // (pieces behind the row of codes: the first of the row, where the tokens' codes are zero)
-  const int pieces = (int)(P.ldb / 16);
   i32x4 acc[TB];
   f32x4 low[TB];
 #pragma unroll
@@ -79,7 +78,7 @@ template <int TB, int WAVES> __global__ __launch_bounds__(64 * WAVES) void few_k
     for (int u = 0; u < U; ++u) {
       const int s = s0 + WAVES * u;
       if (s < P.steps) {
-        x[u] = *reinterpret_cast<const u32x4 *>(b + (4 * s + kq < pieces ? 64 * s + 16 * kq : 0));
+        x[u] = *reinterpret_cast<const u32x4 *>(b + (4 * s + kq < P.b_pieces ? 64 * s + 16 * kq : 0));      // (behind those: the first, the tokens' codes are zero)
 #pragma unroll
         for (int i = 0; i < TB; ++i) y[u][i] = *reinterpret_cast<const u32x4 *>(a[i] + 64 * s);
       } else {
@@ -143,6 +142,7 @@ hipError_t few_launch(rsvd_ctx *, hipStream_t s, const FewDesc &d) {
   P.A = (const char *)d.A; P.B = (const char *)d.B;
   P.lda = d.lda; P.ldb = d.ldb; P.M = d.M; P.N = d.N;
   P.steps = (int)(d.k / 64);
+  P.b_pieces = (int)(d.b_bytes / 16);
   P.E = layer8_epilogue(d.out);
   P.sums = d.sums; P.splits = d.splits;
   const dim3 grid((unsigned)ceil_div(d.N, 16));

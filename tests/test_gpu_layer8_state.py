@@ -90,3 +90,18 @@ def test_a_graph_captured_on_the_stream_of_ordinary_calls_keeps_its_workspace(to
         for a, b in zip(beside, step(Rsvd(0), more, dmore, large)):
             assert torch.equal(a, b)
         assert all(bool((t == 7).all()) for t in filled)
+
+
+@pytest.mark.parametrize("tokens", [1, 7, 20, 40, 100])
+@pytest.mark.parametrize("rows,n,first,last", [(4, 11008, 8256, 11008), (33, 640, 16, 640), (20, 256, 16, 250)])
+def test_the_last_shard_of_a_layer(tokens, rows, n, first, last):
+    """Columns at the end of a larger tensor, taken as they are: nothing behind its last byte belongs to them."""
+    from paper_2110_03423_amd import Weight8
+    g = gen(tokens + rows)
+    whole = torch.randint(-127, 128, (rows, n), device="cuda", generator=g, dtype=torch.int32).to(torch.int8)
+    scale, x = torch.rand(rows, device="cuda", generator=g), activations(g, tokens, last - first, F32)
+    shard = Weight8(whole[:, first:last], scale)
+    assert shard.codes.data_ptr() == whole.data_ptr() + first
+    y = ctx().rsvd_q8_product(x, shard)
+    assert torch.equal(y, ctx().rsvd_q8_product(x, Weight8(whole[:, first:last].clone(), scale)))
+    check(y, *product_reference(x, shard), "shard")

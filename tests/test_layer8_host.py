@@ -179,3 +179,19 @@ def test_a_captured_call_leaves_the_kept_workspace_alone(plan):
     assert room(100) is small
     grown = room(1000)
     assert grown[0] not in (recorded[0], larger[0]) and room(100) is grown
+
+
+def test_rows_of_codes_that_end_with_their_storage():
+    """Of a row, whole 16-byte pieces are read: a tensor whose last row ends in the middle of one is copied, one whose rows hold them is not."""
+    torch = pytest.importorskip("torch")
+
+    def read_inside(t):
+        return (t.storage_offset() + (t.shape[0] - 1) * t.stride(0) + (t.shape[1] + 15) // 16 * 16) <= t.untyped_storage().nbytes()
+
+    short = torch.as_strided(torch.arange(3 * 128 + 100, dtype=torch.int32).to(torch.int8), (4, 100), (128, 1))
+    shard = torch.zeros(4, 11008, dtype=torch.int8)[:, 8256:]
+    for codes, same in ((short, False), (shard, True)):
+        w = binding.Weight8(codes, torch.zeros(4))
+        kept = binding.Kept8(codes, torch.zeros(4, (codes.shape[1] + 31) // 32, dtype=torch.uint8), torch.bfloat16)
+        for t in (w.codes, kept.codes):
+            assert torch.equal(t, codes) and read_inside(t) and (t.data_ptr() == codes.data_ptr()) == same

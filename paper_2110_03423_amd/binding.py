@@ -138,13 +138,12 @@ def _laid_out(codes):
     return out
 
 
-def _rows(t, cols, what, rows=None, dtype=None):
-    """A matrix with `cols` columns (and `rows` rows of `dtype`) whose rows are contiguous, on the GPU."""
-    if not t.is_cuda or t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1) or t.stride(0) < 0:
-        raise ValueError(f"{what}: a row-major GPU matrix with {cols} columns is needed")
-    if (rows is not None and t.shape[0] != rows) or (dtype is not None and t.dtype != dtype):
-        raise ValueError(f"{what}: {rows} rows of {dtype} are needed")
-    return t.shape[0]
+def _together(first, **others):
+    """The device that all of a layer's (or a kept activation's) tensors are on."""
+    for name, t in others.items():
+        if t is not None and t.device != first.device:
+            raise ValueError(f"{name}: on {t.device}, the codes on {first.device}")
+    return first.device
 
 
 def _ld(t):
@@ -168,6 +167,7 @@ class Weight8:
             raise ValueError("scale: one fp32 value for each row of codes")
         if (U is None) != (Vt is None):
             raise ValueError("U and Vt come together")
+        self.device = _together(codes, scale=scale, U=U, Vt=Vt, bias=bias)
         self.codes, self.scale = _laid_out(codes), scale.contiguous()
         self.m, self.n, self.r = m, n, 0
         self.U = self.Vt = None
@@ -181,6 +181,7 @@ class Weight8:
         if bias is not None and bias.shape != (m,):
             raise ValueError("bias: m values")
         self.bias = None if bias is None else bias.float().contiguous()
+        self._index = self.codes.get_device()      # (-1: not on a GPU)
         self._sizes = (n, m, self.r)
 
     # The factors by rows of the other index, for the backward pass.  Made anew each time: nothing tells reliably whether U and Vt
@@ -210,20 +211,18 @@ class Kept8:
         if powers.shape != (codes.shape[0], -(-codes.shape[1] // 32)):
             raise ValueError("powers: one byte for each 32 columns of codes")
         _xtype_code(dtype)
+        _together(codes, powers=powers)
         self._set(_laid_out(codes), powers if powers.stride(1) == 1 or powers.shape[1] == 1 else powers.contiguous(), dtype)
 
     def _set(self, codes, powers, dtype):
         self.codes, self.powers, self.dtype = codes, powers, dtype
         self.tokens, self.n = codes.shape
+        self.device, self._index = codes.device, codes.get_device()
         return self
 
 
 def _at(t):
     return t.data_ptr() if t is not None else None
-
-
-def _given(workspace):
-    return workspace.data_ptr(), workspace.numel()
 
 
 def _ptr(t):
@@ -243,12 +242,12 @@ class Rsvd:
         h = C.c_void_p()
         if device is None:
             self.torch = None
-            self.device = None
+            self.device = self._index = None
             rc = self.lib.rsvd_create(C.byref(h), DEVICE_NONE)
         else:
             import torch
             self.torch = torch
-            self.device = torch.device("cuda", device)
+            self.device, self._index = torch.device("cuda", device), device
             rc = self.lib.rsvd_create(C.byref(h), device)
         if rc != 0:
             raise RsvdError(rc, "rsvd_create failed (no such device?)")
@@ -475,9 +474,29 @@ class Rsvd:
         return U
 
     # ---- a linear layer held in 8 bits
+    def _rows(self, t, cols, what, rows=None, dtype=None):
+        """A matrix with `cols` columns (and `rows` rows of `dtype`) whose rows are contiguous, on the context's GPU."""
+        if t.get_device() != self._index:
+            self._elsewhere(t, what)
+        if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1) or t.stride(0) < 0:
+            raise ValueError(f"{what}: a row-major GPU matrix with {cols} columns is needed")
+        if (rows is not None and t.shape[0] != rows) or (dtype is not None and t.dtype != dtype):
+            raise ValueError(f"{what}: {rows} rows of {dtype} are needed")
+        return t.shape[0]
+
+    def _elsewhere(self, t, what):
+        raise ValueError(f"{what}: on {t.device}, not on the context's device ({self.device or 'none: it is for planning'})")
+
+    def _given(self, workspace):
+        if workspace.get_device() != self._index:
+            self._elsewhere(workspace, "workspace")
+        if not workspace.is_contiguous():
+            raise ValueError("workspace: a contiguous tensor is needed")
+        return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
     def rsvd_q8_rows(self, X):
         """Rows of X (bf16, fp16, fp32) to 8 bits.  Returns (codes int8, scale fp32), the codes laid out for Weight8."""
-        _rows(X, X.shape[1], "X")
+        self._rows(X, X.shape[1], "X")
         rows, n = X.shape
         codes = _empty_codes(rows, n, X.device)
         scale = self.torch.empty(rows, dtype=self.torch.float32, device=X.device)
@@ -511,12 +530,14 @@ class Rsvd:
         """X (tokens x n) through the layer `weight` (Weight8): tokens x m, in the type of X."""
         w = weight
         n, m, r = sizes = w._sizes
-        tokens, xt = _rows(X, n, "X"), _xtype_code(X.dtype)
+        tokens, xt = self._rows(X, n, "X"), _xtype_code(X.dtype)
+        if w._index != self._index:
+            self._elsewhere(w, "weight")
         stream = self._raw_stream()
-        ws = _given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_q8_product_bytes", (xt, tokens, *sizes))
+        ws = self._given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_q8_product_bytes", (xt, tokens, *sizes))
         Y = X.new_empty((tokens, m)) if out is None else out
         if out is not None:
-            _rows(out, m, "out", tokens, X.dtype)
+            self._rows(out, m, "out", tokens, X.dtype)
         self._check(self.lib.rsvd_q8_product(self.h, stream, xt, tokens, n, m, r, X.data_ptr(), _ld(X),
                                              w.codes.data_ptr(), _ld(w.codes), w.scale.data_ptr(),
                                              _at(w.U), r, _at(w.Vt), n, _at(w.bias), Y.data_ptr(), _ld(Y), ws[0], ws[1]))
@@ -526,13 +547,15 @@ class Rsvd:
         """Gradient of rsvd_q8_product with respect to X: dY (tokens x m) to tokens x n, in the type of dY."""
         w = weight
         n, m, r = sizes = w._sizes
-        tokens, xt = _rows(dY, m, "dY"), _xtype_code(dY.dtype)
+        tokens, xt = self._rows(dY, m, "dY"), _xtype_code(dY.dtype)
+        if w._index != self._index:
+            self._elsewhere(w, "weight")
         stream = self._raw_stream()
-        ws = _given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_q8_product_grad_bytes", (xt, tokens, *sizes))
+        ws = self._given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_q8_product_grad_bytes", (xt, tokens, *sizes))
         Ut, V = w.Ut, w.V
         dX = dY.new_empty((tokens, n)) if out is None else out
         if out is not None:
-            _rows(out, n, "out", tokens, dY.dtype)
+            self._rows(out, n, "out", tokens, dY.dtype)
         self._check(self.lib.rsvd_q8_product_grad(self.h, stream, xt, tokens, n, m, r, dY.data_ptr(), _ld(dY),
                                                   w.codes.data_ptr(), _ld(w.codes), w.scale.data_ptr(),
                                                   _at(Ut), m, _at(V), r, dX.data_ptr(), _ld(dX), ws[0], ws[1]))
@@ -540,7 +563,7 @@ class Rsvd:
 
     def rsvd_keep8_save(self, X):
         """X (tokens x n) kept in 8 bits for the backward pass (Kept8)."""
-        tokens, n = _rows(X, X.shape[-1], "X"), X.shape[1]
+        tokens, n = self._rows(X, X.shape[-1], "X"), X.shape[1]
         codes = _empty_codes(tokens, n, X.device)
         powers = X.new_empty((tokens, -(-n // 32)), dtype=self.torch.uint8)
         self._check(self.lib.rsvd_keep8_save(self.h, self._raw_stream(), _xtype_code(X.dtype), tokens, n, X.data_ptr(), _ld(X),
@@ -549,10 +572,12 @@ class Rsvd:
 
     def rsvd_keep8_load(self, kept, out=None):
         """The kept activations, in their type."""
+        if kept._index != self._index:
+            self._elsewhere(kept, "kept")
         tokens, n, codes, powers = kept.tokens, kept.n, kept.codes, kept.powers
         X = codes.new_empty((tokens, n), dtype=kept.dtype) if out is None else out
         if out is not None:
-            _rows(out, n, "out", tokens, kept.dtype)
+            self._rows(out, n, "out", tokens, kept.dtype)
         self._check(self.lib.rsvd_keep8_load(self.h, self._raw_stream(), _xtype_code(kept.dtype), tokens, n,
                                              codes.data_ptr(), _ld(codes), powers.data_ptr(), _ld(powers), X.data_ptr(), _ld(X)))
         return X
@@ -562,7 +587,9 @@ class Rsvd:
         `out` = (dW, db) of the caller, db may be None; accumulate: they are added to."""
         if dY.shape[0] != kept.tokens:
             raise ValueError("dY: one row for each kept token")
-        _rows(dY, dY.shape[1], "dY")
+        self._rows(dY, dY.shape[1], "dY")
+        if kept._index != self._index:
+            self._elsewhere(kept, "kept")
         if accumulate and out is None:
             raise ValueError("accumulate: into which gradients?")
         xt, m = _xtype_code(dY.dtype), dY.shape[1]
@@ -572,11 +599,13 @@ class Rsvd:
             db = t.empty(m, dtype=t.float32, device=dY.device)
         else:
             dW, db = out
-            _rows(dW, kept.n, "dW")
+            self._rows(dW, kept.n, "dW")
             if dW.dtype != t.float32 or dW.shape[0] != m or (db is not None and (db.dtype != t.float32 or db.shape != (m,) or not db.is_contiguous())):
                 raise ValueError("out: fp32 gradients, m x n and m")
+            if db is not None and db.get_device() != self._index:
+                self._elsewhere(db, "db")
         stream = self._raw_stream()
-        ws = _given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_keep8_grad_bytes", (xt, kept.tokens, kept.n, m))
+        ws = self._given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_keep8_grad_bytes", (xt, kept.tokens, kept.n, m))
         self._check(self.lib.rsvd_keep8_grad(
             self.h, stream, xt, kept.tokens, kept.n, m, _at(dY), _ld(dY), _at(kept.codes), _ld(kept.codes),
             _at(kept.powers), _ld(kept.powers), _at(dW), _ld(dW), _at(db), int(accumulate), ws[0], ws[1]))

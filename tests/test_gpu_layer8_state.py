@@ -105,3 +105,30 @@ def test_the_last_shard_of_a_layer(tokens, rows, n, first, last):
     y = ctx().rsvd_q8_product(x, shard)
     assert torch.equal(y, ctx().rsvd_q8_product(x, Weight8(whole[:, first:last].clone(), scale)))
     check(y, *product_reference(x, shard), "shard")
+
+
+def test_tensors_in_host_memory_are_refused():
+    """By the binding, before anything is launched."""
+    from paper_2110_03423_amd import Kept8, Weight8
+    g, c = gen(9), ctx()
+    w = weight(g, 40, 64, 4)
+    x, dy = activations(g, 9, 64, BF16), activations(g, 9, 40, BF16)
+    kept = c.rsvd_keep8_save(x)
+    on_host = Weight8(w.codes.cpu(), w.scale.cpu(), w.U.cpu(), w.Vt.cpu(), w.bias.cpu())
+    kept_on_host = Kept8(kept.codes.cpu(), kept.powers.cpu(), BF16)
+    room, strided = torch.empty(1 << 22, dtype=torch.uint8), torch.empty(1, dtype=torch.uint8, device="cuda").expand(1 << 22)
+    dW, db = torch.empty(40, 64, device="cuda"), torch.empty(40, device="cuda")
+    for call in (lambda: c.rsvd_q8_rows(x.cpu()), lambda: c.rsvd_q8_product(x.cpu(), w), lambda: c.rsvd_q8_product(x, on_host),
+                 lambda: c.rsvd_q8_product_grad(dy.cpu(), w), lambda: c.rsvd_q8_product_grad(dy, on_host), lambda: c.rsvd_keep8_save(x.cpu()),
+                 lambda: c.rsvd_keep8_load(kept_on_host), lambda: c.rsvd_keep8_load(kept, out=torch.empty(9, 64, dtype=BF16)),
+                 lambda: c.rsvd_keep8_grad(dy.cpu(), kept), lambda: c.rsvd_keep8_grad(dy, kept_on_host),
+                 lambda: c.rsvd_keep8_grad(dy, kept, out=(dW.cpu(), db)), lambda: c.rsvd_keep8_grad(dy, kept, out=(dW, db.cpu())),
+                 lambda: c.rsvd_q8_product(x, w, out=torch.empty(9, 40, dtype=BF16)), lambda: c.rsvd_q8_product_grad(dy, w, out=torch.empty(9, 64, dtype=BF16)),
+                 *[lambda s=s: c.rsvd_q8_product(x, w, workspace=s) for s in (room, strided)],
+                 *[lambda s=s: c.rsvd_q8_product_grad(dy, w, workspace=s) for s in (room, strided)],
+                 *[lambda s=s: c.rsvd_keep8_grad(dy, kept, workspace=s) for s in (room, strided)]):
+        with pytest.raises(ValueError):
+            call()
+    # a workspace of the caller's, of any type
+    own = torch.empty(1 << 20, device="cuda")
+    assert torch.equal(c.rsvd_q8_product(x, w, workspace=own), c.rsvd_q8_product(x, w))

@@ -195,3 +195,22 @@ def test_rows_of_codes_that_end_with_their_storage():
         kept = binding.Kept8(codes, torch.zeros(4, (codes.shape[1] + 31) // 32, dtype=torch.uint8), torch.bfloat16)
         for t in (w.codes, kept.codes):
             assert torch.equal(t, codes) and read_inside(t) and (t.data_ptr() == codes.data_ptr()) == same
+
+
+def test_tensors_of_a_layer_are_on_one_device(plan):
+    torch = pytest.importorskip("torch")
+    codes, scale, bias = torch.zeros(6, 5, dtype=torch.int8), torch.zeros(6), torch.zeros(6)
+    U, Vt = torch.zeros(6, 2, dtype=torch.bfloat16), torch.zeros(2, 5, dtype=torch.bfloat16)
+    powers = torch.zeros(6, 1, dtype=torch.uint8)
+    assert binding.Weight8(codes, scale, U, Vt, bias).device.type == "cpu" and binding.Kept8(codes, powers, torch.float32).device.type == "cpu"
+    for bad in ((codes, scale.to("meta")), (codes, scale, U.to("meta"), Vt), (codes, scale, U, Vt.to("meta")), (codes, scale, U, Vt, bias.to("meta"))):
+        with pytest.raises(ValueError):
+            binding.Weight8(*bad)
+    with pytest.raises(ValueError):
+        binding.Kept8(codes, powers.to("meta"), torch.float32)
+    # a context of no device, tensors on none
+    w, kept, x = binding.Weight8(codes, scale), binding.Kept8(codes, powers, torch.float32), torch.zeros(3, 5)
+    for call in (lambda: plan.rsvd_q8_rows(x), lambda: plan.rsvd_q8_product(x, w), lambda: plan.rsvd_q8_product_grad(torch.zeros(3, 6), w),
+                 lambda: plan.rsvd_keep8_save(x), lambda: plan.rsvd_keep8_load(kept), lambda: plan.rsvd_keep8_grad(torch.zeros(6, 4), kept)):
+        with pytest.raises(ValueError):
+            call()

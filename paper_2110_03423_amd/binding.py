@@ -128,12 +128,12 @@ def _empty_codes(rows, n, device):
 
 def _laid_out(codes):
     """The codes in rows as the C entry points want them (a copy unless they are already)."""
-    if codes.dim() == 2 and codes.stride(1) == 1 and codes.stride(0) % 128 == 0 and codes.data_ptr() % 16 == 0:
+    rows, n = codes.shape
+    if codes.stride(1) == 1 and codes.stride(0) % 128 == 0 and codes.stride(0) >= n and codes.data_ptr() % 16 == 0:
         # (rows are read in 16-byte pieces; the last one's may reach behind what the tensor was cut out of)
-        end = codes.storage_offset() + (codes.shape[0] - 1) * codes.stride(0) + -(-codes.shape[1] // 16) * 16
-        if end <= codes.untyped_storage().nbytes():
+        if codes.storage_offset() + (rows - 1) * codes.stride(0) + -(-n // 16) * 16 <= codes.untyped_storage().nbytes():
             return codes
-    out = _empty_codes(codes.shape[0], codes.shape[1], codes.device)
+    out = _empty_codes(rows, n, codes.device)
     out.copy_(codes)
     return out
 
@@ -212,7 +212,9 @@ class Kept8:
             raise ValueError("powers: one byte for each 32 columns of codes")
         _xtype_code(dtype)
         _together(codes, powers=powers)
-        self._set(_laid_out(codes), powers if powers.stride(1) == 1 or powers.shape[1] == 1 else powers.contiguous(), dtype)
+        if powers.stride(0) < powers.shape[1] or (powers.stride(1) != 1 and powers.shape[1] > 1):
+            powers = powers.contiguous()
+        self._set(_laid_out(codes), powers, dtype)
 
     def _set(self, codes, powers, dtype):
         self.codes, self.powers, self.dtype = codes, powers, dtype

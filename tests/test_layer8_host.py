@@ -214,3 +214,17 @@ def test_tensors_of_a_layer_are_on_one_device(plan):
                  lambda: plan.rsvd_keep8_save(x), lambda: plan.rsvd_keep8_load(kept), lambda: plan.rsvd_keep8_grad(torch.zeros(6, 4), kept)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("rows,n", [(1, 5), (6, 5), (6, 128), (6, 1), (3, 300)])
+def test_rows_that_share_their_memory(rows, n):
+    """One row for all (a stride of zero), columns apart, overlapping rows: laid out as the entry points want them."""
+    torch = pytest.importorskip("torch")
+    flat = (torch.arange(20000) % 251).to(torch.int8)
+    blocks = (n + 31) // 32
+    for codes in (flat[None, :n].expand(rows, n), flat[:rows, None].expand(rows, n), torch.as_strided(flat, (rows, n), (64, 1)), torch.as_strided(flat, (rows, n), (0, 1))):
+        powers = torch.arange(blocks, dtype=torch.uint8)[None].expand(rows, blocks)
+        w, kept = binding.Weight8(codes, torch.zeros(rows)), binding.Kept8(codes, powers, torch.float32)
+        for t in (w.codes, kept.codes):
+            assert torch.equal(t, codes) and (t.stride(1) == 1 or n == 1) and binding._ld(t) >= n and binding._ld(t) % 16 == 0 and t.data_ptr() % 16 == 0
+        assert torch.equal(kept.powers, powers) and binding._ld(kept.powers) >= blocks

@@ -304,7 +304,9 @@ int rsvd_stage_lift(rsvd_ctx *ctx, void *stream, rsvd_dtype dtype,
  *   - tokens, n, m are at least 1 (tokens may be 0: nothing is launched, apart
  *     from the zeros of rsvd_keep8_grad); r may be 0, the factors then NULL.
  *     r at most 1024; n and m at most RSVD_Q8_MAX_FEATURES, beyond which sums of
- *     8-bit products leave 32 bits (RSVD_ERR_UNSUPPORTED).
+ *     8-bit products leave 32 bits (RSVD_ERR_UNSUPPORTED).  At most 4194304 tokens;
+ *     gradients whose operands are more than 2^34 numbers (tokens x m, n x m or
+ *     tokens x n) may be refused the same way.
  *   - X, Y, dX, dY, the factors and the bias may have any leading dimension and
  *     the alignment of their elements; 16-byte aligned rows are faster.
  *   - 8-bit codes have rows of ldq bytes, ldq a multiple of 16 and at least n,

@@ -161,6 +161,8 @@ template <int XT, bool CHECK = true> __device__ __forceinline__ void split_opera
 
 // Leading dimensions that rows in tiles may have: 32-bit offsets inside a tile.
 constexpr int64_t kMaxLd = (int64_t)1 << 23;
+// (sums over tokens, indexes of workgroups, threads of a launch of one workgroup a token)
+constexpr int64_t kMaxTokens = (int64_t)1 << 22;
 
 // ---------------------------------------------------------------- layer8_rows.hip
 // Rows of X (rows x n) to codes with a scale each; a row of codes is written up to `width` (>= n, a multiple of 8) with zeros behind n.
@@ -193,6 +195,11 @@ hipError_t grad_front_launch(rsvd_ctx *ctx, hipStream_t s, rsvd_xtype type, int6
                              const void *F, int64_t ldf, float *sums, const float *dy_factor, uint16_t *planes, int64_t planes_width,
                              int64_t rows, int64_t n, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp, uint16_t *plane,
                              int64_t width);
+// Whether the operands of that many elements (planes of dY, codes; 0: not wanted) are few enough for a launch, which has fewer than 2^32 threads, eight elements
+// of dY or sixteen codes each.  (2^28 of them are more than the low-rank sums take.)
+inline bool grad_front_fits(int64_t tokens, int64_t planes_width, int64_t rows, int64_t n) {
+  return tokens * (planes_width / 8) + rows * ceil_div(n, 16) < ((int64_t)1 << 32) - ((int64_t)1 << 28);
+}
 // t [tokens][parts][rank_places(r)]: the sums added up, as bf16 numbers, the largest first.
 hipError_t lowrank_join_launch(hipStream_t s, const float *sums, int splits, int64_t tokens, int64_t r, int parts, uint16_t *t);
 

@@ -22,9 +22,6 @@ bool valid_xtype(rsvd_xtype t) { return t == RSVD_X_BF16 || t == RSVD_X_F16 || t
 bool valid_codes(const void *p) { return p != nullptr && ((uintptr_t)p & 15) == 0; }
 bool element_aligned(const void *p, int64_t size) { return ((uintptr_t)p & (uintptr_t)(size - 1)) == 0; }
 
-// (sums over tokens and indexes of workgroups)
-constexpr int64_t kMaxTokens = (int64_t)1 << 22;
-
 // Sums over ranges of k times ranks up to which the product of a few tokens takes them as they are (eight pieces of 32 for each of its
 // wavefronts); beyond, a launch that joins them first is less.
 constexpr int64_t kFewUnjoined = 2048;
@@ -244,12 +241,13 @@ int rsvd_q8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t t
   const GradLayout L = product_grad_layout(ctx, type, tokens, n, m, r);
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0) return -19;
   if (workspace_bytes < L.total) return -20;
+  // (the scale goes to dY before that is split, and the codes stay exact)
+  const bool as_codes = kn_takes_codes(ctx, false, tokens, n, m, L.planes, r > 0, ldq, 0);
+  if (!grad_front_fits(tokens, L.width, as_codes ? 0 : m, n)) return RSVD_ERR_UNSUPPORTED;
   if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
   hipStream_t s = (hipStream_t)stream;
   char *ws = (char *)workspace;
   uint16_t *a = (uint16_t *)(ws + L.a), *b = (uint16_t *)(ws + L.b), *t = (uint16_t *)(ws + L.t);
-  // (the scale goes to dY before that is split, and the codes stay exact)
-  const bool as_codes = kn_takes_codes(ctx, false, tokens, n, m, L.planes, r > 0, ldq, 0);
   {
     ProfScope ps(ctx, s, PK_SMALL);
     float *sums = (float *)(ws + L.sums);
@@ -341,11 +339,12 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
   const GradLayout L = keep8_grad_layout(ctx, type, tokens, n, m);
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0) return -17;
   if (workspace_bytes < L.total) return -18;
+  const bool direct = takes_rows(type, dY, m, lddy), as_codes = kn_takes_codes(ctx, true, m, n, tokens, L.planes, false, ldc, ldp);
+  if (!grad_front_fits(direct ? 0 : tokens, L.width, as_codes ? 0 : tokens, n)) return RSVD_ERR_UNSUPPORTED;
   if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
   char *ws = (char *)workspace;
   uint16_t *a = (uint16_t *)(ws + L.a), *b = (uint16_t *)(ws + L.b);
   float *sums = db != nullptr ? (float *)(ws + L.sums) : nullptr;
-  const bool direct = takes_rows(type, dY, m, lddy), as_codes = kn_takes_codes(ctx, true, m, n, tokens, L.planes, false, ldc, ldp);
   {
     ProfScope ps(ctx, s, PK_SMALL);
     RSVD_TRY(grad_front_launch(ctx, s, type, tokens, m, 0, dY, lddy, nullptr, 0, nullptr, nullptr, direct ? nullptr : a, L.width, tokens, n, codes,

@@ -17,11 +17,17 @@ template <int XT> static void rows8_typed(hipStream_t s, const Rows8Params &P) {
 
 hipError_t rows8_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, int8_t *codes, int64_t ldq,
                         int64_t width, float *scale, const float *sums, int splits, int64_t r, int parts, uint16_t *t) {
-  const Rows8Params P = {(const char *)X, ldx, rows, (int)n, codes, ldq, (int)width, scale, sums, splits, (int)rank_places(r), parts, t};
-  if (type == RSVD_X_BF16) rows8_typed<RSVD_X_BF16>(s, P);
-  else if (type == RSVD_X_F16) rows8_typed<RSVD_X_F16>(s, P);
-  else rows8_typed<RSVD_X_F32>(s, P);
-  return hipGetLastError();
+  // (a launch has fewer than 2^32 threads; with sums there are kMaxTokens rows at the most, and one launch)
+  for (int64_t row = 0; row < rows; row += kMaxTokens) {
+    const int64_t some = rows - row < kMaxTokens ? rows - row : kMaxTokens;
+    const Rows8Params P = {(const char *)X + row * ldx * xtype_size(type), ldx, some, (int)n, codes + row * ldq, ldq, (int)width, scale + row, sums,
+                           splits, (int)rank_places(r), parts, t};
+    if (type == RSVD_X_BF16) rows8_typed<RSVD_X_BF16>(s, P);
+    else if (type == RSVD_X_F16) rows8_typed<RSVD_X_F16>(s, P);
+    else rows8_typed<RSVD_X_F32>(s, P);
+    if (const hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 // ---------------------------------------------------------------- blocks of 32 with a power of two

@@ -132,3 +132,15 @@ def test_tensors_in_host_memory_are_refused():
     # a workspace of the caller's, of any type
     own = torch.empty(1 << 20, device="cuda")
     assert torch.equal(c.rsvd_q8_product(x, w, workspace=own), c.rsvd_q8_product(x, w))
+
+
+def test_rows_to_codes_of_more_rows_than_a_launch_has_workgroups():
+    """2^24 workgroups of 256 threads are no launch."""
+    rows = (1 << 24) + 5
+    x = activations(gen(1), rows, 3, BF16)
+    codes, scale = ctx().rsvd_q8_rows(x)
+    top = x.float().abs().amax(dim=1)
+    assert scale.shape == (rows,) and torch.equal(scale, top / torch.full_like(top, 127.0))
+    for at in (0, (1 << 22) - 3, 1 << 22, (1 << 23) + 1, rows - 9):
+        some, s = ctx().rsvd_q8_rows(x[at:at + 9])
+        assert torch.equal(codes[at:at + 9], some) and torch.equal(scale[at:at + 9], s)

@@ -228,3 +228,17 @@ def test_rows_that_share_their_memory(rows, n):
         for t in (w.codes, kept.codes):
             assert torch.equal(t, codes) and (t.stride(1) == 1 or n == 1) and binding._ld(t) >= n and binding._ld(t) % 16 == 0 and t.data_ptr() % 16 == 0
         assert torch.equal(kept.powers, powers) and binding._ld(kept.powers) >= blocks
+
+
+def test_gradients_of_more_operands_than_a_launch_has_threads(plan):
+    """2^32 threads of eight or sixteen operands each."""
+    most = 1 << 22
+    base = dict(ctx=plan.h, stream=NULL, type=X_F16, tokens=most, n=4096, m=4096, dY=PTR, lddy=8192, codes=PTR, ldc=8192, powers=ODD, ldp=256, dW=PTR,
+                lddw=8192, db=PTR, accumulate=0, ws=PTR, bytes=1 << 60)
+    call = lambda **kw: _call(plan, "rsvd_keep8_grad", WGRAD, base, **kw)
+    assert call() == ERR_NO_DEVICE and call(m=8192) == UNSUPPORTED and call(type=X_BF16, m=8192) == ERR_NO_DEVICE
+    assert call(type=X_BF16, m=8192, n=16384, ldc=16384, ldp=512, lddw=16384) == UNSUPPORTED
+    base = dict(ctx=plan.h, stream=NULL, type=X_BF16, tokens=most, n=512, m=4096, r=0, dY=PTR, lddy=8192, codes=PTR, ldq=512, scale=PTR, Ut=NULL,
+                ldut=0, V=NULL, ldv=0, dX=PTR, lddx=512, ws=PTR, bytes=1 << 60)
+    call = lambda **kw: _call(plan, "rsvd_q8_product_grad", GRAD, base, **kw)
+    assert call() == ERR_NO_DEVICE and call(m=8192) == UNSUPPORTED

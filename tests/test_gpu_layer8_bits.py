@@ -14,8 +14,8 @@ from test_gpu_layer8 import BF16, DEV, activations, gen, weight
 pytestmark = pytest.mark.gpu
 
 
-# 64 rows and columns with codes as they are and as a matrix; 128; 256; a single token
-@pytest.mark.parametrize("tokens,n,m,r", [(1, 4096, 1030, 20), (130, 1000, 700, 33), (300, 2100, 900, 0), (1024, 2050, 500, 64), (4090, 4100, 600, 40)])
+# 64 rows and columns with codes as they are (a single token first) and as a matrix; 128; 256
+@pytest.mark.parametrize("tokens,n,m,r", [(1, 4096, 1030, 20), (130, 1000, 700, 33), (300, 2100, 900, 0), (1024, 2050, 500, 64), (4090, 4100, 600, 40), (3970, 4033, 190, 33)])
 def test_product_gradient_in_bf16_loses_nothing_but_its_own_rounding(tokens, n, m, r):
     say("bits of the product gradient", tokens, n, m, r)
     g = gen(tokens + m)
@@ -27,3 +27,12 @@ def test_product_gradient_in_bf16_loses_nothing_but_its_own_rounding(tokens, n, 
         want += (dy.double() @ w.U.double()) @ w.Vt.double()
     own = float((want.float().bfloat16().double() - want).norm())
     assert float((dx - want).norm()) <= 1.01 * own
+
+
+def test_codes_next_to_ties_come_from_two_roundings():
+    """codes = x (127 (1 / a)): at a tie, the two roundings of the factor decide.  (One rounded quotient 127 / a would give the other neighbour in each of these
+    rows; worked out by hand from the fp32 neighbours of 1 / a and 127 / a.)"""
+    ties = [(15.0, 7.5, 64), (19.0, 9.5, 64), (47.0, 23.5, 63), (51.0, 25.5, 64), (83.0, 41.5, 63), (94.0, 47.0, 63), (101.0, 50.5, 63)]
+    x = torch.tensor([[a, t, -t] for a, t, _ in ties], device=DEV)
+    codes, _ = ctx().rsvd_q8_rows(x)
+    assert codes.tolist() == [[127, q, -q] for _, _, q in ties]

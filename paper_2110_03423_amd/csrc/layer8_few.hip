@@ -48,12 +48,14 @@ template <int TB, int WAVES> __global__ __launch_bounds__(64 * WAVES) void few_k
       const int c = c0 + WAVES * u < low_steps ? c0 + WAVES * u : c0;
       const int which = 32 * c / E.rp, p = 32 * c - which * E.rp + 8 * kq;
       g[u] = factor8(E, row, p);
-      if (c0 + WAVES * u >= low_steps) g[u] = (u32x4)0u;
+      const bool none = c0 + WAVES * u >= low_steps;      // (zeros on both sides: sums may be infinite)
+      if (none) g[u] = (u32x4)0u;
 #pragma unroll
       for (int i = 0; i < TB; ++i) {
         const int64_t m = 16 * i + r16 < P.M ? 16 * i + r16 : P.M - 1;
         if (P.sums != nullptr) t[u][i] = raw_load8<RSVD_X_F32>(reinterpret_cast<const char *>(P.sums + ((int64_t)which * P.M + m) * E.rp + p), 8);
         else t[u][i].w[0] = *reinterpret_cast<const u32x4 *>(E.t + (m * E.parts + which) * E.rp + p);
+        if (none) t[u][i].w[0] = t[u][i].w[1] = (u32x4)0u;
       }
     }
   };

@@ -174,3 +174,18 @@ def test_weight_gradient_with_an_infinity_in_every_type(dtype, tokens, n, m):
     assert dW[5, 11].isnan() and db[5] == torch.inf and db[m - 1] == -torch.inf
     keep = [i for i in range(m) if i not in (5, m - 1)]
     assert torch.equal(db[keep], clean_b[keep])
+
+
+@pytest.mark.parametrize("tokens", [1, 3, 20, 40, 100])
+@pytest.mark.parametrize("r", [1, 40, 300])
+def test_low_rank_sums_beyond_fp32_are_infinite(tokens, r):
+    """Finite tokens whose sum with Vt is not: infinities of its sign, times U, and not NaN."""
+    from paper_2110_03423_amd import Weight8
+    U, Vt = torch.ones(50, r, dtype=BF16, device=DEV), torch.ones(r, 64, dtype=BF16, device=DEV)
+    U[7] = -1.0
+    w = Weight8(torch.zeros(50, 64, dtype=torch.int8, device=DEV), torch.ones(50, device=DEV), U, Vt)      # (codes of 0: nothing else is infinite)
+    x = torch.full((tokens, 64), 3e38, device=DEV)
+    y = ctx().rsvd_q8_product(x, w)
+    assert (y[:, 7] == -torch.inf).all()
+    y[:, 7] = torch.inf
+    assert (y == torch.inf).all()

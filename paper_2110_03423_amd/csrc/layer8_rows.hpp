@@ -138,11 +138,11 @@ template <int XT, bool SCALED> __device__ __forceinline__ void split_rows_group(
   const char *x = P.X + (row * P.ldx + j) * XTraits<XT>::SIZE;
   u32x4 out[PARTS];
   if constexpr (SCALED) {
-    float v[8];
+    float v[8], f[8];
     x_load8<XT>(x, left, v);
+    x_load8<RSVD_X_F32>(reinterpret_cast<const char *>(P.factor + j), left, f);
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
-      if (u < left) v[u] *= P.factor[j + u];
+    for (int u = 0; u < 8; ++u) v[u] *= f[u];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       unsigned p[PARTS];

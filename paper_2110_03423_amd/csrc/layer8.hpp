@@ -24,7 +24,7 @@ inline int64_t xtype_size(rsvd_xtype t) { return t == RSVD_X_F32 ? 4 : 2; }
 // bf16 numbers whose sum is exactly a number of the type.
 inline int xtype_parts(rsvd_xtype t) { return t == RSVD_X_BF16 ? 1 : t == RSVD_X_F16 ? 2 : 3; }
 // bf16 numbers that hold such a number times an fp32 scale: to 2^-17 of it (two; results of 16 bits), or as fp32 has it (three).  One, with the scale
-// rounded into the weight, would be half the product, and was not kept: an error of 1.24 times the rounding of a bf16 result.
+// rounded into the weight, would be half the product, and was not kept: an error of 1.24 to 1.4 times the rounding of a bf16 result.
 inline int scaled_parts(rsvd_xtype t) { return t == RSVD_X_F32 ? 3 : 2; }
 // Rows that may be read and written in 16-byte pieces.
 inline bool rows_aligned(const void *p, int64_t ld, int64_t size) { return ((uintptr_t)p & 15) == 0 && ld * size % 16 == 0; }

@@ -270,7 +270,6 @@ int rsvd_q8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t t
   return RSVD_OK;
 }
 
-// Arguments that saving and loading have in common, in the order of each.
 int rsvd_keep8_save(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n, const void *X, int64_t ldx, int8_t *codes,
                     int64_t ldc, uint8_t *powers, int64_t ldp) {
   if (ctx == nullptr) return -1;

@@ -7,8 +7,8 @@
 // Both operands go from memory to registers and from there to LDS, among the matrix instructions of the tile before, and a register is loaded
 // for the tile after next (or, of small tiles, which are done before a load arrives, the one behind) as soon as it has been written.  (Loads
 // straight to LDS: the compiler lets the transposing loads wait for all of them, wherever they go.) Large products are bound by power like
-// those of codes (60 % of the matrix pipe's cycles at 1.8 GHz): gradient of a weight 16384 x 4096 over 16384 tokens 1823 to 1929 us (1.14 to
-// 1.2 PFLOP/s; the library takes 1932 for operands in these orders), 4096 tokens of 16384 to 4096 445 to 479 us (1.15 to 1.24).  Eight
+// those of codes (60 % of the matrix pipe's cycles at 1.8 GHz): gradient of a weight 16384 x 4096 over 16384 tokens 1805 to 1933 us (1.14 to
+// 1.22 PFLOP/s; the library takes 1932 for operands in these orders), 4096 tokens of 16384 to 4096 in two planes 840 to 970 us (1.13 to 1.31).  Eight
 // wavefronts of 128 x 64: four of 128 x 128 would have no registers left for what they stage. Several planes of A are taken as further k, the
 // smallest first; by small tiles together with each k-tile of B, which is then staged and read once for all of them (2048 x 2048 x 1024
 // tokens, three planes: 60 -> 47 us; larger tiles would have no room for two workgroups on a CU). Where few rows of tiles need it, B is taken
@@ -395,8 +395,9 @@ template <bool A_KROWS> static hipError_t kn_run_tile(hipStream_t s, const KnPar
 // Every row of tiles makes bf16 numbers of all the codes again, and so does every plane that is further k; a matrix of them is made once and read twice as
 // long.  Rows of tiles (times such planes) up to which the codes are taken as they are, measured as codes / matrix.  Weight: 4096 x 4096 codes with
 // 64 columns of dY in bf16 (1) 18 / 34 us, fp32 (1) 23 / 33, 256 of bf16 (4) 31 / 42, 512 (8) 49 / 51, 512 of fp16 (8) 68 / 66; 2048 x 2048 with 1024 of
-// bf16 (16) 28 / 33.  X, where a launch before the product is needed anyway: 128 tokens with 16384 x 4096 codes, bf16 (1) 62 / 81 us, fp32 (3)
-// 126 / 145; 256 with 4096 x 4096 (4) 43 / 46, 512 (8) 52 / 48; fp16 54 / 57 and 67 / 66.
+// bf16 (16) 28 / 33.  X, where a launch before the product is needed anyway: 4096 x 4096 codes and 64 tokens (1) 20 / 34 us (bf16, fp16) and 22 / 35 (fp32),
+// 128 (2) 25 / 34 and 30 / 38, 256 (4) 35 / 42 and 43 / 50; 128 tokens with 16384 x 4096 codes (2) 60 / 92 and 73 / 111.  (Not at its end: with 320
+// (5) 44 / 50 and 55 / 61, 512 (8) 56 / 61 and 71 / 75, 301 tokens of 2000 x 1410 (5) 19 / 21 and 25 / 28.)
 bool kn_takes_codes(const rsvd_ctx *ctx, bool a_krows, int64_t M, int64_t N, int64_t K, int planes, bool lowrank, int64_t ldc,
                     int64_t ldp) {
   const TileChoice c = kn_choose(ctx, M, N, K, planes, lowrank);

@@ -137,7 +137,7 @@ template <int XT, int RB, int TB> __global__ __launch_bounds__(256, 2) void lowr
 }
 
 // The same, and behind it the operands of the gradients: three things that have nothing to do with each other, in one launch.  (4096 x 16384 bf16 with 64
-// ranks beside 16384 x 4096 codes: 66 us for 335 MB, 5.1 TB/s.)
+// ranks, to two planes, beside 16384 x 4096 codes: 136 us for 330 MB read and 412 written, 5.5 TB/s.)
 struct GradFrontParams {
   LowrankParams L; int64_t lowrank_groups;
   SplitParams S;

@@ -76,8 +76,9 @@ __device__ __forceinline__ void store_blocks(const Layer8Epilogue &E, int64_t M,
   }
 }
 
-// Keeps sums in the accumulation registers, half of what a wavefront of the largest tiles has: among the others the compiler moves them about,
-// and spills.
+// Keeps sums in the accumulation registers, half of what a wavefront of the largest tiles has: among the others the compiler moves them about in the
+// main loop, and spills.  (The ends of the 256 x 256 kernels still spill, 83 to 104 registers: operands of the low-rank term and of the stores, outside of the
+// loop over k.)
 template <bool PIN, typename vec_t> __device__ __forceinline__ void pin(vec_t &v) {
   if constexpr (PIN) {
     asm volatile("" : "+a"(v));

@@ -4,7 +4,7 @@
   gated_grad    dX = D W, dW = D^T X                   D = (dH * u * act'(g), dH * act(g)); g, u as they were kept, or computed again
   f8            Y = X^ W^^T                            X to 8-bit floats in blocks of 128 features of a token, W held in blocks of 128 x 128
   f8_grad       dX = dY^ W^                            dY to blocks of 128 outputs of a token
-  f8_weight     dW = dY^^T X^  (fp32)                  both to blocks of 128 tokens of a feature
+  f8_weight     dW = dY^^T X^                          both to blocks of 128 tokens of a feature
   orthogonal    X <- a X + (b A + c A^2) X, A = X X^T  five times from G / |G|, for every matrix of a batch
 
 8-bit floats (e4m3): a block shares a power of two 2^e, the least with max |x| <= 448 2^e, e at least -126; a code is x 2^-e rounded to even.
@@ -110,7 +110,7 @@ def work(case):
     if case["op"] == "gated_grad":
         return {"bytes": es * (t * m + 2 * t * n + 4 * m * n + (2 * t * m if case["keep"] else 0)), "flops": flops}
     if case["op"] == "f8_weight":
-        return {"bytes": es * t * (m + n) + 4 * m * n, "flops": flops}
+        return {"bytes": es * (t * (m + n) + m * n), "flops": flops}
     return {"bytes": es * t * (m + n) + m * n + -(-m // 128) * -(-n // 128), "flops": flops}
 
 
@@ -268,7 +268,7 @@ def _run_plain(state):
             return (_rounded8(state["x"], 1, 128) @ w.t()).to(dtype)
         return (_rounded8(state["dy"], 1, 128) @ w).to(dtype)
     if op == "f8_weight":
-        return _rounded8(state["dy"], 128, 1).t() @ _rounded8(state["x"], 128, 1)
+        return (_rounded8(state["dy"], 128, 1).t() @ _rounded8(state["x"], 128, 1)).to(dtype)
     a, b, c = STEP
     x = state["G"].float()
     norm = x.double().square().sum(dim=(1, 2), keepdim=True).sqrt().float()

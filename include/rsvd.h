@@ -374,6 +374,94 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
                     const void *dY, int64_t lddy, const int8_t *codes, int64_t ldc, const uint8_t *powers, int64_t ldp,
                     float *dW, int64_t lddw, float *db, int accumulate, void *workspace, size_t workspace_bytes);
 
+/* ---- a gated feed-forward block ----
+ *
+ * W (2 m x n) holds the gate projection in its first m rows and the up projection
+ * in the others:  H = act(X Wg^T) * (X Wu^T), element by element, in one kernel.
+ * X, W, H and gradients have one type (bf16, fp16, fp32); products of fp32 numbers
+ * are taken as six products of bf16 numbers (2^-24 of the largest left out).
+ * Sums are held in 32 bits.  tokens, n, m as for the layers above (tokens may be 0);
+ * matrices may have any leading dimension and the alignment of their elements.  A
+ * matrix lies as the products read it if it is 16-bit, n is a multiple of 8, its rows
+ * start at 16-byte aligned addresses and its leading dimension is at most 2^22;
+ * otherwise it is copied to the workspace on the way (more than 64 tokens, gradients).
+ * gelu is x (1 + erf(x / sqrt 2)) / 2, gelu_tanh its usual approximation. */
+typedef enum { RSVD_ACT_SILU = 0, RSVD_ACT_GELU = 1, RSVD_ACT_GELU_TANH = 2, RSVD_ACT_RELU = 3 } rsvd_act;
+
+/* Bytes of device workspace.  lie: bit 0, X lies as the products read it; bit 1, W does;
+ * bit 2 (gradient), the products were kept. */
+int rsvd_gated_product_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int lie, size_t *bytes);
+int rsvd_gated_product_grad_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int lie, size_t *bytes);
+
+/* H (tokens x m).  kept (tokens x 2 m, ldk >= 2 m, may be NULL) receives X Wg^T and X Wu^T
+ * for the backward pass. */
+int rsvd_gated_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_act act, int64_t tokens, int64_t n, int64_t m,
+                       const void *X, int64_t ldx, const void *W, int64_t ldw, void *H, int64_t ldh, void *kept, int64_t ldk,
+                       void *workspace, size_t workspace_bytes);
+
+/* With g, u the two products, as they were kept or (kept NULL) computed again, and
+ * D = (dH u act'(g), dH act(g)), rounded to the type (fp32: not):  dX (tokens x n) = D W,
+ * dW (2 m x n) = D^T X.  dX or dW may be NULL: not wanted.  dW has the type of the others, or fp32
+ * (dw_f32 != 0); an fp32 one may be added to (accumulate != 0).  X may be NULL where kept is given and
+ * dW is not wanted, W where kept is given and dX is not. */
+int rsvd_gated_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_act act, int64_t tokens, int64_t n, int64_t m,
+                            const void *dH, int64_t lddh, const void *X, int64_t ldx, const void *W, int64_t ldw,
+                            const void *kept, int64_t ldk, void *dX, int64_t lddx, void *dW, int64_t lddw, int dw_f32, int accumulate,
+                            void *workspace, size_t workspace_bytes);
+
+/* ---- products in 8-bit floats with a power of two for each block of 128 ----
+ *
+ * Codes are e4m3 numbers (one sign, four exponent, three mantissa bits, no infinities,
+ * largest 448).  A block of 128 numbers of a token, or of 128 x 128 of a weight,
+ * shares 2^e, the least with max |x| <= 448 2^e, e at least -126, held as the byte e + 127;
+ * codes are x 2^-e rounded to nearest, ties to even.  A block that holds an infinity or NaN
+ * has the byte 255 and codes that are NaN.
+ *   - codes: rows of ldq bytes, ldq a multiple of 16 and at least n up to a multiple of 128, from a
+ *     16-byte aligned address; the codes from n on to that multiple are zeros.
+ *   - powers: a row for each 128 rows of codes, a byte for each 128 columns, ldp bytes apart, ldp a multiple
+ *     of 4, from a 4-byte aligned address; all bytes to the next multiple of 4 may be read.  Values 1 to 254, or 255.
+ *   - Tokens are rounded on the way, in blocks of 128 of a token (of 128 tokens for the gradient of a
+ *     weight); the rounding is passed straight through.
+ *   - fp32 results are sums of exact products in fp32.  For 16-bit results the matrix instruction for
+ *     8-bit floats multiplies, which cuts products off below 2^-13 of the largest of eight
+ *     (about 1.5e-5 of a result). */
+
+/* W (m x n) to codes and powers; codes_t (n x m, may be NULL) and powers_t: the same in the other
+ * order, which the gradient reads. */
+int rsvd_f8_weight(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t m, int64_t n, const void *W, int64_t ldw,
+                   uint8_t *codes, int64_t ldq, uint8_t *powers, int64_t ldp, uint8_t *codes_t, int64_t ldqt, uint8_t *powers_t, int64_t ldpt);
+
+int rsvd_f8_product_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, size_t *bytes);
+int rsvd_f8_product_grad_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, size_t *bytes);
+int rsvd_f8_weight_grad_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int dw_f32, size_t *bytes);
+
+/* Y (tokens x m) = X^ W^^T.  (workspace may be NULL where no bytes are needed: up to 64 tokens) */
+int rsvd_f8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, const void *X, int64_t ldx,
+                    const uint8_t *codes, int64_t ldq, const uint8_t *powers, int64_t ldp, void *Y, int64_t ldy, void *workspace, size_t workspace_bytes);
+
+/* dX (tokens x n) = dY^ W^ */
+int rsvd_f8_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, const void *dY, int64_t lddy,
+                         const uint8_t *codes_t, int64_t ldqt, const uint8_t *powers_t, int64_t ldpt, void *dX, int64_t lddx,
+                         void *workspace, size_t workspace_bytes);
+
+/* dW (m x n) = dY^^T X^, in the type of both or in fp32 (dw_f32 != 0); an fp32 one may be added to. */
+int rsvd_f8_weight_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, const void *dY, int64_t lddy,
+                        const void *X, int64_t ldx, void *dW, int64_t lddw, int dw_f32, int accumulate, void *workspace, size_t workspace_bytes);
+
+/* ---- an update made orthogonal ----
+ *
+ * Of each of `batch` matrices G (m x n, ldg, stride_g elements apart): X = G / |G| (Frobenius; zeros stay
+ * zeros), then for each step  X <- a X + (b A + c A^2) X,  A = X X^T (X^T X where m > n),
+ * with the step's three coefficients (host, a, b, c of the first step, of the second, ..).  Singular vectors stay as they are,
+ * every singular value goes through the odd polynomials: about one with those of Newton-Schulz iterations, so that the
+ * result is near U V^T.  bf16 results come from iterates in fp16, others from iterates in two fp16 numbers (22 bits); sums are
+ * held in 32 bits.  An infinity or NaN makes the whole matrix NaN.
+ * Coefficients that take a singular value out of [-2.7, 2.7], or b x^2 + c x^4 out of [-7.5, 7.5], are turned away
+ * (RSVD_ERR_UNSUPPORTED), 1 to 64 steps.  O may be G. */
+int rsvd_orthogonalize_bytes(rsvd_ctx *ctx, rsvd_xtype type, int batch, int64_t m, int64_t n, size_t *bytes);
+int rsvd_orthogonalize(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int batch, int64_t m, int64_t n, const void *G, int64_t ldg, int64_t stride_g,
+                       int steps, const float *coefficients, void *O, int64_t ldo, int64_t stride_o, void *workspace, size_t workspace_bytes);
+
 #ifdef __cplusplus
 }
 #endif

@@ -69,8 +69,23 @@ PROTOTYPES = {
     "rsvd_keep8_save": [_VP, _VP, _INT, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64],
     "rsvd_keep8_load": [_VP, _VP, _INT, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64],
     "rsvd_keep8_grad": [_VP, _VP, _INT, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _INT, _VP, _SZ],
+    "rsvd_gated_product_bytes": [_VP, _INT, _I64, _I64, _I64, _INT, C.POINTER(_SZ)],
+    "rsvd_gated_product_grad_bytes": [_VP, _INT, _I64, _I64, _I64, _INT, C.POINTER(_SZ)],
+    "rsvd_gated_product": [_VP, _VP, _INT, _INT, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _SZ],
+    "rsvd_gated_product_grad": [_VP, _VP, _INT, _INT, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _INT,
+                                _INT, _VP, _SZ],
+    "rsvd_f8_weight": [_VP, _VP, _INT, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64],
+    "rsvd_f8_product_bytes": [_VP, _INT, _I64, _I64, _I64, C.POINTER(_SZ)],
+    "rsvd_f8_product_grad_bytes": [_VP, _INT, _I64, _I64, _I64, C.POINTER(_SZ)],
+    "rsvd_f8_weight_grad_bytes": [_VP, _INT, _I64, _I64, _I64, _INT, C.POINTER(_SZ)],
+    "rsvd_f8_product": [_VP, _VP, _INT, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _SZ],
+    "rsvd_f8_product_grad": [_VP, _VP, _INT, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _VP, _SZ],
+    "rsvd_f8_weight_grad": [_VP, _VP, _INT, _I64, _I64, _I64, _VP, _I64, _VP, _I64, _VP, _I64, _INT, _INT, _VP, _SZ],
+    "rsvd_orthogonalize_bytes": [_VP, _INT, _INT, _I64, _I64, C.POINTER(_SZ)],
+    "rsvd_orthogonalize": [_VP, _VP, _INT, _INT, _I64, _I64, _VP, _I64, _I64, _INT, C.POINTER(C.c_float), _VP, _I64, _I64, _VP, _SZ],
 }
 X_BF16, X_F16, X_F32 = 0, 1, 2
+ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
 
 
 def load_library():
@@ -220,6 +235,56 @@ class Kept8:
         self.codes, self.powers, self.dtype = codes, powers, dtype
         self.tokens, self.n = codes.shape
         self.device, self._index = codes.device, codes.get_device()
+        return self
+
+
+def _blocks(n):
+    """128s that n numbers fill."""
+    return -(-n // 128)
+
+
+def _empty_f8(rows, n, device):
+    """Room for rows of codes and their powers as rsvd_f8_product reads them: (codes, rows of whole 128s; powers, rows of whole 4s)."""
+    import torch
+    return (torch.empty((rows, _blocks(n) * 128), dtype=torch.uint8, device=device),
+            torch.empty((_blocks(rows), -(-_blocks(n) // 4) * 4), dtype=torch.uint8, device=device))
+
+
+class WeightF8:
+    """A weight (m x n) in 8-bit floats (torch.float8_e4m3fn) with a power of two for each block of 128 x 128, as rsvd_f8_product takes it:
+    codes, and powers (uint8, e + 127 for 2^e; 255 makes the block NaN), a row for each 128 rows, a byte for each 128 columns.  A copy of them is laid out
+    here once, in the order of the product and (`backward`) in that of its gradient: `codes`, `powers` are views of the first, and a layer whose values change
+    is made anew, here or by Rsvd.rsvd_f8_weight."""
+
+    def __init__(self, codes, powers, backward=True):
+        import torch
+        if codes.dtype != torch.float8_e4m3fn or codes.dim() != 2:
+            raise TypeError("codes: a float8_e4m3fn matrix")
+        m, n = codes.shape
+        if m < 1 or n < 1:
+            raise ValueError("codes: at least one row and one column")
+        if powers.dtype != torch.uint8 or powers.shape != (_blocks(m), _blocks(n)):
+            raise ValueError("powers: one byte for each 128 x 128 codes")
+        _together(codes, powers=powers)
+
+        def lay(c, p):
+            q, e = _empty_f8(c.shape[0], c.shape[1], c.device)
+            q[:, c.shape[1]:] = 0
+            q[:, :c.shape[1]].copy_(c)
+            e.fill_(127)
+            e[:, :p.shape[1]].copy_(p)
+            return q, e
+
+        bytes_ = codes.view(torch.uint8)
+        self._set(m, n, lay(bytes_, powers), lay(bytes_.t(), powers.t()) if backward else None)
+
+    def _set(self, m, n, forward, backward):
+        import torch
+        self.m, self.n = m, n
+        self._forward, self._backward = forward, backward
+        self.codes = forward[0][:, :n].view(torch.float8_e4m3fn)
+        self.powers = forward[1][:, :_blocks(n)]
+        self.device, self._index = forward[0].device, forward[0].get_device()
         return self
 
 
@@ -612,3 +677,161 @@ class Rsvd:
             self.h, stream, xt, kept.tokens, kept.n, m, _at(dY), _ld(dY), _at(kept.codes), _ld(kept.codes),
             _at(kept.powers), _ld(kept.powers), _at(dW), _ld(dW), _at(db), int(accumulate), ws[0], ws[1]))
         return dW, db
+
+    # ---- a gated feed-forward block
+    def _lies(self, t):
+        """Whether a matrix is read by the large products as it lies."""
+        return t.element_size() == 2 and t.shape[1] % 8 == 0 and t.data_ptr() % 16 == 0 and _ld(t) % 8 == 0 and _ld(t) <= 1 << 22
+
+    def _gated(self, X, W, act):
+        """Sizes and type of a gated block, checked."""
+        if act not in ACTS:
+            raise ValueError(f"act: one of {', '.join(ACTS)}")
+        n = W.shape[-1]
+        rows = self._rows(W, n, "W")
+        if rows < 2 or rows % 2 or n < 1:
+            raise ValueError("W: as many rows of the up projection behind as many of the gate")
+        return self._rows(X, n, "X"), n, rows // 2, _xtype_code(W.dtype)
+
+    def _like(self, t, cols, what, rows, dtype):
+        self._rows(t, cols, what, rows, dtype)
+        return t
+
+    def rsvd_gated_product(self, X, W, act="silu", keep=False, workspace=None, out=None):
+        """act(X Wg^T) * (X Wu^T) of tokens X (tokens x n) and W (2 m x n), the rows of Wg before those of Wu, both of one type (bf16, fp16, fp32):
+        tokens x m.  act: silu, gelu, gelu_tanh or relu.  keep: returns (H, kept), kept (tokens x 2 m) the two products for the backward pass."""
+        tokens, n, m, xt = self._gated(X, W, act)
+        if X.dtype != W.dtype:
+            raise TypeError("X, W: one type")
+        lie = self._lies(X) + 2 * self._lies(W)
+        stream = self._raw_stream()
+        ws = self._given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_gated_product_bytes", (xt, tokens, n, m, lie))
+        H = X.new_empty((tokens, m)) if out is None else self._like(out, m, "out", tokens, X.dtype)
+        kept = X.new_empty((tokens, 2 * m)) if keep else None
+        self._check(self.lib.rsvd_gated_product(self.h, stream, xt, ACTS[act], tokens, n, m, X.data_ptr(), _ld(X), W.data_ptr(), _ld(W),
+                                                H.data_ptr(), _ld(H), _at(kept), 2 * m, ws[0], ws[1]))
+        return (H, kept) if keep else H
+
+    def rsvd_gated_product_grad(self, dH, X, W, act="silu", kept=None, out=None, accumulate=False, workspace=None):
+        """Gradients of rsvd_gated_product: (dX (tokens x n), dW (2 m x n)) from dH (tokens x m).  kept: what the forward pass kept; without it both products
+        are computed again.  `out` = (dX, dW) of the caller, either of them None: not wanted; dW in fp32 or the type of W; accumulate: an fp32 dW is added to."""
+        tokens, n, m, xt = self._gated(X, W, act)
+        if X.dtype != W.dtype:
+            raise TypeError("X, W: one type")
+        self._like(dH, m, "dH", tokens, W.dtype)
+        if kept is not None:
+            self._like(kept, 2 * m, "kept", tokens, W.dtype)
+        if accumulate and out is None:
+            raise ValueError("accumulate: into which gradients?")
+        if out is None:
+            dX, dW = X.new_empty((tokens, n)), W.new_empty((2 * m, n))
+        else:
+            dX, dW = out
+            if dX is not None:
+                self._like(dX, n, "dX", tokens, X.dtype)
+            if dW is not None:
+                self._weight_out(dW, 2 * m, n, W.dtype, accumulate)
+        lie = self._lies(X) + 2 * self._lies(W) + 4 * (kept is not None)
+        stream = self._raw_stream()
+        ws = self._given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_gated_product_grad_bytes", (xt, tokens, n, m, lie))
+        self._check(self.lib.rsvd_gated_product_grad(
+            self.h, stream, xt, ACTS[act], tokens, n, m, _at(dH), _ld(dH), _at(X), _ld(X), _at(W), _ld(W), _at(kept), _ld(kept) if kept is not None else 0,
+            _at(dX), _ld(dX) if dX is not None else 0, _at(dW), _ld(dW) if dW is not None else 0,
+            int(dW is not None and dW.dtype == self.torch.float32), int(accumulate and dW is not None), ws[0], ws[1]))
+        return dX, dW
+
+    def _weight_out(self, dW, m, n, dtype, accumulate):
+        f32 = self.torch.float32
+        if dW.dtype != f32 and (accumulate or dW.dtype != dtype):
+            raise ValueError(f"dW: fp32{'' if accumulate else f' or {dtype}'}")
+        self._like(dW, n, "dW", m, dW.dtype)
+
+    # ---- products in 8-bit floats
+    def rsvd_f8_weight(self, W, backward=True):
+        """W (m x n; bf16, fp16, fp32) rounded to 8-bit floats with a power of two for each 128 x 128: a WeightF8.  backward: for rsvd_f8_product_grad, too."""
+        m, n = self._rows(W, W.shape[-1], "W"), W.shape[-1]
+        if m < 1 or n < 1:
+            raise ValueError("W: at least one row and one column")
+        xt = _xtype_code(W.dtype)
+        q, p = _empty_f8(m, n, W.device)
+        back = _empty_f8(n, m, W.device) if backward else None
+        qt, pt = back if backward else (None, None)
+        self._check(self.lib.rsvd_f8_weight(self.h, self._raw_stream(), xt, m, n, W.data_ptr(), _ld(W), _at(q), q.stride(0), _at(p), p.stride(0),
+                                            _at(qt), qt.stride(0) if backward else 0, _at(pt), pt.stride(0) if backward else 0))
+        return WeightF8.__new__(WeightF8)._set(m, n, (q, p), back)
+
+    def _f8(self, name, X, weight, laid_out, n, m, workspace, out):
+        tokens, xt = self._rows(X, n, "X" if name == "rsvd_f8_product" else "dY"), _xtype_code(X.dtype)
+        if weight._index != self._index:
+            self._elsewhere(weight, "weight")
+        stream = self._raw_stream()
+        ws = self._given(workspace) if workspace is not None else self._layer_ws(stream, name + "_bytes", (xt, tokens, weight.n, weight.m))
+        Y = X.new_empty((tokens, m)) if out is None else self._like(out, m, "out", tokens, X.dtype)
+        q, p = laid_out
+        self._check(getattr(self.lib, name)(self.h, stream, xt, tokens, weight.n, weight.m, X.data_ptr(), _ld(X), q.data_ptr(), q.stride(0),
+                                            p.data_ptr(), p.stride(0), Y.data_ptr(), _ld(Y), ws[0], ws[1]))
+        return Y
+
+    def rsvd_f8_product(self, X, weight, workspace=None, out=None):
+        """X (tokens x n), rounded to 8-bit floats in blocks of 128, times the transpose of `weight` (WeightF8): tokens x m, in the type of X."""
+        return self._f8("rsvd_f8_product", X, weight, weight._forward, weight.n, weight.m, workspace, out)
+
+    def rsvd_f8_product_grad(self, dY, weight, workspace=None, out=None):
+        """Gradient of rsvd_f8_product with respect to X: dY (tokens x m), rounded likewise, times `weight`: tokens x n, in the type of dY."""
+        if weight._backward is None:
+            raise ValueError("weight: made without backward=True")
+        return self._f8("rsvd_f8_product_grad", dY, weight, weight._backward, weight.m, weight.n, workspace, out)
+
+    def rsvd_f8_weight_grad(self, dY, X, out=None, accumulate=False, workspace=None):
+        """Gradient of a weight (m x n): the transpose of dY (tokens x m) times X (tokens x n), both of one type and rounded to 8-bit floats in blocks of 128
+        tokens; in their type, or into `out` (fp32 or their type).  accumulate: an fp32 `out` is added to."""
+        m, n = dY.shape[-1], X.shape[-1]
+        tokens, xt = self._rows(X, n, "X"), _xtype_code(X.dtype)
+        self._like(dY, m, "dY", tokens, X.dtype)
+        if accumulate and out is None:
+            raise ValueError("accumulate: into which gradient?")
+        if out is not None:
+            self._weight_out(out, m, n, X.dtype, accumulate)
+        dW = X.new_empty((m, n)) if out is None else out
+        f32 = int(dW.dtype == self.torch.float32)
+        stream = self._raw_stream()
+        ws = self._given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_f8_weight_grad_bytes", (xt, tokens, n, m, f32))
+        self._check(self.lib.rsvd_f8_weight_grad(self.h, stream, xt, tokens, n, m, _at(dY), _ld(dY), _at(X), _ld(X), _at(dW), _ld(dW), f32, int(accumulate),
+                                                 ws[0], ws[1]))
+        return dW
+
+    # ---- updates made orthogonal
+    def rsvd_orthogonalize(self, G, steps=5, coefficients=(3.4445, -4.7750, 2.0315), workspace=None, out=None):
+        """G (m x n, or batch x m x n; bf16, fp16, fp32) with its singular values brought near one and its singular vectors as they are: `steps` times
+        X <- a X + (b A + c A^2) X, A = X X^T, from G / |G|.  coefficients: (a, b, c), or one such triple for each step.  out may be G."""
+        if G.dim() not in (2, 3):
+            raise ValueError("G: a matrix, or a batch of them")
+        if G.get_device() != self._index:
+            self._elsewhere(G, "G")
+        batch, m, n = (1, *G.shape) if G.dim() == 2 else G.shape
+        xt = _xtype_code(G.dtype)
+        if m < 1 or n < 1:
+            raise ValueError("G: at least one row and one column")
+        if out is not None and (out.shape != G.shape or out.dtype != G.dtype):
+            raise ValueError("out: shape and type of G")
+        if out is not None and out.get_device() != self._index:
+            self._elsewhere(out, "out")
+        steps = int(steps)
+        if not 1 <= steps <= 64:
+            raise ValueError("steps: 1 to 64")
+        flat = [float(v) for v in coefficients] * steps if not hasattr(coefficients[0], "__len__") else [float(v) for c in coefficients for v in c]
+        if len(flat) != 3 * steps:
+            raise ValueError("coefficients: three numbers, or three for each step")
+        O = G.new_empty(G.shape) if out is None else out
+
+        def strides(t, what):
+            if (n > 1 and t.stride(-1) != 1) or (m > 1 and t.stride(-2) < n) or (batch > 1 and G.dim() == 3 and t.stride(0) < 0):
+                raise ValueError(f"{what}: matrices with contiguous rows are needed")
+            return (t.stride(-2) if m > 1 else max(t.stride(-2), n)), (t.stride(0) if t.dim() == 3 and batch > 1 else m * n)
+
+        (ldg, sg), (ldo, so) = strides(G, "G"), strides(O, "out")
+        stream = self._raw_stream()
+        ws = self._given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_orthogonalize_bytes", (xt, batch, m, n))
+        self._check(self.lib.rsvd_orthogonalize(self.h, stream, xt, batch, m, n, _at(G), ldg, sg, steps, (C.c_float * len(flat))(*flat), _at(O), ldo, so,
+                                                ws[0], ws[1]))
+        return O

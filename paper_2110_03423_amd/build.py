@@ -16,7 +16,9 @@ OBJ_DIR = os.path.join(HERE, "_build")
 
 SOURCES = ["sketch.hip", "gemm_f32.hip", "gemm_split_n.hip", "gemm_split_t.hip", "gemm_f64.hip", "gemm_f32acc64.hip", "chol.hip",
            "jacobi.hip", "apply.hip", "gram.hip", "rsvd_api.hip",
-           "layer8_rows.hip", "layer8_gemm.hip", "layer8_grad.hip", "layer8_few.hip", "layer8_lowrank.hip", "layer8_api.hip"]
+           "layer8_rows.hip", "layer8_gemm.hip", "layer8_grad.hip", "layer8_few.hip", "layer8_lowrank.hip", "layer8_api.hip",
+           "dense.hip", "dense_nt_bf16.hip", "dense_nt_f16.hip", "dense_nt_f16_linear.hip", "dense_nt_f8.hip", "dense_nt_f8_exact.hip", "dense_kn_bf16.hip",
+           "dense_kn_f16.hip", "gated.hip", "f8.hip", "orthogonal.hip", "dense_api.hip"]
 
 # Packed fp32 instructions are switched off for device code on purpose.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",

@@ -1,0 +1,112 @@
+// Shared declarations of the operators of a gated block: products of 16-bit numbers and of 8-bit floats.
+#pragma once
+
+#include "layer8.hpp"
+
+namespace rsvd {
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// What the operands of a product are: 16-bit numbers, or codes of 8-bit floats (e4m3) with a power of two for 128 of them along k.
+// DK_F8 multiplies codes as they are; DK_F8_EXACT makes bf16 numbers of codes and powers first, see dense_nt.hpp.
+enum DenseKind { DK_BF16 = 0, DK_F16 = 1, DK_F8 = 2, DK_F8_EXACT = 3 };
+
+// Products of planes: numbers that are sums of several 16-bit numbers, whose products are taken as further k, the smallest first.  Nibble s of
+// `a` and `b`: planes of the two operands in part s of k.
+struct DenseSegs { int count; uint32_t a, b; };
+inline DenseSegs dense_segs(int planes) {
+  if (planes == 3) return {6, 0x001012u, 0x010210u};       // (2,0) (1,1) (0,2) (1,0) (0,1) (0,0): 2^-24 of the largest is left out
+  if (planes == 2) return {3, 0x001u, 0x010u};             // (1,0) (0,1) (0,0): 2^-22
+  return {1, 0u, 0u};
+}
+
+// value = alpha sum + beta D, stored in `type`, or as two fp16 numbers `plane` bytes apart (planes = 2).  D: fp16 numbers, `planes` of them.
+struct LinearOut {
+  float alpha = 1.f, beta = 0.f;
+  const uint16_t *D = nullptr; int64_t ldd = 0, d_plane = 0, d_batch = 0;      // (elements, bytes, elements)
+  int d_planes = 1;
+  void *C = nullptr; int64_t ldc = 0, c_plane = 0, c_batch = 0;               // (elements, bytes, elements)
+  int type = RSVD_X_F32, planes = 1, accumulate = 0;
+  int64_t width = 0;                       // columns stored, zeros from N on (0: N)
+};
+
+enum GatedAct { GATED_SILU = 0, GATED_GELU = 1, GATED_GELU_TANH = 2, GATED_RELU = 3, GATED_ACTS = 4 };
+
+// gate, up -> act(gate) up, and both of them as they are (kept: N columns of gate, N of up); or, with dH, their gradients to `planes` planes of D.
+struct GatedOut {
+  int act = GATED_SILU, type = RSVD_X_BF16;
+  void *H = nullptr; int64_t ldh = 0;
+  void *kept = nullptr; int64_t ldk = 0;
+  const void *dH = nullptr; int64_t lddh = 0;
+  uint16_t *D = nullptr; int64_t ldD = 0, plane = 0;      // (elements, bytes)
+};
+
+// ---------------------------------------------------------------- products
+// C (M x N) = sum over k < K of A_mk B_kn, for each of `batch` problems.
+// Strides in bytes.  gated: B has 2 N rows, gate and up, and N counts the outputs.
+struct DenseDesc {
+  int kind = DK_BF16, batch = 1;
+  int64_t M = 0, N = 0, K = 0;
+  bool gated = false, symmetric = false;   // symmetric (M = N): the tiles on and below the diagonal are computed, and stored twice
+  const void *A = nullptr; int64_t lda = 0, a_plane = 0, a_batch = 0;
+  const void *B = nullptr; int64_t ldb = 0, b_plane = 0, b_batch = 0;
+  int planes = 1;                          // of both
+  // 8-bit floats: powers, row (index >> shift), a byte for 128 k; rows are a multiple of 4 bytes from a 4-byte aligned address
+  const uint8_t *a_pow = nullptr, *b_pow = nullptr; int64_t ld_apow = 0, ld_bpow = 0; int a_shift = 0, b_shift = 0;
+  LinearOut out;
+  GatedOut gate;
+  float *partial = nullptr; size_t partial_bytes = 0;
+};
+size_t dense_partial_bytes(const rsvd_ctx *ctx, const DenseDesc &d);
+
+// Both operands with consecutive k (M rows, N or 2 N rows), rows of whole 16-byte pieces from 16-byte aligned addresses.  (8-bit floats: rows of whole k-tiles of 128,
+// zeros behind the last k.)
+hipError_t dense_nt_launch(rsvd_ctx *ctx, hipStream_t s, const DenseDesc &d);
+// B with rows of n (K x N); A with rows of k, or with rows of m (a_krows: K x M).  Rows as above; zeros from k = K to the next multiple of 8 in A.
+hipError_t dense_kn_launch(rsvd_ctx *ctx, hipStream_t s, const DenseDesc &d, bool a_krows);
+hipError_t dense_init_device(rsvd_ctx *ctx);
+
+// ---------------------------------------------------------------- gated.hip
+hipError_t zero_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, void *C, int64_t ldc);
+constexpr int64_t kGatedFew = 64;
+// The forward product of up to kGatedFew tokens.
+struct GatedFewDesc {
+  rsvd_xtype type; int64_t tokens, n, m;
+  const void *X; int64_t ldx;
+  const void *W; int64_t ldw;
+  GatedOut out;
+};
+hipError_t gated_few_launch(rsvd_ctx *ctx, hipStream_t s, const GatedFewDesc &d);
+// D from kept products.
+hipError_t gated_slope_launch(hipStream_t s, int64_t tokens, int64_t m, const GatedOut &o);
+// A matrix as the products want it: 16-bit numbers in rows of `width` (a multiple of 8) with zeros behind n; fp32 as three bf16 planes.
+hipError_t planes_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint16_t *out, int64_t width, int64_t plane);
+
+// ---------------------------------------------------------------- f8.hip
+constexpr int64_t kF8Few = 64;
+// X (rows x n) to codes in blocks of 128: of a row (codes: rows x width, powers rows x ldp), or of 128 rows (codes: n x width, powers n x ldp; width = rows up to a
+// multiple of 128).  Zeros behind the last number.
+hipError_t f8_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint8_t *codes, int64_t width, uint8_t *powers, int64_t ldp);
+hipError_t f8_columns_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint8_t *codes, int64_t width, uint8_t *powers, int64_t ldp);
+// W (m x n) to codes in blocks of 128 x 128, and the same in the other order (NULL: not wanted).
+hipError_t f8_weight_launch(hipStream_t s, rsvd_xtype type, int64_t m, int64_t n, const void *W, int64_t ldw, uint8_t *codes, int64_t ldq, uint8_t *powers, int64_t ldp,
+                            uint8_t *codes_t, int64_t ldqt, uint8_t *powers_t, int64_t ldpt);
+// The product of up to kF8Few tokens, X rounded on the way.
+struct F8FewDesc {
+  rsvd_xtype type; int64_t tokens, n, m;
+  const void *X; int64_t ldx;
+  const uint8_t *codes; int64_t ldq;
+  const uint8_t *powers; int64_t ldp;
+  void *Y; int64_t ldy;
+};
+hipError_t f8_few_launch(rsvd_ctx *ctx, hipStream_t s, const F8FewDesc &d);
+
+// ---------------------------------------------------------------- orthogonal.hip
+// |G| of every matrix by parts (kNormParts doubles each), and G / |G| times 2^13 as one or two fp16 planes with zeros up to `width`.
+constexpr int kNormParts = 64;
+hipError_t norm_launch(hipStream_t s, rsvd_xtype type, int batch, int64_t m, int64_t n, const void *G, int64_t ldg, int64_t stride, double *parts);
+hipError_t unit_launch(hipStream_t s, rsvd_xtype type, int batch, int64_t m, int64_t n, const void *G, int64_t ldg, int64_t stride, const double *parts,
+                       uint16_t *X, int64_t width, int64_t plane, int planes);
+
+}  // namespace rsvd

@@ -1,0 +1,184 @@
+// Products of 16-bit numbers where B has rows of n, and A rows of k or of m: gradients, and polynomials times a matrix.
+//
+// Tiles [k][x] in LDS are read with the transposing LDS load (sixteen lanes read four k of sixteen columns and get one column of four k each); rows of k
+// lie with their 32-byte pieces exchanged by the low bits of k, so that the eight rows that half a wavefront reads start at different banks.  Both operands go
+// from memory to registers and from there to LDS, among the matrix instructions of the tile before.
+#pragma once
+
+#include <type_traits>
+
+#include "dense_tile.hpp"
+#include "layer8_staged.hpp"
+
+namespace rsvd {
+
+template <int BM, int BN> struct DenseKnCfg {
+  static constexpr int A = BM * 128, B = BN * 128, STAGE = A + B, DEPTH = BM == 256 ? 1 : 2;
+  static constexpr size_t lds = 2 * (size_t)STAGE;      // (more than the wavefronts need in the end)
+};
+
+template <int KIND, bool A_KROWS, int BM, int BN, int WGM, int WGN>
+__global__ __launch_bounds__(64 * WGM * WGN, 2) void dense_kn_kernel(const DenseParams P) {
+  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, DEPTH = DenseKnCfg<BM, BN>::DEPTH;
+  constexpr int STAGE = DenseKnCfg<BM, BN>::STAGE, B_LDS = DenseKnCfg<BM, BN>::A;
+  extern __shared__ __attribute__((aligned(16))) char dense_lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, kq = lane >> 4;
+  const int wave_m = wave / WGN, wave_n = wave % WGN, wm0 = wave_m * WM, wn0 = wave_n * WN;
+  int tile_m, tile_n, split, batch;
+  dense_tile_of(P, tile_m, tile_n, split, batch);
+  const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
+  const int kt_begin = split * P.kt_per_split, nkt = P.kt_all - kt_begin < P.kt_per_split ? P.kt_all - kt_begin : P.kt_per_split;
+
+  f32x4 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      acc[i][j] = (f32x4)0.f;
+      pin<BM == 256>(acc[i][j]);
+    }
+
+  // the k-tile that is loaded next: its part of k, its place there, and how many k of it exist
+  int next_seg = __builtin_amdgcn_readfirstlane(kt_begin / P.ktiles), next_kt = __builtin_amdgcn_readfirstlane(kt_begin - next_seg * P.ktiles);
+  const char *const a_first = P.A + batch * P.a_batch + (A_KROWS ? m0 * 2 : m0 * P.lda), *const b_first = P.B + batch * P.b_batch + n0 * 2;
+  const char *a_now, *b_now;
+  int left;
+  auto point = [&]() RSVD_INLINE {
+    const int64_t k = (int64_t)next_kt * kKnK;
+    a_now = a_first + (int64_t)(P.segs.a >> (4 * next_seg) & 15) * P.a_plane + (A_KROWS ? k * P.lda : k * 2);
+    b_now = b_first + (int64_t)(P.segs.b >> (4 * next_seg) & 15) * P.b_plane + k * P.ldb;
+    left = (int)(P.K - k < kKnK ? P.K - k : kKnK);
+  };
+  auto advance = [&]() RSVD_INLINE {                    // (behind the last tile of this workgroup's range: loads stay inside the operands)
+    if (++next_kt == P.ktiles) {
+      next_kt = 0;
+      if (next_seg + 1 < P.segs.count) ++next_seg;
+    }
+    point();
+  };
+  Staged<NT, BM, A_KROWS, DEPTH> sa;
+  Staged<NT, BN, true, DEPTH> sb;
+  sa.init(P.lda, P.M - m0, tid);
+  sb.init(P.ldb, P.N - n0, tid);
+  constexpr int NA = decltype(sa)::N, PIECES = NA + decltype(sb)::N;
+  auto load = [&](int set, int p) RSVD_INLINE {
+    if (p < NA) sa.load(set, p, a_now, P.lda, left);
+    else sb.load(set, p - NA, b_now, P.ldb, left);
+  };
+  auto write = [&](int set, int p, int buf) RSVD_INLINE {
+    if (p < NA) sa.write(set, p, dense_lds + buf * STAGE);
+    else sb.write(set, p - NA, dense_lds + buf * STAGE + B_LDS);
+  };
+
+  // ---- operands of this lane
+  constexpr int A_ROW = decltype(sa)::ROW;
+  const int key_row = 8 * kq + (r16 >> 2), part = (r16 & 3) * 8;
+  // (blocks of 16 columns differ from the first one of the wavefront in the bits that are exchanged)
+  static_assert((TM == 8 || TM == 4 || TM == 2) && (TN == 8 || TN == 4 || TN == 2), "blocks of a power of two");
+  const int a_at = A_KROWS ? key_row * A_ROW + (krow_piece<BM>(wm0 / 16, key_row) << 5) + part : (wm0 + r16) * 128;
+  const int b_at = B_LDS + key_row * (BN * 2) + (krow_piece<BN>(wn0 / 16, key_row) << 5) + part;
+  typedef short s16x4 __attribute__((ext_vector_type(4)));
+  auto transposed = [&](const char *p, int row_bytes) RSVD_INLINE {
+    const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p)));
+    const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)(p + 4 * row_bytes)));
+    return u32x4{lo[0], lo[1], hi[0], hi[1]};
+  };
+  // A barrier that waits for what was written to LDS but not for loads.
+  auto meet = [&]() RSVD_INLINE {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(tile_wait(63));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // The matrix instructions of a tile, with the next one going to LDS in step.  (Behind the last tile that is one that nobody reads: no branches.)
+  auto body = [&](int buf, auto from) RSVD_INLINE {
+    constexpr int SET = decltype(from)::value;
+    const int a_lds = a_at + buf * STAGE, b_lds = b_at + buf * STAGE;
+    auto read_a = [&](int step) RSVD_INLINE {
+      const int h = step / TM, i = step % TM;
+      return A_KROWS ? transposed(dense_lds + (a_lds ^ (i << 5)) + h * 32 * A_ROW, A_ROW)
+                     : *reinterpret_cast<const u32x4 *>(dense_lds + a_lds + i * 2048 + (((4 * h + kq) ^ (r16 & 7)) << 4));
+    };
+    auto read_b = [&](int h, int j) RSVD_INLINE { return transposed(dense_lds + (b_lds ^ (j << 5)) + h * 32 * BN * 2, BN * 2); };
+    constexpr int AHEAD = TM >= 4 ? 3 : 1;             // rows of blocks read ahead, not all of them: registers
+    u32x4 a[AHEAD + 1], b[2][TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) b[0][j] = read_b(0, j);
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) a[i] = read_a(i);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int step = 0; step < 2 * TM; ++step) {
+      const int h = step / TM, i = step % TM;
+      if (step + AHEAD < 2 * TM) a[(step + AHEAD) % (AHEAD + 1)] = read_a(step + AHEAD);
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        if (h == 0 && i == j * TM / TN) b[1][j] = read_b(1, j);
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        acc[i][j] = KIND == DK_BF16 ? mfma_bf16(b[h][j], a[step % (AHEAD + 1)], acc[i][j]) : mfma_f16(b[h][j], a[step % (AHEAD + 1)], acc[i][j]);
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p)
+        if (p * (2 * TM) / PIECES == step) {
+          write(SET, p, buf ^ 1);
+          load(SET, p);
+        }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  };
+  // Tile kt goes through register set kt mod DEPTH.
+  point();
+#pragma unroll
+  for (int set = 0; set < DEPTH; ++set) {
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) load(set, p);
+    advance();
+  }
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    write(0, p, 0);
+    load(0, p);
+  }
+  advance();
+  meet();
+  auto tile = [&](int buf, auto from) RSVD_INLINE {
+    body(buf, from);
+    advance();
+    meet();
+  };
+  if constexpr (DEPTH == 1) {
+    for (int kt = 0; kt < nkt; ++kt) tile(kt & 1, std::integral_constant<int, 0>());
+  } else {
+    for (int kt = 0; kt < nkt; kt += 2) {
+      tile(0, std::integral_constant<int, 1>());
+      if (kt + 1 < nkt) tile(1, std::integral_constant<int, 0>());
+    }
+  }
+  int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
+  asm volatile("" : "+v"(last_lane));
+  // (behind the last meeting nobody reads the tiles)
+  dense_finish<false, TM, TN>(P, acc, split, batch, m0 + wm0, n0 + wn0, P.symmetric && tile_m != tile_n, last_lane,
+                                         reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
+}
+
+template <int KIND, bool A_KROWS, int BM, int BN, int WGM, int WGN> hipError_t dense_kn_run(hipStream_t s, const DenseParams &P) {
+  hipLaunchKernelGGL((dense_kn_kernel<KIND, A_KROWS, BM, BN, WGM, WGN>), dim3(dense_groups(P)), dim3(64 * WGM * WGN), (DenseKnCfg<BM, BN>::lds), s, P);
+  return hipGetLastError();
+}
+template <int KIND, bool A_KROWS> hipError_t dense_kn_tile(hipStream_t s, const DenseParams &P, int b) {
+  if (b == 256) return dense_kn_run<KIND, A_KROWS, 256, 256, 2, 4>(s, P);
+  if (b == 128) return dense_kn_run<KIND, A_KROWS, 128, 128, 2, 2>(s, P);
+  return dense_kn_run<KIND, A_KROWS, 64, 64, 2, 2>(s, P);
+}
+template <int KIND, bool A_KROWS> hipError_t dense_kn_init() {
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, 256, 256, 2, 4>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)DenseKnCfg<256, 256>::lds);
+}
+#define DENSE_KN(KIND, A_KROWS)                                                                      \
+  template hipError_t dense_kn_tile<KIND, A_KROWS>(hipStream_t s, const DenseParams &P, int b);     \
+  template hipError_t dense_kn_init<KIND, A_KROWS>();
+
+}  // namespace rsvd

@@ -1,0 +1,292 @@
+// Products of two matrices with consecutive k: 16-bit numbers, and codes of 8-bit floats with a power of two for 128 of them.
+//
+// Tiles of BM x BN by WGM x WGN wavefronts.  A k-tile is 128 bytes of every row of both operands (64 numbers, 128 codes); two of them (three of small tiles) have
+// room in LDS, which is filled by loads that write there themselves, issued among the matrix instructions of the tile before.  LDS is written in the order of the
+// lanes, 16 bytes each, so a lane fetches the piece that belongs to its place: piece ch of row r lies in place ch ^ (r mod 8), which lets the eight rows that are
+// read together start at different banks.  What is behind the last k is written over with zeros once it has arrived: a load has no mask.
+//
+// gated: a tile's rows of B are sixteen of the gate and the sixteen of the up projection that belong to them in turn, so that a lane ends with both
+// numbers of an output in its registers.
+//
+// Codes are multiplied with their powers by the scaled matrix instruction (one for 128 k).  It takes eight k at a time and cuts each product off, towards zero, below
+// 2^-13 of the largest of them, as all instructions for 8-bit floats do: measured 1.4e-5 of a result of normal numbers, 1.5e-4 of the sum of
+// magnitudes at the worst.  That is lost in the rounding of a 16-bit result; for fp32 results DK_F8_EXACT makes bf16 numbers of the codes and
+// their powers, exactly, and multiplies those at half the rate.
+#pragma once
+
+#include "dense_tile.hpp"
+
+namespace rsvd {
+
+template <int BM, int BN> struct DenseNtCfg {
+  static constexpr int STAGE = (BM + BN) * 128, RING = BM == 64 ? 3 : 2;
+  static constexpr size_t lds = RING * (size_t)STAGE;      // (more than the wavefronts need in the end)
+};
+
+// The loads of ROWS rows of a k-tile by NT threads.
+template <int NT, int ROWS, bool GATED> struct DenseLoad {
+  static constexpr int N = ROWS * 8 / NT;
+  static_assert(ROWS * 8 % NT == 0 && NT % 64 == 0, "whole rounds");
+  uint32_t off[N];
+  __device__ __forceinline__ void init(int64_t ld, int64_t rows_left, int tid) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int q = tid + NT * i, r = q >> 3, wanted = GATED ? (r >> 5 << 4) + (r & 15) : r;
+      const int row = wanted < rows_left ? wanted : (int)rows_left - 1;
+      off[i] = (uint32_t)row * (uint32_t)ld + (uint32_t)(((q & 7) ^ (r & 7)) << 4);
+      asm volatile("" : "+v"(off[i]));                   // (one register, not the pair that the product came in)
+    }
+  }
+  // Load i of a thread, from the tile's first row on (gated: `up` bytes behind it for rows of the up projection; a wavefront has eight rows of one of
+  // both).  left: pieces of the k-tile that exist; another one is read in the place of those that do not.
+  __device__ __forceinline__ void issue(int i, const char *base, int64_t up, char *lds, int left, int wave, int tid) {
+    uint32_t o = off[i];
+    if (left < 8) {
+      const int q = tid + NT * i, ch = (q & 7) ^ ((q >> 3) & 7);
+      if (ch >= left) o -= (uint32_t)ch << 4;
+    }
+    if (GATED && ((wave * 8 + NT / 8 * i) >> 4 & 1)) base += up;
+    const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00027000);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(all, (__attribute__((address_space(3))) void *)(lds + (wave * 64 + NT * i) * 16), 16, o, 0, 0, 0);
+  }
+};
+
+// Sixteen codes times a power of two as bf16 numbers (exactly, but for results below the least bf16 number).
+__device__ __forceinline__ void f8_widen(u32x4 codes, float unit, u32x4 (&out)[2]) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const unsigned four = codes[w];
+    out[w >> 1][2 * (w & 1)] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, unit, false));
+    out[w >> 1][2 * (w & 1) + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, unit, true));
+  }
+}
+__device__ __forceinline__ float f8_unit(unsigned power) {
+  return power == 255u ? __uint_as_float(0x7fc00000u) : power == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(power << 23);
+}
+
+__device__ __forceinline__ i32x8 f8_both(const u32x4 (&p)[2]) {
+  return i32x8{(int)p[0][0], (int)p[0][1], (int)p[0][2], (int)p[0][3], (int)p[1][0], (int)p[1][1], (int)p[1][2], (int)p[1][3]};
+}
+
+template <int KIND, bool GATED, int BM, int BN, int WGM, int WGN>
+__global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_kernel(const DenseParams P) {
+  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = DenseNtCfg<BM, BN>::STAGE, RING = DenseNtCfg<BM, BN>::RING;
+  constexpr bool CODES = KIND >= DK_F8;
+  extern __shared__ __attribute__((aligned(16))) char dense_lds[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, kq = lane >> 4;
+  const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
+  int tile_m, tile_n, split, batch;
+  dense_tile_of(P, tile_m, tile_n, split, batch);
+  const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * (GATED ? BN / 2 : BN);
+  const int kt_begin = split * P.kt_per_split, nkt = P.kt_all - kt_begin < P.kt_per_split ? P.kt_all - kt_begin : P.kt_per_split;
+
+  f32x4 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      acc[i][j] = (f32x4)0.f;
+      pin<BM == 256>(acc[i][j]);
+    }
+
+  DenseLoad<NT, BM, false> la;
+  DenseLoad<NT, BN, GATED> lb;
+  la.init(P.lda, P.M - m0, tid);
+  lb.init(P.ldb, P.N - n0, tid);
+  constexpr int LOADS = decltype(la)::N + decltype(lb)::N;
+  const char *const a_row = P.A + batch * P.a_batch + m0 * P.lda, *const b_row = P.B + batch * P.b_batch + n0 * P.ldb;
+  const int last_left = (int)((P.K * (CODES ? 1 : 2) - (int64_t)(P.ktiles - 1) * 128) >> 4);      // pieces of the last k-tile that exist
+
+  // the k-tile that is loaded next, and the one that is multiplied next: its part of k and its place there
+  int next_seg = __builtin_amdgcn_readfirstlane(kt_begin / P.ktiles), next_kt = __builtin_amdgcn_readfirstlane(kt_begin - next_seg * P.ktiles), next = 0;
+  int now_kt = next_kt;
+  const char *a_now, *b_now;
+  int left;
+  auto point = [&]() RSVD_INLINE {
+    a_now = a_row + (int64_t)(P.segs.a >> (4 * next_seg) & 15) * P.a_plane + (int64_t)next_kt * 128;
+    b_now = b_row + (int64_t)(P.segs.b >> (4 * next_seg) & 15) * P.b_plane + (int64_t)next_kt * 128;
+    left = next_kt == P.ktiles - 1 ? last_left : 8;
+  };
+  auto advance = [&]() RSVD_INLINE {                    // (behind the last tile that one again, where nobody reads it: no branches around loads)
+    if (++next < nkt) {
+      if (++next_kt == P.ktiles) {
+        next_kt = 0;
+        ++next_seg;
+      }
+    }
+    point();
+  };
+  auto issue = [&](int kt, int l) RSVD_INLINE {
+    char *st = dense_lds + (kt % RING) * STAGE;
+    if (l < decltype(la)::N) la.issue(l, a_now, 0, st, left, wave, tid);
+    else lb.issue(l - decltype(la)::N, b_now, P.b_up, st + BM * 128, left, wave, tid);
+  };
+  point();
+#pragma unroll
+  for (int t = 0; t < RING - 1; ++t) {
+#pragma unroll
+    for (int l = 0; l < LOADS; ++l) issue(t, l);
+    advance();
+  }
+
+  // powers of four k-tiles at a time, fetched four ahead
+  unsigned pa[2][CODES ? TM : 1], pb[2][CODES ? TN : 1];
+  const uint8_t *a_pow[CODES ? TM : 1], *b_pow[CODES ? TN : 1];
+  if constexpr (CODES) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int64_t m = m0 + wm0 + 16 * i + r16;
+      a_pow[i] = P.a_pow + ((m < P.M ? m : P.M - 1) >> P.a_shift) * P.ld_apow;
+    }
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int64_t n = n0 + wn0 + 16 * j + r16;
+      b_pow[j] = P.b_pow + ((n < P.N ? n : P.N - 1) >> P.b_shift) * P.ld_bpow;
+    }
+  }
+  auto fetch_powers = [&](int kt) RSVD_INLINE {         // (of the range's k-tile kt, a multiple of four; behind the last: those again)
+    const int at = kt_begin + (kt < nkt ? kt : (nkt - 1) & ~3);
+#pragma unroll
+    for (int i = 0; i < (CODES ? TM : 0); ++i) pa[1][i] = *reinterpret_cast<const unsigned *>(a_pow[i] + at);
+#pragma unroll
+    for (int j = 0; j < (CODES ? TN : 0); ++j) pb[1][j] = *reinterpret_cast<const unsigned *>(b_pow[j] + at);
+  };
+  if constexpr (CODES) fetch_powers(0);
+
+  const int swz = r16 & 7;                       // (rows of a wavefront's blocks start at multiples of 16)
+  const char *const a_lds = dense_lds + (wm0 + r16) * 128, *const b_lds = dense_lds + BM * 128 + (wn0 + r16) * 128;
+  for (int kt = 0; kt < nkt; ++kt) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(tile_wait((RING - 2) * LOADS));
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    const int at = (kt % RING) * STAGE;
+    if constexpr (!CODES) {
+      if (now_kt == P.ktiles - 1 && last_left < 8) {
+        for (int q = tid; q < (BM + BN) * 8; q += NT)
+          if (((q & 7) ^ (q >> 3 & 7)) >= last_left) *reinterpret_cast<u32x4 *>(dense_lds + at + q * 16) = (u32x4)0u;
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_waitcnt(tile_wait(63));
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+      }
+      if (++now_kt == P.ktiles) now_kt = 0;
+    }
+    constexpr int AHEAD = TM >= 4 ? 3 : 1;             // rows of blocks read ahead, not all of them: registers
+    auto piece_a = [&](int i, int h) RSVD_INLINE { return *reinterpret_cast<const u32x4 *>(a_lds + at + i * 2048 + (((4 * h + kq) ^ swz) << 4)); };
+    auto piece_b = [&](int j, int h) RSVD_INLINE { return *reinterpret_cast<const u32x4 *>(b_lds + at + j * 2048 + (((4 * h + kq) ^ swz) << 4)); };
+    auto load_next = [&](int step) RSVD_INLINE {
+#pragma unroll
+      for (int l = 0; l < LOADS; ++l)
+        if (l * TM / LOADS == step) issue(kt + RING - 1, l);
+    };
+    if constexpr (CODES) {
+      if ((kt & 3) == 0) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) pa[0][i] = pa[1][i];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) pb[0][j] = pb[1][j];
+        fetch_powers(kt + 4);
+      } else {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) pa[0][i] >>= 8;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) pb[0][j] >>= 8;
+      }
+    }
+    if constexpr (KIND == DK_F8) {
+      u32x4 a[AHEAD + 1][2], b[TN][2];
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) b[j][h] = piece_b(j, h);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) a[i][h] = piece_a(i, h);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int step = 0; step < TM; ++step) {
+        if (step + AHEAD < TM)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) a[(step + AHEAD) % (AHEAD + 1)][h] = piece_a(step + AHEAD, h);
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          acc[step][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_both(b[j]), f8_both(a[step % (AHEAD + 1)]), acc[step][j], 0, 0, 0, (int)pb[0][j], 0, (int)pa[0][step]);
+        load_next(step);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else if constexpr (KIND == DK_F8_EXACT) {
+      float ua[TM], ub[TN];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) ua[i] = f8_unit(pa[0][i] & 255u);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) ub[j] = f8_unit(pb[0][j] & 255u);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 b[TN][2];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) f8_widen(piece_b(j, h), ub[j], b[j]);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          u32x4 a[2];
+          f8_widen(piece_a(i, h), ua[i], a);
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(b[j][q], a[q], acc[i][j]);
+          if (h == 0) load_next(i);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    } else {
+      u32x4 a[AHEAD + 1], b[2][TN];
+#pragma unroll
+      for (int j = 0; j < TN; ++j) b[0][j] = piece_b(j, 0);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) a[i] = piece_a(i, 0);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int step = 0; step < 2 * TM; ++step) {
+        const int h = step / TM, i = step % TM;
+        if (step + AHEAD < 2 * TM) a[(step + AHEAD) % (AHEAD + 1)] = piece_a((step + AHEAD) % TM, (step + AHEAD) / TM);
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          if (h == 0 && i == j * TM / TN) b[1][j] = piece_b(j, 1);
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          acc[i][j] = KIND == DK_BF16 ? mfma_bf16(b[h][j], a[step % (AHEAD + 1)], acc[i][j]) : mfma_f16(b[h][j], a[step % (AHEAD + 1)], acc[i][j]);
+        load_next(step);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+    advance();
+  }
+
+  __builtin_amdgcn_s_waitcnt(tile_wait(0));            // (nothing may land in LDS any more)
+  __syncthreads();
+  int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
+  asm volatile("" : "+v"(last_lane));
+  dense_finish<GATED, TM, TN>(P, acc, split, batch, m0 + wm0, n0 + (GATED ? wn0 / 2 : wn0), P.symmetric && tile_m != tile_n, last_lane,
+                                         reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
+}
+
+template <int KIND, bool GATED, int BM, int BN, int WGM, int WGN> hipError_t dense_nt_run(hipStream_t s, const DenseParams &P) {
+  hipLaunchKernelGGL((dense_nt_kernel<KIND, GATED, BM, BN, WGM, WGN>), dim3(dense_groups(P)), dim3(64 * WGM * WGN), (DenseNtCfg<BM, BN>::lds), s, P);
+  return hipGetLastError();
+}
+template <int KIND, bool GATED> hipError_t dense_nt_tile(hipStream_t s, const DenseParams &P, int b) {
+  if (b == 256) return dense_nt_run<KIND, GATED, 256, 256, 2, 2>(s, P);
+  if (b == 128) return dense_nt_run<KIND, GATED, 128, 128, 2, 2>(s, P);
+  return dense_nt_run<KIND, GATED, 64, 64, 2, 2>(s, P);
+}
+template <int KIND, bool GATED> hipError_t dense_nt_init() {
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, 256, 256, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)DenseNtCfg<256, 256>::lds);
+}
+#define DENSE_NT(KIND, GATED)                                                                        \
+  template hipError_t dense_nt_tile<KIND, GATED>(hipStream_t s, const DenseParams &P, int b);       \
+  template hipError_t dense_nt_init<KIND, GATED>();
+
+}  // namespace rsvd

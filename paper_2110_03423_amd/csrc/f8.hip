@@ -1,0 +1,311 @@
+// 8-bit floats (e4m3) in blocks of 128 that share a power of two: rounding to them, and the product of a few tokens.
+//
+// With a = max |x| of a block, its power 2^e is the least with a <= 448 2^e (448 is the largest code), e at least -126; held as the byte e + 127.  With a = 1.f 2^E
+// that is E - 8, and one more where 1.f > 1.75: read off the bits.  x 2^-e is exact, the rounding to a code (nearest, ties to even) is the conversion instruction's.
+// A block with an infinity or NaN has the byte 255 and codes that are NaN.
+#include "dense_nt.hpp"
+
+namespace rsvd {
+
+__device__ __forceinline__ unsigned f8_magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+// The power byte of a block whose largest magnitude has these bits, and the factor for its numbers.
+__device__ __forceinline__ unsigned f8_power(unsigned top) {
+  const unsigned expo = top >> 23, more = (top & 0x7fffffu) > 0x600000u ? 1u : 0u;
+  if (expo == 255u) return 255u;
+  return expo + more > 9u ? expo + more - 8u : 1u;
+}
+__device__ __forceinline__ float f8_factor(unsigned power) { return power == 255u ? __uint_as_float(0x7fc00000u) : __uint_as_float((254u - power) << 23); }
+// Four codes.  (A NaN: what the conversion makes of one.)
+__device__ __forceinline__ unsigned f8_codes4(float a, float b, float c, float d, float by) {
+  const int low = __builtin_amdgcn_cvt_pk_fp8_f32(a * by, b * by, 0, false);
+  return (unsigned)__builtin_amdgcn_cvt_pk_fp8_f32(c * by, d * by, low, true);
+}
+__device__ __forceinline__ u32x2 f8_codes8(const float (&v)[8], float by) { return u32x2{f8_codes4(v[0], v[1], v[2], v[3], by), f8_codes4(v[4], v[5], v[6], v[7], by)}; }
+__device__ __forceinline__ unsigned f8_top8(const float (&v)[8], unsigned top) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) top = max(top, f8_magnitude(v[e]));
+  return top;
+}
+template <int XT> __device__ __forceinline__ void x_values(const Raw8<XT> &r, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (XT == RSVD_X_F32) v[e] = __uint_as_float(r.w[e >> 2][e & 3]);
+    else if constexpr (XT == RSVD_X_BF16) v[e] = e & 1 ? bf16_high(r.w[0][e >> 1]) : bf16_low(r.w[0][e >> 1]);
+    else {
+      const unsigned pair = r.w[0][e >> 1];
+      v[e] = (float)__builtin_bit_cast(f16x2, pair)[e & 1];
+    }
+  }
+}
+// (As integers the magnitudes' bits are ordered like them, infinity and NaN on top.)
+__device__ __forceinline__ unsigned f8_shared(unsigned top, int mask) { return max(top, (unsigned)__shfl_xor((int)top, mask)); }
+
+// Blocks of a row: eight lanes a block, sixteen numbers each.  Memory is the bound.
+template <int XT> __global__ __launch_bounds__(256) void f8_rows_kernel(const char *X, int64_t ldx, int64_t rows, int64_t n, uint8_t *codes, int64_t width,
+                                                                       uint8_t *powers, int64_t ldp) {
+  constexpr int SIZE = XTraits<XT>::SIZE;
+  const int64_t per_row = width / 16, total = rows * per_row, step = (int64_t)gridDim.x * 256;
+  // (whole blocks end together: eight lanes have one)
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += step) {
+    const int64_t r = e / per_row, c = (e - r * per_row) * 16;
+    float v[2][8];
+    unsigned top = 0u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      x_load8<XT>(X + (r * ldx + c + 8 * h) * SIZE, n - c - 8 * h, v[h]);
+      top = f8_top8(v[h], top);
+    }
+#pragma unroll
+    for (int d = 1; d < 8; d <<= 1) top = f8_shared(top, d);
+    const unsigned power = f8_power(top);
+    const float by = f8_factor(power);
+    const u32x2 a = f8_codes8(v[0], by), b = f8_codes8(v[1], by);
+    *reinterpret_cast<u32x4 *>(codes + r * width + c) = u32x4{a[0], a[1], b[0], b[1]};
+    if ((threadIdx.x & 7) == 0) powers[r * ldp + c / 128] = (uint8_t)power;
+  }
+}
+
+// Blocks of 128 rows, 64 columns a workgroup: through LDS, a column a thread and then a row of codes.
+template <int XT> __global__ __launch_bounds__(256) void f8_columns_kernel(const char *X, int64_t ldx, int64_t rows, int64_t n, uint8_t *codes, int64_t width,
+                                                                          uint8_t *powers, int64_t ldp) {
+  constexpr int SIZE = XTraits<XT>::SIZE, PITCH = 65, OUT = 144;
+  __shared__ __attribute__((aligned(16))) float tile[128 * PITCH];
+  __shared__ unsigned tops[4][64];
+  const int tid = threadIdx.x, c = tid & 63, q = tid >> 6;
+  const int64_t r0 = (int64_t)blockIdx.y * 128, c0 = (int64_t)blockIdx.x * 64;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int row = (tid >> 3) + 32 * p, col = 8 * (tid & 7);
+    float v[8];
+    x_load8<XT>(X + ((r0 + row) * ldx + c0 + col) * SIZE, r0 + row < rows ? n - c0 - col : 0, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) tile[row * PITCH + col + e] = v[e];
+  }
+  __syncthreads();
+  float v[4][8];
+  unsigned top = 0u;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[p][e] = tile[(32 * q + 8 * p + e) * PITCH + c];
+    top = f8_top8(v[p], top);
+  }
+  tops[q][c] = top;
+  __syncthreads();
+  top = max(max(tops[0][c], tops[1][c]), max(tops[2][c], tops[3][c]));
+  const unsigned power = f8_power(top);
+  const float by = f8_factor(power);
+  if (q == 0 && c0 + c < n) powers[(c0 + c) * ldp + blockIdx.y] = (uint8_t)power;
+  char *const out = reinterpret_cast<char *>(tile);      // (everybody has read the tile)
+#pragma unroll
+  for (int p = 0; p < 4; p += 2) {
+    const u32x2 a = f8_codes8(v[p], by), b = f8_codes8(v[p + 1], by);
+    *reinterpret_cast<u32x4 *>(out + c * OUT + 32 * q + 8 * p) = u32x4{a[0], a[1], b[0], b[1]};
+  }
+  __syncthreads();
+#pragma unroll
+  for (int p = 0; p < 2; ++p) {
+    const int row = (tid >> 3) + 32 * p, at = 16 * (tid & 7);
+    if (c0 + row < n) *reinterpret_cast<u32x4 *>(codes + (c0 + row) * width + r0 + at) = *reinterpret_cast<const u32x4 *>(out + row * OUT + at);
+  }
+}
+
+// Blocks of 128 x 128, one a workgroup, in both orders.
+template <int XT> __global__ __launch_bounds__(256) void f8_weight_kernel(const char *W, int64_t ldw, int64_t m, int64_t n, uint8_t *codes, int64_t ldq, uint8_t *powers,
+                                                                         int64_t ldp, uint8_t *codes_t, int64_t ldqt, uint8_t *powers_t, int64_t ldpt) {
+  constexpr int SIZE = XTraits<XT>::SIZE, PITCH = 132;
+  __shared__ __attribute__((aligned(16))) uint8_t tile[128 * PITCH];
+  __shared__ unsigned tops[4];
+  const int tid = threadIdx.x, line = tid >> 1, half = (tid & 1) * 64;
+  const int64_t r0 = (int64_t)blockIdx.y * 128, c0 = (int64_t)blockIdx.x * 128;
+  float v[8][8];
+  unsigned top = 0u;
+#pragma unroll
+  for (int p = 0; p < 8; ++p) {
+    x_load8<XT>(W + ((r0 + line) * ldw + c0 + half + 8 * p) * SIZE, r0 + line < m ? n - c0 - half - 8 * p : 0, v[p]);
+    top = f8_top8(v[p], top);
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = f8_shared(top, d);
+  if ((tid & 63) == 0) tops[tid >> 6] = top;
+  __syncthreads();
+  top = max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+  const unsigned power = f8_power(top);
+  const float by = f8_factor(power);
+  if (tid == 0) {
+    powers[blockIdx.y * ldp + blockIdx.x] = (uint8_t)power;
+    if (powers_t != nullptr) powers_t[blockIdx.x * ldpt + blockIdx.y] = (uint8_t)power;
+  }
+#pragma unroll
+  for (int p = 0; p < 8; p += 2) {
+    const u32x2 a = f8_codes8(v[p], by), b = f8_codes8(v[p + 1], by);
+    if (r0 + line < m) *reinterpret_cast<u32x4 *>(codes + (r0 + line) * ldq + c0 + half + 8 * p) = u32x4{a[0], a[1], b[0], b[1]};
+    unsigned *to = reinterpret_cast<unsigned *>(tile + line * PITCH + half + 8 * p);
+    to[0] = a[0]; to[1] = a[1]; to[2] = b[0]; to[3] = b[1];
+  }
+  if (codes_t == nullptr) return;
+  __syncthreads();
+  if (c0 + line >= n) return;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    u32x4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint8_t *from = tile + (half + 16 * p + 4 * e) * PITCH + line;
+      w[e] = (unsigned)from[0] | (unsigned)from[PITCH] << 8 | (unsigned)from[2 * PITCH] << 16 | (unsigned)from[3 * PITCH] << 24;
+    }
+    *reinterpret_cast<u32x4 *>(codes_t + (c0 + line) * ldqt + r0 + half + 16 * p) = w;
+  }
+}
+
+hipError_t f8_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint8_t *codes, int64_t width, uint8_t *powers,
+                          int64_t ldp) {
+  int64_t groups = ceil_div(rows * (width / 16), 256);
+  if (groups > 65536) groups = 65536;
+  const dim3 grid((unsigned)groups);
+  const char *x = (const char *)X;
+  if (type == RSVD_X_BF16) hipLaunchKernelGGL((f8_rows_kernel<RSVD_X_BF16>), grid, dim3(256), 0, s, x, ldx, rows, n, codes, width, powers, ldp);
+  else if (type == RSVD_X_F16) hipLaunchKernelGGL((f8_rows_kernel<RSVD_X_F16>), grid, dim3(256), 0, s, x, ldx, rows, n, codes, width, powers, ldp);
+  else hipLaunchKernelGGL((f8_rows_kernel<RSVD_X_F32>), grid, dim3(256), 0, s, x, ldx, rows, n, codes, width, powers, ldp);
+  return hipGetLastError();
+}
+
+hipError_t f8_columns_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint8_t *codes, int64_t width, uint8_t *powers,
+                             int64_t ldp) {
+  const dim3 grid((unsigned)ceil_div(n, 64), (unsigned)ceil_div(rows, 128));
+  const char *x = (const char *)X;
+  if (type == RSVD_X_BF16) hipLaunchKernelGGL((f8_columns_kernel<RSVD_X_BF16>), grid, dim3(256), 0, s, x, ldx, rows, n, codes, width, powers, ldp);
+  else if (type == RSVD_X_F16) hipLaunchKernelGGL((f8_columns_kernel<RSVD_X_F16>), grid, dim3(256), 0, s, x, ldx, rows, n, codes, width, powers, ldp);
+  else hipLaunchKernelGGL((f8_columns_kernel<RSVD_X_F32>), grid, dim3(256), 0, s, x, ldx, rows, n, codes, width, powers, ldp);
+  return hipGetLastError();
+}
+
+hipError_t f8_weight_launch(hipStream_t s, rsvd_xtype type, int64_t m, int64_t n, const void *W, int64_t ldw, uint8_t *codes, int64_t ldq, uint8_t *powers, int64_t ldp,
+                            uint8_t *codes_t, int64_t ldqt, uint8_t *powers_t, int64_t ldpt) {
+  const dim3 grid((unsigned)ceil_div(n, 128), (unsigned)ceil_div(m, 128));
+  const char *w = (const char *)W;
+#define WEIGHT(XT) hipLaunchKernelGGL((f8_weight_kernel<XT>), grid, dim3(256), 0, s, w, ldw, m, n, codes, ldq, powers, ldp, codes_t, ldqt, powers_t, ldpt)
+  if (type == RSVD_X_BF16) WEIGHT(RSVD_X_BF16);
+  else if (type == RSVD_X_F16) WEIGHT(RSVD_X_F16);
+  else WEIGHT(RSVD_X_F32);
+#undef WEIGHT
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- a few tokens
+// Memory is the bound: the weight passes once, sixteen rows a workgroup, straight from memory into the matrix instructions; the wavefronts take the steps of
+// 128 k in turn and add up at the end.  Every workgroup rounds the tokens again: a lane has 32 numbers of a token's block, and their codes are its operand as they are.
+struct F8FewParams {
+  const char *X; int64_t ldx, tokens, n, m;
+  const uint8_t *codes, *powers; int64_t ldq, ldp;
+  int steps;                       // of 128 k
+  void *Y; int64_t ldy;
+};
+
+template <int XT, int TB, int WAVES> __global__ __launch_bounds__(64 * WAVES) void f8_few_kernel(const F8FewParams P) {
+  constexpr int SIZE = XTraits<XT>::SIZE, U = TB == 1 ? (SIZE == 2 ? 4 : 2) : TB == 2 ? (SIZE == 2 ? 2 : 1) : 1;      // steps whose loads are issued together
+  __shared__ f32x4 part[WAVES][TB][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, kq = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t row = n0 + r16 < P.m ? n0 + r16 : P.m - 1;
+  const uint8_t *const w = P.codes + row * P.ldq + 32 * kq, *const powers = P.powers + (n0 >> 7) * P.ldp;
+  const char *x[TB];
+#pragma unroll
+  for (int i = 0; i < TB; ++i) {
+    const int64_t t = 16 * i + r16;
+    x[i] = P.X + (t < P.tokens ? t : P.tokens - 1) * P.ldx * SIZE;
+  }
+  f32x4 acc[TB];
+#pragma unroll
+  for (int i = 0; i < TB; ++i) acc[i] = (f32x4)0.f;
+  u32x4 b[U][2];
+  unsigned pb[U];
+  Raw8<XT> a[U][TB][4];
+  for (int s0 = wave; s0 < P.steps; s0 += WAVES * U) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + WAVES * u < P.steps ? s0 + WAVES * u : s0;      // (behind the last step: the first one again, its tokens zeros)
+      pb[u] = powers[s];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) b[u][h] = *reinterpret_cast<const u32x4 *>(w + (int64_t)128 * s + 16 * h);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = 128 * (int64_t)(s0 + WAVES * u) + 32 * kq;
+      const int64_t left = s0 + WAVES * u < P.steps ? P.n - k : 0;
+#pragma unroll
+      for (int i = 0; i < TB; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) a[u][i][q] = raw_load8<XT>(x[i] + (k + 8 * q) * SIZE, left - 8 * q);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s0 + WAVES * u >= P.steps) break;
+#pragma unroll
+      for (int i = 0; i < TB; ++i) {
+        float v[4][8];
+        unsigned top = 0u;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          x_values<XT>(a[u][i][q], v[q]);
+          top = f8_top8(v[q], top);
+        }
+        top = f8_shared(f8_shared(top, 16), 32);
+        const unsigned power = f8_power(top);
+        const float by = f8_factor(power);
+        u32x4 y[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const u32x2 c = f8_codes8(v[2 * h], by), d = f8_codes8(v[2 * h + 1], by);
+          y[h] = u32x4{c[0], c[1], d[0], d[1]};
+        }
+        if constexpr (XT == RSVD_X_F32) {
+          const float ub = f8_unit(pb[u]), ua = f8_unit(power);
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            u32x4 bw[2], aw[2];
+            f8_widen(b[u][h], ub, bw);
+            f8_widen(y[h], ua, aw);
+#pragma unroll
+            for (int z = 0; z < 2; ++z) acc[i] = mfma_bf16(bw[z], aw[z], acc[i]);
+          }
+        } else {
+          acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_both(b[u]), f8_both(y), acc[i], 0, 0, 0, (int)pb[u], 0, (int)power);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < TB; ++i) part[wave][i][lane] = acc[i];
+  __syncthreads();
+  if (wave >= TB) return;
+  f32x4 y = (f32x4)0.f;
+#pragma unroll
+  for (int v = 0; v < WAVES; ++v) y += part[v][wave][lane];
+  const int64_t t = 16 * wave + r16, n = n0 + 4 * kq;
+  if (t < P.tokens && n < P.m) put4<XT>(P.Y, t * P.ldy + n, left_of(n, P.m), y);
+}
+
+template <int XT> static void f8_few_run(hipStream_t s, const F8FewParams &P, dim3 grid, bool wide) {
+#define FEW(TB)                                                                     \
+  if (wide) hipLaunchKernelGGL((f8_few_kernel<XT, TB, 8>), grid, dim3(512), 0, s, P); \
+  else hipLaunchKernelGGL((f8_few_kernel<XT, TB, 4>), grid, dim3(256), 0, s, P)
+  if (P.tokens <= 16) { FEW(1); }
+  else if (P.tokens <= 32) { FEW(2); }
+  else { FEW(4); }
+#undef FEW
+}
+
+hipError_t f8_few_launch(rsvd_ctx *, hipStream_t s, const F8FewDesc &d) {
+  if (d.tokens < 1 || d.tokens > kF8Few) return hipErrorInvalidValue;
+  const F8FewParams P = {(const char *)d.X, d.ldx, d.tokens, d.n, d.m, d.codes, d.powers, d.ldq, d.ldp, (int)ceil_div(d.n, 128), d.Y, d.ldy};
+  const dim3 grid((unsigned)ceil_div(d.m, 16));
+  const bool wide = P.steps > 8;
+  if (d.type == RSVD_X_BF16) f8_few_run<RSVD_X_BF16>(s, P, grid, wide);
+  else if (d.type == RSVD_X_F16) f8_few_run<RSVD_X_F16>(s, P, grid, wide);
+  else f8_few_run<RSVD_X_F32>(s, P, grid, wide);
+  return hipGetLastError();
+}
+
+}  // namespace rsvd

@@ -1,0 +1,167 @@
+// A gated block beside its large products: a few tokens, gradients of kept products, operands in the order that the products want.
+#include "dense_tile.hpp"
+
+namespace rsvd {
+
+// ---------------------------------------------------------------- a few tokens
+// Memory is the bound: the weight passes once, sixteen outputs a workgroup (their rows of gate and of up), straight from memory into the matrix instructions;
+// the wavefronts take the steps of 32 k in turn and add up at the end.
+struct GatedFewParams {
+  const char *X, *W;
+  int64_t ldx, ldw, tokens, n, m;
+  int steps;                       // of 32 k
+  GatedOut out;
+};
+
+template <int XT> __device__ __forceinline__ f32x4 few_multiply(const Raw8<XT> &w, const Raw8<XT> &x, f32x4 acc) {
+  if constexpr (XT == RSVD_X_BF16) {
+    return mfma_bf16(w.w[0], x.w[0], acc);
+  } else if constexpr (XT == RSVD_X_F16) {
+    return mfma_f16(w.w[0], x.w[0], acc);
+  } else {                                             // (the products that dense_segs names)
+    u32x4 a[3], b[3];
+    split_operand<XT>(w, a);
+    split_operand<XT>(x, b);
+    acc = mfma_bf16(a[2], b[0], acc);
+    acc = mfma_bf16(a[1], b[1], acc);
+    acc = mfma_bf16(a[0], b[2], acc);
+    acc = mfma_bf16(a[1], b[0], acc);
+    acc = mfma_bf16(a[0], b[1], acc);
+    return mfma_bf16(a[0], b[0], acc);
+  }
+}
+
+// TB blocks of sixteen tokens, WAVES wavefronts.
+template <int XT, int TB, int WAVES> __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(const GatedFewParams P) {
+  constexpr int SIZE = XTraits<XT>::SIZE, U = TB == 1 ? (SIZE == 2 ? 8 : 4) : TB == 2 ? (SIZE == 2 ? 4 : 2) : 2;      // steps whose loads are issued together
+  __shared__ f32x4 part[WAVES][2][TB][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, kq = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t row = n0 + r16 < P.m ? n0 + r16 : P.m - 1;
+  const char *w[2] = {P.W + row * P.ldw * SIZE, P.W + (P.m + row) * P.ldw * SIZE}, *x[TB];
+#pragma unroll
+  for (int i = 0; i < TB; ++i) {
+    const int64_t t = 16 * i + r16;
+    x[i] = P.X + (t < P.tokens ? t : P.tokens - 1) * P.ldx * SIZE;
+  }
+  f32x4 acc[2][TB];
+#pragma unroll
+  for (int i = 0; i < TB; ++i) acc[0][i] = acc[1][i] = (f32x4)0.f;
+  Raw8<XT> a[U][2], b[U][TB];
+  auto load = [&](int s0) RSVD_INLINE {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t k = 32 * (int64_t)(s0 + WAVES * u) + 8 * kq, left = s0 + WAVES * u < P.steps ? P.n - k : 0;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) a[u][h] = raw_load8<XT>(w[h] + k * SIZE, left);
+#pragma unroll
+      for (int i = 0; i < TB; ++i) b[u][i] = raw_load8<XT>(x[i] + k * SIZE, left);
+    }
+  };
+  for (int s0 = wave; s0 < P.steps; s0 += WAVES * U) {
+    load(s0);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < TB; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) acc[h][i] = few_multiply<XT>(a[u][h], b[u][i], acc[h][i]);
+  }
+#pragma unroll
+  for (int i = 0; i < TB; ++i) {
+    part[wave][0][i][lane] = acc[0][i];
+    part[wave][1][i][lane] = acc[1][i];
+  }
+  __syncthreads();
+  if (wave >= TB) return;
+  f32x4 g = (f32x4)0.f, u = g;
+#pragma unroll
+  for (int v = 0; v < WAVES; ++v) {
+    g += part[v][0][wave][lane];
+    u += part[v][1][wave][lane];
+  }
+  const int64_t t = 16 * wave + r16, n = n0 + 4 * kq;
+  if (t < P.tokens && n < P.m) gated_end(P.out, P.m, t, n, g, u);
+}
+
+template <int XT> static void gated_few_run(hipStream_t s, const GatedFewParams &P, dim3 grid, bool wide) {
+#define FEW(TB)                                                                        \
+  if (wide) hipLaunchKernelGGL((gated_few_kernel<XT, TB, 8>), grid, dim3(512), 0, s, P); \
+  else hipLaunchKernelGGL((gated_few_kernel<XT, TB, 4>), grid, dim3(256), 0, s, P)
+  if (P.tokens <= 16) { FEW(1); }
+  else if (P.tokens <= 32) { FEW(2); }
+  else { FEW(4); }
+#undef FEW
+}
+
+hipError_t gated_few_launch(rsvd_ctx *, hipStream_t s, const GatedFewDesc &d) {
+  if (d.tokens < 1 || d.tokens > kGatedFew) return hipErrorInvalidValue;
+  const GatedFewParams P = {(const char *)d.X, (const char *)d.W, d.ldx, d.ldw, d.tokens, d.n, d.m, (int)ceil_div(d.n, 32), d.out};
+  const dim3 grid((unsigned)ceil_div(d.m, 16));
+  const bool wide = P.steps > 32;
+  if (d.type == RSVD_X_BF16) gated_few_run<RSVD_X_BF16>(s, P, grid, wide);
+  else if (d.type == RSVD_X_F16) gated_few_run<RSVD_X_F16>(s, P, grid, wide);
+  else gated_few_run<RSVD_X_F32>(s, P, grid, wide);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- gradients of gate and up from the kept products; memory is the bound
+__global__ __launch_bounds__(256) void gated_slope_kernel(const GatedOut O, int64_t tokens, int64_t m) {
+  const int64_t per_row = (m + 3) / 4, total = tokens * per_row;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
+    const int64_t t = e / per_row, n = (e - t * per_row) * 4;
+    const int left = left_of(n, m);
+    const f32x4 g = load4(O.type, O.kept, t * O.ldk + n, left), u = load4(O.type, O.kept, t * O.ldk + m + n, left);
+    slope_end(O, m, t, n, g, u);
+  }
+}
+hipError_t gated_slope_launch(hipStream_t s, int64_t tokens, int64_t m, const GatedOut &o) {
+  int64_t groups = ceil_div(tokens * ceil_div(m, 4), 256);
+  if (groups > 16384) groups = 16384;
+  hipLaunchKernelGGL(gated_slope_kernel, dim3((unsigned)groups), dim3(256), 0, s, o, tokens, m);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- operands
+template <int XT> __global__ __launch_bounds__(256) void planes_kernel(const char *X, int64_t ldx, int64_t rows, int64_t n, uint16_t *out, int64_t width, int64_t plane) {
+  constexpr int SIZE = XTraits<XT>::SIZE;
+  const int64_t per_row = width / 8, total = rows * per_row;
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
+    const int64_t r = e / per_row, c = (e - r * per_row) * 8;
+    const Raw8<XT> v = raw_load8<XT>(X + (r * ldx + c) * SIZE, n - c);
+    uint16_t *to = out + r * width + c;
+    if constexpr (XT == RSVD_X_F32) {
+      u32x4 p[3];
+      split_operand<XT>(v, p);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x4 *>(to + q * (plane / 2)) = p[q];
+    } else {
+      *reinterpret_cast<u32x4 *>(to) = v.w[0];
+    }
+  }
+}
+hipError_t planes_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint16_t *out, int64_t width, int64_t plane) {
+  int64_t groups = ceil_div(rows * (width / 8), 256);
+  if (groups > 16384) groups = 16384;
+  if (type == RSVD_X_F32)
+    hipLaunchKernelGGL((planes_kernel<RSVD_X_F32>), dim3((unsigned)groups), dim3(256), 0, s, (const char *)X, ldx, rows, n, out, width, plane);
+  else
+    hipLaunchKernelGGL((planes_kernel<RSVD_X_F16>), dim3((unsigned)groups), dim3(256), 0, s, (const char *)X, ldx, rows, n, out, width, plane);
+  return hipGetLastError();
+}
+
+
+// ---------------------------------------------------------------- the gradient of no tokens
+template <typename T> __global__ __launch_bounds__(256) void zero_kernel(T *C, int64_t ldc, int64_t rows, int64_t n) {
+  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < rows * n; e += (int64_t)gridDim.x * 256) C[e / n * ldc + e % n] = 0;
+}
+hipError_t zero_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, void *C, int64_t ldc) {
+  int64_t groups = ceil_div(rows * n, 256);
+  if (groups > 16384) groups = 16384;
+  if (type == RSVD_X_F32) hipLaunchKernelGGL((zero_kernel<uint32_t>), dim3((unsigned)groups), dim3(256), 0, s, (uint32_t *)C, ldc, rows, n);
+  else hipLaunchKernelGGL((zero_kernel<uint16_t>), dim3((unsigned)groups), dim3(256), 0, s, (uint16_t *)C, ldc, rows, n);
+  return hipGetLastError();
+}
+
+}  // namespace rsvd

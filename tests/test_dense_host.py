@@ -1,0 +1,134 @@
+"""Argument checks and workspace sizes of the gated block, of products in 8-bit floats and of orthogonalised updates, on a planning context: no GPU.  The fake device
+pointers are never dereferenced."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2110_03423_amd import binding
+from paper_2110_03423_amd.binding import ERR_NO_DEVICE, X_BF16, X_F16, X_F32
+
+UNSUPPORTED = 4
+PTR = C.c_void_p(1 << 20)
+ODD = C.c_void_p((1 << 20) + 1)
+HALF = C.c_void_p((1 << 20) + 2)
+NULL = C.c_void_p(0)
+
+
+@pytest.fixture(scope="module")
+def plan():
+    import os
+    if not os.path.exists(binding.library_path()):
+        from paper_2110_03423_amd import build
+        build.build_library()
+    return binding.Rsvd(device=None)
+
+
+def caller(plan, name, order, **base):
+    order = order.split()
+    return lambda **kw: getattr(plan.lib, name)(*[dict(base, **kw)[k] for k in order])
+
+
+def bytes_of(plan, name, *args):
+    need = C.c_size_t()
+    assert getattr(plan.lib, name)(plan.h, *args, C.byref(need)) == 0
+    return need.value
+
+
+def test_gated_product_checks_every_argument(plan):
+    call = caller(plan, "rsvd_gated_product", "ctx stream type act tokens n m X ldx W ldw H ldh kept ldk ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, act=0,
+                  tokens=100, n=72, m=50, X=PTR, ldx=72, W=PTR, ldw=72, H=PTR, ldh=50, kept=PTR, ldk=100, ws=PTR, bytes=1 << 40)
+    assert call() == ERR_NO_DEVICE and call(tokens=0, X=NULL) == 0
+    assert call(ctx=None) == -1 and call(type=3) == -3 and call(act=4) == -4 and call(act=-1) == -4 and call(tokens=-1) == -5
+    assert call(n=0) == -6 and call(m=0) == -7 and call(X=NULL) == -8 and call(X=ODD) == -8 and call(type=X_F32, X=HALF) == -8
+    assert call(ldx=71) == -9 and call(W=NULL) == -10 and call(W=ODD) == -10 and call(ldw=71) == -11 and call(H=NULL) == -12 and call(ldh=49) == -13
+    assert call(kept=ODD) == -14 and call(ldk=99) == -15 and call(kept=NULL, ldk=0) == ERR_NO_DEVICE
+    assert call(ws=NULL, bytes=0, tokens=64) == ERR_NO_DEVICE
+    # a matrix that does not lie as the products read it needs room
+    both, neither = (bytes_of(plan, "rsvd_gated_product_bytes", X_BF16, 100, 72, 50, lie) for lie in (3, 0))
+    assert neither >= both + 2 * 72 * (100 + 100)
+    assert call(bytes=both) == ERR_NO_DEVICE and (both == 0 or call(bytes=both - 1) == -17)
+    assert call(X=HALF, ldx=73, W=HALF, bytes=neither) == ERR_NO_DEVICE and call(X=HALF, W=HALF, bytes=neither - 1) == -17
+    assert call(X=HALF, W=HALF, ws=NULL) == -16 and call(X=HALF, W=HALF, ws=C.c_void_p((1 << 20) + 128)) == -16
+    assert bytes_of(plan, "rsvd_gated_product_bytes", X_F32, 100, 72, 50, 3) >= 6 * 72 * 200
+    assert call(n=131073, ldx=131073, ldw=131073) == UNSUPPORTED and call(tokens=(1 << 22) + 1) == UNSUPPORTED
+    assert call(tokens=1 << 22, m=8192, ldh=8192, ldk=16384) == UNSUPPORTED
+
+
+def test_gated_gradient_checks_every_argument(plan):
+    call = caller(plan, "rsvd_gated_product_grad", "ctx stream type act tokens n m dH lddh X ldx W ldw kept ldk dX lddx dW lddw f32 acc ws bytes", ctx=plan.h, stream=NULL,
+                  type=X_F16, act=1, tokens=100, n=72, m=50, dH=PTR, lddh=50, X=PTR, ldx=72, W=PTR, ldw=72, kept=PTR, ldk=100, dX=PTR, lddx=72, dW=PTR, lddw=72,
+                  f32=0, acc=0, ws=PTR, bytes=1 << 40)
+    assert call() == ERR_NO_DEVICE
+    assert call(ctx=None) == -1 and call(type=7) == -3 and call(act=9) == -4 and call(tokens=-1) == -5 and call(n=0) == -6 and call(m=0) == -7
+    assert call(dH=NULL) == -8 and call(lddh=49) == -9 and call(X=NULL) == -10 and call(X=ODD) == -10 and call(ldx=71) == -11
+    assert call(W=NULL) == -12 and call(ldw=71) == -13 and call(kept=ODD) == -14 and call(ldk=99) == -15 and call(dX=ODD) == -16 and call(lddx=71) == -17
+    assert call(dW=ODD) == -18 and call(dW=HALF, f32=1) == -18 and call(lddw=71) == -19 and call(acc=1) == -21 and call(acc=1, f32=1) == ERR_NO_DEVICE
+    assert call(ws=NULL) == -22 and call(bytes=0) == -23
+    # what is not wanted need not be there
+    assert call(dW=NULL, X=NULL) == ERR_NO_DEVICE and call(dX=NULL, W=NULL) == ERR_NO_DEVICE
+    assert call(dW=NULL, X=NULL, kept=NULL) == -10 and call(dX=NULL, W=NULL, kept=NULL) == -12
+    assert call(tokens=0, dH=NULL, X=NULL, dX=NULL) == ERR_NO_DEVICE       # (zeros are written)
+    for lie in range(8):
+        need = bytes_of(plan, "rsvd_gated_product_grad_bytes", X_F16, 100, 72, 50, lie)
+        args = dict(X=PTR if lie & 1 else HALF, W=PTR if lie & 2 else HALF, kept=PTR if lie & 4 else NULL)
+        assert call(bytes=need, **args) == ERR_NO_DEVICE and call(bytes=need - 1, **args) == -23
+
+
+def test_f8_checks_every_argument(plan):
+    call = caller(plan, "rsvd_f8_weight", "ctx stream type m n W ldw q ldq p ldp qt ldqt pt ldpt", ctx=plan.h, stream=NULL, type=X_F32, m=130, n=70, W=PTR, ldw=70,
+                  q=PTR, ldq=128, p=PTR, ldp=4, qt=PTR, ldqt=256, pt=PTR, ldpt=4)
+    assert call() == ERR_NO_DEVICE and call(qt=NULL, pt=NULL, ldqt=0, ldpt=0) == ERR_NO_DEVICE
+    assert call(ctx=None) == -1 and call(type=3) == -3 and call(m=0) == -4 and call(n=0) == -5 and call(W=HALF) == -6 and call(ldw=69) == -7
+    assert call(q=HALF) == -8 and call(ldq=112) == -9 and call(ldq=130) == -9 and call(p=HALF) == -10 and call(ldp=1) == -11 and call(ldp=6) == -11
+    assert call(qt=HALF) == -12 and call(ldqt=128) == -13 and call(pt=NULL) == -14 and call(ldpt=2) == -15
+    for name, n, m in (("rsvd_f8_product", 200, 50), ("rsvd_f8_product_grad", 50, 200)):
+        call = caller(plan, name, "ctx stream type tokens n m X ldx q ldq p ldp Y ldy ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, tokens=100, n=n, m=m, X=PTR,
+                      ldx=200, q=PTR, ldq=256, p=PTR, ldp=4, Y=PTR, ldy=50, ws=PTR, bytes=1 << 40)
+        assert call() == ERR_NO_DEVICE and call(tokens=0, X=NULL) == 0
+        assert call(ctx=None) == -1 and call(type=5) == -3 and call(tokens=-2) == -4 and call(n=0) == -5 and call(m=0) == -6
+        assert call(X=ODD) == -7 and call(ldx=199) == -8 and call(q=HALF) == -9 and call(ldq=240) == -10 and call(ldq=264) == -10
+        assert call(p=ODD) == -11 and call(ldp=1) == -12 and call(ldp=5) == -12 and call(Y=NULL) == -13 and call(ldy=49) == -14
+        need = bytes_of(plan, name + "_bytes", X_BF16, 100, n, m)
+        assert need > 0 and call(ws=NULL) == -15 and call(bytes=need - 1) == -16 and call(bytes=need) == ERR_NO_DEVICE
+        assert bytes_of(plan, name + "_bytes", X_BF16, 64, n, m) == 0 and call(tokens=64, ws=NULL, bytes=0) == ERR_NO_DEVICE
+        assert call(ldq=(1 << 23) + 16) == UNSUPPORTED
+    call = caller(plan, "rsvd_f8_weight_grad", "ctx stream type tokens n m dY lddy X ldx dW lddw f32 acc ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, tokens=100,
+                  n=70, m=50, dY=PTR, lddy=50, X=PTR, ldx=70, dW=PTR, lddw=70, f32=0, acc=0, ws=PTR, bytes=1 << 40)
+    assert call() == ERR_NO_DEVICE and call(tokens=0, dY=NULL, X=NULL) == ERR_NO_DEVICE
+    assert call(type=3) == -3 and call(tokens=-1) == -4 and call(n=0) == -5 and call(m=0) == -6 and call(dY=NULL) == -7 and call(lddy=49) == -8
+    assert call(X=NULL) == -9 and call(ldx=69) == -10 and call(dW=NULL) == -11 and call(f32=1, dW=HALF) == -11 and call(lddw=69) == -12
+    assert call(acc=1) == -14 and call(acc=1, f32=1) == ERR_NO_DEVICE and call(ws=NULL) == -15
+    need = bytes_of(plan, "rsvd_f8_weight_grad_bytes", X_BF16, 100, 70, 50, 0)
+    assert call(bytes=need) == ERR_NO_DEVICE and call(bytes=need - 1) == -16
+
+
+def test_orthogonalize_checks_every_argument(plan):
+    coef = (C.c_float * 6)(3.4445, -4.775, 2.0315, 1.5, -0.5, 0.0)
+    call = caller(plan, "rsvd_orthogonalize", "ctx stream type batch m n G ldg sg steps coef O ldo so ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, batch=3, m=50,
+                  n=70, G=PTR, ldg=70, sg=3500, steps=2, coef=coef, O=PTR, ldo=70, so=3500, ws=PTR, bytes=1 << 40)
+    assert call() == ERR_NO_DEVICE and call(batch=0, G=NULL) == 0 and call(sg=0) == ERR_NO_DEVICE
+    assert call(ctx=None) == -1 and call(type=3) == -3 and call(batch=-1) == -4 and call(m=0) == -5 and call(n=0) == -6 and call(G=ODD) == -7
+    assert call(ldg=69) == -8 and call(sg=-1) == -9 and call(steps=0) == -10 and call(steps=65) == -10 and call(coef=None) == -11 and call(O=NULL) == -12
+    assert call(ldo=69) == -13 and call(so=3499) == -14 and call(ws=NULL) == -15
+    need = bytes_of(plan, "rsvd_orthogonalize_bytes", X_BF16, 3, 50, 70)
+    assert call(bytes=need) == ERR_NO_DEVICE and call(bytes=need - 1) == -16
+    for bad in ((4.0, 0.0, 0.0), (3.4445, -4.775, 4.5), (float("nan"), 0.0, 0.0), (1.0, float("inf"), 0.0), (1.0, -9.0, 0.5)):
+        assert call(steps=1, coef=(C.c_float * 3)(*bad)) == UNSUPPORTED
+    assert call(batch=65536) == UNSUPPORTED and call(m=131073, so=1 << 40) == UNSUPPORTED
+
+
+def test_a_weight_of_8_bit_floats_is_checked_and_laid_out():
+    from paper_2110_03423_amd import WeightF8
+    codes = torch.arange(130 * 70).remainder(126).to(torch.uint8).view(130, 70).view(torch.float8_e4m3fn)
+    powers = torch.tensor([[120], [130]], dtype=torch.uint8)
+    w = WeightF8(codes, powers)
+    assert torch.equal(w.codes.view(torch.uint8), codes.view(torch.uint8)) and torch.equal(w.powers, powers) and (w.m, w.n) == (130, 70)
+    (q, p), (qt, pt) = w._forward, w._backward
+    assert q.shape == (130, 128) and not q[:, 70:].any() and qt.shape == (70, 256) and not qt[:, 130:].any()
+    assert torch.equal(qt[:, :130], codes.view(torch.uint8).t()) and p.shape == (2, 4) and pt.shape == (1, 4) and pt[0, :2].tolist() == [120, 130]
+    assert WeightF8(codes, powers, backward=False)._backward is None
+    for error, args in ((TypeError, (codes.view(torch.uint8), powers)), (TypeError, (codes[0], powers)), (ValueError, (codes, powers.int())), (ValueError, (codes, powers[:1])),
+                        (ValueError, (codes[:0], powers[:0]))):
+        with pytest.raises(error):
+            WeightF8(*args)

@@ -1,0 +1,180 @@
+"""Updates made orthogonal, against the definition in 64 bits.
+
+Exact: matrices of few entries +-1 with 4^k of them in all have the norm 2^k, and one step with coefficients that are short binary fractions is a short binary fraction in every
+element, so that results are equal to the rounded definition.
+
+Tolerances of iterations.  An iterate, its square and the polynomial are held in fp16 (bf16 results; 2^-11 of each element) or in two fp16 numbers (2^-22), beside fp32 sums
+whose error is below that.  The model rounds in the same places in 64-bit arithmetic; two computations that round there and differ in the last bits of their sums
+are each as far from the definition, so they differ by no more than the sum of both; twice that and the output's rounding is allowed, as a 2-norm.
+"""
+import math
+
+import pytest
+import torch
+
+from gpu_util import ctx, say
+from test_gpu_gated import rounded
+from test_gpu_layer8 import BF16, F16, F32, TYPES, UNIT, gen
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+STEP = (3.4445, -4.7750, 2.0315)
+
+
+def definition(G, steps, coef, hold=lambda v: v):
+    X = G.double()
+    norm = torch.linalg.matrix_norm(X)
+    X = hold(torch.where(norm > 0, X / norm, 0.0))
+    wide = X.shape[0] <= X.shape[1]
+    for s in range(steps):
+        a, b, c = [float(torch.tensor(v, dtype=F32)) for v in coef[s]]
+        A = hold(X @ X.t() if wide else X.t() @ X)
+        B = hold(b * A + c * (A @ A))
+        X = a * X + (B @ X if wide else X @ B)
+        if s + 1 < steps:
+            X = hold(X)
+    return X
+
+
+def held(v, planes):
+    v = v * 8192.0
+    high = v.to(F32).to(F16).double()
+    return (high if planes == 1 else high + (v - high).to(F32).to(F16).double()) / 8192.0
+
+
+def iterated(g, steps=5, coef=None, got=None):
+    coef = coef or [STEP] * steps
+    got = ctx().rsvd_orthogonalize(g, steps, coef) if got is None else got
+    assert got.dtype == g.dtype and got.shape == g.shape
+    want = definition(g, steps, coef)
+    planes = 1 if g.dtype == BF16 else 2
+    model = definition(g, steps, coef, lambda v: held(v, planes))
+    lost, norm = torch.linalg.matrix_norm(model - want), torch.linalg.matrix_norm(want)
+    # (sums of up to n terms in fp32 in every product, where two fp16 numbers hold more than those)
+    sums = 0.0 if planes == 1 else 2.0 ** -24 * math.sqrt(max(g.shape)) * 16 * norm
+    off = torch.linalg.matrix_norm(got.double() - want)
+    assert float(off) <= float(4 * lost + sums + UNIT[g.dtype] * norm), (tuple(g.shape), float(off / norm), float(lost / norm))
+    return got
+
+
+def momentum(g, m, n, dtype):
+    k = max(1, min(m, n) // 4)
+    low = (torch.randn(m, k, device=DEV, generator=g) * torch.arange(1, k + 1, device=DEV) ** -0.5) @ torch.randn(k, n, device=DEV, generator=g)
+    return (1e-3 * (low / low.square().mean().sqrt() + 0.5 * torch.randn(m, n, device=DEV, generator=g))).to(dtype)
+
+
+SIZES = [(1, 1), (1, 40), (40, 1), (2, 3), (7, 5), (64, 64), (65, 130), (130, 65), (128, 500), (777, 333), (256, 2048), (1500, 257), (1024, 1024)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n", SIZES)
+def test_five_steps(dtype, m, n):
+    say("orthogonalize", dtype, m, n)
+    got = iterated(momentum(gen(m + n), m, n, TYPES[dtype]))
+    s = torch.linalg.svdvals(got.double())
+    assert float(s.max()) < 1.3
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n", [(64, 200), (300, 70)])
+def test_other_coefficients_and_steps(dtype, m, n):
+    g = momentum(gen(m), m, n, TYPES[dtype])
+    for coef in ([(1.5, -0.5, 0.0)], [(1.875, -1.25, 0.375)] * 8, [(3.4445, -4.775, 2.0315), (2.5, -2.0, 0.6), (1.875, -1.25, 0.375)]):
+        iterated(g, len(coef), coef)
+    a = ctx().rsvd_orthogonalize(g, 3, STEP)
+    assert torch.equal(a, ctx().rsvd_orthogonalize(g, 3, [STEP] * 3)) and torch.equal(ctx().rsvd_orthogonalize(g), ctx().rsvd_orthogonalize(g, 5, STEP))
+
+
+def sparse(g, m, n, entries, dtype):
+    """+-1 in 4^k places, columns and rows spread over all."""
+    at = torch.randperm(m * n, device=DEV, generator=g)[:entries]
+    out = torch.zeros(m * n, device=DEV)
+    out[at] = torch.where(torch.rand(entries, device=DEV, generator=g) < 0.5, -1.0, 1.0)
+    return out.view(m, n).to(dtype)
+
+
+EXACT = [(16, 16, 64), (64, 64, 256), (65, 127, 256), (200, 90, 256), (1, 300, 256), (300, 1, 256), (513, 1000, 1024), (2000, 130, 1024), (100, 5000, 1024), (1025, 1025, 4096), (4000, 2100, 4096),
+         (2048, 4096, 4096)]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n,entries", EXACT)
+def test_one_step_is_exact(dtype, m, n, entries):
+    say("orthogonalize exact", dtype, m, n)
+    T = TYPES[dtype]
+    G = sparse(gen(m + n), m, n, entries, T)
+    for coef in ((1.5, -0.5, 0.0), (0.5, 0.0, 1.0), (1.0, 0.0, 0.0)):
+        want = definition(G, 1, [coef])
+        if min(m, n) == 1 and coef[2]:
+            want = G.double() / G.double().norm() * 1.5
+        assert torch.equal(ctx().rsvd_orthogonalize(G, 1, coef), rounded(want, T))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n", [(50, 70), (300, 130), (128, 128), (33, 1000)])
+def test_a_batch_is_its_matrices(dtype, m, n):
+    T, g = TYPES[dtype], gen(m)
+    G = torch.stack([momentum(g, m, n, T) * 10.0 ** (i - 1) for i in range(4)])
+    G[2] = 0.0
+    got = ctx().rsvd_orthogonalize(G)
+    assert not got[2].any()
+    for i in (0, 1, 3):
+        iterated(G[i], got=got[i])
+    # views: the batch inside the rows, rows of wider tensors, every other matrix; in place
+    big = torch.full((m, 4, n + 5), 7.0, device=DEV, dtype=T)
+    view = big.permute(1, 0, 2)[:, :, 2:n + 2]
+    view.copy_(G)
+    room = torch.full((8, m, n + 3), 7.0, device=DEV, dtype=T)
+    out = room[::2, :, 1:n + 1]
+    ctx().rsvd_orthogonalize(view, out=out)
+    assert torch.equal(out, got) and bool((room[1::2] == 7).all()) and bool((room[:, :, 0] == 7).all()) and bool((room[:, :, n + 1:] == 7).all())
+    assert bool((big[:, :, :2] == 7).all()) and bool((big[:, :, n + 2:] == 7).all())
+    again = G.clone()
+    assert ctx().rsvd_orthogonalize(again, out=again) is again and torch.equal(again, got)
+    assert torch.equal(ctx().rsvd_orthogonalize(G[0].expand(3, m, n))[2], ctx().rsvd_orthogonalize(G[:1].expand(3, m, n).contiguous())[0])
+    assert ctx().rsvd_orthogonalize(G[:0]).shape == (0, m, n)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+def test_scale_does_not_matter_and_what_is_not_finite_stays_in_its_matrix(dtype):
+    T, g = TYPES[dtype], gen(3)
+    G = momentum(g, 40, 90, F32) * 1e3
+    for by in (2.0 ** -7, 2.0 ** 9) if dtype == "f16" else (2.0 ** -100, 2.0 ** 100):
+        scaled = G.to(T) * by                             # (in fp16 some of these are subnormal numbers, rounded: what they are is what counts)
+        assert torch.equal(ctx().rsvd_orthogonalize(scaled), ctx().rsvd_orthogonalize((scaled.double() / by).to(T)))
+    both = torch.stack([G, G]).to(T)
+    want = ctx().rsvd_orthogonalize(both)
+    for bad in (math.nan, math.inf, -math.inf):
+        both[0, 3, 4] = bad
+        got = ctx().rsvd_orthogonalize(both)
+        assert got[0].isnan().all() and torch.equal(got[1], want[1])
+
+
+def test_singular_vectors_stay_and_values_come_near_one():
+    """Against the library's own decomposition."""
+    g = gen(8)
+    G = momentum(g, 96, 300, F32)
+    S, U, Vt, _ = ctx().rsvd_run(G, 96, 0, 3)
+    O = ctx().rsvd_orthogonalize(G, 12, [STEP] * 4 + [(1.875, -1.25, 0.375)] * 8)
+    # twelve steps take every singular value above 2e-3 of the norm to one; U and Vt are good to 1e-4 of what separates singular values here
+    assert float(S.min() / G.norm()) > 2e-3
+    assert float((O - U @ Vt).abs().max()) < 1e-2
+
+
+def test_refusals():
+    c, G = ctx(), torch.randn(3, 20, 30, device=DEV)
+    for call in (lambda: c.rsvd_orthogonalize(G[0, 0]), lambda: c.rsvd_orthogonalize(G.cpu()), lambda: c.rsvd_orthogonalize(G, 0), lambda: c.rsvd_orthogonalize(G, 65),
+                 lambda: c.rsvd_orthogonalize(G, 2, [STEP]), lambda: c.rsvd_orthogonalize(G, 2, (1.0, 2.0)), lambda: c.rsvd_orthogonalize(G.transpose(1, 2)),
+                 lambda: c.rsvd_orthogonalize(G, out=G[:2]), lambda: c.rsvd_orthogonalize(G, out=torch.empty(3, 20, 30)), lambda: c.rsvd_orthogonalize(G[:, :0])):
+        with pytest.raises(ValueError):
+            call()
+    from paper_2110_03423_amd import RsvdError
+    for coef in ((4.0, 0.0, 0.0), (math.nan, 0.0, 0.0)):
+        with pytest.raises(RsvdError):
+            c.rsvd_orthogonalize(G, 3, coef)
+    with pytest.raises(TypeError):
+        c.rsvd_orthogonalize(G.double())
+    out = torch.empty(3, 20, 30, device=DEV)[:1].expand(3, 20, 30)
+    with pytest.raises(RsvdError):
+        c.rsvd_orthogonalize(G, out=out)

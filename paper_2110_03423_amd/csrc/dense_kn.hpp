@@ -160,8 +160,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void dense_kn_kernel(const Dense
   int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
   asm volatile("" : "+v"(last_lane));
   // (behind the last meeting nobody reads the tiles)
-  dense_finish<false, TM, TN>(P, acc, split, batch, m0 + wm0, n0 + wn0, P.symmetric && tile_m != tile_n, last_lane,
-                                         reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
+  dense_finish<TM, TN>(P, acc, split, batch, m0 + wm0, n0 + wn0, P.symmetric && tile_m != tile_n, last_lane,
+                       reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
 }
 
 template <int KIND, bool A_KROWS, int BM, int BN, int WGM, int WGN> hipError_t dense_kn_run(hipStream_t s, const DenseParams &P) {

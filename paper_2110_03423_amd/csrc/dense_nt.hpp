@@ -5,14 +5,17 @@
 // lanes, 16 bytes each, so a lane fetches the piece that belongs to its place: piece ch of row r lies in place ch ^ (r mod 8), which lets the eight rows that are
 // read together start at different banks.  What is behind the last k is written over with zeros once it has arrived: a load has no mask.
 //
-// gated: a tile's rows of B are sixteen of the gate and the sixteen of the up projection that belong to them in turn, so that a lane ends with both
-// numbers of an output in its registers.
+// Rows of B are the columns of C.  Two blocks of sixteen share 32 rows so that a lane ends with eight consecutive columns of each row in its registers, four from either,
+// and stores them as they are: row r of block 2 p + b is row 32 p + 8 (r / 4) + 4 b + r mod 4 of the tile, and pieces of B are exchanged by r mod 4 and bit 3 of the row.
+// gated: 32 rows of the gate and the 32 of the up projection that belong to them in turn (16, and blocks as they come, where a wavefront has no more than two blocks).
 //
 // Codes are multiplied with their powers by the scaled matrix instruction (one for 128 k).  It takes eight k at a time and cuts each product off, towards zero, below
 // 2^-13 of the largest of them, as all instructions for 8-bit floats do: measured 1.4e-5 of a result of normal numbers, 1.5e-4 of the sum of
 // magnitudes at the worst.  That is lost in the rounding of a 16-bit result; for fp32 results DK_F8_EXACT makes bf16 numbers of the codes and
 // their powers, exactly, and multiplies those at half the rate.
 #pragma once
+
+#include <type_traits>
 
 #include "dense_tile.hpp"
 
@@ -23,29 +26,33 @@ template <int BM, int BN> struct DenseNtCfg {
   static constexpr size_t lds = RING * (size_t)STAGE;      // (more than the wavefronts need in the end)
 };
 
-// The loads of ROWS rows of a k-tile by NT threads.
-template <int NT, int ROWS, bool GATED> struct DenseLoad {
+// What the exchange of a row's pieces goes by.  PAIRED: rows of B that share blocks as above.
+template <bool PAIRED> __device__ __forceinline__ int dense_swizzle(int row) { return PAIRED ? (row & 3) | ((row >> 1) & 4) : row & 7; }
+
+// The loads of ROWS rows of a k-tile by NT threads.  GROUP: rows of gate and of up in turn (0: one matrix).
+template <int NT, int ROWS, bool PAIRED, int GROUP> struct DenseLoad {
   static constexpr int N = ROWS * 8 / NT;
   static_assert(ROWS * 8 % NT == 0 && NT % 64 == 0, "whole rounds");
   uint32_t off[N];
+  static __device__ __forceinline__ int piece(int q) { return (q & 7) ^ dense_swizzle<PAIRED>(q >> 3); }      // of the k-tile, in place q
   __device__ __forceinline__ void init(int64_t ld, int64_t rows_left, int tid) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int q = tid + NT * i, r = q >> 3, wanted = GATED ? (r >> 5 << 4) + (r & 15) : r;
+      const int q = tid + NT * i, r = q >> 3, wanted = GROUP ? r / (2 * (GROUP ? GROUP : 1)) * GROUP + r % (GROUP ? GROUP : 1) : r;
       const int row = wanted < rows_left ? wanted : (int)rows_left - 1;
-      off[i] = (uint32_t)row * (uint32_t)ld + (uint32_t)(((q & 7) ^ (r & 7)) << 4);
+      off[i] = (uint32_t)row * (uint32_t)ld + (uint32_t)(piece(q) << 4);
       asm volatile("" : "+v"(off[i]));                   // (one register, not the pair that the product came in)
     }
   }
-  // Load i of a thread, from the tile's first row on (gated: `up` bytes behind it for rows of the up projection; a wavefront has eight rows of one of
+  // Load i of a thread, from the tile's first row on (`up` bytes behind it for rows of the up projection; a wavefront has eight rows of one of
   // both).  left: pieces of the k-tile that exist; another one is read in the place of those that do not.
   __device__ __forceinline__ void issue(int i, const char *base, int64_t up, char *lds, int left, int wave, int tid) {
     uint32_t o = off[i];
     if (left < 8) {
-      const int q = tid + NT * i, ch = (q & 7) ^ ((q >> 3) & 7);
+      const int ch = piece(tid + NT * i);
       if (ch >= left) o -= (uint32_t)ch << 4;
     }
-    if (GATED && ((wave * 8 + NT / 8 * i) >> 4 & 1)) base += up;
+    if (GROUP && ((wave * 8 + NT / 8 * i) / (GROUP ? GROUP : 1) & 1)) base += up;
     const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00027000);
     __builtin_amdgcn_raw_ptr_buffer_load_lds(all, (__attribute__((address_space(3))) void *)(lds + (wave * 64 + NT * i) * 16), 16, o, 0, 0, 0);
   }
@@ -90,17 +97,18 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
       pin<BM == 256>(acc[i][j]);
     }
 
-  DenseLoad<NT, BM, false> la;
-  DenseLoad<NT, BN, GATED> lb;
+  constexpr bool PAIRED = !GATED || TN > 2;
+  DenseLoad<NT, BM, false, 0> la;
+  DenseLoad<NT, BN, PAIRED, !GATED ? 0 : PAIRED ? 32 : 16> lb;
   la.init(P.lda, P.M - m0, tid);
   lb.init(P.ldb, P.N - n0, tid);
   constexpr int LOADS = decltype(la)::N + decltype(lb)::N;
   const char *const a_row = P.A + batch * P.a_batch + m0 * P.lda, *const b_row = P.B + batch * P.b_batch + n0 * P.ldb;
   const int last_left = (int)((P.K * (CODES ? 1 : 2) - (int64_t)(P.ktiles - 1) * 128) >> 4);      // pieces of the last k-tile that exist
 
-  // the k-tile that is loaded next, and the one that is multiplied next: its part of k and its place there
+  // the k-tile that is loaded next: its part of k and its place there
   int next_seg = __builtin_amdgcn_readfirstlane(kt_begin / P.ktiles), next_kt = __builtin_amdgcn_readfirstlane(kt_begin - next_seg * P.ktiles), next = 0;
-  int now_kt = next_kt;
+  const int first_kt = next_kt;
   const char *a_now, *b_now;
   int left;
   auto point = [&]() RSVD_INLINE {
@@ -122,13 +130,6 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
     if (l < decltype(la)::N) la.issue(l, a_now, 0, st, left, wave, tid);
     else lb.issue(l - decltype(la)::N, b_now, P.b_up, st + BM * 128, left, wave, tid);
   };
-  point();
-#pragma unroll
-  for (int t = 0; t < RING - 1; ++t) {
-#pragma unroll
-    for (int l = 0; l < LOADS; ++l) issue(t, l);
-    advance();
-  }
 
   // powers of four k-tiles at a time, fetched four ahead
   unsigned pa[2][CODES ? TM : 1], pb[2][CODES ? TN : 1];
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
     }
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      const int64_t n = n0 + wn0 + 16 * j + r16;
+      const int64_t n = n0 + wn0 + 32 * (j / 2) + 8 * (r16 >> 2) + 4 * (j & 1) + (r16 & 3);
       b_pow[j] = P.b_pow + ((n < P.N ? n : P.N - 1) >> P.b_shift) * P.ld_bpow;
     }
   }
@@ -152,124 +153,165 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
 #pragma unroll
     for (int j = 0; j < (CODES ? TN : 0); ++j) pb[1][j] = *reinterpret_cast<const unsigned *>(b_pow[j] + at);
   };
+  auto take_powers = [&](int kt) RSVD_INLINE {
+    if ((kt & 3) == 0) {
+#pragma unroll
+      for (int i = 0; i < (CODES ? TM : 0); ++i) pa[0][i] = pa[1][i];
+#pragma unroll
+      for (int j = 0; j < (CODES ? TN : 0); ++j) pb[0][j] = pb[1][j];
+      fetch_powers(kt + 4);
+    } else {
+#pragma unroll
+      for (int i = 0; i < (CODES ? TM : 0); ++i) pa[0][i] >>= 8;
+#pragma unroll
+      for (int j = 0; j < (CODES ? TN : 0); ++j) pb[0][j] >>= 8;
+    }
+  };
   if constexpr (CODES) fetch_powers(0);
 
-  const int swz = r16 & 7;                       // (rows of a wavefront's blocks start at multiples of 16)
-  const char *const a_lds = dense_lds + (wm0 + r16) * 128, *const b_lds = dense_lds + BM * 128 + (wn0 + r16) * 128;
-  for (int kt = 0; kt < nkt; ++kt) {
+  constexpr int AHEAD = TM >= 4 ? 3 : 1;               // rows of blocks read ahead, not all of them: registers
+  constexpr int FIRST = KIND == DK_F8 || LOADS < 2 * AHEAD ? LOADS : 2 * AHEAD;      // loads of a tile that are issued behind a meeting
+  // (rows of a wavefront's blocks start at multiples of 32, or of 16 where they are not shared: what pieces are exchanged by is the lane's)
+  const int b_first = PAIRED ? 8 * (r16 >> 2) + (r16 & 3) : r16, a_swz = dense_swizzle<false>(r16), b_swz = dense_swizzle<PAIRED>(b_first);
+  const char *const a_lds = dense_lds + (wm0 + r16) * 128, *const b_lds = dense_lds + BM * 128 + (wn0 + b_first) * 128;
+  auto piece_a = [&](int kt, int i, int h) RSVD_INLINE {
+    return *reinterpret_cast<const u32x4 *>(a_lds + (kt % RING) * STAGE + i * 2048 + (((4 * h + kq) ^ a_swz) << 4));
+  };
+  auto piece_b = [&](int kt, int j, int h) RSVD_INLINE {
+    return *reinterpret_cast<const u32x4 *>(b_lds + (kt % RING) * STAGE + (PAIRED ? j / 2 * 4096 + (j & 1) * 512 : j * 2048) + (((4 * h + kq) ^ b_swz) << 4));
+  };
+  // Everybody has read its last of the tile before kt, and kt has arrived: `flying` loads are of later tiles.
+  auto meet = [&](auto flying, int kt) RSVD_INLINE {
     asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_waitcnt(tile_wait((RING - 2) * LOADS));
+    __builtin_amdgcn_s_waitcnt(tile_wait(decltype(flying)::value));
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    const int at = (kt % RING) * STAGE;
     if constexpr (!CODES) {
-      if (now_kt == P.ktiles - 1 && last_left < 8) {
+      if (last_left < 8 && (first_kt + kt + 1) % P.ktiles == 0) {      // zeros behind the last k
         for (int q = tid; q < (BM + BN) * 8; q += NT)
-          if (((q & 7) ^ (q >> 3 & 7)) >= last_left) *reinterpret_cast<u32x4 *>(dense_lds + at + q * 16) = (u32x4)0u;
+          if ((q < BM * 8 ? decltype(la)::piece(q) : decltype(lb)::piece(q - BM * 8)) >= last_left) *reinterpret_cast<u32x4 *>(dense_lds + (kt % RING) * STAGE + q * 16) = (u32x4)0u;
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(tile_wait(63));
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
       }
-      if (++now_kt == P.ktiles) now_kt = 0;
     }
-    constexpr int AHEAD = TM >= 4 ? 3 : 1;             // rows of blocks read ahead, not all of them: registers
-    auto piece_a = [&](int i, int h) RSVD_INLINE { return *reinterpret_cast<const u32x4 *>(a_lds + at + i * 2048 + (((4 * h + kq) ^ swz) << 4)); };
-    auto piece_b = [&](int j, int h) RSVD_INLINE { return *reinterpret_cast<const u32x4 *>(b_lds + at + j * 2048 + (((4 * h + kq) ^ swz) << 4)); };
-    auto load_next = [&](int step) RSVD_INLINE {
+  };
+  point();
 #pragma unroll
-      for (int l = 0; l < LOADS; ++l)
-        if (l * TM / LOADS == step) issue(kt + RING - 1, l);
-    };
-    if constexpr (CODES) {
-      if ((kt & 3) == 0) {
+  for (int t = 0; t < RING - 1; ++t) {
 #pragma unroll
-        for (int i = 0; i < TM; ++i) pa[0][i] = pa[1][i];
+    for (int l = 0; l < LOADS; ++l) issue(t, l);
+    advance();
+  }
 #pragma unroll
-        for (int j = 0; j < TN; ++j) pb[0][j] = pb[1][j];
-        fetch_powers(kt + 4);
-      } else {
+  for (int l = 0; l < FIRST; ++l) issue(RING - 1, l);
+  meet(std::integral_constant<int, (RING - 2) * LOADS + FIRST>(), 0);
+
+  // Where the rows of blocks of a tile that are read ahead would be those of the next one, wavefronts meet, and go on with the next tile's: no wavefront
+  // waits for LDS at the start of a tile.  (The loads of a tile go to the place of the one that is multiplied before, from the meeting on.)
+  if constexpr (KIND == DK_F8) {
+    // a tile's last rows of blocks column by column, so that an operand of B is free for the next tile's as soon as it can be
+    u32x4 a[AHEAD + 1][2], b[TN][2];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) pa[0][i] >>= 8;
+    for (int j = 0; j < TN; ++j)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) pb[0][j] >>= 8;
-      }
-    }
-    if constexpr (KIND == DK_F8) {
-      u32x4 a[AHEAD + 1][2], b[TN][2];
+      for (int h = 0; h < 2; ++h) b[j][h] = piece_b(0, j, h);
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
+    for (int h = 0; h < 2; ++h) a[0][h] = piece_a(0, 0, h);
+    for (int kt = 0; kt < nkt; ++kt) {
+      take_powers(kt);
+      auto multiply = [&](int i, int j) RSVD_INLINE {
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_both(b[j]), f8_both(a[i % (AHEAD + 1)]), acc[i][j], 0, 0, 0, (int)pb[0][j], 0, (int)pa[0][i]);
+      };
 #pragma unroll
-        for (int h = 0; h < 2; ++h) b[j][h] = piece_b(j, h);
+      for (int i = 1; i < AHEAD; ++i)
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) a[i][h] = piece_a(i, h);
+        for (int h = 0; h < 2; ++h) a[i][h] = piece_a(kt, i, h);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int step = 0; step < TM; ++step) {
-        if (step + AHEAD < TM)
+      for (int i = 0; i < TM - AHEAD; ++i) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) a[(step + AHEAD) % (AHEAD + 1)][h] = piece_a(step + AHEAD, h);
+        for (int h = 0; h < 2; ++h) a[(i + AHEAD) % (AHEAD + 1)][h] = piece_a(kt, i + AHEAD, h);
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
-          acc[step][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_both(b[j]), f8_both(a[step % (AHEAD + 1)]), acc[step][j], 0, 0, 0, (int)pb[0][j], 0, (int)pa[0][step]);
-        load_next(step);
+        for (int j = 0; j < TN; ++j) multiply(i, j);
         __builtin_amdgcn_sched_barrier(0);
       }
-    } else if constexpr (KIND == DK_F8_EXACT) {
-      float ua[TM], ub[TN];
+      meet(std::integral_constant<int, (RING - 2) * LOADS>(), kt + 1);
+      advance();
 #pragma unroll
-      for (int i = 0; i < TM; ++i) ua[i] = f8_unit(pa[0][i] & 255u);
+      for (int h = 0; h < 2; ++h) a[0][h] = piece_a(kt + 1, 0, h);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) ub[j] = f8_unit(pb[0][j] & 255u);
+      for (int j = 0; j < TN; ++j) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        u32x4 b[TN][2];
+        for (int i = TM - AHEAD; i < TM; ++i) multiply(i, j);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) f8_widen(piece_b(j, h), ub[j], b[j]);
+        for (int l = 0; l < LOADS; ++l)
+          if (l * TN / LOADS == j) issue(kt, l);
 #pragma unroll
-        for (int i = 0; i < TM; ++i) {
-          u32x4 a[2];
-          f8_widen(piece_a(i, h), ua[i], a);
-#pragma unroll
-          for (int q = 0; q < 2; ++q)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(b[j][q], a[q], acc[i][j]);
-          if (h == 0) load_next(i);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        for (int h = 0; h < 2; ++h) b[j][h] = piece_b(kt + 1, j, h);
+        __builtin_amdgcn_sched_barrier(0);
       }
-    } else {
-      u32x4 a[AHEAD + 1], b[2][TN];
+    }
+  } else {
+    // (of 8-bit floats as bf16 numbers: two steps of 32 k out of a piece)
+    constexpr int Q = KIND == DK_F8_EXACT ? 2 : 1;
+    u32x4 a[AHEAD + 1], b[2][TN];
 #pragma unroll
-      for (int j = 0; j < TN; ++j) b[0][j] = piece_b(j, 0);
+    for (int j = 0; j < TN; ++j) b[0][j] = piece_b(0, j, 0);
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) a[i] = piece_a(i, 0);
+    for (int i = 0; i < AHEAD; ++i) a[i] = piece_a(0, i, 0);
+    for (int kt = 0; kt < nkt; ++kt) {
+      if constexpr (CODES) take_powers(kt);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int step = 0; step < 2 * TM; ++step) {
-        const int h = step / TM, i = step % TM;
-        if (step + AHEAD < 2 * TM) a[(step + AHEAD) % (AHEAD + 1)] = piece_a((step + AHEAD) % TM, (step + AHEAD) / TM);
+        const int h = step / TM, i = step % TM, ahead = step + AHEAD;
+        if (step == 2 * TM - AHEAD) {
+          meet(std::integral_constant<int, (RING - 2) * LOADS>(), kt + 1);
+          advance();
+        }
+        u32x4 now = a[step % (AHEAD + 1)];
+        a[ahead % (AHEAD + 1)] = piece_a(ahead < 2 * TM ? kt : kt + 1, ahead % TM, ahead / TM % 2);
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
-          if (h == 0 && i == j * TM / TN) b[1][j] = piece_b(j, 1);
+        for (int j = 0; j < TN; ++j) {
+          if (h == 0 && i == j * TM / TN) b[1][j] = piece_b(kt, j, 1);
+          if (step >= 2 * TM - AHEAD && (step - 2 * TM + AHEAD) == j * AHEAD / TN) b[0][j] = piece_b(kt + 1, j, 0);
+        }
+        if constexpr (KIND == DK_F8_EXACT) {
+          u32x4 wide_a[2];
+          f8_widen(now, f8_unit(pa[0][i] & 255u), wide_a);
 #pragma unroll
-        for (int j = 0; j < TN; ++j)
-          acc[i][j] = KIND == DK_BF16 ? mfma_bf16(b[h][j], a[step % (AHEAD + 1)], acc[i][j]) : mfma_f16(b[h][j], a[step % (AHEAD + 1)], acc[i][j]);
-        load_next(step);
+          for (int j = 0; j < TN; ++j) {
+            u32x4 wide_b[2];
+            f8_widen(b[h][j], f8_unit(pb[0][j] & 255u), wide_b);
+#pragma unroll
+            for (int q = 0; q < Q; ++q) acc[i][j] = mfma_bf16(wide_b[q], wide_a[q], acc[i][j]);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[i][j] = KIND == DK_BF16 ? mfma_bf16(b[h][j], now, acc[i][j]) : mfma_f16(b[h][j], now, acc[i][j]);
+        }
+#pragma unroll
+        for (int l = 0; l < LOADS; ++l) {
+          if (l < FIRST ? step == 2 * TM - AHEAD + l / 2 : step == (l - FIRST) / 2) issue(l < FIRST ? kt : kt + RING - 1, l);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
     }
-    advance();
   }
 
-  __builtin_amdgcn_s_waitcnt(tile_wait(0));            // (nothing may land in LDS any more)
-  __syncthreads();
+  const int64_t m1 = m0 + wm0, n1 = n0 + (GATED ? wn0 / 2 : wn0);
   int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
   asm volatile("" : "+v"(last_lane));
-  dense_finish<GATED, TM, TN>(P, acc, split, batch, m0 + wm0, n0 + (GATED ? wn0 / 2 : wn0), P.symmetric && tile_m != tile_n, last_lane,
-                                         reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
+  dense_finish_rows<GATED, TM, TN>(P, acc, split, batch, m1, n1, last_lane);
+  if constexpr (!GATED && !CODES) {
+    if (P.symmetric && tile_m != tile_n) {
+      __builtin_amdgcn_s_waitcnt(tile_wait(0));          // (nothing may land in LDS any more)
+      __syncthreads();
+      dense_finish_mirror<TM, TN>(P, acc, split, batch, m1, n1, last_lane, reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
+    }
+  }
 }
 
 template <int KIND, bool GATED, int BM, int BN, int WGM, int WGN> hipError_t dense_nt_run(hipStream_t s, const DenseParams &P) {

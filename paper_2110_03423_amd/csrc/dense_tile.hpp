@@ -1,6 +1,8 @@
 // What the product kernels of the gated block's operators have in common: places of tiles, and the end of a tile.
 #pragma once
 
+#include <type_traits>
+
 #include "dense.hpp"
 #include "layer8_tile.hpp"
 
@@ -102,129 +104,268 @@ template <int TYPE> __device__ __forceinline__ void put4(void *p, int64_t at, in
 __device__ __forceinline__ f32x4 load4(int type, const void *p, int64_t at, int left) {
   return type == RSVD_X_F32 ? load4<RSVD_X_F32>(p, at, left) : type == RSVD_X_BF16 ? load4<RSVD_X_BF16>(p, at, left) : load4<RSVD_X_F16>(p, at, left);
 }
-__device__ __forceinline__ void put4(int type, void *p, int64_t at, int left, f32x4 v) {
-  if (type == RSVD_X_F32) put4<RSVD_X_F32>(p, at, left, v);
-  else if (type == RSVD_X_BF16) put4<RSVD_X_BF16>(p, at, left, v);
-  else put4<RSVD_X_F16>(p, at, left, v);
-}
-__device__ __forceinline__ int left_of(int64_t n, int64_t N) { return N - n >= 4 ? 4 : (int)(N - n); }
+// V times four columns from n on that exist.
+template <int V = 1> __device__ __forceinline__ int left_of(int64_t n, int64_t N) { return N - n >= 4 * V ? 4 * V : (int)(N - n); }
 
-// Columns n to n + 3 of row m, of which those before `width` are stored and those from N on are zeros.
-__device__ __forceinline__ void linear_end(const LinearOut &O, int64_t N, int batch, int64_t m, int64_t n, f32x4 v) {
-  const int have = left_of(n, N), left = left_of(n, O.width);
-  v *= O.alpha;
+// V times four numbers, of which `left` exist.
+template <int TYPE, int V> __device__ __forceinline__ void load_row(const void *p, int64_t at, int left, f32x4 (&v)[V]) {
+  if constexpr (V == 2 && TYPE != RSVD_X_F32) {
+    if (left >= 8) {
+      const u32x4 w = *reinterpret_cast<const u32x4_any *>(reinterpret_cast<const uint16_t *>(p) + at);
+#pragma unroll
+      for (int h = 0; h < 4; ++h) {
+        const unsigned pair = w[h];
+        if constexpr (TYPE == RSVD_X_BF16) {
+          v[h >> 1][2 * (h & 1)] = bf16_low(pair);
+          v[h >> 1][2 * (h & 1) + 1] = bf16_high(pair);
+        } else {
+          const f16x2 f = __builtin_bit_cast(f16x2, pair);
+          v[h >> 1][2 * (h & 1)] = (float)f[0];
+          v[h >> 1][2 * (h & 1) + 1] = (float)f[1];
+        }
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < V; ++x) v[x] = load4<TYPE>(p, at + 4 * x, left - 4 * x);
+}
+template <int TYPE, int V> __device__ __forceinline__ void put_row(void *p, int64_t at, int left, const f32x4 (&v)[V]) {
+  if constexpr (V == 2 && TYPE != RSVD_X_F32) {
+    if (left >= 8) {
+      const u32x2 a = halves4<TYPE>(v[0]), b = halves4<TYPE>(v[1]);
+      *reinterpret_cast<u32x4_any *>(reinterpret_cast<uint16_t *>(p) + at) = u32x4{a[0], a[1], b[0], b[1]};
+      return;
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < V; ++x) put4<TYPE>(p, at + 4 * x, left - 4 * x, v[x]);
+}
+
+// f with the type, or the activation, as a constant.
+template <typename F> __device__ __forceinline__ void with_type(int type, F f) {
+  if (type == RSVD_X_BF16) f(std::integral_constant<int, RSVD_X_BF16>());
+  else if (type == RSVD_X_F16) f(std::integral_constant<int, RSVD_X_F16>());
+  else f(std::integral_constant<int, RSVD_X_F32>());
+}
+template <typename F> __device__ __forceinline__ void with_act(int act, F f) {
+  if (act == GATED_SILU) f(std::integral_constant<int, GATED_SILU>());
+  else if (act == GATED_GELU) f(std::integral_constant<int, GATED_GELU>());
+  else if (act == GATED_GELU_TANH) f(std::integral_constant<int, GATED_GELU_TANH>());
+  else f(std::integral_constant<int, GATED_RELU>());
+}
+
+// The end of C groups of V times four columns.  Group c has row m[c] (if it is there) and columns from n[c] on, of which those before `width` are stored and those from N on are
+// zeros.  All loads come before the stores.  WHOLE: all rows and columns exist (no branches between loads).
+template <int C, int V, bool WHOLE>
+__device__ __forceinline__ void linear_end(const LinearOut &O, int64_t N, int batch, const int64_t (&m)[C], const int64_t (&n)[C], const bool (&there)[C], f32x4 (&v)[C][V]) {
+  auto have = [&](int c) RSVD_INLINE { return WHOLE ? 4 * V : there[c] ? left_of<V>(n[c], N) : 0; };
+  auto left = [&](int c) RSVD_INLINE { return WHOLE ? 4 * V : there[c] ? left_of<V>(n[c], O.width) : 0; };
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int x = 0; x < V; ++x) v[c][x] *= O.alpha;
   if (O.D != nullptr) {
     const uint16_t *d = O.D + batch * O.d_batch;
-    f32x4 sum = load4<RSVD_X_F16>(d, m * O.ldd + n, have);
-    if (O.d_planes == 2) sum += load4<RSVD_X_F16>(d + O.d_plane / 2, m * O.ldd + n, have);
-    v += O.beta * sum;
+    f32x4 sum[C][V], low[C][V];
+#pragma unroll
+    for (int c = 0; c < C; ++c) load_row<RSVD_X_F16, V>(d, m[c] * O.ldd + n[c], have(c), sum[c]);
+    if (O.d_planes == 2) {
+#pragma unroll
+      for (int c = 0; c < C; ++c) load_row<RSVD_X_F16, V>(d + O.d_plane / 2, m[c] * O.ldd + n[c], have(c), low[c]);
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int x = 0; x < V; ++x) sum[c][x] += low[c][x];
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int x = 0; x < V; ++x) v[c][x] += O.beta * sum[c][x];
   }
+  if constexpr (!WHOLE) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = e < have ? v[e] : 0.f;
-  const int64_t at = batch * O.c_batch + m * O.ldc + n;
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+      for (int e = 0; e < 4 * V; ++e) v[c][e >> 2][e & 3] = e < have(c) ? v[c][e >> 2][e & 3] : 0.f;
+  }
+  const int64_t at = batch * O.c_batch;
   if (O.planes == 2) {
-    put4<RSVD_X_F16>(O.C, at, left, v);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] -= (float)(_Float16)v[e];
-    put4<RSVD_X_F16>(reinterpret_cast<char *>(O.C) + O.c_plane, at, left, v);
+    for (int c = 0; c < C; ++c) {
+      put_row<RSVD_X_F16, V>(O.C, at + m[c] * O.ldc + n[c], left(c), v[c]);
+#pragma unroll
+      for (int e = 0; e < 4 * V; ++e) v[c][e >> 2][e & 3] -= (float)(_Float16)v[c][e >> 2][e & 3];
+      put_row<RSVD_X_F16, V>(reinterpret_cast<char *>(O.C) + O.c_plane, at + m[c] * O.ldc + n[c], left(c), v[c]);
+    }
     return;
   }
-  if (O.accumulate) v += load4(O.type, O.C, at, left);
-  put4(O.type, O.C, at, left, v);
+  with_type(O.type, [&](auto type) RSVD_INLINE {
+    constexpr int TYPE = decltype(type)::value;
+    if constexpr (TYPE == RSVD_X_F32)
+      if (O.accumulate) {
+        f32x4 old[C][V];
+#pragma unroll
+        for (int c = 0; c < C; ++c) load_row<TYPE, V>(O.C, at + m[c] * O.ldc + n[c], left(c), old[c]);
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int x = 0; x < V; ++x) v[c][x] += old[c][x];
+      }
+#pragma unroll
+    for (int c = 0; c < C; ++c) put_row<TYPE, V>(O.C, at + m[c] * O.ldc + n[c], left(c), v[c]);
+  });
+}
+__device__ __forceinline__ void linear_end1(const LinearOut &O, int64_t N, int batch, int64_t m, int64_t n, f32x4 v) {
+  const int64_t row[1] = {m}, column[1] = {n};
+  const bool there[1] = {true};
+  f32x4 vs[1][1] = {{v}};
+  linear_end<1, 1, false>(O, N, batch, row, column, there, vs);
 }
 
 // The activation (g times a share of it) and its derivative.  The shares are written so that none is a difference of numbers near one: 1 / 2 + erf / 2 as a
 // complement, 1 / 2 + tanh(y) / 2 as 1 / (1 + exp(-2 y)).
-__device__ __forceinline__ float act_share(int act, float g) {
-  if (act == GATED_SILU) return 1.f / (1.f + __expf(-g));
-  if (act == GATED_GELU) return 0.5f * erfcf(-0.70710678f * g);
-  return 1.f / (1.f + __expf(-1.5957691f * (g + 0.044715f * g * g * g)));
+template <int ACT> __device__ __forceinline__ float act_share(float g) {
+  if constexpr (ACT == GATED_SILU) return 1.f / (1.f + __expf(-g));
+  else if constexpr (ACT == GATED_GELU) return 0.5f * erfcf(-0.70710678f * g);
+  else return 1.f / (1.f + __expf(-1.5957691f * (g + 0.044715f * g * g * g)));
 }
-__device__ __forceinline__ float act_value(int act, float g) {
-  if (act == GATED_RELU) return g > 0.f ? g : g != g ? g : 0.f;
-  return g * act_share(act, g);
+template <int ACT> __device__ __forceinline__ float act_value(float g) {
+  if constexpr (ACT == GATED_RELU) return g > 0.f ? g : g != g ? g : 0.f;
+  else return g * act_share<ACT>(g);
 }
-__device__ __forceinline__ float act_slope(int act, float g, float &value) {
-  if (act == GATED_RELU) {
+template <int ACT> __device__ __forceinline__ float act_slope(float g, float &value) {
+  if constexpr (ACT == GATED_RELU) {
     value = g > 0.f ? g : g != g ? g : 0.f;
     return g > 0.f ? 1.f : 0.f;
-  }
-  const float s = act_share(act, g);
-  value = g * s;
-  if (act == GATED_SILU) return s + value * (1.f - s);
-  if (act == GATED_GELU) return s + g * __expf(-0.5f * g * g) * 0.39894228f;
-  return s + value * (1.f - s) * 1.5957691f * (1.f + 0.134145f * g * g);
-}
-
-// Gradients of gate and up, four columns from n on, to the planes of D (gate from column 0 on, up from column m on).
-__device__ __forceinline__ void slope_end(const GatedOut &O, int64_t N, int64_t m, int64_t n, f32x4 g, f32x4 u) {
-  const int left = left_of(n, N);
-  const f32x4 dh = load4(O.type, O.dH, m * O.lddh + n, left);
-  f32x4 dg, du;
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    float value;
-    const float slope = act_slope(O.act, g[e], value);
-    dg[e] = dh[e] * u[e] * slope;
-    du[e] = dh[e] * value;
-  }
-  const int64_t at = m * O.ldD + n;
-  if (n + 4 >= N)                                        // (the zeros behind them)
-    for (int64_t c = 2 * N; c < O.ldD; ++c)
-      for (int q = 0; q < (O.type == RSVD_X_F32 ? 3 : 1); ++q) O.D[q * (O.plane / 2) + m * O.ldD + c] = 0;
-  if (O.type == RSVD_X_F16) {
-    put4<RSVD_X_F16>(O.D, at, left, dg);
-    put4<RSVD_X_F16>(O.D, at + N, left, du);
-  } else if (O.type == RSVD_X_BF16) {
-    put4<RSVD_X_BF16>(O.D, at, left, dg);
-    put4<RSVD_X_BF16>(O.D, at + N, left, du);
   } else {
-    unsigned p[2][2][3];
-    bf16_parts2<3>(dg[0], dg[1], p[0][0]);
-    bf16_parts2<3>(dg[2], dg[3], p[0][1]);
-    bf16_parts2<3>(du[0], du[1], p[1][0]);
-    bf16_parts2<3>(du[2], du[3], p[1][1]);
+    const float s = act_share<ACT>(g);
+    value = g * s;
+    if constexpr (ACT == GATED_SILU) return s + value * (1.f - s);
+    else if constexpr (ACT == GATED_GELU) return s + g * __expf(-0.5f * g * g) * 0.39894228f;
+    else return s + value * (1.f - s) * 1.5957691f * (1.f + 0.134145f * g * g);
+  }
+}
+// Gradients of gate and up, V times four columns from n on, to the planes of D (gate from column 0 on, up from column N on, zeros behind both).
+template <int TYPE, int V> __device__ __forceinline__ void slope_put(const GatedOut &O, int64_t N, int64_t m, int64_t n, int left, const f32x4 (&dg)[V], const f32x4 (&du)[V]) {
+  constexpr int PLANES = TYPE == RSVD_X_F32 ? 3 : 1;
+  const int64_t at = m * O.ldD + n;
+  if (2 * N != O.ldD && n < N && n + 4 * V >= N)
+    for (int64_t c = 2 * N; c < O.ldD; ++c)
+      for (int q = 0; q < PLANES; ++q) O.D[q * (O.plane / 2) + m * O.ldD + c] = 0;
+  if constexpr (TYPE != RSVD_X_F32) {
+    put_row<TYPE, V>(O.D, at, left, dg);
+    put_row<TYPE, V>(O.D, at + N, left, du);
+  } else {
 #pragma unroll
-    for (int q = 0; q < 3; ++q)
+    for (int x = 0; x < V; ++x) {
+      unsigned p[2][2][3];
+      bf16_parts2<3>(dg[x][0], dg[x][1], p[0][0]);
+      bf16_parts2<3>(dg[x][2], dg[x][3], p[0][1]);
+      bf16_parts2<3>(du[x][0], du[x][1], p[1][0]);
+      bf16_parts2<3>(du[x][2], du[x][3], p[1][1]);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint16_t *c = O.D + q * (O.plane / 2) + at + h * N;
-        if (left >= 4) *reinterpret_cast<u32x2_any *>(c) = u32x2{p[h][0][q], p[h][1][q]};
-        else
+      for (int q = 0; q < 3; ++q)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (e < left) c[e] = (uint16_t)(p[h][e >> 1][q] >> (16 * (e & 1)));
-      }
+        for (int h = 0; h < 2; ++h) {
+          uint16_t *c = O.D + q * (O.plane / 2) + at + 4 * x + h * N;
+          if (left >= 4 * x + 4) *reinterpret_cast<u32x2_any *>(c) = u32x2{p[h][0][q], p[h][1][q]};
+          else
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (4 * x + e < left) c[e] = (uint16_t)(p[h][e >> 1][q] >> (16 * (e & 1)));
+        }
+    }
   }
 }
 
-__device__ __forceinline__ void gated_end(const GatedOut &O, int64_t N, int64_t m, int64_t n, f32x4 g, f32x4 u) {
-  if (O.dH != nullptr) {
-    slope_end(O, N, m, n, g, u);
-    return;
-  }
-  const int left = left_of(n, N);
-  f32x4 h;
+// The end of C groups of V times four outputs, as linear_end: all loads, then all activations, then the stores.
+template <int C, int V, bool WHOLE>
+__device__ __forceinline__ void gated_end(const GatedOut &O, int64_t N, const int64_t (&m)[C], const int64_t (&n)[C], const bool (&there)[C], f32x4 (&g)[C][V], f32x4 (&u)[C][V]) {
+  auto left = [&](int c) RSVD_INLINE { return WHOLE ? 4 * V : there[c] ? left_of<V>(n[c], N) : 0; };
+  with_type(O.type, [&](auto type) RSVD_INLINE {
+    constexpr int TYPE = decltype(type)::value;
+    if (O.dH != nullptr) {
+      f32x4 dh[C][V];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) h[e] = act_value(O.act, g[e]) * u[e];
-  put4(O.type, O.H, m * O.ldh + n, left, h);
-  if (O.kept != nullptr) {
-    put4(O.type, O.kept, m * O.ldk + n, left, g);
-    put4(O.type, O.kept, m * O.ldk + N + n, left, u);
-  }
+      for (int c = 0; c < C; ++c) load_row<TYPE, V>(O.dH, m[c] * O.lddh + n[c], left(c), dh[c]);
+      with_act(O.act, [&](auto act) RSVD_INLINE {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int x = 0; x < V; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float value;
+              const float slope = act_slope<decltype(act)::value>(g[c][x][e], value);
+              g[c][x][e] = dh[c][x][e] * u[c][x][e] * slope;
+              u[c][x][e] = dh[c][x][e] * value;
+            }
+      });
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (WHOLE || there[c]) slope_put<TYPE, V>(O, N, m[c], n[c], left(c), g[c], u[c]);
+    } else {
+      if (O.kept != nullptr) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+          put_row<TYPE, V>(O.kept, m[c] * O.ldk + n[c], left(c), g[c]);
+          put_row<TYPE, V>(O.kept, m[c] * O.ldk + N + n[c], left(c), u[c]);
+        }
+      }
+      with_act(O.act, [&](auto act) RSVD_INLINE {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int x = 0; x < V; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) g[c][x][e] = act_value<decltype(act)::value>(g[c][x][e]) * u[c][x][e];
+      });
+#pragma unroll
+      for (int c = 0; c < C; ++c) put_row<TYPE, V>(O.H, m[c] * O.ldh + n[c], left(c), g[c]);
+    }
+  });
+}
+__device__ __forceinline__ void gated_end1(const GatedOut &O, int64_t N, int64_t m, int64_t n, f32x4 g, f32x4 u) {
+  const int64_t row[1] = {m}, column[1] = {n};
+  const bool there[1] = {true};
+  f32x4 gs[1][1] = {{g}}, us[1][1] = {{u}};
+  gated_end<1, 1, false>(O, N, row, column, there, gs, us);
 }
 
 // ---------------------------------------------------------------- the end of a wavefront's TM x TN blocks of 16 x 16
-// Through LDS, sixteen rows at a time, so that lanes next to each other write what is next to each other: block (i, j) of lane L holds row 16 i + L % 16 and
-// four columns from 16 j + 4 (L / 16) on.  gated: blocks are gate and up in turn, (m1, n1) counts outputs.  lds: the wavefront's finish_lds<TN>() bytes.
-template <bool GATED, int TM, int TN>
+// (m1, n1): the first row and column of the wavefront's.  partial: the sums are a part, one range of k.
+__device__ __forceinline__ float *partial_of(const DenseParams &P, int split, int batch, int64_t columns) {
+  return P.partial + ((int64_t)batch * P.splits + split) * P.M * columns;
+}
+
+// Sixteen rows of a wavefront's blocks in LDS, with their rows and columns exchanged: lane e has column e / 4 and four of the rows.
+template <int TN> __device__ __forceinline__ void mirror_rows(const DenseParams &P, float *partial, int batch, int64_t m2, int64_t n1, int lane, const float *lds) {
+  constexpr int PITCH = 16 * TN + 4;
+  const int64_t width = P.splits > 1 ? P.N : P.out.width;
+#pragma unroll 1
+  for (int e = lane; e < 64 * TN; e += 64) {
+    const int c = e >> 2, q = 4 * (e & 3);
+    f32x4 v;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) v[x] = lds[(q + x) * PITCH + c];
+    const int64_t mm = n1 + c, nn = m2 + q;
+    if (mm < P.M && nn < width) {
+      if (P.splits > 1) put4<RSVD_X_F32>(partial, mm * P.N + nn, left_of(nn, P.N), v);
+      else linear_end1(P.out, P.N, batch, mm, nn, v);
+    }
+  }
+}
+
+// Block (i, j) of lane L holds row 16 i + L % 16 and four columns from 16 j + 4 (L / 16) on: through LDS, sixteen rows at a time, so that lanes next to each
+// other write what is next to each other.  mirror: and the same with rows and columns exchanged.  lds: the wavefront's finish_lds<TN>() bytes.
+template <int TM, int TN>
 __device__ __forceinline__ void dense_finish(const DenseParams &P, f32x4 (&acc)[TM][TN], int split, int batch, int64_t m1, int64_t n1, bool mirror, int lane, float *lds) {
-  constexpr int PITCH = 16 * TN + 4, PER_ROW = (GATED ? 2 : 4) * TN, ROWS = 64 / PER_ROW, PASSES = 16 / ROWS;
+  constexpr int PITCH = 16 * TN + 4, PER_ROW = 4 * TN, ROWS = 64 / PER_ROW, PASSES = 16 / ROWS, C = PASSES < 4 ? PASSES : 4;
   const int r16 = lane & 15, kq = lane >> 4, row = lane / PER_ROW, col = 4 * (lane % PER_ROW);
-  const int at = GATED ? 32 * (col / 16) + col % 16 : col;
-  const int64_t columns = GATED ? 2 * P.N : P.N, n = n1 + col;
-  float *const partial = P.partial + ((int64_t)batch * P.splits + split) * P.M * columns;
-  const int64_t width = GATED || P.splits > 1 ? P.N : P.out.width;
+  float *const partial = partial_of(P, split, batch, P.N);
+  const int64_t width = P.splits > 1 ? P.N : P.out.width;
+  const bool whole = m1 + 16 * TM <= P.M && n1 + 16 * TN <= P.N;
 #pragma unroll 1
   for (int i = 0; i < TM; ++i) {                        // (one copy of what follows, not one for each row of blocks)
 #pragma unroll
@@ -236,42 +377,98 @@ __device__ __forceinline__ void dense_finish(const DenseParams &P, f32x4 (&acc)[
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll 1
-    for (int p = 0; p < PASSES; ++p) {
-      const float *from = lds + (p * ROWS + row) * PITCH + at;
-      const int64_t m = m1 + 16 * i + p * ROWS + row;
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(from);
-      if (m < P.M && n < width) {
-        if constexpr (GATED) {
-          const f32x4 u = *reinterpret_cast<const f32x4 *>(from + 16);
-          if (P.splits > 1) {
-            put4<RSVD_X_F32>(partial, m * columns + n, left_of(n, P.N), v);
-            put4<RSVD_X_F32>(partial, m * columns + P.N + n, left_of(n, P.N), u);
-          } else {
-            gated_end(P.gate, P.N, m, n, v, u);
-          }
-        } else if (P.splits > 1) {
-          put4<RSVD_X_F32>(partial, m * columns + n, left_of(n, P.N), v);
-        } else {
-          linear_end(P.out, P.N, batch, m, n, v);
-        }
-      }
-    }
-    if (!GATED && mirror) {                             // rows and columns exchanged: lane e has column e / 4 and four of the rows
-#pragma unroll 1
-      for (int e = lane; e < 64 * TN; e += 64) {
-        const int c = e >> 2, q = 4 * (e & 3);
-        f32x4 v;
+    for (int p = 0; p < PASSES; p += C) {
+      f32x4 v[C][1];
+      int64_t m[C], n[C];
+      bool there[C];
 #pragma unroll
-        for (int x = 0; x < 4; ++x) v[x] = lds[(q + x) * PITCH + c];
-        const int64_t mm = n1 + c, nn = m1 + 16 * i + q;
-        if (mm < P.M && nn < width) {
-          if (P.splits > 1) put4<RSVD_X_F32>(partial, mm * columns + nn, left_of(nn, P.N), v);
-          else linear_end(P.out, P.N, batch, mm, nn, v);
-        }
+      for (int c = 0; c < C; ++c) {
+        v[c][0] = *reinterpret_cast<const f32x4 *>(lds + ((p + c) * ROWS + row) * PITCH + col);
+        m[c] = m1 + 16 * i + (p + c) * ROWS + row;
+        n[c] = n1 + col;
+        there[c] = m[c] < P.M && n[c] < width;
+      }
+      if (P.splits > 1) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+          if (there[c]) put4<RSVD_X_F32>(partial, m[c] * P.N + n[c], left_of(n[c], P.N), v[c][0]);
+      } else if (whole) {
+        linear_end<C, 1, true>(P.out, P.N, batch, m, n, there, v);
+      } else {
+        linear_end<C, 1, false>(P.out, P.N, batch, m, n, there, v);
       }
     }
+    if (mirror) mirror_rows<TN>(P, partial, batch, m1 + 16 * i, n1, lane, lds);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The mirrored half for blocks in the order of dense_finish_rows.
+template <int TM, int TN> __device__ __forceinline__ void dense_finish_mirror(const DenseParams &P, f32x4 (&acc)[TM][TN], int split, int batch, int64_t m1, int64_t n1, int lane, float *lds) {
+  constexpr int PITCH = 16 * TN + 4;
+  const int r16 = lane & 15, kq = lane >> 4;
+  float *const partial = partial_of(P, split, batch, P.N);
+#pragma unroll 1
+  for (int i = 0; i < TM; ++i) {
+#pragma unroll
+    for (int x = 0; x < TM; ++x)
+      if (i == x) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) *reinterpret_cast<f32x4 *>(lds + r16 * PITCH + 32 * (j / 2) + 8 * kq + 4 * (j & 1)) = acc[x][j];
+      }
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+    mirror_rows<TN>(P, partial, batch, m1 + 16 * i, n1, lane, lds);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// Blocks (i, 2 p) and (i, 2 p + 1) of lane L hold row 16 i + L % 16 and eight columns from 32 p + 8 (L / 16) on: stored as they are.  gated: p even is the gate and p odd the
+// up projection of 32 outputs; with two blocks, these are the gate and the up projection of sixteen, four of them a lane.
+template <bool GATED, int TM, int TN> __device__ __forceinline__ void dense_finish_rows(const DenseParams &P, f32x4 (&acc)[TM][TN], int split, int batch, int64_t m1, int64_t n1, int lane) {
+  constexpr int V = GATED && TN == 2 ? 1 : 2, C = GATED ? TN / (2 * V) : TN / 2;      // groups of a row, and vectors of four in each
+  const int64_t columns = GATED ? 2 * P.N : P.N, width = GATED || P.splits > 1 ? P.N : P.out.width;
+  float *const partial = partial_of(P, split, batch, columns);
+  const bool whole = m1 + 16 * TM <= P.M && n1 + 4 * V * 4 * C <= P.N;
+  int64_t m[C], n[C];
+  bool there[C];
+#pragma unroll
+  for (int c = 0; c < C; ++c) n[c] = n1 + 16 * V * c + 4 * V * (lane >> 4);
+#pragma unroll 1
+  for (int i = 0; i < TM; ++i) {                        // (one copy of what follows, not one for each row of blocks)
+    f32x4 v[C][V], u[C][V];
+#pragma unroll
+    for (int x = 0; x < TM; ++x)
+      if (i == x) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int y = 0; y < V; ++y) {
+            v[c][y] = acc[x][(GATED ? 2 * V : V) * c + y];
+            if constexpr (GATED) u[c][y] = acc[x][2 * V * c + V + y];
+          }
+      }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      m[c] = m1 + 16 * i + (lane & 15);
+      there[c] = m[c] < P.M && n[c] < width;
+    }
+    if (P.splits > 1) {
+#pragma unroll
+      for (int c = 0; c < C; ++c)
+        if (there[c]) {
+          put_row<RSVD_X_F32, V>(partial, m[c] * columns + n[c], left_of<V>(n[c], P.N), v[c]);
+          if constexpr (GATED) put_row<RSVD_X_F32, V>(partial, m[c] * columns + P.N + n[c], left_of<V>(n[c], P.N), u[c]);
+        }
+    } else if constexpr (GATED) {
+      if (whole) gated_end<C, V, true>(P.gate, P.N, m, n, there, v, u);
+      else gated_end<C, V, false>(P.gate, P.N, m, n, there, v, u);
+    } else {
+      if (whole) linear_end<C, V, true>(P.out, P.N, batch, m, n, there, v);
+      else linear_end<C, V, false>(P.out, P.N, batch, m, n, there, v);
+    }
   }
 }
 
@@ -288,8 +485,8 @@ template <bool GATED> __global__ __launch_bounds__(256) void dense_reduce_kernel
       v += load4<RSVD_X_F32>(p, 0, left);
       if constexpr (GATED) u += load4<RSVD_X_F32>(p + P.N, 0, left);
     }
-    if constexpr (GATED) gated_end(P.gate, P.N, m, n, v, u);
-    else linear_end(P.out, P.N, (int)batch, m, n, v);
+    if constexpr (GATED) gated_end1(P.gate, P.N, m, n, v, u);
+    else linear_end1(P.out, P.N, (int)batch, m, n, v);
   }
 }
 

@@ -82,7 +82,7 @@ template <int XT, int TB, int WAVES> __global__ __launch_bounds__(64 * WAVES) vo
     u += part[v][1][wave][lane];
   }
   const int64_t t = 16 * wave + r16, n = n0 + 4 * kq;
-  if (t < P.tokens && n < P.m) gated_end(P.out, P.m, t, n, g, u);
+  if (t < P.tokens && n < P.m) gated_end1(P.out, P.m, t, n, g, u);
 }
 
 template <int XT> static void gated_few_run(hipStream_t s, const GatedFewParams &P, dim3 grid, bool wide) {
@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256) void gated_slope_kernel(const GatedOut O, int6
     const int64_t t = e / per_row, n = (e - t * per_row) * 4;
     const int left = left_of(n, m);
     const f32x4 g = load4(O.type, O.kept, t * O.ldk + n, left), u = load4(O.type, O.kept, t * O.ldk + m + n, left);
-    slope_end(O, m, t, n, g, u);
+    gated_end1(O, m, t, n, g, u);
   }
 }
 hipError_t gated_slope_launch(hipStream_t s, int64_t tokens, int64_t m, const GatedOut &o) {

@@ -13,38 +13,42 @@ static int64_t dense_tiles(const DenseDesc &d, int b) {
   return d.symmetric ? rows * (rows + 1) / 2 : rows * columns;
 }
 
-// The time of each tile and number of ranges is estimated, and the least taken: a k-tile (128 bytes of a row) takes a CU 0.22, 0.55 and 2.05 us for each
-// workgroup of 64, 128 and 256 rows and columns, but no less than 0.33, 0.78 and 1.8 us, a launch 5 us beside that; ranges of k are a second launch, and their
-// sums are written and read (5 bytes / ps).
-TileChoice dense_choose(const rsvd_ctx *ctx, const DenseDesc &d) {
-  const struct { int b; double step, least; } tile[3] = {{64, 0.22, 0.33}, {128, 0.55, 0.78}, {256, 2.05, 1.8}};
-  static const int ranges[8] = {1, 2, 3, 4, 6, 8, 12, 16};
-  const int64_t all = ceil_div(d.K, dense_k(d.kind)) * dense_segs(d.planes).count, whole = d.kind >= DK_F8 ? 4 : 1;
-  TileChoice best = {64, 64, 1, all, all};
+// The time of each tile and number of ranges is estimated, and the least taken: a k-tile (128 bytes of a row) takes a CU 0.22, 0.55 and 1.75 us for each
+// workgroup of 64, 128 and 256 rows and columns, but no less than 0.33, 0.78 and 1.55 us, a launch 5 us beside that.  Tiles that fill the chip a number of times are
+// worked out whole; of what is left k may be in ranges, for all CUs to have a part: a second launch, and their sums are written and read (5 bytes / ps).
+static DenseChoice dense_choose(const rsvd_ctx *ctx, const DenseDesc &d) {
+  const struct { int b, at_once; double step, least; } tile[3] = {{64, 3, 0.22, 0.33}, {128, 2, 0.55, 0.78}, {256, 1, 1.75, 1.55}};
+  static const int ranges[9] = {1, 2, 3, 4, 6, 8, 12, 16, 24};
+  const int64_t kt = ceil_div(d.K, dense_k(d.kind)) * dense_segs(d.planes).count, cu = ctx->cu_count;
+  DenseChoice best = {};
   double least = 1e300;
   for (const auto &t : tile) {
-    const int64_t tiles = dense_tiles(d, t.b) * d.batch;
+    const int64_t tiles = dense_tiles(d, t.b) * d.batch, full = cu * t.at_once;
+    auto time = [&](int64_t groups, int64_t k) {
+      const double each = (double)ceil_div(groups, cu) * t.step;
+      return groups == 0 ? 0.0 : (double)k * (each > t.least ? each : t.least);
+    };
     for (const int r : ranges) {
-      if (r > 1 && all < 4 * r) break;
-      const int64_t per = (int64_t)align_up((size_t)ceil_div(all, r), (size_t)whole), used = ceil_div(all, per);
-      const double step = (double)ceil_div(tiles * used, ctx->cu_count) * t.step;
-      double us = (double)(used > 1 ? per : all) * (step > t.least ? step : t.least);
-      if (used > 1) us += 3.0 + (double)used * (double)d.batch * (double)d.M * (double)(d.gated ? 2 * d.N : d.N) * 8.0 / 5e6;
+      if (r > 1 && kt < 4 * r) break;
+      const int64_t per = r > 1 ? ceil_div(kt, r) : kt, used = ceil_div(kt, per);
+      if (r > 1 && used < 2) continue;
+      const int64_t whole = used > 1 ? tiles / full * full : tiles, rest = tiles - whole;
+      if (used > 1 && rest == 0) continue;
+      double us = time(whole, kt) + time(rest * used, per);
+      if (used > 1) us += 3.0 + (double)used * (double)rest * t.b * t.b * 8.0 / 5e6;
       if (us < least) {
         least = us;
-        best = TileChoice{t.b, t.b, (int)used, used > 1 ? per : all, all};
+        best = DenseChoice{t.b, dense_tiles(d, t.b), whole, rest, used, kt, per};
       }
     }
   }
   return best;
 }
 
-static size_t partial_bytes(const TileChoice &c, const DenseDesc &d) {
-  return c.splits > 1 ? (size_t)c.splits * d.batch * d.M * (d.gated ? 2 * d.N : d.N) * 4 : 0;
-}
-size_t dense_partial_bytes(const rsvd_ctx *ctx, const DenseDesc &d) { return partial_bytes(dense_choose(ctx, d), d); }
+static size_t partial_bytes(const DenseChoice &c) { return c.splits > 1 ? (size_t)(c.rest * c.splits) * c.b * c.b * 4 : 0; }
+size_t dense_partial_bytes(const rsvd_ctx *ctx, const DenseDesc &d) { return partial_bytes(dense_choose(ctx, d)); }
 
-DenseParams dense_params(const TileChoice &c, const DenseDesc &d) {
+static DenseParams dense_params(const DenseChoice &c, const DenseDesc &d) {
   DenseParams P;
   P.A = (const char *)d.A; P.B = (const char *)d.B;
   P.lda = d.lda; P.ldb = d.ldb; P.a_plane = d.a_plane; P.b_plane = d.b_plane; P.a_batch = d.a_batch; P.b_batch = d.b_batch;
@@ -54,54 +58,55 @@ DenseParams dense_params(const TileChoice &c, const DenseDesc &d) {
   P.M = d.M; P.N = d.N; P.K = d.K;
   P.ktiles = (int)ceil_div(d.K, dense_k(d.kind));
   if (d.kind >= DK_F8) P.K = (int64_t)P.ktiles * 128;
-  P.tiles_m = (int)ceil_div(d.M, c.bm); P.tiles_n = (int)ceil_div(d.gated ? 2 * d.N : d.N, c.bn);
-  P.tiles = (int)dense_tiles(d, c.bm);
-  P.splits = c.splits; P.kt_all = (int)c.kt; P.kt_per_split = (int)c.kt_per_split;
-  P.batch = d.batch; P.symmetric = d.symmetric;
+  P.tiles_m = (int)ceil_div(d.M, c.b); P.tiles_n = (int)ceil_div(d.gated ? 2 * d.N : d.N, c.b);
+  P.tiles = (int)c.tiles; P.batch = d.batch;
+  P.kt_all = (int)c.kt;
+  P.whole = (int)c.whole; P.rest = (int)c.rest; P.splits = (int)c.splits; P.kt_per_split = (int)c.kt_per_split;
+  P.symmetric = d.symmetric;
   P.partial = d.partial;
   P.out = d.out; P.gate = d.gate;
   if (P.out.width == 0) P.out.width = d.N;
   return P;
 }
 
-hipError_t dense_reduce_launch(hipStream_t s, const DenseParams &P, bool gated) {
-  const int64_t width = gated ? P.N : P.out.width;
-  int64_t groups = ceil_div(P.batch * P.M * ceil_div(width, 4), 256);
-  if (groups > 4096) groups = 4096;
-  if (gated) hipLaunchKernelGGL((dense_reduce_kernel<true>), dim3((unsigned)groups), dim3(256), 0, s, P, width);
-  else hipLaunchKernelGGL((dense_reduce_kernel<false>), dim3((unsigned)groups), dim3(256), 0, s, P, width);
+static hipError_t dense_reduce_launch(hipStream_t s, const DenseParams &P, int b, bool gated) {
+  const int across = (gated ? b / 2 : b) / 32;
+  const dim3 grid((unsigned)(P.rest * across * (b / 32)));
+  if (!gated) hipLaunchKernelGGL((dense_reduce_kernel<0>), grid, dim3(256), 0, s, P, b);
+  else if (b > 64) hipLaunchKernelGGL((dense_reduce_kernel<32>), grid, dim3(256), 0, s, P, b);
+  else hipLaunchKernelGGL((dense_reduce_kernel<16>), grid, dim3(256), 0, s, P, b);
   return hipGetLastError();
 }
 
 // Whether the operands, the room for parts and the grid are what the kernels take.
-static bool fits(const TileChoice &c, const DenseDesc &d) {
-  if (c.splits > 1 && (d.partial == nullptr || d.partial_bytes < partial_bytes(c, d))) return false;
+static bool fits(const DenseChoice &c, const DenseDesc &d) {
+  if (c.splits > 1 && (d.partial == nullptr || d.partial_bytes < partial_bytes(c))) return false;
   if (d.symmetric && (d.M != d.N || d.gated)) return false;
   const auto pieces = [](const void *p, int64_t ld) { return p != nullptr && ((uintptr_t)p & 15) == 0 && ld % 16 == 0 && ld <= kMaxLd; };
-  return pieces(d.A, d.lda) && pieces(d.B, d.ldb) && dense_tiles(d, c.bm) * c.splits * d.batch < (1 << 22);
+  return pieces(d.A, d.lda) && pieces(d.B, d.ldb) && c.whole + c.rest * c.splits < (1 << 22);
 }
 
 hipError_t dense_nt_launch(rsvd_ctx *ctx, hipStream_t s, const DenseDesc &d) {
-  const TileChoice c = dense_choose(ctx, d);
+  const DenseChoice c = dense_choose(ctx, d);
   if (!fits(c, d) || (d.kind < DK_F8 && d.K % 8 != 0)) return hipErrorInvalidValue;
   const DenseParams P = dense_params(c, d);
   hipError_t e = hipErrorInvalidValue;
-  if (d.kind == DK_BF16 && d.gated) e = dense_nt_tile<DK_BF16, true>(s, P, c.bm);
-  else if (d.kind == DK_F16 && d.gated) e = dense_nt_tile<DK_F16, true>(s, P, c.bm);
-  else if (d.kind == DK_F16) e = dense_nt_tile<DK_F16, false>(s, P, c.bm);
-  else if (d.kind == DK_F8 && !d.gated) e = dense_nt_tile<DK_F8, false>(s, P, c.bm);
-  else if (d.kind == DK_F8_EXACT && !d.gated) e = dense_nt_tile<DK_F8_EXACT, false>(s, P, c.bm);
-  return e == hipSuccess && c.splits > 1 ? dense_reduce_launch(s, P, d.gated) : e;
+  if (d.kind == DK_BF16 && d.gated) e = dense_nt_tile<DK_BF16, true>(s, P, c.b);
+  else if (d.kind == DK_F16 && d.gated) e = dense_nt_tile<DK_F16, true>(s, P, c.b);
+  else if (d.kind == DK_F16) e = dense_nt_tile<DK_F16, false>(s, P, c.b);
+  else if (d.kind == DK_F8 && !d.gated) e = dense_nt_tile<DK_F8, false>(s, P, c.b);
+  else if (d.kind == DK_F8_EXACT && !d.gated) e = dense_nt_tile<DK_F8_EXACT, false>(s, P, c.b);
+  return e == hipSuccess && c.splits > 1 ? dense_reduce_launch(s, P, c.b, d.gated) : e;
 }
 
 hipError_t dense_kn_launch(rsvd_ctx *ctx, hipStream_t s, const DenseDesc &d, bool a_krows) {
-  const TileChoice c = dense_choose(ctx, d);
+  const DenseChoice c = dense_choose(ctx, d);
   if (!fits(c, d) || d.kind >= DK_F8 || d.gated) return hipErrorInvalidValue;
   const DenseParams P = dense_params(c, d);
   hipError_t e;
-  if (d.kind == DK_BF16) e = a_krows ? dense_kn_tile<DK_BF16, true>(s, P, c.bm) : dense_kn_tile<DK_BF16, false>(s, P, c.bm);
-  else e = a_krows ? dense_kn_tile<DK_F16, true>(s, P, c.bm) : dense_kn_tile<DK_F16, false>(s, P, c.bm);
-  return e == hipSuccess && c.splits > 1 ? dense_reduce_launch(s, P, false) : e;
+  if (d.kind == DK_BF16) e = a_krows ? dense_kn_tile<DK_BF16, true>(s, P, c.b) : dense_kn_tile<DK_BF16, false>(s, P, c.b);
+  else e = a_krows ? dense_kn_tile<DK_F16, true>(s, P, c.b) : dense_kn_tile<DK_F16, false>(s, P, c.b);
+  return e == hipSuccess && c.splits > 1 ? dense_reduce_launch(s, P, c.b, false) : e;
 }
 
 hipError_t dense_init_device(rsvd_ctx *) {

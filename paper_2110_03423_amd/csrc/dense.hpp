@@ -104,7 +104,7 @@ hipError_t f8_few_launch(rsvd_ctx *ctx, hipStream_t s, const F8FewDesc &d);
 
 // ---------------------------------------------------------------- orthogonal.hip
 // |G| of every matrix by parts (kNormParts doubles each), and G / |G| times 2^13 as one or two fp16 planes with zeros up to `width`.
-constexpr int kNormParts = 64;
+constexpr int kNormParts = 256;
 hipError_t norm_launch(hipStream_t s, rsvd_xtype type, int batch, int64_t m, int64_t n, const void *G, int64_t ldg, int64_t stride, double *parts);
 hipError_t unit_launch(hipStream_t s, rsvd_xtype type, int batch, int64_t m, int64_t n, const void *G, int64_t ldg, int64_t stride, const double *parts,
                        uint16_t *X, int64_t width, int64_t plane, int planes);

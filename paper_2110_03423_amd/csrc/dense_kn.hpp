@@ -25,10 +25,9 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void dense_kn_kernel(const Dense
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
   const int wave_m = wave / WGN, wave_n = wave % WGN, wm0 = wave_m * WM, wn0 = wave_n * WN;
-  int tile_m, tile_n, split, batch;
-  dense_tile_of(P, tile_m, tile_n, split, batch);
+  const DenseWork work = dense_work<BM * BN>(P);
+  const int tile_m = work.tile_m, tile_n = work.tile_n, batch = work.batch, kt_begin = work.kt_begin, nkt = work.nkt;
   const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
-  const int kt_begin = split * P.kt_per_split, nkt = P.kt_all - kt_begin < P.kt_per_split ? P.kt_all - kt_begin : P.kt_per_split;
 
   f32x4 acc[TM][TN];
 #pragma unroll
@@ -157,10 +156,11 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void dense_kn_kernel(const Dense
       if (kt + 1 < nkt) tile(1, std::integral_constant<int, 0>());
     }
   }
+  float *const partial = work.partial != nullptr ? work.partial + wm0 * BN + wn0 : nullptr;
   int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
   asm volatile("" : "+v"(last_lane));
   // (behind the last meeting nobody reads the tiles)
-  dense_finish<TM, TN>(P, acc, split, batch, m0 + wm0, n0 + wn0, P.symmetric && tile_m != tile_n, last_lane,
+  dense_finish<BN, TM, TN>(P, acc, partial, batch, m0 + wm0, n0 + wn0, P.symmetric && tile_m != tile_n, last_lane,
                        reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
 }
 

@@ -21,8 +21,8 @@
 
 namespace rsvd {
 
-template <int BM, int BN> struct DenseNtCfg {
-  static constexpr int STAGE = (BM + BN) * 128, RING = BM == 64 ? 3 : 2;
+template <int KIND, int BM, int BN> struct DenseNtCfg {
+  static constexpr int POWERS = (BM + BN) * 128, STAGE = POWERS + (KIND >= DK_F8 ? (BM + BN) * 4 : 0), RING = BM == 64 ? 3 : 2;      // behind the codes, a word of powers a row
   static constexpr size_t lds = RING * (size_t)STAGE;      // (more than the wavefronts need in the end)
 };
 
@@ -77,16 +77,15 @@ __device__ __forceinline__ i32x8 f8_both(const u32x4 (&p)[2]) {
 
 template <int KIND, bool GATED, int BM, int BN, int WGM, int WGN>
 __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_kernel(const DenseParams P) {
-  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = DenseNtCfg<BM, BN>::STAGE, RING = DenseNtCfg<BM, BN>::RING;
+  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = DenseNtCfg<KIND, BM, BN>::STAGE, RING = DenseNtCfg<KIND, BM, BN>::RING;
   constexpr bool CODES = KIND >= DK_F8;
   extern __shared__ __attribute__((aligned(16))) char dense_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
   const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
-  int tile_m, tile_n, split, batch;
-  dense_tile_of(P, tile_m, tile_n, split, batch);
+  const DenseWork work = dense_work<BM * BN>(P);
+  const int tile_m = work.tile_m, tile_n = work.tile_n, batch = work.batch, kt_begin = work.kt_begin, nkt = work.nkt;
   const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * (GATED ? BN / 2 : BN);
-  const int kt_begin = split * P.kt_per_split, nkt = P.kt_all - kt_begin < P.kt_per_split ? P.kt_all - kt_begin : P.kt_per_split;
 
   f32x4 acc[TM][TN];
 #pragma unroll
@@ -102,7 +101,17 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
   DenseLoad<NT, BN, PAIRED, !GATED ? 0 : PAIRED ? 32 : 16> lb;
   la.init(P.lda, P.M - m0, tid);
   lb.init(P.ldb, P.N - n0, tid);
-  constexpr int LOADS = decltype(la)::N + decltype(lb)::N;
+  // of codes, too: the words that hold the powers of the tile's rows, one row a lane (small tiles: by two wavefronts each)
+  constexpr int POWER_LOADS = !CODES ? 0 : BM + BN < NT ? 1 : (BM + BN) / NT, LOADS = decltype(la)::N + decltype(lb)::N + POWER_LOADS;
+  uint32_t pow_off[CODES ? POWER_LOADS : 1];
+  if constexpr (CODES) {
+#pragma unroll
+    for (int i = 0; i < POWER_LOADS; ++i) {
+      const int r = (tid + NT * i) & (BM + BN - 1);
+      const int64_t m = m0 + r < P.M ? m0 + r : P.M - 1, n = n0 + r - BM < P.N ? n0 + r - BM : P.N - 1;
+      pow_off[i] = r < BM ? (uint32_t)((m >> P.a_shift) * P.ld_apow) : (uint32_t)((n >> P.b_shift) * P.ld_bpow);
+    }
+  }
   const char *const a_row = P.A + batch * P.a_batch + m0 * P.lda, *const b_row = P.B + batch * P.b_batch + n0 * P.ldb;
   const int last_left = (int)((P.K * (CODES ? 1 : 2) - (int64_t)(P.ktiles - 1) * 128) >> 4);      // pieces of the last k-tile that exist
 
@@ -127,47 +136,17 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
   };
   auto issue = [&](int kt, int l) RSVD_INLINE {
     char *st = dense_lds + (kt % RING) * STAGE;
-    if (l < decltype(la)::N) la.issue(l, a_now, 0, st, left, wave, tid);
-    else lb.issue(l - decltype(la)::N, b_now, P.b_up, st + BM * 128, left, wave, tid);
-  };
-
-  // powers of four k-tiles at a time, fetched four ahead
-  unsigned pa[2][CODES ? TM : 1], pb[2][CODES ? TN : 1];
-  const uint8_t *a_pow[CODES ? TM : 1], *b_pow[CODES ? TN : 1];
-  if constexpr (CODES) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int64_t m = m0 + wm0 + 16 * i + r16;
-      a_pow[i] = P.a_pow + ((m < P.M ? m : P.M - 1) >> P.a_shift) * P.ld_apow;
-    }
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int64_t n = n0 + wn0 + 32 * (j / 2) + 8 * (r16 >> 2) + 4 * (j & 1) + (r16 & 3);
-      b_pow[j] = P.b_pow + ((n < P.N ? n : P.N - 1) >> P.b_shift) * P.ld_bpow;
-    }
-  }
-  auto fetch_powers = [&](int kt) RSVD_INLINE {         // (of the range's k-tile kt, a multiple of four; behind the last: those again)
-    const int at = kt_begin + (kt < nkt ? kt : (nkt - 1) & ~3);
-#pragma unroll
-    for (int i = 0; i < (CODES ? TM : 0); ++i) pa[1][i] = *reinterpret_cast<const unsigned *>(a_pow[i] + at);
-#pragma unroll
-    for (int j = 0; j < (CODES ? TN : 0); ++j) pb[1][j] = *reinterpret_cast<const unsigned *>(b_pow[j] + at);
-  };
-  auto take_powers = [&](int kt) RSVD_INLINE {
-    if ((kt & 3) == 0) {
-#pragma unroll
-      for (int i = 0; i < (CODES ? TM : 0); ++i) pa[0][i] = pa[1][i];
-#pragma unroll
-      for (int j = 0; j < (CODES ? TN : 0); ++j) pb[0][j] = pb[1][j];
-      fetch_powers(kt + 4);
-    } else {
-#pragma unroll
-      for (int i = 0; i < (CODES ? TM : 0); ++i) pa[0][i] >>= 8;
-#pragma unroll
-      for (int j = 0; j < (CODES ? TN : 0); ++j) pb[0][j] >>= 8;
+    if (l < decltype(la)::N) {
+      la.issue(l, a_now, 0, st, left, wave, tid);
+    } else if (l < decltype(la)::N + decltype(lb)::N) {
+      lb.issue(l - decltype(la)::N, b_now, P.b_up, st + BM * 128, left, wave, tid);
+    } else if constexpr (CODES) {
+      const int i = l - decltype(la)::N - decltype(lb)::N, first = (wave * 64 + NT * i) & (BM + BN - 1);
+      const uint8_t *base = (first < BM ? P.a_pow : P.b_pow) + (next_kt & ~3);
+      const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00027000);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(all, (__attribute__((address_space(3))) void *)(st + DenseNtCfg<KIND, BM, BN>::POWERS + first * 4), 4, pow_off[i], 0, 0, 0);
     }
   };
-  if constexpr (CODES) fetch_powers(0);
 
   constexpr int AHEAD = TM >= 4 ? 3 : 1;               // rows of blocks read ahead, not all of them: registers
   constexpr int FIRST = KIND == DK_F8 || LOADS < 2 * AHEAD ? LOADS : 2 * AHEAD;      // loads of a tile that are issued behind a meeting
@@ -179,6 +158,23 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
   };
   auto piece_b = [&](int kt, int j, int h) RSVD_INLINE {
     return *reinterpret_cast<const u32x4 *>(b_lds + (kt % RING) * STAGE + (PAIRED ? j / 2 * 4096 + (j & 1) * 512 : j * 2048) + (((4 * h + kq) ^ b_swz) << 4));
+  };
+  // powers of the rows of a lane's blocks: in words of four k-tiles, and of the one that is multiplied
+  unsigned words_a[CODES ? TM : 1], words_b[CODES ? TN : 1], pa[CODES ? TM : 1], pb[CODES ? TN : 1];
+  const char *const pow_lds = dense_lds + DenseNtCfg<KIND, BM, BN>::POWERS;
+  auto read_powers = [&](int kt) RSVD_INLINE {
+#pragma unroll
+    for (int i = 0; i < (CODES ? TM : 0); ++i) words_a[i] = *reinterpret_cast<const unsigned *>(pow_lds + (kt % RING) * STAGE + (wm0 + 16 * i + r16) * 4);
+#pragma unroll
+    for (int j = 0; j < (CODES ? TN : 0); ++j)
+      words_b[j] = *reinterpret_cast<const unsigned *>(pow_lds + (kt % RING) * STAGE + (BM + wn0 + 32 * (j / 2) + 4 * (j & 1) + b_first) * 4);
+  };
+  auto take_powers = [&](int kt) RSVD_INLINE {
+    const int by = 8 * ((kt_begin + kt) & 3);
+#pragma unroll
+    for (int i = 0; i < (CODES ? TM : 0); ++i) pa[i] = words_a[i] >> by;
+#pragma unroll
+    for (int j = 0; j < (CODES ? TN : 0); ++j) pb[j] = words_b[j] >> by;
   };
   // Everybody has read its last of the tile before kt, and kt has arrived: `flying` loads are of later tiles.
   auto meet = [&](auto flying, int kt) RSVD_INLINE {
@@ -219,10 +215,11 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
       for (int h = 0; h < 2; ++h) b[j][h] = piece_b(0, j, h);
 #pragma unroll
     for (int h = 0; h < 2; ++h) a[0][h] = piece_a(0, 0, h);
+    read_powers(0);
     for (int kt = 0; kt < nkt; ++kt) {
       take_powers(kt);
       auto multiply = [&](int i, int j) RSVD_INLINE {
-        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_both(b[j]), f8_both(a[i % (AHEAD + 1)]), acc[i][j], 0, 0, 0, (int)pb[0][j], 0, (int)pa[0][i]);
+        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_both(b[j]), f8_both(a[i % (AHEAD + 1)]), acc[i][j], 0, 0, 0, (int)pb[j], 0, (int)pa[i]);
       };
 #pragma unroll
       for (int i = 1; i < AHEAD; ++i)
@@ -241,6 +238,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
       advance();
 #pragma unroll
       for (int h = 0; h < 2; ++h) a[0][h] = piece_a(kt + 1, 0, h);
+      read_powers(kt + 1);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
 #pragma unroll
@@ -261,6 +259,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
     for (int j = 0; j < TN; ++j) b[0][j] = piece_b(0, j, 0);
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) a[i] = piece_a(0, i, 0);
+    if constexpr (CODES) read_powers(0);
+    u32x4 wide[Q == 2 ? TN : 1][2];
     for (int kt = 0; kt < nkt; ++kt) {
       if constexpr (CODES) take_powers(kt);
       __builtin_amdgcn_sched_barrier(0);
@@ -270,8 +270,9 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
         if (step == 2 * TM - AHEAD) {
           meet(std::integral_constant<int, (RING - 2) * LOADS>(), kt + 1);
           advance();
+          if constexpr (CODES) read_powers(kt + 1);
         }
-        u32x4 now = a[step % (AHEAD + 1)];
+        const u32x4 now = a[step % (AHEAD + 1)];
         a[ahead % (AHEAD + 1)] = piece_a(ahead < 2 * TM ? kt : kt + 1, ahead % TM, ahead / TM % 2);
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
@@ -280,14 +281,15 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
         }
         if constexpr (KIND == DK_F8_EXACT) {
           u32x4 wide_a[2];
-          f8_widen(now, f8_unit(pa[0][i] & 255u), wide_a);
+          f8_widen(now, f8_unit(pa[i] & 255u), wide_a);
+          if (i == 0) {
 #pragma unroll
-          for (int j = 0; j < TN; ++j) {
-            u32x4 wide_b[2];
-            f8_widen(b[h][j], f8_unit(pb[0][j] & 255u), wide_b);
-#pragma unroll
-            for (int q = 0; q < Q; ++q) acc[i][j] = mfma_bf16(wide_b[q], wide_a[q], acc[i][j]);
+            for (int j = 0; j < TN; ++j) f8_widen(b[h][j], f8_unit(pb[j] & 255u), wide[j]);
           }
+#pragma unroll
+          for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(wide[j][q], wide_a[q], acc[i][j]);
         } else {
 #pragma unroll
           for (int j = 0; j < TN; ++j) acc[i][j] = KIND == DK_BF16 ? mfma_bf16(b[h][j], now, acc[i][j]) : mfma_f16(b[h][j], now, acc[i][j]);
@@ -302,20 +304,21 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
   }
 
   const int64_t m1 = m0 + wm0, n1 = n0 + (GATED ? wn0 / 2 : wn0);
+  float *const partial = work.partial != nullptr ? work.partial + wm0 * BN + wn0 : nullptr;
   int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
   asm volatile("" : "+v"(last_lane));
-  dense_finish_rows<GATED, TM, TN>(P, acc, split, batch, m1, n1, last_lane);
+  dense_finish_rows<GATED, BN, TM, TN>(P, acc, partial, batch, m1, n1, last_lane);
   if constexpr (!GATED && !CODES) {
-    if (P.symmetric && tile_m != tile_n) {
+    if (P.symmetric && tile_m != tile_n && partial == nullptr) {
       __builtin_amdgcn_s_waitcnt(tile_wait(0));          // (nothing may land in LDS any more)
       __syncthreads();
-      dense_finish_mirror<TM, TN>(P, acc, split, batch, m1, n1, last_lane, reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
+      dense_finish_mirror<TM, TN>(P, acc, batch, m1, n1, last_lane, reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
     }
   }
 }
 
 template <int KIND, bool GATED, int BM, int BN, int WGM, int WGN> hipError_t dense_nt_run(hipStream_t s, const DenseParams &P) {
-  hipLaunchKernelGGL((dense_nt_kernel<KIND, GATED, BM, BN, WGM, WGN>), dim3(dense_groups(P)), dim3(64 * WGM * WGN), (DenseNtCfg<BM, BN>::lds), s, P);
+  hipLaunchKernelGGL((dense_nt_kernel<KIND, GATED, BM, BN, WGM, WGN>), dim3(dense_groups(P)), dim3(64 * WGM * WGN), (DenseNtCfg<KIND, BM, BN>::lds), s, P);
   return hipGetLastError();
 }
 template <int KIND, bool GATED> hipError_t dense_nt_tile(hipStream_t s, const DenseParams &P, int b) {
@@ -325,7 +328,7 @@ template <int KIND, bool GATED> hipError_t dense_nt_tile(hipStream_t s, const De
 }
 template <int KIND, bool GATED> hipError_t dense_nt_init() {
   return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, 256, 256, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)DenseNtCfg<256, 256>::lds);
+                             (int)DenseNtCfg<KIND, 256, 256>::lds);
 }
 #define DENSE_NT(KIND, GATED)                                                                        \
   template hipError_t dense_nt_tile<KIND, GATED>(hipStream_t s, const DenseParams &P, int b);       \

@@ -15,9 +15,11 @@ struct DenseParams {
   const uint8_t *a_pow, *b_pow; int64_t ld_apow, ld_bpow; int a_shift, b_shift;
   DenseSegs segs;
   int64_t M, N, K;
-  int ktiles, tiles_m, tiles_n, tiles, splits, kt_all, kt_per_split, batch;      // tiles: of a problem; k-tiles: of a part of k, and of all
+  int ktiles, tiles_m, tiles_n, tiles, batch;      // k-tiles of a part of k; tiles of a problem
+  int kt_all;                              // k-tiles
+  int whole, rest, splits, kt_per_split;   // tiles of all problems that are worked out at once, and behind them those whose k is in `splits` ranges
   int symmetric;
-  float *partial;                          // splits > 1: [batch][split][M][columns], of gated products gate and up side by side
+  float *partial;                          // [rest][splits][tile], fp32
   LinearOut out;
   GatedOut gate;
 };
@@ -26,16 +28,8 @@ __device__ __forceinline__ f32x4 mfma_f16(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 
-// Tiles: a contiguous run for each of the eight XCDs, which have an L2 each, problem by problem, range of k by range of k.  Within one, strips of eight rows of
-// tiles, column by column; of symmetric results the tiles on and below the diagonal, row by row.
-__device__ __forceinline__ void dense_tile_of(const DenseParams &P, int &tile_m, int &tile_n, int &split, int &batch) {
-  const int total = (int)gridDim.x, pid = (int)blockIdx.x;
-  const int per = (total + 7) >> 3, tall = (total & 7) ? (total & 7) : 8, xcd = pid & 7, local = pid >> 3;
-  int t = xcd < tall ? xcd * per + local : tall * per + (xcd - tall) * (per - 1) + local;
-  batch = __builtin_amdgcn_readfirstlane(t / (P.tiles * P.splits));
-  t -= batch * P.tiles * P.splits;
-  split = __builtin_amdgcn_readfirstlane(t / P.tiles);
-  t -= split * P.tiles;
+// Where tile t of a problem lies: strips of eight rows of tiles, column by column; of symmetric results the tiles on and below the diagonal, row by row.
+__device__ __forceinline__ void dense_place(const DenseParams &P, int t, int &tile_m, int &tile_n) {
   if (P.symmetric) {
     int row = (int)((__builtin_sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
     while (row * (row + 1) / 2 > t) --row;                // (the root is rounded)
@@ -49,6 +43,47 @@ __device__ __forceinline__ void dense_tile_of(const DenseParams &P, int &tile_m,
   t -= strip * 8 * P.tiles_n;
   tile_n = __builtin_amdgcn_readfirstlane(t / high);
   tile_m = first + t - tile_n * high;
+}
+
+// What a workgroup works out.
+struct DenseWork {
+  int tile_m, tile_n, batch, kt_begin, nkt;
+  float *partial;                          // the tile's place for a range of k, or NULL
+};
+// Workgroups of the whole tiles first, then range of k by range of k those of the rest; in each a contiguous run for each of the eight XCDs, which have an L2 each.
+template <int SIZE> __device__ __forceinline__ DenseWork dense_work(const DenseParams &P) {
+  DenseWork w;
+  const bool part = (int)blockIdx.x >= P.whole;
+  const int total = part ? P.rest * P.splits : P.whole, pid = (int)blockIdx.x - (part ? P.whole : 0);
+  const int per = (total + 7) >> 3, tall = (total & 7) ? (total & 7) : 8, xcd = pid & 7, local = pid >> 3;
+  int t = xcd < tall ? xcd * per + local : tall * per + (xcd - tall) * (per - 1) + local;
+  w.kt_begin = 0;
+  w.nkt = P.kt_all;
+  w.partial = nullptr;
+  if (part) {
+    const int split = __builtin_amdgcn_readfirstlane(t / P.rest);
+    t -= split * P.rest;
+    w.partial = P.partial + ((int64_t)t * P.splits + split) * SIZE;
+    w.kt_begin = split * P.kt_per_split;
+    w.nkt = P.kt_all - w.kt_begin < P.kt_per_split ? P.kt_all - w.kt_begin : P.kt_per_split;
+    t += P.whole;
+  }
+  w.batch = __builtin_amdgcn_readfirstlane(t / P.tiles);
+  dense_place(P, __builtin_amdgcn_readfirstlane(t - w.batch * P.tiles), w.tile_m, w.tile_n);
+  return w;
+}
+
+// Eight numbers as fp32.
+template <int XT> __device__ __forceinline__ void x_values(const Raw8<XT> &r, float (&v)[8]) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if constexpr (XT == RSVD_X_F32) v[e] = __uint_as_float(r.w[e >> 2][e & 3]);
+    else if constexpr (XT == RSVD_X_BF16) v[e] = e & 1 ? bf16_high(r.w[0][e >> 1]) : bf16_low(r.w[0][e >> 1]);
+    else {
+      const unsigned pair = r.w[0][e >> 1];
+      v[e] = (float)__builtin_bit_cast(f16x2, pair)[e & 1];
+    }
+  }
 }
 
 // ---------------------------------------------------------------- four consecutive results
@@ -334,37 +369,27 @@ __device__ __forceinline__ void gated_end1(const GatedOut &O, int64_t N, int64_t
 }
 
 // ---------------------------------------------------------------- the end of a wavefront's TM x TN blocks of 16 x 16
-// (m1, n1): the first row and column of the wavefront's.  partial: the sums are a part, one range of k.
-__device__ __forceinline__ float *partial_of(const DenseParams &P, int split, int batch, int64_t columns) {
-  return P.partial + ((int64_t)batch * P.splits + split) * P.M * columns;
-}
+// (m1, n1): the first row and column of the wavefront's.  partial: where its first sum goes if it has a range of k, rows of BN sums; or NULL.
 
 // Sixteen rows of a wavefront's blocks in LDS, with their rows and columns exchanged: lane e has column e / 4 and four of the rows.
-template <int TN> __device__ __forceinline__ void mirror_rows(const DenseParams &P, float *partial, int batch, int64_t m2, int64_t n1, int lane, const float *lds) {
+template <int TN> __device__ __forceinline__ void mirror_rows(const DenseParams &P, int batch, int64_t m2, int64_t n1, int lane, const float *lds) {
   constexpr int PITCH = 16 * TN + 4;
-  const int64_t width = P.splits > 1 ? P.N : P.out.width;
 #pragma unroll 1
   for (int e = lane; e < 64 * TN; e += 64) {
     const int c = e >> 2, q = 4 * (e & 3);
     f32x4 v;
 #pragma unroll
     for (int x = 0; x < 4; ++x) v[x] = lds[(q + x) * PITCH + c];
-    const int64_t mm = n1 + c, nn = m2 + q;
-    if (mm < P.M && nn < width) {
-      if (P.splits > 1) put4<RSVD_X_F32>(partial, mm * P.N + nn, left_of(nn, P.N), v);
-      else linear_end1(P.out, P.N, batch, mm, nn, v);
-    }
+    if (n1 + c < P.M && m2 + q < P.out.width) linear_end1(P.out, P.N, batch, n1 + c, m2 + q, v);
   }
 }
 
 // Block (i, j) of lane L holds row 16 i + L % 16 and four columns from 16 j + 4 (L / 16) on: through LDS, sixteen rows at a time, so that lanes next to each
 // other write what is next to each other.  mirror: and the same with rows and columns exchanged.  lds: the wavefront's finish_lds<TN>() bytes.
-template <int TM, int TN>
-__device__ __forceinline__ void dense_finish(const DenseParams &P, f32x4 (&acc)[TM][TN], int split, int batch, int64_t m1, int64_t n1, bool mirror, int lane, float *lds) {
+template <int BN, int TM, int TN>
+__device__ __forceinline__ void dense_finish(const DenseParams &P, f32x4 (&acc)[TM][TN], float *partial, int batch, int64_t m1, int64_t n1, bool mirror, int lane, float *lds) {
   constexpr int PITCH = 16 * TN + 4, PER_ROW = 4 * TN, ROWS = 64 / PER_ROW, PASSES = 16 / ROWS, C = PASSES < 4 ? PASSES : 4;
   const int r16 = lane & 15, kq = lane >> 4, row = lane / PER_ROW, col = 4 * (lane % PER_ROW);
-  float *const partial = partial_of(P, split, batch, P.N);
-  const int64_t width = P.splits > 1 ? P.N : P.out.width;
   const bool whole = m1 + 16 * TM <= P.M && n1 + 16 * TN <= P.N;
 #pragma unroll 1
   for (int i = 0; i < TM; ++i) {                        // (one copy of what follows, not one for each row of blocks)
@@ -386,29 +411,27 @@ __device__ __forceinline__ void dense_finish(const DenseParams &P, f32x4 (&acc)[
         v[c][0] = *reinterpret_cast<const f32x4 *>(lds + ((p + c) * ROWS + row) * PITCH + col);
         m[c] = m1 + 16 * i + (p + c) * ROWS + row;
         n[c] = n1 + col;
-        there[c] = m[c] < P.M && n[c] < width;
+        there[c] = m[c] < P.M && n[c] < P.out.width;
       }
-      if (P.splits > 1) {
+      if (partial != nullptr) {
 #pragma unroll
-        for (int c = 0; c < C; ++c)
-          if (there[c]) put4<RSVD_X_F32>(partial, m[c] * P.N + n[c], left_of(n[c], P.N), v[c][0]);
+        for (int c = 0; c < C; ++c) *reinterpret_cast<f32x4 *>(partial + (16 * i + (p + c) * ROWS + row) * BN + col) = v[c][0];
       } else if (whole) {
         linear_end<C, 1, true>(P.out, P.N, batch, m, n, there, v);
       } else {
         linear_end<C, 1, false>(P.out, P.N, batch, m, n, there, v);
       }
     }
-    if (mirror) mirror_rows<TN>(P, partial, batch, m1 + 16 * i, n1, lane, lds);
+    if (mirror && partial == nullptr) mirror_rows<TN>(P, batch, m1 + 16 * i, n1, lane, lds);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
   }
 }
 
 // The mirrored half for blocks in the order of dense_finish_rows.
-template <int TM, int TN> __device__ __forceinline__ void dense_finish_mirror(const DenseParams &P, f32x4 (&acc)[TM][TN], int split, int batch, int64_t m1, int64_t n1, int lane, float *lds) {
+template <int TM, int TN> __device__ __forceinline__ void dense_finish_mirror(const DenseParams &P, f32x4 (&acc)[TM][TN], int batch, int64_t m1, int64_t n1, int lane, float *lds) {
   constexpr int PITCH = 16 * TN + 4;
   const int r16 = lane & 15, kq = lane >> 4;
-  float *const partial = partial_of(P, split, batch, P.N);
 #pragma unroll 1
   for (int i = 0; i < TM; ++i) {
 #pragma unroll
@@ -419,7 +442,7 @@ template <int TM, int TN> __device__ __forceinline__ void dense_finish_mirror(co
       }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
-    mirror_rows<TN>(P, partial, batch, m1 + 16 * i, n1, lane, lds);
+    mirror_rows<TN>(P, batch, m1 + 16 * i, n1, lane, lds);
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();
   }
@@ -427,10 +450,9 @@ template <int TM, int TN> __device__ __forceinline__ void dense_finish_mirror(co
 
 // Blocks (i, 2 p) and (i, 2 p + 1) of lane L hold row 16 i + L % 16 and eight columns from 32 p + 8 (L / 16) on: stored as they are.  gated: p even is the gate and p odd the
 // up projection of 32 outputs; with two blocks, these are the gate and the up projection of sixteen, four of them a lane.
-template <bool GATED, int TM, int TN> __device__ __forceinline__ void dense_finish_rows(const DenseParams &P, f32x4 (&acc)[TM][TN], int split, int batch, int64_t m1, int64_t n1, int lane) {
+template <bool GATED, int BN, int TM, int TN> __device__ __forceinline__ void dense_finish_rows(const DenseParams &P, f32x4 (&acc)[TM][TN], float *partial, int batch, int64_t m1, int64_t n1,
+                                                                                               int lane) {
   constexpr int V = GATED && TN == 2 ? 1 : 2, C = GATED ? TN / (2 * V) : TN / 2;      // groups of a row, and vectors of four in each
-  const int64_t columns = GATED ? 2 * P.N : P.N, width = GATED || P.splits > 1 ? P.N : P.out.width;
-  float *const partial = partial_of(P, split, batch, columns);
   const bool whole = m1 + 16 * TM <= P.M && n1 + 4 * V * 4 * C <= P.N;
   int64_t m[C], n[C];
   bool there[C];
@@ -453,14 +475,16 @@ template <bool GATED, int TM, int TN> __device__ __forceinline__ void dense_fini
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       m[c] = m1 + 16 * i + (lane & 15);
-      there[c] = m[c] < P.M && n[c] < width;
+      there[c] = m[c] < P.M && n[c] < (GATED ? P.N : P.out.width);
     }
-    if (P.splits > 1) {
+    if (partial != nullptr) {
+      float *to = partial + (16 * i + (lane & 15)) * BN + 4 * V * (lane >> 4);
 #pragma unroll
       for (int c = 0; c < C; ++c)
-        if (there[c]) {
-          put_row<RSVD_X_F32, V>(partial, m[c] * columns + n[c], left_of<V>(n[c], P.N), v[c]);
-          if constexpr (GATED) put_row<RSVD_X_F32, V>(partial, m[c] * columns + P.N + n[c], left_of<V>(n[c], P.N), u[c]);
+#pragma unroll
+        for (int y = 0; y < V; ++y) {
+          *reinterpret_cast<f32x4 *>(to + (GATED ? 32 * V : 16 * V) * c + 4 * y) = v[c][y];
+          if constexpr (GATED) *reinterpret_cast<f32x4 *>(to + 32 * V * c + 16 * V + 4 * y) = u[c][y];
         }
     } else if constexpr (GATED) {
       if (whole) gated_end<C, V, true>(P.gate, P.N, m, n, there, v, u);
@@ -472,30 +496,54 @@ template <bool GATED, int TM, int TN> __device__ __forceinline__ void dense_fini
   }
 }
 
-// Ranges of k added up, in their order.
-template <bool GATED> __global__ __launch_bounds__(256) void dense_reduce_kernel(const DenseParams P, int64_t width) {
-  const int64_t columns = GATED ? 2 * P.N : P.N, per_row = (width + 3) / 4, total = (int64_t)P.batch * P.M * per_row;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
-    const int64_t row = e / per_row, n = (e - row * per_row) * 4, batch = row / P.M, m = row - batch * P.M;
-    const float *p = P.partial + (batch * P.splits * P.M + m) * columns + n;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f}, u = v;
-    const int left = left_of(n, P.N);
-#pragma unroll 4
-    for (int s = 0; s < P.splits; ++s, p += P.M * columns) {
-      v += load4<RSVD_X_F32>(p, 0, left);
-      if constexpr (GATED) u += load4<RSVD_X_F32>(p + P.N, 0, left);
+// Ranges of k added up, in their order: 32 x 32 sums a workgroup, four a thread.  GROUP: outputs whose gate stands before their up projection (0: no gate).
+template <int GROUP> __global__ __launch_bounds__(256) void dense_reduce_kernel(const DenseParams P, int b) {
+  const int across = (GROUP ? b / 2 : b) / 32, shares = across * (b / 32), q = (int)blockIdx.x / shares, share = (int)blockIdx.x - q * shares;
+  const int t = P.whole + q, batch = t / P.tiles, tid = threadIdx.x;
+  int tile_m, tile_n;
+  dense_place(P, t - batch * P.tiles, tile_m, tile_n);
+  const int64_t size = (int64_t)b * b;
+  const int row0 = share / across * 32, col0 = share % across * 32, row = row0 + (tid >> 3), col = col0 + 4 * (tid & 7);
+  const int64_t m0 = (int64_t)tile_m * b, n0 = (int64_t)tile_n * (GROUP ? b / 2 : b), width = GROUP ? P.N : P.out.width;
+  const bool mirror = GROUP == 0 && P.symmetric && tile_m != tile_n;
+  if (m0 + row0 >= P.M || (n0 + col0 >= width && !mirror)) return;
+  auto add = [&](int at) RSVD_INLINE {
+    const float *p = P.partial + (int64_t)q * P.splits * size + at;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < P.splits; s += 8) {
+      f32x4 v[8];                                        // (eight loads in flight)
+#pragma unroll
+      for (int x = 0; x < 8; ++x) v[x] = *reinterpret_cast<const f32x4 *>(p + (s + x < P.splits ? s + x : s) * size);
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        if (s + x < P.splits) sum += v[x];
     }
-    if constexpr (GATED) gated_end1(P.gate, P.N, m, n, v, u);
-    else linear_end1(P.out, P.N, (int)batch, m, n, v);
+    return sum;
+  };
+  const int64_t m = m0 + row, n = n0 + col;
+  if constexpr (GROUP) {
+    const int at = row * b + col / GROUP * 2 * GROUP + col % GROUP;
+    const f32x4 g = add(at), u = add(at + GROUP);
+    if (m < P.M && n < width) gated_end1(P.gate, P.N, m, n, g, u);
+  } else {
+    const f32x4 v = add(row * b + col);
+    if (m < P.M && n < width) linear_end1(P.out, P.N, batch, m, n, v);
+    if (!mirror) return;
+    __shared__ __attribute__((aligned(16))) float block[32][36];
+    *reinterpret_cast<f32x4 *>(&block[tid >> 3][4 * (tid & 7)]) = v;
+    __syncthreads();
+    f32x4 w;                                             // a column and four of its rows
+#pragma unroll
+    for (int x = 0; x < 4; ++x) w[x] = block[4 * (tid & 7) + x][tid >> 3];
+    const int64_t mm = n0 + col0 + (tid >> 3), nn = m0 + row0 + 4 * (tid & 7);
+    if (mm < P.M && nn < P.out.width) linear_end1(P.out, P.N, batch, mm, nn, w);
   }
 }
 
 // ---------------------------------------------------------------- host
-// (the same for all products; TileChoice::bn counts rows of B)
-TileChoice dense_choose(const rsvd_ctx *ctx, const DenseDesc &d);
-DenseParams dense_params(const TileChoice &c, const DenseDesc &d);
-hipError_t dense_reduce_launch(hipStream_t s, const DenseParams &P, bool gated);
-inline unsigned dense_groups(const DenseParams &P) { return (unsigned)((int64_t)P.batch * P.splits * P.tiles); }
+// Tiles of b rows and columns (of gated products: of B), and which of them have their k in ranges.
+struct DenseChoice { int b; int64_t tiles, whole, rest, splits, kt, kt_per_split; };
+inline unsigned dense_groups(const DenseParams &P) { return (unsigned)(P.whole + P.rest * P.splits); }
 inline int dense_k(int kind) { return kind >= DK_F8 ? 128 : 64; }      // k of a k-tile: 128 bytes
 
 }  // namespace rsvd

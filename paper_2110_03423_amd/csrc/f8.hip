@@ -4,6 +4,7 @@
 // that is E - 8, and one more where 1.f > 1.75: read off the bits.  x 2^-e is exact, the rounding to a code (nearest, ties to even) is the conversion instruction's.
 // A block with an infinity or NaN has the byte 255 and codes that are NaN.
 #include "dense_nt.hpp"
+#include "layer8_rows.hpp"
 
 namespace rsvd {
 
@@ -26,17 +27,6 @@ __device__ __forceinline__ unsigned f8_top8(const float (&v)[8], unsigned top) {
   for (int e = 0; e < 8; ++e) top = max(top, f8_magnitude(v[e]));
   return top;
 }
-template <int XT> __device__ __forceinline__ void x_values(const Raw8<XT> &r, float (&v)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if constexpr (XT == RSVD_X_F32) v[e] = __uint_as_float(r.w[e >> 2][e & 3]);
-    else if constexpr (XT == RSVD_X_BF16) v[e] = e & 1 ? bf16_high(r.w[0][e >> 1]) : bf16_low(r.w[0][e >> 1]);
-    else {
-      const unsigned pair = r.w[0][e >> 1];
-      v[e] = (float)__builtin_bit_cast(f16x2, pair)[e & 1];
-    }
-  }
-}
 // (As integers the magnitudes' bits are ordered like them, infinity and NaN on top.)
 __device__ __forceinline__ unsigned f8_shared(unsigned top, int mask) { return max(top, (unsigned)__shfl_xor((int)top, mask)); }
 
@@ -44,10 +34,15 @@ __device__ __forceinline__ unsigned f8_shared(unsigned top, int mask) { return m
 template <int XT> __global__ __launch_bounds__(256) void f8_rows_kernel(const char *X, int64_t ldx, int64_t rows, int64_t n, uint8_t *codes, int64_t width,
                                                                        uint8_t *powers, int64_t ldp) {
   constexpr int SIZE = XTraits<XT>::SIZE;
-  const int64_t per_row = width / 16, total = rows * per_row, step = (int64_t)gridDim.x * 256;
+  const int per_row = (int)(width / 16);
+  const int64_t total = rows * per_row;
   // (whole blocks end together: eight lanes have one)
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += step) {
-    const int64_t r = e / per_row, c = (e - r * per_row) * 16;
+  for (int64_t group = blockIdx.x; group * 256 < total; group += gridDim.x) {
+    int64_t r;
+    int place;
+    piece_of(group, per_row, r, place);
+    if (r >= rows) continue;
+    const int64_t c = 16 * (int64_t)place;
     float v[2][8];
     unsigned top = 0u;
 #pragma unroll

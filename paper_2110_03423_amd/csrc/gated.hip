@@ -1,5 +1,6 @@
 // A gated block beside its large products: a few tokens, gradients of kept products, operands in the order that the products want.
 #include "dense_tile.hpp"
+#include "layer8_rows.hpp"
 
 namespace rsvd {
 
@@ -108,16 +109,26 @@ hipError_t gated_few_launch(rsvd_ctx *, hipStream_t s, const GatedFewDesc &d) {
 
 // ---------------------------------------------------------------- gradients of gate and up from the kept products; memory is the bound
 __global__ __launch_bounds__(256) void gated_slope_kernel(const GatedOut O, int64_t tokens, int64_t m) {
-  const int64_t per_row = (m + 3) / 4, total = tokens * per_row;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
-    const int64_t t = e / per_row, n = (e - t * per_row) * 4;
-    const int left = left_of(n, m);
-    const f32x4 g = load4(O.type, O.kept, t * O.ldk + n, left), u = load4(O.type, O.kept, t * O.ldk + m + n, left);
-    gated_end1(O, m, t, n, g, u);
+  const int per_row = (int)((m + 7) / 8);
+  const int64_t total = tokens * per_row;
+  for (int64_t group = blockIdx.x; group * 256 < total; group += gridDim.x) {
+    int64_t t[1], n[1];
+    int place;
+    piece_of(group, per_row, t[0], place);
+    n[0] = 8 * (int64_t)place;
+    const bool there[1] = {t[0] < tokens};
+    if (!there[0]) continue;
+    const int left = left_of<2>(n[0], m);
+    f32x4 g[1][2], u[1][2];
+    with_type(O.type, [&](auto type) RSVD_INLINE {
+      load_row<decltype(type)::value, 2>(O.kept, t[0] * O.ldk + n[0], left, g[0]);
+      load_row<decltype(type)::value, 2>(O.kept, t[0] * O.ldk + m + n[0], left, u[0]);
+    });
+    gated_end<1, 2, false>(O, m, t, n, there, g, u);
   }
 }
 hipError_t gated_slope_launch(hipStream_t s, int64_t tokens, int64_t m, const GatedOut &o) {
-  int64_t groups = ceil_div(tokens * ceil_div(m, 4), 256);
+  int64_t groups = ceil_div(tokens * ceil_div(m, 8), 256);
   if (groups > 16384) groups = 16384;
   hipLaunchKernelGGL(gated_slope_kernel, dim3((unsigned)groups), dim3(256), 0, s, o, tokens, m);
   return hipGetLastError();
@@ -126,9 +137,14 @@ hipError_t gated_slope_launch(hipStream_t s, int64_t tokens, int64_t m, const Ga
 // ---------------------------------------------------------------- operands
 template <int XT> __global__ __launch_bounds__(256) void planes_kernel(const char *X, int64_t ldx, int64_t rows, int64_t n, uint16_t *out, int64_t width, int64_t plane) {
   constexpr int SIZE = XTraits<XT>::SIZE;
-  const int64_t per_row = width / 8, total = rows * per_row;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
-    const int64_t r = e / per_row, c = (e - r * per_row) * 8;
+  const int per_row = (int)(width / 8);
+  const int64_t total = rows * per_row;
+  for (int64_t group = blockIdx.x; group * 256 < total; group += gridDim.x) {
+    int64_t r;
+    int place;
+    piece_of(group, per_row, r, place);
+    if (r >= rows) continue;
+    const int64_t c = 8 * (int64_t)place;
     const Raw8<XT> v = raw_load8<XT>(X + (r * ldx + c) * SIZE, n - c);
     uint16_t *to = out + r * width + c;
     if constexpr (XT == RSVD_X_F32) {

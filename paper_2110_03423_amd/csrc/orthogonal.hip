@@ -1,23 +1,36 @@
 // Orthogonalising an update: its norm, and the first iterate.
 #include "dense_tile.hpp"
+#include "layer8_rows.hpp"
 
 namespace rsvd {
 
-// Sums of squares of a matrix in fp64, kNormParts parts of it, added by whoever needs the norm in their order.  (fp32 squares would leave its range for gradients of
-// 1e-20 or 1e20.)
+// Sums of squares of a matrix in fp64, in kNormParts parts, added by whoever needs the norm, always in the same order.  (fp32 squares would leave its range for
+// gradients of 1e-20 or 1e20.)
 template <int XT> __global__ __launch_bounds__(256) void norm_kernel(const char *G, int64_t ldg, int64_t stride, int64_t m, int64_t n, double *parts) {
   constexpr int SIZE = XTraits<XT>::SIZE;
   __shared__ double wave_sum[4];
   const int tid = threadIdx.x;
   const char *g = G + (int64_t)blockIdx.y * stride * SIZE;
-  const int64_t per_row = (n + 7) / 8, total = m * per_row;
+  const int per_row = (int)((n + 7) / 8);
+  const int64_t total = m * per_row;
   double sum = 0.0;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + tid; e < total; e += (int64_t)kNormParts * 256) {
-    const int64_t r = e / per_row, c = (e - r * per_row) * 8;
-    float v[8];
-    x_load8<XT>(g + (r * ldg + c) * SIZE, n - c, v);
+  constexpr int U = 4;                                   // loads in flight
+  for (int64_t group = blockIdx.x; group * 256 < total; group += U * kNormParts) {
+    Raw8<XT> v[U];
 #pragma unroll
-    for (int x = 0; x < 8; ++x) sum += (double)v[x] * (double)v[x];
+    for (int u = 0; u < U; ++u) {
+      int64_t r;
+      int c;
+      piece_of(group + u * kNormParts, per_row, r, c);
+      v[u] = raw_load8<XT>(g + (r * ldg + 8 * c) * SIZE, r < m ? n - 8 * c : 0);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float x[8];
+      x_values<XT>(v[u], x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum += (double)x[e] * (double)x[e];
+    }
   }
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_down(sum, d);
@@ -29,27 +42,43 @@ template <int XT> __global__ __launch_bounds__(256) void norm_kernel(const char 
 template <int XT> __global__ __launch_bounds__(256) void unit_kernel(const char *G, int64_t ldg, int64_t stride, int64_t m, int64_t n, const double *parts,
                                                                     uint16_t *X, int64_t width, int64_t plane, int planes) {
   constexpr int SIZE = XTraits<XT>::SIZE;
-  const double *p = parts + (int64_t)blockIdx.y * kNormParts;
-  double sum = 0.0;
-  for (int i = 0; i < kNormParts; ++i) sum += p[i];
+  static_assert(kNormParts == 256, "one a thread");
+  __shared__ double wave_sum[4];
+  const int tid = threadIdx.x;
+  double sum = parts[(int64_t)blockIdx.y * kNormParts + tid];
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) sum += __shfl_down(sum, d);
+  if ((tid & 63) == 0) wave_sum[tid >> 6] = sum;
+  __syncthreads();
+  sum = (wave_sum[0] + wave_sum[1]) + (wave_sum[2] + wave_sum[3]);
   const double norm = sqrt(sum);
   // (a matrix of zeros stays one; with an infinity or NaN everything is NaN)
   const double scale = norm > 0.0 ? (norm < 1e300 ? 8192.0 / norm : (double)__uint_as_float(0x7fc00000u)) : norm == 0.0 ? 0.0 : norm;
   const char *g = G + (int64_t)blockIdx.y * stride * SIZE;
   uint16_t *x = X + (int64_t)blockIdx.y * m * width;
-  const int64_t per_row = width / 4, total = m * per_row;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < total; e += (int64_t)gridDim.x * 256) {
-    const int64_t r = e / per_row, c = (e - r * per_row) * 4;
-    const int left = left_of(c, n);
-    f32x4 v = load4<XT>(g, r * ldg + c, left);
+  const int per_row = (int)(width / 8);
+  const int64_t total = m * per_row;
+  for (int64_t group = blockIdx.x; group * 256 < total; group += gridDim.x) {
+    int64_t r;
+    int c;
+    piece_of(group, per_row, r, c);
+    if (r >= m) continue;
+    const int64_t left = n - 8 * c;
+    float v[8];
+    x_values<XT>(raw_load8<XT>(g + (r * ldg + 8 * c) * SIZE, left), v);
+    u32x4 high, low;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) v[q] = q < left ? (float)((double)v[q] * scale) : 0.f;
-    put4<RSVD_X_F16>(x, r * width + c, 4, v);
-    if (planes == 2) {
+    for (int q = 0; q < 4; ++q) {
+      f32x2 y;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) v[q] -= (float)(_Float16)v[q];
-      put4<RSVD_X_F16>(reinterpret_cast<char *>(x) + plane, r * width + c, 4, v);
+      for (int h = 0; h < 2; ++h) y[h] = 2 * q + h < left ? (float)((double)v[2 * q + h] * scale) : 0.f;
+      const f16x2 f = __builtin_convertvector(y, f16x2);
+      high[q] = __builtin_bit_cast(unsigned, f);
+      low[q] = __builtin_bit_cast(unsigned, __builtin_convertvector(y - __builtin_convertvector(f, f32x2), f16x2));
     }
+    uint16_t *to = x + r * width + 8 * c;
+    *reinterpret_cast<u32x4 *>(to) = high;
+    if (planes == 2) *reinterpret_cast<u32x4 *>(reinterpret_cast<char *>(to) + plane) = low;
   }
 }
 
@@ -64,7 +93,7 @@ hipError_t norm_launch(hipStream_t s, rsvd_xtype type, int batch, int64_t m, int
 
 hipError_t unit_launch(hipStream_t s, rsvd_xtype type, int batch, int64_t m, int64_t n, const void *G, int64_t ldg, int64_t stride, const double *parts,
                        uint16_t *X, int64_t width, int64_t plane, int planes) {
-  int64_t groups = ceil_div(m * (width / 4), 256);
+  int64_t groups = ceil_div(m * (width / 8), 256);
   if (groups > 2048) groups = 2048;
   const dim3 grid((unsigned)groups, (unsigned)batch);
   const char *g = (const char *)G;

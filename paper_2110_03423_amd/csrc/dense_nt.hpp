@@ -67,10 +67,8 @@ __device__ __forceinline__ void f8_widen(u32x4 codes, float unit, u32x4 (&out)[2
     out[w >> 1][2 * (w & 1) + 1] = __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(four, unit, true));
   }
 }
-__device__ __forceinline__ float f8_unit(unsigned power) {
-  return power == 255u ? __uint_as_float(0x7fc00000u) : power == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(power << 23);
-}
-
+// 2^e of the byte e + 127, NaN for 255.  (No branches: arithmetic on the bits; 0 is 2^-127.)
+__device__ __forceinline__ float f8_unit(unsigned power) { return __uint_as_float(max(power << 23, 0x00400000u) + ((power + 1) >> 8 << 22)); }
 __device__ __forceinline__ i32x8 f8_both(const u32x4 (&p)[2]) {
   return i32x8{(int)p[0][0], (int)p[0][1], (int)p[0][2], (int)p[0][3], (int)p[1][0], (int)p[1][1], (int)p[1][2], (int)p[1][3]};
 }

@@ -371,16 +371,26 @@ __device__ __forceinline__ void gated_end1(const GatedOut &O, int64_t N, int64_t
 // ---------------------------------------------------------------- the end of a wavefront's TM x TN blocks of 16 x 16
 // (m1, n1): the first row and column of the wavefront's.  partial: where its first sum goes if it has a range of k, rows of BN sums; or NULL.
 
-// Sixteen rows of a wavefront's blocks in LDS, with their rows and columns exchanged: lane e has column e / 4 and four of the rows.
+// Sixteen rows of a wavefront's blocks in LDS, with their rows and columns exchanged: group e of four has column e / 4 and four of the rows.
 template <int TN> __device__ __forceinline__ void mirror_rows(const DenseParams &P, int batch, int64_t m2, int64_t n1, int lane, const float *lds) {
-  constexpr int PITCH = 16 * TN + 4;
+  constexpr int PITCH = 16 * TN + 4, C = TN < 4 ? TN : 4;
+  const bool whole = n1 + 16 * TN <= P.M && m2 + 16 <= P.N;
 #pragma unroll 1
-  for (int e = lane; e < 64 * TN; e += 64) {
-    const int c = e >> 2, q = 4 * (e & 3);
-    f32x4 v;
+  for (int e0 = lane; e0 < 64 * TN; e0 += 64 * C) {
+    f32x4 v[C][1];
+    int64_t m[C], n[C];
+    bool there[C];
 #pragma unroll
-    for (int x = 0; x < 4; ++x) v[x] = lds[(q + x) * PITCH + c];
-    if (n1 + c < P.M && m2 + q < P.out.width) linear_end1(P.out, P.N, batch, n1 + c, m2 + q, v);
+    for (int c = 0; c < C; ++c) {
+      const int e = e0 + 64 * c, col = e >> 2, q = 4 * (e & 3);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) v[c][0][x] = lds[(q + x) * PITCH + col];
+      m[c] = n1 + col;
+      n[c] = m2 + q;
+      there[c] = m[c] < P.M && n[c] < P.out.width;
+    }
+    if (whole) linear_end<C, 1, true>(P.out, P.N, batch, m, n, there, v);
+    else linear_end<C, 1, false>(P.out, P.N, batch, m, n, there, v);
   }
 }
 

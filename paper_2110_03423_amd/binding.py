@@ -86,6 +86,7 @@ PROTOTYPES = {
 }
 X_BF16, X_F16, X_F32 = 0, 1, 2
 ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
+GATED_FEW = F8_FEW = 64      # tokens up to which these products need no workspace
 
 
 def load_library():
@@ -679,19 +680,22 @@ class Rsvd:
         return dW, db
 
     # ---- a gated feed-forward block
-    def _lies(self, t):
+    @staticmethod
+    def _lies(t, ld):
         """Whether a matrix is read by the large products as it lies."""
-        return t.element_size() == 2 and t.shape[1] % 8 == 0 and t.data_ptr() % 16 == 0 and _ld(t) % 8 == 0 and _ld(t) <= 1 << 22
+        return t.element_size() == 2 and t.shape[1] % 8 == 0 and ld % 8 == 0 and ld <= 1 << 22 and t.data_ptr() % 16 == 0
 
     def _gated(self, X, W, act):
-        """Sizes and type of a gated block, checked."""
-        if act not in ACTS:
-            raise ValueError(f"act: one of {', '.join(ACTS)}")
+        """Sizes, type and activation of a gated block, checked."""
         n = W.shape[-1]
-        rows = self._rows(W, n, "W")
+        rows, tokens, dtype = self._rows(W, n, "W"), self._rows(X, n, "X"), W.dtype
         if rows < 2 or rows % 2 or n < 1:
             raise ValueError("W: as many rows of the up projection behind as many of the gate")
-        return self._rows(X, n, "X"), n, rows // 2, _xtype_code(W.dtype)
+        if X.dtype != dtype:
+            raise TypeError("X, W: one type")
+        if act not in ACTS:
+            raise ValueError(f"act: one of {', '.join(ACTS)}")
+        return tokens, n, rows // 2, _xtype_code(dtype), ACTS[act]
 
     def _like(self, t, cols, what, rows, dtype):
         self._rows(t, cols, what, rows, dtype)
@@ -700,24 +704,24 @@ class Rsvd:
     def rsvd_gated_product(self, X, W, act="silu", keep=False, workspace=None, out=None):
         """act(X Wg^T) * (X Wu^T) of tokens X (tokens x n) and W (2 m x n), the rows of Wg before those of Wu, both of one type (bf16, fp16, fp32):
         tokens x m.  act: silu, gelu, gelu_tanh or relu.  keep: returns (H, kept), kept (tokens x 2 m) the two products for the backward pass."""
-        tokens, n, m, xt = self._gated(X, W, act)
-        if X.dtype != W.dtype:
-            raise TypeError("X, W: one type")
-        lie = self._lies(X) + 2 * self._lies(W)
-        stream = self._raw_stream()
-        ws = self._given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_gated_product_bytes", (xt, tokens, n, m, lie))
+        tokens, n, m, xt, code = self._gated(X, W, act)
+        ldx, ldw, stream = _ld(X), _ld(W), self._raw_stream()
+        if workspace is not None:
+            ws = self._given(workspace)
+        elif tokens <= GATED_FEW:
+            ws = (None, 0)
+        else:
+            ws = self._layer_ws(stream, "rsvd_gated_product_bytes", (xt, tokens, n, m, self._lies(X, ldx) + 2 * self._lies(W, ldw)))
         H = X.new_empty((tokens, m)) if out is None else self._like(out, m, "out", tokens, X.dtype)
         kept = X.new_empty((tokens, 2 * m)) if keep else None
-        self._check(self.lib.rsvd_gated_product(self.h, stream, xt, ACTS[act], tokens, n, m, X.data_ptr(), _ld(X), W.data_ptr(), _ld(W),
-                                                H.data_ptr(), _ld(H), _at(kept), 2 * m, ws[0], ws[1]))
+        self._check(self.lib.rsvd_gated_product(self.h, stream, xt, code, tokens, n, m, X.data_ptr(), ldx, W.data_ptr(), ldw,
+                                                H.data_ptr(), m if out is None else _ld(H), _at(kept), 2 * m, ws[0], ws[1]))
         return (H, kept) if keep else H
 
     def rsvd_gated_product_grad(self, dH, X, W, act="silu", kept=None, out=None, accumulate=False, workspace=None):
         """Gradients of rsvd_gated_product: (dX (tokens x n), dW (2 m x n)) from dH (tokens x m).  kept: what the forward pass kept; without it both products
         are computed again.  `out` = (dX, dW) of the caller, either of them None: not wanted; dW in fp32 or the type of W; accumulate: an fp32 dW is added to."""
-        tokens, n, m, xt = self._gated(X, W, act)
-        if X.dtype != W.dtype:
-            raise TypeError("X, W: one type")
+        tokens, n, m, xt, code = self._gated(X, W, act)
         self._like(dH, m, "dH", tokens, W.dtype)
         if kept is not None:
             self._like(kept, 2 * m, "kept", tokens, W.dtype)
@@ -731,11 +735,11 @@ class Rsvd:
                 self._like(dX, n, "dX", tokens, X.dtype)
             if dW is not None:
                 self._weight_out(dW, 2 * m, n, W.dtype, accumulate)
-        lie = self._lies(X) + 2 * self._lies(W) + 4 * (kept is not None)
+        lie = self._lies(X, _ld(X)) + 2 * self._lies(W, _ld(W)) + 4 * (kept is not None)
         stream = self._raw_stream()
         ws = self._given(workspace) if workspace is not None else self._layer_ws(stream, "rsvd_gated_product_grad_bytes", (xt, tokens, n, m, lie))
         self._check(self.lib.rsvd_gated_product_grad(
-            self.h, stream, xt, ACTS[act], tokens, n, m, _at(dH), _ld(dH), _at(X), _ld(X), _at(W), _ld(W), _at(kept), _ld(kept) if kept is not None else 0,
+            self.h, stream, xt, code, tokens, n, m, _at(dH), _ld(dH), _at(X), _ld(X), _at(W), _ld(W), _at(kept), _ld(kept) if kept is not None else 0,
             _at(dX), _ld(dX) if dX is not None else 0, _at(dW), _ld(dW) if dW is not None else 0,
             int(dW is not None and dW.dtype == self.torch.float32), int(accumulate and dW is not None), ws[0], ws[1]))
         return dX, dW
@@ -765,11 +769,16 @@ class Rsvd:
         if weight._index != self._index:
             self._elsewhere(weight, "weight")
         stream = self._raw_stream()
-        ws = self._given(workspace) if workspace is not None else self._layer_ws(stream, name + "_bytes", (xt, tokens, weight.n, weight.m))
+        if workspace is not None:
+            ws = self._given(workspace)
+        elif tokens <= F8_FEW:
+            ws = (None, 0)
+        else:
+            ws = self._layer_ws(stream, name + "_bytes", (xt, tokens, weight.n, weight.m))
         Y = X.new_empty((tokens, m)) if out is None else self._like(out, m, "out", tokens, X.dtype)
         q, p = laid_out
         self._check(getattr(self.lib, name)(self.h, stream, xt, tokens, weight.n, weight.m, X.data_ptr(), _ld(X), q.data_ptr(), q.stride(0),
-                                            p.data_ptr(), p.stride(0), Y.data_ptr(), _ld(Y), ws[0], ws[1]))
+                                            p.data_ptr(), p.stride(0), Y.data_ptr(), m if out is None else _ld(Y), ws[0], ws[1]))
         return Y
 
     def rsvd_f8_product(self, X, weight, workspace=None, out=None):

@@ -13,29 +13,34 @@ static int64_t dense_tiles(const DenseDesc &d, int b) {
   return d.symmetric ? rows * (rows + 1) / 2 : rows * columns;
 }
 
-// The time of each tile and number of ranges is estimated, and the least taken: a k-tile (128 bytes of a row) takes a CU 0.22, 0.55 and 1.75 us for each
-// workgroup of 64, 128 and 256 rows and columns, but no less than 0.33, 0.78 and 1.55 us, a launch 5 us beside that.  Tiles that fill the chip a number of times are
-// worked out whole; of what is left k may be in ranges, for all CUs to have a part: a second launch, and their sums are written and read (5 bytes / ps).
+// The time of each tile and number of ranges is estimated, and the least taken.  What bounds a k-tile (128 bytes of a row) of the smaller tiles is what a CU gets out of the
+// L2 caches, 50 to 60 GB/s: 0.26 and 0.55 us for each workgroup of 64 and 128 rows and columns, but no less than 0.32 and 0.68 us; tiles of 256 take 1.75 us, near the rate of the
+// matrix instructions.  Small tiles take a k-tile of all planes at once: as many times 0.26 us (two: no less than 1.05).  Beside that 3, 5 and 8 us for each workgroup that a CU has behind
+// another.  Tiles that fill the chip a number of times are worked out whole; of what is left k may be in ranges, for all CUs to have a part: a second launch, and their sums are
+// written and read (5 bytes / ps).
 static DenseChoice dense_choose(const rsvd_ctx *ctx, const DenseDesc &d) {
-  const struct { int b, at_once; double step, least; } tile[3] = {{64, 3, 0.22, 0.33}, {128, 2, 0.55, 0.78}, {256, 1, 1.75, 1.55}};
+  const int products = dense_segs(d.planes).count;
+  const struct { int b, at_once; double step, least, more; } tile[3] = {{64, d.planes == 3 ? 1 : d.planes == 2 ? 2 : 3, 0.26 * d.planes, d.planes == 2 ? 1.05 : 0.32 * d.planes, 3.0},
+                                                                        {128, 2, 0.55, 0.68, 5.0}, {256, 1, 1.75, 1.75, 8.0}};
   static const int ranges[9] = {1, 2, 3, 4, 6, 8, 12, 16, 24};
-  const int64_t kt = ceil_div(d.K, dense_k(d.kind)) * dense_segs(d.planes).count, cu = ctx->cu_count;
+  const int64_t ktiles = ceil_div(d.K, dense_k(d.kind)), cu = ctx->cu_count;
   DenseChoice best = {};
   double least = 1e300;
   for (const auto &t : tile) {
+    const int64_t kt = t.b == 64 ? ktiles : ktiles * products;
     const int64_t tiles = dense_tiles(d, t.b) * d.batch, full = cu * t.at_once;
     auto time = [&](int64_t groups, int64_t k) {
       const double each = (double)ceil_div(groups, cu) * t.step;
-      return groups == 0 ? 0.0 : (double)k * (each > t.least ? each : t.least);
+      return groups == 0 ? 0.0 : (double)ceil_div(groups, full) * t.more + (double)k * (each > t.least ? each : t.least);
     };
     for (const int r : ranges) {
-      if (r > 1 && kt < 4 * r) break;
-      const int64_t per = r > 1 ? ceil_div(kt, r) : kt, used = ceil_div(kt, per);
+      if (r > 1 && kt < 2 * r) break;
+      const int64_t per = ceil_div(kt, r), used = ceil_div(kt, per);
       if (r > 1 && used < 2) continue;
       const int64_t whole = used > 1 ? tiles / full * full : tiles, rest = tiles - whole;
       if (used > 1 && rest == 0) continue;
       double us = time(whole, kt) + time(rest * used, per);
-      if (used > 1) us += 3.0 + (double)used * (double)rest * t.b * t.b * 8.0 / 5e6;
+      if (used > 1) us += 4.0 + (double)used * (double)rest * t.b * t.b * 8.0 / 5e6;
       if (us < least) {
         least = us;
         best = DenseChoice{t.b, dense_tiles(d, t.b), whole, rest, used, kt, per};

@@ -15,6 +15,7 @@ enum DenseKind { DK_BF16 = 0, DK_F16 = 1, DK_F8 = 2, DK_F8_EXACT = 3 };
 // Products of planes: numbers that are sums of several 16-bit numbers, whose products are taken as further k, the smallest first.  Nibble s of
 // `a` and `b`: planes of the two operands in part s of k.
 struct DenseSegs { int count; uint32_t a, b; };
+// (Small tiles take all planes of a k-tile at once and multiply them there, in this order.)
 inline DenseSegs dense_segs(int planes) {
   if (planes == 3) return {6, 0x001012u, 0x010210u};       // (2,0) (1,1) (0,2) (1,0) (0,1) (0,0): 2^-24 of the largest is left out
   if (planes == 2) return {3, 0x001u, 0x010u};             // (1,0) (0,1) (0,0): 2^-22

@@ -12,15 +12,16 @@
 
 namespace rsvd {
 
-template <int BM, int BN> struct DenseKnCfg {
-  static constexpr int A = BM * 128, B = BN * 128, STAGE = A + B, DEPTH = BM == 256 ? 1 : 2;
+template <int PL, int BM, int BN> struct DenseKnCfg {
+  static constexpr int A = BM * 128, B = BN * 128, PLANE = A + B, STAGE = PL * PLANE, DEPTH = BM == 256 ? 1 : 2;
   static constexpr size_t lds = 2 * (size_t)STAGE;      // (more than the wavefronts need in the end)
 };
 
-template <int KIND, bool A_KROWS, int BM, int BN, int WGM, int WGN>
-__global__ __launch_bounds__(64 * WGM * WGN, 2) void dense_kn_kernel(const DenseParams P) {
-  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, DEPTH = DenseKnCfg<BM, BN>::DEPTH;
-  constexpr int STAGE = DenseKnCfg<BM, BN>::STAGE, B_LDS = DenseKnCfg<BM, BN>::A;
+// PL planes of both operands are multiplied while a k-tile of all is in LDS; 1: the products of planes are further k.
+template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN>
+__global__ __launch_bounds__(64 * WGM * WGN, PL == 3 ? 1 : 2) void dense_kn_kernel(const DenseParams P) {
+  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, DEPTH = DenseKnCfg<PL, BM, BN>::DEPTH;
+  constexpr int STAGE = DenseKnCfg<PL, BM, BN>::STAGE, PLANE = DenseKnCfg<PL, BM, BN>::PLANE, B_LDS = DenseKnCfg<PL, BM, BN>::A;
   extern __shared__ __attribute__((aligned(16))) char dense_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
@@ -45,29 +46,31 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void dense_kn_kernel(const Dense
   int left;
   auto point = [&]() RSVD_INLINE {
     const int64_t k = (int64_t)next_kt * kKnK;
-    a_now = a_first + (int64_t)(P.segs.a >> (4 * next_seg) & 15) * P.a_plane + (A_KROWS ? k * P.lda : k * 2);
-    b_now = b_first + (int64_t)(P.segs.b >> (4 * next_seg) & 15) * P.b_plane + k * P.ldb;
+    a_now = a_first + (PL > 1 ? 0 : (int64_t)(P.segs.a >> (4 * next_seg) & 15) * P.a_plane) + (A_KROWS ? k * P.lda : k * 2);
+    b_now = b_first + (PL > 1 ? 0 : (int64_t)(P.segs.b >> (4 * next_seg) & 15) * P.b_plane) + k * P.ldb;
     left = (int)(P.K - k < kKnK ? P.K - k : kKnK);
   };
   auto advance = [&]() RSVD_INLINE {                    // (behind the last tile of this workgroup's range: loads stay inside the operands)
     if (++next_kt == P.ktiles) {
       next_kt = 0;
-      if (next_seg + 1 < P.segs.count) ++next_seg;
+      if (PL == 1 && next_seg + 1 < P.segs.count) ++next_seg;
     }
     point();
   };
-  Staged<NT, BM, A_KROWS, DEPTH> sa;
-  Staged<NT, BN, true, DEPTH> sb;
+  Staged<NT, BM, A_KROWS, DEPTH * PL> sa;
+  Staged<NT, BN, true, DEPTH * PL> sb;
   sa.init(P.lda, P.M - m0, tid);
   sb.init(P.ldb, P.N - n0, tid);
-  constexpr int NA = decltype(sa)::N, PIECES = NA + decltype(sb)::N;
-  auto load = [&](int set, int p) RSVD_INLINE {
-    if (p < NA) sa.load(set, p, a_now, P.lda, left);
-    else sb.load(set, p - NA, b_now, P.ldb, left);
+  constexpr int NA = decltype(sa)::N, EACH = NA + decltype(sb)::N, PIECES = PL * EACH;
+  auto load = [&](int set, int piece) RSVD_INLINE {
+    const int q = piece / EACH, p = piece % EACH;
+    if (p < NA) sa.load(PL * set + q, p, a_now + q * P.a_plane, P.lda, left);
+    else sb.load(PL * set + q, p - NA, b_now + q * P.b_plane, P.ldb, left);
   };
-  auto write = [&](int set, int p, int buf) RSVD_INLINE {
-    if (p < NA) sa.write(set, p, dense_lds + buf * STAGE);
-    else sb.write(set, p - NA, dense_lds + buf * STAGE + B_LDS);
+  auto write = [&](int set, int piece, int buf) RSVD_INLINE {
+    const int q = piece / EACH, p = piece % EACH;
+    if (p < NA) sa.write(PL * set + q, p, dense_lds + buf * STAGE + q * PLANE);
+    else sb.write(PL * set + q, p - NA, dense_lds + buf * STAGE + q * PLANE + B_LDS);
   };
 
   // ---- operands of this lane
@@ -96,29 +99,39 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void dense_kn_kernel(const Dense
   auto body = [&](int buf, auto from) RSVD_INLINE {
     constexpr int SET = decltype(from)::value;
     const int a_lds = a_at + buf * STAGE, b_lds = b_at + buf * STAGE;
-    auto read_a = [&](int step) RSVD_INLINE {
+    auto read_a = [&](int step, int q) RSVD_INLINE {
       const int h = step / TM, i = step % TM;
-      return A_KROWS ? transposed(dense_lds + (a_lds ^ (i << 5)) + h * 32 * A_ROW, A_ROW)
-                     : *reinterpret_cast<const u32x4 *>(dense_lds + a_lds + i * 2048 + (((4 * h + kq) ^ (r16 & 7)) << 4));
+      return A_KROWS ? transposed(dense_lds + q * PLANE + (a_lds ^ (i << 5)) + h * 32 * A_ROW, A_ROW)
+                     : *reinterpret_cast<const u32x4 *>(dense_lds + q * PLANE + a_lds + i * 2048 + (((4 * h + kq) ^ (r16 & 7)) << 4));
     };
-    auto read_b = [&](int h, int j) RSVD_INLINE { return transposed(dense_lds + (b_lds ^ (j << 5)) + h * 32 * BN * 2, BN * 2); };
+    auto read_b = [&](int h, int j, int q) RSVD_INLINE { return transposed(dense_lds + q * PLANE + (b_lds ^ (j << 5)) + h * 32 * BN * 2, BN * 2); };
     constexpr int AHEAD = TM >= 4 ? 3 : 1;             // rows of blocks read ahead, not all of them: registers
-    u32x4 a[AHEAD + 1], b[2][TN];
+    u32x4 a[AHEAD + 1][PL], b[2][TN][PL];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) b[0][j] = read_b(0, j);
+    for (int q = 0; q < PL; ++q) {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) a[i] = read_a(i);
+      for (int j = 0; j < TN; ++j) b[0][j][q] = read_b(0, j, q);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) a[i][q] = read_a(i, q);
+    }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int step = 0; step < 2 * TM; ++step) {
       const int h = step / TM, i = step % TM;
-      if (step + AHEAD < 2 * TM) a[(step + AHEAD) % (AHEAD + 1)] = read_a(step + AHEAD);
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
-        if (h == 0 && i == j * TM / TN) b[1][j] = read_b(1, j);
+      for (int q = 0; q < PL; ++q) {
+        if (step + AHEAD < 2 * TM) a[(step + AHEAD) % (AHEAD + 1)][q] = read_a(step + AHEAD, q);
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
-        acc[i][j] = KIND == DK_BF16 ? mfma_bf16(b[h][j], a[step % (AHEAD + 1)], acc[i][j]) : mfma_f16(b[h][j], a[step % (AHEAD + 1)], acc[i][j]);
+        for (int j = 0; j < TN; ++j)
+          if (h == 0 && i == j * TM / TN) b[1][j][q] = read_b(1, j, q);
+      }
+      with_segs<PL>([&](auto pa, auto pb) RSVD_INLINE {
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const u32x4 x = b[h][j][decltype(pb)::value], y = a[step % (AHEAD + 1)][decltype(pa)::value];
+          acc[i][j] = KIND == DK_BF16 ? mfma_bf16(x, y, acc[i][j]) : mfma_f16(x, y, acc[i][j]);
+        }
+      });
 #pragma unroll
       for (int p = 0; p < PIECES; ++p)
         if (p * (2 * TM) / PIECES == step) {
@@ -148,6 +161,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void dense_kn_kernel(const Dense
     advance();
     meet();
   };
+  // (the tile behind goes to LDS out of the set that holds it)
   if constexpr (DEPTH == 1) {
     for (int kt = 0; kt < nkt; ++kt) tile(kt & 1, std::integral_constant<int, 0>());
   } else {
@@ -164,18 +178,25 @@ __global__ __launch_bounds__(64 * WGM * WGN, 2) void dense_kn_kernel(const Dense
                        reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
 }
 
-template <int KIND, bool A_KROWS, int BM, int BN, int WGM, int WGN> hipError_t dense_kn_run(hipStream_t s, const DenseParams &P) {
-  hipLaunchKernelGGL((dense_kn_kernel<KIND, A_KROWS, BM, BN, WGM, WGN>), dim3(dense_groups(P)), dim3(64 * WGM * WGN), (DenseKnCfg<BM, BN>::lds), s, P);
+template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN> hipError_t dense_kn_run(hipStream_t s, const DenseParams &P) {
+  hipLaunchKernelGGL((dense_kn_kernel<KIND, A_KROWS, PL, BM, BN, WGM, WGN>), dim3(dense_groups(P)), dim3(64 * WGM * WGN), (DenseKnCfg<PL, BM, BN>::lds), s, P);
   return hipGetLastError();
 }
+// The planes that small tiles of a kind take at once.
+template <int KIND> constexpr int dense_kn_planes() { return KIND == DK_BF16 ? 3 : 2; }
 template <int KIND, bool A_KROWS> hipError_t dense_kn_tile(hipStream_t s, const DenseParams &P, int b) {
-  if (b == 256) return dense_kn_run<KIND, A_KROWS, 256, 256, 2, 4>(s, P);
-  if (b == 128) return dense_kn_run<KIND, A_KROWS, 128, 128, 2, 2>(s, P);
-  return dense_kn_run<KIND, A_KROWS, 64, 64, 2, 2>(s, P);
+  if (b == 256) return dense_kn_run<KIND, A_KROWS, 1, 256, 256, 2, 4>(s, P);
+  if (b == 128) return dense_kn_run<KIND, A_KROWS, 1, 128, 128, 2, 2>(s, P);
+  if (P.segs.count > 1) return dense_kn_run<KIND, A_KROWS, dense_kn_planes<KIND>(), 64, 64, 2, 2>(s, P);
+  return dense_kn_run<KIND, A_KROWS, 1, 64, 64, 2, 2>(s, P);
 }
 template <int KIND, bool A_KROWS> hipError_t dense_kn_init() {
-  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, 256, 256, 2, 4>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)DenseKnCfg<256, 256>::lds);
+  constexpr int PL = dense_kn_planes<KIND>();
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, 1, 256, 256, 2, 4>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           (int)DenseKnCfg<1, 256, 256>::lds);
+  if (e != hipSuccess) return e;
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, PL, 64, 64, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)DenseKnCfg<PL, 64, 64>::lds);
 }
 #define DENSE_KN(KIND, A_KROWS)                                                                      \
   template hipError_t dense_kn_tile<KIND, A_KROWS>(hipStream_t s, const DenseParams &P, int b);     \

@@ -21,8 +21,8 @@
 
 namespace rsvd {
 
-template <int KIND, int BM, int BN> struct DenseNtCfg {
-  static constexpr int POWERS = (BM + BN) * 128, STAGE = POWERS + (KIND >= DK_F8 ? (BM + BN) * 4 : 0), RING = BM == 64 ? 3 : 2;      // behind the codes, a word of powers a row
+template <int KIND, int PL, int BM, int BN> struct DenseNtCfg {
+  static constexpr int POWERS = PL * (BM + BN) * 128, STAGE = POWERS + (KIND >= DK_F8 ? (BM + BN) * 4 : 0), RING = BM > 64 || PL == 2 ? 2 : 3;      // behind the codes, a word of powers a row
   static constexpr size_t lds = RING * (size_t)STAGE;      // (more than the wavefronts need in the end)
 };
 
@@ -73,9 +73,10 @@ __device__ __forceinline__ i32x8 f8_both(const u32x4 (&p)[2]) {
   return i32x8{(int)p[0][0], (int)p[0][1], (int)p[0][2], (int)p[0][3], (int)p[1][0], (int)p[1][1], (int)p[1][2], (int)p[1][3]};
 }
 
-template <int KIND, bool GATED, int BM, int BN, int WGM, int WGN>
-__global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_kernel(const DenseParams P) {
-  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = DenseNtCfg<KIND, BM, BN>::STAGE, RING = DenseNtCfg<KIND, BM, BN>::RING;
+// PL planes of both operands are multiplied while a k-tile of all is in LDS; 1: the products of planes are further k.
+template <int KIND, bool GATED, int PL, int BM, int BN, int WGM, int WGN>
+__global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void dense_nt_kernel(const DenseParams P) {
+  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = DenseNtCfg<KIND, PL, BM, BN>::STAGE, RING = DenseNtCfg<KIND, PL, BM, BN>::RING;
   constexpr bool CODES = KIND >= DK_F8;
   extern __shared__ __attribute__((aligned(16))) char dense_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
   la.init(P.lda, P.M - m0, tid);
   lb.init(P.ldb, P.N - n0, tid);
   // of codes, too: the words that hold the powers of the tile's rows, one row a lane (small tiles: by two wavefronts each)
-  constexpr int POWER_LOADS = !CODES ? 0 : BM + BN < NT ? 1 : (BM + BN) / NT, LOADS = decltype(la)::N + decltype(lb)::N + POWER_LOADS;
+  constexpr int POWER_LOADS = !CODES ? 0 : BM + BN < NT ? 1 : (BM + BN) / NT, TILE_LOADS = decltype(la)::N + decltype(lb)::N, LOADS = PL * TILE_LOADS + POWER_LOADS;
   uint32_t pow_off[CODES ? POWER_LOADS : 1];
   if constexpr (CODES) {
 #pragma unroll
@@ -119,8 +120,8 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
   const char *a_now, *b_now;
   int left;
   auto point = [&]() RSVD_INLINE {
-    a_now = a_row + (int64_t)(P.segs.a >> (4 * next_seg) & 15) * P.a_plane + (int64_t)next_kt * 128;
-    b_now = b_row + (int64_t)(P.segs.b >> (4 * next_seg) & 15) * P.b_plane + (int64_t)next_kt * 128;
+    a_now = a_row + (PL > 1 ? 0 : (int64_t)(P.segs.a >> (4 * next_seg) & 15) * P.a_plane) + (int64_t)next_kt * 128;
+    b_now = b_row + (PL > 1 ? 0 : (int64_t)(P.segs.b >> (4 * next_seg) & 15) * P.b_plane) + (int64_t)next_kt * 128;
     left = next_kt == P.ktiles - 1 ? last_left : 8;
   };
   auto advance = [&]() RSVD_INLINE {                    // (behind the last tile that one again, where nobody reads it: no branches around loads)
@@ -134,32 +135,33 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
   };
   auto issue = [&](int kt, int l) RSVD_INLINE {
     char *st = dense_lds + (kt % RING) * STAGE;
-    if (l < decltype(la)::N) {
-      la.issue(l, a_now, 0, st, left, wave, tid);
-    } else if (l < decltype(la)::N + decltype(lb)::N) {
-      lb.issue(l - decltype(la)::N, b_now, P.b_up, st + BM * 128, left, wave, tid);
+    const int q = l / TILE_LOADS, at = l % TILE_LOADS;   // (planes: those of A and B in turn)
+    if (q < PL && at < decltype(la)::N) {
+      la.issue(at, a_now + q * P.a_plane, 0, st + q * (BM + BN) * 128, left, wave, tid);
+    } else if (q < PL) {
+      lb.issue(at - decltype(la)::N, b_now + q * P.b_plane, P.b_up, st + (q * (BM + BN) + BM) * 128, left, wave, tid);
     } else if constexpr (CODES) {
-      const int i = l - decltype(la)::N - decltype(lb)::N, first = (wave * 64 + NT * i) & (BM + BN - 1);
+      const int i = l - TILE_LOADS, first = (wave * 64 + NT * i) & (BM + BN - 1);
       const uint8_t *base = (first < BM ? P.a_pow : P.b_pow) + (next_kt & ~3);
       const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7fffffff, 0x00027000);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(all, (__attribute__((address_space(3))) void *)(st + DenseNtCfg<KIND, BM, BN>::POWERS + first * 4), 4, pow_off[i], 0, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(all, (__attribute__((address_space(3))) void *)(st + DenseNtCfg<KIND, PL, BM, BN>::POWERS + first * 4), 4, pow_off[i], 0, 0, 0);
     }
   };
 
   constexpr int AHEAD = TM >= 4 ? 3 : 1;               // rows of blocks read ahead, not all of them: registers
-  constexpr int FIRST = KIND == DK_F8 || LOADS < 2 * AHEAD ? LOADS : 2 * AHEAD;      // loads of a tile that are issued behind a meeting
+  constexpr int FIRST = KIND == DK_F8 || BM == 64 || LOADS < 2 * AHEAD ? LOADS : 2 * AHEAD;      // loads of a tile that are issued behind a meeting
   // (rows of a wavefront's blocks start at multiples of 32, or of 16 where they are not shared: what pieces are exchanged by is the lane's)
   const int b_first = PAIRED ? 8 * (r16 >> 2) + (r16 & 3) : r16, a_swz = dense_swizzle<false>(r16), b_swz = dense_swizzle<PAIRED>(b_first);
   const char *const a_lds = dense_lds + (wm0 + r16) * 128, *const b_lds = dense_lds + BM * 128 + (wn0 + b_first) * 128;
-  auto piece_a = [&](int kt, int i, int h) RSVD_INLINE {
-    return *reinterpret_cast<const u32x4 *>(a_lds + (kt % RING) * STAGE + i * 2048 + (((4 * h + kq) ^ a_swz) << 4));
+  auto piece_a = [&](int kt, int i, int h, int q = 0) RSVD_INLINE {
+    return *reinterpret_cast<const u32x4 *>(a_lds + (kt % RING) * STAGE + q * (BM + BN) * 128 + i * 2048 + (((4 * h + kq) ^ a_swz) << 4));
   };
-  auto piece_b = [&](int kt, int j, int h) RSVD_INLINE {
-    return *reinterpret_cast<const u32x4 *>(b_lds + (kt % RING) * STAGE + (PAIRED ? j / 2 * 4096 + (j & 1) * 512 : j * 2048) + (((4 * h + kq) ^ b_swz) << 4));
+  auto piece_b = [&](int kt, int j, int h, int q = 0) RSVD_INLINE {
+    return *reinterpret_cast<const u32x4 *>(b_lds + (kt % RING) * STAGE + q * (BM + BN) * 128 + (PAIRED ? j / 2 * 4096 + (j & 1) * 512 : j * 2048) + (((4 * h + kq) ^ b_swz) << 4));
   };
   // powers of the rows of a lane's blocks: in words of four k-tiles, and of the one that is multiplied
   unsigned words_a[CODES ? TM : 1], words_b[CODES ? TN : 1], pa[CODES ? TM : 1], pb[CODES ? TN : 1];
-  const char *const pow_lds = dense_lds + DenseNtCfg<KIND, BM, BN>::POWERS;
+  const char *const pow_lds = dense_lds + DenseNtCfg<KIND, PL, BM, BN>::POWERS;
   auto read_powers = [&](int kt) RSVD_INLINE {
 #pragma unroll
     for (int i = 0; i < (CODES ? TM : 0); ++i) words_a[i] = *reinterpret_cast<const unsigned *>(pow_lds + (kt % RING) * STAGE + (wm0 + 16 * i + r16) * 4);
@@ -183,7 +185,10 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
     if constexpr (!CODES) {
       if (last_left < 8 && (first_kt + kt + 1) % P.ktiles == 0) {      // zeros behind the last k
         for (int q = tid; q < (BM + BN) * 8; q += NT)
-          if ((q < BM * 8 ? decltype(la)::piece(q) : decltype(lb)::piece(q - BM * 8)) >= last_left) *reinterpret_cast<u32x4 *>(dense_lds + (kt % RING) * STAGE + q * 16) = (u32x4)0u;
+          if ((q < BM * 8 ? decltype(la)::piece(q) : decltype(lb)::piece(q - BM * 8)) >= last_left) {
+#pragma unroll
+            for (int p = 0; p < PL; ++p) *reinterpret_cast<u32x4 *>(dense_lds + (kt % RING) * STAGE + (p * (BM + BN) * 8 + q) * 16) = (u32x4)0u;
+          }
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(tile_wait(63));
         __builtin_amdgcn_s_barrier();
@@ -204,7 +209,97 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
 
   // Where the rows of blocks of a tile that are read ahead would be those of the next one, wavefronts meet, and go on with the next tile's: no wavefront
   // waits for LDS at the start of a tile.  (The loads of a tile go to the place of the one that is multiplied before, from the meeting on.)
-  if constexpr (KIND == DK_F8) {
+  if constexpr (BM == 64) {
+    // small tiles: all operands of the next tile are read while one is multiplied (LDS takes longer to answer than a row of blocks takes)
+    u32x4 a[2][TM][2][PL], b[2][TN][2][PL];
+    unsigned words[2][2][CODES ? TM : 1];
+    static_assert(TM == TN, "square tiles");
+    auto fetch = [&](auto to, int kt) RSVD_INLINE {
+      constexpr int S = decltype(to)::value;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int q = PL - 1; q >= 0; --q) {
+            a[S][i][h][q] = piece_a(kt, i, h, q);
+            b[S][i][h][q] = piece_b(kt, i, h, q);
+          }
+      if constexpr (CODES) {
+        read_powers(kt);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          words[S][0][i] = words_a[i];
+          words[S][1][i] = words_b[i];
+        }
+      }
+    };
+    auto multiply = [&](auto of, int kt) RSVD_INLINE {
+      constexpr int S = decltype(of)::value;
+      if constexpr (CODES) {
+        const int by = 8 * ((kt_begin + kt) & 3);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          pa[i] = words[S][0][i] >> by;
+          pb[i] = words[S][1][i] >> by;
+        }
+      }
+      if constexpr (KIND == DK_F8) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            const u32x4 x[2] = {b[S][j][0][0], b[S][j][1][0]}, y[2] = {a[S][i][0][0], a[S][i][1][0]};
+            acc[i][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_both(x), f8_both(y), acc[i][j], 0, 0, 0, (int)pb[j], 0, (int)pa[i]);
+          }
+      } else if constexpr (KIND == DK_F8_EXACT) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 x[TN][2], y[TM][2];
+#pragma unroll
+          for (int i = 0; i < TM; ++i) {
+            f8_widen(b[S][i][h][0], f8_unit(pb[i] & 255u), x[i]);
+            f8_widen(a[S][i][h][0], f8_unit(pa[i] & 255u), y[i]);
+          }
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+              for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(x[j][q], y[i][q], acc[i][j]);
+        }
+      } else {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          with_segs<PL>([&](auto qa, auto qb) RSVD_INLINE {
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+              for (int j = 0; j < TN; ++j) {
+                const u32x4 x = b[S][j][h][decltype(qb)::value], y = a[S][i][h][decltype(qa)::value];
+                acc[i][j] = KIND == DK_BF16 ? mfma_bf16(x, y, acc[i][j]) : mfma_f16(x, y, acc[i][j]);
+              }
+          });
+      }
+    };
+    auto tile = [&](auto now, auto then, int kt) RSVD_INLINE {
+      meet(std::integral_constant<int, (RING - 2) * LOADS>(), kt + 1);
+      advance();
+      fetch(then, kt + 1);
+#pragma unroll
+      for (int l = 0; l < LOADS; ++l) issue(kt, l);
+      __builtin_amdgcn_sched_barrier(0);
+      multiply(now, kt);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    typedef std::integral_constant<int, 0> even;
+    typedef std::integral_constant<int, 1> odd;
+    fetch(even(), 0);
+    for (int kt = 0; kt < nkt; kt += 2) {
+      tile(even(), odd(), kt);
+      if (kt + 1 < nkt) tile(odd(), even(), kt + 1);
+    }
+  } else if constexpr (KIND == DK_F8) {
     // a tile's last rows of blocks column by column, so that an operand of B is free for the next tile's as soon as it can be
     u32x4 a[AHEAD + 1][2], b[TN][2];
 #pragma unroll
@@ -252,11 +347,14 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
   } else {
     // (of 8-bit floats as bf16 numbers: two steps of 32 k out of a piece)
     constexpr int Q = KIND == DK_F8_EXACT ? 2 : 1;
-    u32x4 a[AHEAD + 1], b[2][TN];
+    u32x4 a[AHEAD + 1][PL], b[2][TN][PL];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) b[0][j] = piece_b(0, j, 0);
+    for (int q = 0; q < PL; ++q) {
 #pragma unroll
-    for (int i = 0; i < AHEAD; ++i) a[i] = piece_a(0, i, 0);
+      for (int j = 0; j < TN; ++j) b[0][j][q] = piece_b(0, j, 0, q);
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) a[i][q] = piece_a(0, i, 0, q);
+    }
     if constexpr (CODES) read_powers(0);
     u32x4 wide[Q == 2 ? TN : 1][2];
     for (int kt = 0; kt < nkt; ++kt) {
@@ -270,31 +368,41 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
           advance();
           if constexpr (CODES) read_powers(kt + 1);
         }
-        const u32x4 now = a[step % (AHEAD + 1)];
-        a[ahead % (AHEAD + 1)] = piece_a(ahead < 2 * TM ? kt : kt + 1, ahead % TM, ahead / TM % 2);
+        u32x4 now[PL];
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          if (h == 0 && i == j * TM / TN) b[1][j] = piece_b(kt, j, 1);
-          if (step >= 2 * TM - AHEAD && (step - 2 * TM + AHEAD) == j * AHEAD / TN) b[0][j] = piece_b(kt + 1, j, 0);
+        for (int q = 0; q < PL; ++q) {
+          now[q] = a[step % (AHEAD + 1)][q];
+          a[ahead % (AHEAD + 1)][q] = piece_a(ahead < 2 * TM ? kt : kt + 1, ahead % TM, ahead / TM % 2, q);
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            if (h == 0 && i == j * TM / TN) b[1][j][q] = piece_b(kt, j, 1, q);
+            if (step >= 2 * TM - AHEAD && (step - 2 * TM + AHEAD) == j * AHEAD / TN) b[0][j][q] = piece_b(kt + 1, j, 0, q);
+          }
         }
         if constexpr (KIND == DK_F8_EXACT) {
           u32x4 wide_a[2];
-          f8_widen(now, f8_unit(pa[i] & 255u), wide_a);
+          f8_widen(now[0], f8_unit(pa[i] & 255u), wide_a);
           if (i == 0) {
 #pragma unroll
-            for (int j = 0; j < TN; ++j) f8_widen(b[h][j], f8_unit(pb[j] & 255u), wide[j]);
+            for (int j = 0; j < TN; ++j) f8_widen(b[h][j][0], f8_unit(pb[j] & 255u), wide[j]);
           }
 #pragma unroll
           for (int q = 0; q < Q; ++q)
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = mfma_bf16(wide[j][q], wide_a[q], acc[i][j]);
         } else {
+          with_segs<PL>([&](auto pa_, auto pb_) RSVD_INLINE {
 #pragma unroll
-          for (int j = 0; j < TN; ++j) acc[i][j] = KIND == DK_BF16 ? mfma_bf16(b[h][j], now, acc[i][j]) : mfma_f16(b[h][j], now, acc[i][j]);
+            for (int j = 0; j < TN; ++j)
+              acc[i][j] = KIND == DK_BF16 ? mfma_bf16(b[h][j][decltype(pb_)::value], now[decltype(pa_)::value], acc[i][j])
+                                          : mfma_f16(b[h][j][decltype(pb_)::value], now[decltype(pa_)::value], acc[i][j]);
+          });
         }
 #pragma unroll
         for (int l = 0; l < LOADS; ++l) {
-          if (l < FIRST ? step == 2 * TM - AHEAD + l / 2 : step == (l - FIRST) / 2) issue(l < FIRST ? kt : kt + RING - 1, l);
+          // (FIRST of them behind the meeting; the others two a step, or as many as it takes to have them all before the next)
+          constexpr int EACH = (LOADS - FIRST + 2 * TM - AHEAD - 1) / (2 * TM - AHEAD) > 2 ? (LOADS - FIRST + 2 * TM - AHEAD - 1) / (2 * TM - AHEAD) : 2;
+          if (l < FIRST ? step == 2 * TM - AHEAD + l / 2 : step == (l - FIRST) / EACH) issue(l < FIRST ? kt : kt + RING - 1, l);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -315,18 +423,25 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 ? 1 : 2) void dense_nt_ke
   }
 }
 
-template <int KIND, bool GATED, int BM, int BN, int WGM, int WGN> hipError_t dense_nt_run(hipStream_t s, const DenseParams &P) {
-  hipLaunchKernelGGL((dense_nt_kernel<KIND, GATED, BM, BN, WGM, WGN>), dim3(dense_groups(P)), dim3(64 * WGM * WGN), (DenseNtCfg<KIND, BM, BN>::lds), s, P);
+template <int KIND, bool GATED, int PL, int BM, int BN, int WGM, int WGN> hipError_t dense_nt_run(hipStream_t s, const DenseParams &P) {
+  hipLaunchKernelGGL((dense_nt_kernel<KIND, GATED, PL, BM, BN, WGM, WGN>), dim3(dense_groups(P)), dim3(64 * WGM * WGN), (DenseNtCfg<KIND, PL, BM, BN>::lds), s, P);
   return hipGetLastError();
 }
+// The planes that small tiles of a kind take at once: three of bf16 numbers, two of fp16 numbers of a plain product.
+template <int KIND, bool GATED> constexpr int dense_nt_planes() { return KIND == DK_BF16 ? 3 : KIND == DK_F16 && !GATED ? 2 : 1; }
 template <int KIND, bool GATED> hipError_t dense_nt_tile(hipStream_t s, const DenseParams &P, int b) {
-  if (b == 256) return dense_nt_run<KIND, GATED, 256, 256, 2, 2>(s, P);
-  if (b == 128) return dense_nt_run<KIND, GATED, 128, 128, 2, 2>(s, P);
-  return dense_nt_run<KIND, GATED, 64, 64, 2, 2>(s, P);
+  if (b == 256) return dense_nt_run<KIND, GATED, 1, 256, 256, 2, 2>(s, P);
+  if (b == 128) return dense_nt_run<KIND, GATED, 1, 128, 128, 2, 2>(s, P);
+  if (P.segs.count > 1) return dense_nt_run<KIND, GATED, dense_nt_planes<KIND, GATED>(), 64, 64, 2, 2>(s, P);
+  return dense_nt_run<KIND, GATED, 1, 64, 64, 2, 2>(s, P);
 }
 template <int KIND, bool GATED> hipError_t dense_nt_init() {
-  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, 256, 256, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                             (int)DenseNtCfg<KIND, 256, 256>::lds);
+  constexpr int PL = dense_nt_planes<KIND, GATED>();
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, 1, 256, 256, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                           (int)DenseNtCfg<KIND, 1, 256, 256>::lds);
+  if (e != hipSuccess || PL == 1) return e;
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, PL, 64, 64, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)DenseNtCfg<KIND, PL, 64, 64>::lds);
 }
 #define DENSE_NT(KIND, GATED)                                                                        \
   template hipError_t dense_nt_tile<KIND, GATED>(hipStream_t s, const DenseParams &P, int b);       \

@@ -73,6 +73,21 @@ template <int SIZE> __device__ __forceinline__ DenseWork dense_work(const DenseP
   return w;
 }
 
+// f with the planes of both operands in each product of numbers of PL planes, in the order of dense_segs.
+template <int PL, typename F> __device__ __forceinline__ void with_segs(F f) {
+  using std::integral_constant;
+  if constexpr (PL == 3) {
+    f(integral_constant<int, 2>(), integral_constant<int, 0>());
+    f(integral_constant<int, 1>(), integral_constant<int, 1>());
+    f(integral_constant<int, 0>(), integral_constant<int, 2>());
+  }
+  if constexpr (PL >= 2) {
+    f(integral_constant<int, 1>(), integral_constant<int, 0>());
+    f(integral_constant<int, 0>(), integral_constant<int, 1>());
+  }
+  f(integral_constant<int, 0>(), integral_constant<int, 0>());
+}
+
 // Eight numbers as fp32.
 template <int XT> __device__ __forceinline__ void x_values(const Raw8<XT> &r, float (&v)[8]) {
 #pragma unroll

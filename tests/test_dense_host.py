@@ -55,6 +55,11 @@ def test_gated_product_checks_every_argument(plan):
     assert call(tokens=1 << 22, m=8192, ldh=8192, ldk=16384) == UNSUPPORTED
 
 
+def test_the_binding_knows_how_many_tokens_need_no_workspace(plan):
+    for few, name, more in ((binding.GATED_FEW, "rsvd_gated_product_bytes", (0,)), (binding.F8_FEW, "rsvd_f8_product_bytes", ()), (binding.F8_FEW, "rsvd_f8_product_grad_bytes", ())):
+        assert bytes_of(plan, name, X_BF16, few, 100, 200, *more) == 0 and bytes_of(plan, name, X_BF16, few + 1, 100, 200, *more) > 0
+
+
 def test_gated_gradient_checks_every_argument(plan):
     call = caller(plan, "rsvd_gated_product_grad", "ctx stream type act tokens n m dH lddh X ldx W ldw kept ldk dX lddx dW lddw f32 acc ws bytes", ctx=plan.h, stream=NULL,
                   type=X_F16, act=1, tokens=100, n=72, m=50, dH=PTR, lddh=50, X=PTR, ldx=72, W=PTR, ldw=72, kept=PTR, ldk=100, dX=PTR, lddx=72, dW=PTR, lddw=72,

@@ -22,11 +22,14 @@ inline DenseSegs dense_segs(int planes) {
   return {1, 0u, 0u};
 }
 
-// value = alpha sum + beta D, stored in `type`, or as two fp16 numbers `plane` bytes apart (planes = 2).  D: fp16 numbers, `planes` of them.
+// value = alpha sum + (beta + gamma (rows_m + columns_n)) D, stored in `type`, or as two fp16 numbers c_plane bytes apart (planes = 2).  D: fp16 numbers, d_planes of them.
+// diagonal: the values of row m = column m go there in fp32, with rows_m (beta + gamma rows_m) added (rows are then the diagonal of D, which has zeros), and zeros to C.
 struct LinearOut {
   float alpha = 1.f, beta = 0.f;
   const uint16_t *D = nullptr; int64_t ldd = 0, d_plane = 0, d_batch = 0;      // (elements, bytes, elements)
   int d_planes = 1;
+  float gamma = 0.f;
+  const float *rows = nullptr, *columns = nullptr; float *diagonal = nullptr; int64_t v_batch = 0;      // (NULL: zeros, not wanted; elements from problem to problem, of all three)
   void *C = nullptr; int64_t ldc = 0, c_plane = 0, c_batch = 0;               // (elements, bytes, elements)
   int type = RSVD_X_F32, planes = 1, accumulate = 0;
   int64_t width = 0;                       // columns stored, zeros from N on (0: N)
@@ -79,17 +82,18 @@ struct GatedFewDesc {
   GatedOut out;
 };
 hipError_t gated_few_launch(rsvd_ctx *ctx, hipStream_t s, const GatedFewDesc &d);
-// D from kept products.
-hipError_t gated_slope_launch(hipStream_t s, int64_t tokens, int64_t m, const GatedOut &o);
-// A matrix as the products want it: 16-bit numbers in rows of `width` (a multiple of 8) with zeros behind n; fp32 as three bf16 planes.
-hipError_t planes_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint16_t *out, int64_t width, int64_t plane);
+// What has to be laid out before the products, in one launch: matrices of `n` columns as 16-bit numbers in rows of `width` (a multiple of 8) with zeros behind n, fp32 as three
+// bf16 planes `plane` bytes apart (rows = 0: none); and D from kept products (slope.kept; tokens = 0: none).
+struct LayOut { const void *X; int64_t ldx, rows; uint16_t *out; int64_t plane; };
+hipError_t lay_out_launch(hipStream_t s, rsvd_xtype type, int64_t n, int64_t width, const LayOut &x, const LayOut &w, int64_t tokens, int64_t m, const GatedOut &slope);
 
 // ---------------------------------------------------------------- f8.hip
 constexpr int64_t kF8Few = 64;
-// X (rows x n) to codes in blocks of 128: of a row (codes: rows x width, powers rows x ldp), or of 128 rows (codes: n x width, powers n x ldp; width = rows up to a
-// multiple of 128).  Zeros behind the last number.
+// X (rows x n) to codes in blocks of 128 of a row (codes: rows x width, powers rows x ldp), zeros behind the last number; Y (rows x m) and X (rows x n) to codes in blocks of 128
+// rows (m x width and n x width, powers of rows of ldp; width = rows up to a multiple of 128).
 hipError_t f8_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint8_t *codes, int64_t width, uint8_t *powers, int64_t ldp);
-hipError_t f8_columns_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint8_t *codes, int64_t width, uint8_t *powers, int64_t ldp);
+hipError_t f8_columns_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t m, const void *Y, int64_t ldy, uint8_t *y_codes, uint8_t *y_powers, int64_t n, const void *X,
+                             int64_t ldx, uint8_t *x_codes, uint8_t *x_powers, int64_t width, int64_t ldp);
 // W (m x n) to codes in blocks of 128 x 128, and the same in the other order (NULL: not wanted).
 hipError_t f8_weight_launch(hipStream_t s, rsvd_xtype type, int64_t m, int64_t n, const void *W, int64_t ldw, uint8_t *codes, int64_t ldq, uint8_t *powers, int64_t ldp,
                             uint8_t *codes_t, int64_t ldqt, uint8_t *powers_t, int64_t ldpt);
@@ -104,10 +108,10 @@ struct F8FewDesc {
 hipError_t f8_few_launch(rsvd_ctx *ctx, hipStream_t s, const F8FewDesc &d);
 
 // ---------------------------------------------------------------- orthogonal.hip
-// |G| of every matrix by parts (kNormParts doubles each), and G / |G| times 2^13 as one or two fp16 planes with zeros up to `width`.
+// |G| of every matrix by parts (kNormParts doubles each), and G / |G| times 2^13 as two fp16 planes with zeros up to `width`.
 constexpr int kNormParts = 256;
 hipError_t norm_launch(hipStream_t s, rsvd_xtype type, int batch, int64_t m, int64_t n, const void *G, int64_t ldg, int64_t stride, double *parts);
 hipError_t unit_launch(hipStream_t s, rsvd_xtype type, int batch, int64_t m, int64_t n, const void *G, int64_t ldg, int64_t stride, const double *parts,
-                       uint16_t *X, int64_t width, int64_t plane, int planes);
+                       uint16_t *X, int64_t width, int64_t plane);
 
 }  // namespace rsvd

@@ -176,10 +176,14 @@ int f8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int
 }
 
 // ---- orthogonalised updates
-// fp16 numbers that hold an iterate: their 2^-12 is lost in the rounding of a bf16 result; two of them leave out 2^-22.
+// What is held of an iteration.  An iterate X is two fp16 numbers (2^-22 left out): what a rounding of X adds in directions of small singular values would be taken for a part
+// of them and grow with them (four large singular values among hundreds, a hundred times the others: 4 % of a result, 0.15 % with two numbers until the last two steps).  The square A and the
+// polynomial B = b A + c A^2 are fp16 numbers off their diagonals, which are held in fp32: near the end B is close to -2.7 times the unit matrix and a I + B to 0.7 of it.
+// bf16 results: products take the first number of each (what that leaves out is a relative error of A and B alone, 4 to 9e-4 of a result beside the 1.7e-3 of its
+// rounding); others take two of each, and three products, for 2^-22.
 int iterate_planes(rsvd_xtype type) { return type == RSVD_X_BF16 ? 1 : 2; }
 
-struct OrthogonalLayout { size_t parts, X[2], A, B, partial, partial_bytes, total; int64_t small, x_ld, a_ld, x_plane, a_plane; };
+struct OrthogonalLayout { size_t parts, X[2], A, B, a_diagonal, b_diagonal, partial, partial_bytes, total; int64_t small, x_ld, a_ld, x_plane, a_plane; };
 
 DenseDesc gram_desc(rsvd_xtype type, int batch, int64_t m, int64_t n) {
   DenseDesc d;
@@ -214,9 +218,11 @@ OrthogonalLayout orthogonal_layout(const rsvd_ctx *ctx, rsvd_xtype type, int bat
   L.x_plane = (int64_t)batch * m * L.x_ld * 2;
   L.a_plane = (int64_t)batch * L.small * L.a_ld * 2;
   L.parts = take((size_t)batch * kNormParts * 8);
-  for (int i = 0; i < 2; ++i) L.X[i] = take((size_t)planes * L.x_plane);
+  for (int i = 0; i < 2; ++i) L.X[i] = take((size_t)2 * L.x_plane);
   L.A = take((size_t)planes * L.a_plane);
   L.B = take((size_t)planes * L.a_plane);
+  L.a_diagonal = take((size_t)batch * L.small * 4);
+  L.b_diagonal = take((size_t)batch * L.small * 4);
   L.partial_bytes = most(dense_partial_bytes(ctx, gram_desc(type, batch, m, n)), dense_partial_bytes(ctx, square_desc(type, batch, L.small)));
   L.partial_bytes = most(L.partial_bytes, dense_partial_bytes(ctx, apply_desc(type, batch, m, n)));
   L.partial = take(L.partial_bytes);
@@ -291,15 +297,11 @@ int rsvd_gated_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_act ac
   const int64_t width = width_of(n);
   Operand x = in_place(X, ldx), w = in_place(W, ldw);
   if (!x_lies || !w_lies) {
+    if (!x_lies) x = in_planes(ws + L.x, tokens, width);
+    if (!w_lies) w = in_planes(ws + L.w, 2 * m, width);
     ProfScope ps(ctx, s, PK_SMALL);
-    if (!x_lies) {
-      x = in_planes(ws + L.x, tokens, width);
-      RSVD_TRY(planes_launch(s, type, tokens, n, X, ldx, (uint16_t *)(ws + L.x), width, x.plane), "operands of the gated product");
-    }
-    if (!w_lies) {
-      w = in_planes(ws + L.w, 2 * m, width);
-      RSVD_TRY(planes_launch(s, type, 2 * m, n, W, ldw, (uint16_t *)(ws + L.w), width, w.plane), "operands of the gated product");
-    }
+    RSVD_TRY(lay_out_launch(s, type, n, width, {X, ldx, x_lies ? 0 : tokens, (uint16_t *)(ws + L.x), x.plane},
+                            {W, ldw, w_lies ? 0 : 2 * m, (uint16_t *)(ws + L.w), w.plane}, 0, m, o), "operands of the gated product");
   }
   DenseDesc d = gated_desc(type, tokens, n, m);
   d.A = x.p; d.lda = x.ld; d.a_plane = x.plane;
@@ -374,16 +376,11 @@ int rsvd_gated_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_a
   o.dH = dH; o.lddh = lddh;
   o.D = (uint16_t *)(ws + L.D); o.ldD = width_of(2 * m); o.plane = D.plane;
   if (!x_lies || !w_lies || !recompute) {
+    if (!x_lies) x = in_planes(ws + L.x, tokens, width);
+    if (!w_lies) w = in_planes(ws + L.w, 2 * m, width);
     ProfScope ps(ctx, s, PK_SMALL);
-    if (!x_lies) {
-      x = in_planes(ws + L.x, tokens, width);
-      RSVD_TRY(planes_launch(s, type, tokens, n, X, ldx, (uint16_t *)(ws + L.x), width, x.plane), "operands of the gated gradient");
-    }
-    if (!w_lies) {
-      w = in_planes(ws + L.w, 2 * m, width);
-      RSVD_TRY(planes_launch(s, type, 2 * m, n, W, ldw, (uint16_t *)(ws + L.w), width, w.plane), "operands of the gated gradient");
-    }
-    if (!recompute) RSVD_TRY(gated_slope_launch(s, tokens, m, o), "gradients of gate and up");
+    RSVD_TRY(lay_out_launch(s, type, n, width, {X, ldx, x_lies ? 0 : tokens, (uint16_t *)(ws + L.x), x.plane},
+                            {W, ldw, w_lies ? 0 : 2 * m, (uint16_t *)(ws + L.w), w.plane}, recompute ? 0 : tokens, m, o), "operands of the gated gradient");
   }
   float *partial = (float *)(ws + L.partial);
   if (recompute) {
@@ -513,8 +510,7 @@ int rsvd_f8_weight_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t to
   const int64_t width = f8_width(tokens), ldp = f8_powers(tokens);
   {
     ProfScope ps(ctx, s, PK_SMALL);
-    RSVD_TRY(f8_columns_launch(s, type, tokens, m, dY, lddy, a, width, a_pow, ldp), "gradients to 8-bit floats");
-    RSVD_TRY(f8_columns_launch(s, type, tokens, n, X, ldx, b, width, b_pow, ldp), "tokens to 8-bit floats");
+    RSVD_TRY(f8_columns_launch(s, type, tokens, m, dY, lddy, a, a_pow, n, X, ldx, b, b_pow, width, ldp), "gradients and tokens to 8-bit floats");
   }
   DenseDesc d = f8_desc(wtype == RSVD_X_F32, m, n, tokens);
   d.A = a; d.lda = width; d.a_pow = a_pow; d.ld_apow = ldp;
@@ -573,20 +569,27 @@ int rsvd_orthogonalize(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int batch, 
   {
     ProfScope ps(ctx, s, PK_SMALL);
     RSVD_TRY(norm_launch(s, type, batch, m, n, G, ldg, stride_g, (double *)(ws + L.parts)), "norm");
-    RSVD_TRY(unit_launch(s, type, batch, m, n, G, ldg, stride_g, (const double *)(ws + L.parts), (uint16_t *)(ws + L.X[0]), L.x_ld, L.x_plane, planes), "first iterate");
+    RSVD_TRY(unit_launch(s, type, batch, m, n, G, ldg, stride_g, (const double *)(ws + L.parts), (uint16_t *)(ws + L.X[0]), L.x_ld, L.x_plane), "first iterate");
   }
   ProfScope ps(ctx, s, PK_GRAM);
   float *partial = (float *)(ws + L.partial);
   constexpr float kUnit = 8192.f;                     // what iterates, their squares and polynomials are held times
-  auto half = [&](LinearOut &o, size_t at) {
-    o.C = ws + at; o.type = RSVD_X_F16; o.planes = planes;
+  auto half = [&](LinearOut &o, size_t at, int n) {
+    o.C = ws + at; o.type = RSVD_X_F16; o.planes = n;
   };
+  float *const a_diagonal = (float *)(ws + L.a_diagonal), *const b_diagonal = (float *)(ws + L.b_diagonal);
+  // (how much what is lost of an iterate may grow until the last: from 16 times on, bf16 results need both numbers, too)
+  float grows[65];
+  grows[steps] = 1.f;
+  for (int step = steps - 1; step >= 0; --step) grows[step] = grows[step + 1] * fmaxf(1.f, fabsf(coefficients[3 * step]));
+  auto numbers = [&](int step) { return planes == 2 || grows[step] >= 16.f ? 2 : 1; };
   for (int step = 0; step < steps; ++step) {
     const char *X = ws + L.X[step & 1];
     DenseDesc g = gram_desc(type, batch, m, n);
     g.A = g.B = X; g.lda = g.ldb = L.x_ld * 2; g.a_plane = g.b_plane = L.x_plane; g.a_batch = g.b_batch = m * L.x_ld * 2;
     g.out.alpha = 1.f / kUnit;
-    half(g.out, L.A);
+    half(g.out, L.A, planes);
+    g.out.diagonal = a_diagonal; g.out.v_batch = L.small;
     g.out.ldc = L.a_ld; g.out.c_plane = L.a_plane; g.out.c_batch = L.small * L.a_ld; g.out.width = width_of(L.small);
     g.partial = partial; g.partial_bytes = L.partial_bytes;
     if (wide) RSVD_TRY(dense_nt_launch(ctx, s, g), "square of an iterate");
@@ -598,6 +601,8 @@ int rsvd_orthogonalize(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int batch, 
     p.out.C = ws + L.B;
     p.out.alpha = coefficients[3 * step + 2] / kUnit; p.out.beta = coefficients[3 * step + 1];
     p.out.D = (const uint16_t *)(ws + L.A); p.out.ldd = L.a_ld; p.out.d_plane = L.a_plane; p.out.d_batch = L.small * L.a_ld; p.out.d_planes = planes;
+    // (with A = O + diag d:  A^2 = O^2 + d_m O + O d_n off the diagonal, and d^2 on it)
+    p.out.gamma = p.out.alpha; p.out.rows = p.out.columns = a_diagonal; p.out.diagonal = b_diagonal;
     p.partial = partial; p.partial_bytes = L.partial_bytes;
     RSVD_TRY(dense_nt_launch(ctx, s, p), "polynomial of an iterate");
 
@@ -609,11 +614,13 @@ int rsvd_orthogonalize(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int batch, 
     a.ldb = wide ? L.x_ld * 2 : L.a_ld * 2; a.b_plane = wide ? L.x_plane : L.a_plane; a.b_batch = wide ? x_batch : b_batch;
     a.out.alpha = last ? 1.f / (kUnit * kUnit) : 1.f / kUnit;
     a.out.beta = last ? coefficients[3 * step] / kUnit : coefficients[3 * step];
-    a.out.D = (const uint16_t *)X; a.out.ldd = L.x_ld; a.out.d_plane = L.x_plane; a.out.d_batch = m * L.x_ld; a.out.d_planes = planes;
+    a.out.D = (const uint16_t *)X; a.out.ldd = L.x_ld; a.out.d_plane = L.x_plane; a.out.d_batch = m * L.x_ld; a.out.d_planes = numbers(step);
+    a.out.gamma = a.out.alpha; a.out.v_batch = L.small;
+    if (wide) a.out.rows = b_diagonal; else a.out.columns = b_diagonal;
     if (last) {
       a.out.C = O; a.out.ldc = ldo; a.out.c_batch = stride_o; a.out.type = type;
     } else {
-      half(a.out, L.X[(step + 1) & 1]);
+      half(a.out, L.X[(step + 1) & 1], numbers(step + 1));
       a.out.ldc = L.x_ld; a.out.c_plane = L.x_plane; a.out.c_batch = m * L.x_ld; a.out.width = width_of(n);
     }
     a.partial = partial; a.partial_bytes = L.partial_bytes;

@@ -205,33 +205,95 @@ template <typename F> __device__ __forceinline__ void with_act(int act, F f) {
   else f(std::integral_constant<int, GATED_RELU>());
 }
 
+// Eight numbers of each of C groups of D as they lie, both planes, and rows_m.
+template <int C> struct DRows { u32x4 high[C], low[C]; float row; };
+
 // The end of C groups of V times four columns.  Group c has row m[c] (if it is there) and columns from n[c] on, of which those before `width` are stored and those from N on are
-// zeros.  All loads come before the stores.  WHOLE: all rows and columns exist (no branches between loads).
-template <int C, int V, bool WHOLE>
-__device__ __forceinline__ void linear_end(const LinearOut &O, int64_t N, int batch, const int64_t (&m)[C], const int64_t (&n)[C], const bool (&there)[C], f32x4 (&v)[C][V]) {
+// zeros.  All loads come before the stores.  WHOLE: all rows and columns exist (no branches between loads).  AHEAD: D, rows and columns
+// (a vector of them for each of v's) were loaded before (V = 2).
+template <int C, int V, bool WHOLE, bool AHEAD = false>
+__device__ __forceinline__ void linear_end(const LinearOut &O, int64_t N, int batch, const int64_t (&m)[C], const int64_t (&n)[C], const bool (&there)[C], f32x4 (&v)[C][V],
+                                           const DRows<AHEAD ? C : 1> ahead = {}, const f32x4 (*ahead_columns)[V] = nullptr) {
+  // (one by one, in scalar registers: arguments of the kernel that are read together and under conditions would go through memory)
+  float alpha = O.alpha, beta = O.beta, gamma = O.gamma;
+  const uint16_t *d = O.D;
+  asm volatile("" : "+s"(alpha), "+s"(beta), "+s"(gamma), "+s"(d));
+  const int64_t ldd = O.ldd, d_plane = O.d_plane / 2;
+  const bool has_d = d != nullptr, two = O.d_planes == 2;
+  d += batch * O.d_batch;
+  const float *const rows = O.rows, *const columns = O.columns;
+  float *const diagonal = O.diagonal;
+  const int64_t v_first = batch * O.v_batch, width = O.width;
   auto have = [&](int c) RSVD_INLINE { return WHOLE ? 4 * V : there[c] ? left_of<V>(n[c], N) : 0; };
-  auto left = [&](int c) RSVD_INLINE { return WHOLE ? 4 * V : there[c] ? left_of<V>(n[c], O.width) : 0; };
+  auto left = [&](int c) RSVD_INLINE { return WHOLE ? 4 * V : there[c] ? left_of<V>(n[c], width) : 0; };
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
-    for (int x = 0; x < V; ++x) v[c][x] *= O.alpha;
-  if (O.D != nullptr) {
-    const uint16_t *d = O.D + batch * O.d_batch;
+    for (int x = 0; x < V; ++x) v[c][x] *= alpha;
+  if (has_d) {
     f32x4 sum[C][V], low[C][V];
-#pragma unroll
-    for (int c = 0; c < C; ++c) load_row<RSVD_X_F16, V>(d, m[c] * O.ldd + n[c], have(c), sum[c]);
-    if (O.d_planes == 2) {
-#pragma unroll
-      for (int c = 0; c < C; ++c) load_row<RSVD_X_F16, V>(d + O.d_plane / 2, m[c] * O.ldd + n[c], have(c), low[c]);
+    if constexpr (AHEAD) {
 #pragma unroll
       for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int x = 0; x < V; ++x) sum[c][x] += low[c][x];
+        for (int h = 0; h < 4; ++h) {
+          const unsigned high2 = ahead.high[c][h], low2 = two ? ahead.low[c][h] : 0u;
+          const f16x2 x = __builtin_bit_cast(f16x2, high2), y = __builtin_bit_cast(f16x2, low2);
+          sum[c][h >> 1][2 * (h & 1)] = (float)x[0] + (float)y[0];
+          sum[c][h >> 1][2 * (h & 1) + 1] = (float)x[1] + (float)y[1];
+        }
+    } else {
+#pragma unroll
+      for (int c = 0; c < C; ++c) load_row<RSVD_X_F16, V>(d, m[c] * ldd + n[c], have(c), sum[c]);
+      if (two) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) load_row<RSVD_X_F16, V>(d + d_plane, m[c] * ldd + n[c], have(c), low[c]);
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+          for (int x = 0; x < V; ++x) sum[c][x] += low[c][x];
+      }
+    }
+    f32x4 by[C][V];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      float row = beta;
+      if constexpr (AHEAD) row += gamma * ahead.row;
+      else if (rows != nullptr && (WHOLE || there[c])) row += gamma * rows[v_first + m[c]];
+#pragma unroll
+      for (int x = 0; x < V; ++x) {
+        by[c][x] = (f32x4)row;
+        if constexpr (AHEAD) by[c][x] += gamma * ahead_columns[c][x];
+        else if (columns != nullptr) by[c][x] += gamma * load4<RSVD_X_F32>(columns + v_first, n[c] + 4 * x, have(c) - 4 * x);
+      }
     }
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int x = 0; x < V; ++x) v[c][x] += O.beta * sum[c][x];
+      for (int x = 0; x < V; ++x) v[c][x] += by[c][x] * sum[c][x];
+  }
+  if (diagonal != nullptr) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int at = (int)(m[c] - n[c]);                 // (the value on the diagonal, if the group has it)
+      if ((WHOLE || there[c]) && at >= 0 && at < 4 * V) {
+        float own = 0.f;
+        if (rows != nullptr) own = rows[v_first + m[c]];
+        float value = own * (beta + gamma * own);
+#pragma unroll
+        for (int x = 0; x < V; ++x) {
+          const f32x4 old = v[c][x];
+          f32x4 rest;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            value += at == 4 * x + e ? old[e] : 0.f;
+            rest[e] = at == 4 * x + e ? 0.f : old[e];
+          }
+          v[c][x] = rest;
+        }
+        diagonal[v_first + m[c]] = value;
+      }
+    }
   }
   if constexpr (!WHOLE) {
 #pragma unroll
@@ -483,6 +545,32 @@ template <bool GATED, int BN, int TM, int TN> __device__ __forceinline__ void de
   bool there[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) n[c] = n1 + 16 * V * c + 4 * V * (lane >> 4);
+  // (D of the next row of blocks is under way while this one ends: 8 to 10 % of the time of a product of 4096 k with D)
+  constexpr bool AHEAD = !GATED && V == 2;
+  const uint16_t *d_first = P.out.D;
+  asm volatile("" : "+s"(d_first));
+  const bool d_ahead = AHEAD && whole && partial == nullptr && d_first != nullptr;
+  const uint16_t *const d_high = d_first + batch * P.out.d_batch, *const d_low = P.out.d_planes == 2 ? d_high + P.out.d_plane / 2 : d_high;
+  const int64_t ldd = P.out.ldd;
+  DRows<AHEAD ? C : 1> next = {};
+  const float *const rows = P.out.rows, *const columns = P.out.columns;
+  const int64_t v_first = batch * P.out.v_batch;
+  f32x4 column[C][V];
+#pragma unroll
+  for (int c = 0; c < (AHEAD ? C : 0); ++c)
+#pragma unroll
+    for (int x = 0; x < V; ++x) column[c][x] = d_ahead && columns != nullptr ? *reinterpret_cast<const f32x4_any *>(columns + v_first + n[c] + 4 * x) : (f32x4)0.f;
+  auto load_next = [&](int i) RSVD_INLINE {
+    if constexpr (AHEAD) {
+      const int64_t row = m1 + 16 * (i < TM ? i : TM - 1) + (lane & 15), at = row * ldd;
+      if (rows != nullptr) next.row = rows[v_first + row];
+#pragma unroll
+      for (int c = 0; c < C; ++c) next.high[c] = *reinterpret_cast<const u32x4_any *>(d_high + at + n[c]);
+#pragma unroll
+      for (int c = 0; c < C; ++c) next.low[c] = *reinterpret_cast<const u32x4_any *>(d_low + at + n[c]);
+    }
+  };
+  if (d_ahead) load_next(0);
 #pragma unroll 1
   for (int i = 0; i < TM; ++i) {                        // (one copy of what follows, not one for each row of blocks)
     f32x4 v[C][V], u[C][V];
@@ -515,8 +603,17 @@ template <bool GATED, int BN, int TM, int TN> __device__ __forceinline__ void de
       if (whole) gated_end<C, V, true>(P.gate, P.N, m, n, there, v, u);
       else gated_end<C, V, false>(P.gate, P.N, m, n, there, v, u);
     } else {
-      if (whole) linear_end<C, V, true>(P.out, P.N, batch, m, n, there, v);
-      else linear_end<C, V, false>(P.out, P.N, batch, m, n, there, v);
+      if (d_ahead) {
+        if constexpr (AHEAD) {
+          const DRows<C> now = next;
+          load_next(i + 1);
+          linear_end<C, V, true, true>(P.out, P.N, batch, m, n, there, v, now, column);
+        }
+      } else if (whole) {
+        linear_end<C, V, true>(P.out, P.N, batch, m, n, there, v);
+      } else {
+        linear_end<C, V, false>(P.out, P.N, batch, m, n, there, v);
+      }
     }
   }
 }

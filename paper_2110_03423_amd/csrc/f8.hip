@@ -61,13 +61,21 @@ template <int XT> __global__ __launch_bounds__(256) void f8_rows_kernel(const ch
 }
 
 // Blocks of 128 rows, 64 columns a workgroup: through LDS, a column a thread and then a row of codes.
-template <int XT> __global__ __launch_bounds__(256) void f8_columns_kernel(const char *X, int64_t ldx, int64_t rows, int64_t n, uint8_t *codes, int64_t width,
-                                                                          uint8_t *powers, int64_t ldp) {
+// Two matrices of the same rows in one launch, one behind the other (block by block of rows in turn, 16384 x 8192 and 4096 took a product of them 3 % more).
+struct F8Columns { const char *X; int64_t ldx, n; uint8_t *codes, *powers; };
+template <int XT> __global__ __launch_bounds__(256) void f8_columns_kernel(const F8Columns A, const F8Columns B, int a_groups, int64_t rows, int64_t width, int64_t ldp) {
   constexpr int SIZE = XTraits<XT>::SIZE, PITCH = 65, OUT = 144;
   __shared__ __attribute__((aligned(16))) float tile[128 * PITCH];
   __shared__ unsigned tops[4][64];
   const int tid = threadIdx.x, c = tid & 63, q = tid >> 6;
-  const int64_t r0 = (int64_t)blockIdx.y * 128, c0 = (int64_t)blockIdx.x * 64;
+  const int row_blocks = (int)((rows + 127) / 128);
+  const bool first = (int)blockIdx.x < a_groups * row_blocks;
+  const int at = (int)blockIdx.x - (first ? 0 : a_groups * row_blocks);
+  const char *const X = first ? A.X : B.X;
+  const int64_t ldx = first ? A.ldx : B.ldx, n = first ? A.n : B.n;
+  uint8_t *const codes = first ? A.codes : B.codes, *const powers = first ? A.powers : B.powers;
+  const int across = (int)((n + 63) / 64), row_block = at / across;
+  const int64_t r0 = (int64_t)row_block * 128, c0 = (int64_t)(at - row_block * across) * 64;
 #pragma unroll
   for (int p = 0; p < 4; ++p) {
     const int row = (tid >> 3) + 32 * p, col = 8 * (tid & 7);
@@ -90,7 +98,7 @@ template <int XT> __global__ __launch_bounds__(256) void f8_columns_kernel(const
   top = max(max(tops[0][c], tops[1][c]), max(tops[2][c], tops[3][c]));
   const unsigned power = f8_power(top);
   const float by = f8_factor(power);
-  if (q == 0 && c0 + c < n) powers[(c0 + c) * ldp + blockIdx.y] = (uint8_t)power;
+  if (q == 0 && c0 + c < n) powers[(c0 + c) * ldp + row_block] = (uint8_t)power;
   char *const out = reinterpret_cast<char *>(tile);      // (everybody has read the tile)
 #pragma unroll
   for (int p = 0; p < 4; p += 2) {
@@ -165,13 +173,14 @@ hipError_t f8_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t 
   return hipGetLastError();
 }
 
-hipError_t f8_columns_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint8_t *codes, int64_t width, uint8_t *powers,
-                             int64_t ldp) {
-  const dim3 grid((unsigned)ceil_div(n, 64), (unsigned)ceil_div(rows, 128));
-  const char *x = (const char *)X;
-  if (type == RSVD_X_BF16) hipLaunchKernelGGL((f8_columns_kernel<RSVD_X_BF16>), grid, dim3(256), 0, s, x, ldx, rows, n, codes, width, powers, ldp);
-  else if (type == RSVD_X_F16) hipLaunchKernelGGL((f8_columns_kernel<RSVD_X_F16>), grid, dim3(256), 0, s, x, ldx, rows, n, codes, width, powers, ldp);
-  else hipLaunchKernelGGL((f8_columns_kernel<RSVD_X_F32>), grid, dim3(256), 0, s, x, ldx, rows, n, codes, width, powers, ldp);
+hipError_t f8_columns_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t m, const void *Y, int64_t ldy, uint8_t *y_codes, uint8_t *y_powers, int64_t n, const void *X,
+                             int64_t ldx, uint8_t *x_codes, uint8_t *x_powers, int64_t width, int64_t ldp) {
+  const F8Columns A = {(const char *)Y, ldy, m, y_codes, y_powers}, B = {(const char *)X, ldx, n, x_codes, x_powers};
+  const int a_groups = (int)ceil_div(m, 64);
+  const dim3 grid((unsigned)((a_groups + ceil_div(n, 64)) * ceil_div(rows, 128)));
+  if (type == RSVD_X_BF16) hipLaunchKernelGGL((f8_columns_kernel<RSVD_X_BF16>), grid, dim3(256), 0, s, A, B, a_groups, rows, width, ldp);
+  else if (type == RSVD_X_F16) hipLaunchKernelGGL((f8_columns_kernel<RSVD_X_F16>), grid, dim3(256), 0, s, A, B, a_groups, rows, width, ldp);
+  else hipLaunchKernelGGL((f8_columns_kernel<RSVD_X_F32>), grid, dim3(256), 0, s, A, B, a_groups, rows, width, ldp);
   return hipGetLastError();
 }
 

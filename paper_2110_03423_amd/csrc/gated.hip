@@ -107,66 +107,59 @@ hipError_t gated_few_launch(rsvd_ctx *, hipStream_t s, const GatedFewDesc &d) {
   return hipGetLastError();
 }
 
-// ---------------------------------------------------------------- gradients of gate and up from the kept products; memory is the bound
-__global__ __launch_bounds__(256) void gated_slope_kernel(const GatedOut O, int64_t tokens, int64_t m) {
-  const int per_row = (int)((m + 7) / 8);
-  const int64_t total = tokens * per_row;
-  for (int64_t group = blockIdx.x; group * 256 < total; group += gridDim.x) {
-    int64_t t[1], n[1];
-    int place;
-    piece_of(group, per_row, t[0], place);
-    n[0] = 8 * (int64_t)place;
-    const bool there[1] = {t[0] < tokens};
-    if (!there[0]) continue;
-    const int left = left_of<2>(n[0], m);
-    f32x4 g[1][2], u[1][2];
-    with_type(O.type, [&](auto type) RSVD_INLINE {
-      load_row<decltype(type)::value, 2>(O.kept, t[0] * O.ldk + n[0], left, g[0]);
-      load_row<decltype(type)::value, 2>(O.kept, t[0] * O.ldk + m + n[0], left, u[0]);
-    });
-    gated_end<1, 2, false>(O, m, t, n, there, g, u);
-  }
-}
-hipError_t gated_slope_launch(hipStream_t s, int64_t tokens, int64_t m, const GatedOut &o) {
-  int64_t groups = ceil_div(tokens * ceil_div(m, 8), 256);
-  if (groups > 16384) groups = 16384;
-  hipLaunchKernelGGL(gated_slope_kernel, dim3((unsigned)groups), dim3(256), 0, s, o, tokens, m);
-  return hipGetLastError();
-}
-
 // ---------------------------------------------------------------- operands
-template <int XT> __global__ __launch_bounds__(256) void planes_kernel(const char *X, int64_t ldx, int64_t rows, int64_t n, uint16_t *out, int64_t width, int64_t plane) {
+// Gradients of gate and up from the kept products, and matrices as the products want them; memory is the bound.  One launch: workgroups of the one, then of the others.
+template <int TYPE> __device__ __forceinline__ void slope_group(const GatedOut &O, int64_t tokens, int64_t m, int64_t group) {
+  int64_t t[1], n[1];
+  int place;
+  piece_of(group, (int)((m + 7) / 8), t[0], place);
+  n[0] = 8 * (int64_t)place;
+  const bool there[1] = {t[0] < tokens};
+  if (!there[0]) return;
+  const int left = left_of<2>(n[0], m);
+  f32x4 g[1][2], u[1][2];
+  load_row<TYPE, 2>(O.kept, t[0] * O.ldk + n[0], left, g[0]);
+  load_row<TYPE, 2>(O.kept, t[0] * O.ldk + m + n[0], left, u[0]);
+  gated_end<1, 2, false>(O, m, t, n, there, g, u);
+}
+template <int XT> __device__ __forceinline__ void planes_group(const LayOut &L, int64_t n, int64_t width, int64_t group) {
   constexpr int SIZE = XTraits<XT>::SIZE;
-  const int per_row = (int)(width / 8);
-  const int64_t total = rows * per_row;
-  for (int64_t group = blockIdx.x; group * 256 < total; group += gridDim.x) {
-    int64_t r;
-    int place;
-    piece_of(group, per_row, r, place);
-    if (r >= rows) continue;
-    const int64_t c = 8 * (int64_t)place;
-    const Raw8<XT> v = raw_load8<XT>(X + (r * ldx + c) * SIZE, n - c);
-    uint16_t *to = out + r * width + c;
-    if constexpr (XT == RSVD_X_F32) {
-      u32x4 p[3];
-      split_operand<XT>(v, p);
+  int64_t r;
+  int place;
+  piece_of(group, (int)(width / 8), r, place);
+  if (r >= L.rows) return;
+  const int64_t c = 8 * (int64_t)place;
+  const Raw8<XT> v = raw_load8<XT>(reinterpret_cast<const char *>(L.X) + (r * L.ldx + c) * SIZE, n - c);
+  uint16_t *to = L.out + r * width + c;
+  if constexpr (XT == RSVD_X_F32) {
+    u32x4 p[3];
+    split_operand<XT>(v, p);
 #pragma unroll
-      for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x4 *>(to + q * (plane / 2)) = p[q];
-    } else {
-      *reinterpret_cast<u32x4 *>(to) = v.w[0];
-    }
+    for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x4 *>(to + q * (L.plane / 2)) = p[q];
+  } else {
+    *reinterpret_cast<u32x4 *>(to) = v.w[0];
   }
 }
-hipError_t planes_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint16_t *out, int64_t width, int64_t plane) {
-  int64_t groups = ceil_div(rows * (width / 8), 256);
-  if (groups > 16384) groups = 16384;
-  if (type == RSVD_X_F32)
-    hipLaunchKernelGGL((planes_kernel<RSVD_X_F32>), dim3((unsigned)groups), dim3(256), 0, s, (const char *)X, ldx, rows, n, out, width, plane);
-  else
-    hipLaunchKernelGGL((planes_kernel<RSVD_X_F16>), dim3((unsigned)groups), dim3(256), 0, s, (const char *)X, ldx, rows, n, out, width, plane);
+struct LayOutGroups { int64_t slope, x, w; };
+template <int XT> __global__ __launch_bounds__(256) void lay_out_kernel(const LayOutGroups G, int64_t n, int64_t width, const LayOut X, const LayOut W, int64_t tokens, int64_t m,
+                                                                       const GatedOut O) {
+  for (int64_t group = blockIdx.x; group < G.slope + G.x + G.w; group += gridDim.x) {
+    if (group < G.slope) slope_group<XT>(O, tokens, m, group);
+    else if (group < G.slope + G.x) planes_group<XT>(X, n, width, group - G.slope);
+    else planes_group<XT>(W, n, width, group - G.slope - G.x);
+  }
+}
+hipError_t lay_out_launch(hipStream_t s, rsvd_xtype type, int64_t n, int64_t width, const LayOut &x, const LayOut &w, int64_t tokens, int64_t m, const GatedOut &slope) {
+  const LayOutGroups G = {ceil_div(tokens * ceil_div(m, 8), 256), ceil_div(x.rows * (width / 8), 256), ceil_div(w.rows * (width / 8), 256)};
+  int64_t groups = G.slope + G.x + G.w;
+  if (groups == 0) return hipSuccess;
+  if (groups > 65536) groups = 65536;
+  const dim3 grid((unsigned)groups);
+  if (type == RSVD_X_F32) hipLaunchKernelGGL((lay_out_kernel<RSVD_X_F32>), grid, dim3(256), 0, s, G, n, width, x, w, tokens, m, slope);
+  else if (type == RSVD_X_F16) hipLaunchKernelGGL((lay_out_kernel<RSVD_X_F16>), grid, dim3(256), 0, s, G, n, width, x, w, tokens, m, slope);
+  else hipLaunchKernelGGL((lay_out_kernel<RSVD_X_BF16>), grid, dim3(256), 0, s, G, n, width, x, w, tokens, m, slope);
   return hipGetLastError();
 }
-
 
 // ---------------------------------------------------------------- the gradient of no tokens
 template <typename T> __global__ __launch_bounds__(256) void zero_kernel(T *C, int64_t ldc, int64_t rows, int64_t n) {

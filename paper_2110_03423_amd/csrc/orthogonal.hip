@@ -40,7 +40,7 @@ template <int XT> __global__ __launch_bounds__(256) void norm_kernel(const char 
 }
 
 template <int XT> __global__ __launch_bounds__(256) void unit_kernel(const char *G, int64_t ldg, int64_t stride, int64_t m, int64_t n, const double *parts,
-                                                                    uint16_t *X, int64_t width, int64_t plane, int planes) {
+                                                                    uint16_t *X, int64_t width, int64_t plane) {
   constexpr int SIZE = XTraits<XT>::SIZE;
   static_assert(kNormParts == 256, "one a thread");
   __shared__ double wave_sum[4];
@@ -78,7 +78,7 @@ template <int XT> __global__ __launch_bounds__(256) void unit_kernel(const char 
     }
     uint16_t *to = x + r * width + 8 * c;
     *reinterpret_cast<u32x4 *>(to) = high;
-    if (planes == 2) *reinterpret_cast<u32x4 *>(reinterpret_cast<char *>(to) + plane) = low;
+    *reinterpret_cast<u32x4 *>(reinterpret_cast<char *>(to) + plane) = low;
   }
 }
 
@@ -92,14 +92,14 @@ hipError_t norm_launch(hipStream_t s, rsvd_xtype type, int batch, int64_t m, int
 }
 
 hipError_t unit_launch(hipStream_t s, rsvd_xtype type, int batch, int64_t m, int64_t n, const void *G, int64_t ldg, int64_t stride, const double *parts,
-                       uint16_t *X, int64_t width, int64_t plane, int planes) {
+                       uint16_t *X, int64_t width, int64_t plane) {
   int64_t groups = ceil_div(m * (width / 8), 256);
   if (groups > 2048) groups = 2048;
   const dim3 grid((unsigned)groups, (unsigned)batch);
   const char *g = (const char *)G;
-  if (type == RSVD_X_BF16) hipLaunchKernelGGL((unit_kernel<RSVD_X_BF16>), grid, dim3(256), 0, s, g, ldg, stride, m, n, parts, X, width, plane, planes);
-  else if (type == RSVD_X_F16) hipLaunchKernelGGL((unit_kernel<RSVD_X_F16>), grid, dim3(256), 0, s, g, ldg, stride, m, n, parts, X, width, plane, planes);
-  else hipLaunchKernelGGL((unit_kernel<RSVD_X_F32>), grid, dim3(256), 0, s, g, ldg, stride, m, n, parts, X, width, plane, planes);
+  if (type == RSVD_X_BF16) hipLaunchKernelGGL((unit_kernel<RSVD_X_BF16>), grid, dim3(256), 0, s, g, ldg, stride, m, n, parts, X, width, plane);
+  else if (type == RSVD_X_F16) hipLaunchKernelGGL((unit_kernel<RSVD_X_F16>), grid, dim3(256), 0, s, g, ldg, stride, m, n, parts, X, width, plane);
+  else hipLaunchKernelGGL((unit_kernel<RSVD_X_F32>), grid, dim3(256), 0, s, g, ldg, stride, m, n, parts, X, width, plane);
   return hipGetLastError();
 }
 

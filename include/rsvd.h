@@ -384,7 +384,8 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
  * matrices may have any leading dimension and the alignment of their elements.  A
  * matrix lies as the products read it if it is 16-bit, n is a multiple of 8, its rows
  * start at 16-byte aligned addresses and its leading dimension is at most 2^22;
- * otherwise it is copied to the workspace on the way (more than 64 tokens, gradients).
+ * otherwise it is copied to the workspace on the way (more than 32 tokens, gradients; up to
+ * 64 tokens of fp32 need none either).
  * gelu is x (1 + erf(x / sqrt 2)) / 2, gelu_tanh its usual approximation. */
 typedef enum { RSVD_ACT_SILU = 0, RSVD_ACT_GELU = 1, RSVD_ACT_GELU_TANH = 2, RSVD_ACT_RELU = 3 } rsvd_act;
 
@@ -435,7 +436,7 @@ int rsvd_f8_product_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_
 int rsvd_f8_product_grad_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, size_t *bytes);
 int rsvd_f8_weight_grad_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int dw_f32, size_t *bytes);
 
-/* Y (tokens x m) = X^ W^^T.  (workspace may be NULL where no bytes are needed: up to 64 tokens) */
+/* Y (tokens x m) = X^ W^^T.  (workspace may be NULL where no bytes are needed: up to 16 tokens) */
 int rsvd_f8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, const void *X, int64_t ldx,
                     const uint8_t *codes, int64_t ldq, const uint8_t *powers, int64_t ldp, void *Y, int64_t ldy, void *workspace, size_t workspace_bytes);
 

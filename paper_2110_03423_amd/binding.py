@@ -86,7 +86,7 @@ PROTOTYPES = {
 }
 X_BF16, X_F16, X_F32 = 0, 1, 2
 ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
-GATED_FEW = F8_FEW = 64      # tokens up to which these products need no workspace
+GATED_FEW, F8_FEW = (32, 32, 64), 16      # tokens up to which these products need no workspace (of a gated block: by type)
 
 
 def load_library():
@@ -708,7 +708,7 @@ class Rsvd:
         ldx, ldw, stream = _ld(X), _ld(W), self._raw_stream()
         if workspace is not None:
             ws = self._given(workspace)
-        elif tokens <= GATED_FEW:
+        elif tokens <= GATED_FEW[xt]:
             ws = (None, 0)
         else:
             ws = self._layer_ws(stream, "rsvd_gated_product_bytes", (xt, tokens, n, m, self._lies(X, ldx) + 2 * self._lies(W, ldw)))

@@ -206,109 +206,96 @@ struct F8FewParams {
   void *Y; int64_t ldy;
 };
 
-template <int XT, int TB, int WAVES> __global__ __launch_bounds__(64 * WAVES) void f8_few_kernel(const F8FewParams P) {
-  constexpr int SIZE = XTraits<XT>::SIZE, U = TB == 1 ? (SIZE == 2 ? 4 : 2) : TB == 2 ? (SIZE == 2 ? 2 : 1) : 1;      // steps whose loads are issued together
-  __shared__ f32x4 part[WAVES][TB][64];
+template <int XT, int WAVES> __global__ __launch_bounds__(64 * WAVES, 4) void f8_few_kernel(const F8FewParams P) {
+  constexpr int SIZE = XTraits<XT>::SIZE, U = 2;        // steps whose weights are under way together (four: more registers than two workgroups on a CU allow, 10.9 for 10.1 us at 4096 -> 8192)
+  __shared__ f32x4 part[WAVES][64];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
   const int64_t n0 = (int64_t)blockIdx.x * 16;
   const int64_t row = n0 + r16 < P.m ? n0 + r16 : P.m - 1;
   const uint8_t *const w = P.codes + row * P.ldq + 32 * kq, *const powers = P.powers + (n0 >> 7) * P.ldp;
-  const char *x[TB];
+  const char *const x = P.X + (r16 < P.tokens ? r16 : P.tokens - 1) * P.ldx * SIZE;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  u32x4 b[U][2], y[U][2];
+  unsigned pb[U], power[U];
+  Raw8<XT> a[2][4];
+  auto load_tokens = [&](int set, int s) RSVD_INLINE {
+    const int64_t k = 128 * (int64_t)s + 32 * kq, left = s < P.steps ? P.n - k : 0;      // (behind the last step: none, zeros)
 #pragma unroll
-  for (int i = 0; i < TB; ++i) {
-    const int64_t t = 16 * i + r16;
-    x[i] = P.X + (t < P.tokens ? t : P.tokens - 1) * P.ldx * SIZE;
-  }
-  f32x4 acc[TB];
-#pragma unroll
-  for (int i = 0; i < TB; ++i) acc[i] = (f32x4)0.f;
-  u32x4 b[U][2];
-  unsigned pb[U];
-  Raw8<XT> a[U][TB][4];
+    for (int q = 0; q < 4; ++q) a[set][q] = raw_load8<XT>(x + (k + 8 * q) * SIZE, left - 8 * q);
+  };
   for (int s0 = wave; s0 < P.steps; s0 += WAVES * U) {
+    load_tokens(0, s0);
+    load_tokens(1, s0 + WAVES);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int s = s0 + WAVES * u < P.steps ? s0 + WAVES * u : s0;      // (behind the last step: the first one again, its tokens zeros)
+      const int s = s0 + WAVES * u < P.steps ? s0 + WAVES * u : s0;      // (behind the last step: the first one again, unused)
       pb[u] = powers[s];
 #pragma unroll
       for (int h = 0; h < 2; ++h) b[u][h] = *reinterpret_cast<const u32x4 *>(w + (int64_t)128 * s + 16 * h);
     }
+    // tokens, out of a cache, are rounded while weights come
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t k = 128 * (int64_t)(s0 + WAVES * u) + 32 * kq;
-      const int64_t left = s0 + WAVES * u < P.steps ? P.n - k : 0;
+      float v[4][8];
+      unsigned top = 0u;
 #pragma unroll
-      for (int i = 0; i < TB; ++i)
+      for (int q = 0; q < 4; ++q) {
+        x_values<XT>(a[u & 1][q], v[q]);
+        top = f8_top8(v[q], top);
+      }
+      if (u + 2 < U) load_tokens(u & 1, s0 + WAVES * (u + 2));
+      top = f8_shared(f8_shared(top, 16), 32);
+      power[u] = f8_power(top);
+      const float by = f8_factor(power[u]);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) a[u][i][q] = raw_load8<XT>(x[i] + (k + 8 * q) * SIZE, left - 8 * q);
+      for (int h = 0; h < 2; ++h) {
+        const u32x2 c = f8_codes8(v[2 * h], by), d = f8_codes8(v[2 * h + 1], by);
+        y[u][h] = u32x4{c[0], c[1], d[0], d[1]};
+      }
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       if (s0 + WAVES * u >= P.steps) break;
-#pragma unroll
-      for (int i = 0; i < TB; ++i) {
-        float v[4][8];
-        unsigned top = 0u;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          x_values<XT>(a[u][i][q], v[q]);
-          top = f8_top8(v[q], top);
-        }
-        top = f8_shared(f8_shared(top, 16), 32);
-        const unsigned power = f8_power(top);
-        const float by = f8_factor(power);
-        u32x4 y[2];
+      if constexpr (XT == RSVD_X_F32) {
+        const float ub = f8_unit(pb[u]), ua = f8_unit(power[u]);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const u32x2 c = f8_codes8(v[2 * h], by), d = f8_codes8(v[2 * h + 1], by);
-          y[h] = u32x4{c[0], c[1], d[0], d[1]};
-        }
-        if constexpr (XT == RSVD_X_F32) {
-          const float ub = f8_unit(pb[u]), ua = f8_unit(power);
+          u32x4 bw[2], aw[2];
+          f8_widen(b[u][h], ub, bw);
+          f8_widen(y[u][h], ua, aw);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            u32x4 bw[2], aw[2];
-            f8_widen(b[u][h], ub, bw);
-            f8_widen(y[h], ua, aw);
-#pragma unroll
-            for (int z = 0; z < 2; ++z) acc[i] = mfma_bf16(bw[z], aw[z], acc[i]);
-          }
-        } else {
-          acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_both(b[u]), f8_both(y), acc[i], 0, 0, 0, (int)pb[u], 0, (int)power);
+          for (int z = 0; z < 2; ++z) acc = mfma_bf16(bw[z], aw[z], acc);
         }
+      } else {
+        acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_both(b[u]), f8_both(y[u]), acc, 0, 0, 0, (int)pb[u], 0, (int)power[u]);
       }
     }
   }
-#pragma unroll
-  for (int i = 0; i < TB; ++i) part[wave][i][lane] = acc[i];
+  part[wave][lane] = acc;
   __syncthreads();
-  if (wave >= TB) return;
-  f32x4 y = (f32x4)0.f;
+  if (wave > 0) return;
+  acc = part[0][lane];
 #pragma unroll
-  for (int v = 0; v < WAVES; ++v) y += part[v][wave][lane];
-  const int64_t t = 16 * wave + r16, n = n0 + 4 * kq;
-  if (t < P.tokens && n < P.m) put4<XT>(P.Y, t * P.ldy + n, left_of(n, P.m), y);
+  for (int v = 1; v < WAVES; ++v) acc += part[v][lane];
+  const int64_t n = n0 + 4 * kq;
+  if (r16 < P.tokens && n < P.m) put4<XT>(P.Y, r16 * P.ldy + n, left_of(n, P.m), acc);
 }
 
-template <int XT> static void f8_few_run(hipStream_t s, const F8FewParams &P, dim3 grid, bool wide) {
-#define FEW(TB)                                                                     \
-  if (wide) hipLaunchKernelGGL((f8_few_kernel<XT, TB, 8>), grid, dim3(512), 0, s, P); \
-  else hipLaunchKernelGGL((f8_few_kernel<XT, TB, 4>), grid, dim3(256), 0, s, P)
-  if (P.tokens <= 16) { FEW(1); }
-  else if (P.tokens <= 32) { FEW(2); }
-  else { FEW(4); }
-#undef FEW
+template <int XT> static void f8_few_run(hipStream_t s, const F8FewParams &P, dim3 grid) {
+  // (16 wavefronts: 4096 -> 8192 one token of bf16 10.1 us, 8: 11.3; 16384 -> 4096 18.4 and 21.0)
+  if (P.steps > 16) hipLaunchKernelGGL((f8_few_kernel<XT, 16>), grid, dim3(1024), 0, s, P);
+  else if (P.steps > 8) hipLaunchKernelGGL((f8_few_kernel<XT, 8>), grid, dim3(512), 0, s, P);
+  else hipLaunchKernelGGL((f8_few_kernel<XT, 4>), grid, dim3(256), 0, s, P);
 }
 
 hipError_t f8_few_launch(rsvd_ctx *, hipStream_t s, const F8FewDesc &d) {
   if (d.tokens < 1 || d.tokens > kF8Few) return hipErrorInvalidValue;
   const F8FewParams P = {(const char *)d.X, d.ldx, d.tokens, d.n, d.m, d.codes, d.powers, d.ldq, d.ldp, (int)ceil_div(d.n, 128), d.Y, d.ldy};
   const dim3 grid((unsigned)ceil_div(d.m, 16));
-  const bool wide = P.steps > 8;
-  if (d.type == RSVD_X_BF16) f8_few_run<RSVD_X_BF16>(s, P, grid, wide);
-  else if (d.type == RSVD_X_F16) f8_few_run<RSVD_X_F16>(s, P, grid, wide);
-  else f8_few_run<RSVD_X_F32>(s, P, grid, wide);
+  if (d.type == RSVD_X_BF16) f8_few_run<RSVD_X_BF16>(s, P, grid);
+  else if (d.type == RSVD_X_F16) f8_few_run<RSVD_X_F16>(s, P, grid);
+  else f8_few_run<RSVD_X_F32>(s, P, grid);
   return hipGetLastError();
 }
 

@@ -92,12 +92,12 @@ template <int XT> static void gated_few_run(hipStream_t s, const GatedFewParams 
   else hipLaunchKernelGGL((gated_few_kernel<XT, TB, 4>), grid, dim3(256), 0, s, P)
   if (P.tokens <= 16) { FEW(1); }
   else if (P.tokens <= 32) { FEW(2); }
-  else { FEW(4); }
+  else if constexpr (XT == RSVD_X_F32) { FEW(4); }
 #undef FEW
 }
 
 hipError_t gated_few_launch(rsvd_ctx *, hipStream_t s, const GatedFewDesc &d) {
-  if (d.tokens < 1 || d.tokens > kGatedFew) return hipErrorInvalidValue;
+  if (d.tokens < 1 || d.tokens > gated_few(d.type)) return hipErrorInvalidValue;
   const GatedFewParams P = {(const char *)d.X, (const char *)d.W, d.ldx, d.ldw, d.tokens, d.n, d.m, (int)ceil_div(d.n, 32), d.out};
   const dim3 grid((unsigned)ceil_div(d.m, 16));
   const bool wide = P.steps > 32;

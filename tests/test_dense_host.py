@@ -43,7 +43,7 @@ def test_gated_product_checks_every_argument(plan):
     assert call(n=0) == -6 and call(m=0) == -7 and call(X=NULL) == -8 and call(X=ODD) == -8 and call(type=X_F32, X=HALF) == -8
     assert call(ldx=71) == -9 and call(W=NULL) == -10 and call(W=ODD) == -10 and call(ldw=71) == -11 and call(H=NULL) == -12 and call(ldh=49) == -13
     assert call(kept=ODD) == -14 and call(ldk=99) == -15 and call(kept=NULL, ldk=0) == ERR_NO_DEVICE
-    assert call(ws=NULL, bytes=0, tokens=64) == ERR_NO_DEVICE
+    assert call(ws=NULL, bytes=0, tokens=16) == ERR_NO_DEVICE
     # a matrix that does not lie as the products read it needs room
     both, neither = (bytes_of(plan, "rsvd_gated_product_bytes", X_BF16, 100, 72, 50, lie) for lie in (3, 0))
     assert neither >= both + 2 * 72 * (100 + 100)
@@ -56,8 +56,9 @@ def test_gated_product_checks_every_argument(plan):
 
 
 def test_the_binding_knows_how_many_tokens_need_no_workspace(plan):
-    for few, name, more in ((binding.GATED_FEW, "rsvd_gated_product_bytes", (0,)), (binding.F8_FEW, "rsvd_f8_product_bytes", ()), (binding.F8_FEW, "rsvd_f8_product_grad_bytes", ())):
-        assert bytes_of(plan, name, X_BF16, few, 100, 200, *more) == 0 and bytes_of(plan, name, X_BF16, few + 1, 100, 200, *more) > 0
+    for xt in (X_BF16, X_F16, X_F32):
+        for few, name, more in ((binding.GATED_FEW[xt], "rsvd_gated_product_bytes", (0,)), (binding.F8_FEW, "rsvd_f8_product_bytes", ()), (binding.F8_FEW, "rsvd_f8_product_grad_bytes", ())):
+            assert bytes_of(plan, name, xt, few, 100, 200, *more) == 0 and bytes_of(plan, name, xt, few + 1, 100, 200, *more) > 0
 
 
 def test_gated_gradient_checks_every_argument(plan):
@@ -96,7 +97,7 @@ def test_f8_checks_every_argument(plan):
         assert call(p=ODD) == -11 and call(ldp=1) == -12 and call(ldp=5) == -12 and call(Y=NULL) == -13 and call(ldy=49) == -14
         need = bytes_of(plan, name + "_bytes", X_BF16, 100, n, m)
         assert need > 0 and call(ws=NULL) == -15 and call(bytes=need - 1) == -16 and call(bytes=need) == ERR_NO_DEVICE
-        assert bytes_of(plan, name + "_bytes", X_BF16, 64, n, m) == 0 and call(tokens=64, ws=NULL, bytes=0) == ERR_NO_DEVICE
+        assert bytes_of(plan, name + "_bytes", X_BF16, 16, n, m) == 0 and call(tokens=16, ws=NULL, bytes=0) == ERR_NO_DEVICE
         assert call(ldq=(1 << 23) + 16) == UNSUPPORTED
     call = caller(plan, "rsvd_f8_weight_grad", "ctx stream type tokens n m dY lddy X ldx dW lddw f32 acc ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, tokens=100,
                   n=70, m=50, dY=PTR, lddy=50, X=PTR, ldx=70, dW=PTR, lddw=70, f32=0, acc=0, ws=PTR, bytes=1 << 40)

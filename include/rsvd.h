@@ -380,7 +380,9 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
  * in the others:  H = act(X Wg^T) * (X Wu^T), element by element, in one kernel.
  * X, W, H and gradients have one type (bf16, fp16, fp32); products of fp32 numbers
  * are taken as six products of bf16 numbers (2^-24 of the largest left out).
- * Sums are held in 32 bits.  tokens, n, m as for the layers above (tokens may be 0);
+ * Sums are held in 32 bits; results that an infinity among fp32 numbers enters (more than
+ * 3.39e38) are infinite or NaN.  Of these and the products below no result may lie on an operand
+ * or another result (columns beside it in one wider matrix may).  tokens, n, m as for the layers above (tokens may be 0);
  * matrices may have any leading dimension and the alignment of their elements.  A
  * matrix lies as the products read it if it is 16-bit, n is a multiple of 8, its rows
  * start at 16-byte aligned addresses and its leading dimension is at most 2^22;
@@ -420,7 +422,7 @@ int rsvd_gated_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_a
  *   - codes: rows of ldq bytes, ldq a multiple of 16 and at least n up to a multiple of 128, from a
  *     16-byte aligned address; the codes from n on to that multiple are zeros.
  *   - powers: a row for each 128 rows of codes, a byte for each 128 columns, ldp bytes apart, ldp a multiple
- *     of 4, from a 4-byte aligned address; all bytes to the next multiple of 4 may be read.  Values 1 to 254, or 255.
+ *     of 4 (at most 2^20 for the products), from a 4-byte aligned address; all bytes to the next multiple of 4 may be read.  Values 1 to 254, or 255.
  *   - Tokens are rounded on the way, in blocks of 128 of a token (of 128 tokens for the gradient of a
  *     weight); the rounding is passed straight through.
  *   - fp32 results are sums of exact products in fp32.  For 16-bit results the matrix instruction for
@@ -455,10 +457,10 @@ int rsvd_f8_weight_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t to
  * zeros), then for each step  X <- a X + (b A + c A^2) X,  A = X X^T (X^T X where m > n),
  * with the step's three coefficients (host, a, b, c of the first step, of the second, ..).  Singular vectors stay as they are,
  * every singular value goes through the odd polynomials: about one with those of Newton-Schulz iterations, so that the
- * result is near U V^T.  bf16 results come from iterates in fp16, others from iterates in two fp16 numbers (22 bits); sums are
- * held in 32 bits.  An infinity or NaN makes the whole matrix NaN.
+ * result is near U V^T.  Iterates are two fp16 numbers (22 bits); products of bf16 matrices take the first of them, others both.  Diagonals
+ * of A and of b A + c A^2, and sums, are held in 32 bits.  An infinity or NaN makes the whole matrix NaN.
  * Coefficients that take a singular value out of [-2.7, 2.7], or b x^2 + c x^4 out of [-7.5, 7.5], are turned away
- * (RSVD_ERR_UNSUPPORTED), 1 to 64 steps.  O may be G. */
+ * (RSVD_ERR_UNSUPPORTED), 1 to 64 steps.  Of a batch, tiles of 256 x 256 are fewer than 2^22.  O may be G, or lie on it. */
 int rsvd_orthogonalize_bytes(rsvd_ctx *ctx, rsvd_xtype type, int batch, int64_t m, int64_t n, size_t *bytes);
 int rsvd_orthogonalize(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int batch, int64_t m, int64_t n, const void *G, int64_t ldg, int64_t stride_g,
                        int steps, const float *coefficients, void *O, int64_t ldo, int64_t stride_o, void *workspace, size_t workspace_bytes);

@@ -41,7 +41,7 @@ static DenseChoice dense_choose(const rsvd_ctx *ctx, const DenseDesc &d) {
       const int64_t per = ceil_div(kt, r), used = ceil_div(kt, per);
       if (r > 1 && used < 2) continue;
       const int64_t whole = used > 1 ? tiles / full * full : tiles, rest = tiles - whole;
-      if (used > 1 && rest == 0) continue;
+      if ((used > 1 && rest == 0) || whole + rest * used >= kDenseGroups) continue;
       double us = time(whole, kt) + time(rest * used, per);
       if (used > 1) us += 4.0 + (double)used * (double)rest * t.b * t.b * 8.0 / 5e6;
       if (us < least) {
@@ -91,7 +91,7 @@ static bool fits(const DenseChoice &c, const DenseDesc &d) {
   if (c.splits > 1 && (d.partial == nullptr || d.partial_bytes < partial_bytes(c))) return false;
   if (d.symmetric && (d.M != d.N || d.gated)) return false;
   const auto pieces = [](const void *p, int64_t ld) { return p != nullptr && ((uintptr_t)p & 15) == 0 && ld % 16 == 0 && ld <= kMaxLd; };
-  return pieces(d.A, d.lda) && pieces(d.B, d.ldb) && c.whole + c.rest * c.splits < (1 << 22);
+  return pieces(d.A, d.lda) && pieces(d.B, d.ldb) && c.b != 0 && c.whole + c.rest * c.splits < kDenseGroups;
 }
 
 hipError_t dense_nt_launch(rsvd_ctx *ctx, hipStream_t s, const DenseDesc &d) {

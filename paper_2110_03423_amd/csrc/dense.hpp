@@ -62,6 +62,8 @@ struct DenseDesc {
   GatedOut gate;
   float *partial = nullptr; size_t partial_bytes = 0;
 };
+// Workgroups of a launch: fewer than this (a grid has fewer than 2^32 threads).  Tiles of 256 have to be fewer; others are taken where they are.
+constexpr int64_t kDenseGroups = (int64_t)1 << 22;
 size_t dense_partial_bytes(const rsvd_ctx *ctx, const DenseDesc &d);
 
 // Both operands with consecutive k (M rows, N or 2 N rows), rows of whole 16-byte pieces from 16-byte aligned addresses.  (8-bit floats: rows of whole k-tiles of 128,

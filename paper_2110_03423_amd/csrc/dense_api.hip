@@ -31,6 +31,45 @@ struct Take {
   size_t operator()(size_t bytes) { const size_t o = off; off = align_up(off + bytes, 256); return o; }
 };
 
+// A matrix in memory: rows of `width` bytes, `step` bytes apart (p = NULL: none).
+struct Span { const void *p; int64_t rows, width, step; };
+Span span(const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t size) { return {p, rows, cols * size, ld * size}; }
+// Whether two have a byte in common; columns of one wider matrix have none.
+bool overlap(const Span &a, const Span &b) {
+  if (a.p == nullptr || b.p == nullptr || a.rows < 1 || b.rows < 1) return false;
+  const uintptr_t at = (uintptr_t)a.p, bt = (uintptr_t)b.p;
+  const uintptr_t a_end = at + (uintptr_t)((a.rows - 1) * a.step + a.width), b_end = bt + (uintptr_t)((b.rows - 1) * b.step + b.width);
+  if (a_end <= bt || b_end <= at) return false;
+  if (a.step != b.step || a.rows == 1 || b.rows == 1) return true;
+  const int64_t step = a.step, d = at <= bt ? (int64_t)((bt - at) % (uintptr_t)step) : (step - (int64_t)((at - bt) % (uintptr_t)step)) % step;
+  return !(d >= a.width && d + b.width <= step);
+}
+template <int N> bool overlap(const Span &a, const Span (&others)[N]) {
+  for (const Span &b : others)
+    if (overlap(a, b)) return true;
+  return false;
+}
+
+// The context's device while a call launches: the null stream is the current device's.
+struct OnDevice {
+  int back = -1;
+  hipError_t error;
+  explicit OnDevice(const rsvd_ctx *ctx) {
+    int now = -1;
+    error = hipGetDevice(&now);
+    if (error != hipSuccess || now == ctx->device) return;
+    error = hipSetDevice(ctx->device);
+    if (error == hipSuccess) back = now;
+  }
+  ~OnDevice() {
+    if (back >= 0) (void)hipSetDevice(back);
+  }
+};
+#define RSVD_ON_DEVICE()                                        \
+  if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;               \
+  const OnDevice on(ctx);                                       \
+  RSVD_TRY(on.error, "the context's device")
+
 // Whether a matrix of n columns can be an operand as it lies.
 bool laid_out(rsvd_xtype type, int64_t n, const void *p, int64_t ld) {
   return type != RSVD_X_F32 && n % 8 == 0 && rows_aligned(p, ld, 2) && ld <= kMaxLd / 2;
@@ -99,6 +138,8 @@ GatedLayout gated_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, i
 // ---- 8-bit floats
 int64_t f8_width(int64_t n) { return (int64_t)align_up((size_t)n, 128); }
 int64_t f8_powers(int64_t n) { return (int64_t)align_up((size_t)ceil_div(n, 128), 4); }
+// (1024 rows of powers within the 31 bits that loads count bytes in)
+constexpr int64_t kMaxPowersLd = (int64_t)1 << 20;
 bool valid_codes8(const void *p) { return p != nullptr && ((uintptr_t)p & 15) == 0; }
 bool valid_powers(const void *p) { return p != nullptr && ((uintptr_t)p & 3) == 0; }
 
@@ -147,11 +188,12 @@ int f8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int
   if (ldp < f8_powers(n) || ldp % 4 != 0) return -12;
   if (!valid(Y, es)) return -13;
   if (ldy < m) return -14;
-  if (!sizes_supported(tokens, n, m) || ldq > kMaxLd) return RSVD_ERR_UNSUPPORTED;
+  if (!sizes_supported(tokens, n, m) || ldq > kMaxLd || ldp > kMaxPowersLd) return RSVD_ERR_UNSUPPORTED;
+  if (overlap(span(Y, tokens, m, ldy, es), {span(X, tokens, n, ldx, es), span(codes, m, f8_width(n), ldq, 1)})) return -13;
   const F8Layout L = f8_product_layout(ctx, type, tokens, n, m);
   if (L.total > 0 && (workspace == nullptr || ((uintptr_t)workspace & 255) != 0)) return -15;
   if (workspace_bytes < L.total) return -16;
-  if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
+  RSVD_ON_DEVICE();
   hipStream_t s = (hipStream_t)stream;
   if (tokens <= kF8Few) {
     const F8FewDesc d = {type, tokens, n, m, X, ldx, codes, ldq, powers, ldp, Y, ldy};
@@ -278,11 +320,14 @@ int rsvd_gated_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_act ac
   if (!element_aligned(kept, es)) return -14;
   if (kept != nullptr && ldk < 2 * m) return -15;
   if (!sizes_supported(tokens, n, m)) return RSVD_ERR_UNSUPPORTED;
+  const Span x_span = span(X, tokens, n, ldx, es), w_span = span(W, 2 * m, n, ldw, es), h_span = span(H, tokens, m, ldh, es);
+  if (overlap(h_span, {x_span, w_span})) return -12;
+  if (overlap(span(kept, tokens, 2 * m, ldk, es), {x_span, w_span, h_span})) return -14;
   const bool few = tokens <= gated_few(type), x_lies = laid_out(type, n, X, ldx), w_lies = laid_out(type, n, W, ldw);
   const GatedLayout L = few ? GatedLayout{} : gated_layout(ctx, type, tokens, n, m, x_lies, w_lies, false, false);
   if (L.total > 0 && (workspace == nullptr || ((uintptr_t)workspace & 255) != 0)) return -16;
   if (workspace_bytes < L.total) return -17;
-  if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
+  RSVD_ON_DEVICE();
   hipStream_t s = (hipStream_t)stream;
   GatedOut o;
   o.act = act; o.type = type;
@@ -355,16 +400,20 @@ int rsvd_gated_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_a
   if (!sizes_supported(tokens, n, m)) return RSVD_ERR_UNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   if (tokens == 0) {
-    if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
+    RSVD_ON_DEVICE();
     if (dW != nullptr && !accumulate) RSVD_TRY(zero_launch(s, wtype, 2 * m, n, dW, lddw), "zeros");
     return RSVD_OK;
   }
+  const Span inputs[4] = {span(dH, tokens, m, lddh, es), span(X, tokens, n, ldx, es), span(W, 2 * m, n, ldw, es), span(kept, tokens, 2 * m, ldk, es)};
+  const Span dx_span = span(dX, tokens, n, lddx, es), dw_span = span(dW, 2 * m, n, lddw, xtype_size(wtype));
+  if (overlap(dx_span, inputs)) return -16;
+  if (overlap(dw_span, inputs) || overlap(dw_span, dx_span)) return -18;
   const bool x_needed = recompute || dW != nullptr, w_needed = recompute || dX != nullptr;
   const bool x_lies = !x_needed || laid_out(type, n, X, ldx), w_lies = !w_needed || laid_out(type, n, W, ldw);
   const GatedLayout L = gated_layout(ctx, type, tokens, n, m, x_lies, w_lies, true, !recompute);
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0) return -22;
   if (workspace_bytes < L.total) return -23;
-  if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
+  RSVD_ON_DEVICE();
   if (dX == nullptr && dW == nullptr) return RSVD_OK;
   char *ws = (char *)workspace;
   const int64_t width = width_of(n);
@@ -429,7 +478,10 @@ int rsvd_f8_weight(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t m, int6
   if (codes_t != nullptr && !valid_powers(powers_t)) return -14;
   if (codes_t != nullptr && (ldpt < f8_powers(m) || ldpt % 4 != 0)) return -15;
   if (!sizes_supported(1, n, m)) return RSVD_ERR_UNSUPPORTED;
-  if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
+  const Span w_span = span(W, m, n, ldw, xtype_size(type)), q_span = span(codes, m, f8_width(n), ldq, 1);
+  if (overlap(q_span, w_span)) return -8;
+  if (overlap(span(codes_t, n, f8_width(m), ldqt, 1), {w_span, q_span})) return -12;
+  RSVD_ON_DEVICE();
   ProfScope ps(ctx, (hipStream_t)stream, PK_SMALL);
   RSVD_TRY(f8_weight_launch((hipStream_t)stream, type, m, n, W, ldw, codes, ldq, powers, ldp, codes_t, ldqt, codes_t != nullptr ? powers_t : nullptr, ldpt),
            "weight to 8-bit floats");
@@ -497,14 +549,15 @@ int rsvd_f8_weight_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t to
   if (!sizes_supported(tokens, n, m)) return RSVD_ERR_UNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   if (tokens == 0) {
-    if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
+    RSVD_ON_DEVICE();
     if (!accumulate) RSVD_TRY(zero_launch(s, wtype, m, n, dW, lddw), "zeros");
     return RSVD_OK;
   }
+  if (overlap(span(dW, m, n, lddw, xtype_size(wtype)), {span(dY, tokens, m, lddy, es), span(X, tokens, n, ldx, es)})) return -11;
   const F8Layout L = f8_weight_grad_layout(ctx, wtype == RSVD_X_F32, tokens, n, m);
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0) return -15;
   if (workspace_bytes < L.total) return -16;
-  if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
+  RSVD_ON_DEVICE();
   char *ws = (char *)workspace;
   uint8_t *a = (uint8_t *)(ws + L.a), *a_pow = (uint8_t *)(ws + L.a_pow), *b = (uint8_t *)(ws + L.b), *b_pow = (uint8_t *)(ws + L.b_pow);
   const int64_t width = f8_width(tokens), ldp = f8_powers(tokens);
@@ -530,7 +583,8 @@ static int check_matrices(rsvd_xtype type, int batch, int64_t m, int64_t n, int 
   return 0;
 }
 static bool matrices_supported(int batch, int64_t m, int64_t n) {
-  return batch <= 65535 && m <= RSVD_Q8_MAX_FEATURES && n <= RSVD_Q8_MAX_FEATURES && (int64_t)batch * m * n <= (int64_t)1 << 34;
+  return batch <= 65535 && m <= RSVD_Q8_MAX_FEATURES && n <= RSVD_Q8_MAX_FEATURES && (int64_t)batch * m * n <= (int64_t)1 << 34 &&
+         batch * ceil_div(m, 256) * ceil_div(n, 256) < kDenseGroups;
 }
 
 int rsvd_orthogonalize_bytes(rsvd_ctx *ctx, rsvd_xtype type, int batch, int64_t m, int64_t n, size_t *bytes) {
@@ -561,7 +615,7 @@ int rsvd_orthogonalize(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int batch, 
   const OrthogonalLayout L = orthogonal_layout(ctx, type, batch, m, n);
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0) return -15;
   if (workspace_bytes < L.total) return -16;
-  if (ctx->device < 0) return RSVD_ERR_NO_DEVICE;
+  RSVD_ON_DEVICE();
   hipStream_t s = (hipStream_t)stream;
   char *ws = (char *)workspace;
   const int planes = iterate_planes(type);

@@ -355,7 +355,7 @@ template <int ACT> __device__ __forceinline__ float act_slope(float g, float &va
     value = g * s;
     if constexpr (ACT == GATED_SILU) return s + value * (1.f - s);
     else if constexpr (ACT == GATED_GELU) return s + g * __expf(-0.5f * g * g) * 0.39894228f;
-    else return s + value * (1.f - s) * 1.5957691f * (1.f + 0.134145f * g * g);
+    else return s + value * (1.f - s) * 1.5957691f * (1.f + 0.134145f * fminf(g * g, 1e30f));      // (0, not 0 times infinity, where the share is 0 or 1)
   }
 }
 // Gradients of gate and up, V times four columns from n on, to the planes of D (gate from column 0 on, up from column N on, zeros behind both).

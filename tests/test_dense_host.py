@@ -13,6 +13,7 @@ PTR = C.c_void_p(1 << 20)
 ODD = C.c_void_p((1 << 20) + 1)
 HALF = C.c_void_p((1 << 20) + 2)
 NULL = C.c_void_p(0)
+OUT, OUT2 = C.c_void_p(1 << 44), C.c_void_p(1 << 45)
 
 
 @pytest.fixture(scope="module")
@@ -37,7 +38,7 @@ def bytes_of(plan, name, *args):
 
 def test_gated_product_checks_every_argument(plan):
     call = caller(plan, "rsvd_gated_product", "ctx stream type act tokens n m X ldx W ldw H ldh kept ldk ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, act=0,
-                  tokens=100, n=72, m=50, X=PTR, ldx=72, W=PTR, ldw=72, H=PTR, ldh=50, kept=PTR, ldk=100, ws=PTR, bytes=1 << 40)
+                  tokens=100, n=72, m=50, X=PTR, ldx=72, W=PTR, ldw=72, H=OUT, ldh=50, kept=OUT2, ldk=100, ws=PTR, bytes=1 << 40)
     assert call() == ERR_NO_DEVICE and call(tokens=0, X=NULL) == 0
     assert call(ctx=None) == -1 and call(type=3) == -3 and call(act=4) == -4 and call(act=-1) == -4 and call(tokens=-1) == -5
     assert call(n=0) == -6 and call(m=0) == -7 and call(X=NULL) == -8 and call(X=ODD) == -8 and call(type=X_F32, X=HALF) == -8
@@ -63,7 +64,7 @@ def test_the_binding_knows_how_many_tokens_need_no_workspace(plan):
 
 def test_gated_gradient_checks_every_argument(plan):
     call = caller(plan, "rsvd_gated_product_grad", "ctx stream type act tokens n m dH lddh X ldx W ldw kept ldk dX lddx dW lddw f32 acc ws bytes", ctx=plan.h, stream=NULL,
-                  type=X_F16, act=1, tokens=100, n=72, m=50, dH=PTR, lddh=50, X=PTR, ldx=72, W=PTR, ldw=72, kept=PTR, ldk=100, dX=PTR, lddx=72, dW=PTR, lddw=72,
+                  type=X_F16, act=1, tokens=100, n=72, m=50, dH=PTR, lddh=50, X=PTR, ldx=72, W=PTR, ldw=72, kept=PTR, ldk=100, dX=OUT, lddx=72, dW=OUT2, lddw=72,
                   f32=0, acc=0, ws=PTR, bytes=1 << 40)
     assert call() == ERR_NO_DEVICE
     assert call(ctx=None) == -1 and call(type=7) == -3 and call(act=9) == -4 and call(tokens=-1) == -5 and call(n=0) == -6 and call(m=0) == -7
@@ -83,14 +84,14 @@ def test_gated_gradient_checks_every_argument(plan):
 
 def test_f8_checks_every_argument(plan):
     call = caller(plan, "rsvd_f8_weight", "ctx stream type m n W ldw q ldq p ldp qt ldqt pt ldpt", ctx=plan.h, stream=NULL, type=X_F32, m=130, n=70, W=PTR, ldw=70,
-                  q=PTR, ldq=128, p=PTR, ldp=4, qt=PTR, ldqt=256, pt=PTR, ldpt=4)
+                  q=OUT, ldq=128, p=PTR, ldp=4, qt=OUT2, ldqt=256, pt=PTR, ldpt=4)
     assert call() == ERR_NO_DEVICE and call(qt=NULL, pt=NULL, ldqt=0, ldpt=0) == ERR_NO_DEVICE
     assert call(ctx=None) == -1 and call(type=3) == -3 and call(m=0) == -4 and call(n=0) == -5 and call(W=HALF) == -6 and call(ldw=69) == -7
     assert call(q=HALF) == -8 and call(ldq=112) == -9 and call(ldq=130) == -9 and call(p=HALF) == -10 and call(ldp=1) == -11 and call(ldp=6) == -11
     assert call(qt=HALF) == -12 and call(ldqt=128) == -13 and call(pt=NULL) == -14 and call(ldpt=2) == -15
     for name, n, m in (("rsvd_f8_product", 200, 50), ("rsvd_f8_product_grad", 50, 200)):
         call = caller(plan, name, "ctx stream type tokens n m X ldx q ldq p ldp Y ldy ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, tokens=100, n=n, m=m, X=PTR,
-                      ldx=200, q=PTR, ldq=256, p=PTR, ldp=4, Y=PTR, ldy=50, ws=PTR, bytes=1 << 40)
+                      ldx=200, q=PTR, ldq=256, p=PTR, ldp=4, Y=OUT, ldy=50, ws=PTR, bytes=1 << 40)
         assert call() == ERR_NO_DEVICE and call(tokens=0, X=NULL) == 0
         assert call(ctx=None) == -1 and call(type=5) == -3 and call(tokens=-2) == -4 and call(n=0) == -5 and call(m=0) == -6
         assert call(X=ODD) == -7 and call(ldx=199) == -8 and call(q=HALF) == -9 and call(ldq=240) == -10 and call(ldq=264) == -10
@@ -98,15 +99,52 @@ def test_f8_checks_every_argument(plan):
         need = bytes_of(plan, name + "_bytes", X_BF16, 100, n, m)
         assert need > 0 and call(ws=NULL) == -15 and call(bytes=need - 1) == -16 and call(bytes=need) == ERR_NO_DEVICE
         assert bytes_of(plan, name + "_bytes", X_BF16, 16, n, m) == 0 and call(tokens=16, ws=NULL, bytes=0) == ERR_NO_DEVICE
-        assert call(ldq=(1 << 23) + 16) == UNSUPPORTED
+        assert call(ldq=(1 << 23) + 16) == UNSUPPORTED and call(ldp=(1 << 20) + 4) == UNSUPPORTED and call(ldp=1 << 20) == ERR_NO_DEVICE
     call = caller(plan, "rsvd_f8_weight_grad", "ctx stream type tokens n m dY lddy X ldx dW lddw f32 acc ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, tokens=100,
-                  n=70, m=50, dY=PTR, lddy=50, X=PTR, ldx=70, dW=PTR, lddw=70, f32=0, acc=0, ws=PTR, bytes=1 << 40)
+                  n=70, m=50, dY=PTR, lddy=50, X=PTR, ldx=70, dW=OUT, lddw=70, f32=0, acc=0, ws=PTR, bytes=1 << 40)
     assert call() == ERR_NO_DEVICE and call(tokens=0, dY=NULL, X=NULL) == ERR_NO_DEVICE
     assert call(type=3) == -3 and call(tokens=-1) == -4 and call(n=0) == -5 and call(m=0) == -6 and call(dY=NULL) == -7 and call(lddy=49) == -8
     assert call(X=NULL) == -9 and call(ldx=69) == -10 and call(dW=NULL) == -11 and call(f32=1, dW=HALF) == -11 and call(lddw=69) == -12
     assert call(acc=1) == -14 and call(acc=1, f32=1) == ERR_NO_DEVICE and call(ws=NULL) == -15
     need = bytes_of(plan, "rsvd_f8_weight_grad_bytes", X_BF16, 100, 70, 50, 0)
     assert call(bytes=need) == ERR_NO_DEVICE and call(bytes=need - 1) == -16
+
+
+def at(p):
+    return C.c_void_p(p)
+
+
+def test_results_may_not_lie_on_operands(plan):
+    x = 1 << 30
+    call = caller(plan, "rsvd_gated_product", "ctx stream type act tokens n m X ldx W ldw H ldh kept ldk ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, act=0,
+                  tokens=100, n=50, m=50, X=at(x), ldx=50, W=at(2 * x), ldw=50, H=OUT, ldh=50, kept=OUT2, ldk=100, ws=PTR, bytes=1 << 40)
+    assert call() == ERR_NO_DEVICE and call(H=at(x)) == -12 and call(kept=at(2 * x)) == -14 and call(kept=OUT) == -14
+    # one byte, from either side
+    assert call(H=at(x + 9998)) == -12 and call(H=at(x + 10000)) == ERR_NO_DEVICE and call(H=at(x - 9998)) == -12 and call(H=at(x - 10000)) == ERR_NO_DEVICE
+    assert call(tokens=20, H=at(x)) == -12
+    # columns beside the operand's, in one wider matrix
+    wide = dict(ldx=120, ldh=120)
+    assert call(H=at(x + 100), **wide) == ERR_NO_DEVICE and call(H=at(x + 140), **wide) == ERR_NO_DEVICE and call(H=at(x + 98), **wide) == -12
+    assert call(H=at(x + 142), **wide) == -12 and call(H=at(x + 240 * 7 + 100), **wide) == ERR_NO_DEVICE and call(H=at(x - 240 * 7 - 100), **wide) == ERR_NO_DEVICE
+    assert call(H=at(x - 240 * 7 - 98), **wide) == -12 and call(H=at(x + 100), ldx=120, ldh=122) == -12
+
+    call = caller(plan, "rsvd_gated_product_grad", "ctx stream type act tokens n m dH lddh X ldx W ldw kept ldk dX lddx dW lddw f32 acc ws bytes", ctx=plan.h, stream=NULL,
+                  type=X_F16, act=1, tokens=100, n=50, m=50, dH=at(x), lddh=50, X=at(2 * x), ldx=50, W=at(3 * x), ldw=50, kept=at(4 * x), ldk=100, dX=OUT, lddx=50, dW=OUT2,
+                  lddw=50, f32=0, acc=0, ws=PTR, bytes=1 << 40)
+    assert call() == ERR_NO_DEVICE
+    for i in range(1, 5):
+        assert call(dX=at(i * x)) == -16 and call(dW=at(i * x)) == -18
+    assert call(dW=OUT) == -18 and call(dW=OUT, dX=NULL) == ERR_NO_DEVICE and call(dW=at(4 * x), kept=NULL, ldk=0) == ERR_NO_DEVICE
+
+    call = caller(plan, "rsvd_f8_weight", "ctx stream type m n W ldw q ldq p ldp qt ldqt pt ldpt", ctx=plan.h, stream=NULL, type=X_F32, m=128, n=128, W=at(x), ldw=128,
+                  q=OUT, ldq=128, p=PTR, ldp=4, qt=OUT2, ldqt=128, pt=PTR, ldpt=4)
+    assert call() == ERR_NO_DEVICE and call(q=at(x)) == -8 and call(qt=at(x)) == -12 and call(qt=OUT) == -12
+    call = caller(plan, "rsvd_f8_product", "ctx stream type tokens n m X ldx q ldq p ldp Y ldy ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, tokens=3, n=128, m=128,
+                  X=at(x), ldx=128, q=at(2 * x), ldq=128, p=PTR, ldp=4, Y=OUT, ldy=128, ws=PTR, bytes=1 << 40)
+    assert call() == ERR_NO_DEVICE and call(Y=at(x)) == -13 and call(Y=at(2 * x)) == -13
+    call = caller(plan, "rsvd_f8_weight_grad", "ctx stream type tokens n m dY lddy X ldx dW lddw f32 acc ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, tokens=100,
+                  n=70, m=50, dY=at(x), lddy=50, X=at(2 * x), ldx=70, dW=OUT, lddw=70, f32=0, acc=0, ws=PTR, bytes=1 << 40)
+    assert call() == ERR_NO_DEVICE and call(dW=at(x)) == -11 and call(dW=at(2 * x)) == -11
 
 
 def test_orthogonalize_checks_every_argument(plan):
@@ -121,6 +159,8 @@ def test_orthogonalize_checks_every_argument(plan):
     assert call(bytes=need) == ERR_NO_DEVICE and call(bytes=need - 1) == -16
     for bad in ((4.0, 0.0, 0.0), (3.4445, -4.775, 4.5), (float("nan"), 0.0, 0.0), (1.0, float("inf"), 0.0), (1.0, -9.0, 0.5)):
         assert call(steps=1, coef=(C.c_float * 3)(*bad)) == UNSUPPORTED
+    big = dict(sg=1 << 30, so=1 << 30, bytes=1 << 62)
+    assert call(batch=65535, m=16, n=16384, ldg=16384, ldo=16384, **big) == ERR_NO_DEVICE and call(batch=65535, m=1, n=131072, ldg=131072, ldo=131072, **big) == UNSUPPORTED
     assert call(batch=65536) == UNSUPPORTED and call(m=131073, so=1 << 40) == UNSUPPORTED
 
 

@@ -32,7 +32,7 @@ def act64(g, act):
         s = torch.sigmoid(g)
         return g * s, s * (1 + g * (1 - s)), s * (1 + g.abs() * (1 - s))
     if act == "gelu":
-        s, p = torch.special.ndtr(g), torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+        s, p = torch.erfc(-g / math.sqrt(2)) / 2, torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
         return g * s, s + g * p, s + g.abs() * p
     r = math.sqrt(8 / math.pi)
     s = torch.sigmoid(r * g * (1 + 0.044715 * g * g))

@@ -120,21 +120,26 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
   const char *a_now, *b_now;
   int left;
   auto point = [&]() RSVD_INLINE {
-    a_now = a_row + (PL > 1 ? 0 : (int64_t)(P.segs.a >> (4 * next_seg) & 15) * P.a_plane) + (int64_t)next_kt * 128;
-    b_now = b_row + (PL > 1 ? 0 : (int64_t)(P.segs.b >> (4 * next_seg) & 15) * P.b_plane) + (int64_t)next_kt * 128;
-    left = next_kt == P.ktiles - 1 ? last_left : 8;
+    a_now = a_row + (PL > 1 || CODES ? 0 : (int64_t)(P.segs.a >> (4 * next_seg) & 15) * P.a_plane) + (int64_t)next_kt * 128;
+    b_now = b_row + (PL > 1 || CODES ? 0 : (int64_t)(P.segs.b >> (4 * next_seg) & 15) * P.b_plane) + (int64_t)next_kt * 128;
   };
+  auto remain = [&]() RSVD_INLINE { left = CODES ? 8 : next_kt == P.ktiles - 1 ? last_left : 8; };
   auto advance = [&]() RSVD_INLINE {                    // (behind the last tile that one again, where nobody reads it: no branches around loads)
-    if (++next < nkt) {
-      if (++next_kt == P.ktiles) {
-        next_kt = 0;
-        ++next_seg;
-      }
+    const int step = ++next < nkt ? 1 : 0;
+    next_kt += step;
+    a_now += 128 * step;
+    b_now += 128 * step;
+    if (PL == 1 && !CODES && next_kt == P.ktiles) {
+      next_kt = 0;
+      ++next_seg;
+      point();
     }
-    point();
+    remain();
   };
-  auto issue = [&](int kt, int l) RSVD_INLINE {
-    char *st = dense_lds + (kt % RING) * STAGE;
+  // (where a tile lies: `place` bytes into LDS)
+  auto place = [&](int kt) RSVD_INLINE { return (kt % RING) * STAGE; };
+  auto issue = [&](int at_lds, int l) RSVD_INLINE {
+    char *st = dense_lds + at_lds;
     const int q = l / TILE_LOADS, at = l % TILE_LOADS;   // (planes: those of A and B in turn)
     if (q < PL && at < decltype(la)::N) {
       la.issue(at, a_now + q * P.a_plane, 0, st + q * (BM + BN) * 128, left, wave, tid);
@@ -153,21 +158,21 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
   // (rows of a wavefront's blocks start at multiples of 32, or of 16 where they are not shared: what pieces are exchanged by is the lane's)
   const int b_first = PAIRED ? 8 * (r16 >> 2) + (r16 & 3) : r16, a_swz = dense_swizzle<false>(r16), b_swz = dense_swizzle<PAIRED>(b_first);
   const char *const a_lds = dense_lds + (wm0 + r16) * 128, *const b_lds = dense_lds + BM * 128 + (wn0 + b_first) * 128;
-  auto piece_a = [&](int kt, int i, int h, int q = 0) RSVD_INLINE {
-    return *reinterpret_cast<const u32x4 *>(a_lds + (kt % RING) * STAGE + q * (BM + BN) * 128 + i * 2048 + (((4 * h + kq) ^ a_swz) << 4));
+  auto piece_a = [&](int at_lds, int i, int h, int q = 0) RSVD_INLINE {
+    return *reinterpret_cast<const u32x4 *>(a_lds + at_lds + q * (BM + BN) * 128 + i * 2048 + (((4 * h + kq) ^ a_swz) << 4));
   };
-  auto piece_b = [&](int kt, int j, int h, int q = 0) RSVD_INLINE {
-    return *reinterpret_cast<const u32x4 *>(b_lds + (kt % RING) * STAGE + q * (BM + BN) * 128 + (PAIRED ? j / 2 * 4096 + (j & 1) * 512 : j * 2048) + (((4 * h + kq) ^ b_swz) << 4));
+  auto piece_b = [&](int at_lds, int j, int h, int q = 0) RSVD_INLINE {
+    return *reinterpret_cast<const u32x4 *>(b_lds + at_lds + q * (BM + BN) * 128 + (PAIRED ? j / 2 * 4096 + (j & 1) * 512 : j * 2048) + (((4 * h + kq) ^ b_swz) << 4));
   };
   // powers of the rows of a lane's blocks: in words of four k-tiles, and of the one that is multiplied
   unsigned words_a[CODES ? TM : 1], words_b[CODES ? TN : 1], pa[CODES ? TM : 1], pb[CODES ? TN : 1];
   const char *const pow_lds = dense_lds + DenseNtCfg<KIND, PL, BM, BN>::POWERS;
-  auto read_powers = [&](int kt) RSVD_INLINE {
+  auto read_powers = [&](int at_lds) RSVD_INLINE {
 #pragma unroll
-    for (int i = 0; i < (CODES ? TM : 0); ++i) words_a[i] = *reinterpret_cast<const unsigned *>(pow_lds + (kt % RING) * STAGE + (wm0 + 16 * i + r16) * 4);
+    for (int i = 0; i < (CODES ? TM : 0); ++i) words_a[i] = *reinterpret_cast<const unsigned *>(pow_lds + at_lds + (wm0 + 16 * i + r16) * 4);
 #pragma unroll
     for (int j = 0; j < (CODES ? TN : 0); ++j)
-      words_b[j] = *reinterpret_cast<const unsigned *>(pow_lds + (kt % RING) * STAGE + (BM + wn0 + 32 * (j / 2) + 4 * (j & 1) + b_first) * 4);
+      words_b[j] = *reinterpret_cast<const unsigned *>(pow_lds + at_lds + (BM + wn0 + 32 * (j / 2) + 4 * (j & 1) + b_first) * 4);
   };
   auto take_powers = [&](int kt) RSVD_INLINE {
     const int by = 8 * ((kt_begin + kt) & 3);
@@ -177,7 +182,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
     for (int j = 0; j < (CODES ? TN : 0); ++j) pb[j] = words_b[j] >> by;
   };
   // Everybody has read its last of the tile before kt, and kt has arrived: `flying` loads are of later tiles.
-  auto meet = [&](auto flying, int kt) RSVD_INLINE {
+  auto meet = [&](auto flying, int kt, int at_lds) RSVD_INLINE {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(tile_wait(decltype(flying)::value));
     __builtin_amdgcn_s_barrier();
@@ -187,7 +192,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
         for (int q = tid; q < (BM + BN) * 8; q += NT)
           if ((q < BM * 8 ? decltype(la)::piece(q) : decltype(lb)::piece(q - BM * 8)) >= last_left) {
 #pragma unroll
-            for (int p = 0; p < PL; ++p) *reinterpret_cast<u32x4 *>(dense_lds + (kt % RING) * STAGE + (p * (BM + BN) * 8 + q) * 16) = (u32x4)0u;
+            for (int p = 0; p < PL; ++p) *reinterpret_cast<u32x4 *>(dense_lds + at_lds + (p * (BM + BN) * 8 + q) * 16) = (u32x4)0u;
           }
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_waitcnt(tile_wait(63));
@@ -197,15 +202,16 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
     }
   };
   point();
+  remain();
 #pragma unroll
   for (int t = 0; t < RING - 1; ++t) {
 #pragma unroll
-    for (int l = 0; l < LOADS; ++l) issue(t, l);
+    for (int l = 0; l < LOADS; ++l) issue(t * STAGE, l);
     advance();
   }
 #pragma unroll
-  for (int l = 0; l < FIRST; ++l) issue(RING - 1, l);
-  meet(std::integral_constant<int, (RING - 2) * LOADS + FIRST>(), 0);
+  for (int l = 0; l < FIRST; ++l) issue((RING - 1) * STAGE, l);
+  meet(std::integral_constant<int, (RING - 2) * LOADS + FIRST>(), 0, 0);
 
   // Where the rows of blocks of a tile that are read ahead would be those of the next one, wavefronts meet, and go on with the next tile's: no wavefront
   // waits for LDS at the start of a tile.  (The loads of a tile go to the place of the one that is multiplied before, from the meeting on.)
@@ -214,7 +220,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
     u32x4 a[2][TM][2][PL], b[2][TN][2][PL];
     unsigned words[2][2][CODES ? TM : 1];
     static_assert(TM == TN, "square tiles");
-    auto fetch = [&](auto to, int kt) RSVD_INLINE {
+    auto fetch = [&](auto to, int at_lds) RSVD_INLINE {
       constexpr int S = decltype(to)::value;
 #pragma unroll
       for (int h = 0; h < 2; ++h)
@@ -222,11 +228,11 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
         for (int i = 0; i < TM; ++i)
 #pragma unroll
           for (int q = PL - 1; q >= 0; --q) {
-            a[S][i][h][q] = piece_a(kt, i, h, q);
-            b[S][i][h][q] = piece_b(kt, i, h, q);
+            a[S][i][h][q] = piece_a(at_lds, i, h, q);
+            b[S][i][h][q] = piece_b(at_lds, i, h, q);
           }
       if constexpr (CODES) {
-        read_powers(kt);
+        read_powers(at_lds);
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
           words[S][0][i] = words_a[i];
@@ -282,12 +288,15 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
           });
       }
     };
+    int here = 0, there = STAGE;                         // where a tile and the next one lie
     auto tile = [&](auto now, auto then, int kt) RSVD_INLINE {
-      meet(std::integral_constant<int, (RING - 2) * LOADS>(), kt + 1);
+      meet(std::integral_constant<int, (RING - 2) * LOADS>(), kt + 1, there);
       advance();
-      fetch(then, kt + 1);
+      fetch(then, there);
 #pragma unroll
-      for (int l = 0; l < LOADS; ++l) issue(kt, l);
+      for (int l = 0; l < LOADS; ++l) issue(here, l);
+      here = there;
+      there = there == (RING - 1) * STAGE ? 0 : there + STAGE;
       __builtin_amdgcn_sched_barrier(0);
       multiply(now, kt);
       __builtin_amdgcn_sched_barrier(0);
@@ -317,30 +326,30 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
 #pragma unroll
       for (int i = 1; i < AHEAD; ++i)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) a[i][h] = piece_a(kt, i, h);
+        for (int h = 0; h < 2; ++h) a[i][h] = piece_a(place(kt), i, h);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < TM - AHEAD; ++i) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) a[(i + AHEAD) % (AHEAD + 1)][h] = piece_a(kt, i + AHEAD, h);
+        for (int h = 0; h < 2; ++h) a[(i + AHEAD) % (AHEAD + 1)][h] = piece_a(place(kt), i + AHEAD, h);
 #pragma unroll
         for (int j = 0; j < TN; ++j) multiply(i, j);
         __builtin_amdgcn_sched_barrier(0);
       }
-      meet(std::integral_constant<int, (RING - 2) * LOADS>(), kt + 1);
+      meet(std::integral_constant<int, (RING - 2) * LOADS>(), kt + 1, place(kt + 1));
       advance();
 #pragma unroll
-      for (int h = 0; h < 2; ++h) a[0][h] = piece_a(kt + 1, 0, h);
-      read_powers(kt + 1);
+      for (int h = 0; h < 2; ++h) a[0][h] = piece_a(place(kt + 1), 0, h);
+      read_powers(place(kt + 1));
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
 #pragma unroll
         for (int i = TM - AHEAD; i < TM; ++i) multiply(i, j);
 #pragma unroll
         for (int l = 0; l < LOADS; ++l)
-          if (l * TN / LOADS == j) issue(kt, l);
+          if (l * TN / LOADS == j) issue(place(kt), l);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) b[j][h] = piece_b(kt + 1, j, h);
+        for (int h = 0; h < 2; ++h) b[j][h] = piece_b(place(kt + 1), j, h);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
@@ -364,19 +373,19 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
       for (int step = 0; step < 2 * TM; ++step) {
         const int h = step / TM, i = step % TM, ahead = step + AHEAD;
         if (step == 2 * TM - AHEAD) {
-          meet(std::integral_constant<int, (RING - 2) * LOADS>(), kt + 1);
+          meet(std::integral_constant<int, (RING - 2) * LOADS>(), kt + 1, place(kt + 1));
           advance();
-          if constexpr (CODES) read_powers(kt + 1);
+          if constexpr (CODES) read_powers(place(kt + 1));
         }
         u32x4 now[PL];
 #pragma unroll
         for (int q = 0; q < PL; ++q) {
           now[q] = a[step % (AHEAD + 1)][q];
-          a[ahead % (AHEAD + 1)][q] = piece_a(ahead < 2 * TM ? kt : kt + 1, ahead % TM, ahead / TM % 2, q);
+          a[ahead % (AHEAD + 1)][q] = piece_a(place(ahead < 2 * TM ? kt : kt + 1), ahead % TM, ahead / TM % 2, q);
 #pragma unroll
           for (int j = 0; j < TN; ++j) {
-            if (h == 0 && i == j * TM / TN) b[1][j][q] = piece_b(kt, j, 1, q);
-            if (step >= 2 * TM - AHEAD && (step - 2 * TM + AHEAD) == j * AHEAD / TN) b[0][j][q] = piece_b(kt + 1, j, 0, q);
+            if (h == 0 && i == j * TM / TN) b[1][j][q] = piece_b(place(kt), j, 1, q);
+            if (step >= 2 * TM - AHEAD && (step - 2 * TM + AHEAD) == j * AHEAD / TN) b[0][j][q] = piece_b(place(kt + 1), j, 0, q);
           }
         }
         if constexpr (KIND == DK_F8_EXACT) {
@@ -402,7 +411,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
         for (int l = 0; l < LOADS; ++l) {
           // (FIRST of them behind the meeting; the others two a step, or as many as it takes to have them all before the next)
           constexpr int EACH = (LOADS - FIRST + 2 * TM - AHEAD - 1) / (2 * TM - AHEAD) > 2 ? (LOADS - FIRST + 2 * TM - AHEAD - 1) / (2 * TM - AHEAD) : 2;
-          if (l < FIRST ? step == 2 * TM - AHEAD + l / 2 : step == (l - FIRST) / EACH) issue(l < FIRST ? kt : kt + RING - 1, l);
+          if (l < FIRST ? step == 2 * TM - AHEAD + l / 2 : step == (l - FIRST) / EACH) issue(place(l < FIRST ? kt : kt + RING - 1), l);
         }
         __builtin_amdgcn_sched_barrier(0);
       }

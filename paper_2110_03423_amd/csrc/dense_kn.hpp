@@ -50,12 +50,17 @@ __global__ __launch_bounds__(64 * WGM * WGN, PL == 3 ? 1 : 2) void dense_kn_kern
     b_now = b_first + (PL > 1 ? 0 : (int64_t)(P.segs.b >> (4 * next_seg) & 15) * P.b_plane) + k * P.ldb;
     left = (int)(P.K - k < kKnK ? P.K - k : kKnK);
   };
+  const int64_t a_step = A_KROWS ? kKnK * P.lda : 2 * kKnK, b_step = kKnK * P.ldb;
+  const int last_left = (int)(P.K - (int64_t)(P.ktiles - 1) * kKnK);
   auto advance = [&]() RSVD_INLINE {                    // (behind the last tile of this workgroup's range: loads stay inside the operands)
+    a_now += a_step;
+    b_now += b_step;
     if (++next_kt == P.ktiles) {
       next_kt = 0;
       if (PL == 1 && next_seg + 1 < P.segs.count) ++next_seg;
+      point();
     }
-    point();
+    left = next_kt == P.ktiles - 1 ? last_left : kKnK;
   };
   Staged<NT, BM, A_KROWS, DEPTH * PL> sa;
   Staged<NT, BN, true, DEPTH * PL> sb;

@@ -13,6 +13,10 @@
 // 2^-13 of the largest of them, as all instructions for 8-bit floats do: measured 1.4e-5 of a result of normal numbers, 1.5e-4 of the sum of
 // magnitudes at the worst.  That is lost in the rounding of a 16-bit result; for fp32 results DK_F8_EXACT makes bf16 numbers of the codes and
 // their powers, exactly, and multiplies those at half the rate.
+//
+// Measured: bf16 8192 x 4096 x 16384 890 us with its gate (1.23 PFLOP/s; the library's largest product 1.41), 8-bit floats 482 us (2.28 PFLOP/s, library 2.67), at the
+// clocks that the power budget leaves (1.93 to 1.98 GHz, matrix pipe busy 55 to 59 %).  Small tiles are bound by what a wavefront issues beside its matrix instructions and by the
+// time of its loads: 0.3 us a k-tile.  So what can be counted on from k-tile to k-tile is not worked out anew (36.8 to 31.6 us for 512 x 4096 x 8192).
 #pragma once
 
 #include <type_traits>

@@ -21,14 +21,16 @@ template <int PL, int BM, int BN> struct DenseKnCfg {
 };
 
 // PL planes of both operands are multiplied while a k-tile of all is in LDS; 1: the products of planes are further k.
-template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN>
-__global__ __launch_bounds__(64 * WGM * WGN, PL == 3 ? 1 : 2) void dense_kn_kernel(const DenseParams P) {
-  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, DEPTH = DenseKnCfg<PL, BM, BN>::DEPTH;
+// KG: groups of wavefronts that have the whole tile and a half of every k-tile (2), or all of it (1).
+template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN, int KG>
+__global__ __launch_bounds__(64 * WGM * WGN * KG, KG == 1 ? 2 : PL == 3 ? 2 : 4) void dense_kn_kernel(const DenseParams P) {
+  static_assert(KG == 1 || (KG == 2 && BM == 64 && PL > 1), "halves of the k-tiles of small tiles of planes");
+  constexpr int NT = 64 * WGM * WGN * KG, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, DEPTH = DenseKnCfg<PL, BM, BN>::DEPTH;
   constexpr int STAGE = DenseKnCfg<PL, BM, BN>::STAGE, PLANE = DenseKnCfg<PL, BM, BN>::PLANE, B_LDS = DenseKnCfg<PL, BM, BN>::A;
   extern __shared__ __attribute__((aligned(16))) char dense_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
-  const int wave_m = wave / WGN, wave_n = wave % WGN, wm0 = wave_m * WM, wn0 = wave_n * WN;
+  const int group = KG == 1 ? 0 : wave / (WGM * WGN), wave_m = wave / WGN - group * WGM, wave_n = wave % WGN, wm0 = wave_m * WM, wn0 = wave_n * WN;
   const DenseWork work = dense_work<BM * BN>(P);
   const int tile_m = work.tile_m, tile_n = work.tile_n, batch = work.batch, kt_begin = work.kt_begin, nkt = work.nkt;
   const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * BN;
@@ -107,14 +109,18 @@ __global__ __launch_bounds__(64 * WGM * WGN, PL == 3 ? 1 : 2) void dense_kn_kern
   auto body = [&](int buf, auto from) RSVD_INLINE {
     constexpr int SET = decltype(from)::value;
     const int a_lds = a_at + buf * STAGE, b_lds = b_at + buf * STAGE;
+    constexpr int STEPS = 2 / KG * TM;                 // rows of blocks, for either half of k or for the group's
     auto read_a = [&](int step, int q) RSVD_INLINE {
-      const int h = step / TM, i = step % TM;
+      const int h = KG == 1 ? step / TM : group, i = step % TM;
       return A_KROWS ? transposed(dense_lds + q * PLANE + (a_lds ^ (i << 5)) + h * 32 * A_ROW, A_ROW)
                      : *reinterpret_cast<const u32x4 *>(dense_lds + q * PLANE + a_lds + i * 2048 + (((4 * h + kq) ^ (r16 & 7)) << 4));
     };
-    auto read_b = [&](int h, int j, int q) RSVD_INLINE { return transposed(dense_lds + q * PLANE + (b_lds ^ (j << 5)) + h * 32 * BN * 2, BN * 2); };
+    auto read_b = [&](int of, int j, int q) RSVD_INLINE {
+      const int h = KG == 1 ? of : group;
+      return transposed(dense_lds + q * PLANE + (b_lds ^ (j << 5)) + h * 32 * BN * 2, BN * 2);
+    };
     constexpr int AHEAD = TM >= 4 ? 3 : 1;             // rows of blocks read ahead, not all of them: registers
-    u32x4 a[AHEAD + 1][PL], b[2][TN][PL];
+    u32x4 a[AHEAD + 1][PL], b[2 / KG][TN][PL];
 #pragma unroll
     for (int q = 0; q < PL; ++q) {
 #pragma unroll
@@ -124,14 +130,14 @@ __global__ __launch_bounds__(64 * WGM * WGN, PL == 3 ? 1 : 2) void dense_kn_kern
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int step = 0; step < 2 * TM; ++step) {
+    for (int step = 0; step < STEPS; ++step) {
       const int h = step / TM, i = step % TM;
 #pragma unroll
       for (int q = 0; q < PL; ++q) {
-        if (step + AHEAD < 2 * TM) a[(step + AHEAD) % (AHEAD + 1)][q] = read_a(step + AHEAD, q);
+        if (step + AHEAD < STEPS) a[(step + AHEAD) % (AHEAD + 1)][q] = read_a(step + AHEAD, q);
 #pragma unroll
         for (int j = 0; j < TN; ++j)
-          if (h == 0 && i == j * TM / TN) b[1][j][q] = read_b(1, j, q);
+          if (KG == 1 && h == 0 && i == j * TM / TN) b[KG == 1][j][q] = read_b(1, j, q);
       }
       with_segs<PL>([&](auto pa, auto pb) RSVD_INLINE {
 #pragma unroll
@@ -142,7 +148,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, PL == 3 ? 1 : 2) void dense_kn_kern
       });
 #pragma unroll
       for (int p = 0; p < PIECES; ++p)
-        if (p * (2 * TM) / PIECES == step) {
+        if (p * STEPS / PIECES == step) {
           write(SET, p, buf ^ 1);
           load(SET, p);
         }
@@ -181,13 +187,36 @@ __global__ __launch_bounds__(64 * WGM * WGN, PL == 3 ? 1 : 2) void dense_kn_kern
   float *const partial = work.partial != nullptr ? work.partial + wm0 * BN + wn0 : nullptr;
   int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
   asm volatile("" : "+v"(last_lane));
+  // Of groups that have halves of k, each ends with one row of blocks: its own sums and the other's, through LDS behind what the end takes.
   // (behind the last meeting nobody reads the tiles)
-  dense_finish<BN, TM, TN>(P, acc, partial, batch, m0 + wm0, n0 + wn0, P.symmetric && tile_m != tile_n, last_lane,
-                       reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
+  constexpr int ROWS = TM / KG;
+  f32x4 sums[ROWS][TN];
+  if constexpr (KG == 2) {
+    constexpr int ROOM = WGM * WGN * KG * finish_lds<TN>();
+    static_assert(TM == 2 && ROOM % 16 == 0 && ROOM + WGM * WGN * 2 * TN * 1024 <= 2 * STAGE, "a row of blocks a group");
+    f32x4 *const mine = reinterpret_cast<f32x4 *>(dense_lds + ROOM) + wave * TN * 64 + last_lane;
+    f32x4 *const other = reinterpret_cast<f32x4 *>(dense_lds + ROOM) + (wave + (group == 0 ? WGM * WGN : -WGM * WGN)) * TN * 64 + last_lane;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      mine[j * 64] = group == 0 ? acc[1][j] : acc[0][j];
+      sums[0][j] = group == 0 ? acc[0][j] : acc[1][j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sums[0][j] += other[j * 64];
+  } else {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) sums[i][j] = acc[i][j];
+  }
+  const int below = KG == 1 ? 0 : 16 * group;
+  dense_finish<BN, ROWS, TN>(P, sums, partial == nullptr ? nullptr : partial + below * BN, batch, m0 + wm0 + below, n0 + wn0, P.symmetric && tile_m != tile_n, last_lane,
+                             reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
 }
 
-template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN> hipError_t dense_kn_run(hipStream_t s, const DenseParams &P) {
-  hipLaunchKernelGGL((dense_kn_kernel<KIND, A_KROWS, PL, BM, BN, WGM, WGN>), dim3(dense_groups(P)), dim3(64 * WGM * WGN), (DenseKnCfg<PL, BM, BN>::lds), s, P);
+template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN, int KG = 1> hipError_t dense_kn_run(hipStream_t s, const DenseParams &P) {
+  hipLaunchKernelGGL((dense_kn_kernel<KIND, A_KROWS, PL, BM, BN, WGM, WGN, KG>), dim3(dense_groups(P)), dim3(64 * WGM * WGN * KG), (DenseKnCfg<PL, BM, BN>::lds), s, P);
   return hipGetLastError();
 }
 // The planes that small tiles of a kind take at once.
@@ -195,15 +224,15 @@ template <int KIND> constexpr int dense_kn_planes() { return KIND == DK_BF16 ? 3
 template <int KIND, bool A_KROWS> hipError_t dense_kn_tile(hipStream_t s, const DenseParams &P, int b) {
   if (b == 256) return dense_kn_run<KIND, A_KROWS, 1, 256, 256, 2, 4>(s, P);
   if (b == 128) return dense_kn_run<KIND, A_KROWS, 1, 128, 128, 2, 2>(s, P);
-  if (P.segs.count > 1) return dense_kn_run<KIND, A_KROWS, dense_kn_planes<KIND>(), 64, 64, 2, 2>(s, P);
+  if (P.segs.count > 1) return dense_kn_run<KIND, A_KROWS, dense_kn_planes<KIND>(), 64, 64, 2, 2, 2>(s, P);
   return dense_kn_run<KIND, A_KROWS, 1, 64, 64, 2, 2>(s, P);
 }
 template <int KIND, bool A_KROWS> hipError_t dense_kn_init() {
   constexpr int PL = dense_kn_planes<KIND>();
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, 1, 256, 256, 2, 4>), hipFuncAttributeMaxDynamicSharedMemorySize,
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, 1, 256, 256, 2, 4, 1>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                            (int)DenseKnCfg<1, 256, 256>::lds);
   if (e != hipSuccess) return e;
-  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, PL, 64, 64, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, PL, 64, 64, 2, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
                              (int)DenseKnCfg<PL, 64, 64>::lds);
 }
 #define DENSE_KN(KIND, A_KROWS)                                                                      \

@@ -78,14 +78,16 @@ __device__ __forceinline__ i32x8 f8_both(const u32x4 (&p)[2]) {
 }
 
 // PL planes of both operands are multiplied while a k-tile of all is in LDS; 1: the products of planes are further k.
-template <int KIND, bool GATED, int PL, int BM, int BN, int WGM, int WGN>
-__global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void dense_nt_kernel(const DenseParams P) {
-  constexpr int NT = 64 * WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = DenseNtCfg<KIND, PL, BM, BN>::STAGE, RING = DenseNtCfg<KIND, PL, BM, BN>::RING;
+// KG: groups of wavefronts that have the whole tile and a half of every k-tile (2), or all of it (1).
+template <int KIND, bool GATED, int PL, int BM, int BN, int WGM, int WGN, int KG>
+__global__ __launch_bounds__(64 * WGM * WGN * KG, BM == 256 ? 1 : KG == 1 ? 2 : PL == 3 ? 2 : 4) void dense_nt_kernel(const DenseParams P) {
+  static_assert(KG == 1 || (KG == 2 && BM == 64 && PL > 1), "halves of the k-tiles of small tiles of planes");
+  constexpr int NT = 64 * WGM * WGN * KG, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = DenseNtCfg<KIND, PL, BM, BN>::STAGE, RING = DenseNtCfg<KIND, PL, BM, BN>::RING;
   constexpr bool CODES = KIND >= DK_F8;
   extern __shared__ __attribute__((aligned(16))) char dense_lds[];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int r16 = lane & 15, kq = lane >> 4;
-  const int wm0 = (wave / WGN) * WM, wn0 = (wave % WGN) * WN;
+  const int group = KG == 1 ? 0 : wave / (WGM * WGN), wave_m = wave / WGN - group * WGM, wm0 = wave_m * WM, wn0 = (wave % WGN) * WN;
   const DenseWork work = dense_work<BM * BN>(P);
   const int tile_m = work.tile_m, tile_n = work.tile_n, batch = work.batch, kt_begin = work.kt_begin, nkt = work.nkt;
   const int64_t m0 = (int64_t)tile_m * BM, n0 = (int64_t)tile_n * (GATED ? BN / 2 : BN);
@@ -221,19 +223,19 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
   // waits for LDS at the start of a tile.  (The loads of a tile go to the place of the one that is multiplied before, from the meeting on.)
   if constexpr (BM == 64) {
     // small tiles: all operands of the next tile are read while one is multiplied (LDS takes longer to answer than a row of blocks takes)
-    u32x4 a[2][TM][2][PL], b[2][TN][2][PL];
+    u32x4 a[2][TM][2 / KG][PL], b[2][TN][2 / KG][PL];
     unsigned words[2][2][CODES ? TM : 1];
     static_assert(TM == TN, "square tiles");
     auto fetch = [&](auto to, int at_lds) RSVD_INLINE {
       constexpr int S = decltype(to)::value;
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+      for (int h = 0; h < 2 / KG; ++h)
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
           for (int q = PL - 1; q >= 0; --q) {
-            a[S][i][h][q] = piece_a(at_lds, i, h, q);
-            b[S][i][h][q] = piece_b(at_lds, i, h, q);
+            a[S][i][h][q] = piece_a(at_lds, i, KG == 1 ? h : group, q);
+            b[S][i][h][q] = piece_b(at_lds, i, KG == 1 ? h : group, q);
           }
       if constexpr (CODES) {
         read_powers(at_lds);
@@ -280,7 +282,7 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
         }
       } else {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2 / KG; ++h)
           with_segs<PL>([&](auto qa, auto qb) RSVD_INLINE {
 #pragma unroll
             for (int i = 0; i < TM; ++i)
@@ -422,22 +424,46 @@ __global__ __launch_bounds__(64 * WGM * WGN, BM == 256 || PL == 3 ? 1 : 2) void 
     }
   }
 
-  const int64_t m1 = m0 + wm0, n1 = n0 + (GATED ? wn0 / 2 : wn0);
-  float *const partial = work.partial != nullptr ? work.partial + wm0 * BN + wn0 : nullptr;
   int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
   asm volatile("" : "+v"(last_lane));
-  dense_finish_rows<GATED, BN, TM, TN>(P, acc, partial, batch, m1, n1, last_lane);
+  const int64_t n1 = n0 + (GATED ? wn0 / 2 : wn0);
+  float *const partial = work.partial != nullptr ? work.partial + wm0 * BN + wn0 : nullptr;
+  // Of groups that have halves of k, each ends with one row of blocks: its own sums and the other's.
+  constexpr int ROWS = TM / KG;
+  f32x4 sums[ROWS][TN];
+  if constexpr (KG == 2) {
+    static_assert(TM == 2 && WGM * WGN * 2 * TN * 1024 <= RING * STAGE, "a row of blocks a group");
+    __builtin_amdgcn_s_waitcnt(tile_wait(0));            // (nothing may land in LDS any more)
+    __syncthreads();
+    f32x4 *const mine = reinterpret_cast<f32x4 *>(dense_lds) + wave * TN * 64 + last_lane;
+    f32x4 *const other = reinterpret_cast<f32x4 *>(dense_lds) + (wave + (group == 0 ? WGM * WGN : -WGM * WGN)) * TN * 64 + last_lane;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      mine[j * 64] = group == 0 ? acc[1][j] : acc[0][j];
+      sums[0][j] = group == 0 ? acc[0][j] : acc[1][j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < TN; ++j) sums[0][j] += other[j * 64];
+  } else {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) sums[i][j] = acc[i][j];
+  }
+  const int64_t m1 = m0 + wm0 + (KG == 1 ? 0 : 16 * group);
+  dense_finish_rows<GATED, BN, ROWS, TN>(P, sums, KG == 1 || partial == nullptr ? partial : partial + 16 * group * BN, batch, m1, n1, last_lane);
   if constexpr (!GATED && !CODES) {
     if (P.symmetric && tile_m != tile_n && partial == nullptr) {
       __builtin_amdgcn_s_waitcnt(tile_wait(0));          // (nothing may land in LDS any more)
       __syncthreads();
-      dense_finish_mirror<TM, TN>(P, acc, batch, m1, n1, last_lane, reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
+      dense_finish_mirror<ROWS, TN>(P, sums, batch, m1, n1, last_lane, reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
     }
   }
 }
 
-template <int KIND, bool GATED, int PL, int BM, int BN, int WGM, int WGN> hipError_t dense_nt_run(hipStream_t s, const DenseParams &P) {
-  hipLaunchKernelGGL((dense_nt_kernel<KIND, GATED, PL, BM, BN, WGM, WGN>), dim3(dense_groups(P)), dim3(64 * WGM * WGN), (DenseNtCfg<KIND, PL, BM, BN>::lds), s, P);
+template <int KIND, bool GATED, int PL, int BM, int BN, int WGM, int WGN, int KG = 1> hipError_t dense_nt_run(hipStream_t s, const DenseParams &P) {
+  hipLaunchKernelGGL((dense_nt_kernel<KIND, GATED, PL, BM, BN, WGM, WGN, KG>), dim3(dense_groups(P)), dim3(64 * WGM * WGN * KG), (DenseNtCfg<KIND, PL, BM, BN>::lds), s, P);
   return hipGetLastError();
 }
 // The planes that small tiles of a kind take at once: three of bf16 numbers, two of fp16 numbers of a plain product.
@@ -445,15 +471,16 @@ template <int KIND, bool GATED> constexpr int dense_nt_planes() { return KIND ==
 template <int KIND, bool GATED> hipError_t dense_nt_tile(hipStream_t s, const DenseParams &P, int b) {
   if (b == 256) return dense_nt_run<KIND, GATED, 1, 256, 256, 2, 2>(s, P);
   if (b == 128) return dense_nt_run<KIND, GATED, 1, 128, 128, 2, 2>(s, P);
-  if (P.segs.count > 1) return dense_nt_run<KIND, GATED, dense_nt_planes<KIND, GATED>(), 64, 64, 2, 2>(s, P);
+  constexpr int PL = dense_nt_planes<KIND, GATED>();
+  if (P.segs.count > 1) return dense_nt_run<KIND, GATED, PL, 64, 64, 2, 2, PL == 1 ? 1 : 2>(s, P);
   return dense_nt_run<KIND, GATED, 1, 64, 64, 2, 2>(s, P);
 }
 template <int KIND, bool GATED> hipError_t dense_nt_init() {
   constexpr int PL = dense_nt_planes<KIND, GATED>();
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, 1, 256, 256, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, 1, 256, 256, 2, 2, 1>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                            (int)DenseNtCfg<KIND, 1, 256, 256>::lds);
   if (e != hipSuccess || PL == 1) return e;
-  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, PL, 64, 64, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, PL, 64, 64, 2, 2, PL == 1 ? 1 : 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
                              (int)DenseNtCfg<KIND, PL, 64, 64>::lds);
 }
 #define DENSE_NT(KIND, GATED)                                                                        \

@@ -5,7 +5,7 @@
 // from memory to registers and from there to LDS, among the matrix instructions of the tile before.
 //
 // Measured: bf16 8192 x 16384 x 4096 829 us (1.33 PFLOP/s, matrix pipe busy 69 % at 1.84 GHz: power; the library's product in this order 1.25), with rows of m 888 us (1.24; library 1.11).
-// fp32 301 x 2820 x 2999 in tiles of 64 with all planes at once 48.7 us, 2820 x 301 x 2999 in tiles of 128 45.4.
+// fp32 301 x 2820 x 2999 in tiles of 64 with all planes at once 47.3 us, 2820 x 301 x 2999 in tiles of 128 45.4.
 #pragma once
 
 #include <type_traits>
@@ -21,7 +21,7 @@ template <int PL, int BM, int BN> struct DenseKnCfg {
 };
 
 // PL planes of both operands are multiplied while a k-tile of all is in LDS; 1: the products of planes are further k.
-// KG: groups of wavefronts that have the whole tile and a half of every k-tile (2), or all of it (1).
+// KG: groups of wavefronts that have the whole tile and a half of every k-tile (2: two wavefronts a SIMD, one waits while the other multiplies), or all of it (1).
 template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN, int KG>
 __global__ __launch_bounds__(64 * WGM * WGN * KG, KG == 1 ? 2 : PL == 3 ? 2 : 4) void dense_kn_kernel(const DenseParams P) {
   static_assert(KG == 1 || (KG == 2 && BM == 64 && PL > 1), "halves of the k-tiles of small tiles of planes");

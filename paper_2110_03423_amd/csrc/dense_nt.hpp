@@ -78,7 +78,8 @@ __device__ __forceinline__ i32x8 f8_both(const u32x4 (&p)[2]) {
 }
 
 // PL planes of both operands are multiplied while a k-tile of all is in LDS; 1: the products of planes are further k.
-// KG: groups of wavefronts that have the whole tile and a half of every k-tile (2), or all of it (1).
+// KG: groups of wavefronts that have the whole tile and a half of every k-tile (2: two wavefronts a SIMD, one waits while the other multiplies; gated fp32
+// 384 x 2048 -> 2048 59.8 us, with one group 70.0), or all of it (1).
 template <int KIND, bool GATED, int PL, int BM, int BN, int WGM, int WGN, int KG>
 __global__ __launch_bounds__(64 * WGM * WGN * KG, BM == 256 ? 1 : KG == 1 ? 2 : PL == 3 ? 2 : 4) void dense_nt_kernel(const DenseParams P) {
   static_assert(KG == 1 || (KG == 2 && BM == 64 && PL > 1), "halves of the k-tiles of small tiles of planes");

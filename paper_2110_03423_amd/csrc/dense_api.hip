@@ -40,8 +40,8 @@ bool overlap(const Span &a, const Span &b) {
   const uintptr_t at = (uintptr_t)a.p, bt = (uintptr_t)b.p;
   const uintptr_t a_end = at + (uintptr_t)((a.rows - 1) * a.step + a.width), b_end = bt + (uintptr_t)((b.rows - 1) * b.step + b.width);
   if (a_end <= bt || b_end <= at) return false;
-  if (a.step != b.step || a.rows == 1 || b.rows == 1) return true;
-  const int64_t step = a.step, d = at <= bt ? (int64_t)((bt - at) % (uintptr_t)step) : (step - (int64_t)((at - bt) % (uintptr_t)step)) % step;
+  if ((a.rows == 1 && b.rows == 1) || (a.rows > 1 && b.rows > 1 && a.step != b.step)) return true;
+  const int64_t step = a.rows > 1 ? a.step : b.step, d = at <= bt ? (int64_t)((bt - at) % (uintptr_t)step) : (step - (int64_t)((at - bt) % (uintptr_t)step)) % step;
   return !(d >= a.width && d + b.width <= step);
 }
 template <int N> bool overlap(const Span &a, const Span (&others)[N]) {

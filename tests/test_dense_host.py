@@ -126,6 +126,10 @@ def test_results_may_not_lie_on_operands(plan):
     wide = dict(ldx=120, ldh=120)
     assert call(H=at(x + 100), **wide) == ERR_NO_DEVICE and call(H=at(x + 140), **wide) == ERR_NO_DEVICE and call(H=at(x + 98), **wide) == -12
     assert call(H=at(x + 142), **wide) == -12 and call(H=at(x + 240 * 7 + 100), **wide) == ERR_NO_DEVICE and call(H=at(x - 240 * 7 - 100), **wide) == ERR_NO_DEVICE
+    # one row, too
+    one = dict(wide, tokens=1, kept=NULL, ldk=0, ldw=120)
+    assert call(H=at(2 * x + 240 * 7 + 100), **one) == ERR_NO_DEVICE and call(H=at(2 * x + 240 * 7 + 98), **one) == -12 and call(H=at(2 * x + 240 * 7 + 142), **one) == -12
+    assert call(H=at(2 * x - 98), **one) == -12 and call(H=at(2 * x - 100), **one) == ERR_NO_DEVICE and call(H=at(x + 98), **one) == -12
     assert call(H=at(x - 240 * 7 - 98), **wide) == -12 and call(H=at(x + 100), ldx=120, ldh=122) == -12
 
     call = caller(plan, "rsvd_gated_product_grad", "ctx stream type act tokens n m dH lddh X ldx W ldw kept ldk dX lddx dW lddw f32 acc ws bytes", ctx=plan.h, stream=NULL,

@@ -438,7 +438,8 @@ int rsvd_f8_product_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_
 int rsvd_f8_product_grad_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, size_t *bytes);
 int rsvd_f8_weight_grad_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int dw_f32, size_t *bytes);
 
-/* Y (tokens x m) = X^ W^^T.  (workspace may be NULL where no bytes are needed: up to 16 tokens) */
+/* Y (tokens x m) = X^ W^^T.  (workspace may be NULL where no bytes are needed: up to 16 tokens, but not of
+ * the largest weights) */
 int rsvd_f8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, const void *X, int64_t ldx,
                     const uint8_t *codes, int64_t ldq, const uint8_t *powers, int64_t ldp, void *Y, int64_t ldy, void *workspace, size_t workspace_bytes);
 

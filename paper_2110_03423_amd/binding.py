@@ -86,7 +86,8 @@ PROTOTYPES = {
 }
 X_BF16, X_F16, X_F32 = 0, 1, 2
 ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
-GATED_FEW, F8_FEW = (32, 32, 64), 16      # tokens up to which these products need no workspace (of a gated block: by type)
+# by type, tokens up to which these products need no workspace, and of 8-bit floats (up to 16) tokens times inputs times outputs, 4096 of them at least
+GATED_FEW, F8_FEW = (32, 32, 64), (1 << 29, 1 << 29, 3 << 26)
 
 
 def load_library():
@@ -771,7 +772,7 @@ class Rsvd:
         stream = self._raw_stream()
         if workspace is not None:
             ws = self._given(workspace)
-        elif tokens <= F8_FEW:
+        elif tokens <= 16 and tokens * n * max(m, 4096) <= F8_FEW[xt]:
             ws = (None, 0)
         else:
             ws = self._layer_ws(stream, name + "_bytes", (xt, tokens, weight.n, weight.m))

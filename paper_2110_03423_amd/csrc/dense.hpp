@@ -91,8 +91,15 @@ struct LayOut { const void *X; int64_t ldx, rows; uint16_t *out; int64_t plane; 
 hipError_t lay_out_launch(hipStream_t s, rsvd_xtype type, int64_t n, int64_t width, const LayOut &x, const LayOut &w, int64_t tokens, int64_t m, const GatedOut &slope);
 
 // ---------------------------------------------------------------- f8.hip
-// Tokens up to which every workgroup rounds them again: 4096 -> 8192 in bf16 17 tokens 18.5 and 18.3 us.
-constexpr int64_t kF8Few = 16;
+// Whether each workgroup rounds the tokens itself, and whether a weight is read straight from memory for tokens that were rounded before; tiles are faster for more tokens and for
+// large weights, whose tokens come out of a cache again for every sixteen rows.  4096 -> 4096 in bf16 16 tokens 8.6 us, 17 rounded before 11.0, in tiles 13.7, 32: 12.7 and 14.1;
+// 4096 -> 16384 8 tokens 21.9, 16: 29.0, in tiles 19.3; fp32 4096 -> 8192 8 tokens 17.6, 12: 20.5, in tiles 21.2.
+// (Fewer than 4096 outputs leave CUs without a workgroup: each takes as long.)
+inline int64_t f8_rounded(int64_t tokens, int64_t n, int64_t m) { return tokens * n * (m > 4096 ? m : 4096); }
+inline bool f8_few(rsvd_xtype type, int64_t tokens, int64_t n, int64_t m) {
+  return tokens <= 16 && f8_rounded(tokens, n, m) <= (type == RSVD_X_F32 ? (int64_t)3 << 26 : (int64_t)1 << 29);
+}
+inline bool f8_few_codes(int64_t tokens, int64_t n, int64_t m) { return tokens <= 32 && f8_rounded(tokens, n, m) <= (int64_t)1 << 29; }
 // X (rows x n) to codes in blocks of 128 of a row (codes: rows x width, powers rows x ldp), zeros behind the last number; Y (rows x m) and X (rows x n) to codes in blocks of 128
 // rows (m x width and n x width, powers of rows of ldp; width = rows up to a multiple of 128).
 hipError_t f8_rows_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, const void *X, int64_t ldx, uint8_t *codes, int64_t width, uint8_t *powers, int64_t ldp);
@@ -101,7 +108,7 @@ hipError_t f8_columns_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64
 // W (m x n) to codes in blocks of 128 x 128, and the same in the other order (NULL: not wanted).
 hipError_t f8_weight_launch(hipStream_t s, rsvd_xtype type, int64_t m, int64_t n, const void *W, int64_t ldw, uint8_t *codes, int64_t ldq, uint8_t *powers, int64_t ldp,
                             uint8_t *codes_t, int64_t ldqt, uint8_t *powers_t, int64_t ldpt);
-// The product of up to kF8Few tokens, X rounded on the way.
+// The product of a few tokens, X rounded on the way.
 struct F8FewDesc {
   rsvd_xtype type; int64_t tokens, n, m;
   const void *X; int64_t ldx;
@@ -110,6 +117,8 @@ struct F8FewDesc {
   void *Y; int64_t ldy;
 };
 hipError_t f8_few_launch(rsvd_ctx *ctx, hipStream_t s, const F8FewDesc &d);
+// The same of up to 32 tokens, rounded before.
+hipError_t f8_codes_launch(rsvd_ctx *ctx, hipStream_t s, const F8FewDesc &d, const uint8_t *x, int64_t ldx, const uint8_t *x_powers, int64_t ldxp);
 
 // ---------------------------------------------------------------- orthogonal.hip
 // |G| of every matrix by parts (kNormParts doubles each), and G / |G| times 2^13 as two fp16 planes with zeros up to `width`.

@@ -154,10 +154,10 @@ struct F8Layout { size_t a, a_pow, b, b_pow, partial, partial_bytes, total; };
 F8Layout f8_product_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m) {
   F8Layout L = {};
   Take take;
-  if (tokens > kF8Few) {
+  if (!f8_few(type, tokens, n, m)) {
     L.a = take((size_t)tokens * f8_width(n));
     L.a_pow = take((size_t)tokens * f8_powers(n));
-    L.partial_bytes = dense_partial_bytes(ctx, f8_desc(type == RSVD_X_F32, tokens, m, n));
+    L.partial_bytes = f8_few_codes(tokens, n, m) ? 0 : dense_partial_bytes(ctx, f8_desc(type == RSVD_X_F32, tokens, m, n));
     L.partial = take(L.partial_bytes);
   }
   L.total = take.off;
@@ -195,7 +195,7 @@ int f8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int
   if (workspace_bytes < L.total) return -16;
   RSVD_ON_DEVICE();
   hipStream_t s = (hipStream_t)stream;
-  if (tokens <= kF8Few) {
+  if (f8_few(type, tokens, n, m)) {
     const F8FewDesc d = {type, tokens, n, m, X, ldx, codes, ldq, powers, ldp, Y, ldy};
     ProfScope ps(ctx, s, prof);
     RSVD_TRY(f8_few_launch(ctx, s, d), "product of a few tokens");
@@ -206,6 +206,12 @@ int f8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int
   {
     ProfScope ps(ctx, s, PK_SMALL);
     RSVD_TRY(f8_rows_launch(s, type, tokens, n, X, ldx, q, f8_width(n), p, f8_powers(n)), "tokens to 8-bit floats");
+  }
+  if (f8_few_codes(tokens, n, m)) {
+    const F8FewDesc d = {type, tokens, n, m, X, ldx, codes, ldq, powers, ldp, Y, ldy};
+    ProfScope ps(ctx, s, prof);
+    RSVD_TRY(f8_codes_launch(ctx, s, d, q, f8_width(n), p, f8_powers(n)), "product of a few tokens");
+    return RSVD_OK;
   }
   DenseDesc d = f8_desc(type == RSVD_X_F32, tokens, m, n);
   d.A = q; d.lda = f8_width(n); d.a_pow = p; d.ld_apow = f8_powers(n);

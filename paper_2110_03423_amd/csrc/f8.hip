@@ -291,6 +291,97 @@ template <int XT, int WAVES> __global__ __launch_bounds__(64 * WAVES, 4) void f8
   if (r16 < P.tokens && n < P.m) put4<XT>(P.Y, r16 * P.ldy + n, left_of(n, P.m), acc);
 }
 
+// Up to 32 tokens that were rounded before (rounding 32 tokens again would take every workgroup as long as its weights).
+struct F8CodesParams {
+  const uint8_t *x, *x_powers; int64_t ldx, ldxp, tokens, m;
+  const uint8_t *codes, *powers; int64_t ldq, ldp;
+  int steps;                       // of 128 k
+  void *Y; int64_t ldy;
+};
+template <int XT, int WAVES> __global__ __launch_bounds__(64 * WAVES, 4) void f8_codes_kernel(const F8CodesParams P) {
+  constexpr int U = 2, TB = 2;
+  __shared__ f32x4 part[WAVES][TB][64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int r16 = lane & 15, kq = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t row = n0 + r16 < P.m ? n0 + r16 : P.m - 1;
+  const uint8_t *const w = P.codes + row * P.ldq + 32 * kq, *const powers = P.powers + (n0 >> 7) * P.ldp;
+  const uint8_t *x[TB], *x_powers[TB];
+#pragma unroll
+  for (int i = 0; i < TB; ++i) {
+    const int64_t t = 16 * i + r16 < P.tokens ? 16 * i + r16 : P.tokens - 1;
+    x[i] = P.x + t * P.ldx + 32 * kq;
+    x_powers[i] = P.x_powers + t * P.ldxp;
+  }
+  f32x4 acc[TB];
+#pragma unroll
+  for (int i = 0; i < TB; ++i) acc[i] = (f32x4)0.f;
+  for (int s0 = wave; s0 < P.steps; s0 += WAVES * U) {
+    u32x4 b[U][2], y[U][TB][2];
+    unsigned pb[U], pa[U][TB];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int s = s0 + WAVES * u < P.steps ? s0 + WAVES * u : s0;      // (behind the last step: the first one again, unused)
+      pb[u] = powers[s];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) b[u][h] = *reinterpret_cast<const u32x4 *>(w + (int64_t)128 * s + 16 * h);
+#pragma unroll
+      for (int i = 0; i < TB; ++i) {
+        pa[u][i] = x_powers[i][s];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) y[u][i][h] = *reinterpret_cast<const u32x4 *>(x[i] + (int64_t)128 * s + 16 * h);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (s0 + WAVES * u >= P.steps) break;
+      if constexpr (XT == RSVD_X_F32) {
+        const float ub = f8_unit(pb[u]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          u32x4 bw[2], aw[2];
+          f8_widen(b[u][h], ub, bw);
+#pragma unroll
+          for (int i = 0; i < TB; ++i) {
+            f8_widen(y[u][i][h], f8_unit(pa[u][i]), aw);
+#pragma unroll
+            for (int z = 0; z < 2; ++z) acc[i] = mfma_bf16(bw[z], aw[z], acc[i]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < TB; ++i)
+          acc[i] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(f8_both(b[u]), f8_both(y[u][i]), acc[i], 0, 0, 0, (int)pb[u], 0, (int)pa[u][i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < TB; ++i) part[wave][i][lane] = acc[i];
+  __syncthreads();
+  if (wave >= TB) return;
+  f32x4 sum = part[0][wave][lane];
+#pragma unroll
+  for (int v = 1; v < WAVES; ++v) sum += part[v][wave][lane];
+  const int64_t t = 16 * wave + r16, n = n0 + 4 * kq;
+  if (t < P.tokens && n < P.m) put4<XT>(P.Y, t * P.ldy + n, left_of(n, P.m), sum);
+}
+
+template <int XT> static void f8_codes_run(hipStream_t s, const F8CodesParams &P, dim3 grid) {
+  if (P.steps > 16) hipLaunchKernelGGL((f8_codes_kernel<XT, 16>), grid, dim3(1024), 0, s, P);
+  else if (P.steps > 8) hipLaunchKernelGGL((f8_codes_kernel<XT, 8>), grid, dim3(512), 0, s, P);
+  else hipLaunchKernelGGL((f8_codes_kernel<XT, 4>), grid, dim3(256), 0, s, P);
+}
+
+hipError_t f8_codes_launch(rsvd_ctx *, hipStream_t s, const F8FewDesc &d, const uint8_t *x, int64_t ldx, const uint8_t *x_powers, int64_t ldxp) {
+  if (d.tokens < 1 || d.tokens > 32) return hipErrorInvalidValue;
+  const F8CodesParams P = {x, x_powers, ldx, ldxp, d.tokens, d.m, d.codes, d.powers, d.ldq, d.ldp, (int)ceil_div(d.n, 128), d.Y, d.ldy};
+  const dim3 grid((unsigned)ceil_div(d.m, 16));
+  if (d.type == RSVD_X_BF16) f8_codes_run<RSVD_X_BF16>(s, P, grid);
+  else if (d.type == RSVD_X_F16) f8_codes_run<RSVD_X_F16>(s, P, grid);
+  else f8_codes_run<RSVD_X_F32>(s, P, grid);
+  return hipGetLastError();
+}
+
 template <int XT> static void f8_few_run(hipStream_t s, const F8FewParams &P, dim3 grid) {
   // (16 wavefronts: 4096 -> 8192 one token of bf16 10.1 us, 8: 11.3; 16384 -> 4096 18.4 and 21.0)
   if (P.steps > 16) hipLaunchKernelGGL((f8_few_kernel<XT, 16>), grid, dim3(1024), 0, s, P);
@@ -299,7 +390,7 @@ template <int XT> static void f8_few_run(hipStream_t s, const F8FewParams &P, di
 }
 
 hipError_t f8_few_launch(rsvd_ctx *, hipStream_t s, const F8FewDesc &d) {
-  if (d.tokens < 1 || d.tokens > kF8Few) return hipErrorInvalidValue;
+  if (d.tokens < 1 || d.tokens > 16) return hipErrorInvalidValue;
   const F8FewParams P = {(const char *)d.X, d.ldx, d.tokens, d.n, d.m, d.codes, d.powers, d.ldq, d.ldp, (int)ceil_div(d.n, 128), d.Y, d.ldy};
   const dim3 grid((unsigned)ceil_div(d.m, 16));
   if (d.type == RSVD_X_BF16) f8_few_run<RSVD_X_BF16>(s, P, grid);

@@ -58,8 +58,14 @@ def test_gated_product_checks_every_argument(plan):
 
 def test_the_binding_knows_how_many_tokens_need_no_workspace(plan):
     for xt in (X_BF16, X_F16, X_F32):
-        for few, name, more in ((binding.GATED_FEW[xt], "rsvd_gated_product_bytes", (0,)), (binding.F8_FEW, "rsvd_f8_product_bytes", ()), (binding.F8_FEW, "rsvd_f8_product_grad_bytes", ())):
-            assert bytes_of(plan, name, xt, few, 100, 200, *more) == 0 and bytes_of(plan, name, xt, few + 1, 100, 200, *more) > 0
+        few = binding.GATED_FEW[xt]
+        assert bytes_of(plan, "rsvd_gated_product_bytes", xt, few, 100, 200, 0) == 0 and bytes_of(plan, "rsvd_gated_product_bytes", xt, few + 1, 100, 200, 0) > 0
+        n = binding.F8_FEW[xt] // (16 * 4096)
+        for name, turned in (("rsvd_f8_product_bytes", False), ("rsvd_f8_product_grad_bytes", True)):
+            for rows in (4096, 50):
+                small, large = ((rows, n), (rows, n + 1)) if turned else ((n, rows), (n + 1, rows))
+                assert bytes_of(plan, name, xt, 16, *small) == 0 and bytes_of(plan, name, xt, 17, *small) > 0
+                assert bytes_of(plan, name, xt, 16, *large) > 0 and bytes_of(plan, name, xt, 8, *large) == 0
 
 
 def test_gated_gradient_checks_every_argument(plan):

@@ -105,7 +105,7 @@ def test_rounding_at_the_edges(dtype):
         assert torch.equal(got[~small], value[~small].to(T)) and float(got[small].abs().max() if small.any() else 0) < 2.0 ** -125
 
 
-SIZES = [(1, 1, 1), (1, 128, 16), (2, 300, 17), (16, 1000, 200), (17, 257, 130), (33, 4096, 100), (64, 129, 1000), (65, 128, 128), (66, 5, 300), (200, 1000, 129), (513, 640, 384),
+SIZES = [(1, 1, 1), (1, 128, 16), (2, 300, 17), (16, 1000, 200), (17, 257, 130), (32, 2200, 35), (33, 4096, 100), (64, 129, 1000), (65, 128, 128), (66, 5, 300), (200, 1000, 129), (513, 640, 384),
          (1025, 333, 777)]
 
 
@@ -128,7 +128,7 @@ def test_product_and_gradients(dtype, t, n, m):
     assert torch.equal(more, f32 + 0.25)
 
 
-EXACT = [(1, 4096, 48), (15, 200, 4000), (40, 16384, 33), (64, 640, 130), (65, 16384, 64), (129, 4097, 129), (300, 1100, 1000), (1000, 130, 2048), (2048, 512, 2048), (4100, 200, 4000),
+EXACT = [(1, 4096, 48), (15, 200, 4000), (25, 1500, 1000), (32, 9000, 20), (12, 8200, 8192), (6, 8200, 8192), (40, 16384, 33), (64, 640, 130), (65, 16384, 64), (129, 4097, 129), (300, 1100, 1000), (1000, 130, 2048), (2048, 512, 2048), (4100, 200, 4000),
          (8200, 129, 1600), (6000, 2000, 256)]
 
 
@@ -150,7 +150,7 @@ def test_integers_are_exact(dtype, t, n, m):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("t", [3, 70])
+@pytest.mark.parametrize("t", [3, 20, 70])
 def test_powers_of_blocks_are_taken_where_they_belong(dtype, t):
     """Blocks of very different size, of tokens and of the weight: each output sees them all."""
     T, g, n, m = TYPES[dtype], gen(t), 1300, 300
@@ -166,7 +166,7 @@ def test_powers_of_blocks_are_taken_where_they_belong(dtype, t):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("t", [4, 150])
+@pytest.mark.parametrize("t", [4, 20, 150])
 def test_infinities_and_nan(dtype, t):
     T, g = TYPES[dtype], gen(t)
     x, w = activations(g, t, 200, T), weight(g, 150, 200)
@@ -194,7 +194,7 @@ def test_infinities_and_nan(dtype, t):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("t", [5, 90])
+@pytest.mark.parametrize("t", [5, 20, 90])
 def test_views_with_other_strides(dtype, t):
     T, g, n, m = TYPES[dtype], gen(t), 131, 70
     h = ctx().rsvd_f8_weight(weight(g, m, n))

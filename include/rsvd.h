@@ -386,8 +386,8 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
  * matrices may have any leading dimension and the alignment of their elements.  A
  * matrix lies as the products read it if it is 16-bit, n is a multiple of 8, its rows
  * start at 16-byte aligned addresses and its leading dimension is at most 2^22;
- * otherwise it is copied to the workspace on the way (more than 32 tokens, gradients; up to
- * 64 tokens of fp32 need none either).
+ * otherwise it is copied to the workspace on the way (not for the forward product of a few
+ * tokens, which reads everything as it lies and needs no bytes: at most 32 of 16-bit numbers, 64 of fp32).
  * gelu is x (1 + erf(x / sqrt 2)) / 2, gelu_tanh its usual approximation. */
 typedef enum { RSVD_ACT_SILU = 0, RSVD_ACT_GELU = 1, RSVD_ACT_GELU_TANH = 2, RSVD_ACT_RELU = 3 } rsvd_act;
 

@@ -86,8 +86,17 @@ PROTOTYPES = {
 }
 X_BF16, X_F16, X_F32 = 0, 1, 2
 ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
-# by type, tokens up to which these products need no workspace, and of 8-bit floats (up to 16) tokens times inputs times outputs, 4096 of them at least
-GATED_FEW, F8_FEW = (32, 32, 64), (1 << 29, 1 << 29, 3 << 26)
+
+
+# forward products of so few tokens need no workspace
+def _gated_few(xt, tokens, n, m):
+    if xt == X_F32:
+        return tokens <= (64 if m >= 2048 else 16)
+    return tokens <= 20 and tokens * n <= 196608 if m >= 8192 else tokens <= 32 and tokens * n <= 98304
+
+
+def _f8_few(xt, tokens, n, m):
+    return tokens <= 16 and tokens * n * max(m, 4096) <= (3 << 26 if xt == X_F32 else 1 << 29)
 
 
 def load_library():
@@ -709,7 +718,7 @@ class Rsvd:
         ldx, ldw, stream = _ld(X), _ld(W), self._raw_stream()
         if workspace is not None:
             ws = self._given(workspace)
-        elif tokens <= GATED_FEW[xt]:
+        elif _gated_few(xt, tokens, n, m):
             ws = (None, 0)
         else:
             ws = self._layer_ws(stream, "rsvd_gated_product_bytes", (xt, tokens, n, m, self._lies(X, ldx) + 2 * self._lies(W, ldw)))
@@ -772,7 +781,7 @@ class Rsvd:
         stream = self._raw_stream()
         if workspace is not None:
             ws = self._given(workspace)
-        elif tokens <= 16 and tokens * n * max(m, 4096) <= F8_FEW[xt]:
+        elif _f8_few(xt, tokens, n, m):
             ws = (None, 0)
         else:
             ws = self._layer_ws(stream, name + "_bytes", (xt, tokens, weight.n, weight.m))

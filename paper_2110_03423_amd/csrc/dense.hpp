@@ -75,9 +75,13 @@ hipError_t dense_init_device(rsvd_ctx *ctx);
 
 // ---------------------------------------------------------------- gated.hip
 hipError_t zero_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, void *C, int64_t ldc);
-// The forward product of up to so many tokens: the large products need to read a weight once, too, and those of 16-bit numbers are faster from 33 on (33 tokens, 4096 -> 8192: 37 and
-// 33 us); fp32 weights would be laid out before (65 tokens: 254 us, 64: 165).
-inline int64_t gated_few(rsvd_xtype type) { return type == RSVD_X_F32 ? 64 : 32; }
+// Whether a few tokens go by the weight as it lies.  In tiles a weight is read once, too; every workgroup of sixteen outputs reads all tokens, and few outputs leave CUs without one.
+// bf16 4096 -> 4096 32 tokens 18.6 us (33 in tiles: 19.3), 4096 -> 8192 17 tokens 34.2, 32: 40.0 (35.2), 8192 -> 2048 8 tokens 22.4, 32: 33.0 (19.0), 8192 -> 8192 16
+// tokens 60.7 (70.6), 24: 69.9 (69.9).  fp32 weights would be laid
+// out before: 4096 -> 8192 64 tokens 166 (65 in tiles: 256), 1024 -> 1024 17 tokens 21, 64: 36 (22).
+inline bool gated_few(rsvd_xtype type, int64_t tokens, int64_t n, int64_t m) {
+  return type == RSVD_X_F32 ? tokens <= (m >= 2048 ? 64 : 16) : m >= 8192 ? tokens <= 20 && tokens * n <= 3 << 16 : tokens <= 32 && tokens * n <= 3 << 15;
+}
 struct GatedFewDesc {
   rsvd_xtype type; int64_t tokens, n, m;
   const void *X; int64_t ldx;

@@ -97,7 +97,7 @@ template <int XT> static void gated_few_run(hipStream_t s, const GatedFewParams 
 }
 
 hipError_t gated_few_launch(rsvd_ctx *, hipStream_t s, const GatedFewDesc &d) {
-  if (d.tokens < 1 || d.tokens > gated_few(d.type)) return hipErrorInvalidValue;
+  if (d.tokens < 1 || d.tokens > (d.type == RSVD_X_F32 ? 64 : 32)) return hipErrorInvalidValue;
   const GatedFewParams P = {(const char *)d.X, (const char *)d.W, d.ldx, d.ldw, d.tokens, d.n, d.m, (int)ceil_div(d.n, 32), d.out};
   const dim3 grid((unsigned)ceil_div(d.m, 16));
   const bool wide = P.steps > 32;

@@ -44,7 +44,7 @@ def test_gated_product_checks_every_argument(plan):
     assert call(n=0) == -6 and call(m=0) == -7 and call(X=NULL) == -8 and call(X=ODD) == -8 and call(type=X_F32, X=HALF) == -8
     assert call(ldx=71) == -9 and call(W=NULL) == -10 and call(W=ODD) == -10 and call(ldw=71) == -11 and call(H=NULL) == -12 and call(ldh=49) == -13
     assert call(kept=ODD) == -14 and call(ldk=99) == -15 and call(kept=NULL, ldk=0) == ERR_NO_DEVICE
-    assert call(ws=NULL, bytes=0, tokens=16) == ERR_NO_DEVICE
+    assert call(ws=NULL, bytes=0, tokens=32) == ERR_NO_DEVICE
     # a matrix that does not lie as the products read it needs room
     both, neither = (bytes_of(plan, "rsvd_gated_product_bytes", X_BF16, 100, 72, 50, lie) for lie in (3, 0))
     assert neither >= both + 2 * 72 * (100 + 100)
@@ -57,15 +57,20 @@ def test_gated_product_checks_every_argument(plan):
 
 
 def test_the_binding_knows_how_many_tokens_need_no_workspace(plan):
+    few = {"rsvd_gated_product_bytes": 0, "rsvd_f8_product_bytes": 0, "rsvd_f8_product_grad_bytes": 0}
     for xt in (X_BF16, X_F16, X_F32):
-        few = binding.GATED_FEW[xt]
-        assert bytes_of(plan, "rsvd_gated_product_bytes", xt, few, 100, 200, 0) == 0 and bytes_of(plan, "rsvd_gated_product_bytes", xt, few + 1, 100, 200, 0) > 0
-        n = binding.F8_FEW[xt] // (16 * 4096)
-        for name, turned in (("rsvd_f8_product_bytes", False), ("rsvd_f8_product_grad_bytes", True)):
-            for rows in (4096, 50):
-                small, large = ((rows, n), (rows, n + 1)) if turned else ((n, rows), (n + 1, rows))
-                assert bytes_of(plan, name, xt, 16, *small) == 0 and bytes_of(plan, name, xt, 17, *small) > 0
-                assert bytes_of(plan, name, xt, 16, *large) > 0 and bytes_of(plan, name, xt, 8, *large) == 0
+        for tokens in (1, 2, 5, 8, 15, 16, 17, 20, 21, 31, 32, 33, 63, 64, 65):
+            for n in (1, 100, 3000, 4096, 6144, 6145, 8192, 12288, 49153, 131072):
+                for m in (1, 100, 2047, 2048, 4096, 5000, 8191, 8192, 16384, 131072):
+                    none = binding._gated_few(xt, tokens, n, m)
+                    # (lie = 0: whatever is not read as it lies has to be laid out)
+                    assert (bytes_of(plan, "rsvd_gated_product_bytes", xt, tokens, n, m, 0) == 0) == none
+                    few["rsvd_gated_product_bytes"] += none
+                    for name, inputs, outputs in (("rsvd_f8_product_bytes", n, m), ("rsvd_f8_product_grad_bytes", m, n)):
+                        none = binding._f8_few(xt, tokens, inputs, outputs)
+                        assert (bytes_of(plan, name, xt, tokens, n, m) == 0) == none
+                        few[name] += none
+    assert all(few.values())
 
 
 def test_gated_gradient_checks_every_argument(plan):

@@ -88,7 +88,7 @@ X_BF16, X_F16, X_F32 = 0, 1, 2
 ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
 
 
-# forward products of so few tokens need no workspace
+# forward products of so few tokens need no workspace, however their operands lie
 def _gated_few(xt, tokens, n, m):
     if xt == X_F32:
         return tokens <= (64 if m >= 2048 else 16)

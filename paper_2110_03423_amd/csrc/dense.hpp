@@ -79,8 +79,10 @@ hipError_t zero_launch(hipStream_t s, rsvd_xtype type, int64_t rows, int64_t n, 
 // bf16 4096 -> 4096 32 tokens 18.6 us (33 in tiles: 19.3), 4096 -> 8192 17 tokens 34.2, 32: 40.0 (35.2), 8192 -> 2048 8 tokens 22.4, 32: 33.0 (19.0), 8192 -> 8192 16
 // tokens 60.7 (70.6), 24: 69.9 (69.9).  fp32 weights would be laid
 // out before: 4096 -> 8192 64 tokens 166 (65 in tiles: 256), 1024 -> 1024 17 tokens 21, 64: 36 (22).
-inline bool gated_few(rsvd_xtype type, int64_t tokens, int64_t n, int64_t m) {
-  return type == RSVD_X_F32 ? tokens <= (m >= 2048 ? 64 : 16) : m >= 8192 ? tokens <= 20 && tokens * n <= 3 << 16 : tokens <= 32 && tokens * n <= 3 << 15;
+inline bool gated_few(rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, bool w_lies) {
+  if (type == RSVD_X_F32) return tokens <= (m >= 2048 ? 64 : 16);
+  if (!w_lies && m >= 4096) return tokens <= 32;       // (it would be laid out before)
+  return m >= 8192 ? tokens <= 20 && tokens * n <= 3 << 16 : tokens <= 32 && tokens * n <= 3 << 15;
 }
 struct GatedFewDesc {
   rsvd_xtype type; int64_t tokens, n, m;

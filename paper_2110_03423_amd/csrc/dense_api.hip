@@ -303,7 +303,7 @@ int rsvd_gated_product_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int
   if (bytes == nullptr) return -7;
   if (!sizes_supported(tokens, n, m)) return RSVD_ERR_UNSUPPORTED;
   const bool can = type != RSVD_X_F32 && n % 8 == 0;
-  *bytes = gated_few(type, tokens, n, m) ? 0 : gated_layout(ctx, type, tokens, n, m, can && (lie & 1), can && (lie & 2), false, false).total;
+  *bytes = gated_few(type, tokens, n, m, can && (lie & 2)) ? 0 : gated_layout(ctx, type, tokens, n, m, can && (lie & 1), can && (lie & 2), false, false).total;
   return RSVD_OK;
 }
 
@@ -329,7 +329,7 @@ int rsvd_gated_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_act ac
   const Span x_span = span(X, tokens, n, ldx, es), w_span = span(W, 2 * m, n, ldw, es), h_span = span(H, tokens, m, ldh, es);
   if (overlap(h_span, {x_span, w_span})) return -12;
   if (overlap(span(kept, tokens, 2 * m, ldk, es), {x_span, w_span, h_span})) return -14;
-  const bool few = gated_few(type, tokens, n, m), x_lies = laid_out(type, n, X, ldx), w_lies = laid_out(type, n, W, ldw);
+  const bool x_lies = laid_out(type, n, X, ldx), w_lies = laid_out(type, n, W, ldw), few = gated_few(type, tokens, n, m, w_lies);
   const GatedLayout L = few ? GatedLayout{} : gated_layout(ctx, type, tokens, n, m, x_lies, w_lies, false, false);
   if (L.total > 0 && (workspace == nullptr || ((uintptr_t)workspace & 255) != 0)) return -16;
   if (workspace_bytes < L.total) return -17;

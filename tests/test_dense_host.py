@@ -63,8 +63,10 @@ def test_the_binding_knows_how_many_tokens_need_no_workspace(plan):
             for n in (1, 100, 3000, 4096, 6144, 6145, 8192, 12288, 49153, 131072):
                 for m in (1, 100, 2047, 2048, 4096, 5000, 8191, 8192, 16384, 131072):
                     none = binding._gated_few(xt, tokens, n, m)
-                    # (lie = 0: whatever is not read as it lies has to be laid out)
-                    assert (bytes_of(plan, "rsvd_gated_product_bytes", xt, tokens, n, m, 0) == 0) == none
+                    # (lie = 2: a weight that lies as it is read, tokens that do not and would have to be laid out)
+                    assert none <= (bytes_of(plan, "rsvd_gated_product_bytes", xt, tokens, n, m, 0) == 0)
+                    if xt == X_F32 or n % 8 == 0:
+                        assert none == (bytes_of(plan, "rsvd_gated_product_bytes", xt, tokens, n, m, 2) == 0)
                     few["rsvd_gated_product_bytes"] += none
                     for name, inputs, outputs in (("rsvd_f8_product_bytes", n, m), ("rsvd_f8_product_grad_bytes", m, n)):
                         none = binding._f8_few(xt, tokens, inputs, outputs)

@@ -56,6 +56,7 @@ struct DenseDesc {
   const void *A = nullptr; int64_t lda = 0, a_plane = 0, a_batch = 0;
   const void *B = nullptr; int64_t ldb = 0, b_plane = 0, b_batch = 0;
   int planes = 1;                          // of both
+  bool b_wide = false;                     // B is fp32 numbers, rows of n at any address of a number (dense_kn_launch, where dense_takes_wide)
   // 8-bit floats: powers, row (index >> shift), a byte for 128 k; rows are a multiple of 4 bytes from a 4-byte aligned address
   const uint8_t *a_pow = nullptr, *b_pow = nullptr; int64_t ld_apow = 0, ld_bpow = 0; int a_shift = 0, b_shift = 0;
   LinearOut out;
@@ -71,6 +72,8 @@ size_t dense_partial_bytes(const rsvd_ctx *ctx, const DenseDesc &d);
 hipError_t dense_nt_launch(rsvd_ctx *ctx, hipStream_t s, const DenseDesc &d);
 // B with rows of n (K x N); A with rows of k, or with rows of m (a_krows: K x M).  Rows as above; zeros from k = K to the next multiple of 8 in A.
 hipError_t dense_kn_launch(rsvd_ctx *ctx, hipStream_t s, const DenseDesc &d, bool a_krows);
+// Whether small tiles will be chosen, which make three bf16 numbers of fp32 ones on the way.
+bool dense_takes_wide(const rsvd_ctx *ctx, const DenseDesc &d);
 hipError_t dense_init_device(rsvd_ctx *ctx);
 
 // ---------------------------------------------------------------- gated.hip

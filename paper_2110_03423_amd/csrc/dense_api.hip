@@ -430,12 +430,18 @@ int rsvd_gated_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_a
   o.kept = (void *)kept; o.ldk = ldk;
   o.dH = dH; o.lddh = lddh;
   o.D = (uint16_t *)(ws + L.D); o.ldD = width_of(2 * m); o.plane = D.plane;
-  if (!x_lies || !w_lies || !recompute) {
-    if (!x_lies) x = in_planes(ws + L.x, tokens, width);
-    if (!w_lies) w = in_planes(ws + L.w, 2 * m, width);
+  // (fp32 operands of small tiles are read as they lie)
+  const bool x_wide = type == RSVD_X_F32 && !recompute && dW != nullptr && ldx <= kMaxLd / 4 && dense_takes_wide(ctx, slope_w_desc(type, tokens, n, m));
+  const bool w_wide = type == RSVD_X_F32 && !recompute && dX != nullptr && ldw <= kMaxLd / 4 && dense_takes_wide(ctx, slope_x_desc(type, tokens, n, m));
+  const bool lay_x = !x_lies && !x_wide, lay_w = !w_lies && !w_wide;
+  if (x_wide) x = {X, ldx * 4, 0};
+  if (w_wide) w = {W, ldw * 4, 0};
+  if (lay_x || lay_w || !recompute) {
+    if (lay_x) x = in_planes(ws + L.x, tokens, width);
+    if (lay_w) w = in_planes(ws + L.w, 2 * m, width);
     ProfScope ps(ctx, s, PK_SMALL);
-    RSVD_TRY(lay_out_launch(s, type, n, width, {X, ldx, x_lies ? 0 : tokens, (uint16_t *)(ws + L.x), x.plane},
-                            {W, ldw, w_lies ? 0 : 2 * m, (uint16_t *)(ws + L.w), w.plane}, recompute ? 0 : tokens, m, o), "operands of the gated gradient");
+    RSVD_TRY(lay_out_launch(s, type, n, width, {X, ldx, lay_x ? tokens : 0, (uint16_t *)(ws + L.x), x.plane},
+                            {W, ldw, lay_w ? 2 * m : 0, (uint16_t *)(ws + L.w), w.plane}, recompute ? 0 : tokens, m, o), "operands of the gated gradient");
   }
   float *partial = (float *)(ws + L.partial);
   if (recompute) {
@@ -451,7 +457,7 @@ int rsvd_gated_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_a
   if (dX != nullptr) {
     DenseDesc d = slope_x_desc(type, tokens, n, m);
     d.A = D.p; d.lda = D.ld; d.a_plane = D.plane;
-    d.B = w.p; d.ldb = w.ld; d.b_plane = w.plane;
+    d.B = w.p; d.ldb = w.ld; d.b_plane = w.plane; d.b_wide = w_wide;
     d.out.C = dX; d.out.ldc = lddx; d.out.type = type;
     d.partial = partial; d.partial_bytes = L.partial_bytes;
     RSVD_TRY(dense_kn_launch(ctx, s, d, false), "gradient of tokens");
@@ -459,7 +465,7 @@ int rsvd_gated_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_a
   if (dW != nullptr) {
     DenseDesc d = slope_w_desc(type, tokens, n, m);
     d.A = D.p; d.lda = D.ld; d.a_plane = D.plane;
-    d.B = x.p; d.ldb = x.ld; d.b_plane = x.plane;
+    d.B = x.p; d.ldb = x.ld; d.b_plane = x.plane; d.b_wide = x_wide;
     d.out.C = dW; d.out.ldc = lddw; d.out.type = wtype; d.out.accumulate = accumulate;
     d.partial = partial; d.partial_bytes = L.partial_bytes;
     RSVD_TRY(dense_kn_launch(ctx, s, d, true), "gradient of a weight");

@@ -5,7 +5,7 @@
 // from memory to registers and from there to LDS, among the matrix instructions of the tile before.
 //
 // Measured: bf16 8192 x 16384 x 4096 829 us (1.33 PFLOP/s, matrix pipe busy 69 % at 1.84 GHz: power; the library's product in this order 1.25), with rows of m 888 us (1.24; library 1.11).
-// fp32 301 x 2820 x 2999 in tiles of 64 with all planes at once 47.3 us, 2820 x 301 x 2999 in tiles of 128 45.4.
+// fp32 301 x 2820 x 2999 in tiles of 64 with all planes at once 47.3 us (fp32 numbers of B as they lie 55.3, without the 13 that laying them out takes), 2820 x 301 x 2999 in tiles of 128 45.4.
 #pragma once
 
 #include <type_traits>
@@ -20,10 +20,74 @@ template <int PL, int BM, int BN> struct DenseKnCfg {
   static constexpr size_t lds = 2 * (size_t)STAGE;      // (more than the wavefronts need in the end)
 };
 
+// Rows of k of B that are fp32 numbers as they lie, for tiles of 64: eight numbers of a row a thread, which become three bf16 numbers each on the way to LDS.  A piece that ends
+// behind the last column is read further to the left, and its numbers moved (at least four columns).
+template <int NT, int DEPTH> struct WideStaged {
+  static_assert(NT == 512, "a piece a thread");
+  u32x4 reg[DEPTH][2];
+  uint32_t off[2];
+  int moved, place;
+  // n0: the tile's first column; columns: how many there are
+  __device__ __forceinline__ void init(int64_t ld, int64_t n0, int64_t columns, int tid) {
+    const int row = tid >> 3, pos = tid & 7;
+    place = row * 128 + (krow_piece<64>(pos >> 1, row) << 5) + ((pos & 1) << 4);
+    moved = 0;
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const int64_t first = n0 + 8 * pos + 4 * q;
+      const int64_t from = first + 4 <= columns ? first : first < columns ? columns - 4 : 0;
+      if (first + 4 > columns && first < columns) moved |= (int)(first - from) << (4 * q);
+      off[q] = (uint32_t)row * (uint32_t)ld + (uint32_t)from * 4u;
+      asm volatile("" : "+v"(off[q]));
+    }
+  }
+  // base: the tile's first row; rows that do not exist are read beyond the end of the buffer, which gives zeros
+  __device__ __forceinline__ void load(int set, const char *base, int64_t ld, int k_left) {
+    const __amdgpu_buffer_rsrc_t all = __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, (int)(k_left * (uint32_t)ld), 0x00027000);
+#pragma unroll
+    for (int q = 0; q < 2; ++q) reg[set][q] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(all, off[q], 0, 0));
+  }
+  // whole: every column of the tile exists
+  __device__ __forceinline__ void write(int set, char *lds, int plane, bool whole) const {
+    Raw8<RSVD_X_F32> v = {{reg[set][0], reg[set][1]}};
+    if (!whole) {
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const int by = moved >> (4 * q) & 3;
+        u32x4 w = v.w[q];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = by & 1 ? (e < 3 ? w[e < 3 ? e + 1 : 3] : 0u) : w[e];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = by & 2 ? (e < 2 ? w[e < 2 ? e + 2 : 3] : 0u) : w[e];
+        v.w[q] = w;
+      }
+    }
+    u32x4 x[3];
+    unsigned top = 0u;                                   // (one question for all of what bf16 numbers round to infinity, or that is it)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) top = max(top, v.w[e >> 2][e & 3] << 1);
+    if (top < 0x7f7f8000u << 1) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        unsigned p[3];
+        bf16_parts2<3, false>(__uint_as_float(v.w[e >> 1][2 * (e & 1)]), __uint_as_float(v.w[e >> 1][2 * (e & 1) + 1]), p);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) x[q][e] = p[q];
+      }
+    } else {
+      split_operand<RSVD_X_F32>(v, x);
+    }
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *reinterpret_cast<u32x4 *>(lds + p * plane + place) = x[p];
+  }
+};
+
 // PL planes of both operands are multiplied while a k-tile of all is in LDS; 1: the products of planes are further k.
 // KG: groups of wavefronts that have the whole tile and a half of every k-tile (2: two wavefronts a SIMD, one waits while the other multiplies), or all of it (1).
-template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN, int KG>
+// WIDE: B is fp32 numbers as they lie.
+template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN, int KG, bool WIDE>
 __global__ __launch_bounds__(64 * WGM * WGN * KG, KG == 1 ? 2 : PL == 3 ? 2 : 4) void dense_kn_kernel(const DenseParams P) {
+  static_assert(!WIDE || (KIND == DK_BF16 && PL == 3 && KG == 2), "three bf16 numbers of each");
   static_assert(KG == 1 || (KG == 2 && BM == 64 && PL > 1), "halves of the k-tiles of small tiles of planes");
   constexpr int NT = 64 * WGM * WGN * KG, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, DEPTH = DenseKnCfg<PL, BM, BN>::DEPTH;
   constexpr int STAGE = DenseKnCfg<PL, BM, BN>::STAGE, PLANE = DenseKnCfg<PL, BM, BN>::PLANE, B_LDS = DenseKnCfg<PL, BM, BN>::A;
@@ -46,7 +110,7 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, KG == 1 ? 2 : PL == 3 ? 2 : 4)
 
   // the k-tile that is loaded next: its part of k, its place there, and how many k of it exist
   int next_seg = __builtin_amdgcn_readfirstlane(kt_begin / P.ktiles), next_kt = __builtin_amdgcn_readfirstlane(kt_begin - next_seg * P.ktiles);
-  const char *const a_first = P.A + batch * P.a_batch + (A_KROWS ? m0 * 2 : m0 * P.lda), *const b_first = P.B + batch * P.b_batch + n0 * 2;
+  const char *const a_first = P.A + batch * P.a_batch + (A_KROWS ? m0 * 2 : m0 * P.lda), *const b_first = P.B + batch * P.b_batch + (WIDE ? 0 : n0 * 2);
   const char *a_now, *b_now;
   int left;
   auto point = [&]() RSVD_INLINE {
@@ -68,19 +132,31 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, KG == 1 ? 2 : PL == 3 ? 2 : 4)
     left = next_kt == P.ktiles - 1 ? last_left : kKnK;
   };
   Staged<NT, BM, A_KROWS, DEPTH * PL> sa;
-  Staged<NT, BN, true, DEPTH * PL> sb;
+  std::conditional_t<WIDE, WideStaged<NT, DEPTH>, Staged<NT, BN, true, DEPTH * PL>> sb;
   sa.init(P.lda, P.M - m0, tid);
-  sb.init(P.ldb, P.N - n0, tid);
-  constexpr int NA = decltype(sa)::N, EACH = NA + decltype(sb)::N, PIECES = PL * EACH;
+  if constexpr (WIDE) sb.init(P.ldb, n0, P.N, tid);
+  else sb.init(P.ldb, P.N - n0, tid);
+  constexpr int NA = decltype(sa)::N, NB = Staged<NT, BN, true, DEPTH * PL>::N, EACH = WIDE ? NA : NA + NB, PIECES = PL * EACH + (WIDE ? 1 : 0);
+  const bool b_whole = n0 + BN <= P.N;
   auto load = [&](int set, int piece) RSVD_INLINE {
     const int q = piece / EACH, p = piece % EACH;
+    if constexpr (WIDE)
+      if (piece == PL * NA) {
+        sb.load(set, b_now, P.ldb, left);
+        return;
+      }
     if (p < NA) sa.load(PL * set + q, p, a_now + q * P.a_plane, P.lda, left);
-    else sb.load(PL * set + q, p - NA, b_now + q * P.b_plane, P.ldb, left);
+    else if constexpr (!WIDE) sb.load(PL * set + q, p - NA, b_now + q * P.b_plane, P.ldb, left);
   };
   auto write = [&](int set, int piece, int buf) RSVD_INLINE {
     const int q = piece / EACH, p = piece % EACH;
+    if constexpr (WIDE)
+      if (piece == PL * NA) {
+        sb.write(set, dense_lds + buf * STAGE + B_LDS, PLANE, b_whole);
+        return;
+      }
     if (p < NA) sa.write(PL * set + q, p, dense_lds + buf * STAGE + q * PLANE);
-    else sb.write(PL * set + q, p - NA, dense_lds + buf * STAGE + q * PLANE + B_LDS);
+    else if constexpr (!WIDE) sb.write(PL * set + q, p - NA, dense_lds + buf * STAGE + q * PLANE + B_LDS);
   };
 
   // ---- operands of this lane
@@ -215,13 +291,15 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, KG == 1 ? 2 : PL == 3 ? 2 : 4)
                              reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
 }
 
-template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN, int KG = 1> hipError_t dense_kn_run(hipStream_t s, const DenseParams &P) {
-  hipLaunchKernelGGL((dense_kn_kernel<KIND, A_KROWS, PL, BM, BN, WGM, WGN, KG>), dim3(dense_groups(P)), dim3(64 * WGM * WGN * KG), (DenseKnCfg<PL, BM, BN>::lds), s, P);
+template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN, int KG = 1, bool WIDE = false> hipError_t dense_kn_run(hipStream_t s, const DenseParams &P) {
+  hipLaunchKernelGGL((dense_kn_kernel<KIND, A_KROWS, PL, BM, BN, WGM, WGN, KG, WIDE>), dim3(dense_groups(P)), dim3(64 * WGM * WGN * KG), (DenseKnCfg<PL, BM, BN>::lds), s, P);
   return hipGetLastError();
 }
 // The planes that small tiles of a kind take at once.
 template <int KIND> constexpr int dense_kn_planes() { return KIND == DK_BF16 ? 3 : 2; }
-template <int KIND, bool A_KROWS> hipError_t dense_kn_tile(hipStream_t s, const DenseParams &P, int b) {
+template <int KIND, bool A_KROWS> hipError_t dense_kn_tile(hipStream_t s, const DenseParams &P, int b, bool wide) {
+  if constexpr (KIND == DK_BF16)
+    if (wide) return b == 64 && P.segs.count == 6 ? dense_kn_run<KIND, A_KROWS, 3, 64, 64, 2, 2, 2, true>(s, P) : hipErrorInvalidValue;
   if (b == 256) return dense_kn_run<KIND, A_KROWS, 1, 256, 256, 2, 4>(s, P);
   if (b == 128) return dense_kn_run<KIND, A_KROWS, 1, 128, 128, 2, 2>(s, P);
   if (P.segs.count > 1) return dense_kn_run<KIND, A_KROWS, dense_kn_planes<KIND>(), 64, 64, 2, 2, 2>(s, P);
@@ -229,14 +307,19 @@ template <int KIND, bool A_KROWS> hipError_t dense_kn_tile(hipStream_t s, const 
 }
 template <int KIND, bool A_KROWS> hipError_t dense_kn_init() {
   constexpr int PL = dense_kn_planes<KIND>();
-  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, 1, 256, 256, 2, 4, 1>), hipFuncAttributeMaxDynamicSharedMemorySize,
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, 1, 256, 256, 2, 4, 1, false>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                            (int)DenseKnCfg<1, 256, 256>::lds);
   if (e != hipSuccess) return e;
-  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, PL, 64, 64, 2, 2, 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
+  if constexpr (KIND == DK_BF16) {
+    const hipError_t e2 = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, PL, 64, 64, 2, 2, 2, true>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                              (int)DenseKnCfg<PL, 64, 64>::lds);
+    if (e2 != hipSuccess) return e2;
+  }
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_kn_kernel<KIND, A_KROWS, PL, 64, 64, 2, 2, 2, false>), hipFuncAttributeMaxDynamicSharedMemorySize,
                              (int)DenseKnCfg<PL, 64, 64>::lds);
 }
 #define DENSE_KN(KIND, A_KROWS)                                                                      \
-  template hipError_t dense_kn_tile<KIND, A_KROWS>(hipStream_t s, const DenseParams &P, int b);     \
+  template hipError_t dense_kn_tile<KIND, A_KROWS>(hipStream_t s, const DenseParams &P, int b, bool wide);     \
   template hipError_t dense_kn_init<KIND, A_KROWS>();
 
 }  // namespace rsvd

@@ -108,7 +108,7 @@ hipError_t gated_few_launch(rsvd_ctx *, hipStream_t s, const GatedFewDesc &d) {
 }
 
 // ---------------------------------------------------------------- operands
-// Gradients of gate and up from the kept products, and matrices as the products want them; memory is the bound (301 x 2999 -> 1410 in fp32: 106 MB in 17.6 us).  One launch: workgroups of the one, then of the others.
+// Gradients of gate and up from the kept products, and matrices as the products want them; memory is the bound (301 x 2999 -> 1410 in fp32 with its weight: 106 MB in 17.6 us).  One launch: workgroups of the one, then of the others.
 template <int TYPE> __device__ __forceinline__ void slope_group(const GatedOut &O, int64_t tokens, int64_t m, int64_t group) {
   int64_t t[1], n[1];
   int place;

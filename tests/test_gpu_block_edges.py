@@ -7,7 +7,7 @@ import torch
 
 from gpu_util import ctx, say
 from test_gpu_f8 import weight_values
-from test_gpu_gated import ACTS, E, FLOOR, UNIT, act64, block, integers, rounded, share
+from test_gpu_gated import ACTS, E, FLOOR, UNIT, act64, block, integers, rounded, share, slopes64
 from test_gpu_layer8 import BF16, F16, F32, TYPES, gen
 from test_gpu_orthogonalize import iterated, momentum
 
@@ -165,3 +165,29 @@ def test_what_is_not_finite_stays_in_its_rows_of_large_tiles(dtype, t, n, m):
                                (lambda v: ctx().rsvd_f8_product(v, f), x, y), (lambda v: ctx().rsvd_f8_product_grad(v, f), dh, d)):
         want, got = run(clean), run(broken)
         assert torch.equal(got[keep], want[keep]) and not got[bad].isfinite().any()
+
+
+@pytest.mark.parametrize("t,n,m", [(100, 67, 20), (700, 70, 330)])
+def test_large_fp32_numbers_and_infinities_stay_in_their_columns(t, n, m):
+    """Numbers above 3.39e38 round to infinity in bf16: their parts are taken otherwise.  (Bound: what D is off by, times the large number - of a gate of -10 its
+    activation is good to 1e-4 only -, 2^-22 of that term for its product and the output's rounding, and the others beside it.)"""
+    g = gen(t)
+    x, w, dh = block(g, t, n, m, F32)
+    kept = ctx().rsvd_gated_product(x, w, keep=True)[1]
+    dx, dw = ctx().rsvd_gated_product_grad(dh, x, w, kept=kept)
+    for value in (math.inf, -math.inf, math.nan, 3.4e38):
+        say("large", t, n, m, value)
+        v, y = w.clone(), x.clone()
+        v[3, 5], y[9, n - 1] = value, value
+        other, _ = ctx().rsvd_gated_product_grad(dh, x, v, kept=kept)
+        _, again = ctx().rsvd_gated_product_grad(dh, y, w, kept=kept)
+        keep = [c for c in range(n) if c != 5]
+        assert torch.equal(other[:, keep], dx[:, keep]) and torch.equal(again[:, :n - 1], dw[:, :n - 1])
+        if not math.isfinite(value):
+            assert not other[:, 5].isfinite().any() and not again[:, n - 1].isfinite().any()
+            continue
+        none = torch.zeros(t, m, device=DEV, dtype=torch.float64)
+        d, ed = slopes64(kept[:, :m].double(), kept[:, m:].double(), none, none, dh, "silu")
+        for got, one, off, rest in ((other[:, 5], d[:, 3] * v[3, 5].double(), ed[:, 3], d.abs() @ w.double().abs()[:, 5]),
+                                    (again[:, n - 1], d[9] * y[9, n - 1].double(), ed[9], d.abs().t() @ x.double().abs()[:, n - 1])):
+            assert bool(((got.double() - one).abs() <= 2.0 ** -22 * one.abs() + off * value + 2 * rest).all())

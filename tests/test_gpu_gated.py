@@ -154,7 +154,7 @@ def rounded(v, dtype):
 
 
 # every tile and number of ranges that the choice knows, with last k-tiles of one to eight pieces, and operands that are laid out first
-EXACT = [(1, 4096, 33), (30, 4001, 4096), (64, 100, 2100), (48, 72, 2049), (20, 5000, 64), (3, 40000, 33), (5, 20001, 50), (16, 1000, 130), (33, 40, 4000), (64, 2056, 640), (65, 8, 8), (100, 4104, 48), (129, 129, 129), (300, 1096, 1000), (1000, 136, 2048), (2048, 512, 2048),
+EXACT = [(1, 4096, 33), (9, 3, 20), (9, 4, 20), (70, 6, 33), (130, 61, 95), (77, 67, 31), (301, 999, 141), (30, 4001, 4096), (64, 100, 2100), (48, 72, 2049), (20, 5000, 64), (3, 40000, 33), (5, 20001, 50), (16, 1000, 130), (33, 40, 4000), (64, 2056, 640), (65, 8, 8), (100, 4104, 48), (129, 129, 129), (300, 1096, 1000), (1000, 136, 2048), (2048, 512, 2048),
          (4100, 200, 4000), (333, 16392, 50), (8200, 80, 1600)]
 
 

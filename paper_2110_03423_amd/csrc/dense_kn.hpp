@@ -88,7 +88,7 @@ template <int NT, int DEPTH> struct WideStaged {
 template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN, int KG, bool WIDE>
 __global__ __launch_bounds__(64 * WGM * WGN * KG, KG == 1 ? 2 : PL == 3 ? 2 : 4) void dense_kn_kernel(const DenseParams P) {
   static_assert(!WIDE || (KIND == DK_BF16 && PL == 3 && KG == 2), "three bf16 numbers of each");
-  static_assert(KG == 1 || (KG == 2 && BM == 64 && PL > 1), "halves of the k-tiles of small tiles of planes");
+  static_assert(KG == 1 || (KG == 2 && BM == 64), "halves of the k-tiles of small tiles");
   constexpr int NT = 64 * WGM * WGN * KG, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, DEPTH = DenseKnCfg<PL, BM, BN>::DEPTH;
   constexpr int STAGE = DenseKnCfg<PL, BM, BN>::STAGE, PLANE = DenseKnCfg<PL, BM, BN>::PLANE, B_LDS = DenseKnCfg<PL, BM, BN>::A;
   extern __shared__ __attribute__((aligned(16))) char dense_lds[];
@@ -263,13 +263,15 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, KG == 1 ? 2 : PL == 3 ? 2 : 4)
   float *const partial = work.partial != nullptr ? work.partial + wm0 * BN + wn0 : nullptr;
   int last_lane = lane;                                // (anew: what follows from it would be worked out before the main loop otherwise, and kept)
   asm volatile("" : "+v"(last_lane));
-  // Of groups that have halves of k, each ends with one row of blocks: its own sums and the other's, through LDS behind what the end takes.
+  // Of groups that have halves of k, each ends with one row of blocks: its own sums and the other's, through LDS (behind what the end takes, where there is room).
   // (behind the last meeting nobody reads the tiles)
   constexpr int ROWS = TM / KG;
   f32x4 sums[ROWS][TN];
   if constexpr (KG == 2) {
-    constexpr int ROOM = WGM * WGN * KG * finish_lds<TN>();
-    static_assert(TM == 2 && ROOM % 16 == 0 && ROOM + WGM * WGN * 2 * TN * 1024 <= 2 * STAGE, "a row of blocks a group");
+    constexpr int END = WGM * WGN * KG * finish_lds<TN>(), EXCHANGE = WGM * WGN * 2 * TN * 1024;
+    constexpr bool APART = END + EXCHANGE <= 2 * STAGE;
+    constexpr int ROOM = APART ? END : 0;
+    static_assert(TM == 2 && END % 16 == 0 && ROOM + EXCHANGE <= 2 * STAGE, "a row of blocks a group");
     f32x4 *const mine = reinterpret_cast<f32x4 *>(dense_lds + ROOM) + wave * TN * 64 + last_lane;
     f32x4 *const other = reinterpret_cast<f32x4 *>(dense_lds + ROOM) + (wave + (group == 0 ? WGM * WGN : -WGM * WGN)) * TN * 64 + last_lane;
 #pragma unroll
@@ -280,6 +282,7 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, KG == 1 ? 2 : PL == 3 ? 2 : 4)
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < TN; ++j) sums[0][j] += other[j * 64];
+    if constexpr (!APART) __syncthreads();
   } else {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -303,7 +306,7 @@ template <int KIND, bool A_KROWS> hipError_t dense_kn_tile(hipStream_t s, const 
   if (b == 256) return dense_kn_run<KIND, A_KROWS, 1, 256, 256, 2, 4>(s, P);
   if (b == 128) return dense_kn_run<KIND, A_KROWS, 1, 128, 128, 2, 2>(s, P);
   if (P.segs.count > 1) return dense_kn_run<KIND, A_KROWS, dense_kn_planes<KIND>(), 64, 64, 2, 2, 2>(s, P);
-  return dense_kn_run<KIND, A_KROWS, 1, 64, 64, 2, 2>(s, P);
+  return dense_kn_run<KIND, A_KROWS, 1, 64, 64, 2, 2, 2>(s, P);
 }
 template <int KIND, bool A_KROWS> hipError_t dense_kn_init() {
   constexpr int PL = dense_kn_planes<KIND>();

@@ -79,10 +79,10 @@ __device__ __forceinline__ i32x8 f8_both(const u32x4 (&p)[2]) {
 
 // PL planes of both operands are multiplied while a k-tile of all is in LDS; 1: the products of planes are further k.
 // KG: groups of wavefronts that have the whole tile and a half of every k-tile (2: two wavefronts a SIMD, one waits while the other multiplies; gated fp32
-// 384 x 2048 -> 2048 59.8 us, with one group 70.0), or all of it (1).
+// 384 x 2048 -> 2048 59.8 us, with one group 70.0; updates of 1000 x 2000 in bf16 201 and 225; but gated bf16 384 x 2048 -> 2048 16.0 and 14.8, several workgroups a CU), or all of it (1).
 template <int KIND, bool GATED, int PL, int BM, int BN, int WGM, int WGN, int KG>
 __global__ __launch_bounds__(64 * WGM * WGN * KG, BM == 256 ? 1 : KG == 1 ? 2 : PL == 3 ? 2 : 4) void dense_nt_kernel(const DenseParams P) {
-  static_assert(KG == 1 || (KG == 2 && BM == 64 && PL > 1), "halves of the k-tiles of small tiles of planes");
+  static_assert(KG == 1 || (KG == 2 && BM == 64 && KIND < DK_F8), "halves of the k-tiles of small tiles");
   constexpr int NT = 64 * WGM * WGN * KG, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16, STAGE = DenseNtCfg<KIND, PL, BM, BN>::STAGE, RING = DenseNtCfg<KIND, PL, BM, BN>::RING;
   constexpr bool CODES = KIND >= DK_F8;
   extern __shared__ __attribute__((aligned(16))) char dense_lds[];
@@ -473,15 +473,15 @@ template <int KIND, bool GATED> hipError_t dense_nt_tile(hipStream_t s, const De
   if (b == 256) return dense_nt_run<KIND, GATED, 1, 256, 256, 2, 2>(s, P);
   if (b == 128) return dense_nt_run<KIND, GATED, 1, 128, 128, 2, 2>(s, P);
   constexpr int PL = dense_nt_planes<KIND, GATED>();
-  if (P.segs.count > 1) return dense_nt_run<KIND, GATED, PL, 64, 64, 2, 2, PL == 1 ? 1 : 2>(s, P);
-  return dense_nt_run<KIND, GATED, 1, 64, 64, 2, 2>(s, P);
+  if (P.segs.count > 1) return dense_nt_run<KIND, GATED, PL, 64, 64, 2, 2, (PL > 1 ? 2 : 1)>(s, P);
+  return dense_nt_run<KIND, GATED, 1, 64, 64, 2, 2, KIND == DK_F16 && !GATED ? 2 : 1>(s, P);
 }
 template <int KIND, bool GATED> hipError_t dense_nt_init() {
   constexpr int PL = dense_nt_planes<KIND, GATED>();
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, 1, 256, 256, 2, 2, 1>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                            (int)DenseNtCfg<KIND, 1, 256, 256>::lds);
   if (e != hipSuccess || PL == 1) return e;
-  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, PL, 64, 64, 2, 2, PL == 1 ? 1 : 2>), hipFuncAttributeMaxDynamicSharedMemorySize,
+  return hipFuncSetAttribute(reinterpret_cast<const void *>(&dense_nt_kernel<KIND, GATED, PL, 64, 64, 2, 2, (PL > 1 ? 2 : 1)>), hipFuncAttributeMaxDynamicSharedMemorySize,
                              (int)DenseNtCfg<KIND, PL, 64, 64>::lds);
 }
 #define DENSE_NT(KIND, GATED)                                                                        \

@@ -14,15 +14,15 @@ static int64_t dense_tiles(const DenseDesc &d, int b) {
 }
 
 // The time of each tile and number of ranges is estimated, and the least taken.  What bounds a k-tile (128 bytes of a row) of the smaller tiles is what a CU gets out of the
-// L2 caches, 50 to 60 GB/s: 0.22 (0.3 where operands go through registers) and 0.5 us for each workgroup of 64 and 128 rows and columns on a CU, but 0.3 and 0.7 us where there are not as many as CUs; tiles of 256 take
+// L2 caches, 50 to 60 GB/s: 0.22 (0.3 where operands go through registers, 0.19 of fp16 numbers that do not) and 0.5 us for each workgroup of 64 and 128 rows and columns on a CU, but 0.3 and 0.7 us where there are not as many as CUs; tiles of 256 take
 // 1.7 us, near the rate of the matrix instructions (1.4 where CUs are idle and operands do not go through registers).  Small tiles take a k-tile of all planes at once (two 0.55 us, three 1.0; 0.9 and 0.95).  Beside that 3, 5 and
 // 8 us for each workgroup that a CU has behind another.  Tiles that fill the chip a number of times are worked out whole; of what is left k may be in ranges, for all CUs to
 // have a part: a second launch, and their sums are written and read (5 bytes / ps).  Measured for 130 products of 80 to 3000 tokens with all tiles and one to sixteen ranges: what is
 // chosen takes up to 6 % more than the best of them, fourteen times up to 17 %.
 static DenseChoice dense_choose(const rsvd_ctx *ctx, const DenseDesc &d) {
   const int products = dense_segs(d.planes).count;
-  const bool through = !d.gated && d.kind < DK_F8;      // operands through registers (nearly all such products)
-  const double small = d.planes == 3 ? 1.0 : d.planes == 2 ? 0.55 : through ? 0.3 : 0.22, alone = d.planes == 3 ? 0.95 : d.planes == 2 ? 0.9 : 0.3;
+  const bool through = d.rows_of_n;                      // operands through registers
+  const double small = d.planes == 3 ? 1.0 : d.planes == 2 ? 0.55 : through ? 0.3 : d.gated || d.kind >= DK_F8 ? 0.22 : 0.19, alone = d.planes == 3 ? 0.95 : d.planes == 2 ? 0.9 : 0.3;
   const struct { int b, at_once; double step, alone, more; } tile[3] = {{64, d.planes == 3 ? 1 : d.planes == 2 ? 2 : 3, small, alone, 3.0}, {128, 2, 0.5, 0.7, 5.0},
                                                                          {256, 1, 1.7, through ? 1.55 : 1.4, 8.0}};
   static const int ranges[9] = {1, 2, 3, 4, 6, 8, 12, 16, 24};
@@ -101,7 +101,7 @@ static bool fits(const DenseChoice &c, const DenseDesc &d) {
 
 hipError_t dense_nt_launch(rsvd_ctx *ctx, hipStream_t s, const DenseDesc &d) {
   const DenseChoice c = dense_choose(ctx, d);
-  if (!fits(c, d) || d.b_wide || (d.kind < DK_F8 && d.K % 8 != 0)) return hipErrorInvalidValue;
+  if (!fits(c, d) || d.b_wide || d.rows_of_n || (d.kind < DK_F8 && d.K % 8 != 0)) return hipErrorInvalidValue;
   const DenseParams P = dense_params(c, d);
   hipError_t e = hipErrorInvalidValue;
   if (d.kind == DK_BF16 && d.gated) e = dense_nt_tile<DK_BF16, true>(s, P, c.b);
@@ -114,7 +114,7 @@ hipError_t dense_nt_launch(rsvd_ctx *ctx, hipStream_t s, const DenseDesc &d) {
 
 hipError_t dense_kn_launch(rsvd_ctx *ctx, hipStream_t s, const DenseDesc &d, bool a_krows) {
   const DenseChoice c = dense_choose(ctx, d);
-  if (!fits(c, d) || d.kind >= DK_F8 || d.gated || (d.b_wide && d.kind != DK_BF16)) return hipErrorInvalidValue;
+  if (!fits(c, d) || !d.rows_of_n || d.kind >= DK_F8 || d.gated || (d.b_wide && d.kind != DK_BF16)) return hipErrorInvalidValue;
   const DenseParams P = dense_params(c, d);
   hipError_t e;
   if (d.kind == DK_BF16) e = a_krows ? dense_kn_tile<DK_BF16, true>(s, P, c.b, d.b_wide) : dense_kn_tile<DK_BF16, false>(s, P, c.b, d.b_wide);

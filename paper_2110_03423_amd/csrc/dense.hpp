@@ -52,6 +52,7 @@ struct GatedOut {
 struct DenseDesc {
   int kind = DK_BF16, batch = 1;
   int64_t M = 0, N = 0, K = 0;
+  bool rows_of_n = false;                  // B has rows of n: for dense_kn_launch
   bool gated = false, symmetric = false;   // symmetric (M = N): the tiles on and below the diagonal are computed, and stored twice
   const void *A = nullptr; int64_t lda = 0, a_plane = 0, a_batch = 0;
   const void *B = nullptr; int64_t ldb = 0, b_plane = 0, b_batch = 0;

@@ -107,6 +107,7 @@ DenseDesc slope_x_desc(rsvd_xtype type, int64_t tokens, int64_t n, int64_t m) {
   DenseDesc d;
   d.kind = kind_of(type); d.planes = planes_of(type);
   d.M = tokens; d.N = n; d.K = 2 * m;
+  d.rows_of_n = true;
   return d;
 }
 // dW = D^T X: k counts tokens
@@ -114,6 +115,7 @@ DenseDesc slope_w_desc(rsvd_xtype type, int64_t tokens, int64_t n, int64_t m) {
   DenseDesc d;
   d.kind = kind_of(type); d.planes = planes_of(type);
   d.M = 2 * m; d.N = n; d.K = tokens;
+  d.rows_of_n = true;
   return d;
 }
 
@@ -238,6 +240,7 @@ DenseDesc gram_desc(rsvd_xtype type, int batch, int64_t m, int64_t n) {
   d.kind = DK_F16; d.planes = iterate_planes(type); d.batch = batch;
   d.M = d.N = m <= n ? m : n;
   d.K = m <= n ? width_of(n) : m;
+  d.rows_of_n = m > n;
   d.symmetric = true;
   return d;
 }
@@ -253,6 +256,7 @@ DenseDesc apply_desc(rsvd_xtype type, int batch, int64_t m, int64_t n) {
   d.kind = DK_F16; d.planes = iterate_planes(type); d.batch = batch;
   d.M = m; d.N = n;
   d.K = m <= n ? m : width_of(n);
+  d.rows_of_n = m <= n;
   return d;
 }
 

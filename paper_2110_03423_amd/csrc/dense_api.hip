@@ -282,17 +282,44 @@ OrthogonalLayout orthogonal_layout(const rsvd_ctx *ctx, rsvd_xtype type, int bat
   return L;
 }
 
-// Whether singular values that start in [0, 1] stay where fp16 numbers times 2^13 hold them, their squares and the polynomials: followed on a grid.
-bool stays_in_range(int steps, const float *c) {
-  constexpr int POINTS = 512;
-  for (int i = 0; i <= POINTS; ++i) {
-    double x = (double)i / POINTS;
-    for (int s = 0; s < steps; ++s) {
-      const double y = x * x, p = y * (c[3 * s + 1] + y * c[3 * s + 2]);
-      if (!(fabs(p) <= 7.5)) return false;
-      x = x * (c[3 * s] + p);
-      if (!(fabs(x) <= 2.7)) return false;
+// Whether singular values that start in [0, 1] stay where fp16 numbers times 2^13 hold them, their squares and the polynomials.  What a step makes of an interval is an interval again, whose
+// ends are values at the old ones and where the derivative is zero; it is followed, not single values: between any two of those an iteration may have one that leaves.  Only what is off the diagonals of A and
+// of b A + c A^2 is held in fp16, and is at most half of what their eigenvalues spread by.
+// Every step's interval is widened by what rounding moves: `slack` of the magnitudes that are added up.  For bf16 results, whose products take 11 bits of each number, 2^-10: matrices of one
+// magnitude round all entries alike, and 2^-12 too much at the end of a range that the next steps stretch tenfold each made NaN of them.  Others keep 22 bits: 2^-18.
+bool stays_in_range(rsvd_xtype type, int steps, const float *c) {
+  const double slack = type == RSVD_X_BF16 ? 0x1p-10 : 0x1p-18;
+  double low = 0.0, high = 1.0;                          // of singular values, whose sign a step may change
+  for (int s = 0; s < steps; ++s) {
+    const double a = c[3 * s], b = c[3 * s + 1], g = c[3 * s + 2];
+    if (!isfinite(a) || !isfinite(b) || !isfinite(g)) return false;
+    auto p = [&](double y) { return y * (b + y * g); };
+    auto f = [&](double x) { return x * (a + p(x * x)); };
+    const double reach = fmax(fabs(low), fabs(high)), y_high = reach * reach, y_low = low <= 0.0 && high >= 0.0 ? 0.0 : fmin(low * low, high * high);
+    double p_low = fmin(p(y_low), p(y_high)), p_high = fmax(p(y_low), p(y_high));
+    if (g != 0.0 && -b / (2.0 * g) > y_low && -b / (2.0 * g) < y_high) {
+      p_low = fmin(p_low, p(-b / (2.0 * g)));
+      p_high = fmax(p_high, p(-b / (2.0 * g)));
     }
+    double f_low = fmin(f(low), f(high)), f_high = fmax(f(low), f(high));
+    auto turn = [&](double y) {                          // (where a + 3 b y + 5 g y^2 = 0 for y = x^2)
+      if (!(y > 0.0) || !isfinite(y)) return;
+      for (const double x : {sqrt(y), -sqrt(y)})
+        if (x > low && x < high) {
+          f_low = fmin(f_low, f(x));
+          f_high = fmax(f_high, f(x));
+        }
+    };
+    const double disc = 9.0 * b * b - 20.0 * a * g;
+    if (disc >= 0.0) {                                   // (both roots without a difference of numbers that may be near each other)
+      const double q = -0.5 * (3.0 * b + copysign(sqrt(disc), b));
+      if (g != 0.0) turn(q / (5.0 * g));
+      if (q != 0.0) turn(a / q);
+    }
+    const double moved = slack * reach * (fabs(a) + fmax(fabs(p_low), fabs(p_high)));
+    low = f_low - moved;
+    high = f_high + moved;
+    if (!(p_high - p_low <= 15.0) || !(fmax(fabs(low), fabs(high)) <= 2.7)) return false;
   }
   return true;
 }
@@ -627,7 +654,7 @@ int rsvd_orthogonalize(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int batch, 
   if (ldo < n) return -13;
   if (batch > 1 && stride_o < (m - 1) * ldo + n) return -14;
   if (!matrices_supported(batch, m, n)) return RSVD_ERR_UNSUPPORTED;
-  if (!stays_in_range(steps, coefficients)) return RSVD_ERR_UNSUPPORTED;
+  if (!stays_in_range(type, steps, coefficients)) return RSVD_ERR_UNSUPPORTED;
   const OrthogonalLayout L = orthogonal_layout(ctx, type, batch, m, n);
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0) return -15;
   if (workspace_bytes < L.total) return -16;

@@ -195,3 +195,32 @@ def test_a_weight_of_8_bit_floats_is_checked_and_laid_out():
                         (ValueError, (codes[:0], powers[:0]))):
         with pytest.raises(error):
             WeightF8(*args)
+
+
+# Each step the odd polynomial whose values on the image of [0.002, 1] under the ones before are nearest to one (a linear programme on a grid), made smaller by 1.01 for rounding.
+SCHEDULE = [(8.3434, -24.2028, 17.5950), (4.0709, -2.9692, 0.5470), (3.6778, -2.6964, 0.5166), (2.7544, -2.0139, 0.4410), (1.9734, -1.3354, 0.3690), (1.8569, -1.2138, 0.3569),
+            (1.875, -1.25, 0.375)]
+
+
+def flat(steps):
+    return (C.c_float * (3 * len(steps)))(*[v for s in steps for v in s])
+
+
+def test_coefficients_are_followed_between_the_ends_of_their_range(plan):
+    call = caller(plan, "rsvd_orthogonalize", "ctx stream type batch m n G ldg sg steps coef O ldo so ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, batch=1, m=50,
+                  n=70, G=PTR, ldg=70, sg=3500, steps=1, coef=None, O=PTR, ldo=70, so=3500, ws=PTR, bytes=1 << 40)
+    step = (3.4445, -4.775, 2.0315)
+    for xt in (X_BF16, X_F16, X_F32):
+        # start values near 0.9923, and few others, end behind 1e13 and 2.9
+        for bad in ([(2.649, -5.722, 2.047)] * 7, [(2.779, -5.08, 1.298)] * 17):
+            assert call(type=xt, steps=len(bad), coef=flat(bad)) == UNSUPPORTED
+        # entries off the diagonal of b A + c A^2 are half of what its eigenvalues spread by at most: 4.2 here, though they reach -8.3
+        assert call(type=xt, coef=flat(SCHEDULE[:1])) == ERR_NO_DEVICE
+        for good in (SCHEDULE, [step] * 64, [(1.5, -0.5, 0.0)] * 64, [(1.875, -1.25, 0.375)] * 64, [(2.0, -1.5, 0.5)] * 64, [step, (2.5, -2.0, 0.6), (1.875, -1.25, 0.375)]):
+            assert call(type=xt, steps=len(good), coef=flat(good)) == ERR_NO_DEVICE
+        # the eigenvalues' spread: b x^2 of [0, 1]
+        assert call(type=xt, coef=flat([(15.0, -14.9, 0.0)])) == UNSUPPORTED and call(type=xt, coef=flat([(0.0, 0.0, float("inf"))])) == UNSUPPORTED
+        assert call(type=xt, coef=flat([(14.9, -14.6, 0.0)])) == UNSUPPORTED and call(type=xt, coef=flat([(0.0, 0.0, 2.6)])) == ERR_NO_DEVICE
+    # without the 1.01 the ends of the range are left by what bf16 results round away, not by 2^-22
+    sharp = [(a * 1.01, b * 1.01 ** 3, c * 1.01 ** 5) for a, b, c in SCHEDULE[:-1]] + SCHEDULE[-1:]
+    assert [call(type=xt, steps=7, coef=flat(sharp)) for xt in (X_BF16, X_F16, X_F32)] == [UNSUPPORTED, ERR_NO_DEVICE, ERR_NO_DEVICE]

@@ -207,3 +207,25 @@ def test_refusals():
     out = torch.empty(3, 20, 30, device=DEV)[:1].expand(3, 20, 30)
     with pytest.raises(RsvdError):
         c.rsvd_orthogonalize(G, out=out)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n", [(20, 33), (64, 200), (300, 70), (1000, 520)])
+def test_a_schedule_that_starts_steeply(dtype, m, n):
+    """First coefficients above 4 and b x^2 + c x^4 down to -8.3.  (The first coefficients multiply to 1260, those of five equal steps to 485: of the sums' errors three times as
+    much is left.)  Also of matrices of one magnitude, whose entries round alike and whose one singular value starts at the end of the range."""
+    from test_dense_host import SCHEDULE
+    steps = len(SCHEDULE)
+    for kind in ("momentum", "one magnitude"):
+        g = gen(m + n)
+        G = momentum(g, m, n, TYPES[dtype])
+        if kind != "momentum":
+            G = (torch.where(torch.rand(m, 1, device=DEV, generator=g) < 0.5, -0.3, 0.3) * torch.where(torch.rand(1, n, device=DEV, generator=g) < 0.5, -1.0, 1.0)).to(TYPES[dtype])
+        say("orthogonalize, steep", dtype, m, n, kind)
+        got = ctx().rsvd_orthogonalize(G, steps, SCHEDULE)
+        want, model = definition(G, steps, SCHEDULE), definition(G, steps, SCHEDULE, 1 if dtype == "bf16" else 2)
+        lost, norm = torch.linalg.matrix_norm(model - want), torch.linalg.matrix_norm(want)
+        off = torch.linalg.matrix_norm(got.double() - want)
+        sums = 3 * 2.0 ** -24 * math.sqrt(max(m, n)) * 16 * norm
+        assert float(off) <= float(4 * lost + sums + UNIT[G.dtype] * norm), (kind, float(off / norm), float(lost / norm))
+        assert float(torch.linalg.svdvals(got.double()).max()) < 1.02

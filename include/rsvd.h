@@ -403,7 +403,8 @@ int rsvd_gated_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_act ac
                        void *workspace, size_t workspace_bytes);
 
 /* With g, u the two products, as they were kept or (kept NULL) computed again, and
- * D = (dH u act'(g), dH act(g)), rounded to the type (fp32: not):  dX (tokens x n) = D W,
+ * D = (dH u act'(g), dH act(g)), rounded to the type (fp32: not; fp16: times a power of two that keeps the largest
+ * in range, so that neither large nor small dH leave it):  dX (tokens x n) = D W,
  * dW (2 m x n) = D^T X.  dX or dW may be NULL: not wanted.  dW has the type of the others, or fp32
  * (dw_f32 != 0); an fp32 one may be added to (accumulate != 0).  X may be NULL where kept is given and
  * dW is not wanted, W where kept is given and dX is not. */

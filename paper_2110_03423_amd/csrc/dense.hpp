@@ -33,6 +33,7 @@ struct LinearOut {
   void *C = nullptr; int64_t ldc = 0, c_plane = 0, c_batch = 0;               // (elements, bytes, elements)
   int type = RSVD_X_F32, planes = 1, accumulate = 0;
   int64_t width = 0;                       // columns stored, zeros from N on (0: N)
+  const float *scale = nullptr;            // a power of two that sums are multiplied by first (dense_kn_launch of fp16 numbers; NULL: 1)
 };
 
 enum GatedAct { GATED_SILU = 0, GATED_GELU = 1, GATED_GELU_TANH = 2, GATED_RELU = 3, GATED_ACTS = 4 };
@@ -44,6 +45,7 @@ struct GatedOut {
   void *kept = nullptr; int64_t ldk = 0;
   const void *dH = nullptr; int64_t lddh = 0;
   uint16_t *D = nullptr; int64_t ldD = 0, plane = 0;      // (elements, bytes)
+  const float *scale = nullptr;            // fp16: D is held times this power of two, see range_launch
 };
 
 // ---------------------------------------------------------------- products
@@ -99,6 +101,12 @@ hipError_t gated_few_launch(rsvd_ctx *ctx, hipStream_t s, const GatedFewDesc &d)
 // bf16 planes `plane` bytes apart (rows = 0: none); and D from kept products (slope.kept; tokens = 0: none).
 struct LayOut { const void *X; int64_t ldx, rows; uint16_t *out; int64_t plane; };
 hipError_t lay_out_launch(hipStream_t s, rsvd_xtype type, int64_t n, int64_t width, const LayOut &x, const LayOut &w, int64_t tokens, int64_t m, const GatedOut &slope);
+
+// What D of fp16 tokens is held times: scale[0], a power of two, and scale[1], which takes it out of sums again.  From dH, and the products that were kept or (kept NULL) X and W.
+// parts: kRangeParts * 3 floats.
+constexpr int kRangeParts = 1024;
+hipError_t range_launch(hipStream_t s, int64_t tokens, int64_t n, int64_t m, const void *dH, int64_t lddh, const void *kept, int64_t ldk, const void *X, int64_t ldx, const void *W,
+                        int64_t ldw, float *parts, float *scale);
 
 // ---------------------------------------------------------------- f8.hip
 // Whether each workgroup rounds the tokens itself, and whether a weight is read straight from memory for tokens that were rounded before; tiles are faster for more tokens and for

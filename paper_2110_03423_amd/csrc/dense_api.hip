@@ -119,7 +119,7 @@ DenseDesc slope_w_desc(rsvd_xtype type, int64_t tokens, int64_t n, int64_t m) {
   return d;
 }
 
-struct GatedLayout { size_t x, w, D, partial, partial_bytes, total; };
+struct GatedLayout { size_t x, w, D, range, partial, partial_bytes, total; };
 size_t most(size_t a, size_t b) { return a > b ? a : b; }
 GatedLayout gated_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, bool x_lies, bool w_lies, bool grad, bool kept) {
   GatedLayout L;
@@ -127,6 +127,7 @@ GatedLayout gated_layout(const rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, i
   L.x = take(x_lies ? 0 : planes_bytes(type, tokens, n));
   L.w = take(w_lies ? 0 : planes_bytes(type, 2 * m, n));
   L.D = take(grad ? planes_bytes(type, tokens, 2 * m) : 0);
+  L.range = take(grad && type == RSVD_X_F16 ? (3 * kRangeParts + 2) * sizeof(float) : 0);
   L.partial_bytes = kept ? 0 : dense_partial_bytes(ctx, gated_desc(type, tokens, n, m));
   if (grad) {
     L.partial_bytes = most(L.partial_bytes, dense_partial_bytes(ctx, slope_x_desc(type, tokens, n, m)));
@@ -461,6 +462,12 @@ int rsvd_gated_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_a
   o.kept = (void *)kept; o.ldk = ldk;
   o.dH = dH; o.lddh = lddh;
   o.D = (uint16_t *)(ws + L.D); o.ldD = width_of(2 * m); o.plane = D.plane;
+  float *const range = (float *)(ws + L.range), *const scale = type == RSVD_X_F16 ? range + 3 * kRangeParts : nullptr;
+  o.scale = scale;
+  if (scale != nullptr) {
+    ProfScope ps(ctx, s, PK_SMALL);
+    RSVD_TRY(range_launch(s, tokens, n, m, dH, lddh, kept, ldk, X, ldx, W, ldw, range, scale), "range of the gated gradient");
+  }
   // (fp32 operands of small tiles are read as they lie)
   const bool x_wide = type == RSVD_X_F32 && !recompute && dW != nullptr && ldx <= kMaxLd / 4 && dense_takes_wide(ctx, slope_w_desc(type, tokens, n, m));
   const bool w_wide = type == RSVD_X_F32 && !recompute && dX != nullptr && ldw <= kMaxLd / 4 && dense_takes_wide(ctx, slope_x_desc(type, tokens, n, m));
@@ -490,6 +497,7 @@ int rsvd_gated_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_a
     d.A = D.p; d.lda = D.ld; d.a_plane = D.plane;
     d.B = w.p; d.ldb = w.ld; d.b_plane = w.plane; d.b_wide = w_wide;
     d.out.C = dX; d.out.ldc = lddx; d.out.type = type;
+    if (scale != nullptr) d.out.scale = scale + 1;
     d.partial = partial; d.partial_bytes = L.partial_bytes;
     RSVD_TRY(dense_kn_launch(ctx, s, d, false), "gradient of tokens");
   }
@@ -498,6 +506,7 @@ int rsvd_gated_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_a
     d.A = D.p; d.lda = D.ld; d.a_plane = D.plane;
     d.B = x.p; d.ldb = x.ld; d.b_plane = x.plane; d.b_wide = x_wide;
     d.out.C = dW; d.out.ldc = lddw; d.out.type = wtype; d.out.accumulate = accumulate;
+    if (scale != nullptr) d.out.scale = scale + 1;
     d.partial = partial; d.partial_bytes = L.partial_bytes;
     RSVD_TRY(dense_kn_launch(ctx, s, d, true), "gradient of a weight");
   }

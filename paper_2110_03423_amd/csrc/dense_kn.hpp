@@ -290,8 +290,11 @@ __global__ __launch_bounds__(64 * WGM * WGN * KG, KG == 1 ? 2 : PL == 3 ? 2 : 4)
       for (int j = 0; j < TN; ++j) sums[i][j] = acc[i][j];
   }
   const int below = KG == 1 ? 0 : 16 * group;
+  float by = 1.f;
+  if constexpr (KIND == DK_F16)
+    if (P.out.scale != nullptr) by = *P.out.scale;
   dense_finish<BN, ROWS, TN>(P, sums, partial == nullptr ? nullptr : partial + below * BN, batch, m0 + wm0 + below, n0 + wn0, P.symmetric && tile_m != tile_n, last_lane,
-                             reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()));
+                             reinterpret_cast<float *>(dense_lds + wave * finish_lds<TN>()), by);
 }
 
 template <int KIND, bool A_KROWS, int PL, int BM, int BN, int WGM, int WGN, int KG = 1, bool WIDE = false> hipError_t dense_kn_run(hipStream_t s, const DenseParams &P) {

@@ -398,6 +398,7 @@ __device__ __forceinline__ void gated_end(const GatedOut &O, int64_t N, const in
   with_type(O.type, [&](auto type) RSVD_INLINE {
     constexpr int TYPE = decltype(type)::value;
     if (O.dH != nullptr) {
+      const float by = TYPE == RSVD_X_F16 ? *O.scale : 1.f;
       f32x4 dh[C][V];
 #pragma unroll
       for (int c = 0; c < C; ++c) load_row<TYPE, V>(O.dH, m[c] * O.lddh + n[c], left(c), dh[c]);
@@ -410,8 +411,8 @@ __device__ __forceinline__ void gated_end(const GatedOut &O, int64_t N, const in
             for (int e = 0; e < 4; ++e) {
               float value;
               const float slope = act_slope<decltype(act)::value>(g[c][x][e], value);
-              g[c][x][e] = dh[c][x][e] * u[c][x][e] * slope;
-              u[c][x][e] = dh[c][x][e] * value;
+              g[c][x][e] = dh[c][x][e] * u[c][x][e] * slope * by;
+              u[c][x][e] = dh[c][x][e] * value * by;
             }
       });
 #pragma unroll
@@ -472,9 +473,11 @@ template <int TN> __device__ __forceinline__ void mirror_rows(const DenseParams 
 }
 
 // Block (i, j) of lane L holds row 16 i + L % 16 and four columns from 16 j + 4 (L / 16) on: through LDS, sixteen rows at a time, so that lanes next to each
-// other write what is next to each other.  mirror: and the same with rows and columns exchanged.  lds: the wavefront's finish_lds<TN>() bytes.
+// other write what is next to each other.  mirror: and the same with rows and columns exchanged.  lds: the wavefront's finish_lds<TN>() bytes.  by: what all
+// sums are multiplied by.
 template <int BN, int TM, int TN>
-__device__ __forceinline__ void dense_finish(const DenseParams &P, f32x4 (&acc)[TM][TN], float *partial, int batch, int64_t m1, int64_t n1, bool mirror, int lane, float *lds) {
+__device__ __forceinline__ void dense_finish(const DenseParams &P, f32x4 (&acc)[TM][TN], float *partial, int batch, int64_t m1, int64_t n1, bool mirror, int lane, float *lds,
+                                             float by) {
   constexpr int PITCH = 16 * TN + 4, PER_ROW = 4 * TN, ROWS = 64 / PER_ROW, PASSES = 16 / ROWS, C = PASSES < 4 ? PASSES : 4;
   const int r16 = lane & 15, kq = lane >> 4, row = lane / PER_ROW, col = 4 * (lane % PER_ROW);
   const bool whole = m1 + 16 * TM <= P.M && n1 + 16 * TN <= P.N;
@@ -484,7 +487,7 @@ __device__ __forceinline__ void dense_finish(const DenseParams &P, f32x4 (&acc)[
     for (int x = 0; x < TM; ++x)
       if (i == x) {
 #pragma unroll
-        for (int j = 0; j < TN; ++j) *reinterpret_cast<f32x4 *>(lds + r16 * PITCH + 16 * j + 4 * kq) = acc[x][j];
+        for (int j = 0; j < TN; ++j) *reinterpret_cast<f32x4 *>(lds + r16 * PITCH + 16 * j + 4 * kq) = acc[x][j] * by;
       }
     asm volatile("" ::: "memory");
     __builtin_amdgcn_wave_barrier();

@@ -107,6 +107,125 @@ hipError_t gated_few_launch(rsvd_ctx *, hipStream_t s, const GatedFewDesc &d) {
   return hipGetLastError();
 }
 
+// ---------------------------------------------------------------- the range of a gradient in fp16
+// D = (dH u act', dH act) of fp16 tokens is held in fp16 times a power of two.  As it is it would leave the range on either side where neither gradient does: dH of 1e-5 lost 4e-3 of dW, and dH u
+// above 65504 was an infinity.  With |act'| <= 1.13, |act| <= |g| and |g|, |u| <= G, |D| <= 1.13 max |dH| G; that, with room for rounding, is brought to 2^15 or more.  G is the largest
+// product that was kept or, of those that are computed again, the largest norm of a row of X times that of a row of W.  What is not finite does not count: it stays what it is.
+// Memory is the bound: 8192 x 4096 -> 8192 kept, 403 MB 84 us (4.8 TB/s), computed again, 335 MB 68 us, of a gradient of 2930; the second launch, one workgroup, takes 2 to 5.
+struct RangeOf { const char *p; int64_t ld, rows, cols; bool norm; };
+
+// Magnitudes of eight fp16 numbers, the largest that is finite.
+__device__ __forceinline__ unsigned range_top8(u32x4 w, unsigned top) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const unsigned v = (w[e >> 1] >> (16 * (e & 1))) & 0x7fffu;
+    top = max(top, v < 0x7c00u ? v : 0u);
+  }
+  return top;
+}
+__device__ __forceinline__ float range_squares8(u32x4 w, float sum) {
+#pragma unroll
+  for (int h = 0; h < 4; ++h) {
+    const unsigned pair = w[h];
+    const f16x2 f = __builtin_bit_cast(f16x2, pair);
+    sum += (float)f[0] * (float)f[0] + (float)f[1] * (float)f[1];
+  }
+  return sum;
+}
+// The largest magnitude of a matrix, or the largest sum of squares of a row, by parts.
+__global__ __launch_bounds__(256) void range_kernel(const RangeOf first, const RangeOf second, const RangeOf third, float *parts) {
+  const RangeOf M = blockIdx.y == 0 ? first : blockIdx.y == 1 ? second : third;
+  __shared__ float wave_top[4];
+  const int tid = threadIdx.x, lane = tid & 63, per_row = (int)((M.cols + 7) / 8);
+  constexpr int U = 4;                                   // loads in flight
+  float most = 0.f;
+  auto finite = [](float v) RSVD_INLINE { return v < __uint_as_float(0x7f800000u) ? v : 0.f; };
+  if (!M.norm) {
+    const int64_t total = M.rows * per_row;
+    unsigned top = 0u;
+    for (int64_t group = blockIdx.x; group * 256 < total; group += U * gridDim.x) {
+      u32x4 v[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        int64_t r;
+        int c;
+        piece_of(group + u * gridDim.x, per_row, r, c);
+        v[u] = halves8(reinterpret_cast<const uint16_t *>(M.p) + r * M.ld + 8 * c, r < M.rows ? M.cols - 8 * c : 0);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) top = range_top8(v[u], top);
+    }
+    most = (float)__builtin_bit_cast(_Float16, (uint16_t)top);
+  } else {
+    // a row by 64 lanes, or by as many of a power of two as have a piece of it
+    int lanes = 64;
+    while (lanes > 1 && lanes / 2 >= per_row) lanes >>= 1;
+    const int at_once = 64 / lanes, place = lane & (lanes - 1);
+    const int64_t wave = (int64_t)blockIdx.x * 4 + (tid >> 6), step = (int64_t)gridDim.x * 4 * at_once;
+    for (int64_t row = wave * at_once + lane / lanes; row - lane / lanes < M.rows; row += U * step) {
+      float sum[U] = {0.f, 0.f, 0.f, 0.f};
+      for (int c = place; c - place < per_row; c += lanes) {
+        u32x4 v[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int64_t r = row + u * step;
+          v[u] = halves8(reinterpret_cast<const uint16_t *>(M.p) + r * M.ld + 8 * c, r < M.rows ? M.cols - 8 * c : 0);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) sum[u] = range_squares8(v[u], sum[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        for (int d = 1; d < lanes; d <<= 1) sum[u] += __shfl_xor(sum[u], d);
+        most = fmaxf(most, finite(sum[u]));
+      }
+    }
+  }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) most = fmaxf(most, __shfl_xor(most, d));
+  if (lane == 0) wave_top[tid >> 6] = most;
+  __syncthreads();
+  if (tid == 0) parts[blockIdx.y * gridDim.x + blockIdx.x] = fmaxf(fmaxf(wave_top[0], wave_top[1]), fmaxf(wave_top[2], wave_top[3]));
+}
+__global__ __launch_bounds__(256) void range_scale_kernel(const float *parts, int count, int norms, float *scale) {
+  __shared__ float wave_top[3][4];
+  const int tid = threadIdx.x;
+  float top[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+  for (int q = 0; q < 3; ++q) {
+    if (q == 2 && norms == 0) break;
+#pragma unroll
+    for (int x = 0; x < kRangeParts; x += 256) top[q] = fmaxf(top[q], x + tid < count ? parts[q * count + x + tid] : 0.f);
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) top[q] = fmaxf(top[q], __shfl_xor(top[q], d));
+  }
+  if ((tid & 63) == 0)
+#pragma unroll
+    for (int q = 0; q < 3; ++q) wave_top[q][tid >> 6] = top[q];
+  __syncthreads();
+  if (tid > 0) return;
+#pragma unroll
+  for (int q = 0; q < 3; ++q) top[q] = fmaxf(fmaxf(wave_top[q][0], wave_top[q][1]), fmaxf(wave_top[q][2], wave_top[q][3]));
+  // (the norms' sums, and the products', are off by up to 1 % of themselves for 2^17 numbers added in turn)
+  const float bound = 1.14f * top[0] * (norms ? 1.02f * sqrtf(top[1]) * sqrtf(top[2]) : top[1]);
+  const int up = bound > 0.f ? 15 - ilogbf(bound) : 0;   // (bounds: 2^-72 to 2^66)
+  scale[0] = ldexpf(1.f, up);
+  scale[1] = ldexpf(1.f, -up);
+}
+hipError_t range_launch(hipStream_t s, int64_t tokens, int64_t n, int64_t m, const void *dH, int64_t lddh, const void *kept, int64_t ldk, const void *X, int64_t ldx, const void *W,
+                        int64_t ldw, float *parts, float *scale) {
+  const bool norms = kept == nullptr;
+  const RangeOf dh = {(const char *)dH, lddh, tokens, m, false};
+  const RangeOf second = norms ? RangeOf{(const char *)X, ldx, tokens, n, true} : RangeOf{(const char *)kept, ldk, tokens, 2 * m, false}, third = {(const char *)W, ldw, 2 * m, n, true};
+  const int64_t pieces = (norms ? (tokens + 2 * m) * ceil_div(n, 8) : tokens * ceil_div(2 * m, 8)) + tokens * ceil_div(m, 8);
+  const int count = pieces >= 1024 * kRangeParts ? kRangeParts : (int)ceil_div(pieces, 1024);
+  hipLaunchKernelGGL(range_kernel, dim3((unsigned)count, norms ? 3 : 2), dim3(256), 0, s, dh, second, third, parts);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(range_scale_kernel, dim3(1), dim3(256), 0, s, parts, count, (int)norms, scale);
+  return hipGetLastError();
+}
+
 // ---------------------------------------------------------------- operands
 // Gradients of gate and up from the kept products, and matrices as the products want them; memory is the bound (301 x 2999 -> 1410 in fp32 with its weight: 106 MB in 17.6 us).  One launch: workgroups of the one, then of the others.
 template <int TYPE> __device__ __forceinline__ void slope_group(const GatedOut &O, int64_t tokens, int64_t m, int64_t group) {

@@ -271,3 +271,58 @@ def test_refusals():
     for call in (lambda: c.rsvd_gated_product(x, w.half()), lambda: c.rsvd_gated_product(x.double(), w.double())):
         with pytest.raises(TypeError):
             call()
+
+
+@pytest.mark.parametrize("size", [1e-5, 1e-3, 2e3])
+@pytest.mark.parametrize("keep", [False, True])
+@pytest.mark.parametrize("t,n,m", [(3, 70, 5), (40, 1030, 33), (65, 64, 30), (200, 264, 100), (513, 1030, 350), (2100, 300, 140), (1000, 2056, 1000)])
+def test_fp16_gradients_of_any_size(t, n, m, keep, size):
+    """D has to leave fp16's range on neither side: gradients that are subnormal numbers, and dH u above 65504 where dX is finite.  (Bound: D is rounded in fp16 times a power of two
+    that brings what it can be at most, 1.14 max |dH| max |g, u|, to 2^15 or more, so that 2^-25 there is 2^-40 of that; of products computed again, which are known by the
+    norms of rows, the most is 1.02 of those.)"""
+    g = gen(t + n)
+    x, w, _ = block(g, t, n, m, F16)
+    x = (x * 6) if size > 1 else x
+    dh = (size * torch.randn(t, m, device=DEV, generator=g)).to(F16)
+    say("fp16 gradients", t, n, m, keep, size)
+    kept = ctx().rsvd_gated_product(x, w, keep=True)[1] if keep else None
+    dx, dw = torch.empty_like(x), torch.empty(2 * m, n, device=DEV)
+    ctx().rsvd_gated_product_grad(dh, x, w, kept=kept, out=(dx, dw))
+    if keep:
+        gu, bound, most = kept.double(), torch.zeros(t, 2 * m, device=DEV, dtype=torch.float64), float(kept.double().abs().max())
+    else:
+        (_, gu), (_, bound) = forward64(x, w, "silu")
+        most = 1.02 * float(x.double().norm(dim=1).max() * w.double().norm(dim=1).max())
+    d, ed = slopes64(gu[:, :m], gu[:, m:], bound[:, :m], bound[:, m:], dh, "silu")
+    if size > 1 and t > 3:
+        assert float(d.abs().max()) > 65504
+    ed = ed + UNIT[F16] * (d.abs() + ed) + 2.0 ** -40 * 1.14 * float(dh.double().abs().max()) * most
+    W, X = w.double(), x.double()
+    want, bx = d @ W, ed @ W.abs() + (2 * m + 64) * E * ((d.abs() + ed) @ W.abs())
+    inside = (want.abs() + bx) * 1.001 < 65504
+    assert float(inside.double().mean()) > 0.9
+    tol = bx + UNIT[F16] * (want.abs() + bx) + FLOOR[F16]
+    assert bool(((dx.double() - want).abs() <= tol)[inside].all()), float(((dx.double() - want).abs() / tol)[inside].max())
+    check(dw, d.t() @ X, ed.t() @ X.abs() + (t + 64) * E * ((d.abs() + ed).t() @ X.abs()), "dW")
+    if size < 1e-4 and t > 100:
+        # what the rounding of D leaves of dW: as much as of larger gradients, 2^-11 at the most and 2^-11 / sqrt 3 on the whole
+        assert float((dw.double() - d.t() @ X).norm() / (d.t() @ X).norm()) < 2.0 ** -11 / 3 ** 0.5
+
+
+def test_fp16_gradients_of_zeros_and_of_what_is_not_finite():
+    x, w, dh = block(gen(5), 70, 72, 40, F16)
+    kept = ctx().rsvd_gated_product(x, w, keep=True)[1]
+    for k in (None, kept):
+        for z in ((torch.zeros_like(dh), x, w, k), (dh, torch.zeros_like(x), w, None), (dh, x, torch.zeros_like(w), None), (dh, x, w, torch.zeros_like(kept))):
+            dx, dw = ctx().rsvd_gated_product_grad(*z[:3], kept=z[3])
+            assert not dx.any() and not dw.any()
+        want = ctx().rsvd_gated_product_grad(dh, x, w, kept=k)
+        for bad in (math.inf, math.nan):
+            d, y = dh.clone(), x.clone()
+            d[4] = bad
+            dx, dw = ctx().rsvd_gated_product_grad(d, x, w, kept=k)
+            keep = [i for i in range(70) if i != 4]
+            assert not dx[4].isfinite().any() and torch.equal(dx[keep], want[0][keep])
+            y[4] = bad
+            dx, dw = ctx().rsvd_gated_product_grad(dh, y, w, kept=k)
+            assert torch.equal(dx[keep], want[0][keep]) and not dw[3].isfinite().any()

@@ -192,7 +192,7 @@ int f8_product(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens, int
   if (!valid(Y, es)) return -13;
   if (ldy < m) return -14;
   if (!sizes_supported(tokens, n, m) || ldq > kMaxLd || ldp > kMaxPowersLd) return RSVD_ERR_UNSUPPORTED;
-  if (overlap(span(Y, tokens, m, ldy, es), {span(X, tokens, n, ldx, es), span(codes, m, f8_width(n), ldq, 1)})) return -13;
+  if (overlap(span(Y, tokens, m, ldy, es), {span(X, tokens, n, ldx, es), span(codes, m, f8_width(n), ldq, 1), span(powers, ceil_div(m, 128), f8_powers(n), ldp, 1)})) return -13;
   const F8Layout L = f8_product_layout(ctx, type, tokens, n, m);
   if (L.total > 0 && (workspace == nullptr || ((uintptr_t)workspace & 255) != 0)) return -15;
   if (workspace_bytes < L.total) return -16;
@@ -532,8 +532,15 @@ int rsvd_f8_weight(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t m, int6
   if (!sizes_supported(1, n, m)) return RSVD_ERR_UNSUPPORTED;
   const Span w_span = span(W, m, n, ldw, xtype_size(type)), q_span = span(codes, m, f8_width(n), ldq, 1);
   if (overlap(q_span, w_span)) return -8;
-  if (overlap(span(codes_t, n, f8_width(m), ldqt, 1), {w_span, q_span})) return -12;
+  const Span qt_span = span(codes_t, n, f8_width(m), ldqt, 1);
+  if (overlap(qt_span, {w_span, q_span})) return -12;
   RSVD_ON_DEVICE();
+  // (behind the question for a device: a plan may name one place for the powers and what is read)
+  const Span p_span = span(powers, ceil_div(m, 128), ceil_div(n, 128), ldp, 1);
+  const Span pt_span = span(codes_t != nullptr ? powers_t : nullptr, ceil_div(n, 128), ceil_div(m, 128), ldpt, 1);
+  if (overlap(p_span, {w_span, q_span})) return -10;
+  if (overlap(qt_span, p_span)) return -12;
+  if (overlap(pt_span, {w_span, q_span, qt_span, p_span})) return -14;
   ProfScope ps(ctx, (hipStream_t)stream, PK_SMALL);
   RSVD_TRY(f8_weight_launch((hipStream_t)stream, type, m, n, W, ldw, codes, ldq, powers, ldp, codes_t, ldqt, codes_t != nullptr ? powers_t : nullptr, ldpt),
            "weight to 8-bit floats");

@@ -224,3 +224,14 @@ def test_coefficients_are_followed_between_the_ends_of_their_range(plan):
     # without the 1.01 the ends of the range are left by what bf16 results round away, not by 2^-22
     sharp = [(a * 1.01, b * 1.01 ** 3, c * 1.01 ** 5) for a, b, c in SCHEDULE[:-1]] + SCHEDULE[-1:]
     assert [call(type=xt, steps=7, coef=flat(sharp)) for xt in (X_BF16, X_F16, X_F32)] == [UNSUPPORTED, ERR_NO_DEVICE, ERR_NO_DEVICE]
+
+
+@pytest.mark.parametrize("name,n,m", [("rsvd_f8_product", 300, 200), ("rsvd_f8_product_grad", 200, 300)])
+def test_results_may_not_lie_on_powers(plan, name, n, m):
+    """Of a weight whose codes are 200 rows of 300: two rows of four bytes of powers, 16 apart."""
+    x = 1 << 30
+    call = caller(plan, name, "ctx stream type tokens n m X ldx q ldq p ldp Y ldy ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, tokens=3, n=n, m=m, X=at(x), ldx=300,
+                  q=at(2 * x), ldq=384, p=at(3 * x), ldp=16, Y=OUT, ldy=200, ws=PTR, bytes=1 << 40)
+    assert call() == ERR_NO_DEVICE and call(Y=at(3 * x)) == -13 and call(Y=at(3 * x + 18)) == -13 and call(Y=at(3 * x + 20)) == ERR_NO_DEVICE
+    assert call(Y=at(3 * x - 1198)) == -13 and call(Y=at(3 * x - 1200)) == ERR_NO_DEVICE
+    assert call(tokens=100, Y=at(3 * x)) == -13

@@ -233,3 +233,28 @@ def test_refusals():
             call()
     with pytest.raises(TypeError):
         c.rsvd_f8_product(x.double(), h)
+
+
+def test_results_of_a_weight_may_not_lie_on_each_other():
+    c, m, n = ctx(), 300, 260
+    W = weight(gen(4), m, n).to(F32)
+    room = torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
+    base = room.data_ptr()
+    base += -base % 256
+    # (codes, powers; the same in the other order: 384 bytes of each row of codes, three rows of three powers, 4 apart)
+    places = dict(q=base, p=base + (1 << 18), qt=base + (1 << 19), pt=base + (1 << 19) + (1 << 18))
+
+    def call(**kw):
+        a = dict(places, **kw)
+        return c.lib.rsvd_f8_weight(c.h, None, 2, m, n, W.data_ptr(), n, a["q"], 384, a["p"], 4, a["qt"], 384, a["pt"], 4)
+
+    assert call() == 0
+    torch.cuda.synchronize()
+    assert call(p=W.data_ptr()) == -10 and call(p=places["q"]) == -10 and call(p=places["q"] + 299 * 384 + 380) == -10 and call(p=places["q"] - 8) == -10
+    assert call(pt=W.data_ptr()) == -14 and call(pt=places["q"]) == -14 and call(pt=places["qt"]) == -14 and call(pt=places["p"]) == -14 and call(pt=places["p"] + 8) == -14
+    assert call(p=places["qt"]) == -12
+    assert call(p=places["q"] + 300 * 384) == 0 and call(pt=places["p"] + 12) == 0
+    torch.cuda.synchronize()
+    h = c.rsvd_f8_weight(W)
+    at = places["p"] - room.data_ptr()
+    assert torch.equal(room[at + 12:at + 24].view(3, 4)[:, :3], h.powers.t())

@@ -392,7 +392,7 @@ int rsvd_keep8_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t tokens
 typedef enum { RSVD_ACT_SILU = 0, RSVD_ACT_GELU = 1, RSVD_ACT_GELU_TANH = 2, RSVD_ACT_RELU = 3 } rsvd_act;
 
 /* Bytes of device workspace.  lie: bit 0, X lies as the products read it; bit 1, W does;
- * bit 2 (gradient), the products were kept. */
+ * bit 2 (gradient), the products were kept.  What is not said may be the case all the same: 0 is enough for any call. */
 int rsvd_gated_product_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int lie, size_t *bytes);
 int rsvd_gated_product_grad_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int64_t n, int64_t m, int lie, size_t *bytes);
 

@@ -88,10 +88,12 @@ X_BF16, X_F16, X_F32 = 0, 1, 2
 ACTS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
 
 
-# forward products of so few tokens need no workspace, however their operands lie
-def _gated_few(xt, tokens, n, m):
+# forward products of so few tokens need no workspace, however their tokens lie (and a weight that does not lie as it is read would be laid out)
+def _gated_few(xt, tokens, n, m, w_lies=True):
     if xt == X_F32:
         return tokens <= (64 if m >= 2048 else 16)
+    if not w_lies and m >= 4096:
+        return tokens <= 32
     return tokens <= 20 and tokens * n <= 196608 if m >= 8192 else tokens <= 32 and tokens * n <= 98304
 
 
@@ -721,7 +723,9 @@ class Rsvd:
         elif _gated_few(xt, tokens, n, m):
             ws = (None, 0)
         else:
-            ws = self._layer_ws(stream, "rsvd_gated_product_bytes", (xt, tokens, n, m, self._lies(X, ldx) + 2 * self._lies(W, ldw)))
+            w_lies = self._lies(W, ldw)
+            ws = (None, 0) if not w_lies and _gated_few(xt, tokens, n, m, False) else \
+                self._layer_ws(stream, "rsvd_gated_product_bytes", (xt, tokens, n, m, self._lies(X, ldx) + 2 * w_lies))
         H = X.new_empty((tokens, m)) if out is None else self._like(out, m, "out", tokens, X.dtype)
         kept = X.new_empty((tokens, 2 * m)) if keep else None
         self._check(self.lib.rsvd_gated_product(self.h, stream, xt, code, tokens, n, m, X.data_ptr(), ldx, W.data_ptr(), ldw,

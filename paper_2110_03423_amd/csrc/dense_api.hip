@@ -334,8 +334,11 @@ int rsvd_gated_product_bytes(rsvd_ctx *ctx, rsvd_xtype type, int64_t tokens, int
   if (const int rc = check_sizes(type, tokens, n, m, 2)) return rc;
   if (bytes == nullptr) return -7;
   if (!sizes_supported(tokens, n, m)) return RSVD_ERR_UNSUPPORTED;
-  const bool can = type != RSVD_X_F32 && n % 8 == 0;
-  *bytes = gated_few(type, tokens, n, m, can && (lie & 2)) ? 0 : gated_layout(ctx, type, tokens, n, m, can && (lie & 1), can && (lie & 2), false, false).total;
+  // (a weight that is not known to lie may do so all the same, and may then go in tiles where it would not)
+  const bool can = type != RSVD_X_F32 && n % 8 == 0, x_lies = can && (lie & 1);
+  *bytes = 0;
+  for (const bool w_lies : {can && (lie & 2), can})
+    if (!gated_few(type, tokens, n, m, w_lies)) *bytes = most(*bytes, gated_layout(ctx, type, tokens, n, m, x_lies, w_lies, false, false).total);
   return RSVD_OK;
 }
 

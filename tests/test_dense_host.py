@@ -235,3 +235,34 @@ def test_results_may_not_lie_on_powers(plan, name, n, m):
     assert call() == ERR_NO_DEVICE and call(Y=at(3 * x)) == -13 and call(Y=at(3 * x + 18)) == -13 and call(Y=at(3 * x + 20)) == ERR_NO_DEVICE
     assert call(Y=at(3 * x - 1198)) == -13 and call(Y=at(3 * x - 1200)) == ERR_NO_DEVICE
     assert call(tokens=100, Y=at(3 * x)) == -13
+
+
+def test_the_workspace_of_what_is_known_to_lie_is_enough_whatever_else_does(plan):
+    call = caller(plan, "rsvd_gated_product", "ctx stream type act tokens n m X ldx W ldw H ldh kept ldk ws bytes", ctx=plan.h, stream=NULL, type=X_BF16, act=0,
+                  tokens=32, n=64, m=64, X=PTR, ldx=64, W=PTR, ldw=64, H=OUT, ldh=64, kept=NULL, ldk=0, ws=PTR, bytes=0)
+    grad = caller(plan, "rsvd_gated_product_grad", "ctx stream type act tokens n m dH lddh X ldx W ldw kept ldk dX lddx dW lddw f32 acc ws bytes", ctx=plan.h, stream=NULL,
+                  type=X_F16, act=1, tokens=100, n=64, m=64, dH=PTR, lddh=64, X=PTR, ldx=64, W=PTR, ldw=64, kept=PTR, ldk=100, dX=OUT, lddx=64, dW=OUT2, lddw=64,
+                  f32=0, acc=0, ws=PTR, bytes=0)
+    grown = 0
+    for xt in (X_BF16, X_F16, X_F32):
+        for tokens in (1, 16, 17, 20, 21, 32, 33, 100):
+            for n, m in ((64, 64), (2048, 4096), (4096, 4096), (8192, 4096), (8192, 8192), (6144, 8200), (1000, 12000), (3001, 4100)):
+                sizes = dict(type=xt, tokens=tokens, n=n, m=m, ldx=n, ldw=n, ldh=m)
+                need = [bytes_of(plan, "rsvd_gated_product_bytes", xt, tokens, n, m, lie) for lie in range(4)]
+                assert need[0] >= max(need) and need[1] >= need[3] and need[2] >= need[3]
+                for lie in range(4):
+                    places = dict(X=PTR if lie & 1 else C.c_void_p((1 << 20) + 4), W=PTR if lie & 2 else C.c_void_p((1 << 20) + 4))
+                    for known in range(4):
+                        if known & ~lie == 0:
+                            assert call(bytes=need[known], **sizes, **places) == ERR_NO_DEVICE
+                    # what the binding takes no workspace for
+                    if binding._gated_few(xt, tokens, n, m, bool(lie & 2)):
+                        assert call(ws=NULL, **sizes, **places) == ERR_NO_DEVICE
+                grown += need[0] > 0 and binding._gated_few(xt, tokens, n, m, False)
+                need = [bytes_of(plan, "rsvd_gated_product_grad_bytes", xt, tokens, n, m, lie) for lie in range(8)]
+                for lie in range(8):
+                    places = dict(X=PTR if lie & 1 else C.c_void_p((1 << 20) + 4), W=PTR if lie & 2 else C.c_void_p((1 << 20) + 4), kept=PTR if lie & 4 else NULL)
+                    for known in range(8):
+                        if known & ~lie == 0:
+                            assert grad(bytes=need[known], ldk=2 * m, lddh=m, lddx=n, lddw=n, **{k: v for k, v in sizes.items() if k != "ldh"}, **places) == ERR_NO_DEVICE
+    assert grown > 0

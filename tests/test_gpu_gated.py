@@ -326,3 +326,17 @@ def test_fp16_gradients_of_zeros_and_of_what_is_not_finite():
             y[4] = bad
             dx, dw = ctx().rsvd_gated_product_grad(dh, y, w, kept=k)
             assert torch.equal(dx[keep], want[0][keep]) and not dw[3].isfinite().any()
+
+
+@pytest.mark.parametrize("t", [20, 32])
+def test_few_tokens_of_a_weight_that_lies_otherwise_need_no_workspace(t):
+    from paper_2110_03423_amd import Rsvd
+    c, n, m = Rsvd(0), 6144, 4096
+    x, w, _ = block(gen(t), t, n, m, BF16)
+    wide = torch.zeros(2 * m, n + 4, device=DEV, dtype=BF16)
+    wide[:, 2:n + 2] = w
+    h = c.rsvd_gated_product(x, wide[:, 2:n + 2])
+    assert not c._layer and c.rsvd_gated_product(x, w).shape == h.shape and c._layer
+    (H, _), (bh, _) = forward64(x, w, "silu")
+    check(h, H, bh, "H")
+    check(c.rsvd_gated_product(x, w), H, bh, "H, in tiles")

@@ -266,8 +266,8 @@ def _empty_f8(rows, n, device):
 class WeightF8:
     """A weight (m x n) in 8-bit floats (torch.float8_e4m3fn) with a power of two for each block of 128 x 128, as rsvd_f8_product takes it:
     codes, and powers (uint8, e + 127 for 2^e; 255 makes the block NaN), a row for each 128 rows, a byte for each 128 columns.  A copy of them is laid out
-    here once, in the order of the product and (`backward`) in that of its gradient: `codes`, `powers` are views of the first, and a layer whose values change
-    is made anew, here or by Rsvd.rsvd_f8_weight."""
+    here once, in the order of the product and (`backward`) in that of its gradient, and keeps its values: `codes` and `powers` are copies, made when they are asked for, and a
+    layer whose values change is made anew, here or by Rsvd.rsvd_f8_weight."""
 
     def __init__(self, codes, powers, backward=True):
         import torch
@@ -292,13 +292,26 @@ class WeightF8:
         self._set(m, n, lay(bytes_, powers), lay(bytes_.t(), powers.t()) if backward else None)
 
     def _set(self, m, n, forward, backward):
-        import torch
         self.m, self.n = m, n
-        self._forward, self._backward = forward, backward
-        self.codes = forward[0][:, :n].view(torch.float8_e4m3fn)
-        self.powers = forward[1][:, :_blocks(n)]
+        self._backward = backward
         self.device, self._index = forward[0].device, forward[0].get_device()
+        self._forward = forward
         return self
+
+    # (a view of one of the two orders could be written to, and the other would not follow)
+    @property
+    def codes(self):
+        import torch
+        return self._forward[0][:, :self.n].clone().view(torch.float8_e4m3fn)
+
+    @property
+    def powers(self):
+        return self._forward[1][:, :_blocks(self.n)].clone()
+
+    def __setattr__(self, name, value):
+        if "_forward" in self.__dict__:
+            raise AttributeError("a WeightF8 keeps its values: make another one")
+        object.__setattr__(self, name, value)
 
 
 def _at(t):

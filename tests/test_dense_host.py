@@ -266,3 +266,23 @@ def test_the_workspace_of_what_is_known_to_lie_is_enough_whatever_else_does(plan
                         if known & ~lie == 0:
                             assert grad(bytes=need[known], ldk=2 * m, lddh=m, lddx=n, lddw=n, **{k: v for k, v in sizes.items() if k != "ldh"}, **places) == ERR_NO_DEVICE
     assert grown > 0
+
+
+def test_a_weight_of_8_bit_floats_keeps_its_values():
+    """Both orders of the codes hold one weight: what is read off it may be written to, and is a copy."""
+    import copy
+    import pickle
+    from paper_2110_03423_amd import WeightF8
+    codes = torch.arange(130 * 70).remainder(126).to(torch.uint8).view(130, 70)
+    powers = torch.tensor([[120], [130]], dtype=torch.uint8)
+    w = WeightF8(codes.view(torch.float8_e4m3fn), powers)
+    w.codes.view(torch.uint8).zero_()
+    w.powers.fill_(1)
+    codes2, powers2 = w.codes, w.powers
+    assert torch.equal(codes2.view(torch.uint8), codes) and codes2.dtype == torch.float8_e4m3fn and torch.equal(powers2, powers)
+    assert torch.equal(w._forward[0][:, :70], codes) and torch.equal(w._backward[0][:, :130], codes.t()) and w._forward[1][:, 0].tolist() == [120, 130]
+    for name, value in (("codes", codes2), ("powers", powers2), ("m", 5), ("n", 5), ("other", 1)):
+        with pytest.raises(AttributeError):
+            setattr(w, name, value)
+    for other in (copy.copy(w), copy.deepcopy(w), pickle.loads(pickle.dumps(w))):
+        assert torch.equal(other.codes.view(torch.uint8), codes) and torch.equal(other._backward[0], w._backward[0]) and (other.m, other.n) == (130, 70)

@@ -314,6 +314,14 @@ class WeightF8:
         object.__setattr__(self, name, value)
 
 
+def _numbers(c):
+    """A number, or several in a row, as a list."""
+    try:
+        return [float(v) for v in c]
+    except TypeError:                                    # (also of tensors without a dimension)
+        return [float(c)]
+
+
 def _at(t):
     return t.data_ptr() if t is not None else None
 
@@ -852,12 +860,15 @@ class Rsvd:
             raise ValueError("out: shape and type of G")
         if out is not None and out.get_device() != self._index:
             self._elsewhere(out, "out")
-        steps = int(steps)
-        if not 1 <= steps <= 64:
+        if int(steps) != steps or not 1 <= steps <= 64:
             raise ValueError("steps: 1 to 64")
-        flat = [float(v) for v in coefficients] * steps if not hasattr(coefficients[0], "__len__") else [float(v) for c in coefficients for v in c]
-        if len(flat) != 3 * steps:
+        steps = int(steps)
+        rows = [_numbers(c) for c in coefficients]       # (one number each: those of every step)
+        if all(len(c) == 1 for c in rows):
+            rows = [sum(rows, [])] * steps
+        if len(rows) != steps or any(len(c) != 3 for c in rows):
             raise ValueError("coefficients: three numbers, or three for each step")
+        flat = sum(rows, [])
         O = G.new_empty(G.shape) if out is None else out
 
         def strides(t, what):

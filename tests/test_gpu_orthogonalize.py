@@ -229,3 +229,19 @@ def test_a_schedule_that_starts_steeply(dtype, m, n):
         sums = 3 * 2.0 ** -24 * math.sqrt(max(m, n)) * 16 * norm
         assert float(off) <= float(4 * lost + sums + UNIT[G.dtype] * norm), (kind, float(off / norm), float(lost / norm))
         assert float(torch.linalg.svdvals(got.double()).max()) < 1.02
+
+
+def test_coefficients_come_as_three_for_each_step():
+    c, G = ctx(), momentum(gen(6), 40, 70, F32)
+    want = c.rsvd_orthogonalize(G, 2, [STEP, (1.5, -0.5, 0.0)])
+    both = torch.tensor([STEP, (1.5, -0.5, 0.0)])
+    for coef in (both, both.double().numpy(), tuple(map(tuple, both.tolist())), [torch.tensor(STEP), [1.5, -0.5, 0.0]]):
+        assert torch.equal(c.rsvd_orthogonalize(G, 2, coef), want)
+    for coef in (torch.tensor(STEP), list(STEP), torch.tensor(STEP).numpy()):
+        assert torch.equal(c.rsvd_orthogonalize(G, 2, coef), c.rsvd_orthogonalize(G, 2, STEP))
+    for coef in ([(1.5, -0.5), (0.0, 1.5, -0.5, 0.0)], [(1.5, -0.5, 0.0, 1.5, -0.5, 0.0), ()], [], [STEP] * 3, (1.5, -0.5, 0.0) * 2, [STEP, 1.0, 2.0]):
+        with pytest.raises(ValueError):
+            c.rsvd_orthogonalize(G, 2, coef)
+    for steps in (2.5, "2", None):
+        with pytest.raises((ValueError, TypeError)):
+            c.rsvd_orthogonalize(G, steps, STEP)

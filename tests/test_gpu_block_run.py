@@ -141,3 +141,59 @@ def test_a_workspace_of_the_callers_is_not_written_behind_its_bytes():
         given.fill_(0xff)                                # (what a workspace holds before does not matter: NaN in every type)
         b = call(given)
         assert torch.equal(a, b) and torch.equal(a, call(None))
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("t,n,m", [(3, 64, 96), (200, 264, 520), (1000, 130, 77)])
+def test_a_step_to_what_its_types_lose(dtype, t, n, m):
+    """2-norms, u the unit of the type.  dX and dW do not see how h is held: dh, both kept products, D and the result are rounded, each to u / sqrt 3 on the whole at the most, slopes
+    change by about as much as what they are of: sqrt 5 of those, twice that is below 4 u; and sums in fp32, of n, then 2 m or t terms, are below 2^-18.  y and dW of the way back
+    see h in blocks, where a number near a border goes the other way: h is off by 2^-22 of itself, or, one time in 2^10 at the most, by 2 u; borders are 2^-4 apart, so
+    one number in 2^14 is off by 2^-3, 2^-10 on the whole.  The update is that of dW as it came out."""
+    from test_gpu_layer8 import UNIT
+    from test_gpu_orthogonalize import iterated
+    T, g = TYPES[dtype], gen(t)
+    x, w, down, dy = parts(g, t, n, m, T)
+    y, dx, dw, ddown, update = step(ctx(), x, w, down, dy)
+    gu = x.double() @ w.double().t()
+    a, s, _ = act64(gu[:, :m], "silu")
+    h = (a * gu[:, m:]).to(T)
+    D = weight_values(ctx().rsvd_f8_weight(down))
+    dh = blocks64(dy, 1, 128)[0] @ D
+    d = torch.cat([dh * gu[:, m:] * s, dh * a], dim=1)
+    u = UNIT[T]
+    own, held = 4 * u + 2.0 ** -18, u + 2.0 ** -10
+    for got, ref, near in ((y, blocks64(h, 1, 128)[0] @ D.t(), held), (dx, d @ w.double(), own), (dw, d.t() @ x.double(), own),
+                           (ddown, blocks64(dy, 128, 1)[0].t() @ blocks64(h, 128, 1)[0], held)):
+        assert float((got.double() - ref).norm() / ref.norm()) < near
+    for i in range(2):
+        iterated(dw.view(2, m, n)[i], got=update[i])
+
+
+@pytest.mark.parametrize("keep", [False, True])
+@pytest.mark.parametrize("t", [40, 700])
+def test_captured_fp16_gradients_take_the_range_of_each_replay(t, keep):
+    """What D is held times follows from the data, on the device: replays with gradients of other sizes, eager calls between them."""
+    from paper_2110_03423_amd import Rsvd
+    c, g, n, m = Rsvd(0), gen(t), 136, 72
+    x, w, dh = block(g, t, n, m, torch.float16)
+    kept = c.rsvd_gated_product(x, w, keep=True)[1] if keep else None
+    dw = torch.empty(2 * m, n, device=DEV)
+    run = lambda ctx_, dx, dw_: ctx_.rsvd_gated_product_grad(dh, x, w, kept=kept, out=(dx, dw_))
+    dx = torch.empty_like(x)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        run(c, dx, dw)
+        stream.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            run(c, dx, dw)
+    for size in (1e-5, 3e3, 1e-2, 0.0, 1e-4):
+        dh.copy_(size * torch.randn(t, m, device=DEV, generator=g))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        a, b = torch.empty_like(x), torch.empty_like(dw)
+        run(Rsvd(0), a, b)
+        assert torch.equal(dx, a) and torch.equal(dw, b) and bool(b.any()) == (size > 0)

@@ -191,3 +191,27 @@ def test_large_fp32_numbers_and_infinities_stay_in_their_columns(t, n, m):
         for got, one, off, rest in ((other[:, 5], d[:, 3] * v[3, 5].double(), ed[:, 3], d.abs() @ w.double().abs()[:, 5]),
                                     (again[:, n - 1], d[9] * y[9, n - 1].double(), ed[9], d.abs().t() @ x.double().abs()[:, n - 1])):
             assert bool(((got.double() - one).abs() <= 2.0 ** -22 * one.abs() + off * value + 2 * rest).all())
+
+
+@pytest.mark.parametrize("keep", [False, True])
+def test_the_range_of_fp16_gradients_is_found_behind_32_bits(keep):
+    """The one large gradient is the last number of more than 2^32: without it D would be 2^16 times too large for fp16."""
+    t, n, m = (1 << 20) + 131, 16, 4100
+    g, c = gen(8), ctx()
+    x, w = integers(g, (t, n), F16), integers(g, (2 * m, n), F16, 1, 0.5)
+    dh = torch.zeros(t, m, device=DEV, dtype=F16)
+    dh[-1], dh[5, 7] = 2.0 ** 13, 2.0 ** -8
+    assert dh.numel() > 1 << 32
+    say("fp16 range, past 32 bits", keep)
+    kept = c.rsvd_gated_product(x, w, "relu", keep=True)[1] if keep else None
+    dx, dw = torch.empty_like(x), torch.empty(2 * m, n, device=DEV)
+    c.rsvd_gated_product_grad(dh, x, w, "relu", kept=kept, out=(dx, dw))
+    del kept
+    rows = [5, t - 1]
+    gu = x[rows].double() @ w.double().t()
+    a, u = gu[:, :m].clamp(min=0), gu[:, m:]
+    d = torch.cat([dh[rows].double() * u * (a > 0), dh[rows].double() * a], dim=1)
+    assert float(d.abs().max()) > 65504
+    assert torch.equal(dw.double(), d.t() @ x[rows].double()) and torch.equal(dx[rows], rounded(d @ w.double(), F16)) and int((dx != 0).any(dim=1).sum()) <= 2
+    del dh, dx, dw, x
+    torch.cuda.empty_cache()

@@ -421,7 +421,7 @@ int rsvd_gated_product_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, rsvd_a
  * codes are x 2^-e rounded to nearest, ties to even.  A block that holds an infinity or NaN
  * has the byte 255 and codes that are NaN.
  *   - codes: rows of ldq bytes, ldq a multiple of 16 and at least n up to a multiple of 128, from a
- *     16-byte aligned address; the codes from n on to that multiple are zeros.
+ *     16-byte aligned address; the codes from n on to that multiple are zeros (NaN in a block whose byte is 255, as rsvd_f8_weight leaves them).
  *   - powers: a row for each 128 rows of codes, a byte for each 128 columns, ldp bytes apart, ldp a multiple
  *     of 4 (at most 2^20 for the products), from a 4-byte aligned address; all bytes to the next multiple of 4 may be read.  Values 1 to 254, or 255.
  *   - Tokens are rounded on the way, in blocks of 128 of a token (of 128 tokens for the gradient of a

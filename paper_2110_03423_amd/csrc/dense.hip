@@ -14,11 +14,12 @@ static int64_t dense_tiles(const DenseDesc &d, int b) {
 }
 
 // The time of each tile and number of ranges is estimated, and the least taken.  What bounds a k-tile (128 bytes of a row) of the smaller tiles is what a CU gets out of the
-// L2 caches, 50 to 60 GB/s: 0.22 (0.3 where operands go through registers, 0.19 of fp16 numbers that do not) and 0.5 us for each workgroup of 64 and 128 rows and columns on a CU, but 0.3 and 0.7 us where there are not as many as CUs; tiles of 256 take
+// L2 caches, 55 to 86 GB/s: 0.22 (0.3 where operands go through registers, 0.19 of fp16 numbers that do not) and 0.5 us for each workgroup of 64 and 128 rows and columns on a CU, but 0.3 and 0.7 us where there are not as many as CUs; tiles of 256 take
 // 1.7 us, near the rate of the matrix instructions (1.4 where CUs are idle and operands do not go through registers).  Small tiles take a k-tile of all planes at once (two 0.55 us, three 1.0; 0.9 and 0.95).  Beside that 3, 5 and
 // 8 us for each workgroup that a CU has behind another.  Tiles that fill the chip a number of times are worked out whole; of what is left k may be in ranges, for all CUs to
-// have a part: a second launch, and their sums are written and read (5 bytes / ps).  Measured for 130 products of 80 to 3000 tokens with all tiles and one to sixteen ranges: what is
-// chosen takes up to 6 % more than the best of them, fourteen times up to 17 %.
+// have a part: a second launch, and their sums are written and read (5 bytes / ps).  Measured for 130 products of 80 to 3000 tokens (bf16 and fp32; gated, both gradients, 8-bit floats
+// and their weights' gradients) with all tiles and one to sixteen ranges: what is chosen takes 0.3 % more than the best of them in the median, 3 % on the average, and fifteen times more than 6 %.  Four of those, 1.2 to 2.0
+// times, are dX in fp32 of 128 to 256 tokens of wide layers: small tiles read the weight as it lies (dense_takes_wide), and that it need not be laid out then is not part of the estimate.
 static DenseChoice dense_choose(const rsvd_ctx *ctx, const DenseDesc &d) {
   const int products = dense_segs(d.planes).count;
   const bool through = d.rows_of_n;                      // operands through registers

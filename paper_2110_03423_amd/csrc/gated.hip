@@ -108,7 +108,7 @@ hipError_t gated_few_launch(rsvd_ctx *, hipStream_t s, const GatedFewDesc &d) {
 }
 
 // ---------------------------------------------------------------- the range of a gradient in fp16
-// D = (dH u act', dH act) of fp16 tokens is held in fp16 times a power of two.  As it is it would leave the range on either side where neither gradient does: dH of 1e-5 lost 4e-3 of dW, and dH u
+// D = (dH u act', dH act) of fp16 tokens is held in fp16 times a power of two.  As it is it would leave the range on either side where neither gradient does: dH of 1e-5 lost 4.3e-3 of dW (2.1e-4 now, as with dH of 1e-2), and dH u
 // above 65504 was an infinity.  With |act'| <= 1.13, |act| <= |g| and |g|, |u| <= G, |D| <= 1.13 max |dH| G; that, with room for rounding, is brought to 2^15 or more.  G is the largest
 // product that was kept or, of those that are computed again, the largest norm of a row of X times that of a row of W.  What is not finite does not count: it stays what it is.
 // Memory is the bound: 8192 x 4096 -> 8192 kept, 403 MB 84 us (4.8 TB/s), computed again, 335 MB 68 us, of a gradient of 2930; the second launch, one workgroup, takes 2 to 5.

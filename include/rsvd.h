@@ -462,7 +462,8 @@ int rsvd_f8_weight_grad(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int64_t to
  * result is near U V^T.  Iterates are two fp16 numbers (22 bits); products of bf16 matrices take the first of them, others both.  Diagonals
  * of A and of b A + c A^2, and sums, are held in 32 bits.  An infinity or NaN makes the whole matrix NaN.
  * Coefficients that may take a singular value out of [-2.7, 2.7], rounding included, or whose b x^2 + c x^4 spreads by more than 15 over all of them, are turned away
- * (RSVD_ERR_UNSUPPORTED; rounding of bf16 results is 2^-10 of the magnitudes that a step adds up, of others 2^-18).  1 to 64 steps.  Of a batch, tiles of 256 x 256 are fewer than 2^22.  O may be G, or lie on it. */
+ * (RSVD_ERR_UNSUPPORTED; rounding of bf16 results is 2^-10 of the magnitudes that a step adds up, of others 2^-18,
+ * or 2^-29 times the long side).  1 to 64 steps.  Of a batch, tiles of 256 x 256 are fewer than 2^22.  O may be G, or lie on it. */
 int rsvd_orthogonalize_bytes(rsvd_ctx *ctx, rsvd_xtype type, int batch, int64_t m, int64_t n, size_t *bytes);
 int rsvd_orthogonalize(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int batch, int64_t m, int64_t n, const void *G, int64_t ldg, int64_t stride_g,
                        int steps, const float *coefficients, void *O, int64_t ldo, int64_t stride_o, void *workspace, size_t workspace_bytes);

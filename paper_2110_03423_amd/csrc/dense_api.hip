@@ -287,9 +287,10 @@ OrthogonalLayout orthogonal_layout(const rsvd_ctx *ctx, rsvd_xtype type, int bat
 // ends are values at the old ones and where the derivative is zero; it is followed, not single values: between any two of those an iteration may have one that leaves.  Only what is off the diagonals of A and
 // of b A + c A^2 is held in fp16, and is at most half of what their eigenvalues spread by.
 // Every step's interval is widened by what rounding moves: `slack` of the magnitudes that are added up.  For bf16 results, whose products take 11 bits of each number, 2^-10: matrices of one
-// magnitude round all entries alike, and 2^-12 too much at the end of a range that the next steps stretch tenfold each made NaN of them.  Others keep 22 bits: 2^-18.
-bool stays_in_range(rsvd_xtype type, int steps, const float *c) {
-  const double slack = type == RSVD_X_BF16 ? 0x1p-10 : 0x1p-18;
+// magnitude round all entries alike, and 2^-12 too much at the end of a range that the next steps stretch tenfold each made NaN of them.  Others keep 22 bits: 2^-18, or
+// what a sum in fp32 of as many equal numbers as the long side has may be off by: 2^-24 for each 32 that an instruction adds.
+bool stays_in_range(rsvd_xtype type, int64_t longer, int steps, const float *c) {
+  const double slack = type == RSVD_X_BF16 ? 0x1p-10 : fmax(0x1p-18, 0x1p-29 * (double)longer);
   double low = 0.0, high = 1.0;                          // of singular values, whose sign a step may change
   for (int s = 0; s < steps; ++s) {
     const double a = c[3 * s], b = c[3 * s + 1], g = c[3 * s + 2];
@@ -673,7 +674,7 @@ int rsvd_orthogonalize(rsvd_ctx *ctx, void *stream, rsvd_xtype type, int batch, 
   if (ldo < n) return -13;
   if (batch > 1 && stride_o < (m - 1) * ldo + n) return -14;
   if (!matrices_supported(batch, m, n)) return RSVD_ERR_UNSUPPORTED;
-  if (!stays_in_range(type, steps, coefficients)) return RSVD_ERR_UNSUPPORTED;
+  if (!stays_in_range(type, m > n ? m : n, steps, coefficients)) return RSVD_ERR_UNSUPPORTED;
   const OrthogonalLayout L = orthogonal_layout(ctx, type, batch, m, n);
   if (workspace == nullptr || ((uintptr_t)workspace & 255) != 0) return -15;
   if (workspace_bytes < L.total) return -16;

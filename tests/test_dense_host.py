@@ -286,3 +286,15 @@ def test_a_weight_of_8_bit_floats_keeps_its_values():
             setattr(w, name, value)
     for other in (copy.copy(w), copy.deepcopy(w), pickle.loads(pickle.dumps(w))):
         assert torch.equal(other.codes.view(torch.uint8), codes) and torch.equal(other._backward[0], w._backward[0]) and (other.m, other.n) == (130, 70)
+
+
+def test_sums_of_a_long_side_move_more_of_the_range(plan):
+    """An fp32 sum of equal numbers is off by 2^-24 of itself for each 32 of them that are added at once: 2^-12 of 131072."""
+    call = caller(plan, "rsvd_orthogonalize", "ctx stream type batch m n G ldg sg steps coef O ldo so ws bytes", ctx=plan.h, stream=NULL, type=X_F32, batch=1, m=50,
+                  n=70, G=PTR, ldg=1 << 17, sg=0, steps=7, coef=None, O=PTR, ldo=1 << 17, so=0, ws=PTR, bytes=1 << 50)
+    sharp = flat([(a * 1.01, b * 1.01 ** 3, c * 1.01 ** 5) for a, b, c in SCHEDULE[:-1]] + SCHEDULE[-1:])
+    for xt in (X_F16, X_F32):
+        for m, n, rc in ((50, 70, ERR_NO_DEVICE), (50, 4096, ERR_NO_DEVICE), (4096, 50, ERR_NO_DEVICE), (50, 131072, UNSUPPORTED), (131072, 50, UNSUPPORTED)):
+            assert call(type=xt, m=m, n=n, coef=sharp) == rc
+    for xt in (X_BF16, X_F16, X_F32):
+        assert call(type=xt, m=50, n=131072, coef=flat(SCHEDULE)) == ERR_NO_DEVICE

@@ -245,3 +245,16 @@ def test_coefficients_come_as_three_for_each_step():
     for steps in (2.5, "2", None):
         with pytest.raises((ValueError, TypeError)):
             c.rsvd_orthogonalize(G, steps, STEP)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("m,n", [(16, 131072), (131072, 16), (256, 65536)])
+def test_sums_of_many_equal_numbers_stay_in_the_range(dtype, m, n):
+    """One singular value, at the end of the range; the last steps make up for what the first are off by, so that the rounding of the result and 2^-10 are left."""
+    from test_dense_host import SCHEDULE
+    say("orthogonalize, equal numbers", dtype, m, n)
+    G = torch.full((m, n), 0.3, device=DEV, dtype=TYPES[dtype])
+    G[:, ::2] *= -1
+    got = ctx().rsvd_orthogonalize(G, len(SCHEDULE), SCHEDULE)
+    want = G.double() / G.double().norm()
+    assert float((got.double() - want).norm()) < UNIT[G.dtype] + 2.0 ** -10
